@@ -23,7 +23,7 @@
  *  - Shapes are given in logical PyTorch order, strides in elements.
  *    The kernels read dense channels-last tensors (NHWC activations, KRSC
  *    filters, row-major matrices).  For MS_CONV2D, MS_CONV_TRANSPOSE2D,
- *    MS_LINEAR, MS_BN_EVAL and MS_AVGPOOL any non-negative strides are
+ *    MS_LINEAR, MS_BN_EVAL, MS_AVGPOOL and MS_LAYER_NORM any non-negative strides are
  *    accepted (NCHW, strided slices, transposed views, broadcast inputs);
  *    output and gradient buffers must not overlap themselves.  Tensors in
  *    another layout are staged: copied into the kernels' layout in transient
@@ -126,10 +126,13 @@ typedef enum {
                             Runs the 2-D kernels on the input with its T depth taps
                             folded into the channels (transient workspace of T / stride_d
                             times x in the forward and weight gradient)                  */
-    MS_CONV_TRANSPOSE3D = 8 /* 3-D MS_CONV_TRANSPOSE2D: x[N,C_in,D,H,W], W[C_in,C_out,T,R,S],
+    MS_CONV_TRANSPOSE3D = 8, /* 3-D MS_CONV_TRANSPOSE2D: x[N,C_in,D,H,W], W[C_in,C_out,T,R,S],
                             b[C_out] or NULL, y[N,C_out,Do,Ho,Wo], Do = (D-1) stride_d
                             - 2 pad_d + T + out_pad_d; the adjoint of the MS_CONV3D with
                             filter W read as [K = C_in, C = C_out, T, R, S]               */
+    MS_LAYER_NORM = 9    /* y = (x - mean) / sqrt(var + eps) * gamma + beta over each row of
+                            x[M,D]; W = gamma[D] and b = beta[D], either may be NULL.
+                            Forward through ms_layer_norm_forward() only                  */
 } ms_kind;
 
 typedef struct {
@@ -260,6 +263,24 @@ uint64_t ms_dropout_blocks(int64_t n);
  */
 ms_status ms_dropout_forward(const ms_tensor *x, const ms_tensor *y, float p, uint64_t seed, uint64_t offset,
                              uint32_t mask, ms_record **rec, void *stream);
+
+/*
+ * ms_layer_norm_forward -- y = h gamma + beta, h = (x - mean) / sqrt(var + eps),
+ * with the mean and the biased variance of each row of x[M, D].
+ *
+ * The norm is linear in its parameters but not in x: its input gradient
+ *   dx = (q - mean(q) - h mean(q h)) / sqrt(var + eps), q = grad_y gamma,
+ * and that of gamma, the sum over rows of grad_y h, need h.  A record borrows
+ * x with either bit INPUT or WEIGHT set, gamma with INPUT, and nothing for
+ * BIAS alone; the statistics are not kept, the backward takes them again from
+ * the x that it reads anyway.
+ * x, y: [M, D], D >= 1, any strides (y not overlapping itself); gamma, beta:
+ * [D], contiguous, or NULL (ones, zeros), of x's dtype.  eps: finite, >= 0
+ * (MS_E_ARG otherwise).  Statistics and sums are in fp32.  Backward is
+ * ms_layer_backward().  ms_layer_forward() rejects MS_LAYER_NORM (MS_E_ARG).
+ */
+ms_status ms_layer_norm_forward(const ms_tensor *x, const ms_tensor *gamma, const ms_tensor *beta, float eps,
+                                uint32_t mask, const ms_tensor *y, ms_record **rec, void *stream);
 
 /*
  * ms_layer_backward -- write exactly the requested gradients for grad_y.

@@ -101,6 +101,17 @@ class Dropout:
     offset: int = 0
 
 
+@dataclass(frozen=True)
+class LayerNorm:
+    """y = (x - mean) / sqrt(var + eps) * gamma + beta over the rows of x[M, D];
+    W = gamma[D], b = beta[D], either may be None.  Its record keeps x (for
+    the gradient of x or gamma) and no statistics: backward takes them again."""
+    eps: float = 1e-5
+
+
+_BLOCKS = (LayerNorm,)   # layers with a C entry point of their own
+
+
 def _pair(v):
     return (int(v), int(v)) if isinstance(v, int) else (int(v[0]), int(v[1]))
 
@@ -181,6 +192,13 @@ class _LayerDesc:
             raise TypeError(f"unknown layer spec {spec!r}")
 
 
+class _BlockDesc:
+    """Stands in for _LayerDesc where the C entry point takes no MsLayer."""
+
+    def __init__(self, spec):
+        self.spec = spec
+
+
 # The current stream's handle without a Stream object around it, where torch has it.
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
 
@@ -248,7 +266,7 @@ def output_shape(spec, x: torch.Tensor, W: Optional[torch.Tensor]):
         return tuple(x.shape)
     if isinstance(spec, AvgPool):
         return (x.shape[0], x.shape[1])
-    if isinstance(spec, (ReLU, Dropout)):
+    if isinstance(spec, (ReLU, Dropout, LayerNorm)):
         return tuple(x.shape)
     raise TypeError(spec)
 
@@ -272,7 +290,7 @@ class Record:
     the tensors it borrows (so the caching allocator sees the same retained
     bytes as the ledger)."""
 
-    def __init__(self, handle: ctypes.c_void_p, desc: _LayerDesc, x, W, b, y_shape, y_like, bits=None):
+    def __init__(self, handle: ctypes.c_void_p, desc: _LayerDesc, x, W, b, y_shape, y_like, bits=None, extra=None):
         self._h = handle
         self._desc = desc
         acct = MsAccount()
@@ -288,8 +306,11 @@ class Record:
             self._keep["W"] = W
         if bor & (MS_SAVED_MEAN | MS_SAVED_VAR):
             self._keep["stats"] = (desc.spec.running_mean, desc.spec.running_var)
+        if extra:
+            self._keep.update(extra)
         self._x_meta = (tuple(x.shape), x.dtype, x.device, tuple(x.stride()))
         self._elementwise = isinstance(desc.spec, (ReLU, Dropout))
+        self._block = isinstance(desc.spec, _BLOCKS)
         self._w_meta = (tuple(W.shape), W.dtype) if W is not None else None
         self._b_meta = (tuple(b.shape), b.dtype) if b is not None else None
         self.y_shape = y_shape
@@ -369,12 +390,37 @@ def _dropout_forward(lib, spec, x, y, mask):
     return h
 
 
+class _BlockCall:
+    """The forward call of a block layer with its C descriptors and buffers."""
+
+    def __init__(self, spec, x, W, b, mask, y):
+        if x.dim() != 2:
+            raise ValueError(f"{type(spec).__name__} takes x[M, D]; got {x.dim()} dims")
+        _on_gpu(x, W, b, y)
+        self.spec, self.x, self.W, self.b, self.mask = spec, x, W, b, int(mask)
+        self.y = torch.empty(output_shape(spec, x, W), dtype=x.dtype, device=x.device) if y is None else y
+        self.kept = {}   # what the record borrows besides x and W
+        self._d = [tensor_desc(t) for t in (x, W, b, self.y)]
+        self._p = [_ptr(d) for d in self._d]
+
+    def __call__(self, lib, h, stream):
+        px, pw, pb, py = self._p
+        check(lib.ms_layer_norm_forward(px, pw, pb, float(self.spec.eps), self.mask, py, h, stream),
+              "ms_layer_norm_forward")
+
+
 def layer_forward(spec, x: torch.Tensor, W: Optional[torch.Tensor] = None, b: Optional[torch.Tensor] = None,
                   mask: int = 0, y: Optional[torch.Tensor] = None):
     """Run the layer's forward kernel on the current stream; return (y, record).
     record is None when mask == 0 (nothing is saved).  A ReLU with the INPUT
     bit gets a fresh 1-bit mask buffer, owned by its record."""
     lib = _lib.load()
+    if isinstance(spec, _BLOCKS):
+        call, h = _BlockCall(spec, x, W, b, mask, y), ctypes.c_void_p()
+        call(lib, ctypes.byref(h), _stream(x.device))
+        if not h.value:
+            return call.y, None
+        return call.y, Record(h, _BlockDesc(spec), x, W, b, tuple(call.y.shape), call.y, extra=call.kept)
     if isinstance(spec, ReLU):
         if W is not None or b is not None:
             raise TypeError("ReLU takes no W or b")
@@ -422,12 +468,15 @@ def layer_backward(rec: Record, grad_y: torch.Tensor, grad_x: Optional[torch.Ten
     if m & MASK_INPUT and grad_x is None:
         if rec._elementwise:   # memory order: the gradient in x's layout
             grad_x = torch.empty_strided(rec._x_meta[0], rec._x_meta[3], dtype=grad_y.dtype, device=grad_y.device)
+        elif rec._block:       # (the loss of a cross entropy has a dtype of its own)
+            grad_x = torch.empty(rec._x_meta[0], dtype=rec._x_meta[1], device=grad_y.device)
         else:
             grad_x = empty_like_layout(rec._x_meta[0], grad_y)
     if m & MASK_WEIGHT and grad_W is None:
-        grad_W = empty_like_layout(rec._w_meta[0], grad_y)
+        grad_W = (torch.empty(rec._w_meta[0], dtype=rec._w_meta[1], device=grad_y.device) if rec._block
+                  else empty_like_layout(rec._w_meta[0], grad_y))
     if m & MASK_BIAS and grad_b is None:
-        grad_b = torch.empty(rec._b_meta[0], dtype=grad_y.dtype, device=grad_y.device)
+        grad_b = torch.empty(rec._b_meta[0], dtype=rec._b_meta[1], device=grad_y.device)
     gy, gx, gw, gb = tensor_desc(grad_y), tensor_desc(grad_x), tensor_desc(grad_W), tensor_desc(grad_b)
     st = lib.ms_layer_backward(rec._h, _ptr(gy), _ptr(gx), _ptr(gw), _ptr(gb), _stream(grad_y.device))
     check(st, "ms_layer_backward")
@@ -495,7 +544,10 @@ class PreparedLayer:
         extra = (spec.running_mean, spec.running_var) if isinstance(spec, BatchNormEval) else ()
         _on_gpu(x, W, b, y, grad_y, grad_x, grad_W, grad_b, *extra)
         self.lib = _lib.load()
-        self.desc = _LayerDesc(spec)
+        self.block = _BlockCall(spec, x, W, b, mask, y) if isinstance(spec, _BLOCKS) else None
+        self.desc = _BlockDesc(spec) if self.block else _LayerDesc(spec)
+        if self.block:
+            y = self.block.y
         if y is None:
             y = torch.empty_like(x) if isinstance(spec, (ReLU, Dropout)) else empty_like_layout(output_shape(spec, x, W), x)
         self.tensors = (x, W, b, y, grad_y, grad_x, grad_W, grad_b)
@@ -506,7 +558,7 @@ class PreparedLayer:
         # a ReLU's 1-bit mask lives as long as this object (reused by every forward)
         self.bits = relu_mask_buffer(x) if self.relu and self.mask & MASK_INPUT else None
         self._d = [tensor_desc(t) for t in self.tensors]
-        self._fa = (ctypes.byref(self.desc.layer),) + tuple(_ptr(d) for d in self._d[:3])
+        self._fa = (None if self.block else ctypes.byref(self.desc.layer),) + tuple(_ptr(d) for d in self._d[:3])
         self._fy = _ptr(self._d[3])
         self._ba = tuple(_ptr(d) for d in self._d[4:])
         self._h = ctypes.c_void_p()
@@ -518,6 +570,9 @@ class PreparedLayer:
         if self._h.value:
             self._free(self._h)
             self._h.value = None
+        if self.block:
+            self.block(self.lib, self._hp, self._stream)
+            return
         if self.relu:
             bits = ctypes.c_void_p(self.bits.data_ptr() if self.bits is not None and self.bits.numel() else None)
             check(self.lib.ms_relu_forward(self._fa[1], self._fy, bits, self.mask, self._hp, self._stream),

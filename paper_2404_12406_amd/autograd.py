@@ -33,7 +33,7 @@ from . import api
 from .api import MASK_BIAS, MASK_INPUT, MASK_WEIGHT
 
 __all__ = ["MSConv2d", "MSConvTranspose2d", "MSConv1d", "MSConvTranspose1d", "MSConv3d", "MSConvTranspose3d",
-           "MSLinear", "MSBatchNorm2dEval", "MSReLU", "MSDropout", "convert"]
+           "MSLinear", "MSBatchNorm2dEval", "MSReLU", "MSDropout", "MSLayerNorm", "convert"]
 
 
 def _cl(t: Optional[torch.Tensor]) -> Optional[torch.Tensor]:
@@ -326,13 +326,33 @@ class MSDropout(nn.Module):
         return _DropoutFn.apply(_dense(x), self.p, seed)
 
 
+class MSLayerNorm(nn.Module):
+    """Layer norm over the last dim (leading dims are flattened into rows),
+    optional weight and bias [D].  Keeps x alone, no statistics."""
+
+    def __init__(self, weight: Optional[torch.Tensor], bias: Optional[torch.Tensor], eps: float = 1e-5):
+        super().__init__()
+        self.weight = weight if (weight is None or isinstance(weight, nn.Parameter)) else nn.Parameter(weight)
+        self.bias = bias if (bias is None or isinstance(bias, nn.Parameter)) else nn.Parameter(bias)
+        self.spec = api.LayerNorm(float(eps))
+
+    def forward(self, x):
+        return _LayerFn.apply(self.spec, x.reshape(-1, x.shape[-1]), self.weight, self.bias).reshape(x.shape)
+
+
 def _convertible_conv(m) -> bool:
     """groups 1, dilation 1, zero padding given as numbers, fp32 or bf16."""
     return (m.groups == 1 and all(d == 1 for d in m.dilation) and m.padding_mode == "zeros"
             and not isinstance(m.padding, str) and m.weight.dtype in (torch.float32, torch.bfloat16))
 
 
-def convert(module: nn.Module) -> nn.Module:
+def _convertible_norm(m) -> bool:
+    """over the last dim alone, fp32 or bf16."""
+    return (isinstance(m, nn.LayerNorm) and len(m.normalized_shape) == 1 and
+            all(p is None or p.dtype in (torch.float32, torch.bfloat16) for p in (m.weight, m.bias)))
+
+
+def convert(module: nn.Module, layer_norm: bool = False) -> nn.Module:
     """Replace, in place, every nn.Conv1d/2d/3d and nn.ConvTranspose1d/2d/3d
     (groups 1, dilation 1, zero padding), nn.Linear,
     nn.BatchNorm2d in evaluation mode and nn.ReLU of `module` by the
@@ -340,7 +360,8 @@ def convert(module: nn.Module) -> nn.Module:
     module (Sec. 4: one call swaps every supported layer); nn.Dropout
     becomes MSDropout with the same p and mode.  A BatchNorm2d
     still in training mode is left as it is (its batch statistics make it
-    non-linear in x); so is any layer outside those limits."""
+    non-linear in x); so is any layer outside those limits.  With layer_norm,
+    nn.LayerNorm over the last dim becomes MSLayerNorm too."""
     for name, child in list(module.named_children()):
         new = None
         if isinstance(child, nn.Conv2d) and _convertible_conv(child):
@@ -366,8 +387,10 @@ def convert(module: nn.Module) -> nn.Module:
         elif isinstance(child, nn.Dropout):
             new = MSDropout(child.p)
             new.train(child.training)
+        elif layer_norm and _convertible_norm(child):
+            new = MSLayerNorm(child.weight, child.bias, child.eps)
         if new is not None:
             setattr(module, name, new)
         else:
-            convert(child)
+            convert(child, layer_norm)
     return module

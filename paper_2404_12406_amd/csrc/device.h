@@ -136,6 +136,15 @@ int launch_relu_bwd(int dtype, const void *dy, const void *bits, int64_t n, void
 int launch_dropout(int dtype, const void *in, int64_t n, void *out, uint64_t seed, uint64_t offset, uint32_t thresh,
                    float scale, int drop_all, void *stream);
 
+// Layer norm of the rows of a dense x[M][D] (gamma and beta may be null), and
+// its backward: any of dx, dgamma, dbeta may be null, and the partial sums of
+// dgamma and dbeta (`params`) take layer_norm_bwd_workspace() bytes.
+int launch_layer_norm_fwd(int dtype, const void *x, const void *gamma, const void *beta, float eps, int64_t M, int64_t D, void *y,
+                          void *stream);
+size_t layer_norm_bwd_workspace(int dtype, int64_t M, int64_t D, bool params);
+int launch_layer_norm_bwd(int dtype, const void *x, const void *dy, const void *gamma, float eps, int64_t M, int64_t D, void *dx,
+                          void *dgamma, void *dbeta, void *ws, void *stream);
+
 // Global average pool x[N][L][C] -> y[N][C] and its adjoint.
 int launch_avgpool_fwd(int dtype, const void *x, int N, int L, int C, void *y, void *stream);
 int launch_avgpool_bwd(int dtype, const void *dy, int N, int L, int C, void *dx, void *stream);
