@@ -23,7 +23,7 @@
  *  - Shapes are given in logical PyTorch order, strides in elements.
  *    The kernels read dense channels-last tensors (NHWC activations, KRSC
  *    filters, row-major matrices).  For MS_CONV2D, MS_CONV_TRANSPOSE2D,
- *    MS_LINEAR, MS_BN_EVAL, MS_AVGPOOL and MS_LAYER_NORM any non-negative strides are
+ *    MS_LINEAR, MS_BN_EVAL, MS_AVGPOOL, MS_LAYER_NORM and MS_GATED_LINEAR any non-negative strides are
  *    accepted (NCHW, strided slices, transposed views, broadcast inputs);
  *    output and gradient buffers must not overlap themselves.  Tensors in
  *    another layout are staged: copied into the kernels' layout in transient
@@ -130,10 +130,22 @@ typedef enum {
                             b[C_out] or NULL, y[N,C_out,Do,Ho,Wo], Do = (D-1) stride_d
                             - 2 pad_d + T + out_pad_d; the adjoint of the MS_CONV3D with
                             filter W read as [K = C_in, C = C_out, T, R, S]               */
-    MS_LAYER_NORM = 9    /* y = (x - mean) / sqrt(var + eps) * gamma + beta over each row of
+    MS_LAYER_NORM = 9,   /* y = (x - mean) / sqrt(var + eps) * gamma + beta over each row of
                             x[M,D]; W = gamma[D] and b = beta[D], either may be NULL.
                             Forward through ms_layer_norm_forward() only                  */
+    MS_GATED_LINEAR = 10 /* y = act(x Wg^T + bg) * (x Wu^T + bu): x[M,D], W = [Wg; Wu][2F,D],
+                            b = [bg; bu][2F] or NULL, y[M,F].  Forward through
+                            ms_gated_linear_forward() only                                */
 } ms_kind;
+
+/* Activations of MS_GATED_LINEAR. */
+typedef enum {
+    MS_ACT_SILU = 0,      /* z / (1 + exp(-z))                                      */
+    MS_ACT_GELU = 1,      /* z times the normal distribution's probability below z  */
+    MS_ACT_GELU_TANH = 2, /* z (1 + tanh(sqrt(2 / pi) (z + 0.044715 z^3))) / 2      */
+    MS_ACT_RELU = 3,      /* max(z, 0)                                              */
+    MS_ACT_SIGMOID = 4    /* 1 / (1 + exp(-z))                                      */
+} ms_activation;
 
 typedef struct {
     int32_t kind;               /* ms_kind */
@@ -155,9 +167,9 @@ typedef struct ms_record ms_record;
  * MS_SAVED_BITS: a ReLU's 1-bit mask; MS_SAVED_Y (policy accounting only):
  * the layer output, which stock PyTorch's ReLU keeps; MS_SAVED_MASK8 (policy
  * accounting only): the one-byte-per-element mask stock PyTorch's dropout
- * keeps. */
+ * keeps.  MS_SAVED_PROJ: a gated linear unit's projections. */
 enum { MS_SAVED_X = 1u, MS_SAVED_W = 2u, MS_SAVED_MEAN = 4u, MS_SAVED_VAR = 8u, MS_SAVED_BITS = 16u,
-       MS_SAVED_Y = 32u, MS_SAVED_MASK8 = 64u };
+       MS_SAVED_Y = 32u, MS_SAVED_MASK8 = 64u, MS_SAVED_PROJ = 128u };
 
 /* Bits of ms_account.kernels: what the record's backward will launch. */
 enum { MS_K_DGRAD = 1u, MS_K_WGRAD = 2u, MS_K_BGRAD = 4u };
@@ -281,6 +293,42 @@ ms_status ms_dropout_forward(const ms_tensor *x, const ms_tensor *y, float p, ui
  */
 ms_status ms_layer_norm_forward(const ms_tensor *x, const ms_tensor *gamma, const ms_tensor *beta, float eps,
                                 uint32_t mask, const ms_tensor *y, ms_record **rec, void *stream);
+
+/*
+ * ms_gated_projection_bytes -- size of the projections of M rows that
+ * ms_gated_linear_forward() keeps in `proj`: [M, 2F] values of 4 bytes for
+ * MS_F32, and of 3 for MS_BF16 (sign, exponent and 15 bits of the fraction,
+ * rounded to nearest even; the two leading bytes of all values, then the third
+ * ones).  In bf16 alone, 7 bits of fraction, the gradients would be a third
+ * further off than their own rounding makes them.  0 where an extent is not
+ * positive.
+ */
+uint64_t ms_gated_projection_bytes(int64_t rows, int64_t F, int32_t dtype);
+
+/*
+ * ms_gated_linear_forward -- y = act(zg) zu, [zg zu] = z = x W^T + b: the first
+ * half of a gated feed-forward block, both projections, the activation and the
+ * product in one pass (its second half is an MS_LINEAR).
+ *
+ * The unit is not linear in x or W: with q = grad_y,
+ *   dz = [q zu act'(zg), q act(zg)],  dx = dz W,  dW = dz^T x,  db = sum of dz,
+ * so every gradient needs z.  The caller chooses what a record keeps for it:
+ *  - proj (caller-allocated device memory of ms_gated_projection_bytes() bytes,
+ *    16-byte aligned, fully overwritten): z, in fp32 for fp32 tensors and in
+ *    fp32's leading 24 bits for bf16 ones (see there), and x only with bit
+ *    WEIGHT set (as MS_LINEAR);
+ *  - proj NULL: x alone, 2F / D times less, and W and b by reference; backward
+ *    takes z again, a third more matrix work than with z.
+ * W is borrowed for bit INPUT or where z is taken again.  With mask 0 nothing is
+ * kept and proj must be NULL.  x[M, D], W[2F, D], y[M, F]: any strides (y not
+ * overlapping itself), D, F >= 1, M * 2F < 2^31; b[2F] contiguous or NULL.  z is
+ * in fp32 until it is rounded into proj; y is rounded once, from fp32.  bf16 operands whose
+ * D is no multiple of 8 run on zero-padded copies, and every backward on a dz in
+ * transient workspace.  Backward is ms_layer_backward().  ms_layer_forward()
+ * rejects MS_GATED_LINEAR (MS_E_ARG).
+ */
+ms_status ms_gated_linear_forward(const ms_tensor *x, const ms_tensor *W, const ms_tensor *b, int32_t activation,
+                                  void *proj, uint32_t mask, const ms_tensor *y, ms_record **rec, void *stream);
 
 /*
  * ms_layer_backward -- write exactly the requested gradients for grad_y.

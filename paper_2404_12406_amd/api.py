@@ -109,7 +109,19 @@ class LayerNorm:
     eps: float = 1e-5
 
 
-_BLOCKS = (LayerNorm,)   # layers with a C entry point of their own
+@dataclass(frozen=True)
+class GatedLinear:
+    """y = act(x Wg^T + bg) * (x Wu^T + bu) for x[M, D], W = [Wg; Wu][2F, D],
+    b = [bg; bu][2F] or None; act is "silu", "gelu", "gelu_tanh", "relu" or
+    "sigmoid".  Its record keeps, for any gradient, both projections
+    (keep="projections", 2F values a row, of 3 bytes for bf16, and x for the
+    weight's gradient) or
+    x alone (keep="input"), from which backward takes them again."""
+    act: str = "silu"
+    keep: str = "projections"
+
+
+_BLOCKS = (LayerNorm, GatedLinear)   # layers with a C entry point of their own
 
 
 def _pair(v):
@@ -262,6 +274,8 @@ def output_shape(spec, x: torch.Tensor, W: Optional[torch.Tensor]):
                                for e, k, ss, pp, oo in zip((D, H, Wd), (T, R, S), s, p, o))
     if isinstance(spec, Linear):
         return (x.shape[0], W.shape[0])
+    if isinstance(spec, GatedLinear):
+        return (x.shape[0], W.shape[0] // 2)
     if isinstance(spec, BatchNormEval):
         return tuple(x.shape)
     if isinstance(spec, AvgPool):
@@ -397,16 +411,36 @@ class _BlockCall:
         if x.dim() != 2:
             raise ValueError(f"{type(spec).__name__} takes x[M, D]; got {x.dim()} dims")
         _on_gpu(x, W, b, y)
-        self.spec, self.x, self.W, self.b, self.mask = spec, x, W, b, int(mask)
+        self.spec, self.mask = spec, int(mask)
+        self.kept = {}   # what the record borrows besides x, W and b
+        if isinstance(spec, GatedLinear):
+            if spec.act not in _lib.MS_ACT:
+                raise ValueError(f"unknown activation {spec.act!r}")
+            if spec.keep not in ("projections", "input"):
+                raise ValueError(f"keep is \"projections\" or \"input\"; got {spec.keep!r}")
+            if W is None or W.dim() != 2:
+                raise TypeError("GatedLinear needs W[2F, D]")
+            if self.mask and spec.keep == "projections":
+                n = _lib.load().ms_gated_projection_bytes(x.shape[0], W.shape[0] // 2, _DT.get(x.dtype, 0))
+                # (an empty buffer has no address: no rows, nothing to keep)
+                self.kept["projections"] = torch.empty(n, dtype=torch.uint8, device=x.device)
+            elif self.mask and b is not None:
+                self.kept["b"] = b
         self.y = torch.empty(output_shape(spec, x, W), dtype=x.dtype, device=x.device) if y is None else y
-        self.kept = {}   # what the record borrows besides x and W
         self._d = [tensor_desc(t) for t in (x, W, b, self.y)]
         self._p = [_ptr(d) for d in self._d]
+        proj = self.kept.get("projections")
+        self._proj = None if proj is None or proj.numel() == 0 else proj.data_ptr()
 
     def __call__(self, lib, h, stream):
         px, pw, pb, py = self._p
-        check(lib.ms_layer_norm_forward(px, pw, pb, float(self.spec.eps), self.mask, py, h, stream),
-              "ms_layer_norm_forward")
+        spec = self.spec
+        if isinstance(spec, LayerNorm):
+            check(lib.ms_layer_norm_forward(px, pw, pb, float(spec.eps), self.mask, py, h, stream),
+                  "ms_layer_norm_forward")
+        else:
+            check(lib.ms_gated_linear_forward(px, pw, pb, _lib.MS_ACT[spec.act], self._proj, self.mask, py, h, stream),
+                  "ms_gated_linear_forward")
 
 
 def layer_forward(spec, x: torch.Tensor, W: Optional[torch.Tensor] = None, b: Optional[torch.Tensor] = None,

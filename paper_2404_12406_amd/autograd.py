@@ -33,7 +33,7 @@ from . import api
 from .api import MASK_BIAS, MASK_INPUT, MASK_WEIGHT
 
 __all__ = ["MSConv2d", "MSConvTranspose2d", "MSConv1d", "MSConvTranspose1d", "MSConv3d", "MSConvTranspose3d",
-           "MSLinear", "MSBatchNorm2dEval", "MSReLU", "MSDropout", "MSLayerNorm", "convert"]
+           "MSLinear", "MSBatchNorm2dEval", "MSReLU", "MSDropout", "MSLayerNorm", "MSGatedLinear", "convert"]
 
 
 def _cl(t: Optional[torch.Tensor]) -> Optional[torch.Tensor]:
@@ -338,6 +338,23 @@ class MSLayerNorm(nn.Module):
 
     def forward(self, x):
         return _LayerFn.apply(self.spec, x.reshape(-1, x.shape[-1]), self.weight, self.bias).reshape(x.shape)
+
+
+class MSGatedLinear(nn.Module):
+    """y = act(x Wg^T + bg) * (x Wu^T + bu) over the last dim (leading dims are
+    flattened into rows): weight [2F, D] is Wg above Wu, bias [2F] or None.
+    keep: what backward is left, "projections" or the "input" alone (see
+    api.GatedLinear)."""
+
+    def __init__(self, weight: torch.Tensor, bias: Optional[torch.Tensor], act: str = "silu", keep: str = "projections"):
+        super().__init__()
+        self.weight = weight if isinstance(weight, nn.Parameter) else nn.Parameter(weight)
+        self.bias = bias if (bias is None or isinstance(bias, nn.Parameter)) else nn.Parameter(bias)
+        self.spec = api.GatedLinear(act, keep)
+
+    def forward(self, x):
+        y = _LayerFn.apply(self.spec, x.reshape(-1, x.shape[-1]), self.weight, self.bias)
+        return y.reshape(*x.shape[:-1], y.shape[-1])
 
 
 def _convertible_conv(m) -> bool:

@@ -13,6 +13,9 @@ namespace ms {
 
 enum Dtype : int { kF32 = 0, kBF16 = 1 };
 
+// Activations of the gated linear unit (ms_activation).
+enum Act : int { kActSilu = 0, kActGelu = 1, kActGeluTanh = 2, kActRelu = 3, kActSigmoid = 4 };
+
 // Convolution geometry.  Activations are NHWC, filters KRSC, all dense.
 // The fully-connected layer is the special case H = W = R = S = P = Q = 1,
 // stride 1, pad 0 (x[M,K_in] = NHWC with N = M, C = K_in; W[N_out,K_in] = KRSC).
@@ -144,6 +147,27 @@ int launch_layer_norm_fwd(int dtype, const void *x, const void *gamma, const voi
 size_t layer_norm_bwd_workspace(int dtype, int64_t M, int64_t D, bool params);
 int launch_layer_norm_bwd(int dtype, const void *x, const void *dy, const void *gamma, float eps, int64_t M, int64_t D, void *dx,
                           void *dgamma, void *dbeta, void *ws, void *stream);
+
+// dst[r][0 .. ld) = src[r][0 .. cols) and zeros (dst 16-byte aligned, ld whole vectors).
+int launch_pad_rows(int dtype, const void *src, int64_t rows, int64_t cols, void *dst, int64_t ld, void *stream);
+
+// Gated linear unit y = act(z_g) z_u, z = x W^T + b [M][2F] (b may be null).
+// bf16 needs operands for which gated_rows_ok() (D a multiple of 8, aligned).
+// `proj` receives z where it is kept (else null): fp32, or for bf16 the leading
+// 24 bits of it, a plane [M][2F] of 16 and one of 8.  launch_gated_dz leaves the
+// gradient of z for that of y in dz, from proj or, where that is null, from z
+// computed again.
+bool gated_rows_ok(int64_t M, int64_t D, int64_t F, const void *x, const void *w, const void *b);
+size_t gated_fwd_workspace(int dtype, int64_t M, int64_t D, int64_t F, bool keep);
+int launch_gated_fwd(int dtype, int64_t M, int64_t D, int64_t F, int act, const void *x, const void *w, const void *b, void *y,
+                     void *proj, void *ws, void *stream);
+size_t gated_dz_workspace(int dtype, int64_t M, int64_t D, int64_t F, bool kept);
+int launch_gated_dz(int dtype, int64_t M, int64_t D, int64_t F, int act, const void *x, const void *w, const void *b,
+                    const void *proj, const void *dy, void *dz, void *ws, void *stream);
+// The gradients of a Linear x[M][K] -> [M][N] (any of dx, dw, db may be null).
+size_t linear_bwd_workspace(int dtype, int64_t M, int64_t K, int64_t N, bool dx, bool dw, bool db);
+int launch_linear_bwd(int dtype, int64_t M, int64_t K, int64_t N, const void *dy, const void *x, const void *w, void *dx, void *dw,
+                      void *db, void *ws, void *stream);
 
 // Global average pool x[N][L][C] -> y[N][C] and its adjoint.
 int launch_avgpool_fwd(int dtype, const void *x, int N, int L, int C, void *y, void *stream);

@@ -1,0 +1,141 @@
+// For the kernels of the transformer layers: vectors of rows of any width and
+// alignment, the joining of softmax statistics, and the activations of the gated
+// linear unit with their derivatives.
+#pragma once
+
+#include "common.h"
+#include "../device.h"
+
+namespace ms {
+
+// A row's 16-byte vector at column c; a last, incomplete one element by element.
+template <typename T> struct Loose;   // 16 bytes at the alignment of an element
+template <> struct Loose<float> { typedef u32x4 type __attribute__((aligned(4))); };
+template <> struct Loose<bf16> { typedef u32x4 type __attribute__((aligned(2))); };
+
+template <typename T>
+__device__ __forceinline__ Vec16<T> load_vec(const T *__restrict__ row, int c, int D) {
+    constexpr int V = Vec16<T>::N;
+    Vec16<T> v;
+    if (c + V <= D) {
+        v.u = *reinterpret_cast<const typename Loose<T>::type *>(row + c);
+    } else {
+#pragma unroll
+        for (int e = 0; e < V; ++e) v.e[e] = c + e < D ? row[c + e] : (T)0.f;
+    }
+    return v;
+}
+
+template <typename T>
+__device__ __forceinline__ void store_vec(T *__restrict__ row, int c, int D, const Vec16<T> &v) {
+    constexpr int V = Vec16<T>::N;
+    if (c + V <= D) {
+        *reinterpret_cast<typename Loose<T>::type *>(row + c) = v.u;
+    } else {
+#pragma unroll
+        for (int e = 0; e < V; ++e)
+            if (c + e < D) row[c + e] = v.e[e];
+    }
+}
+
+// fp32 rounded to its leading 24 bits (to nearest even; NaN stays one), in the low ones.
+__device__ __forceinline__ uint32_t to_f24(float v) {
+    const uint32_t u = __float_as_uint(v);
+    return v != v ? 0x7fc000u : (u + 0x7fu + ((u >> 8) & 1u)) >> 8;
+}
+
+typedef float floatx2 __attribute__((ext_vector_type(2)));
+
+constexpr float kLog2e = 1.44269504088896341f, kLn2 = 0.693147180559945309f;
+
+// (m, s) stands for s 2^m, m the running maximum in powers of two: the sum of two.
+// A maximum of minus infinity (nothing yet) comes with s = 0; a NaN stays in s.
+__device__ __forceinline__ floatx2 join_lse(floatx2 a, floatx2 b) {
+    const float m = fmaxf(a.x, b.x);
+    const float sa = a.x == m ? a.y : a.y * __builtin_amdgcn_exp2f(a.x - m);
+    const float sb = b.x == m ? b.y : b.y * __builtin_amdgcn_exp2f(b.x - m);
+    return floatx2{m, sa + sb};
+}
+
+namespace act {
+
+// FAST: on the hardware's exponential and reciprocal (each within some 2 units
+// in 2^-24), for results that are rounded to bf16; else the library's.
+template <bool FAST>
+__device__ __forceinline__ float exp_(float v) {
+    return FAST ? __builtin_amdgcn_exp2f(v * kLog2e) : expf(v);
+}
+template <bool FAST>
+__device__ __forceinline__ float rcp_(float v) {
+    return FAST ? __builtin_amdgcn_rcpf(v) : 1.f / v;
+}
+template <bool FAST>
+__device__ __forceinline__ float sigmoid(float z) { return rcp_<FAST>(1.f + exp_<FAST>(-z)); }
+
+// The normal distribution's cumulative probability and density.  FAST: the tail
+// from Abramowitz and Stegun, Handbook of Mathematical Functions, 7.1.26
+// (within 1.5e-7), taken on the negative side so that small results do not
+// come from a difference.
+template <bool FAST>
+__device__ __forceinline__ void normal(float z, float &cdf, float &pdf) {
+    const float e = exp_<FAST>(-0.5f * z * z);
+    pdf = 0.398942280401432678f * e;
+    if constexpr (FAST) {
+        const float u = fabsf(z) * 0.707106781186547524f;
+        const float t = __builtin_amdgcn_rcpf(__builtin_fmaf(0.3275911f, u, 1.f));
+        float p = __builtin_fmaf(1.061405429f, t, -1.453152027f);
+        p = __builtin_fmaf(p, t, 1.421413741f);
+        p = __builtin_fmaf(p, t, -0.284496736f);
+        p = __builtin_fmaf(p, t, 0.254829592f);
+        const float tail = 0.5f * p * t * e;
+        cdf = z < 0.f ? tail : 1.f - tail;
+    } else {
+        cdf = 0.5f * erfcf(-z * 0.707106781186547524f);
+    }
+}
+
+// a = act(z), d = act'(z)
+template <bool FAST>
+__device__ __forceinline__ void both(int kind, float z, float &a, float &d) {
+    switch (kind) {
+    case kActSilu: {
+        const float s = sigmoid<FAST>(z);
+        a = z * s;
+        d = __builtin_fmaf(a, 1.f - s, s);
+        return;
+    }
+    case kActGelu: {
+        float cdf, pdf;
+        normal<FAST>(z, cdf, pdf);
+        a = z * cdf;
+        d = __builtin_fmaf(z, pdf, cdf);
+        return;
+    }
+    case kActGeluTanh: {   // 0.5 (1 + tanh(p)) = sigmoid(2 p), p = sqrt(2 / pi) (z + 0.044715 z^3)
+        const float z2 = z * z;
+        const float s = sigmoid<FAST>(1.59576912160573071f * z * __builtin_fmaf(0.044715f, z2, 1.f));
+        a = z * s;
+        d = __builtin_fmaf(a * (1.f - s), 1.59576912160573071f * __builtin_fmaf(0.134145f, z2, 1.f), s);
+        return;
+    }
+    case kActRelu:
+        a = z < 0.f ? 0.f : z;
+        d = z > 0.f ? 1.f : 0.f;
+        return;
+    default: {   // kActSigmoid
+        a = sigmoid<FAST>(z);
+        d = a * (1.f - a);
+        return;
+    }
+    }
+}
+
+template <bool FAST>
+__device__ __forceinline__ float value(int kind, float z) {
+    float a, d;
+    both<FAST>(kind, z, a, d);
+    return a;
+}
+
+}  // namespace act
+}  // namespace ms

@@ -1,0 +1,483 @@
+// bf16 contractions of the transformer layers, each with what follows it done
+// on the sums while they are in registers:
+//   kEpiGate      z = x W^T + b over W = [gate; up]: y = act(z_gate) z_up, and
+//                 optionally z itself (kept for the backward)
+//   kEpiGateGrad  z again, then the gradient of z for that of y: dz_gate = dy
+//                 z_up act'(z_gate), dz_up = dy act(z_gate)
+//   kEpiLse       z = x W^T + b over a vocabulary: the maximum and the sum of
+//                 exponentials of each row's part of a column tile, and the
+//                 target's logit; z is not written
+//   kEpiXent      z again, then dz = (exp(z - lse) - [column = target]) scale
+//   kEpiAdd       dx += dz W for one piece of the vocabulary, in fp32
+//   kEpiStore     the weight gradient dz^T x over the rows that count
+// The main loop is gemm_block_body.inc's.  Everything before the one rounding
+// of what is stored is in fp32.
+#include <hip/hip_ext.h>
+
+#include "gemm_bf16.h"
+#include "block_math.h"
+
+namespace ms {
+namespace g2 {
+
+enum Epi { kEpiStore = 0, kEpiGate = 1, kEpiGateGrad = 2, kEpiLse = 3, kEpiXent = 4, kEpiAdd = 5 };
+
+struct FusedArgs : Args {
+    const int *count;      // rows that count (weight gradient: of the reduction), on the device; null: all
+    const bf16 *fbias;     // bias of the columns (gated: [2F]); null: none
+    // gated
+    int F, act;
+    uint16_t *proj;        // kEpiGate: z in 24 bits (null: not kept): a plane of the leading 16, [M][2F],
+    uint8_t *proj_lo;      // and one of the others
+    const bf16 *dh;        // kEpiGateGrad: dy[M][F]; c is dz[M][2F]
+    // cross entropy; rows are those that count
+    const int *target;     // each row's target in the vocabulary
+    int v0;                // the piece's first word
+    floatx2 *stat;         // kEpiLse: softmax statistics as join_lse()'s, [column tile][rows]
+    float *tlogit;         // kEpiLse: the target's logit
+    int64_t stat_ld;
+    const float *lse, *scale;   // kEpiXent
+    int add;               // kEpiAdd: add to the partials (0: write them)
+};
+
+// Output column of row `row` of a gated tile's B operand, from the tile's first.
+__device__ __forceinline__ int gate_col(int row) { return (row >> 6) * 32 + (row & 31); }
+
+typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+
+// Bias of columns n .. n + 3 (zeros past N), through a descriptor of N entries.
+__device__ __forceinline__ void bias4(__amdgpu_buffer_rsrc_t r, int n, int N, float (&o)[4]) {
+    if ((N & 3) == 0) {
+        const u32x2 w = __builtin_amdgcn_raw_buffer_load_b64(r, n * 2, 0, 0);
+#pragma unroll
+        for (int v = 0; v < 4; ++v) o[v] = __uint_as_float((v & 1) ? (w[v >> 1] & 0xffff0000u) : (w[v >> 1] << 16));
+    } else {
+#pragma unroll
+        for (int v = 0; v < 4; ++v) o[v] = __uint_as_float((uint32_t)__builtin_amdgcn_raw_buffer_load_b16(r, (n + v) * 2, 0, 0) << 16);
+    }
+}
+
+// Rows of COLS bf16 (a multiple of 8) that a wave has staged in LDS, `pitch`
+// apart: 32 of them to dst + row * ld, columns below `ncol`, rows below `nrow`.
+template <int COLS>
+__device__ __forceinline__ void store_rows(const bf16 *stage, int pitch, bf16 *dst, int64_t ld, int nrow, int ncol, int lane) {
+    constexpr int SEG = COLS / 8, RPP = 64 / SEG;
+#pragma unroll
+    for (int r0 = 0; r0 < 32; r0 += RPP) {
+        const int r = r0 + lane / SEG, c = (lane % SEG) * 8;
+        Vec16<bf16> v;
+        v.u = *reinterpret_cast<const u32x4 *>(stage + r * pitch + c);
+        if (r >= nrow || c >= ncol) continue;
+        bf16 *d = dst + (int64_t)r * ld + c;
+        if (c + 8 <= ncol) {
+            *reinterpret_cast<u32x4 *>(d) = v.u;   // (any alignment of the rows)
+        } else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                if (c + e < ncol) d[e] = v.e[e];
+        }
+    }
+}
+
+// Rows of COLS bytes, four of a lane packed in each word of b, through the wave's
+// staging bytes to dst + row * ld.
+template <int COLS, int TG>
+__device__ __forceinline__ void put_bytes(uint8_t *stage, const uint32_t (&b)[TG][4], uint8_t *dst, int64_t ld, int nrow, int ncol,
+                                          int fr, int fh, int lane) {
+    constexpr int PITCH = COLS + 16, SEG = COLS / 16, RPP = 64 / SEG;
+    wait_lgkm0();
+    __builtin_amdgcn_wave_barrier();
+#pragma unroll
+    for (int j = 0; j < TG; ++j)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) *reinterpret_cast<uint32_t *>(stage + fr * PITCH + 32 * j + 8 * q + 4 * fh) = b[j][q];
+    wait_lgkm0();
+    __builtin_amdgcn_wave_barrier();
+#pragma unroll
+    for (int r0 = 0; r0 < 32; r0 += RPP) {
+        const int r = r0 + lane / SEG, c = (lane % SEG) * 16;
+        if (r >= nrow || c >= ncol || r >= 32) continue;
+        const u32x4 v = *reinterpret_cast<const u32x4 *>(stage + r * PITCH + c);
+        uint8_t *d = dst + (int64_t)r * ld + c;
+        if (c + 16 <= ncol) {
+            *reinterpret_cast<u32x4 *>(d) = v;
+        } else {
+#pragma unroll
+            for (int e = 0; e < 16; ++e)
+                if (c + e < ncol) d[e] = (uint8_t)(v[e / 4] >> (8 * (e % 4)));
+        }
+    }
+}
+
+// The lane's 16 sums of tile (i, j) are row 32 i + lane % 32 and columns
+// 32 j + 8 q + 4 (lane / 32) + v, q and v = 0..3.
+template <int EPI, class G>
+__device__ __forceinline__ void fused_epilogue(const FusedArgs &P, char *smem, floatx16 (&acc)[G::TM][G::TN], int M, int m0, int n0,
+                                               int wm0, int wn0, int wave, int lane, int tn, int zsplit) {
+    constexpr int TM = G::TM, TN = G::TN;
+    const int fr = lane & 31, fh = lane >> 5;
+    const int N = P.N;
+    bf16 *stage = reinterpret_cast<bf16 *>(smem) + wave * G::EPI_ROWS * G::EPI_PITCH;
+    if constexpr (EPI == kEpiGate || EPI == kEpiGateGrad) {
+        constexpr int TG = TN / 2, COLS = 32 * TG, PITCH = COLS + 8;
+        static_assert(TN % 2 == 0, "gated tiles pair the column tiles of a wave");
+        const int F = P.F, f0 = (n0 + wn0) / 2;
+        const int ncol = min(F - f0, COLS);
+        const __amdgpu_buffer_rsrc_t rbias = rsrc(P.fbias, P.fbias ? (uint32_t)F * 4u : 0u);
+#pragma unroll
+        for (int i = 0; i < TM; ++i) {
+            const int mb = m0 + wm0 + 32 * i, nrow = M - mb;   // rows of this pass
+            if (EPI == kEpiGateGrad && P.dh) {
+                // dy's tile, whole vectors where they are, into the staging rows
+                constexpr int SEG = COLS / 8, RPP = 64 / SEG;
+#pragma unroll
+                for (int r0 = 0; r0 < 32; r0 += RPP) {
+                    const int r = r0 + lane / SEG, c = (lane % SEG) * 8;
+                    Vec16<bf16> v = zero16<bf16>();
+                    if (r < nrow && c < ncol) {
+                        const bf16 *s = P.dh + (int64_t)(mb + r) * F + f0 + c;
+                        if (c + 8 <= ncol) {
+                            v.u = *reinterpret_cast<const u32x4 *>(s);
+                        } else {
+#pragma unroll
+                            for (int e = 0; e < 8; ++e)
+                                if (c + e < ncol) v.e[e] = s[e];
+                        }
+                    }
+                    *reinterpret_cast<u32x4 *>(stage + r * PITCH + c) = v.u;
+                }
+                wait_lgkm0();
+                __builtin_amdgcn_wave_barrier();
+            }
+            // what the second pass stores: gradients, or (gate, up) projections
+            bf16x4 og[TG][4], ou[TG][4];
+            uint32_t lg[TG][4], lu[TG][4];   // their third bytes
+#pragma unroll
+            for (int j = 0; j < TG; ++j)
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    const int c = 32 * j + 8 * q + 4 * fh;
+                    float bg[4] = {0.f, 0.f, 0.f, 0.f}, bu[4] = {0.f, 0.f, 0.f, 0.f};
+                    if (P.fbias) {   // (columns past F read the other half's: not stored)
+                        bias4(rbias, f0 + c, 2 * F, bg);
+                        bias4(rbias, F + f0 + c, (F & 3) ? 1 : 2 * F, bu);
+                    }
+                    bf16x4 d4;
+                    if constexpr (EPI == kEpiGateGrad) d4 = *reinterpret_cast<const bf16x4 *>(stage + fr * PITCH + c);
+                    lg[j][q] = lu[j][q] = 0u;
+#pragma unroll
+                    for (int v = 0; v < 4; ++v) {
+                        const float zg = acc[i][2 * j][4 * q + v] + bg[v], zu = acc[i][2 * j + 1][4 * q + v] + bu[v];
+                        if constexpr (EPI == kEpiGate) {
+                            acc[i][2 * j][4 * q + v] = act::value<true>(P.act, zg) * zu;
+                            if (P.proj) {
+                                const uint32_t kg = to_f24(zg), ku = to_f24(zu);
+                                og[j][q][v] = __builtin_bit_cast(bf16, (uint16_t)(kg >> 8));
+                                ou[j][q][v] = __builtin_bit_cast(bf16, (uint16_t)(ku >> 8));
+                                lg[j][q] |= (kg & 255u) << (8 * v);
+                                lu[j][q] |= (ku & 255u) << (8 * v);
+                            }
+                        } else {
+                            float a, da;
+                            act::both<true>(P.act, zg, a, da);
+                            const float d = (float)d4[v];
+                            og[j][q][v] = (bf16)(d * zu * da);
+                            ou[j][q][v] = (bf16)(d * a);
+                        }
+                    }
+                }
+            auto put = [&](auto get, bf16 *dst, int64_t ld) __attribute__((always_inline)) {
+                wait_lgkm0();   // the staging rows are free
+                __builtin_amdgcn_wave_barrier();
+#pragma unroll
+                for (int j = 0; j < TG; ++j)
+#pragma unroll
+                    for (int q = 0; q < 4; ++q)
+                        *reinterpret_cast<bf16x4 *>(stage + fr * PITCH + 32 * j + 8 * q + 4 * fh) = get(j, q);
+                wait_lgkm0();
+                __builtin_amdgcn_wave_barrier();
+                store_rows<COLS>(stage, PITCH, dst + (int64_t)mb * ld + f0, ld, nrow, ncol, lane);
+            };
+            if constexpr (EPI == kEpiGate) {
+                put([&](int j, int q) {
+                    bf16x4 o;
+#pragma unroll
+                    for (int v = 0; v < 4; ++v) o[v] = (bf16)acc[i][2 * j][4 * q + v];
+                    return o;
+                }, P.c, F);
+                if (P.proj) {
+                    bf16 *z = reinterpret_cast<bf16 *>(P.proj);
+                    put([&](int j, int q) { return og[j][q]; }, z, 2 * (int64_t)F);
+                    put([&](int j, int q) { return ou[j][q]; }, z + F, 2 * (int64_t)F);
+                    put_bytes<COLS>(reinterpret_cast<uint8_t *>(stage), lg, P.proj_lo + (int64_t)mb * 2 * F + f0, 2 * (int64_t)F, nrow,
+                                    ncol, fr, fh, lane);
+                    put_bytes<COLS>(reinterpret_cast<uint8_t *>(stage), lu, P.proj_lo + (int64_t)mb * 2 * F + F + f0, 2 * (int64_t)F,
+                                    nrow, ncol, fr, fh, lane);
+                }
+            } else {
+                put([&](int j, int q) { return og[j][q]; }, P.c, 2 * (int64_t)F);
+                put([&](int j, int q) { return ou[j][q]; }, P.c + F, 2 * (int64_t)F);
+            }
+            wait_lgkm0();
+            __builtin_amdgcn_wave_barrier();
+        }
+    } else if constexpr (EPI == kEpiLse || EPI == kEpiXent) {
+        if (P.fbias) {
+            const __amdgpu_buffer_rsrc_t rbias = rsrc(P.fbias, (uint32_t)N * 2u);
+#pragma unroll
+            for (int j = 0; j < TN; ++j)
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    float b[4];
+                    bias4(rbias, n0 + wn0 + 32 * j + 8 * q + 4 * fh, N, b);
+#pragma unroll
+                    for (int i = 0; i < TM; ++i)
+#pragma unroll
+                        for (int v = 0; v < 4; ++v) acc[i][j][4 * q + v] += b[v];
+                }
+        }
+        if (n0 + wn0 + G::WN > N) {   // columns past the piece: exponentials of zero
+#pragma unroll
+            for (int j = 0; j < TN; ++j)
+#pragma unroll
+                for (int q = 0; q < 4; ++q)
+#pragma unroll
+                    for (int v = 0; v < 4; ++v) {
+                        const bool past = n0 + wn0 + 32 * j + 8 * q + 4 * fh + v >= N;
+#pragma unroll
+                        for (int i = 0; i < TM; ++i) acc[i][j][4 * q + v] = past ? -INFINITY : acc[i][j][4 * q + v];
+                    }
+        }
+        if constexpr (EPI == kEpiLse) {
+            constexpr int BM = G::A_BYTES / (BK * 2), WC = G::B_BYTES / (BK * 2) / G::WN;   // waves along the columns
+            floatx2 *red = reinterpret_cast<floatx2 *>(smem);   // [WC][BM]
+#pragma unroll
+            for (int i = 0; i < TM; ++i) {
+                const int m = m0 + wm0 + 32 * i + fr;
+                float top = -INFINITY;
+#pragma unroll
+                for (int j = 0; j < TN; ++j)
+#pragma unroll
+                    for (int v = 0; v < 16; ++v) top = fmaxf(top, acc[i][j][v]);
+                top = fmaxf(top, __shfl_xor(top, 32));
+                // (fmaxf passes over NaN: the sum below meets it)
+                const float t2 = top == -INFINITY ? 0.f : top * kLog2e;
+                float s = 0.f;
+#pragma unroll
+                for (int j = 0; j < TN; ++j)
+#pragma unroll
+                    for (int v = 0; v < 16; ++v) s += __builtin_amdgcn_exp2f(__builtin_fmaf(acc[i][j][v], kLog2e, -t2));
+                s += __shfl_xor(s, 32);
+                if (fh == 0) red[(wn0 / G::WN) * BM + wm0 + 32 * i + fr] = floatx2{top == -INFINITY ? top : t2, s};
+                const int t = m < M ? P.target[m] - P.v0 - (n0 + wn0) : -1;   // within this wave's columns?
+                if (__any((unsigned)t < (unsigned)G::WN)) {
+                    float z = 0.f;
+                    bool mine = false;
+#pragma unroll
+                    for (int j = 0; j < TN; ++j)
+#pragma unroll
+                        for (int q = 0; q < 4; ++q)
+#pragma unroll
+                            for (int v = 0; v < 4; ++v)
+                                if (t == 32 * j + 8 * q + 4 * fh + v) {
+                                    z = acc[i][j][4 * q + v];
+                                    mine = true;
+                                }
+                    if (mine && n0 + wn0 + t < N) P.tlogit[m] = z;
+                }
+            }
+            __syncthreads();
+            for (int r = wave * 64 + lane; r < BM; r += G::NT) {
+                if (m0 + r >= M) continue;
+                floatx2 a = red[r];
+#pragma unroll
+                for (int w = 1; w < WC; ++w) a = join_lse(a, red[w * BM + r]);
+                P.stat[(int64_t)tn * P.stat_ld + m0 + r] = a;
+            }
+        } else {
+            constexpr int PITCH = G::EPI_PITCH;
+            const int ncol = min(P.ldc - (n0 + wn0), G::WN);   // the padding columns are zeros
+#pragma unroll
+            for (int i = 0; i < TM; ++i) {
+                const int mb = m0 + wm0 + 32 * i, m = mb + fr;
+                const bool in = m < M;
+                const float l2 = in ? P.lse[m] * kLog2e : 0.f, sc = in ? P.scale[m] : 0.f;
+                const int t = in ? P.target[m] - P.v0 - (n0 + wn0) : -1;
+                const bool any = __any((unsigned)t < (unsigned)G::WN);
+#pragma unroll
+                for (int j = 0; j < TN; ++j)
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) {
+                        bf16x4 o;
+#pragma unroll
+                        for (int v = 0; v < 4; ++v) {
+                            float p = __builtin_amdgcn_exp2f(__builtin_fmaf(acc[i][j][4 * q + v], kLog2e, -l2));
+                            if (any && t == 32 * j + 8 * q + 4 * fh + v) p -= 1.f;
+                            o[v] = (bf16)(p * sc);
+                        }
+                        *reinterpret_cast<bf16x4 *>(stage + fr * PITCH + 32 * j + 8 * q + 4 * fh) = o;
+                    }
+                wait_lgkm0();
+                __builtin_amdgcn_wave_barrier();
+                store_rows<G::WN>(stage, PITCH, P.c + (int64_t)mb * P.ldc + n0 + wn0, P.ldc, M - mb, ncol, lane);
+                wait_lgkm0();
+                __builtin_amdgcn_wave_barrier();
+            }
+        }
+    } else {
+        static_assert(EPI == kEpiAdd, "epilogue");
+        float *W = P.part + (int64_t)zsplit * P.part_stride;
+#pragma unroll
+        for (int i = 0; i < TM; ++i) {
+            const int m = m0 + wm0 + 32 * i + fr;
+            if (m >= M) continue;
+#pragma unroll
+            for (int j = 0; j < TN; ++j)
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    const int n = n0 + wn0 + 32 * j + 8 * q + 4 * fh;
+                    if (n >= N) continue;   // (N is a multiple of 8)
+                    floatx4 *d = reinterpret_cast<floatx4 *>(W + (int64_t)m * N + n);
+                    floatx4 o = {acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]};
+                    if (P.add) o += *d;
+                    *d = o;
+                }
+        }
+    }
+}
+
+#define GEMM_FUSED
+template <int EPI, int MODE, int BM, int BN, int WR, int WC, int STAGES, int OCC>
+__global__ __launch_bounds__(WR * WC * 64, OCC) void gemm_fused_kernel(const FusedArgs P) {
+    constexpr bool UNIT = true, TS = false, D3 = false;
+    constexpr int KG = 1;
+    __shared__ __attribute__((aligned(1024))) char smem[Cfg<MODE, BM, BN, WR, WC, STAGES, KG>::SMEM_BYTES];
+    const int bx = (int)blockIdx.x, bz = (int)blockIdx.z;
+#include "gemm_block_body.inc"
+}
+#undef GEMM_FUSED
+
+// ------------------------------------------------------------------ host
+namespace {
+
+bool al16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+uint32_t bytes_of(int64_t elems) { return (uint32_t)(elems * 2); }
+
+// Tiles of the contractions over k-contiguous operands (gated, cross entropy).
+// Efficiencies as in gemm_bf16.hip's table.
+constexpr Tile kRowTiles[] = {
+    {"256x256", 256, 256, 2, 4, 2, 1, 1.20f, 1.20f},
+    {"128x128", 128, 128, 2, 2, 2, 2, 0.78f, 1.00f},
+    {"128x128s4", 128, 128, 2, 2, 4, 1, 0.90f, 0.90f},
+};
+// Tiles of the gradients of the cross entropy (an operand along m or n).
+constexpr Tile kGradTiles[] = {
+    {"256x256", 256, 256, 2, 4, 2, 1, 1.20f, 1.20f},
+    {"256x128", 256, 128, 2, 4, 3, 1, 1.00f, 1.00f},
+    {"128x128w8", 128, 128, 2, 4, 2, 2, 0.85f, 1.02f},
+};
+
+struct FusedPlan {
+    int tile, splits;
+};
+
+template <int NT>
+FusedPlan plan(const Tile (&tiles)[NT], int ntiles, long M, long N, long K, int max_splits) {
+    FusedPlan p{0, 1};
+    double best = 1e300;
+    for (int t = 0; t < ntiles; ++t)
+        for (int s = 1; s <= max_splits; ++s) {
+            const double us = est_us(tiles[t], M, N, K, 1, s);
+            if (us < best * 0.999) {
+                best = us;
+                p = FusedPlan{t, s};
+            }
+        }
+    return p;
+}
+
+template <int EPI, int MODE, int BM, int BN, int WR, int WC, int STAGES, int OCC>
+int go(unsigned prof, const FusedArgs &a, hipStream_t st) {
+    void *eb = nullptr, *ee = nullptr;
+    const bool timed = prof_pair(prof, &eb, &ee);
+    hipExtLaunchKernelGGL((gemm_fused_kernel<EPI, MODE, BM, BN, WR, WC, STAGES, OCC>), dim3(a.ntm * a.ntn, 1, a.splits),
+                          dim3(WR * WC * 64), 0, st, (hipEvent_t)eb, (hipEvent_t)ee, 0, a);
+    const int err = (int)hipGetLastError();
+    if (timed) prof_pair_done(prof, eb, ee, err == 0);
+    return err;
+}
+
+template <int EPI>
+int go_rows(int tile, unsigned prof, const FusedArgs &a, hipStream_t st) {
+    switch (tile) {
+    case 0: return go<EPI, kFwd, 256, 256, 2, 4, 2, 1>(prof, a, st);
+    case 1: return go<EPI, kFwd, 128, 128, 2, 2, 2, 2>(prof, a, st);
+    default: return go<EPI, kFwd, 128, 128, 2, 2, 4, 1>(prof, a, st);
+    }
+}
+
+template <int EPI, int MODE>
+int go_grad(int tile, unsigned prof, const FusedArgs &a, hipStream_t st) {
+    switch (tile) {
+    case 0: return go<EPI, MODE, 256, 256, 2, 4, 2, 1>(prof, a, st);
+    case 1: return go<EPI, MODE, 256, 128, 2, 4, 3, 1>(prof, a, st);
+    default: return go<EPI, MODE, 128, 128, 2, 4, 2, 2>(prof, a, st);
+    }
+}
+
+// x[M][D] w[N][D]^T
+FusedArgs rows_args(const Tile &t, int64_t M, int64_t N, int64_t D, const void *x, const void *w, int64_t w_rows) {
+    FusedArgs a{};
+    a.a = (const bf16 *)x;
+    a.b = (const bf16 *)w;
+    a.g.N = (int)M; a.g.C = (int)D; a.g.K = (int)N;
+    a.g.H = a.g.W = a.g.R = a.g.S = a.g.P = a.g.Q = a.g.sh = a.g.sw = 1;
+    a.M = (int)M; a.N = (int)N; a.K = (int)D;
+    a.ntm = (int)((M + t.bm - 1) / t.bm);
+    a.ntn = (int)((N + t.bn - 1) / t.bn);
+    a.splits = 1;
+    a.k_split = (int)D;
+    a.a_bytes = bytes_of(M * D);
+    a.b_bytes = bytes_of(w_rows * D);
+    return a;
+}
+
+}  // namespace
+
+// Operands: D a multiple of 8, x and w 16-byte aligned, the bias 4-byte aligned.
+bool rows_ok(int64_t M, int64_t N, int64_t D, const void *x, const void *w) {
+    return D % 8 == 0 && al16(x) && al16(w) && operand_fits(M * D) && operand_fits(N * D);
+}
+
+int gate_fwd(int64_t M, int64_t D, int64_t F, int act, const void *x, const void *w, const void *bias, void *y, void *proj,
+             hipStream_t st) {
+    const FusedPlan p = plan(kRowTiles, 3, M, 2 * F, D, 1);
+    const Tile &t = kRowTiles[p.tile];
+    FusedArgs a = rows_args(t, M, 2 * F, D, x, w, 2 * F);
+    a.ntn = (int)((F + t.bn / 2 - 1) / (t.bn / 2));
+    a.F = (int)F;
+    a.act = act;
+    a.fbias = (const bf16 *)bias;
+    a.c = (bf16 *)y;
+    a.proj = (uint16_t *)proj;
+    a.proj_lo = proj ? static_cast<uint8_t *>(proj) + M * 4 * F : nullptr;
+    return go_rows<kEpiGate>(p.tile, kProfFwd, a, st);
+}
+
+int gate_grad(int64_t M, int64_t D, int64_t F, int act, const void *x, const void *w, const void *bias, const void *dy, void *dz,
+              hipStream_t st) {
+    const FusedPlan p = plan(kRowTiles, 3, M, 2 * F, D, 1);
+    const Tile &t = kRowTiles[p.tile];
+    FusedArgs a = rows_args(t, M, 2 * F, D, x, w, 2 * F);
+    a.ntn = (int)((F + t.bn / 2 - 1) / (t.bn / 2));
+    a.F = (int)F;
+    a.act = act;
+    a.fbias = (const bf16 *)bias;
+    a.dh = (const bf16 *)dy;
+    a.c = (bf16 *)dz;
+    return go_rows<kEpiGateGrad>(p.tile, kProfFwd, a, st);
+}
+
+}  // namespace g2
+}  // namespace ms

@@ -22,41 +22,10 @@
 //    incomplete vector goes element by element.
 #include <algorithm>
 
-#include "common.h"
-#include "../device.h"
+#include "block_math.h"
 
 namespace ms {
 namespace ln {
-
-// 16 bytes at the alignment of an element
-template <typename T> struct Loose;
-template <> struct Loose<float> { typedef u32x4 type __attribute__((aligned(4))); };
-template <> struct Loose<bf16> { typedef u32x4 type __attribute__((aligned(2))); };
-
-template <typename T>
-__device__ __forceinline__ Vec16<T> load_vec(const T *__restrict__ row, int c, int D) {
-    constexpr int V = Vec16<T>::N;
-    Vec16<T> v;
-    if (c + V <= D) {
-        v.u = *reinterpret_cast<const typename Loose<T>::type *>(row + c);
-    } else {
-#pragma unroll
-        for (int e = 0; e < V; ++e) v.e[e] = c + e < D ? row[c + e] : (T)0.f;
-    }
-    return v;
-}
-
-template <typename T>
-__device__ __forceinline__ void store_vec(T *__restrict__ row, int c, int D, const Vec16<T> &v) {
-    constexpr int V = Vec16<T>::N;
-    if (c + V <= D) {
-        *reinterpret_cast<typename Loose<T>::type *>(row + c) = v.u;
-    } else {
-#pragma unroll
-        for (int e = 0; e < V; ++e)
-            if (c + e < D) row[c + e] = v.e[e];
-    }
-}
 
 __device__ __forceinline__ float wave_sum(float v) {
 #pragma unroll

@@ -509,6 +509,8 @@ ms_status ms_layer_forward(const ms_layer *layer, const ms_tensor *x, const ms_t
     if (layer && layer->kind == MS_RELU) return fail(MS_E_ARG, "ReLU runs through ms_relu_forward()");
     if (layer && layer->kind == MS_DROPOUT) return fail(MS_E_ARG, "dropout runs through ms_dropout_forward()");
     if (layer && layer->kind == MS_LAYER_NORM) return fail(MS_E_ARG, "layer norm runs through ms_layer_norm_forward()");
+    if (layer && layer->kind == MS_GATED_LINEAR)
+        return fail(MS_E_ARG, "gated linear units run through ms_gated_linear_forward()");
     Plan pl;
     ms_status st = validate_forward(layer, x, W, b, mask, y, true, &pl);
     if (st) return st;

@@ -326,6 +326,7 @@ inline void release(ms_record *r) {
         r->released = true;
         r->x.data = nullptr;
         r->W.data = nullptr;
+        r->b.data = nullptr;
         r->mean.data = nullptr;
         r->var.data = nullptr;
         r->bits = nullptr;
