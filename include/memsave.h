@@ -23,7 +23,7 @@
  *  - Shapes are given in logical PyTorch order, strides in elements.
  *    The kernels read dense channels-last tensors (NHWC activations, KRSC
  *    filters, row-major matrices).  For MS_CONV2D, MS_CONV_TRANSPOSE2D,
- *    MS_LINEAR, MS_BN_EVAL, MS_AVGPOOL, MS_LAYER_NORM and MS_GATED_LINEAR any non-negative strides are
+ *    MS_LINEAR, MS_BN_EVAL, MS_AVGPOOL, MS_LAYER_NORM, MS_GATED_LINEAR and MS_CROSS_ENTROPY any non-negative strides are
  *    accepted (NCHW, strided slices, transposed views, broadcast inputs);
  *    output and gradient buffers must not overlap themselves.  Tensors in
  *    another layout are staged: copied into the kernels' layout in transient
@@ -35,7 +35,8 @@
  *    MS_RELU and MS_DROPOUT take x dense in any order of its dims with y and
  *    the gradients in x's strides; 1-D tensors (biases, BN statistics) are
  *    contiguous.  Anything else returns MS_E_LAYOUT.
- *  - dtypes: MS_F32 or MS_BF16; all tensors of one call share one dtype.
+ *  - dtypes: MS_F32 or MS_BF16; all tensors of one call share one dtype (but a
+ *    cross entropy's loss, which is MS_F32).
  *    Products are accumulated in fp32 and rounded once to the output dtype
  *    (round to nearest even).
  *  - Every tensor has fewer than 2^31 elements (MS_E_UNSUPPORTED otherwise).
@@ -133,10 +134,16 @@ typedef enum {
     MS_LAYER_NORM = 9,   /* y = (x - mean) / sqrt(var + eps) * gamma + beta over each row of
                             x[M,D]; W = gamma[D] and b = beta[D], either may be NULL.
                             Forward through ms_layer_norm_forward() only                  */
-    MS_GATED_LINEAR = 10 /* y = act(x Wg^T + bg) * (x Wu^T + bu): x[M,D], W = [Wg; Wu][2F,D],
+    MS_GATED_LINEAR = 10, /* y = act(x Wg^T + bg) * (x Wu^T + bu): x[M,D], W = [Wg; Wu][2F,D],
                             b = [bg; bu][2F] or NULL, y[M,F].  Forward through
                             ms_gated_linear_forward() only                                */
+    MS_CROSS_ENTROPY = 11 /* softmax cross entropy of the logits x W^T + b: x[M,D], W[V,D],
+                            b[V] or NULL, loss[1] or loss[M] in fp32.  Forward through
+                            ms_cross_entropy_forward() only                               */
 } ms_kind;
+
+/* Reductions of MS_CROSS_ENTROPY. */
+typedef enum { MS_REDUCE_MEAN = 0, MS_REDUCE_SUM = 1, MS_REDUCE_NONE = 2 } ms_reduction;
 
 /* Activations of MS_GATED_LINEAR. */
 typedef enum {
@@ -167,9 +174,11 @@ typedef struct ms_record ms_record;
  * MS_SAVED_BITS: a ReLU's 1-bit mask; MS_SAVED_Y (policy accounting only):
  * the layer output, which stock PyTorch's ReLU keeps; MS_SAVED_MASK8 (policy
  * accounting only): the one-byte-per-element mask stock PyTorch's dropout
- * keeps.  MS_SAVED_PROJ: a gated linear unit's projections. */
+ * keeps.  MS_SAVED_PROJ: a gated linear unit's projections.  MS_SAVED_LSE: a
+ * cross entropy's log-sum-exp of each row (and its targets). */
 enum { MS_SAVED_X = 1u, MS_SAVED_W = 2u, MS_SAVED_MEAN = 4u, MS_SAVED_VAR = 8u, MS_SAVED_BITS = 16u,
-       MS_SAVED_Y = 32u, MS_SAVED_MASK8 = 64u, MS_SAVED_PROJ = 128u };
+       MS_SAVED_Y = 32u, MS_SAVED_MASK8 = 64u, MS_SAVED_PROJ = 128u,
+       MS_SAVED_LSE = 256u };
 
 /* Bits of ms_account.kernels: what the record's backward will launch. */
 enum { MS_K_DGRAD = 1u, MS_K_WGRAD = 2u, MS_K_BGRAD = 4u };
@@ -329,6 +338,33 @@ uint64_t ms_gated_projection_bytes(int64_t rows, int64_t F, int32_t dtype);
  */
 ms_status ms_gated_linear_forward(const ms_tensor *x, const ms_tensor *W, const ms_tensor *b, int32_t activation,
                                   void *proj, uint32_t mask, const ms_tensor *y, ms_record **rec, void *stream);
+
+/*
+ * ms_cross_entropy_forward -- the loss of a linear head, without its logits.
+ *
+ * z = x W^T + b;  row i with target t costs log(sum over v of exp(z_iv)) - z_it.
+ * The logits of a large vocabulary outweigh every other activation of a model;
+ * here they exist a tile at a time, and a record keeps of the softmax one number
+ * a row: its log-sum-exp.  Backward takes the logits again, a piece of the
+ * vocabulary at a time in transient workspace (at most 512 MiB of them):
+ *   dz = (exp(z - lse) - [v = t]) g,  dx = dz W,  dW = dz^T x,  db = sum of dz,
+ * g the gradient of the row's share of the loss.
+ * target: M contiguous int64 on the device.  Rows whose target is ignore_index
+ * take no part, whatever x holds in them: their loss and their row of dx are 0.
+ * Any other target outside [0, V) makes its loss NaN, and the gradients that it
+ * reaches.  reduction: MS_REDUCE_MEAN over the rows that count (NaN where none
+ * does, and no gradient), MS_REDUCE_SUM (loss[1]) or MS_REDUCE_NONE (loss[M]).
+ * x[M, D], W[V, D]: any strides, D, V >= 1; b[V] contiguous or NULL.  loss: fp32,
+ * contiguous.  With mask != 0, lse is caller-allocated device memory of M floats,
+ * fully overwritten, and borrowed with x, W, b and target (every gradient needs
+ * them all); with mask 0 it may be NULL.  dz is rounded to x's dtype before its
+ * products, everything else is in fp32.  Backward is ms_layer_backward() with
+ * grad_y of the loss's shape, fp32.  ms_layer_forward() rejects MS_CROSS_ENTROPY
+ * (MS_E_ARG).
+ */
+ms_status ms_cross_entropy_forward(const ms_tensor *x, const ms_tensor *W, const ms_tensor *b, const int64_t *target,
+                                   int64_t ignore_index, int32_t reduction, float *lse, uint32_t mask, const ms_tensor *loss,
+                                   ms_record **rec, void *stream);
 
 /*
  * ms_layer_backward -- write exactly the requested gradients for grad_y.

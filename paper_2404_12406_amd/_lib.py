@@ -14,8 +14,9 @@ MS_RG_INPUT, MS_RG_WEIGHT, MS_RG_BIAS = 1, 2, 4
 MS_F32, MS_BF16 = 0, 1
 MS_CONV2D, MS_LINEAR, MS_BN_EVAL, MS_AVGPOOL, MS_RELU, MS_CONV_TRANSPOSE2D, MS_DROPOUT = 0, 1, 2, 3, 4, 5, 6
 MS_CONV3D, MS_CONV_TRANSPOSE3D, MS_LAYER_NORM = 7, 8, 9
-MS_GATED_LINEAR = 10
+MS_GATED_LINEAR, MS_CROSS_ENTROPY = 10, 11
 MS_ACT = {"silu": 0, "gelu": 1, "gelu_tanh": 2, "relu": 3, "sigmoid": 4}
+MS_REDUCE = {"mean": 0, "sum": 1, "none": 2}
 MS_SAVED_X, MS_SAVED_W, MS_SAVED_MEAN, MS_SAVED_VAR, MS_SAVED_BITS, MS_SAVED_Y, MS_SAVED_MASK8 = 1, 2, 4, 8, 16, 32, 64
 MS_K_DGRAD, MS_K_WGRAD, MS_K_BGRAD = 1, 2, 4
 MS_POLICY_SELECTIVE, MS_POLICY_PYTORCH_DEFAULT, MS_POLICY_ALL_TRUE = 0, 1, 2
@@ -28,7 +29,7 @@ EXPORTS = (
     "ms_profile_start", "ms_profile_read", "ms_relu_mask_bytes", "ms_relu_forward",
     "ms_dropout_blocks", "ms_dropout_forward", "ms_layer_backward_noalloc", "ms_noalloc_scratch_bytes",
     "ms_testing_gemm_plan", "ms_testing_float_plan",
-    "ms_layer_norm_forward", "ms_gated_linear_forward", "ms_gated_projection_bytes",
+    "ms_layer_norm_forward", "ms_gated_linear_forward", "ms_gated_projection_bytes", "ms_cross_entropy_forward",
 )
 MS_PROF_FWD, MS_PROF_DGRAD, MS_PROF_WGRAD, MS_PROF_BN, MS_PROF_ACT, MS_PROF_RED = 1, 2, 4, 8, 16, 32
 
@@ -122,6 +123,9 @@ def configure(lib: ctypes.CDLL) -> ctypes.CDLL:
         lib.ms_gated_linear_forward.argtypes = [_T, _T, _T, ctypes.c_int32, ctypes.c_void_p, ctypes.c_uint32, _T,
                                                 ctypes.POINTER(ctypes.c_void_p), ctypes.c_void_p]
         lib.ms_gated_linear_forward.restype = ctypes.c_int
+        lib.ms_cross_entropy_forward.argtypes = [_T, _T, _T, ctypes.c_void_p, ctypes.c_int64, ctypes.c_int32, ctypes.c_void_p,
+                                                 ctypes.c_uint32, _T, ctypes.POINTER(ctypes.c_void_p), ctypes.c_void_p]
+        lib.ms_cross_entropy_forward.restype = ctypes.c_int
         lib.ms_gated_projection_bytes.argtypes = [ctypes.c_int64, ctypes.c_int64, ctypes.c_int32]
         lib.ms_gated_projection_bytes.restype = ctypes.c_uint64
     return lib

@@ -121,7 +121,20 @@ class GatedLinear:
     keep: str = "projections"
 
 
-_BLOCKS = (LayerNorm, GatedLinear)   # layers with a C entry point of their own
+@dataclass
+class LinearCrossEntropy:
+    """Softmax cross entropy of the logits x W^T + b for x[M, D], W[V, D], b[V]
+    or None, without the logits: loss[1] (reduction "mean" over the rows whose
+    target is not ignore_index, or "sum") or loss[M] ("none"), float32.
+    target: int64 [M], each a word in [0, V) or ignore_index.  Its record keeps
+    x, the targets and one number a row.  layer_backward takes the gradient of
+    the loss, float32 in its shape."""
+    target: torch.Tensor
+    ignore_index: int = -100
+    reduction: str = "mean"
+
+
+_BLOCKS = (LayerNorm, GatedLinear, LinearCrossEntropy)   # layers with a C entry point of their own
 
 
 def _pair(v):
@@ -276,6 +289,8 @@ def output_shape(spec, x: torch.Tensor, W: Optional[torch.Tensor]):
         return (x.shape[0], W.shape[0])
     if isinstance(spec, GatedLinear):
         return (x.shape[0], W.shape[0] // 2)
+    if isinstance(spec, LinearCrossEntropy):
+        return (x.shape[0] if spec.reduction == "none" else 1,)
     if isinstance(spec, BatchNormEval):
         return tuple(x.shape)
     if isinstance(spec, AvgPool):
@@ -426,7 +441,29 @@ class _BlockCall:
                 self.kept["projections"] = torch.empty(n, dtype=torch.uint8, device=x.device)
             elif self.mask and b is not None:
                 self.kept["b"] = b
-        self.y = torch.empty(output_shape(spec, x, W), dtype=x.dtype, device=x.device) if y is None else y
+        xent = isinstance(spec, LinearCrossEntropy)
+        if xent:
+            t = spec.target
+            if spec.reduction not in _lib.MS_REDUCE:
+                raise ValueError(f"reduction is \"mean\", \"sum\" or \"none\"; got {spec.reduction!r}")
+            if W is None or W.dim() != 2:
+                raise TypeError("LinearCrossEntropy needs W[V, D]")
+            if t.dtype != torch.int64:
+                raise TypeError(f"target must be int64, got {t.dtype}")
+            if t.shape != (x.shape[0],):
+                raise ValueError("target must have one element a row of x")
+            _on_gpu(x, t)
+            t = t.contiguous()
+            lse = torch.empty(x.shape[0] if self.mask else 0, dtype=torch.float32, device=x.device)
+            self._target, self._lse = (t.data_ptr() or None, lse.data_ptr() or None) if t.numel() else (None, None)
+            self._kept_target = t
+            if self.mask:
+                self.kept.update(lse=lse, target=t)
+                if b is not None:
+                    self.kept["b"] = b
+        if y is None:
+            y = torch.empty(output_shape(spec, x, W), dtype=torch.float32 if xent else x.dtype, device=x.device)
+        self.y = y
         self._d = [tensor_desc(t) for t in (x, W, b, self.y)]
         self._p = [_ptr(d) for d in self._d]
         proj = self.kept.get("projections")
@@ -438,6 +475,9 @@ class _BlockCall:
         if isinstance(spec, LayerNorm):
             check(lib.ms_layer_norm_forward(px, pw, pb, float(spec.eps), self.mask, py, h, stream),
                   "ms_layer_norm_forward")
+        elif isinstance(spec, LinearCrossEntropy):
+            check(lib.ms_cross_entropy_forward(px, pw, pb, self._target, int(spec.ignore_index), _lib.MS_REDUCE[spec.reduction],
+                                               self._lse, self.mask, py, h, stream), "ms_cross_entropy_forward")
         else:
             check(lib.ms_gated_linear_forward(px, pw, pb, _lib.MS_ACT[spec.act], self._proj, self.mask, py, h, stream),
                   "ms_gated_linear_forward")

@@ -33,7 +33,8 @@ from . import api
 from .api import MASK_BIAS, MASK_INPUT, MASK_WEIGHT
 
 __all__ = ["MSConv2d", "MSConvTranspose2d", "MSConv1d", "MSConvTranspose1d", "MSConv3d", "MSConvTranspose3d",
-           "MSLinear", "MSBatchNorm2dEval", "MSReLU", "MSDropout", "MSLayerNorm", "MSGatedLinear", "convert"]
+           "MSLinear", "MSBatchNorm2dEval", "MSReLU", "MSDropout", "MSLayerNorm", "MSGatedLinear", "MSLinearCrossEntropy",
+           "convert"]
 
 
 def _cl(t: Optional[torch.Tensor]) -> Optional[torch.Tensor]:
@@ -355,6 +356,24 @@ class MSGatedLinear(nn.Module):
     def forward(self, x):
         y = _LayerFn.apply(self.spec, x.reshape(-1, x.shape[-1]), self.weight, self.bias)
         return y.reshape(*x.shape[:-1], y.shape[-1])
+
+
+class MSLinearCrossEntropy(nn.Module):
+    """A linear head (weight [V, D], bias [V] or None) with its softmax cross
+    entropy: forward(x, target) is the loss (a scalar, or one a row with
+    reduction="none"), without the logits (see api.LinearCrossEntropy).  Leading
+    dims of x and target are flattened into rows."""
+
+    def __init__(self, weight: torch.Tensor, bias: Optional[torch.Tensor], ignore_index: int = -100, reduction: str = "mean"):
+        super().__init__()
+        self.weight = weight if isinstance(weight, nn.Parameter) else nn.Parameter(weight)
+        self.bias = bias if (bias is None or isinstance(bias, nn.Parameter)) else nn.Parameter(bias)
+        self.ignore_index, self.reduction = int(ignore_index), reduction
+
+    def forward(self, x, target):
+        spec = api.LinearCrossEntropy(target.reshape(-1), self.ignore_index, self.reduction)
+        loss = _LayerFn.apply(spec, x.reshape(-1, x.shape[-1]), self.weight, self.bias)
+        return loss.reshape(target.shape if self.reduction == "none" else ())
 
 
 def _convertible_conv(m) -> bool:

@@ -1,4 +1,5 @@
-// Host runtime of the transformer layers: layer norm and the gated linear unit.
+// Host runtime of the transformer layers: layer norm, the gated linear unit and
+// the cross entropy of a linear head.
 // Validation, the save rule and the records follow memsave.cpp: every check
 // runs before the first launch, a record borrows what its mask's gradients
 // need and nothing else, and all work goes to the caller's stream.
@@ -219,6 +220,38 @@ ms_status gated_backward(ms_record *r, const ms_tensor *gy, const ms_tensor *gx,
     return err ? hip_fail(err, "backward launch") : MS_OK;
 }
 
+// ------------------------------------------------------------------ cross entropy
+struct HeadPads {
+    bool w, b;
+};
+
+HeadPads head_pads(int32_t dtype, int64_t D, const void *w, const void *b) {
+    if (dtype != MS_BF16) return {false, false};
+    return {D % 8 != 0 || !aligned(w, 16), b && !aligned(b, 4)};
+}
+
+ms_status xent_backward(ms_record *r, const ms_tensor *gloss, const ms_tensor *gx, const ms_tensor *gw, const ms_tensor *gb,
+                        void *stream, bool fixed) {
+    const int32_t dt = r->plan.dtype;
+    const int64_t M = r->blk.M, D = r->blk.D, V = r->blk.F;
+    Stager sg;
+    const size_t ox = sg.add(&r->x), ow = sg.add(&r->W), ogx = gx ? sg.add(gx) : kNoStage, ogw = gw ? sg.add(gw) : kNoStage;
+    const HeadPads p = head_pads(dt, D, place(&r->W, ow), r->b.data);
+    const size_t kb = ms::xent_bwd_workspace(dt, M, D, V, p.w, p.b, gx, gw, gb);
+    Work w;
+    ms_status st = take(&w, sg.bytes + kb, stream, fixed);
+    if (st) return st;
+    int err = stage_in(&r->x, w.base, ox, stream);
+    if (!err) err = stage_in(&r->W, w.base, ow, stream);
+    if (!err)
+        err = ms::launch_xent_bwd(dt, M, D, V, kptr(&r->x, w.base, ox), kptr(&r->W, w.base, ow), r->b.data, p.w, p.b, r->blk.target,
+                                  r->blk.ignore, r->blk.reduction, static_cast<const float *>(gloss->data), r->blk.lse, kptr(gx, w.base, ogx),
+                                  kptr(gw, w.base, ogw), gb ? gb->data : nullptr, w.base + sg.bytes, stream);
+    if (!err) err = stage_out(gx, w.base, ogx, stream);
+    if (!err) err = stage_out(gw, w.base, ogw, stream);
+    return err ? hip_fail(err, "backward launch") : MS_OK;
+}
+
 }  // namespace
 
 extern "C" {
@@ -336,6 +369,76 @@ ms_status ms_gated_linear_forward(const ms_tensor *x, const ms_tensor *W, const 
         err = ms::launch_gated_fwd(x->dtype, M, pad.D8, F, activation, xk, wk, bk, kptr(y, w.base, oy), proj, ws,
                                    stream);
     if (!err) err = stage_out(y, w.base, oy, stream);
+    if (err) {
+        delete r;
+        return hip_fail(err, "forward launch");
+    }
+    file_record(r, rec);
+    return MS_OK;
+}
+
+ms_status ms_cross_entropy_forward(const ms_tensor *x, const ms_tensor *W, const ms_tensor *b, const int64_t *target,
+                                   int64_t ignore_index, int32_t reduction, float *lse, uint32_t mask, const ms_tensor *loss,
+                                   ms_record **rec, void *stream) {
+    clear_err();
+    if (!rec) return fail(MS_E_NULL, "rec is NULL");
+    *rec = nullptr;
+    if (!W) return fail(MS_E_NULL, "cross entropy needs W");
+    ms_status st = check_mask(mask, W, b);
+    if (!st) st = check_tensor(x, "x", 2, true);
+    if (!st) st = check_tensor(W, "W", 2, true);
+    if (st) return st;
+    const int64_t M = x->shape[0], D = x->shape[1], V = W->shape[0];
+    if (x->dtype != W->dtype) return fail(MS_E_DTYPE, "x and W dtypes differ");
+    if (D < 1 || V < 1) return fail(MS_E_SHAPE, "W must be [V, D] with V, D >= 1");
+    if (W->shape[1] != D)
+        return fail(MS_E_SHAPE, "W has %lld input features, x has %lld", (long long)W->shape[1], (long long)D);
+    if (!strides_ok(x) || !strides_ok(W)) return fail(MS_E_LAYOUT, "x and W need non-negative strides");
+    // rows padded to whole 16-byte vectors have 32-bit offsets too
+    if (capped_product({std::max(M, V), (D + 7) / 8 * 8}) > kMaxElems - 16)
+        return fail(MS_E_UNSUPPORTED, "operands have more than 2^31-17 elements");
+    if ((st = check_vector(b, "b", V, x->dtype))) return st;
+    if (reduction < MS_REDUCE_MEAN || reduction > MS_REDUCE_NONE) return fail(MS_E_ARG, "unknown reduction %d", reduction);
+    if (M > 0 && !target) return fail(MS_E_NULL, "target is NULL");
+    if (!aligned(target, 8)) return fail(MS_E_ARG, "target must be 8-byte aligned");
+    if ((st = check_tensor(loss, "loss", 1, true))) return st;
+    if (loss->dtype != MS_F32) return fail(MS_E_DTYPE, "loss must be fp32");
+    const int64_t n = reduction == MS_REDUCE_NONE ? M : 1;
+    if (loss->shape[0] != n) return fail(MS_E_SHAPE, "loss must have %lld elements", (long long)n);
+    if (!is_contig1(loss)) return fail(MS_E_LAYOUT, "loss must be contiguous");
+    if (mask && M > 0 && !lse) return fail(MS_E_NULL, "lse is NULL but gradients are asked for");
+    Stager sg;
+    const size_t ox = sg.add(x), ow = sg.add(W);
+    const HeadPads p = head_pads(x->dtype, D, place(W, ow), b ? b->data : nullptr);
+    const size_t kb = ms::xent_fwd_workspace(x->dtype, M, D, V, p.w, p.b, reduction);
+    Work w;
+    if ((st = take(&w, sg.bytes + kb, stream, false))) return st;
+    ms_record *r = nullptr;
+    if (mask) {
+        r = new_record(MS_CROSS_ENTROPY, x, W, b, loss, mask, MS_SAVED_X | MS_SAVED_W | MS_SAVED_LSE, xent_backward);
+        if (!r) return fail(MS_E_NOMEM, "record allocation failed");
+        r->blk.M = M;
+        r->blk.D = D;
+        r->blk.F = V;
+        r->blk.reduction = reduction;
+        r->blk.ignore = ignore_index;
+        r->blk.target = target;
+        r->blk.lse = lse;
+        if (b) {
+            r->b.data = b->data;
+            r->acct.referenced_param_bytes += bytes_of(b);
+        }
+        r->acct.saved_activation_bytes += (uint64_t)M * (sizeof(float) + sizeof(int64_t));
+        const bool dx = mask & MS_RG_INPUT, dw = mask & MS_RG_WEIGHT, db = mask & MS_RG_BIAS;
+        r->acct.transient_workspace_bytes = ms::xent_bwd_workspace(x->dtype, M, D, V, p.w, p.b, dx, dw, db) + staging(x, true) +
+                                            staging(W, true) + staging(x, dx) + staging(W, dw);
+    }
+    int err = stage_in(x, w.base, ox, stream);
+    if (!err) err = stage_in(W, w.base, ow, stream);
+    if (!err)
+        err = ms::launch_xent_fwd(x->dtype, M, D, V, kptr(x, w.base, ox), kptr(W, w.base, ow), b ? b->data : nullptr, p.w, p.b, target,
+                                  ignore_index, reduction, static_cast<float *>(loss->data), mask ? lse : nullptr,
+                                  w.base + sg.bytes, stream);
     if (err) {
         delete r;
         return hip_fail(err, "forward launch");

@@ -169,6 +169,21 @@ size_t linear_bwd_workspace(int dtype, int64_t M, int64_t K, int64_t N, bool dx,
 int launch_linear_bwd(int dtype, int64_t M, int64_t K, int64_t N, const void *dy, const void *x, const void *w, void *dx, void *dw,
                       void *db, void *ws, void *stream);
 
+// Softmax cross entropy of the logits x[M][D] w[V][D]^T + b (b may be null) of the
+// rows whose target is not `ignore` (a target that is no word gives NaN).
+// reduction: 0 mean, 1 sum (loss[1]), 2 none (loss[M]); lse[M] (may be null in the
+// forward) is what the backward needs.  padw, padb: bf16 weight rows that are no
+// whole 16-byte vectors or not so aligned, a bias not 4-byte aligned (they are
+// copied).  In the backward any of dx, dw, db may be null; gloss is the gradient of
+// the loss, fp32.
+size_t xent_fwd_workspace(int dtype, int64_t M, int64_t D, int64_t V, bool padw, bool padb, int reduction);
+int launch_xent_fwd(int dtype, int64_t M, int64_t D, int64_t V, const void *x, const void *w, const void *b, bool padw, bool padb,
+                    const int64_t *target, int64_t ignore, int reduction, float *loss, float *lse, void *ws, void *stream);
+size_t xent_bwd_workspace(int dtype, int64_t M, int64_t D, int64_t V, bool padw, bool padb, bool dx, bool dw, bool db);
+int launch_xent_bwd(int dtype, int64_t M, int64_t D, int64_t V, const void *x, const void *w, const void *b, bool padw, bool padb,
+                    const int64_t *target, int64_t ignore, int reduction, const float *gloss, const float *lse, void *dx, void *dw,
+                    void *db, void *ws, void *stream);
+
 // Global average pool x[N][L][C] -> y[N][C] and its adjoint.
 int launch_avgpool_fwd(int dtype, const void *x, int N, int L, int C, void *y, void *stream);
 int launch_avgpool_bwd(int dtype, const void *dy, int N, int L, int C, void *dx, void *stream);

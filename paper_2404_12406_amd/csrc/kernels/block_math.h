@@ -46,14 +46,18 @@ __device__ __forceinline__ uint32_t to_f24(float v) {
 
 typedef float floatx2 __attribute__((ext_vector_type(2)));
 
-constexpr float kLog2e = 1.44269504088896341f, kLn2 = 0.693147180559945309f;
+constexpr float kLog2e = 1.44269504088896341f;
 
-// (m, s) stands for s 2^m, m the running maximum in powers of two: the sum of two.
-// A maximum of minus infinity (nothing yet) comes with s = 0; a NaN stays in s.
+// exp(v - m).  The difference first: with m the larger one it is a finite number
+// or minus infinity, whatever the sizes of both (v log2(e) - m log2(e) is not).
+__device__ __forceinline__ float exp_below(float v, float m) { return __builtin_amdgcn_exp2f((v - m) * kLog2e); }
+
+// (m, s) stands for s exp(m), m the running maximum: the sum of two.  A maximum of
+// minus infinity (nothing yet) comes with s = 0; a NaN stays in s.
 __device__ __forceinline__ floatx2 join_lse(floatx2 a, floatx2 b) {
     const float m = fmaxf(a.x, b.x);
-    const float sa = a.x == m ? a.y : a.y * __builtin_amdgcn_exp2f(a.x - m);
-    const float sb = b.x == m ? b.y : b.y * __builtin_amdgcn_exp2f(b.x - m);
+    const float sa = a.x == m ? a.y : a.y * exp_below(a.x, m);
+    const float sb = b.x == m ? b.y : b.y * exp_below(b.x, m);
     return floatx2{m, sa + sb};
 }
 

@@ -2107,6 +2107,13 @@ int wgrad_core(const ConvGeom &g, const void *dy, const void *x, void *dw, void 
     return err;
 }
 
+// For a weight gradient's partials made elsewhere: out[M][C] = sum of `splits`
+// arrays [M][C8] (none: out is there already), db[M] that of dbpart's rows.
+int sum_wgrad_partials(const float *part, int splits, int M, int C8, int C, void *out, const float *dbpart, void *db, hipStream_t st) {
+    const int64_t n = part ? (int64_t)M * C8 : 0;
+    return launch_reduce(part, splits, n, n, (bf16 *)out, dbpart, db ? M : 0, (bf16 *)db, nullptr, 1, C8, C < C8 ? C : 0, 2048, st);
+}
+
 int conv_wgrad(const ConvGeom &g, const void *dy, const void *x, void *dw, void *db, void *ws, hipStream_t st) {
     if (!wgrad_applies(g)) return -1;
     if (g.K % 8 == 0) return wgrad_core(g, dy, x, dw, db, ws, st);

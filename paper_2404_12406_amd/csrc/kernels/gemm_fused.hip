@@ -9,7 +9,7 @@
 //                 target's logit; z is not written
 //   kEpiXent      z again, then dz = (exp(z - lse) - [column = target]) scale
 //   kEpiAdd       dx += dz W for one piece of the vocabulary, in fp32
-//   kEpiStore     the weight gradient dz^T x over the rows that count
+//   kEpiStore     the weight gradient dz^T x over the rows that count, times a factor
 // The main loop is gemm_block_body.inc's.  Everything before the one rounding
 // of what is stored is in fp32.
 #include <hip/hip_ext.h>
@@ -36,7 +36,8 @@ struct FusedArgs : Args {
     floatx2 *stat;         // kEpiLse: softmax statistics as join_lse()'s, [column tile][rows]
     float *tlogit;         // kEpiLse: the target's logit
     int64_t stat_ld;
-    const float *lse, *scale;   // kEpiXent
+    const float *lse, *scale;   // kEpiXent: of each row
+    const float *out_scale;     // kEpiStore: the sums' factor
     int add;               // kEpiAdd: add to the partials (0: write them)
 };
 
@@ -46,9 +47,10 @@ __device__ __forceinline__ int gate_col(int row) { return (row >> 6) * 32 + (row
 typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 
-// Bias of columns n .. n + 3 (zeros past N), through a descriptor of N entries.
-__device__ __forceinline__ void bias4(__amdgpu_buffer_rsrc_t r, int n, int N, float (&o)[4]) {
-    if ((N & 3) == 0) {
+// Bias of columns n .. n + 3, zeros past the descriptor's end; `quads`: its length
+// and n are whole fours.
+__device__ __forceinline__ void bias4(__amdgpu_buffer_rsrc_t r, int n, bool quads, float (&o)[4]) {
+    if (quads) {
         const u32x2 w = __builtin_amdgcn_raw_buffer_load_b64(r, n * 2, 0, 0);
 #pragma unroll
         for (int v = 0; v < 4; ++v) o[v] = __uint_as_float((v & 1) ? (w[v >> 1] & 0xffff0000u) : (w[v >> 1] << 16));
@@ -110,6 +112,31 @@ __device__ __forceinline__ void put_bytes(uint8_t *stage, const uint32_t (&b)[TG
     }
 }
 
+// What the sums start from: the bias of their columns and, in the softmax, minus
+// infinity past the last word (nothing is added to it there: W's rows read zeros).
+template <int EPI, class G>
+__device__ __forceinline__ void fused_init(const FusedArgs &P, floatx16 (&acc)[G::TM][G::TN], int n0, int wn0, int lane) {
+    constexpr bool GATED = EPI == kEpiGate || EPI == kEpiGateGrad, SOFTMAX = EPI == kEpiLse || EPI == kEpiXent;
+    const int fh = lane >> 5, nb = GATED ? 2 * P.F : P.N;
+    const __amdgpu_buffer_rsrc_t r = rsrc(P.fbias, P.fbias ? (uint32_t)nb * 2u : 0u);
+#pragma unroll
+    for (int j = 0; j < G::TN; ++j)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            const int c = 8 * q + 4 * fh;
+            float b[4];
+            // (gated columns past F read the other half's: not stored)
+            if constexpr (GATED) bias4(r, (n0 + wn0) / 2 + 32 * (j / 2) + c + (j & 1) * P.F, (P.F & 3) == 0, b);
+            else bias4(r, n0 + wn0 + 32 * j + c, (nb & 3) == 0, b);
+#pragma unroll
+            for (int v = 0; v < 4; ++v) {
+                if (SOFTMAX && n0 + wn0 + 32 * j + c + v >= nb) b[v] = -INFINITY;
+#pragma unroll
+                for (int i = 0; i < G::TM; ++i) acc[i][j][4 * q + v] = b[v];
+            }
+        }
+}
+
 // The lane's 16 sums of tile (i, j) are row 32 i + lane % 32 and columns
 // 32 j + 8 q + 4 (lane / 32) + v, q and v = 0..3.
 template <int EPI, class G>
@@ -124,7 +151,6 @@ __device__ __forceinline__ void fused_epilogue(const FusedArgs &P, char *smem, f
         static_assert(TN % 2 == 0, "gated tiles pair the column tiles of a wave");
         const int F = P.F, f0 = (n0 + wn0) / 2;
         const int ncol = min(F - f0, COLS);
-        const __amdgpu_buffer_rsrc_t rbias = rsrc(P.fbias, P.fbias ? (uint32_t)F * 4u : 0u);
 #pragma unroll
         for (int i = 0; i < TM; ++i) {
             const int mb = m0 + wm0 + 32 * i, nrow = M - mb;   // rows of this pass
@@ -158,17 +184,12 @@ __device__ __forceinline__ void fused_epilogue(const FusedArgs &P, char *smem, f
 #pragma unroll
                 for (int q = 0; q < 4; ++q) {
                     const int c = 32 * j + 8 * q + 4 * fh;
-                    float bg[4] = {0.f, 0.f, 0.f, 0.f}, bu[4] = {0.f, 0.f, 0.f, 0.f};
-                    if (P.fbias) {   // (columns past F read the other half's: not stored)
-                        bias4(rbias, f0 + c, 2 * F, bg);
-                        bias4(rbias, F + f0 + c, (F & 3) ? 1 : 2 * F, bu);
-                    }
                     bf16x4 d4;
                     if constexpr (EPI == kEpiGateGrad) d4 = *reinterpret_cast<const bf16x4 *>(stage + fr * PITCH + c);
                     lg[j][q] = lu[j][q] = 0u;
 #pragma unroll
                     for (int v = 0; v < 4; ++v) {
-                        const float zg = acc[i][2 * j][4 * q + v] + bg[v], zu = acc[i][2 * j + 1][4 * q + v] + bu[v];
+                        const float zg = acc[i][2 * j][4 * q + v], zu = acc[i][2 * j + 1][4 * q + v];
                         if constexpr (EPI == kEpiGate) {
                             acc[i][2 * j][4 * q + v] = act::value<true>(P.act, zg) * zu;
                             if (P.proj) {
@@ -223,37 +244,12 @@ __device__ __forceinline__ void fused_epilogue(const FusedArgs &P, char *smem, f
             __builtin_amdgcn_wave_barrier();
         }
     } else if constexpr (EPI == kEpiLse || EPI == kEpiXent) {
-        if (P.fbias) {
-            const __amdgpu_buffer_rsrc_t rbias = rsrc(P.fbias, (uint32_t)N * 2u);
-#pragma unroll
-            for (int j = 0; j < TN; ++j)
-#pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    float b[4];
-                    bias4(rbias, n0 + wn0 + 32 * j + 8 * q + 4 * fh, N, b);
-#pragma unroll
-                    for (int i = 0; i < TM; ++i)
-#pragma unroll
-                        for (int v = 0; v < 4; ++v) acc[i][j][4 * q + v] += b[v];
-                }
-        }
-        if (n0 + wn0 + G::WN > N) {   // columns past the piece: exponentials of zero
-#pragma unroll
-            for (int j = 0; j < TN; ++j)
-#pragma unroll
-                for (int q = 0; q < 4; ++q)
-#pragma unroll
-                    for (int v = 0; v < 4; ++v) {
-                        const bool past = n0 + wn0 + 32 * j + 8 * q + 4 * fh + v >= N;
-#pragma unroll
-                        for (int i = 0; i < TM; ++i) acc[i][j][4 * q + v] = past ? -INFINITY : acc[i][j][4 * q + v];
-                    }
-        }
         if constexpr (EPI == kEpiLse) {
             constexpr int BM = G::A_BYTES / (BK * 2), WC = G::B_BYTES / (BK * 2) / G::WN;   // waves along the columns
             floatx2 *red = reinterpret_cast<floatx2 *>(smem);   // [WC][BM]
 #pragma unroll
             for (int i = 0; i < TM; ++i) {
+                __builtin_amdgcn_sched_barrier(0);   // one pass at a time: the sums leave few registers
                 const int m = m0 + wm0 + 32 * i + fr;
                 float top = -INFINITY;
 #pragma unroll
@@ -262,14 +258,14 @@ __device__ __forceinline__ void fused_epilogue(const FusedArgs &P, char *smem, f
                     for (int v = 0; v < 16; ++v) top = fmaxf(top, acc[i][j][v]);
                 top = fmaxf(top, __shfl_xor(top, 32));
                 // (fmaxf passes over NaN: the sum below meets it)
-                const float t2 = top == -INFINITY ? 0.f : top * kLog2e;
+                const float t0 = top == -INFINITY ? 0.f : top;
                 float s = 0.f;
 #pragma unroll
                 for (int j = 0; j < TN; ++j)
 #pragma unroll
-                    for (int v = 0; v < 16; ++v) s += __builtin_amdgcn_exp2f(__builtin_fmaf(acc[i][j][v], kLog2e, -t2));
+                    for (int v = 0; v < 16; ++v) s += exp_below(acc[i][j][v], t0);
                 s += __shfl_xor(s, 32);
-                if (fh == 0) red[(wn0 / G::WN) * BM + wm0 + 32 * i + fr] = floatx2{top == -INFINITY ? top : t2, s};
+                if (fh == 0) red[(wn0 / G::WN) * BM + wm0 + 32 * i + fr] = floatx2{top, s};
                 const int t = m < M ? P.target[m] - P.v0 - (n0 + wn0) : -1;   // within this wave's columns?
                 if (__any((unsigned)t < (unsigned)G::WN)) {
                     float z = 0.f;
@@ -300,9 +296,10 @@ __device__ __forceinline__ void fused_epilogue(const FusedArgs &P, char *smem, f
             const int ncol = min(P.ldc - (n0 + wn0), G::WN);   // the padding columns are zeros
 #pragma unroll
             for (int i = 0; i < TM; ++i) {
+                __builtin_amdgcn_sched_barrier(0);   // one pass at a time: the sums leave few registers
                 const int mb = m0 + wm0 + 32 * i, m = mb + fr;
                 const bool in = m < M;
-                const float l2 = in ? P.lse[m] * kLog2e : 0.f, sc = in ? P.scale[m] : 0.f;
+                const float l = in ? P.lse[m] : 0.f, sc = in ? P.scale[m] : 0.f;
                 const int t = in ? P.target[m] - P.v0 - (n0 + wn0) : -1;
                 const bool any = __any((unsigned)t < (unsigned)G::WN);
 #pragma unroll
@@ -312,7 +309,7 @@ __device__ __forceinline__ void fused_epilogue(const FusedArgs &P, char *smem, f
                         bf16x4 o;
 #pragma unroll
                         for (int v = 0; v < 4; ++v) {
-                            float p = __builtin_amdgcn_exp2f(__builtin_fmaf(acc[i][j][4 * q + v], kLog2e, -l2));
+                            float p = exp_below(acc[i][j][4 * q + v], l);
                             if (any && t == 32 * j + 8 * q + 4 * fh + v) p -= 1.f;
                             o[v] = (bf16)(p * sc);
                         }
@@ -477,6 +474,126 @@ int gate_grad(int64_t M, int64_t D, int64_t F, int act, const void *x, const voi
     a.dh = (const bf16 *)dy;
     a.c = (bf16 *)dz;
     return go_rows<kEpiGateGrad>(p.tile, kProfFwd, a, st);
+}
+
+// ------------------------------------------------------------------ cross entropy
+// Column tiles of the statistics (rows of `stat`).
+int xent_lse_tiles(int64_t M, int64_t D, int64_t V) {
+    const Tile &t = kRowTiles[plan(kRowTiles, 2, M, V, D, 1).tile];
+    return (int)((V + t.bn - 1) / t.bn);
+}
+
+int xent_lse(int64_t M, int64_t D, int64_t V, const void *x, const void *w, const void *bias, const int *count, const int *target,
+             void *stat, float *tlogit, hipStream_t st) {
+    const FusedPlan p = plan(kRowTiles, 2, M, V, D, 1);
+    FusedArgs a = rows_args(kRowTiles[p.tile], M, V, D, x, w, V);
+    a.fbias = (const bf16 *)bias;
+    a.count = count;
+    a.target = target;
+    a.stat = (floatx2 *)stat;
+    a.stat_ld = M;
+    a.tlogit = tlogit;
+    return go_rows<kEpiLse>(p.tile, kProfFwd, a, st);
+}
+
+// dz[M][ldz] of the words v0 .. v0 + V - 1, whose rows of W and biases w and
+// bias are; columns V .. ldz - 1 are zeros.
+int xent_grad(int64_t M, int64_t D, int64_t V, const void *x, const void *w, const void *bias, const int *count, const int *target,
+              int v0, const float *lse, const float *scale, void *dz, int64_t ldz, hipStream_t st) {
+    const FusedPlan p = plan(kRowTiles, 2, M, V, D, 1);
+    FusedArgs a = rows_args(kRowTiles[p.tile], M, V, D, x, w, V);
+    a.fbias = (const bf16 *)bias;
+    a.count = count;
+    a.target = target;
+    a.v0 = v0;
+    a.lse = lse;
+    a.scale = scale;
+    a.c = (bf16 *)dz;
+    a.ldc = (int)ldz;
+    return go_rows<kEpiXent>(p.tile, kProfFwd, a, st);
+}
+
+// Splits of dx += dz w over the words of a piece: arrays [M][D] of partials.
+int xent_dx_splits(int64_t M, int64_t D, int64_t V) { return plan(kGradTiles, 3, M, D, V, (int)std::clamp<int64_t>(V / (4 * BK), 1, 16)).splits; }
+
+int xent_dx(int64_t M, int64_t D, int64_t V, int64_t ldz, const void *dz, const void *w, const int *count, float *part, int splits,
+            bool add, hipStream_t st) {
+    // (a last, smaller piece runs with the splits of the others)
+    FusedPlan p{0, splits};
+    double best = 1e300;
+    for (int t = 0; t < 3; ++t) {
+        const double us = est_us(kGradTiles[t], M, D, V, 1, splits);
+        if (us < best) {
+            best = us;
+            p.tile = t;
+        }
+    }
+    const Tile &t = kGradTiles[p.tile];
+    FusedArgs a{};
+    a.a = (const bf16 *)dz;
+    a.b = (const bf16 *)w;
+    a.g.N = (int)M; a.g.C = (int)D; a.g.K = (int)ldz;
+    a.g.H = a.g.W = a.g.R = a.g.S = a.g.P = a.g.Q = a.g.sh = a.g.sw = 1;
+    a.M = (int)M; a.N = (int)D; a.K = (int)ldz;
+    a.ntm = (int)((M + t.bm - 1) / t.bm);
+    a.ntn = (int)((D + t.bn - 1) / t.bn);
+    a.splits = splits;
+    a.k_split = (int)(((ldz + splits - 1) / splits + BK - 1) / BK * BK);
+    a.a_bytes = bytes_of(M * ldz);
+    a.b_bytes = bytes_of(V * D);
+    a.count = count;
+    a.part = part;
+    a.part_stride = M * D;
+    a.add = add;
+    return go_grad<kEpiAdd, kDgradN>(p.tile, kProfDgrad, a, st);
+}
+
+// dw[V][Dr] = *scale dz^T x over the rows that count (x has D >= Dr columns), and db.
+int sum_wgrad_partials(const float *part, int splits, int M, int C8, int C, void *out, const float *dbpart, void *db, hipStream_t st);
+
+namespace {
+FusedPlan dw_plan(int64_t M, int64_t D, int64_t Dr, int64_t V) {
+    FusedPlan p = plan(kGradTiles, 3, V, D, M, (int)std::clamp<int64_t>(M / (4 * BK), 1, 16));
+    if (D != Dr) p.splits = std::max(p.splits, 2);   // the sum of the partials leaves the padding out
+    return p;
+}
+}  // namespace
+
+size_t xent_dw_workspace(int64_t M, int64_t D, int64_t Dr, int64_t V, bool db) {
+    const FusedPlan p = dw_plan(M, D, Dr, V);
+    return ((p.splits > 1 ? (size_t)p.splits * V * D : 0) + (db ? (size_t)p.splits * V : 0)) * sizeof(float);
+}
+
+int xent_dw(int64_t M, int64_t D, int64_t Dr, int64_t V, int64_t ldz, const void *dz, const void *x, const int *count,
+            const float *scale, void *dw, void *db, void *ws, hipStream_t st) {
+    const FusedPlan p = dw_plan(M, D, Dr, V);
+    const Tile &t = kGradTiles[p.tile];
+    FusedArgs a{};
+    a.a = (const bf16 *)dz;
+    a.b = (const bf16 *)x;
+    a.g.N = (int)M; a.g.C = (int)D; a.g.K = (int)ldz;
+    a.g.H = a.g.W = a.g.R = a.g.S = a.g.P = a.g.Q = a.g.sh = a.g.sw = 1;
+    a.M = (int)V; a.N = (int)D; a.K = (int)M;
+    a.ntm = (int)((V + t.bm - 1) / t.bm);
+    a.ntn = (int)((D + t.bn - 1) / t.bn);
+    a.splits = p.splits;
+    a.k_split = (int)M;
+    a.a_bytes = bytes_of(M * ldz);
+    a.b_bytes = bytes_of(M * D);
+    a.count = count;
+    a.out_scale = scale;
+    float *f = static_cast<float *>(ws);
+    if (p.splits > 1) {
+        a.part = f;
+        a.part_stride = V * D;
+        f += (size_t)p.splits * V * D;
+    } else {
+        a.c = (bf16 *)dw;
+    }
+    a.dbpart = db ? f : nullptr;
+    const int err = go_grad<kEpiStore, kWgrad>(p.tile, kProfWgrad, a, st);
+    if (err || (p.splits == 1 && !db)) return err;
+    return sum_wgrad_partials(a.part, p.splits, (int)V, (int)D, (int)Dr, dw, a.dbpart, db, st);
 }
 
 }  // namespace g2

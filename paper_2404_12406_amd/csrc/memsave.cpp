@@ -511,6 +511,8 @@ ms_status ms_layer_forward(const ms_layer *layer, const ms_tensor *x, const ms_t
     if (layer && layer->kind == MS_LAYER_NORM) return fail(MS_E_ARG, "layer norm runs through ms_layer_norm_forward()");
     if (layer && layer->kind == MS_GATED_LINEAR)
         return fail(MS_E_ARG, "gated linear units run through ms_gated_linear_forward()");
+    if (layer && layer->kind == MS_CROSS_ENTROPY)
+        return fail(MS_E_ARG, "cross entropy runs through ms_cross_entropy_forward()");
     Plan pl;
     ms_status st = validate_forward(layer, x, W, b, mask, y, true, &pl);
     if (st) return st;
