@@ -306,7 +306,7 @@ ms_status ms_layer_norm_forward(const ms_tensor *x, const ms_tensor *gamma, cons
 /*
  * ms_gated_projection_bytes -- size of the projections of M rows that
  * ms_gated_linear_forward() keeps in `proj`: [M, 2F] values of 4 bytes for
- * MS_F32, and of 3 for MS_BF16 (sign, exponent and 15 bits of the fraction,
+ * MS_F32 (F rounded up to 16), and of 3 for MS_BF16 (sign, exponent and 15 bits of the fraction,
  * rounded to nearest even; the two leading bytes of all values, then the third
  * ones).  In bf16 alone, 7 bits of fraction, the gradients would be a third
  * further off than their own rounding makes them.  0 where an extent is not

@@ -137,50 +137,7 @@ ms_status norm_backward(ms_record *r, const ms_tensor *gy, const ms_tensor *gx, 
 }
 
 // ------------------------------------------------------------------ gated linear unit
-// bf16 operands of the row contractions as those take them: D whole 16-byte
-// vectors, aligned.  Others get zero-padded copies.
-struct Padded {
-    int64_t D8 = 0;
-    bool x = false, w = false, b = false;
-    size_t ox = 0, ow = 0, ob = 0, bytes = 0;
-};
-
 bool aligned(const void *p, uintptr_t n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; }
-
-// x, w, b: the dense operands, in workspace (aligned) or the caller's
-Padded pad_plan(int32_t dtype, int64_t M, int64_t N, int64_t D, const void *x, const void *w, const void *b) {
-    Padded p;
-    p.D8 = (D + 7) / 8 * 8;
-    if (dtype != MS_BF16) {
-        p.D8 = D;
-        return p;
-    }
-    p.x = D % 8 || !aligned(x, 16);
-    p.w = D % 8 || !aligned(w, 16);
-    p.b = b && !aligned(b, 4);
-    p.ox = 0;
-    p.ow = p.x ? al256((size_t)M * p.D8 * 2) : 0;
-    p.ob = p.ow + (p.w ? al256((size_t)N * p.D8 * 2) : 0);
-    p.bytes = p.ob + (p.b ? al256((size_t)N * 2) : 0);
-    return p;
-}
-
-int pad_run(const Padded &p, int64_t M, int64_t N, int64_t D, char *base, const void **x, const void **w, const void **b, void *stream) {
-    int err = 0;
-    if (p.x) {
-        err = ms::launch_pad_rows(MS_BF16, *x, M, D, base + p.ox, p.D8, stream);
-        *x = base + p.ox;
-    }
-    if (!err && p.w) {
-        err = ms::launch_pad_rows(MS_BF16, *w, N, D, base + p.ow, p.D8, stream);
-        *w = base + p.ow;
-    }
-    if (!err && p.b) {
-        err = ms::launch_pad_rows(MS_BF16, *b, 1, N, base + p.ob, (N + 7) / 8 * 8, stream);
-        *b = base + p.ob;
-    }
-    return err;
-}
 
 // Where a stand-in will lie: aligned, whatever the caller's pointer is.
 const void *place(const ms_tensor *t, size_t off) { return off == kNoStage ? t->data : nullptr; }
@@ -194,27 +151,17 @@ ms_status gated_backward(ms_record *r, const ms_tensor *gy, const ms_tensor *gx,
     Stager sg;
     const size_t oy = sg.add(gy), ox = read_x ? sg.add(&r->x) : kNoStage, ow = read_w ? sg.add(&r->W) : kNoStage;
     const size_t ogx = gx ? sg.add(gx) : kNoStage, ogw = gw ? sg.add(gw) : kNoStage;
-    const Padded pad = again ? pad_plan(dt, M, 2 * F, D, place(&r->x, ox), place(&r->W, ow), r->b.data) : Padded{};
-    const size_t dzb = al256((size_t)M * 2 * F * elt_size(dt));
-    const size_t kb = std::max(ms::gated_dz_workspace(dt, M, D, F, !again),
-                               ms::linear_bwd_workspace(dt, M, D, 2 * F, gx, gw, gb));
+    const size_t kb = ms::gated_bwd_workspace(dt, M, D, F, place(&r->x, ox), place(&r->W, ow), r->b.data, !again, gx, gw, gb);
     Work w;
-    // the padded copies are read before the gradients' workspace is written
-    ms_status st = take(&w, sg.bytes + dzb + std::max(kb, pad.bytes), stream, fixed);
+    ms_status st = take(&w, sg.bytes + kb, stream, fixed);
     if (st) return st;
-    char *dz = w.base + sg.bytes, *ws = dz + dzb;
     int err = stage_in(gy, w.base, oy, stream);
     if (!err && read_x) err = stage_in(&r->x, w.base, ox, stream);
     if (!err && read_w) err = stage_in(&r->W, w.base, ow, stream);
-    const void *xk = kptr(&r->x, w.base, ox), *wk = kptr(&r->W, w.base, ow);
-    const void *xp = xk, *wp = wk, *bp = r->b.data;
-    if (!err && again) err = pad_run(pad, M, 2 * F, D, ws, &xp, &wp, &bp, stream);
     if (!err)
-        err = ms::launch_gated_dz(dt, M, again ? pad.D8 : D, F, r->blk.act, xp, wp, bp, r->blk.proj, kptr(gy, w.base, oy), dz, ws,
-                                  stream);
-    if (!err)
-        err = ms::launch_linear_bwd(dt, M, D, 2 * F, dz, xk, wk, kptr(gx, w.base, ogx), kptr(gw, w.base, ogw),
-                                    gb ? gb->data : nullptr, ws, stream);
+        err = ms::launch_gated_bwd(dt, M, D, F, r->blk.act, kptr(&r->x, w.base, ox), kptr(&r->W, w.base, ow), r->b.data, r->blk.proj,
+                                   kptr(gy, w.base, oy), kptr(gx, w.base, ogx), kptr(gw, w.base, ogw), gb ? gb->data : nullptr,
+                                   w.base + sg.bytes, stream);
     if (!err) err = stage_out(gx, w.base, ogx, stream);
     if (!err) err = stage_out(gw, w.base, ogw, stream);
     return err ? hip_fail(err, "backward launch") : MS_OK;
@@ -303,7 +250,8 @@ ms_status ms_layer_norm_forward(const ms_tensor *x, const ms_tensor *gamma, cons
 }
 
 uint64_t ms_gated_projection_bytes(int64_t rows, int64_t F, int32_t dtype) {
-    return rows > 0 && F > 0 ? (uint64_t)rows * 2u * (uint64_t)F * (dtype == MS_BF16 ? 3u : 4u) : 0u;
+    if (rows <= 0 || F <= 0) return 0;
+    return dtype == MS_BF16 ? (uint64_t)rows * 2u * (uint64_t)F * 3u : (uint64_t)rows * 2u * (uint64_t)((F + 15) / 16 * 16) * 4u;
 }
 
 ms_status ms_gated_linear_forward(const ms_tensor *x, const ms_tensor *W, const ms_tensor *b, int32_t activation,
@@ -331,10 +279,10 @@ ms_status ms_gated_linear_forward(const ms_tensor *x, const ms_tensor *W, const 
     }
     Stager sg;
     const size_t ox = sg.add(x), ow = sg.add(W), oy = sg.add(y);
-    const Padded pad = pad_plan(x->dtype, M, 2 * F, D, place(x, ox), place(W, ow), b ? b->data : nullptr);
-    const size_t kb = ms::gated_fwd_workspace(x->dtype, M, D, F, proj != nullptr);
+    const void *bk = b ? b->data : nullptr;
+    const size_t kb = ms::gated_fwd_workspace(x->dtype, M, D, F, place(x, ox), place(W, ow), bk, proj != nullptr);
     Work w;
-    if ((st = take(&w, sg.bytes + std::max(kb, pad.bytes), stream, false))) return st;
+    if ((st = take(&w, sg.bytes + kb, stream, false))) return st;
     ms_record *r = nullptr;
     if (mask) {
         const bool again = !proj;
@@ -354,20 +302,15 @@ ms_status ms_gated_linear_forward(const ms_tensor *x, const ms_tensor *W, const 
         }
         if (proj) r->acct.saved_activation_bytes += ms_gated_projection_bytes(M, F, x->dtype);
         const bool dx = mask & MS_RG_INPUT, dw = mask & MS_RG_WEIGHT, db = mask & MS_RG_BIAS;
-        const size_t bb = std::max(ms::gated_dz_workspace(x->dtype, M, D, F, !again),
-                                   ms::linear_bwd_workspace(x->dtype, M, D, 2 * F, dx, dw, db));
-        r->acct.transient_workspace_bytes = al256((size_t)M * 2 * F * elt_size(x->dtype)) + std::max(bb, again ? pad.bytes : 0) +
+        r->acct.transient_workspace_bytes = ms::gated_bwd_workspace(x->dtype, M, D, F, place(x, ox), place(W, ow), bk, !again, dx, dw, db) +
                                             staging(y, true) + staging(x, again || dw) + staging(W, again || dx) +
                                             staging(x, dx) + staging(W, dw);
     }
     int err = stage_in(x, w.base, ox, stream);
     if (!err) err = stage_in(W, w.base, ow, stream);
-    const void *xk = kptr(x, w.base, ox), *wk = kptr(W, w.base, ow), *bk = b ? b->data : nullptr;
-    char *ws = w.base + sg.bytes;
-    if (!err) err = pad_run(pad, M, 2 * F, D, ws, &xk, &wk, &bk, stream);
     if (!err)
-        err = ms::launch_gated_fwd(x->dtype, M, pad.D8, F, activation, xk, wk, bk, kptr(y, w.base, oy), proj, ws,
-                                   stream);
+        err = ms::launch_gated_fwd(x->dtype, M, D, F, activation, kptr(x, w.base, ox), kptr(W, w.base, ow), bk, kptr(y, w.base, oy), proj,
+                                   w.base + sg.bytes, stream);
     if (!err) err = stage_out(y, w.base, oy, stream);
     if (err) {
         delete r;

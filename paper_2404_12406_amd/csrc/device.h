@@ -32,6 +32,9 @@ struct ConvGeom : ConvDims {
     // forwards and input gradients: none, they run unsplit): what the runtime falls
     // back to where the workspace cannot be had, and what it captures
     int lean = 0;
+    // the fp32 Linear contractions (1 x 1) take no more than the first *count of the N
+    // rows (their results past them are not written), a number on the device; null: all
+    const int *count = nullptr;
 };
 
 // y = W * x + b (b may be null).  May use conv_fwd_workspace() bytes of
@@ -148,26 +151,34 @@ size_t layer_norm_bwd_workspace(int dtype, int64_t M, int64_t D, bool params);
 int launch_layer_norm_bwd(int dtype, const void *x, const void *dy, const void *gamma, float eps, int64_t M, int64_t D, void *dx,
                           void *dgamma, void *dbeta, void *ws, void *stream);
 
-// dst[r][0 .. ld) = src[r][0 .. cols) and zeros (dst 16-byte aligned, ld whole vectors).
-int launch_pad_rows(int dtype, const void *src, int64_t rows, int64_t cols, void *dst, int64_t ld, void *stream);
+// dst[drows][dld] = src's first `rows` rows of `cols` columns (sld apart) and zeros
+// past them; columns past dld are left out.  At most kCopies at once.
+struct CopyJob {
+    const void *src;
+    int64_t sld, rows, cols;
+    void *dst;
+    int64_t drows, dld;
+};
+constexpr int kCopies = 5;
+int launch_copy_rows(int dtype, const CopyJob *jobs, int n, void *stream);
 
 // Gated linear unit y = act(z_g) z_u, z = x W^T + b [M][2F] (b may be null).
-// bf16 needs operands for which gated_rows_ok() (D a multiple of 8, aligned).
-// `proj` receives z where it is kept (else null): fp32, or for bf16 the leading
-// 24 bits of it, a plane [M][2F] of 16 and one of 8.  launch_gated_dz leaves the
-// gradient of z for that of y in dz, from proj or, where that is null, from z
-// computed again.
-bool gated_rows_ok(int64_t M, int64_t D, int64_t F, const void *x, const void *w, const void *b);
-size_t gated_fwd_workspace(int dtype, int64_t M, int64_t D, int64_t F, bool keep);
+// `proj` receives z where it is kept (else null): for bf16 the leading 24 bits of
+// fp32, a plane [M][2F] of 16 and one of 8; fp32 in rows of 2 F' (F' at most F
+// rounded up to 16).  The backward takes z from proj or, where that is null, again;
+// any of dx, dw, db may be null.  The workspaces go by the operands' alignment.
+size_t gated_fwd_workspace(int dtype, int64_t M, int64_t D, int64_t F, const void *x, const void *w, const void *b, bool keep);
 int launch_gated_fwd(int dtype, int64_t M, int64_t D, int64_t F, int act, const void *x, const void *w, const void *b, void *y,
                      void *proj, void *ws, void *stream);
-size_t gated_dz_workspace(int dtype, int64_t M, int64_t D, int64_t F, bool kept);
-int launch_gated_dz(int dtype, int64_t M, int64_t D, int64_t F, int act, const void *x, const void *w, const void *b,
-                    const void *proj, const void *dy, void *dz, void *ws, void *stream);
-// The gradients of a Linear x[M][K] -> [M][N] (any of dx, dw, db may be null).
+size_t gated_bwd_workspace(int dtype, int64_t M, int64_t D, int64_t F, const void *x, const void *w, const void *b, bool kept, bool dx,
+                           bool dw, bool db);
+int launch_gated_bwd(int dtype, int64_t M, int64_t D, int64_t F, int act, const void *x, const void *w, const void *b, const void *proj,
+                     const void *dy, void *dx, void *dw, void *db, void *ws, void *stream);
+// The gradients of a Linear x[M][K] -> [M][N] (any of dx, dw, db may be null); count:
+// as ConvGeom's.
 size_t linear_bwd_workspace(int dtype, int64_t M, int64_t K, int64_t N, bool dx, bool dw, bool db);
-int launch_linear_bwd(int dtype, int64_t M, int64_t K, int64_t N, const void *dy, const void *x, const void *w, void *dx, void *dw,
-                      void *db, void *ws, void *stream);
+int launch_linear_bwd(int dtype, int64_t M, int64_t K, int64_t N, const int *count, const void *dy, const void *x, const void *w,
+                      void *dx, void *dw, void *db, void *ws, void *stream);
 
 // Softmax cross entropy of the logits x[M][D] w[V][D]^T + b (b may be null) of the
 // rows whose target is not `ignore` (a target that is no word gives NaN).

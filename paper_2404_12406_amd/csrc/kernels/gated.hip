@@ -21,18 +21,26 @@ int gate_grad(int64_t M, int64_t D, int64_t F, int act, const void *x, const voi
               hipStream_t st);
 }  // namespace g2
 
+namespace tok {
+bool applies(int dtype, int64_t M, int64_t N, int64_t K, const void *x, const void *w);
+int gate(int dtype, int64_t M, int64_t D, int64_t F, int act, const void *x, const void *w, const void *b, void *y, void *proj,
+         hipStream_t st);
+}  // namespace tok
+
 namespace gated {
 
 // Rows of a block's y index, then every gridDim.y-th; a thread one vector of each.
-__global__ __launch_bounds__(256) void act_kernel(const float *__restrict__ z, int64_t M, int F, int kind, float *__restrict__ y) {
+// z has rows of 2 Fp, its halves at 0 and Fp.
+__global__ __launch_bounds__(256) void act_kernel(const float *__restrict__ z, int64_t M, int F, int Fp, int kind,
+                                                  float *__restrict__ y) {
     using T = float;
     constexpr int V = Vec16<T>::N;
     constexpr bool FAST = false;
     const int c = ((int)blockIdx.x * 256 + (int)threadIdx.x) * V;
     if (c >= F) return;
     for (int64_t r = blockIdx.y; r < M; r += gridDim.y) {
-        const T *zr = z + r * 2 * F;
-        const Vec16<T> g = load_vec(zr, c, F), u = load_vec(zr + F, c, F);
+        const T *zr = z + r * 2 * Fp;
+        const Vec16<T> g = load_vec(zr, c, F), u = load_vec(zr + Fp, c, F);
         Vec16<T> o;
 #pragma unroll
         for (int e = 0; e < V; ++e) o.e[e] = from_f32<T>(act::value<FAST>(kind, to_f32(g.e[e])) * to_f32(u.e[e]));
@@ -40,29 +48,31 @@ __global__ __launch_bounds__(256) void act_kernel(const float *__restrict__ z, i
     }
 }
 
-// dz may be z itself: a thread reads both halves of its columns before it writes them.
-__global__ __launch_bounds__(256) void grad_kernel(const float *z, const float *__restrict__ dy, int64_t M, int F, int kind,
+// dz may be z itself: a thread reads both halves of its columns before it writes
+// them.  Columns F .. Fp - 1 of both halves become zeros.
+__global__ __launch_bounds__(256) void grad_kernel(const float *z, const float *__restrict__ dy, int64_t M, int F, int Fp, int kind,
                                                    float *dz) {
     using T = float;
     constexpr int V = Vec16<T>::N;
     constexpr bool FAST = false;
     const int c = ((int)blockIdx.x * 256 + (int)threadIdx.x) * V;
-    if (c >= F) return;
+    if (c >= Fp) return;
     for (int64_t r = blockIdx.y; r < M; r += gridDim.y) {
-        const T *zr = z + r * 2 * F;
-        Vec16<T> g = load_vec(zr, c, F), u = load_vec(zr + F, c, F);
-        const Vec16<T> d = load_vec(dy + r * F, c, F);
+        const T *zr = z + r * 2 * Fp;
+        Vec16<T> g = load_vec(zr, c, Fp), u = load_vec(zr + Fp, c, Fp);
+        const Vec16<T> d = c < F ? load_vec(dy + r * F, c, F) : zero16<T>();
 #pragma unroll
         for (int e = 0; e < V; ++e) {
             float a, da;
             act::both<FAST>(kind, to_f32(g.e[e]), a, da);
             const float q = to_f32(d.e[e]);
-            g.e[e] = from_f32<T>(q * to_f32(u.e[e]) * da);
-            u.e[e] = from_f32<T>(q * a);
+            const bool in = c + e < F;
+            g.e[e] = in ? q * to_f32(u.e[e]) * da : 0.f;
+            u.e[e] = in ? q * a : 0.f;
         }
-        T *dr = dz + r * 2 * F;
-        store_vec(dr, c, F, g);
-        store_vec(dr + F, c, F, u);
+        T *dr = dz + r * 2 * Fp;
+        store_vec(dr, c, Fp, g);
+        store_vec(dr + Fp, c, Fp, u);
     }
 }
 
@@ -111,16 +121,22 @@ __global__ __launch_bounds__(256) void grad24_kernel(const uint16_t *__restrict_
     }
 }
 
-// dst[r][0 .. ld) = src[r][0 .. cols), then zeros
+// Up to kCopies copies at once (grid z): dst[r][0 .. dld) = src[r][0 .. cols) and
+// zeros for r < rows, zeros for r to drows (cols at most dld, or the other columns
+// are left out).
+struct Copies {
+    CopyJob job[kCopies];
+};
 template <typename T>
-__global__ __launch_bounds__(256) void pad_rows_kernel(const T *__restrict__ src, int64_t rows, int cols, T *__restrict__ dst, int ld) {
+__global__ __launch_bounds__(256) void copy_rows_kernel(const Copies k) {
     constexpr int V = Vec16<T>::N;
-    const int c = ((int)blockIdx.x * 256 + (int)threadIdx.x) * V;
-    if (c >= ld) return;
-    for (int64_t r = blockIdx.y; r < rows; r += gridDim.y) {
-        const Vec16<T> v = c < cols ? load_vec(src + r * cols, c, cols) : zero16<T>();
-        store16(dst + r * ld + c, v);
-    }
+    const CopyJob &j = k.job[blockIdx.z];
+    const T *src = (const T *)j.src;
+    T *dst = (T *)j.dst;
+    const int cols = (int)min(j.cols, j.dld), dld = (int)j.dld;
+    for (int64_t r = blockIdx.y; r < j.drows; r += gridDim.y)
+        for (int c = ((int)blockIdx.x * 256 + (int)threadIdx.x) * V; c < dld; c += (int)gridDim.x * 256 * V)
+            store_vec(dst + r * dld, c, dld, r < j.rows && c < cols ? load_vec(src + r * j.sld, c, cols) : zero16<T>());
 }
 
 namespace {
@@ -141,13 +157,14 @@ ConvGeom linear(int64_t M, int64_t K, int64_t N) {
 
 size_t al256(size_t n) { return (n + 255) / 256 * 256; }
 
-int run_act(const void *z, int64_t M, int64_t F, int kind, void *y, hipStream_t st) {
-    hipLaunchKernelGGL(act_kernel, grid(M, F, 4), dim3(256), 0, st, (const float *)z, M, (int)F, kind, (float *)y);
+int run_act(const void *z, int64_t M, int64_t F, int64_t Fp, int kind, void *y, hipStream_t st) {
+    hipLaunchKernelGGL(act_kernel, grid(M, F, 4), dim3(256), 0, st, (const float *)z, M, (int)F, (int)Fp, kind, (float *)y);
     return (int)hipGetLastError();
 }
 
-int run_grad(const void *z, const void *dy, int64_t M, int64_t F, int kind, void *dz, hipStream_t st) {
-    hipLaunchKernelGGL(grad_kernel, grid(M, F, 4), dim3(256), 0, st, (const float *)z, (const float *)dy, M, (int)F, kind, (float *)dz);
+int run_grad(const void *z, const void *dy, int64_t M, int64_t F, int64_t Fp, int kind, void *dz, hipStream_t st) {
+    hipLaunchKernelGGL(grad_kernel, grid(M, Fp, 4), dim3(256), 0, st, (const float *)z, (const float *)dy, M, (int)F, (int)Fp, kind,
+                       (float *)dz);
     return (int)hipGetLastError();
 }
 
@@ -157,63 +174,90 @@ int run_grad24(const void *z, const void *dy, int64_t M, int64_t F, int kind, vo
     return (int)hipGetLastError();
 }
 
+bool al(const void *p, uintptr_t n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; }
+
+// Zero-padded copies of operands that the contractions do not take, or take slowly:
+// bf16 rows of D values that are no whole 16-byte vectors, or not so aligned (the
+// copies have D rounded up to 8); for fp32, where D is no multiple of 4 or F is
+// odd, copies with D and F rounded up to 32 and 16 instead of the contractions'
+// 4-byte loads (1001 x 515 -> 2 x 1366, trained: 211 us with those, 165 with copies).
+// Few rows are not worth a copy of W.
+constexpr int64_t kPadRows = 96;
+
+struct Pads {
+    int64_t D, F;            // as the contractions see them
+    bool x, w, b, any;
+    size_t ox, ow, ob, bytes;
+};
+
+Pads pads(int dtype, int64_t M, int64_t D, int64_t F, const void *x, const void *w, const void *b) {
+    Pads p{D, F, false, false, false, false, 0, 0, 0, 0};
+    const size_t e = dtype == kBF16 ? 2 : 4;
+    if (dtype == kBF16) {
+        p.D = (D + 7) / 8 * 8;
+        p.x = p.D != D || !al(x, 16);
+        p.w = p.D != D || !al(w, 16);
+        p.b = b && !al(b, 4);
+    } else if (M >= kPadRows) {
+        if (D % 4 || F % 2) {
+            p.D = (D + 31) / 32 * 32;
+            p.F = (F + 15) / 16 * 16;
+        }
+        p.x = p.D != D || !al(x, 16);
+        p.w = p.D != D || p.F != F || !al(w, 16);
+        p.b = b && p.F != F;
+    }
+    p.any = p.D != D || p.F != F;
+    p.ow = p.x ? al256((size_t)M * p.D * e) : 0;
+    p.ob = p.ow + (p.w ? al256((size_t)2 * p.F * p.D * e) : 0);
+    p.bytes = p.ob + (p.b ? al256((size_t)2 * p.F * e) : 0);
+    return p;
+}
+
+// the copies, in `base`; x, w and b move to them
+int make_pads(const Pads &p, int dtype, int64_t M, int64_t D, int64_t F, char *base, const void **x, const void **w, const void **b,
+              void *stream) {
+    const size_t e = dtype == kBF16 ? 2 : 4;
+    CopyJob j[kCopies];
+    int n = 0;
+    if (p.x) {
+        j[n++] = {*x, D, M, D, base + p.ox, M, p.D};
+        *x = base + p.ox;
+    }
+    if (p.w) {
+        const char *s = static_cast<const char *>(*w);
+        for (int h = 0; h < 2; ++h) j[n++] = {s + (size_t)h * F * D * e, D, F, D, base + p.ow + (size_t)h * p.F * p.D * e, p.F, p.D};
+        *w = base + p.ow;
+    }
+    if (p.b) {
+        const char *s = static_cast<const char *>(*b);
+        for (int h = 0; h < 2; ++h) j[n++] = {s + (size_t)h * F * e, F, 1, F, base + p.ob + (size_t)h * p.F * e, 1, p.F};
+        *b = base + p.ob;
+    }
+    return launch_copy_rows(dtype, j, n, stream);
+}
+
 }  // namespace
 }  // namespace gated
 
-int launch_pad_rows(int dtype, const void *src, int64_t rows, int64_t cols, void *dst, int64_t ld, void *stream) {
-    if (rows == 0 || ld == 0) return 0;
+int launch_copy_rows(int dtype, const CopyJob *jobs, int n, void *stream) {
+    gated::Copies k{};
+    int64_t rows = 0, cols = 0;
+    int used = 0;
+    for (int i = 0; i < n; ++i) {
+        if (jobs[i].drows == 0 || jobs[i].dld == 0) continue;
+        k.job[used++] = jobs[i];
+        rows = std::max(rows, jobs[i].drows);
+        cols = std::max(cols, jobs[i].dld);
+    }
+    if (!used) return 0;
     hipStream_t st = (hipStream_t)stream;
-    if (dtype == kBF16)
-        hipLaunchKernelGGL(gated::pad_rows_kernel<bf16>, gated::grid(rows, ld, 8), dim3(256), 0, st, (const bf16 *)src, rows,
-                           (int)cols, (bf16 *)dst, (int)ld);
-    else
-        hipLaunchKernelGGL(gated::pad_rows_kernel<float>, gated::grid(rows, ld, 4), dim3(256), 0, st, (const float *)src, rows,
-                           (int)cols, (float *)dst, (int)ld);
+    const int V = dtype == kBF16 ? 8 : 4;
+    const int64_t gx = std::min<int64_t>((cols + 256 * V - 1) / (256 * V), 64);
+    const dim3 grid((unsigned)gx, (unsigned)std::max<int64_t>(1, std::min<int64_t>(rows, 4096 / gx)), (unsigned)used);
+    if (dtype == kBF16) hipLaunchKernelGGL(gated::copy_rows_kernel<bf16>, grid, dim3(256), 0, st, k);
+    else hipLaunchKernelGGL(gated::copy_rows_kernel<float>, grid, dim3(256), 0, st, k);
     return (int)hipGetLastError();
-}
-
-bool gated_rows_ok(int64_t M, int64_t D, int64_t F, const void *x, const void *w, const void *b) {
-    return g2::rows_ok(M, 2 * F, D, x, w) && (reinterpret_cast<uintptr_t>(b) & 3u) == 0;
-}
-
-// fp32: z where it is not kept, then the contraction's
-size_t gated_fwd_workspace(int dtype, int64_t M, int64_t D, int64_t F, bool keep) {
-    if (dtype == kBF16 || M == 0) return 0;
-    return (keep ? 0 : gated::al256((size_t)M * 2 * F * 4)) + conv_fwd_workspace(dtype, gated::linear(M, D, 2 * F));
-}
-
-int launch_gated_fwd(int dtype, int64_t M, int64_t D, int64_t F, int act, const void *x, const void *w, const void *b, void *y,
-                     void *proj, void *ws, void *stream) {
-    if (M == 0) return 0;
-    hipStream_t st = (hipStream_t)stream;
-    if (dtype == kBF16) {
-        if (!gated_rows_ok(M, D, F, x, w, b)) return (int)hipErrorInvalidValue;
-        return g2::gate_fwd(M, D, F, act, x, w, b, y, proj, st);
-    }
-    char *p = static_cast<char *>(ws);
-    void *z = proj ? proj : p;
-    if (!proj) p += gated::al256((size_t)M * 2 * F * 4);
-    const int err = launch_conv_fwd(dtype, gated::linear(M, D, 2 * F), x, w, b, z, p, stream);
-    return err ? err : gated::run_act(z, M, F, act, y, st);
-}
-
-// what launch_gated_dz itself needs: the fp32 contraction's
-size_t gated_dz_workspace(int dtype, int64_t M, int64_t D, int64_t F, bool kept) {
-    return dtype == kBF16 || kept || M == 0 ? 0 : conv_fwd_workspace(dtype, gated::linear(M, D, 2 * F));
-}
-
-int launch_gated_dz(int dtype, int64_t M, int64_t D, int64_t F, int act, const void *x, const void *w, const void *b,
-                    const void *proj, const void *dy, void *dz, void *ws, void *stream) {
-    if (M == 0) return 0;
-    hipStream_t st = (hipStream_t)stream;
-    if (proj)
-        return dtype == kBF16 ? gated::run_grad24(proj, dy, M, F, act, dz, st) : gated::run_grad(proj, dy, M, F, act, dz, st);
-    if (dtype == kBF16) {
-        if (!gated_rows_ok(M, D, F, x, w, b)) return (int)hipErrorInvalidValue;
-        return g2::gate_grad(M, D, F, act, x, w, b, dy, dz, st);
-    }
-    const int err = launch_conv_fwd(dtype, gated::linear(M, D, 2 * F), x, w, b, dz, ws, stream);
-    return err ? err : gated::run_grad(dz, dy, M, F, act, dz, st);
 }
 
 size_t linear_bwd_workspace(int dtype, int64_t M, int64_t K, int64_t N, bool dx, bool dw, bool db) {
@@ -225,15 +269,123 @@ size_t linear_bwd_workspace(int dtype, int64_t M, int64_t K, int64_t N, bool dx,
     return ws;
 }
 
-int launch_linear_bwd(int dtype, int64_t M, int64_t K, int64_t N, const void *dy, const void *x, const void *w, void *dx, void *dw,
-                      void *db, void *ws, void *stream) {
-    const ConvGeom g = gated::linear(M, K, N);
+int launch_linear_bwd(int dtype, int64_t M, int64_t K, int64_t N, const int *count, const void *dy, const void *x, const void *w,
+                      void *dx, void *dw, void *db, void *ws, void *stream) {
+    ConvGeom g = gated::linear(M, K, N);
+    g.count = count;
     bool done = false;
     int err = 0;
     if (dx) err = launch_conv_dgrad(dtype, g, dy, w, nullptr, dx, ws, stream, dw ? nullptr : db, &done);
     if (!err && dw) err = launch_conv_wgrad(dtype, g, dy, x, dw, db, ws, stream, &done);
     if (!err && db && !done) err = launch_colsum(dtype, dy, M, (int)N, db, ws, stream);
     return err;
+}
+
+// the copies, then (fp32) z where it is not kept and the contraction's workspace
+size_t gated_fwd_workspace(int dtype, int64_t M, int64_t D, int64_t F, const void *x, const void *w, const void *b, bool keep) {
+    if (M == 0) return 0;
+    const gated::Pads p = gated::pads(dtype, M, D, F, x, w, b);
+    if (dtype == kBF16) return p.bytes;
+    return p.bytes + (keep ? 0 : gated::al256((size_t)M * 2 * p.F * 4)) + conv_fwd_workspace(dtype, gated::linear(M, p.D, 2 * p.F));
+}
+
+int launch_gated_fwd(int dtype, int64_t M, int64_t D, int64_t F, int act, const void *x, const void *w, const void *b, void *y,
+                     void *proj, void *ws, void *stream) {
+    if (M == 0) return 0;
+    hipStream_t st = (hipStream_t)stream;
+    const gated::Pads p = gated::pads(dtype, M, D, F, x, w, b);
+    char *c = static_cast<char *>(ws);
+    int err = gated::make_pads(p, dtype, M, D, F, c, &x, &w, &b, stream);
+    if (err) return err;
+    // (p.F is F wherever the few rows' kernel applies)
+    if (tok::applies(dtype, M, 2 * F, p.D, x, w)) return tok::gate(dtype, M, p.D, F, act, x, w, b, y, proj, st);
+    if (dtype == kBF16) {
+        if (!g2::rows_ok(M, 2 * F, p.D, x, w)) return (int)hipErrorInvalidValue;
+        return g2::gate_fwd(M, p.D, F, act, x, w, b, y, proj, st);
+    }
+    c += p.bytes;
+    void *z = proj ? proj : c;
+    if (!proj) c += gated::al256((size_t)M * 2 * p.F * 4);
+    err = launch_conv_fwd(dtype, gated::linear(M, p.D, 2 * p.F), x, w, b, z, c, stream);
+    return err ? err : gated::run_act(z, M, F, p.F, act, y, st);
+}
+
+namespace gated {
+namespace {
+
+// Workspace of a backward: dz, the copies, padded gradients, the contractions'.
+struct Bwd {
+    Pads p;
+    size_t dz, pad, gx, gw, gb, work, bytes;
+};
+
+Bwd bwd_plan(int dtype, int64_t M, int64_t D, int64_t F, const void *x, const void *w, const void *b, bool kept, bool dx, bool dw, bool db) {
+    Bwd k{};
+    // bf16 contractions of the backward take any D themselves: copies only to take z again
+    k.p = dtype == kBF16 && kept ? Pads{D, F} : pads(dtype, M, D, F, x, w, b);
+    const bool f32 = dtype != kBF16;
+    const size_t e = f32 ? 4 : 2;
+    const int64_t Dp = f32 ? k.p.D : D, Fp = k.p.F;
+    k.dz = 0;
+    k.pad = al256((size_t)M * 2 * Fp * e);
+    k.gx = k.pad + k.p.bytes;
+    k.gw = k.gx + (f32 && dx && Dp != D ? al256((size_t)M * Dp * e) : 0);
+    k.gb = k.gw + (f32 && dw && k.p.any ? al256((size_t)2 * Fp * Dp * e) : 0);
+    k.work = k.gb + (f32 && db && Fp != F ? al256((size_t)2 * Fp * e) : 0);
+    size_t ws = linear_bwd_workspace(dtype, M, Dp, 2 * Fp, dx, dw, db);
+    if (f32 && !kept && M) ws = std::max(ws, conv_fwd_workspace(dtype, linear(M, Dp, 2 * Fp)));
+    k.bytes = k.work + ws;
+    return k;
+}
+
+}  // namespace
+}  // namespace gated
+
+size_t gated_bwd_workspace(int dtype, int64_t M, int64_t D, int64_t F, const void *x, const void *w, const void *b, bool kept, bool dx,
+                           bool dw, bool db) {
+    return gated::bwd_plan(dtype, M, D, F, x, w, b, kept, dx, dw, db).bytes;
+}
+
+int launch_gated_bwd(int dtype, int64_t M, int64_t D, int64_t F, int act, const void *x, const void *w, const void *b, const void *proj,
+                     const void *dy, void *dx, void *dw, void *db, void *ws, void *stream) {
+    hipStream_t st = (hipStream_t)stream;
+    const gated::Bwd k = gated::bwd_plan(dtype, M, D, F, x, w, b, proj != nullptr, dx, dw, db);
+    char *c = static_cast<char *>(ws);
+    void *dz = c + k.dz;
+    const void *xp = x, *wp = w, *bp = b;
+    // (a kept z leaves only the operands of the gradients asked for)
+    gated::Pads p = k.p;
+    if (proj) {
+        p.x = p.x && dw;
+        p.w = p.w && dx;
+        p.b = false;
+    }
+    int err = M ? gated::make_pads(p, dtype, M, D, F, c + k.pad, &xp, &wp, &bp, stream) : 0;
+    if (err) return err;
+    if (dtype == kBF16) {
+        if (M && proj) {
+            err = gated::run_grad24(proj, dy, M, F, act, dz, st);
+        } else if (M) {
+            if (!g2::rows_ok(M, 2 * F, k.p.D, xp, wp)) return (int)hipErrorInvalidValue;
+            err = g2::gate_grad(M, k.p.D, F, act, xp, wp, bp, dy, dz, st);
+        }
+        return err ? err : launch_linear_bwd(dtype, M, D, 2 * F, nullptr, dz, x, w, dx, dw, db, c + k.work, stream);
+    }
+    const int64_t Dp = k.p.D, Fp = k.p.F;
+    if (M && !proj) err = launch_conv_fwd(dtype, gated::linear(M, Dp, 2 * Fp), xp, wp, bp, dz, c + k.work, stream);
+    if (!err && M) err = gated::run_grad(proj ? proj : dz, dy, M, F, Fp, act, dz, st);
+    const bool tx = dx && Dp != D, tw = dw && k.p.any, tb = db && Fp != F;   // gradients by way of padded ones
+    char *gx = c + k.gx, *gw = c + k.gw, *gb = c + k.gb;
+    if (!err)
+        err = launch_linear_bwd(dtype, M, Dp, 2 * Fp, nullptr, dz, xp, wp, tx ? gx : dx, tw ? gw : dw, tb ? gb : db, c + k.work, stream);
+    CopyJob j[kCopies];
+    int n = 0;
+    if (tx) j[n++] = {gx, Dp, M, D, dx, M, D};
+    for (int h = 0; h < 2; ++h) {
+        if (tw) j[n++] = {gw + (size_t)h * Fp * Dp * 4, Dp, F, D, (float *)dw + (size_t)h * F * D, F, D};
+        if (tb) j[n++] = {gb + (size_t)h * Fp * 4, Fp, 1, F, (float *)db + (size_t)h * F, 1, F};
+    }
+    return err ? err : launch_copy_rows(dtype, j, n, stream);
 }
 
 }  // namespace ms

@@ -170,18 +170,30 @@ __global__ __launch_bounds__(256, OCC) void gemm_kernel(const Args P) {
         Kg = f.Rp * f.Sp * g.K;
         ntm = (M + BM - 1) / BM;
     }
+    int k_split = P.k_split, ntm_grid = P.ntm;
+    if (g.count) {   // the tiles (weight gradient: the steps) of those rows, spread as if they were all
+        const int c = __builtin_amdgcn_readfirstlane(*g.count);
+        if constexpr (MODE == kWgrad) {
+            Kg = min(Kg, c);
+            k_split = ((Kg + P.splits - 1) / P.splits + BK - 1) / BK * BK;
+        } else {
+            M = min(M, c);
+            ntm = ntm_grid = (M + BM - 1) / BM;
+            if ((int)blockIdx.x >= ntm_grid * P.ntn) return;
+        }
+    }
     int k_begin = 0, k_end = Kg;
     if (P.splits > 1) {
-        k_begin = min(Kg, zsplit * P.k_split);
-        k_end = min(Kg, k_begin + P.k_split);
+        k_begin = min(Kg, zsplit * k_split);
+        k_end = min(Kg, k_begin + k_split);
     }
     // XCD-aware tile order, 8 row tiles sharing each column sweep
     int tm, tn;
     {
-        const int lt = xcd_remap((int)blockIdx.x, P.ntm * P.ntn);
+        const int lt = xcd_remap((int)blockIdx.x, ntm_grid * P.ntn);
         const int GM = 8, per = GM * P.ntn;
         const int gid = lt / per, first = gid * GM;
-        const int gsz = min(P.ntm - first, GM);
+        const int gsz = min(ntm_grid - first, GM);
         const int r = lt - gid * per;
         tm = first + r % gsz;
         tn = r / gsz;

@@ -12,6 +12,9 @@
 //   kEpiStore     the weight gradient dz^T x over the rows that count, times a factor
 // The main loop is gemm_block_body.inc's.  Everything before the one rounding
 // of what is stored is in fp32.
+#include <cstdlib>
+#include <cstring>
+
 #include <hip/hip_ext.h>
 
 #include "gemm_bf16.h"
@@ -379,11 +382,23 @@ struct FusedPlan {
     int tile, splits;
 };
 
+// MEMSAVE_FUSED_TILE=<name> forces one tile where the table has it (a testing
+// knob); returns its index or -1.
+template <int NT>
+int forced_tile(const Tile (&tiles)[NT], int ntiles) {
+    const char *e = getenv("MEMSAVE_FUSED_TILE");
+    if (!e || !*e) return -1;
+    for (int t = 0; t < ntiles; ++t)
+        if (strcmp(tiles[t].name, e) == 0) return t;
+    return -1;
+}
+
 template <int NT>
 FusedPlan plan(const Tile (&tiles)[NT], int ntiles, long M, long N, long K, int max_splits) {
     FusedPlan p{0, 1};
     double best = 1e300;
-    for (int t = 0; t < ntiles; ++t)
+    const int forced = forced_tile(tiles, ntiles);
+    for (int t = std::max(forced, 0); t < (forced < 0 ? ntiles : forced + 1); ++t)
         for (int s = 1; s <= max_splits; ++s) {
             const double us = est_us(tiles[t], M, N, K, 1, s);
             if (us < best * 0.999) {
@@ -521,7 +536,8 @@ int xent_dx(int64_t M, int64_t D, int64_t V, int64_t ldz, const void *dz, const 
     // (a last, smaller piece runs with the splits of the others)
     FusedPlan p{0, splits};
     double best = 1e300;
-    for (int t = 0; t < 3; ++t) {
+    const int forced = forced_tile(kGradTiles, 3);
+    for (int t = std::max(forced, 0); t < (forced < 0 ? 3 : forced + 1); ++t) {
         const double us = est_us(kGradTiles[t], M, D, V, 1, splits);
         if (us < best) {
             best = us;

@@ -36,6 +36,13 @@ int xent_dw(int64_t M, int64_t D, int64_t Dr, int64_t V, int64_t ldz, const void
             const float *scale, void *dw, void *db, void *ws, hipStream_t st);
 }  // namespace g2
 
+namespace tok {
+bool applies(int dtype, int64_t M, int64_t N, int64_t K, const void *x, const void *w);
+size_t xent_workspace();
+int xent(int dtype, int64_t M, int64_t D, int64_t V, const void *x, const void *w, const void *b, const int64_t *target, int64_t ignore,
+         int reduction, float *loss, float *lse, void *ws, hipStream_t st);
+}  // namespace tok
+
 namespace xent {
 
 // The rows that count, in order: idx[i] the i-th, pos[r] its place or -1, tgt[i]
@@ -228,15 +235,15 @@ __global__ __launch_bounds__(256) void bias_kernel(const bf16 *__restrict__ dz, 
 }
 
 // ------------------------------------------------------------------ fp32 pieces
-// A piece's logits z[i][0 .. V), words v0 on: joins the row's statistics (those
+// A piece's logits z[i][0 .. V) in rows of ldz, words v0 on: joins the row's statistics (those
 // of the first piece start them) and takes the target's logit.  A block a row.
-__global__ __launch_bounds__(256) void lse_rows_kernel(const float *__restrict__ z, int V, int v0, const int *__restrict__ count,
+__global__ __launch_bounds__(256) void lse_rows_kernel(const float *__restrict__ z, int ldz, int V, int v0, const int *__restrict__ count,
                                                        const int *__restrict__ tgt, bool first, floatx2 *__restrict__ stat,
                                                        float *__restrict__ tlogit) {
     __shared__ floatx2 red[4];
     const int n = *count;
     for (int64_t i = blockIdx.x; i < n; i += gridDim.x) {
-        const float *zr = z + i * V;
+        const float *zr = z + i * ldz;
         float top = -INFINITY;
         for (int c = (int)threadIdx.x * 4; c < V; c += 1024) {
             const Vec16<float> v = load_vec(zr, c, V);
@@ -265,8 +272,8 @@ __global__ __launch_bounds__(256) void lse_rows_kernel(const float *__restrict__
     }
 }
 
-// z -> dz in place; the rows that do not count become zeros.
-__global__ __launch_bounds__(256) void grad_rows_kernel(float *__restrict__ z, int V, int v0, int64_t M, const int *__restrict__ count,
+// z -> dz in place; the rows that do not count and the columns past V become zeros.
+__global__ __launch_bounds__(256) void grad_rows_kernel(float *__restrict__ z, int ldz, int V, int v0, int64_t M, const int *__restrict__ count,
                                                         const int *__restrict__ tgt, const float *__restrict__ lse,
                                                         const float *__restrict__ scale) {
     const int n = *count;
@@ -275,14 +282,14 @@ __global__ __launch_bounds__(256) void grad_rows_kernel(float *__restrict__ z, i
         const bool in = i < n;
         const float l = in ? lse[i] : 0.f, sc = in ? scale[i] * factor : 0.f;
         const int t = in ? tgt[i] - v0 : -1;
-        for (int c = (int)threadIdx.x * 4; c < V; c += 1024) {
-            Vec16<float> v = load_vec(z + i * V, c, V);
+        for (int c = (int)threadIdx.x * 4; c < ldz; c += 1024) {
+            Vec16<float> v = load_vec(z + i * ldz, c, ldz);
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 const float p = exp_below(v.e[e], l) - (c + e == t ? 1.f : 0.f);
-                v.e[e] = in ? p * sc : 0.f;
+                v.e[e] = in && c + e < V ? p * sc : 0.f;
             }
-            store_vec(z + i * V, c, V, v);
+            store_vec(z + i * ldz, c, ldz, v);
         }
     }
 }
@@ -321,6 +328,22 @@ ConvGeom linear(int64_t M, int64_t K, int64_t N) {
     return g;
 }
 
+// fp32 contractions take 16-byte loads where widths are multiples of 4 and take
+// twice as long or more where they are not: from kPadRows rows on (fewer are not
+// worth a copy of W) such a piece runs on zero-padded copies of its rows of W and
+// its biases, as wide and as many as these say.
+constexpr int64_t kPadRows = 96;
+int64_t f32_width(int64_t M, int64_t D) { return M >= kPadRows && D % 4 ? (D + 31) / 32 * 32 : D; }
+int64_t f32_words(int64_t M, int64_t V) { return M >= kPadRows && V % 4 ? (V + 31) / 32 * 32 : V; }
+
+// A piece's operands as the contractions take them.
+struct Piece {
+    int64_t n, np;          // words, and columns of z
+    const float *w, *b;
+    float *dw, *db;         // the gradients' places, padded or the caller's
+    bool own;               // padded
+};
+
 // Workspace of a call, carved in order.
 struct Carve {
     char *base;
@@ -346,13 +369,12 @@ struct Rows {
 
 Rows carve_rows(Carve &c, int dtype, int64_t M, int64_t D, int64_t V, bool padw, bool padb) {
     Rows r{};
-    r.D8 = dtype == kBF16 ? (D + 7) / 8 * 8 : (D + 3) / 4 * 4;
+    r.D8 = dtype == kBF16 ? (D + 7) / 8 * 8 : f32_width(M, D);
     r.pos = c.get<int>(M);
     r.idx = c.get<int>(M);
     r.tgt = c.get<int>(M);
     r.count = c.get<int>(1);
-    if (dtype != kBF16) r.D8 = D;
-    r.xc = c.raw((size_t)M * ((D + 7) / 8 * 8) * (dtype == kBF16 ? 2 : 4));
+    r.xc = c.raw((size_t)M * r.D8 * (dtype == kBF16 ? 2 : 4));
     r.wp = padw ? c.raw((size_t)V * r.D8 * 2) : nullptr;
     r.bp = padb ? c.raw((size_t)((V + 7) / 8 * 8) * 2) : nullptr;
     return r;
@@ -362,7 +384,8 @@ struct Fwd {
     Rows r;
     void *stat;
     float *tlogit, *each;
-    float *z;      // fp32: a piece's logits
+    float *z;      // fp32: a piece's logits,
+    float *wp, *bp;   // its padded operands
     void *conv;    // and the contraction's workspace
 };
 
@@ -373,9 +396,13 @@ Fwd carve_fwd(Carve &c, int dtype, int64_t M, int64_t D, int64_t V, bool padw, b
     f.tlogit = c.get<float>(M);
     f.each = each ? c.get<float>(M) : nullptr;
     if (dtype != kBF16) {
-        const int64_t p = piece(dtype, M, V), last = V - (V - 1) / p * p;
-        f.z = c.get<float>(M * p);
-        f.conv = c.raw(std::max(conv_fwd_workspace(dtype, linear(M, D, p)), conv_fwd_workspace(dtype, linear(M, D, last))));
+        const int64_t p = piece(dtype, M, V), last = V - (V - 1) / p * p, most = std::max(f32_words(M, p), f32_words(M, last));
+        f.z = c.get<float>(M * most);
+        f.wp = M >= kPadRows ? c.get<float>(most * f.r.D8) : nullptr;
+        f.bp = M >= kPadRows ? c.get<float>(most) : nullptr;
+        size_t ws = 0;
+        for (int64_t v : {p, last}) ws = std::max(ws, conv_fwd_workspace(dtype, linear(M, f.r.D8, f32_words(M, v))));
+        f.conv = c.raw(ws);
     }
     return f;
 }
@@ -385,6 +412,7 @@ struct Bwd {
     float *lse, *scale;
     void *dz;
     float *part;     // partials of dx (fp32: the sum and a piece's)
+    float *wp, *bp, *gwp, *gbp;   // fp32: a piece's padded operands and gradients
     void *work;      // the contractions' workspace
     int splits;
 };
@@ -395,20 +423,27 @@ Bwd carve_bwd(Carve &c, int dtype, int64_t M, int64_t D, int64_t V, bool padw, b
     b.lse = c.get<float>(M);
     b.scale = c.get<float>(M + 1);
     const int64_t p = piece(dtype, M, V), last = V - (V - 1) / p * p;
-    b.dz = c.raw((size_t)M * ((p + 7) / 8 * 8) * (dtype == kBF16 ? 2 : 4));
+    const int64_t most = dtype == kBF16 ? (p + 7) / 8 * 8 : std::max(f32_words(M, p), f32_words(M, last));
+    b.dz = c.raw((size_t)M * most * (dtype == kBF16 ? 2 : 4));
+    if (dtype != kBF16 && M >= kPadRows) {
+        b.wp = c.get<float>(most * b.r.D8);
+        b.bp = c.get<float>(most);
+        b.gwp = dw ? c.get<float>(most * b.r.D8) : nullptr;
+        b.gbp = db ? c.get<float>(most) : nullptr;
+    }
     b.splits = 1;
     size_t ws = 0;
     for (int64_t v : {p, last}) {
         if (dtype == kBF16) {
             if (dw) ws = std::max(ws, g2::xent_dw_workspace(M, b.r.D8, D, v, db));
         } else {
-            ws = std::max(ws, conv_fwd_workspace(dtype, linear(M, D, v)));
-            ws = std::max(ws, linear_bwd_workspace(dtype, M, D, v, dx, dw, db));
+            ws = std::max(ws, conv_fwd_workspace(dtype, linear(M, b.r.D8, f32_words(M, v))));
+            ws = std::max(ws, linear_bwd_workspace(dtype, M, b.r.D8, f32_words(M, v), dx, dw, db));
         }
     }
     if (dx) {
         if (dtype == kBF16) b.splits = M ? g2::xent_dx_splits(M, b.r.D8, p) : 1;
-        b.part = c.get<float>((dtype == kBF16 ? b.splits : p < V ? 2 : 1) * M * ((D + 7) / 8 * 8));
+        b.part = c.get<float>((dtype == kBF16 ? b.splits : p < V ? 2 : 1) * M * b.r.D8);
     }
     b.work = c.raw(ws);
     return b;
@@ -428,15 +463,42 @@ int start(const Rows &r, int dtype, int64_t M, int64_t D, int64_t V, const void 
         hipLaunchKernelGGL(gather_kernel<float>, dim3(row_grid(M)), dim3(256), 0, st, (const float *)x, r.idx, r.count, M, (int)D,
                            (int)r.D8, true, (float *)r.xc, lse, gloss, reduction, lsec, scale);
     int err = (int)hipGetLastError();
-    if (!err && r.wp) {
-        err = launch_pad_rows(kBF16, *w, V, D, r.wp, r.D8, st);
+    CopyJob j[kCopies];
+    int n = 0;
+    if (r.wp) {
+        j[n++] = {*w, D, V, D, r.wp, V, r.D8};
         *w = r.wp;
     }
-    if (!err && r.bp && *b) {
-        err = launch_pad_rows(kBF16, *b, 1, V, r.bp, (V + 7) / 8 * 8, st);
+    if (r.bp && *b) {
+        j[n++] = {*b, V, 1, V, r.bp, 1, V};
         *b = r.bp;
     }
+    if (!err) err = launch_copy_rows(kBF16, j, n, st);
     return err;
+}
+
+// fp32: the words v0 .. v0 + n - 1, their operands copied where they are to be padded.
+int take_piece(Piece *q, int64_t M, int64_t D, int64_t D8, int64_t v0, int64_t n, const void *w, const void *b, float *wp, float *bp,
+               hipStream_t st) {
+    q->n = n;
+    q->np = f32_words(M, n);
+    q->w = (const float *)w + v0 * D;
+    q->b = b ? (const float *)b + v0 : nullptr;
+    q->own = wp && (q->np != n || D8 != D || (reinterpret_cast<uintptr_t>(q->w) & 15u));
+    if (!q->own) return 0;
+    CopyJob j[kCopies] = {{q->w, D, n, D, wp, q->np, D8}};
+    q->w = wp;
+    if (b) {
+        j[1] = {q->b, n, 1, n, bp, 1, q->np};
+        q->b = bp;
+    }
+    return launch_copy_rows(kF32, j, b ? 2 : 1, st);
+}
+
+int logits(const Piece &q, const Rows &r, int64_t M, float *z, void *ws, hipStream_t st) {
+    ConvGeom g = linear(M, r.D8, q.np);
+    g.count = r.count;
+    return launch_conv_fwd(kF32, g, r.xc, q.w, q.b, z, ws, st);
 }
 
 }  // namespace
@@ -445,13 +507,14 @@ int start(const Rows &r, int dtype, int64_t M, int64_t D, int64_t V, const void 
 size_t xent_fwd_workspace(int dtype, int64_t M, int64_t D, int64_t V, bool padw, bool padb, int reduction) {
     xent::Carve c{nullptr};
     xent::carve_fwd(c, dtype, M, D, V, padw, padb, reduction != 2);
-    return c.off;
+    return std::max(c.off, tok::xent_workspace());
 }
 
 int launch_xent_fwd(int dtype, int64_t M, int64_t D, int64_t V, const void *x, const void *w, const void *b, bool padw, bool padb,
                     const int64_t *target, int64_t ignore, int reduction, float *loss, float *lse, void *ws, void *stream) {
     using namespace xent;
     hipStream_t st = (hipStream_t)stream;
+    if (tok::applies(dtype, M, V, D, x, w)) return tok::xent(dtype, M, D, V, x, w, b, target, ignore, reduction, loss, lse, ws, st);
     Carve c{static_cast<char *>(ws)};
     const Fwd f = carve_fwd(c, dtype, M, D, V, padw, padb, reduction != 2);
     int err = start(f.r, dtype, M, D, V, x, &w, &b, target, ignore, nullptr, nullptr, reduction, nullptr, nullptr, st);
@@ -466,11 +529,12 @@ int launch_xent_fwd(int dtype, int64_t M, int64_t D, int64_t V, const void *x, c
         const int64_t p = piece(dtype, M, V);
         for (int64_t v0 = 0; v0 < V && !err; v0 += p) {
             const int64_t n = std::min(p, V - v0);
-            err = launch_conv_fwd(dtype, linear(M, D, n), f.r.xc, (const float *)w + v0 * D, b ? (const float *)b + v0 : nullptr, f.z,
-                                  f.conv, stream);
+            Piece q;
+            err = take_piece(&q, M, D, f.r.D8, v0, n, w, b, f.wp, f.bp, st);
+            if (!err) err = logits(q, f.r, M, f.z, f.conv, st);
             if (err) break;
-            hipLaunchKernelGGL(lse_rows_kernel, dim3(row_grid(M)), dim3(256), 0, st, f.z, (int)n, (int)v0, f.r.count, f.r.tgt, v0 == 0,
-                               (floatx2 *)f.stat, f.tlogit);
+            hipLaunchKernelGGL(lse_rows_kernel, dim3(row_grid(M)), dim3(256), 0, st, f.z, (int)q.np, (int)n, (int)v0, f.r.count, f.r.tgt,
+                               v0 == 0, (floatx2 *)f.stat, f.tlogit);
             err = (int)hipGetLastError();
         }
     }
@@ -519,21 +583,29 @@ int launch_xent_bwd(int dtype, int64_t M, int64_t D, int64_t V, const void *x, c
                 err = (int)hipGetLastError();
             }
         } else {
-            const float *wv = (const float *)w + v0 * D;
             float *z = (float *)k.dz, *tmp = k.part + (v0 > 0 ? M * D8 : 0);
-            if (M > 0) {
-                err = launch_conv_fwd(dtype, linear(M, D, n), k.r.xc, wv, b ? (const float *)b + v0 : nullptr, z, k.work, stream);
+            float *dwv = dw ? (float *)dw + v0 * D : nullptr, *dbv = db ? (float *)db + v0 : nullptr;
+            Piece q;
+            err = take_piece(&q, M, D, D8, v0, n, w, b, k.wp, k.bp, st);
+            if (!err && M > 0) {
+                err = logits(q, k.r, M, z, k.work, st);
                 if (err) break;
-                hipLaunchKernelGGL(grad_rows_kernel, dim3(row_grid(M)), dim3(256), 0, st, z, (int)n, (int)v0, M, k.r.count, k.r.tgt, k.lse,
-                                   k.scale);
+                hipLaunchKernelGGL(grad_rows_kernel, dim3(row_grid(M)), dim3(256), 0, st, z, (int)q.np, (int)n, (int)v0, M, k.r.count,
+                                   k.r.tgt, k.lse, k.scale);
                 err = (int)hipGetLastError();
             }
+            const bool tw = dw && (q.np != n || D8 != D), tb = db && q.np != n;
             if (!err)
-                err = launch_linear_bwd(dtype, M, D, n, z, k.r.xc, wv, dx && M > 0 ? tmp : nullptr, dw ? (float *)dw + v0 * D : nullptr,
-                                        db ? (float *)db + v0 : nullptr, k.work, stream);
+                err = launch_linear_bwd(dtype, M, D8, q.np, k.r.count, z, k.r.xc, q.w, dx && M > 0 ? tmp : nullptr, tw ? k.gwp : dwv,
+                                        tb ? k.gbp : dbv, k.work, stream);
+            CopyJob j[kCopies];
+            int jobs = 0;
+            if (tw) j[jobs++] = {k.gwp, D8, n, D, dwv, n, D};
+            if (tb) j[jobs++] = {k.gbp, n, 1, n, dbv, 1, n};
+            if (!err) err = launch_copy_rows(kF32, j, jobs, stream);
             if (!err && dx && v0 > 0 && M > 0) {
-                hipLaunchKernelGGL(add_kernel, dim3((unsigned)std::min<int64_t>((M * D + 1023) / 1024, 4096)), dim3(256), 0, st, k.part,
-                                   tmp, M * D);
+                hipLaunchKernelGGL(add_kernel, dim3((unsigned)std::min<int64_t>((M * D8 + 1023) / 1024, 4096)), dim3(256), 0, st, k.part,
+                                   tmp, M * D8);
                 err = (int)hipGetLastError();
             }
         }
