@@ -419,68 +419,121 @@ def _dropout_forward(lib, spec, x, y, mask):
     return h
 
 
-class _BlockCall:
-    """The forward call of a block layer with its C descriptors and buffers."""
+# Block layers are called for single tokens, where the host's time is all there
+# is: their tensors go to C as packed bytes (no MsTensor object), through function
+# objects of their own whose pointer arguments take them.
+def _packed(t: Optional[torch.Tensor]) -> Optional[bytes]:
+    """The bytes of tensor_desc(t)."""
+    if t is None:
+        return None
+    dt = _DT.get(t.dtype)
+    if dt is None:
+        raise TypeError(f"unsupported dtype {t.dtype}; use float32 or bfloat16")
+    shape, stride = t.shape, t.stride()
+    if len(shape) == 2:
+        return _TENSOR.pack(t.data_ptr(), dt, 2, shape[0], shape[1], 0, 0, 0, stride[0], stride[1], 0, 0, 0)
+    if len(shape) == 1:
+        return _TENSOR.pack(t.data_ptr(), dt, 1, shape[0], 0, 0, 0, 0, stride[0], 0, 0, 0, 0)
+    return bytes(tensor_desc(t))
 
-    def __init__(self, spec, x, W, b, mask, y):
-        if x.dim() != 2:
-            raise ValueError(f"{type(spec).__name__} takes x[M, D]; got {x.dim()} dims")
-        _on_gpu(x, W, b, y)
-        self.spec, self.mask = spec, int(mask)
-        self.kept = {}   # what the record borrows besides x, W and b
-        if isinstance(spec, GatedLinear):
-            if spec.act not in _lib.MS_ACT:
-                raise ValueError(f"unknown activation {spec.act!r}")
-            if spec.keep not in ("projections", "input"):
-                raise ValueError(f"keep is \"projections\" or \"input\"; got {spec.keep!r}")
-            if W is None or W.dim() != 2:
-                raise TypeError("GatedLinear needs W[2F, D]")
-            if self.mask and spec.keep == "projections":
-                n = _lib.load().ms_gated_projection_bytes(x.shape[0], W.shape[0] // 2, _DT.get(x.dtype, 0))
-                # (an empty buffer has no address: no rows, nothing to keep)
-                self.kept["projections"] = torch.empty(n, dtype=torch.uint8, device=x.device)
-            elif self.mask and b is not None:
-                self.kept["b"] = b
-        xent = isinstance(spec, LinearCrossEntropy)
-        if xent:
-            t = spec.target
-            if spec.reduction not in _lib.MS_REDUCE:
-                raise ValueError(f"reduction is \"mean\", \"sum\" or \"none\"; got {spec.reduction!r}")
-            if W is None or W.dim() != 2:
-                raise TypeError("LinearCrossEntropy needs W[V, D]")
-            if t.dtype != torch.int64:
-                raise TypeError(f"target must be int64, got {t.dtype}")
-            if t.shape != (x.shape[0],):
-                raise ValueError("target must have one element a row of x")
-            _on_gpu(x, t)
-            t = t.contiguous()
-            lse = torch.empty(x.shape[0] if self.mask else 0, dtype=torch.float32, device=x.device)
-            self._target, self._lse = (t.data_ptr() or None, lse.data_ptr() or None) if t.numel() else (None, None)
-            self._kept_target = t
-            if self.mask:
-                self.kept.update(lse=lse, target=t)
-                if b is not None:
-                    self.kept["b"] = b
+
+_block_fns = {}
+
+
+def _block_fn(name: str):
+    """The C function `name`, taking pointers as void pointers."""
+    f = _block_fns.get(name)
+    if f is None:
+        lib = _lib.load()
+        f = lib[name]
+        args = []
+        for a in getattr(lib, name).argtypes:
+            args.append(ctypes.c_void_p if a in (_lib._T, ctypes.POINTER(ctypes.c_void_p)) else a)
+        f.argtypes, f.restype = args, ctypes.c_int
+        _block_fns[name] = f
+    return f
+
+
+_current_device = torch._C._cuda_getDevice if hasattr(torch._C, "_cuda_getDevice") else torch.cuda.current_device
+
+
+def _one_gpu(x, *ts):
+    """As _on_gpu, for tensors that usually are where they should be."""
+    d = x.get_device()
+    for t in ts:
+        if t is not None and t.get_device() != d:
+            return _on_gpu(x, *ts)
+    if d < 0 or _current_device() != d:
+        _on_gpu(x, *ts)
+
+
+def _block_call(spec, x, W, b, mask, y):
+    """The forward call of a block layer: (y, C function's name, its arguments up
+    to the record, what the record borrows besides x and W by name, what else has
+    to live until the call)."""
+    if x.dim() != 2:
+        raise ValueError(f"{type(spec).__name__} takes x[M, D]; got {x.dim()} dims")
+    _one_gpu(x, W, b, y)
+    if isinstance(spec, LayerNorm):
         if y is None:
-            y = torch.empty(output_shape(spec, x, W), dtype=torch.float32 if xent else x.dtype, device=x.device)
-        self.y = y
-        self._d = [tensor_desc(t) for t in (x, W, b, self.y)]
-        self._p = [_ptr(d) for d in self._d]
-        proj = self.kept.get("projections")
-        self._proj = None if proj is None or proj.numel() == 0 else proj.data_ptr()
+            y = torch.empty_like(x) if x.is_contiguous() else torch.empty(x.shape, dtype=x.dtype, device=x.device)
+        return y, "ms_layer_norm_forward", (_packed(x), _packed(W), _packed(b), spec.eps, mask, _packed(y)), None, None
+    if W is None or W.dim() != 2:
+        raise TypeError(f"{type(spec).__name__} needs a weight of two dims")
+    kept = {}
+    if isinstance(spec, GatedLinear):
+        act = _lib.MS_ACT.get(spec.act)
+        if act is None:
+            raise ValueError(f"unknown activation {spec.act!r}")
+        if spec.keep not in ("projections", "input"):
+            raise ValueError(f"keep is \"projections\" or \"input\"; got {spec.keep!r}")
+        proj = None
+        if mask and spec.keep == "projections":
+            n = _lib.load().ms_gated_projection_bytes(x.shape[0], W.shape[0] // 2, _DT.get(x.dtype, 0))
+            buf = kept["projections"] = torch.empty(n, dtype=torch.uint8, device=x.device)
+            proj = buf.data_ptr() or None   # (no rows, nothing to keep)
+        elif mask and b is not None:
+            kept["b"] = b
+        if y is None:
+            y = torch.empty((x.shape[0], W.shape[0] // 2), dtype=x.dtype, device=x.device)
+        return y, "ms_gated_linear_forward", (_packed(x), _packed(W), _packed(b), act, proj, mask, _packed(y)), kept, None
+    red = _lib.MS_REDUCE.get(spec.reduction)
+    if red is None:
+        raise ValueError(f"reduction is \"mean\", \"sum\" or \"none\"; got {spec.reduction!r}")
+    t = spec.target
+    if t.dtype != torch.int64:
+        raise TypeError(f"target must be int64, got {t.dtype}")
+    if t.shape != x.shape[:1]:
+        raise ValueError("target must have one element a row of x")
+    _one_gpu(x, t)
+    t = t.contiguous()
+    lse = None
+    if mask:
+        lse = kept["lse"] = torch.empty(x.shape[0], dtype=torch.float32, device=x.device)
+        kept["target"] = t
+        if b is not None:
+            kept["b"] = b
+    if y is None:
+        y = torch.empty(x.shape[0] if red == 2 else 1, dtype=torch.float32, device=x.device)
+    args = (_packed(x), _packed(W), _packed(b), t.data_ptr() or None, int(spec.ignore_index), red,
+            (lse.data_ptr() or None) if lse is not None else None, mask, _packed(y))
+    return y, "ms_cross_entropy_forward", args, kept, t
 
-    def __call__(self, lib, h, stream):
-        px, pw, pb, py = self._p
-        spec = self.spec
-        if isinstance(spec, LayerNorm):
-            check(lib.ms_layer_norm_forward(px, pw, pb, float(spec.eps), self.mask, py, h, stream),
-                  "ms_layer_norm_forward")
-        elif isinstance(spec, LinearCrossEntropy):
-            check(lib.ms_cross_entropy_forward(px, pw, pb, self._target, int(spec.ignore_index), _lib.MS_REDUCE[spec.reduction],
-                                               self._lse, self.mask, py, h, stream), "ms_cross_entropy_forward")
-        else:
-            check(lib.ms_gated_linear_forward(px, pw, pb, _lib.MS_ACT[spec.act], self._proj, self.mask, py, h, stream),
-                  "ms_gated_linear_forward")
+
+def _block_backward(rec, grad_y, grad_x, grad_W, grad_b):
+    """layer_backward for a block layer's record."""
+    _one_gpu(grad_y, grad_x, grad_W, grad_b)
+    m = rec.mask
+    out = []
+    for bit, g, meta in ((MASK_INPUT, grad_x, rec._x_meta), (MASK_WEIGHT, grad_W, rec._w_meta), (MASK_BIAS, grad_b, rec._b_meta)):
+        if m & bit and g is None:   # (the loss of a cross entropy has a dtype of its own)
+            g = grad_y.new_empty(meta[0]) if meta[1] == grad_y.dtype else torch.empty(meta[0], dtype=meta[1], device=grad_y.device)
+        out.append(g)
+    check(_block_fn("ms_layer_backward")(rec._h, _packed(grad_y), _packed(out[0]), _packed(out[1]), _packed(out[2]),
+                                         _stream(grad_y.device)), "ms_layer_backward")
+    rec.consumed = True
+    rec.release_refs()
+    return tuple(out)
 
 
 def layer_forward(spec, x: torch.Tensor, W: Optional[torch.Tensor] = None, b: Optional[torch.Tensor] = None,
@@ -490,11 +543,14 @@ def layer_forward(spec, x: torch.Tensor, W: Optional[torch.Tensor] = None, b: Op
     bit gets a fresh 1-bit mask buffer, owned by its record."""
     lib = _lib.load()
     if isinstance(spec, _BLOCKS):
-        call, h = _BlockCall(spec, x, W, b, mask, y), ctypes.c_void_p()
-        call(lib, ctypes.byref(h), _stream(x.device))
+        y, name, args, kept, _alive = _block_call(spec, x, W, b, int(mask), y)
+        h = ctypes.c_void_p()
+        status = _block_fn(name)(*args, ctypes.byref(h), _stream(x.device))
+        if status:
+            check(status, name)
         if not h.value:
-            return call.y, None
-        return call.y, Record(h, _BlockDesc(spec), x, W, b, tuple(call.y.shape), call.y, extra=call.kept)
+            return y, None
+        return y, Record(h, _BlockDesc(spec), x, W, b, tuple(y.shape), y, extra=kept)
     if isinstance(spec, ReLU):
         if W is not None or b is not None:
             raise TypeError("ReLU takes no W or b")
@@ -536,21 +592,20 @@ def layer_backward(rec: Record, grad_y: torch.Tensor, grad_x: Optional[torch.Ten
     """Write exactly the requested gradients; return (grad_x, grad_W, grad_b)
     with None for every gradient the record's mask does not request.
     Gradient buffers not passed in are allocated here."""
+    if rec._block:
+        return _block_backward(rec, grad_y, grad_x, grad_W, grad_b)
     lib = _lib.load()
     _on_gpu(grad_y, grad_x, grad_W, grad_b)
     m = rec.mask
     if m & MASK_INPUT and grad_x is None:
         if rec._elementwise:   # memory order: the gradient in x's layout
             grad_x = torch.empty_strided(rec._x_meta[0], rec._x_meta[3], dtype=grad_y.dtype, device=grad_y.device)
-        elif rec._block:       # (the loss of a cross entropy has a dtype of its own)
-            grad_x = torch.empty(rec._x_meta[0], dtype=rec._x_meta[1], device=grad_y.device)
         else:
             grad_x = empty_like_layout(rec._x_meta[0], grad_y)
     if m & MASK_WEIGHT and grad_W is None:
-        grad_W = (torch.empty(rec._w_meta[0], dtype=rec._w_meta[1], device=grad_y.device) if rec._block
-                  else empty_like_layout(rec._w_meta[0], grad_y))
+        grad_W = empty_like_layout(rec._w_meta[0], grad_y)
     if m & MASK_BIAS and grad_b is None:
-        grad_b = torch.empty(rec._b_meta[0], dtype=rec._b_meta[1], device=grad_y.device)
+        grad_b = torch.empty(rec._b_meta[0], dtype=grad_y.dtype, device=grad_y.device)
     gy, gx, gw, gb = tensor_desc(grad_y), tensor_desc(grad_x), tensor_desc(grad_W), tensor_desc(grad_b)
     st = lib.ms_layer_backward(rec._h, _ptr(gy), _ptr(gx), _ptr(gw), _ptr(gb), _stream(grad_y.device))
     check(st, "ms_layer_backward")
@@ -618,10 +673,10 @@ class PreparedLayer:
         extra = (spec.running_mean, spec.running_var) if isinstance(spec, BatchNormEval) else ()
         _on_gpu(x, W, b, y, grad_y, grad_x, grad_W, grad_b, *extra)
         self.lib = _lib.load()
-        self.block = _BlockCall(spec, x, W, b, mask, y) if isinstance(spec, _BLOCKS) else None
+        self.block = None
+        if isinstance(spec, _BLOCKS):
+            y, *self.block = _block_call(spec, x, W, b, int(mask), y)
         self.desc = _BlockDesc(spec) if self.block else _LayerDesc(spec)
-        if self.block:
-            y = self.block.y
         if y is None:
             y = torch.empty_like(x) if isinstance(spec, (ReLU, Dropout)) else empty_like_layout(output_shape(spec, x, W), x)
         self.tensors = (x, W, b, y, grad_y, grad_x, grad_W, grad_b)
@@ -645,7 +700,8 @@ class PreparedLayer:
             self._free(self._h)
             self._h.value = None
         if self.block:
-            self.block(self.lib, self._hp, self._stream)
+            name, args = self.block[:2]
+            check(_block_fn(name)(*args, self._hp, self._stream), name)
             return
         if self.relu:
             bits = ctypes.c_void_p(self.bits.data_ptr() if self.bits is not None and self.bits.numel() else None)

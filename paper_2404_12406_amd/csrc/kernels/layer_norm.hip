@@ -20,6 +20,9 @@
 //    by finalize_kernel.
 //  * rows of any width and alignment take 16-byte accesses; only a row's last,
 //    incomplete vector goes element by element.
+// Measured: 16384 x 4096 bf16, forward 48 us (5.6 TB/s), input gradient 81 us (5.0
+// TB/s), where a large copy reaches 5.1; 8192 x 768, all gradients: 9.2, 13.5 and
+// 4.0 us, of which some 3 each are a launch's own time and the rest latency.
 #include <algorithm>
 
 #include "block_math.h"
@@ -27,10 +30,19 @@
 namespace ms {
 namespace ln {
 
+// The sum over a wave, by moves within the vector registers (an exchange through
+// LDS takes some 60 clocks a step, and a row's sums are a chain of 24 steps).
 __device__ __forceinline__ float wave_sum(float v) {
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o);
-    return v;
+    auto add = [&](float m) __attribute__((always_inline)) { v += m; };
+#define LN_MOVED(ctrl, rows) __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), ctrl, rows, 0xf, false))
+    add(LN_MOVED(0x111, 0xf));   // from 1, 2, 4 and 8 lanes below, within rows of 16
+    add(LN_MOVED(0x112, 0xf));
+    add(LN_MOVED(0x114, 0xf));
+    add(LN_MOVED(0x118, 0xf));
+    add(LN_MOVED(0x142, 0xa));   // the rows before
+    add(LN_MOVED(0x143, 0xc));
+#undef LN_MOVED
+    return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), 63));
 }
 
 // Sums of N values over the TPR threads of a row.  More than one wave: through
@@ -350,7 +362,9 @@ Plan plan(int dtype, int64_t M, int64_t D, bool params) {
     const int tpr = nvec <= 64 * kVecs ? 64 : nvec <= 256 * kVecs ? 256 : nvec <= 512 * 3 ? 512 : 0;
     if (!tpr) return {0, 0, (int)std::min<int64_t>(M, 2048)};
     const int64_t rows = tpr == 64 ? (M + 3) / 4 : M;
-    // parameter sums leave a partial row a block: two blocks of 256 threads a CU
+    // Parameter sums leave a partial row a block: two blocks of 256 threads a CU.
+    // 8192 x 768 bf16: 13.5 us and 4.0 for the sum of the partials; with four 13.6 and
+    // 6.6 (loading the next row ahead of the one worked on gave nothing, 14.0).
     const int64_t most = params ? (tpr == 512 ? 256 : 512) : 2048;
     return {tpr, (int)((nvec + tpr - 1) / tpr), (int)std::min(rows, most)};
 }

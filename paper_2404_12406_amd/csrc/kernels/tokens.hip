@@ -61,31 +61,30 @@ template <> struct Step<float> {
     }
 };
 
-// The sums of rows r0[t] .. + 15 of W (those below `rows`) with the rows of x, over
-// this wave's steps: lane l holds row 4 (l / 16) + v of tile t and row l % 16 of x.
-template <typename T>
-__device__ __forceinline__ void products(const Args &P, const int (&r0)[2], const int (&end)[2], int wave, int lane, floatx4 (&acc)[2]) {
+// Walks `groups` groups of two 16-row tiles of W, group i's tiles starting at rows
+// first + i stride (+ apart for the second) and ending at end[t]; after the last of
+// a group's steps done(i, acc) has the sums with the rows of x over this wave's
+// steps: lane l holds row 4 (l / 16) + v of tile t and row l % 16 of x.  The loads
+// run DEEP steps ahead, into the next group where this one ends.
+template <typename T, class Done>
+__device__ __forceinline__ void products(const Args &P, int first, int stride, int apart, const int (&end)[2], int groups, int wave,
+                                         int lane, Done done) {
     using S = Step<T>;
     const __amdgpu_buffer_rsrc_t rw = g2::rsrc(P.w, P.w_bytes), rx = g2::rsrc(P.x, P.x_bytes);
     const int g = lane >> 4, r16 = lane & 15;
-    uint32_t ow[2];
-    bool ok[2];
-#pragma unroll
-    for (int t = 0; t < 2; ++t) {
-        ok[t] = r0[t] + r16 < end[t];
-        ow[t] = (uint32_t)(r0[t] + r16) * (uint32_t)P.K;
-        acc[t] = floatx4{0.f, 0.f, 0.f, 0.f};
-    }
     const uint32_t ox = (uint32_t)min(r16, P.M - 1) * (uint32_t)P.K;
+    const int steps = ((P.K + S::K - 1) / S::K + KS - 1) / KS;   // of each wave (some past the end)
+    int li = 0, ls = 0;   // group and step to be loaded
     u32x4 fw[DEEP][2][2], fx[DEEP][2];
-    auto load = [&](int step, u32x4 (&w)[2][2], u32x4 (&x)[2]) __attribute__((always_inline)) {
+    auto load = [&](u32x4 (&w)[2][2], u32x4 (&x)[2]) __attribute__((always_inline)) {
 #pragma unroll
         for (int s = 0; s < 2; ++s) {
-            const int k = step * S::K + S::at(g, s);
-            const bool in = k < P.K;
+            const int k = (wave + ls * KS) * S::K + S::at(g, s);
+            const bool in = k < P.K && li < groups;
 #pragma unroll
             for (int t = 0; t < 2; ++t) {
-                const uint32_t off = in && ok[t] ? (ow[t] + (uint32_t)k) * (uint32_t)sizeof(T) : g2::kOOB;
+                const int row = first + li * stride + t * apart + r16;
+                const uint32_t off = in && row < end[t] ? ((uint32_t)row * (uint32_t)P.K + (uint32_t)k) * (uint32_t)sizeof(T) : g2::kOOB;
                 w[t][s] = __builtin_amdgcn_raw_buffer_load_b128(rw, (int)off, 0, 0);
             }
             const uint32_t off = in ? (ox + (uint32_t)k) * (uint32_t)sizeof(T) : g2::kOOB;
@@ -102,18 +101,30 @@ __device__ __forceinline__ void products(const Args &P, const int (&r0)[2], cons
                 }
             }
         }
+        if (++ls == steps) {
+            ls = 0;
+            ++li;
+        }
     };
-    const int steps = (P.K + S::K - 1) / S::K;
 #pragma unroll
-    for (int d = 0; d < DEEP; ++d) load(wave + d * KS, fw[d], fx[d]);
-    for (int i = wave; i < steps; i += KS * DEEP) {
+    for (int d = 0; d < DEEP; ++d) load(fw[d], fx[d]);
+    floatx4 acc[2] = {floatx4{0.f, 0.f, 0.f, 0.f}, floatx4{0.f, 0.f, 0.f, 0.f}};
+    int i = 0, s0 = 0;   // group and step worked on
+    while (i < groups) {
 #pragma unroll
         for (int d = 0; d < DEEP; ++d) {
+            if (i >= groups) break;
 #pragma unroll
             for (int s = 0; s < 2; ++s)
 #pragma unroll
                 for (int t = 0; t < 2; ++t) acc[t] = S::mac(fw[d][t][s], fx[d][s], acc[t]);
-            load(i + (d + DEEP) * KS, fw[d], fx[d]);   // (past the end: zeros, no memory read)
+            load(fw[d], fx[d]);   // (past the end: zeros, no memory read)
+            if (++s0 == steps) {
+                done(i, acc);
+                acc[0] = acc[1] = floatx4{0.f, 0.f, 0.f, 0.f};
+                s0 = 0;
+                ++i;
+            }
         }
     }
 }
@@ -140,9 +151,12 @@ __global__ __launch_bounds__(KS * 64) void gate_kernel(const Args P) {
     __shared__ float red[(KS - 1) * 2 * 64 * 4];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int f0 = (int)blockIdx.x * 16, F = P.F;
-    const int r0[2] = {f0, F + f0}, end[2] = {F, 2 * F};
+    const int end[2] = {F, 2 * F};
     floatx4 acc[2];
-    products<T>(P, r0, end, wave, lane, acc);
+    products<T>(P, f0, 0, F, end, 1, wave, lane, [&](int, floatx4 (&sums)[2]) {
+        acc[0] = sums[0];
+        acc[1] = sums[1];
+    });
     meet(acc, red, wave, lane);
     const int m = lane & 15, f = f0 + 4 * (lane >> 4);
     if (wave != 0 || m >= P.M) return;
@@ -177,10 +191,11 @@ __global__ __launch_bounds__(KS * 64) void lse_kernel(const Args P) {
     const int m = lane & 15;
     const int64_t t = wave == 0 && m < P.M ? P.target[m] : -1;
     floatx2 a = {-INFINITY, 0.f};
-    for (int v0 = (int)blockIdx.x * 32; v0 < P.V; v0 += (int)gridDim.x * 32) {
-        const int r0[2] = {v0, v0 + 16}, end[2] = {P.V, P.V};
-        floatx4 acc[2];
-        products<T>(P, r0, end, wave, lane, acc);
+    const int end[2] = {P.V, P.V}, all = (P.V + 31) / 32;
+    const int mine = (all - (int)blockIdx.x + (int)gridDim.x - 1) / (int)gridDim.x;
+    products<T>(P, (int)blockIdx.x * 32, (int)gridDim.x * 32, 16, end, mine, wave, lane, [&](int g, floatx4 (&acc)[2]) {
+        const int v0 = ((int)blockIdx.x + g * (int)gridDim.x) * 32;
+        if (g > 0) __syncthreads();   // wave 0 has read the others' last sums
         meet(acc, red, wave, lane);
         if (wave == 0) {
             float top = -INFINITY;
@@ -203,8 +218,7 @@ __global__ __launch_bounds__(KS * 64) void lse_kernel(const Args P) {
                 for (int v = 0; v < 4; ++v) s += exp_below(acc[i][v], t0);
             a = join_lse(a, floatx2{top, s});
         }
-        __syncthreads();   // wave 0 has read the others' sums
-    }
+    });
     if (wave != 0) return;
 #pragma unroll
     for (int o = 16; o < 64; o <<= 1) a = join_lse(a, floatx2{__shfl_xor(a.x, o), __shfl_xor(a.y, o)});
@@ -248,7 +262,7 @@ __global__ __launch_bounds__(1024) void loss_kernel(const floatx2 *__restrict__ 
 
 namespace {
 
-constexpr int kMostBlocks = 1024;
+constexpr int kMostBlocks = 768;
 
 template <typename T>
 Args args(int64_t M, int64_t N, int64_t K, const void *x, const void *w, const void *bias) {
@@ -274,7 +288,11 @@ int gate_t(int64_t M, int64_t D, int64_t F, int act, const void *x, const void *
     return (int)hipGetLastError();
 }
 
-int blocks(int64_t V) { return (int)std::min<int64_t>((V + 31) / 32, kMostBlocks); }
+// As many blocks as the card holds at once, each with as many groups as the others.
+int blocks(int64_t V) {
+    const int64_t groups = (V + 31) / 32, each = (groups + kMostBlocks - 1) / kMostBlocks;
+    return (int)((groups + each - 1) / each);
+}
 
 template <typename T>
 int lse_t(int64_t M, int64_t D, int64_t V, const void *x, const void *w, const void *b, const int64_t *target, floatx2 *stat, float *tlogit,
