@@ -46,6 +46,28 @@ __device__ __forceinline__ uint32_t to_f24(float v) {
 
 typedef float floatx2 __attribute__((ext_vector_type(2)));
 
+// How many ways to split the steps of a contraction whose rows are known on the
+// device only: rounds of blocks over the card, each its share of the steps and some
+// five steps' worth of beginning and end, against the partials' traffic.
+struct SplitRule {
+    int bm, ntn, steps, slots, most;   // tile rows, column tiles, steps, blocks at once, splits at most
+    float step_us, row_us;             // a step of one round; a row of partials
+    __device__ __forceinline__ int splits(int rows) const {
+        const int tiles = (rows + bm - 1) / bm * ntn;
+        int best = 1;
+        float us = INFINITY;
+        for (int s = 1; s <= most; ++s) {
+            const int rounds = (tiles * s + slots - 1) / slots;
+            const float t = (float)rounds * ((float)((steps + s - 1) / s) + 5.f) * step_us + (float)s * (float)rows * row_us;
+            if (t < us) {
+                us = t;
+                best = s;
+            }
+        }
+        return best;
+    }
+};
+
 constexpr float kLog2e = 1.44269504088896341f;
 
 // exp(v - m).  The difference first: with m the larger one it is a finite number

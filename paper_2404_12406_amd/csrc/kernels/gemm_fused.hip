@@ -42,6 +42,7 @@ struct FusedArgs : Args {
     const float *lse, *scale;   // kEpiXent: of each row
     const float *out_scale;     // kEpiStore: the sums' factor
     int add;               // kEpiAdd: add to the partials (0: write them)
+    const int *nsplit;     // kEpiAdd: their number, on the device
 };
 
 // Output column of row `row` of a gated tile's B operand, from the tile's first.
@@ -410,10 +411,10 @@ FusedPlan plan(const Tile (&tiles)[NT], int ntiles, long M, long N, long K, int 
 }
 
 template <int EPI, int MODE, int BM, int BN, int WR, int WC, int STAGES, int OCC>
-int go(unsigned prof, const FusedArgs &a, hipStream_t st) {
+int go(unsigned prof, const FusedArgs &a, hipStream_t st, int times = 1) {
     void *eb = nullptr, *ee = nullptr;
     const bool timed = prof_pair(prof, &eb, &ee);
-    hipExtLaunchKernelGGL((gemm_fused_kernel<EPI, MODE, BM, BN, WR, WC, STAGES, OCC>), dim3(a.ntm * a.ntn, 1, a.splits),
+    hipExtLaunchKernelGGL((gemm_fused_kernel<EPI, MODE, BM, BN, WR, WC, STAGES, OCC>), dim3(a.ntm * a.ntn * times, 1, a.splits),
                           dim3(WR * WC * 64), 0, st, (hipEvent_t)eb, (hipEvent_t)ee, 0, a);
     const int err = (int)hipGetLastError();
     if (timed) prof_pair_done(prof, eb, ee, err == 0);
@@ -430,11 +431,11 @@ int go_rows(int tile, unsigned prof, const FusedArgs &a, hipStream_t st) {
 }
 
 template <int EPI, int MODE>
-int go_grad(int tile, unsigned prof, const FusedArgs &a, hipStream_t st) {
+int go_grad(int tile, unsigned prof, const FusedArgs &a, hipStream_t st, int times = 1) {
     switch (tile) {
-    case 0: return go<EPI, MODE, 256, 256, 2, 4, 2, 1>(prof, a, st);
-    case 1: return go<EPI, MODE, 256, 128, 2, 4, 3, 1>(prof, a, st);
-    default: return go<EPI, MODE, 128, 128, 2, 4, 2, 2>(prof, a, st);
+    case 0: return go<EPI, MODE, 256, 256, 2, 4, 2, 1>(prof, a, st, times);
+    case 1: return go<EPI, MODE, 256, 128, 2, 4, 3, 1>(prof, a, st, times);
+    default: return go<EPI, MODE, 128, 128, 2, 4, 2, 2>(prof, a, st, times);
     }
 }
 
@@ -528,23 +529,32 @@ int xent_grad(int64_t M, int64_t D, int64_t V, const void *x, const void *w, con
     return go_rows<kEpiXent>(p.tile, kProfFwd, a, st);
 }
 
-// Splits of dx += dz w over the words of a piece: arrays [M][D] of partials.
-int xent_dx_splits(int64_t M, int64_t D, int64_t V) { return plan(kGradTiles, 3, M, D, V, (int)std::clamp<int64_t>(V / (4 * BK), 1, 16)).splits; }
+namespace {
+int dx_tile(int64_t M, int64_t D, int64_t V) { return plan(kGradTiles, 3, M, D, V, (int)std::clamp<int64_t>(V / (4 * BK), 1, 16)).tile; }
+}  // namespace
 
-int xent_dx(int64_t M, int64_t D, int64_t V, int64_t ldz, const void *dz, const void *w, const int *count, float *part, int splits,
-            bool add, hipStream_t st) {
-    // (a last, smaller piece runs with the splits of the others)
-    FusedPlan p{0, splits};
-    double best = 1e300;
-    const int forced = forced_tile(kGradTiles, 3);
-    for (int t = std::max(forced, 0); t < (forced < 0 ? 3 : forced + 1); ++t) {
-        const double us = est_us(kGradTiles[t], M, D, V, 1, splits);
-        if (us < best) {
-            best = us;
-            p.tile = t;
-        }
-    }
-    const Tile &t = kGradTiles[p.tile];
+// dx += dz w over the words of a piece, in up to rule.most arrays [M][D] of partials.
+// Few rows of a wide vocabulary are few tiles of many steps: how many ways to split
+// them follows from the rows that count, which only the device knows
+// (SplitRule::splits()).
+SplitRule xent_dx_rule(int64_t M, int64_t D, int64_t V) {
+    const Tile &t = kGradTiles[dx_tile(M, D, V)];
+    SplitRule r;
+    r.bm = t.bm;
+    r.ntn = (int)((D + t.bn - 1) / t.bn);
+    r.steps = (int)((V + BK - 1) / BK);
+    r.slots = kCUs * t.per_cu;
+    r.row_us = (float)(8.0 * D / 5.0e6);   // a partial row, written and read
+    r.step_us = (float)(1.5 * t.bm * t.bn * t.per_cu / (256.0 * 256.0));
+    // at most a quarter gigabyte of partials
+    r.most = (int)std::clamp<int64_t>((int64_t(256) << 20) / std::max<int64_t>(1, M * D * 4), 1, 16);
+    return r;
+}
+
+int xent_dx(int64_t M, int64_t D, int64_t V, int64_t ldz, int64_t piece, const void *dz, const void *w, const int *count,
+            const int *nsplit, float *part, bool add, hipStream_t st) {
+    const int tile = dx_tile(M, D, piece);   // (a last, smaller piece runs as the others)
+    const Tile &t = kGradTiles[tile];
     FusedArgs a{};
     a.a = (const bf16 *)dz;
     a.b = (const bf16 *)w;
@@ -553,15 +563,16 @@ int xent_dx(int64_t M, int64_t D, int64_t V, int64_t ldz, const void *dz, const 
     a.M = (int)M; a.N = (int)D; a.K = (int)ldz;
     a.ntm = (int)((M + t.bm - 1) / t.bm);
     a.ntn = (int)((D + t.bn - 1) / t.bn);
-    a.splits = splits;
-    a.k_split = (int)(((ldz + splits - 1) / splits + BK - 1) / BK * BK);
+    a.splits = 1;
+    a.k_split = (int)ldz;
     a.a_bytes = bytes_of(M * ldz);
     a.b_bytes = bytes_of(V * D);
     a.count = count;
+    a.nsplit = nsplit;
     a.part = part;
     a.part_stride = M * D;
     a.add = add;
-    return go_grad<kEpiAdd, kDgradN>(p.tile, kProfDgrad, a, st);
+    return go_grad<kEpiAdd, kDgradN>(tile, kProfDgrad, a, st, xent_dx_rule(M, D, piece).most);
 }
 
 // dw[V][Dr] = *scale dz^T x over the rows that count (x has D >= Dr columns), and db.
