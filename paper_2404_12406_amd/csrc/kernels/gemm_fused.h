@@ -12,13 +12,15 @@
 //   kEpiStore     the weight gradient dz^T x over the rows that count, times a factor
 // The main loop is gemm_block_body.inc's.  Everything before the one rounding
 // of what is stored is in fp32.
+#pragma once
+
 #include <cstdlib>
 #include <cstring>
 
 #include <hip/hip_ext.h>
 
-#include "gemm_bf16.h"
 #include "block_math.h"
+#include "gemm_bf16.h"
 
 namespace ms {
 namespace g2 {
@@ -29,7 +31,7 @@ struct FusedArgs : Args {
     const int *count;      // rows that count (weight gradient: of the reduction), on the device; null: all
     const bf16 *fbias;     // bias of the columns (gated: [2F]); null: none
     // gated
-    int F, act;
+    int F;
     uint16_t *proj;        // kEpiGate: z in 24 bits (null: not kept): a plane of the leading 16, [M][2F],
     uint8_t *proj_lo;      // and one of the others
     const bf16 *dh;        // kEpiGateGrad: dy[M][F]; c is dz[M][2F]
@@ -47,6 +49,14 @@ struct FusedArgs : Args {
 
 // Output column of row `row` of a gated tile's B operand, from the tile's first.
 __device__ __forceinline__ int gate_col(int row) { return (row >> 6) * 32 + (row & 31); }
+
+// Between a wave's writes to its staging rows and its reads of them, and back: LDS
+// serves a wave's instructions in order, so only the compiler has to keep to it.
+__device__ __forceinline__ void stage_order() {
+    __atomic_signal_fence(__ATOMIC_SEQ_CST);
+    __builtin_amdgcn_wave_barrier();
+    __atomic_signal_fence(__ATOMIC_SEQ_CST);
+}
 
 typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
@@ -92,14 +102,12 @@ template <int COLS, int TG>
 __device__ __forceinline__ void put_bytes(uint8_t *stage, const uint32_t (&b)[TG][4], uint8_t *dst, int64_t ld, int nrow, int ncol,
                                           int fr, int fh, int lane) {
     constexpr int PITCH = COLS + 16, SEG = COLS / 16, RPP = 64 / SEG;
-    wait_lgkm0();
-    __builtin_amdgcn_wave_barrier();
+    stage_order();
 #pragma unroll
     for (int j = 0; j < TG; ++j)
 #pragma unroll
         for (int q = 0; q < 4; ++q) *reinterpret_cast<uint32_t *>(stage + fr * PITCH + 32 * j + 8 * q + 4 * fh) = b[j][q];
-    wait_lgkm0();
-    __builtin_amdgcn_wave_barrier();
+    stage_order();
 #pragma unroll
     for (int r0 = 0; r0 < 32; r0 += RPP) {
         const int r = r0 + lane / SEG, c = (lane % SEG) * 16;
@@ -118,32 +126,50 @@ __device__ __forceinline__ void put_bytes(uint8_t *stage, const uint32_t (&b)[TG
 
 // What the sums start from: the bias of their columns and, in the softmax, minus
 // infinity past the last word (nothing is added to it there: W's rows read zeros).
+// Loaded before the operands' first loads are issued, put into the sums after.
 template <int EPI, class G>
-__device__ __forceinline__ void fused_init(const FusedArgs &P, floatx16 (&acc)[G::TM][G::TN], int n0, int wn0, int lane) {
-    constexpr bool GATED = EPI == kEpiGate || EPI == kEpiGateGrad, SOFTMAX = EPI == kEpiLse || EPI == kEpiXent;
-    const int fh = lane >> 5, nb = GATED ? 2 * P.F : P.N;
-    const __amdgpu_buffer_rsrc_t r = rsrc(P.fbias, P.fbias ? (uint32_t)nb * 2u : 0u);
+struct FusedInit {
+    static constexpr bool GATED = EPI == kEpiGate || EPI == kEpiGateGrad, SOFTMAX = EPI == kEpiLse || EPI == kEpiXent;
+    float b[G::TN][4][4];
+
+    __device__ __forceinline__ FusedInit(const FusedArgs &P, int n0, int wn0, int lane) {
+        const int fh = lane >> 5, nb = GATED ? 2 * P.F : P.N;
 #pragma unroll
-    for (int j = 0; j < G::TN; ++j)
+        for (int j = 0; j < G::TN; ++j)
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
-            const int c = 8 * q + 4 * fh;
-            float b[4];
-            // (gated columns past F read the other half's: not stored)
-            if constexpr (GATED) bias4(r, (n0 + wn0) / 2 + 32 * (j / 2) + c + (j & 1) * P.F, (P.F & 3) == 0, b);
-            else bias4(r, n0 + wn0 + 32 * j + c, (nb & 3) == 0, b);
+            for (int q = 0; q < 4; ++q)
 #pragma unroll
-            for (int v = 0; v < 4; ++v) {
-                if (SOFTMAX && n0 + wn0 + 32 * j + c + v >= nb) b[v] = -INFINITY;
+                for (int v = 0; v < 4; ++v) b[j][q][v] = 0.f;
+        if (!P.fbias) return;
+        const __amdgpu_buffer_rsrc_t r = rsrc(P.fbias, (uint32_t)nb * 2u);
 #pragma unroll
-                for (int i = 0; i < G::TM; ++i) acc[i][j][4 * q + v] = b[v];
+        for (int j = 0; j < G::TN; ++j)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const int c = 8 * q + 4 * fh;
+                // (gated columns past F read the other half's: not stored)
+                if constexpr (GATED) bias4(r, (n0 + wn0) / 2 + 32 * (j / 2) + c + (j & 1) * P.F, (P.F & 3) == 0, b[j][q]);
+                else bias4(r, n0 + wn0 + 32 * j + c, (nb & 3) == 0, b[j][q]);
             }
-        }
-}
+    }
+    __device__ __forceinline__ void put(const FusedArgs &P, floatx16 (&acc)[G::TM][G::TN], int n0, int wn0, int lane) {
+        const int fh = lane >> 5;
+#pragma unroll
+        for (int j = 0; j < G::TN; ++j)
+#pragma unroll
+            for (int q = 0; q < 4; ++q)
+#pragma unroll
+                for (int v = 0; v < 4; ++v) {
+                    if (SOFTMAX && n0 + wn0 + 32 * j + 8 * q + 4 * fh + v >= P.N) b[j][q][v] = -INFINITY;
+#pragma unroll
+                    for (int i = 0; i < G::TM; ++i) acc[i][j][4 * q + v] = b[j][q][v];
+                }
+    }
+};
 
 // The lane's 16 sums of tile (i, j) are row 32 i + lane % 32 and columns
 // 32 j + 8 q + 4 (lane / 32) + v, q and v = 0..3.
-template <int EPI, class G>
+template <int EPI, int ACT, class G>
 __device__ __forceinline__ void fused_epilogue(const FusedArgs &P, char *smem, floatx16 (&acc)[G::TM][G::TN], int M, int m0, int n0,
                                                int wm0, int wn0, int wave, int lane, int tn, int zsplit) {
     constexpr int TM = G::TM, TN = G::TN;
@@ -155,30 +181,35 @@ __device__ __forceinline__ void fused_epilogue(const FusedArgs &P, char *smem, f
         static_assert(TN % 2 == 0, "gated tiles pair the column tiles of a wave");
         const int F = P.F, f0 = (n0 + wn0) / 2;
         const int ncol = min(F - f0, COLS);
+        // dy's tile, whole vectors where they are, every pass's loads in flight at once
+        constexpr int SEG = COLS / 8, RPP = 64 / SEG;
+        Vec16<bf16> dh[EPI == kEpiGateGrad ? TM : 1][32 / RPP];
+        if constexpr (EPI == kEpiGateGrad) {
+#pragma unroll
+            for (int i = 0; i < TM; ++i)
+#pragma unroll
+                for (int h = 0; h < 32 / RPP; ++h) {
+                    const int m = m0 + wm0 + 32 * i + h * RPP + lane / SEG, c = (lane % SEG) * 8;
+                    dh[i][h] = zero16<bf16>();
+                    if (m >= M || c >= ncol) continue;
+                    const bf16 *s = P.dh + (int64_t)m * F + f0 + c;
+                    if (c + 8 <= ncol) {
+                        dh[i][h].u = *reinterpret_cast<const u32x4 *>(s);
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < 8; ++e)
+                            if (c + e < ncol) dh[i][h].e[e] = s[e];
+                    }
+                }
+        }
 #pragma unroll
         for (int i = 0; i < TM; ++i) {
             const int mb = m0 + wm0 + 32 * i, nrow = M - mb;   // rows of this pass
-            if (EPI == kEpiGateGrad && P.dh) {
-                // dy's tile, whole vectors where they are, into the staging rows
-                constexpr int SEG = COLS / 8, RPP = 64 / SEG;
+            if constexpr (EPI == kEpiGateGrad) {
 #pragma unroll
-                for (int r0 = 0; r0 < 32; r0 += RPP) {
-                    const int r = r0 + lane / SEG, c = (lane % SEG) * 8;
-                    Vec16<bf16> v = zero16<bf16>();
-                    if (r < nrow && c < ncol) {
-                        const bf16 *s = P.dh + (int64_t)(mb + r) * F + f0 + c;
-                        if (c + 8 <= ncol) {
-                            v.u = *reinterpret_cast<const u32x4 *>(s);
-                        } else {
-#pragma unroll
-                            for (int e = 0; e < 8; ++e)
-                                if (c + e < ncol) v.e[e] = s[e];
-                        }
-                    }
-                    *reinterpret_cast<u32x4 *>(stage + r * PITCH + c) = v.u;
-                }
-                wait_lgkm0();
-                __builtin_amdgcn_wave_barrier();
+                for (int h = 0; h < 32 / RPP; ++h)
+                    *reinterpret_cast<u32x4 *>(stage + (h * RPP + lane / SEG) * PITCH + (lane % SEG) * 8) = dh[i][h].u;
+                stage_order();
             }
             // what the second pass stores: gradients, or (gate, up) projections
             bf16x4 og[TG][4], ou[TG][4];
@@ -195,7 +226,7 @@ __device__ __forceinline__ void fused_epilogue(const FusedArgs &P, char *smem, f
                     for (int v = 0; v < 4; ++v) {
                         const float zg = acc[i][2 * j][4 * q + v], zu = acc[i][2 * j + 1][4 * q + v];
                         if constexpr (EPI == kEpiGate) {
-                            acc[i][2 * j][4 * q + v] = act::value<true>(P.act, zg) * zu;
+                            acc[i][2 * j][4 * q + v] = act::value<true>(ACT, zg) * zu;
                             if (P.proj) {
                                 const uint32_t kg = to_f24(zg), ku = to_f24(zu);
                                 og[j][q][v] = __builtin_bit_cast(bf16, (uint16_t)(kg >> 8));
@@ -205,7 +236,7 @@ __device__ __forceinline__ void fused_epilogue(const FusedArgs &P, char *smem, f
                             }
                         } else {
                             float a, da;
-                            act::both<true>(P.act, zg, a, da);
+                            act::both<true>(ACT, zg, a, da);
                             const float d = (float)d4[v];
                             og[j][q][v] = (bf16)(d * zu * da);
                             ou[j][q][v] = (bf16)(d * a);
@@ -213,15 +244,13 @@ __device__ __forceinline__ void fused_epilogue(const FusedArgs &P, char *smem, f
                     }
                 }
             auto put = [&](auto get, bf16 *dst, int64_t ld) __attribute__((always_inline)) {
-                wait_lgkm0();   // the staging rows are free
-                __builtin_amdgcn_wave_barrier();
+                stage_order();
 #pragma unroll
                 for (int j = 0; j < TG; ++j)
 #pragma unroll
                     for (int q = 0; q < 4; ++q)
                         *reinterpret_cast<bf16x4 *>(stage + fr * PITCH + 32 * j + 8 * q + 4 * fh) = get(j, q);
-                wait_lgkm0();
-                __builtin_amdgcn_wave_barrier();
+                stage_order();
                 store_rows<COLS>(stage, PITCH, dst + (int64_t)mb * ld + f0, ld, nrow, ncol, lane);
             };
             if constexpr (EPI == kEpiGate) {
@@ -244,10 +273,21 @@ __device__ __forceinline__ void fused_epilogue(const FusedArgs &P, char *smem, f
                 put([&](int j, int q) { return og[j][q]; }, P.c, 2 * (int64_t)F);
                 put([&](int j, int q) { return ou[j][q]; }, P.c + F, 2 * (int64_t)F);
             }
-            wait_lgkm0();
-            __builtin_amdgcn_wave_barrier();
+            stage_order();
         }
     } else if constexpr (EPI == kEpiLse || EPI == kEpiXent) {
+        // the rows' values, every pass's loads in flight at once
+        int tgt[TM];
+        float lse[EPI == kEpiXent ? TM : 1], scale[EPI == kEpiXent ? TM : 1];
+#pragma unroll
+        for (int i = 0; i < TM; ++i) {
+            const int m = min(m0 + wm0 + 32 * i + fr, M - 1);
+            tgt[i] = P.target[m];
+            if constexpr (EPI == kEpiXent) {
+                lse[i] = P.lse[m];
+                scale[i] = P.scale[m];
+            }
+        }
         if constexpr (EPI == kEpiLse) {
             constexpr int BM = G::A_BYTES / (BK * 2), WC = G::B_BYTES / (BK * 2) / G::WN;   // waves along the columns
             floatx2 *red = reinterpret_cast<floatx2 *>(smem);   // [WC][BM]
@@ -270,7 +310,7 @@ __device__ __forceinline__ void fused_epilogue(const FusedArgs &P, char *smem, f
                     for (int v = 0; v < 16; ++v) s += exp_below(acc[i][j][v], t0);
                 s += __shfl_xor(s, 32);
                 if (fh == 0) red[(wn0 / G::WN) * BM + wm0 + 32 * i + fr] = floatx2{top, s};
-                const int t = m < M ? P.target[m] - P.v0 - (n0 + wn0) : -1;   // within this wave's columns?
+                const int t = m < M ? tgt[i] - P.v0 - (n0 + wn0) : -1;   // within this wave's columns?
                 if (__any((unsigned)t < (unsigned)G::WN)) {
                     float z = 0.f;
                     bool mine = false;
@@ -303,8 +343,8 @@ __device__ __forceinline__ void fused_epilogue(const FusedArgs &P, char *smem, f
                 __builtin_amdgcn_sched_barrier(0);   // one pass at a time: the sums leave few registers
                 const int mb = m0 + wm0 + 32 * i, m = mb + fr;
                 const bool in = m < M;
-                const float l = in ? P.lse[m] : 0.f, sc = in ? P.scale[m] : 0.f;
-                const int t = in ? P.target[m] - P.v0 - (n0 + wn0) : -1;
+                const float l = in ? lse[i] : 0.f, sc = in ? scale[i] : 0.f;
+                const int t = in ? tgt[i] - P.v0 - (n0 + wn0) : -1;
                 const bool any = __any((unsigned)t < (unsigned)G::WN);
 #pragma unroll
                 for (int j = 0; j < TN; ++j)
@@ -319,11 +359,9 @@ __device__ __forceinline__ void fused_epilogue(const FusedArgs &P, char *smem, f
                         }
                         *reinterpret_cast<bf16x4 *>(stage + fr * PITCH + 32 * j + 8 * q + 4 * fh) = o;
                     }
-                wait_lgkm0();
-                __builtin_amdgcn_wave_barrier();
+                stage_order();
                 store_rows<G::WN>(stage, PITCH, P.c + (int64_t)mb * P.ldc + n0 + wn0, P.ldc, M - mb, ncol, lane);
-                wait_lgkm0();
-                __builtin_amdgcn_wave_barrier();
+                stage_order();
             }
         }
     } else {
@@ -349,7 +387,7 @@ __device__ __forceinline__ void fused_epilogue(const FusedArgs &P, char *smem, f
 }
 
 #define GEMM_FUSED
-template <int EPI, int MODE, int BM, int BN, int WR, int WC, int STAGES, int OCC>
+template <int EPI, int MODE, int BM, int BN, int WR, int WC, int STAGES, int OCC, int ACT = 0>
 __global__ __launch_bounds__(WR * WC * 64, OCC) void gemm_fused_kernel(const FusedArgs P) {
     constexpr bool UNIT = true, TS = false, D3 = false;
     constexpr int KG = 1;
@@ -362,7 +400,6 @@ __global__ __launch_bounds__(WR * WC * 64, OCC) void gemm_fused_kernel(const Fus
 // ------------------------------------------------------------------ host
 namespace {
 
-bool al16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 uint32_t bytes_of(int64_t elems) { return (uint32_t)(elems * 2); }
 
 // Tiles of the contractions over k-contiguous operands (gated, cross entropy).
@@ -372,13 +409,6 @@ constexpr Tile kRowTiles[] = {
     {"128x128", 128, 128, 2, 2, 2, 2, 0.78f, 1.00f},
     {"128x128s4", 128, 128, 2, 2, 4, 1, 0.90f, 0.90f},
 };
-// Tiles of the gradients of the cross entropy (an operand along m or n).
-constexpr Tile kGradTiles[] = {
-    {"256x256", 256, 256, 2, 4, 2, 1, 1.20f, 1.20f},
-    {"256x128", 256, 128, 2, 4, 3, 1, 1.00f, 1.00f},
-    {"128x128w8", 128, 128, 2, 4, 2, 2, 0.85f, 1.02f},
-};
-
 struct FusedPlan {
     int tile, splits;
 };
@@ -410,32 +440,26 @@ FusedPlan plan(const Tile (&tiles)[NT], int ntiles, long M, long N, long K, int 
     return p;
 }
 
-template <int EPI, int MODE, int BM, int BN, int WR, int WC, int STAGES, int OCC>
+template <int EPI, int MODE, int BM, int BN, int WR, int WC, int STAGES, int OCC, int ACT = 0>
 int go(unsigned prof, const FusedArgs &a, hipStream_t st, int times = 1) {
     void *eb = nullptr, *ee = nullptr;
     const bool timed = prof_pair(prof, &eb, &ee);
-    hipExtLaunchKernelGGL((gemm_fused_kernel<EPI, MODE, BM, BN, WR, WC, STAGES, OCC>), dim3(a.ntm * a.ntn * times, 1, a.splits),
+    hipExtLaunchKernelGGL((gemm_fused_kernel<EPI, MODE, BM, BN, WR, WC, STAGES, OCC, ACT>), dim3(a.ntm * a.ntn * times, 1, a.splits),
                           dim3(WR * WC * 64), 0, st, (hipEvent_t)eb, (hipEvent_t)ee, 0, a);
     const int err = (int)hipGetLastError();
     if (timed) prof_pair_done(prof, eb, ee, err == 0);
     return err;
 }
 
-template <int EPI>
+template <int EPI, int ACT = 0>
 int go_rows(int tile, unsigned prof, const FusedArgs &a, hipStream_t st) {
     switch (tile) {
-    case 0: return go<EPI, kFwd, 256, 256, 2, 4, 2, 1>(prof, a, st);
-    case 1: return go<EPI, kFwd, 128, 128, 2, 2, 2, 2>(prof, a, st);
-    default: return go<EPI, kFwd, 128, 128, 2, 2, 4, 1>(prof, a, st);
-    }
-}
-
-template <int EPI, int MODE>
-int go_grad(int tile, unsigned prof, const FusedArgs &a, hipStream_t st, int times = 1) {
-    switch (tile) {
-    case 0: return go<EPI, MODE, 256, 256, 2, 4, 2, 1>(prof, a, st, times);
-    case 1: return go<EPI, MODE, 256, 128, 2, 4, 3, 1>(prof, a, st, times);
-    default: return go<EPI, MODE, 128, 128, 2, 4, 2, 2>(prof, a, st, times);
+    case 0: return go<EPI, kFwd, 256, 256, 2, 4, 2, 1, ACT>(prof, a, st);
+    case 1: return go<EPI, kFwd, 128, 128, 2, 2, 2, 2, ACT>(prof, a, st);
+    default:
+        // (the softmax's tables leave the third tile out)
+        if constexpr (EPI == kEpiGate || EPI == kEpiGateGrad) return go<EPI, kFwd, 128, 128, 2, 2, 4, 1, ACT>(prof, a, st);
+        else return (int)hipErrorInvalidValue;
     }
 }
 
@@ -457,171 +481,5 @@ FusedArgs rows_args(const Tile &t, int64_t M, int64_t N, int64_t D, const void *
 }
 
 }  // namespace
-
-// Operands: D a multiple of 8, x and w 16-byte aligned, the bias 4-byte aligned.
-bool rows_ok(int64_t M, int64_t N, int64_t D, const void *x, const void *w) {
-    return D % 8 == 0 && al16(x) && al16(w) && operand_fits(M * D) && operand_fits(N * D);
-}
-
-int gate_fwd(int64_t M, int64_t D, int64_t F, int act, const void *x, const void *w, const void *bias, void *y, void *proj,
-             hipStream_t st) {
-    const FusedPlan p = plan(kRowTiles, 3, M, 2 * F, D, 1);
-    const Tile &t = kRowTiles[p.tile];
-    FusedArgs a = rows_args(t, M, 2 * F, D, x, w, 2 * F);
-    a.ntn = (int)((F + t.bn / 2 - 1) / (t.bn / 2));
-    a.F = (int)F;
-    a.act = act;
-    a.fbias = (const bf16 *)bias;
-    a.c = (bf16 *)y;
-    a.proj = (uint16_t *)proj;
-    a.proj_lo = proj ? static_cast<uint8_t *>(proj) + M * 4 * F : nullptr;
-    return go_rows<kEpiGate>(p.tile, kProfFwd, a, st);
-}
-
-int gate_grad(int64_t M, int64_t D, int64_t F, int act, const void *x, const void *w, const void *bias, const void *dy, void *dz,
-              hipStream_t st) {
-    const FusedPlan p = plan(kRowTiles, 3, M, 2 * F, D, 1);
-    const Tile &t = kRowTiles[p.tile];
-    FusedArgs a = rows_args(t, M, 2 * F, D, x, w, 2 * F);
-    a.ntn = (int)((F + t.bn / 2 - 1) / (t.bn / 2));
-    a.F = (int)F;
-    a.act = act;
-    a.fbias = (const bf16 *)bias;
-    a.dh = (const bf16 *)dy;
-    a.c = (bf16 *)dz;
-    return go_rows<kEpiGateGrad>(p.tile, kProfFwd, a, st);
-}
-
-// ------------------------------------------------------------------ cross entropy
-// Column tiles of the statistics (rows of `stat`).
-int xent_lse_tiles(int64_t M, int64_t D, int64_t V) {
-    const Tile &t = kRowTiles[plan(kRowTiles, 2, M, V, D, 1).tile];
-    return (int)((V + t.bn - 1) / t.bn);
-}
-
-int xent_lse(int64_t M, int64_t D, int64_t V, const void *x, const void *w, const void *bias, const int *count, const int *target,
-             void *stat, float *tlogit, hipStream_t st) {
-    const FusedPlan p = plan(kRowTiles, 2, M, V, D, 1);
-    FusedArgs a = rows_args(kRowTiles[p.tile], M, V, D, x, w, V);
-    a.fbias = (const bf16 *)bias;
-    a.count = count;
-    a.target = target;
-    a.stat = (floatx2 *)stat;
-    a.stat_ld = M;
-    a.tlogit = tlogit;
-    return go_rows<kEpiLse>(p.tile, kProfFwd, a, st);
-}
-
-// dz[M][ldz] of the words v0 .. v0 + V - 1, whose rows of W and biases w and
-// bias are; columns V .. ldz - 1 are zeros.
-int xent_grad(int64_t M, int64_t D, int64_t V, const void *x, const void *w, const void *bias, const int *count, const int *target,
-              int v0, const float *lse, const float *scale, void *dz, int64_t ldz, hipStream_t st) {
-    const FusedPlan p = plan(kRowTiles, 2, M, V, D, 1);
-    FusedArgs a = rows_args(kRowTiles[p.tile], M, V, D, x, w, V);
-    a.fbias = (const bf16 *)bias;
-    a.count = count;
-    a.target = target;
-    a.v0 = v0;
-    a.lse = lse;
-    a.scale = scale;
-    a.c = (bf16 *)dz;
-    a.ldc = (int)ldz;
-    return go_rows<kEpiXent>(p.tile, kProfFwd, a, st);
-}
-
-namespace {
-int dx_tile(int64_t M, int64_t D, int64_t V) { return plan(kGradTiles, 3, M, D, V, (int)std::clamp<int64_t>(V / (4 * BK), 1, 16)).tile; }
-}  // namespace
-
-// dx += dz w over the words of a piece, in up to rule.most arrays [M][D] of partials.
-// Few rows of a wide vocabulary are few tiles of many steps: how many ways to split
-// them follows from the rows that count, which only the device knows
-// (SplitRule::splits()).
-SplitRule xent_dx_rule(int64_t M, int64_t D, int64_t V) {
-    const Tile &t = kGradTiles[dx_tile(M, D, V)];
-    SplitRule r;
-    r.bm = t.bm;
-    r.ntn = (int)((D + t.bn - 1) / t.bn);
-    r.steps = (int)((V + BK - 1) / BK);
-    r.slots = kCUs * t.per_cu;
-    r.row_us = (float)(8.0 * D / 5.0e6);   // a partial row, written and read
-    r.step_us = (float)(1.5 * t.bm * t.bn * t.per_cu / (256.0 * 256.0));
-    // at most a quarter gigabyte of partials
-    r.most = (int)std::clamp<int64_t>((int64_t(256) << 20) / std::max<int64_t>(1, M * D * 4), 1, 16);
-    return r;
-}
-
-int xent_dx(int64_t M, int64_t D, int64_t V, int64_t ldz, int64_t piece, const void *dz, const void *w, const int *count,
-            const int *nsplit, float *part, bool add, hipStream_t st) {
-    const int tile = dx_tile(M, D, piece);   // (a last, smaller piece runs as the others)
-    const Tile &t = kGradTiles[tile];
-    FusedArgs a{};
-    a.a = (const bf16 *)dz;
-    a.b = (const bf16 *)w;
-    a.g.N = (int)M; a.g.C = (int)D; a.g.K = (int)ldz;
-    a.g.H = a.g.W = a.g.R = a.g.S = a.g.P = a.g.Q = a.g.sh = a.g.sw = 1;
-    a.M = (int)M; a.N = (int)D; a.K = (int)ldz;
-    a.ntm = (int)((M + t.bm - 1) / t.bm);
-    a.ntn = (int)((D + t.bn - 1) / t.bn);
-    a.splits = 1;
-    a.k_split = (int)ldz;
-    a.a_bytes = bytes_of(M * ldz);
-    a.b_bytes = bytes_of(V * D);
-    a.count = count;
-    a.nsplit = nsplit;
-    a.part = part;
-    a.part_stride = M * D;
-    a.add = add;
-    return go_grad<kEpiAdd, kDgradN>(tile, kProfDgrad, a, st, xent_dx_rule(M, D, piece).most);
-}
-
-// dw[V][Dr] = *scale dz^T x over the rows that count (x has D >= Dr columns), and db.
-int sum_wgrad_partials(const float *part, int splits, int M, int C8, int C, void *out, const float *dbpart, void *db, hipStream_t st);
-
-namespace {
-FusedPlan dw_plan(int64_t M, int64_t D, int64_t Dr, int64_t V) {
-    FusedPlan p = plan(kGradTiles, 3, V, D, M, (int)std::clamp<int64_t>(M / (4 * BK), 1, 16));
-    if (D != Dr) p.splits = std::max(p.splits, 2);   // the sum of the partials leaves the padding out
-    return p;
-}
-}  // namespace
-
-size_t xent_dw_workspace(int64_t M, int64_t D, int64_t Dr, int64_t V, bool db) {
-    const FusedPlan p = dw_plan(M, D, Dr, V);
-    return ((p.splits > 1 ? (size_t)p.splits * V * D : 0) + (db ? (size_t)p.splits * V : 0)) * sizeof(float);
-}
-
-int xent_dw(int64_t M, int64_t D, int64_t Dr, int64_t V, int64_t ldz, const void *dz, const void *x, const int *count,
-            const float *scale, void *dw, void *db, void *ws, hipStream_t st) {
-    const FusedPlan p = dw_plan(M, D, Dr, V);
-    const Tile &t = kGradTiles[p.tile];
-    FusedArgs a{};
-    a.a = (const bf16 *)dz;
-    a.b = (const bf16 *)x;
-    a.g.N = (int)M; a.g.C = (int)D; a.g.K = (int)ldz;
-    a.g.H = a.g.W = a.g.R = a.g.S = a.g.P = a.g.Q = a.g.sh = a.g.sw = 1;
-    a.M = (int)V; a.N = (int)D; a.K = (int)M;
-    a.ntm = (int)((V + t.bm - 1) / t.bm);
-    a.ntn = (int)((D + t.bn - 1) / t.bn);
-    a.splits = p.splits;
-    a.k_split = (int)M;
-    a.a_bytes = bytes_of(M * ldz);
-    a.b_bytes = bytes_of(M * D);
-    a.count = count;
-    a.out_scale = scale;
-    float *f = static_cast<float *>(ws);
-    if (p.splits > 1) {
-        a.part = f;
-        a.part_stride = V * D;
-        f += (size_t)p.splits * V * D;
-    } else {
-        a.c = (bf16 *)dw;
-    }
-    a.dbpart = db ? f : nullptr;
-    const int err = go_grad<kEpiStore, kWgrad>(p.tile, kProfWgrad, a, st);
-    if (err || (p.splits == 1 && !db)) return err;
-    return sum_wgrad_partials(a.part, p.splits, (int)V, (int)D, (int)Dr, dw, a.dbpart, db, st);
-}
-
 }  // namespace g2
 }  // namespace ms
