@@ -387,11 +387,12 @@ __device__ __forceinline__ void fused_epilogue(const FusedArgs &P, char *smem, f
 }
 
 #define GEMM_FUSED
-template <int EPI, int MODE, int BM, int BN, int WR, int WC, int STAGES, int OCC, int ACT = 0>
+template <int EPI, int MODE, int BM, int BN, int WR, int WC, int STAGES, int OCC, int ACT = 0, bool A3 = false>
 __global__ __launch_bounds__(WR * WC * 64, OCC) void gemm_fused_kernel(const FusedArgs P) {
     constexpr bool UNIT = true, TS = false, D3 = false;
     constexpr int KG = 1;
-    __shared__ __attribute__((aligned(1024))) char smem[Cfg<MODE, BM, BN, WR, WC, STAGES, KG>::SMEM_BYTES];
+    using C = Cfg<MODE, BM, BN, WR, WC, STAGES, KG>;
+    __shared__ __attribute__((aligned(1024))) char smem[A3 ? 3 * C::A_BYTES + 2 * C::B_BYTES : C::SMEM_BYTES];
     const int bx = (int)blockIdx.x, bz = (int)blockIdx.z;
 #include "gemm_block_body.inc"
 }
@@ -440,11 +441,11 @@ FusedPlan plan(const Tile (&tiles)[NT], int ntiles, long M, long N, long K, int 
     return p;
 }
 
-template <int EPI, int MODE, int BM, int BN, int WR, int WC, int STAGES, int OCC, int ACT = 0>
+template <int EPI, int MODE, int BM, int BN, int WR, int WC, int STAGES, int OCC, int ACT = 0, bool A3 = false>
 int go(unsigned prof, const FusedArgs &a, hipStream_t st, int times = 1) {
     void *eb = nullptr, *ee = nullptr;
     const bool timed = prof_pair(prof, &eb, &ee);
-    hipExtLaunchKernelGGL((gemm_fused_kernel<EPI, MODE, BM, BN, WR, WC, STAGES, OCC, ACT>), dim3(a.ntm * a.ntn * times, 1, a.splits),
+    hipExtLaunchKernelGGL((gemm_fused_kernel<EPI, MODE, BM, BN, WR, WC, STAGES, OCC, ACT, A3>), dim3(a.ntm * a.ntn * times, 1, a.splits),
                           dim3(WR * WC * 64), 0, st, (hipEvent_t)eb, (hipEvent_t)ee, 0, a);
     const int err = (int)hipGetLastError();
     if (timed) prof_pair_done(prof, eb, ee, err == 0);

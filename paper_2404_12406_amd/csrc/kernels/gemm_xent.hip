@@ -15,7 +15,7 @@ constexpr Tile kGradTiles[] = {
 template <int EPI, int MODE>
 int go_grad(int tile, unsigned prof, const FusedArgs &a, hipStream_t st, int times = 1) {
     switch (tile) {
-    case 0: return go<EPI, MODE, 256, 256, 2, 4, 2, 1>(prof, a, st, times);
+    case 0: return go<EPI, MODE, 256, 256, 2, 4, 2, 1, 0, EPI == kEpiAdd>(prof, a, st, times);
     case 1: return go<EPI, MODE, 256, 128, 2, 4, 3, 1>(prof, a, st, times);
     default: return go<EPI, MODE, 128, 128, 2, 4, 2, 2>(prof, a, st, times);
     }
