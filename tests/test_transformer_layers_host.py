@@ -1,0 +1,276 @@
+"""The transformer layers' entry points without a GPU (blocks.cpp with stub
+launchers): what they refuse, what their records borrow by mask, the ledger,
+tensors in other layouts, a workspace that cannot be had."""
+import ctypes
+import os
+import subprocess
+
+import pytest
+
+from paper_2404_12406_amd import _lib as L
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+NATIVE = os.path.join(ROOT, "tests", "native")
+BUILD = os.path.join(NATIVE, "_build")
+FAKE = 0x7f0000000000   # an aligned address that nobody reads
+DT = {"f32": L.MS_F32, "bf16": L.MS_BF16}
+X, W_, B_ = 1, 2, 4     # mask bits
+SAVED_X, SAVED_W, SAVED_PROJ, SAVED_LSE = 1, 2, 128, 256
+
+
+@pytest.fixture(scope="module")
+def stub():
+    os.makedirs(BUILD, exist_ok=True)
+    so = os.path.join(BUILD, "libmemsave_blocks.so")
+    csrc = os.path.join(ROOT, "paper_2404_12406_amd", "csrc")
+    tmp = so + f".tmp{os.getpid()}"
+    subprocess.run(["g++", "-O1", "-g", "-std=c++17", "-fPIC", "-shared", "-Wall", "-I", os.path.join(ROOT, "include"),
+                    os.path.join(csrc, "memsave.cpp"), os.path.join(csrc, "blocks.cpp"), os.path.join(NATIVE, "host_stub.cpp"),
+                    os.path.join(NATIVE, "blocks_stub.cpp"), "-o", tmp], check=True)
+    os.replace(tmp, so)
+    lib = L.configure(ctypes.CDLL(so))
+    for f in ("blocks_log", "blocks_violations", "stub_log"):
+        getattr(lib, f).restype = ctypes.c_char_p
+    lib.blocks_reset()
+    lib.stub_reset()
+    return lib
+
+
+@pytest.fixture(autouse=True)
+def clean(stub):
+    live0 = live(stub)
+    yield
+    assert stub.blocks_violations() == b""
+    assert live(stub) == live0
+    stub.blocks_reset()
+    stub.stub_reset()
+
+
+def live(lib):
+    a, b = ctypes.c_uint64(), ctypes.c_uint64()
+    lib.ms_ledger_read(ctypes.byref(a), ctypes.byref(b))
+    return a.value
+
+
+def tensor(shape, dtype="bf16", strides=None, addr=FAKE):
+    t = L.MsTensor()
+    t.data, t.dtype, t.ndim = addr, DT.get(dtype, dtype), len(shape)
+    if strides is None:
+        strides, n = [], 1
+        for s in reversed(shape):
+            strides.insert(0, n)
+            n *= max(s, 1)
+    for i, (s, st) in enumerate(zip(shape, strides)):
+        t.shape[i], t.stride[i] = s, st
+    return t
+
+
+def ref(t):
+    return ctypes.byref(t) if t is not None else None
+
+
+M, D, F, V = 12, 40, 24, 100
+
+
+class Call:
+    """One layer's forward with its good arguments, any of which a test replaces."""
+
+    def __init__(self, lib, kind, dtype="bf16", **over):
+        self.lib, self.kind, self.dtype = lib, kind, dtype
+        self.a = dict(x=tensor((M, D), dtype), mask=7, rec=True, eps=1e-5, act=0, reduction=0, target=FAKE, lse=FAKE, ignore=-100, proj=None)
+        if kind == "norm":
+            self.a.update(W=tensor((D,), dtype), b=tensor((D,), dtype), y=tensor((M, D), dtype))
+        elif kind == "gated":
+            self.a.update(W=tensor((2 * F, D), dtype), b=tensor((2 * F,), dtype), y=tensor((M, F), dtype), proj=FAKE)
+        else:
+            self.a.update(W=tensor((V, D), dtype), b=tensor((V,), dtype), y=tensor((1,), "f32"))
+        self.a.update(over)
+        self.h = ctypes.c_void_p()
+
+    def forward(self):
+        a = self.a
+        hp = ctypes.byref(self.h) if a["rec"] else None
+        head, tail = (ref(a["x"]), ref(a["W"]), ref(a["b"])), (a["mask"], ref(a["y"]), hp, None)
+        if self.kind == "norm":
+            return self.lib.ms_layer_norm_forward(*head, a["eps"], *tail)
+        if self.kind == "gated":
+            return self.lib.ms_gated_linear_forward(*head, a["act"], a["proj"], *tail)
+        return self.lib.ms_cross_entropy_forward(*head, a["target"], a["ignore"], a["reduction"], a["lse"], *tail)
+
+    def backward(self, dy="default", entry="ms_layer_backward", mask=None):
+        a, m = self.a, self.a["mask"] if mask is None else mask
+        if dy == "default":
+            dy = a["y"]
+        return getattr(self.lib, entry)(self.h, ref(dy), ref(a["x"]) if m & 1 else None, ref(a["W"]) if m & 2 else None,
+                                        ref(a["b"]) if m & 4 else None, None)
+
+    def account(self):
+        acct = L.MsAccount()
+        assert self.lib.ms_record_account(self.h, ctypes.byref(acct)) == 0
+        return acct
+
+    def free(self):
+        self.lib.ms_record_free(self.h)
+
+
+KINDS = ["norm", "gated", "xent"]
+
+
+@pytest.mark.parametrize("mask", range(8))
+@pytest.mark.parametrize("kind", KINDS)
+def test_records_borrow_what_the_mask_needs(stub, kind, mask):
+    c = Call(stub, kind, mask=mask, **({"proj": FAKE if mask else None} if kind == "gated" else {}))
+    before = live(stub)
+    assert c.forward() == 0
+    names = {"norm": "norm;", "gated": "gated+proj;" if mask else "gated;", "xent": "xent+lse;" if mask else "xent;"}
+    assert stub.blocks_log().decode() == names[kind]
+    if not mask:
+        assert not c.h.value and live(stub) == before
+        return
+    acct = c.account()
+    xb, proj = M * D * 2, M * 2 * F * 3
+    if kind == "norm":   # its input for dx or dgamma, the scale for dx; the shift's gradient needs neither
+        want = (SAVED_X if mask & 3 else 0) | (SAVED_W if mask & 1 else 0)
+        kept, params = (xb if mask & 3 else 0), (D * 2 if mask & 1 else 0)
+    elif kind == "gated":   # kept projections: x for dW alone, W for dx alone
+        want = SAVED_PROJ | (SAVED_X if mask & 2 else 0) | (SAVED_W if mask & 1 else 0)
+        kept, params = proj + (xb if mask & 2 else 0), (4 * F * D if mask & 1 else 0)
+    else:                # z is taken again: x, W, b, a row's lse and target
+        want, kept, params = SAVED_X | SAVED_W | SAVED_LSE, xb + M * 12, V * D * 2 + V * 2
+    assert (acct.borrowed, acct.saved_activation_bytes, acct.referenced_param_bytes) == (want, kept, params)
+    assert live(stub) == before + kept
+    stub.blocks_reset()
+    stub.stub_reset()
+    assert c.backward() == 0
+    grads = (("+dx" if mask & 1 else ""), ("+dg" if kind == "norm" else "+dw") if mask & 2 else "", "+db" if mask & 4 else "")
+    if kind == "norm" and mask == 4:
+        assert (stub.blocks_log(), stub.stub_log()) == (b"", b"colsum;")   # a sum of the rows of grad_y
+    else:
+        assert stub.blocks_log().decode() == f"{kind}_bwd{''.join(grads)};"
+    assert c.backward() == L.MS_E_CONSUMED
+    c.free()
+
+
+@pytest.mark.parametrize("mask", range(1, 8))
+def test_gated_unit_from_its_input_alone(stub, mask):
+    c = Call(stub, "gated", mask=mask, proj=None)
+    assert c.forward() == 0
+    acct = c.account()
+    assert acct.borrowed == SAVED_X | SAVED_W
+    assert acct.saved_activation_bytes == M * D * 2 and acct.referenced_param_bytes == 4 * F * D + 4 * F
+    assert c.backward() == 0
+    c.free()
+
+
+@pytest.mark.parametrize("rows,f,dtype,want", [(0, 5, 0, 0), (3, 0, 1, 0), (12, 24, 1, 12 * 48 * 3), (7, 17, 0, 7 * 64 * 4),
+                                              (2 ** 20, 2 ** 13, 1, 2 ** 34 * 3), (-1, 4, 0, 0)])
+def test_projection_bytes(stub, rows, f, dtype, want):
+    assert (L.MS_F32, L.MS_BF16) == (0, 1)
+    assert stub.ms_gated_projection_bytes(rows, f, dtype) == want
+
+
+COMMON = [
+    (L.MS_E_NULL, dict(rec=False)),
+    (L.MS_E_NULL, dict(x=None)),
+    (L.MS_E_NULL, dict(x=tensor((M, D), addr=None))),
+    (L.MS_E_NULL, dict(y=None)),
+    (L.MS_E_MASK, dict(mask=8)),
+    (L.MS_E_MASK, dict(mask=4, b=None)),
+    (L.MS_E_SHAPE, dict(x=tensor((M, D, 1)))),
+    (L.MS_E_SHAPE, dict(x=tensor((M, 0)))),
+    (L.MS_E_SHAPE, dict(x=tensor((M, D + 1)))),
+    (L.MS_E_SHAPE, dict(x=tensor((-1, D)))),
+    (L.MS_E_DTYPE, dict(x=tensor((M, D), "f32"))),
+    (L.MS_E_DTYPE, dict(x=tensor((M, D), 9))),
+    (L.MS_E_LAYOUT, dict(x=tensor((M, D), strides=(-D, 1)))),
+    (L.MS_E_LAYOUT, dict(b=tensor((V,), strides=(2,)))),
+]
+REFUSED = [(k, s, o) for k in KINDS for s, o in COMMON if not ("b" in o and o["b"] is not None)] + [
+    ("norm", L.MS_E_ARG, dict(eps=-1e-5)), ("norm", L.MS_E_ARG, dict(eps=float("nan"))), ("norm", L.MS_E_ARG, dict(eps=float("inf"))),
+    ("norm", L.MS_E_MASK, dict(W=None, mask=2)),
+    ("norm", L.MS_E_SHAPE, dict(W=tensor((D + 1,)))), ("norm", L.MS_E_SHAPE, dict(b=tensor((1, D)))),
+    ("norm", L.MS_E_DTYPE, dict(b=tensor((D,), "f32"))), ("norm", L.MS_E_LAYOUT, dict(W=tensor((D,), strides=(0,)))),
+    ("norm", L.MS_E_SHAPE, dict(y=tensor((M, D - 1)))), ("norm", L.MS_E_LAYOUT, dict(y=tensor((M, D), strides=(0, 1)))),
+    ("gated", L.MS_E_NULL, dict(W=None)), ("gated", L.MS_E_SHAPE, dict(W=tensor((2 * F + 1, D)))),
+    ("gated", L.MS_E_SHAPE, dict(W=tensor((0, D)))), ("gated", L.MS_E_SHAPE, dict(b=tensor((F,)))),
+    ("gated", L.MS_E_ARG, dict(act=-1)), ("gated", L.MS_E_ARG, dict(act=5)),
+    ("gated", L.MS_E_ARG, dict(mask=0)),                       # kept projections of no gradient
+    ("gated", L.MS_E_ARG, dict(proj=FAKE + 8)), ("gated", L.MS_E_LAYOUT, dict(b=tensor((2 * F,), strides=(2,)))),
+    ("gated", L.MS_E_UNSUPPORTED, dict(x=tensor((2 ** 26, D)), y=tensor((2 ** 26, F)))),
+    ("xent", L.MS_E_NULL, dict(W=None)), ("xent", L.MS_E_NULL, dict(target=None)), ("xent", L.MS_E_NULL, dict(lse=None)),
+    ("xent", L.MS_E_ARG, dict(target=FAKE + 4)), ("xent", L.MS_E_ARG, dict(reduction=3)), ("xent", L.MS_E_ARG, dict(reduction=-1)),
+    ("xent", L.MS_E_SHAPE, dict(W=tensor((0, D)))), ("xent", L.MS_E_SHAPE, dict(b=tensor((V + 1,)))),
+    ("xent", L.MS_E_DTYPE, dict(y=tensor((1,), "bf16"))), ("xent", L.MS_E_SHAPE, dict(y=tensor((M,), "f32"))),
+    ("xent", L.MS_E_SHAPE, dict(reduction=2)), ("xent", L.MS_E_LAYOUT, dict(reduction=2, y=tensor((M,), "f32", strides=(2,)))),
+    ("xent", L.MS_E_UNSUPPORTED, dict(x=tensor((2 ** 26, D)))),
+    ("xent", L.MS_E_UNSUPPORTED, dict(W=tensor((2 ** 26, D)), b=None, mask=1)),
+]
+
+
+@pytest.mark.parametrize("kind,status,over", REFUSED, ids=lambda v: v if isinstance(v, str) else "+".join(v) if isinstance(v, dict) else str(v))
+def test_refusals_launch_nothing(stub, kind, status, over):
+    c = Call(stub, kind, **over)
+    assert c.forward() == status, stub.ms_last_error()
+    assert not c.h.value and stub.blocks_log() == b"" and stub.stub_log() == b""
+
+
+@pytest.mark.parametrize("kind", KINDS)
+def test_backward_refusals_leave_the_record_usable(stub, kind):
+    c = Call(stub, kind)
+    assert c.forward() == 0
+    stub.blocks_reset()
+    rows = c.a["y"].shape[0]
+    assert c.backward(dy=None) == L.MS_E_NULL
+    assert c.backward(mask=3) == L.MS_E_MASK             # no place for a gradient that was asked for
+    bad = tensor((rows + 1,) + ((c.a["y"].shape[1],) if c.a["y"].ndim == 2 else ()), "f32" if kind == "xent" else "bf16")
+    assert c.backward(dy=bad) == L.MS_E_SHAPE
+    stub.ms_testing_fail_next_workspace(1)
+    assert c.backward() == L.MS_E_NOMEM
+    assert stub.blocks_log() == b""
+    assert c.backward() == 0
+    c.free()
+
+
+@pytest.mark.parametrize("kind", KINDS)
+def test_forward_without_memory(stub, kind):
+    c = Call(stub, kind, x=tensor((M, D), strides=(2 * D, 2)))   # (staged: the norm takes no other workspace)
+    stub.ms_testing_fail_next_workspace(1)
+    assert c.forward() == L.MS_E_NOMEM and not c.h.value
+    assert stub.blocks_log() == b"" and stub.stub_log() == b""
+    assert c.forward() == 0
+    c.free()
+
+
+@pytest.mark.parametrize("kind", KINDS)
+def test_other_layouts_are_staged(stub, kind):
+    y = {"norm": tensor((M, D), strides=(1, M)), "gated": tensor((M, F), strides=(1, M)), "xent": tensor((1,), "f32")}[kind]
+    c = Call(stub, kind, x=tensor((M, D), strides=(1, M)), y=y)
+    assert c.forward() == 0
+    copies = {"norm": 2, "gated": 2, "xent": 1}[kind]           # x in, y out
+    assert stub.stub_log() == b"copy4;" * copies
+    stub.stub_reset()
+    assert c.backward() == 0
+    assert stub.stub_log() == b"copy4;" * (copies + 1)           # dx out too
+    c.free()
+
+
+@pytest.mark.parametrize("kind", KINDS)
+def test_no_rows(stub, kind):
+    over = dict(x=tensor((0, D), addr=None))
+    if kind != "xent":
+        over["y"] = tensor((0, {"norm": D, "gated": F}[kind]), addr=None)
+    c = Call(stub, kind, **over)
+    assert c.forward() == 0 and c.backward() == 0
+    c.free()
+
+
+@pytest.mark.parametrize("kind", KINDS)
+def test_backward_from_the_fixed_scratch(stub, kind):
+    c = Call(stub, kind)
+    assert c.forward() == 0
+    stub.stub_reset()
+    stub.ms_testing_fail_next_workspace(1)
+    assert c.backward(entry="ms_layer_backward_noalloc") == 0
+    assert stub.stub_log() == b"scratch;"
+    stub.ms_testing_fail_next_workspace(0)
+    c.free()
