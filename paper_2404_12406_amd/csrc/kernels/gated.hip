@@ -121,7 +121,7 @@ __global__ __launch_bounds__(256) void grad24_kernel(const uint16_t *__restrict_
     }
 }
 
-// Up to kCopies copies at once (grid z): dst[r][0 .. dld) = src[r][0 .. cols) and
+// Up to kCopies copies at once (grid y): dst[r][0 .. dld) = src[r][0 .. cols) and
 // zeros for r < rows, zeros for r to drows (cols at most dld, or the other columns
 // are left out).
 struct Copies {
@@ -130,13 +130,22 @@ struct Copies {
 template <typename T>
 __global__ __launch_bounds__(256) void copy_rows_kernel(const Copies k) {
     constexpr int V = Vec16<T>::N;
-    const CopyJob &j = k.job[blockIdx.z];
+    const CopyJob &j = k.job[blockIdx.y];
     const T *src = (const T *)j.src;
     T *dst = (T *)j.dst;
-    const int cols = (int)min(j.cols, j.dld), dld = (int)j.dld;
-    for (int64_t r = blockIdx.y; r < j.drows; r += gridDim.y)
-        for (int c = ((int)blockIdx.x * 256 + (int)threadIdx.x) * V; c < dld; c += (int)gridDim.x * 256 * V)
-            store_vec(dst + r * dld, c, dld, r < j.rows && c < cols ? load_vec(src + r * j.sld, c, cols) : zero16<T>());
+    const int cols = (int)min(j.cols, j.dld), dld = (int)j.dld, per = (dld + V - 1) / V;
+    // (row, vector of the row) of this thread, moved on by whole steps of the grid
+    const int step = (int)gridDim.x * 256, dr = step / per, dc = step % per;
+    const int i = (int)blockIdx.x * 256 + (int)threadIdx.x;
+    int64_t r = i / per;
+    for (int c = i % per; r < j.drows; r += dr) {
+        store_vec(dst + r * dld, c * V, dld, r < j.rows && c * V < cols ? load_vec(src + r * j.sld, c * V, cols) : zero16<T>());
+        c += dc;
+        if (c >= per) {
+            c -= per;
+            ++r;
+        }
+    }
 }
 
 namespace {
@@ -242,19 +251,17 @@ int make_pads(const Pads &p, int dtype, int64_t M, int64_t D, int64_t F, char *b
 
 int launch_copy_rows(int dtype, const CopyJob *jobs, int n, void *stream) {
     gated::Copies k{};
-    int64_t rows = 0, cols = 0;
+    const int V = dtype == kBF16 ? 8 : 4;
+    int64_t most = 0;   // vectors of the largest
     int used = 0;
     for (int i = 0; i < n; ++i) {
         if (jobs[i].drows == 0 || jobs[i].dld == 0) continue;
         k.job[used++] = jobs[i];
-        rows = std::max(rows, jobs[i].drows);
-        cols = std::max(cols, jobs[i].dld);
+        most = std::max(most, jobs[i].drows * ((jobs[i].dld + V - 1) / V));
     }
     if (!used) return 0;
     hipStream_t st = (hipStream_t)stream;
-    const int V = dtype == kBF16 ? 8 : 4;
-    const int64_t gx = std::min<int64_t>((cols + 256 * V - 1) / (256 * V), 64);
-    const dim3 grid((unsigned)gx, (unsigned)std::max<int64_t>(1, std::min<int64_t>(rows, 4096 / gx)), (unsigned)used);
+    const dim3 grid((unsigned)std::min<int64_t>((most + 255) / 256, 4096), (unsigned)used);
     if (dtype == kBF16) hipLaunchKernelGGL(gated::copy_rows_kernel<bf16>, grid, dim3(256), 0, st, k);
     else hipLaunchKernelGGL(gated::copy_rows_kernel<float>, grid, dim3(256), 0, st, k);
     return (int)hipGetLastError();
