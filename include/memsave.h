@@ -175,10 +175,11 @@ typedef struct ms_record ms_record;
  * the layer output, which stock PyTorch's ReLU keeps; MS_SAVED_MASK8 (policy
  * accounting only): the one-byte-per-element mask stock PyTorch's dropout
  * keeps.  MS_SAVED_PROJ: a gated linear unit's projections.  MS_SAVED_LSE: a
- * cross entropy's log-sum-exp of each row (and its targets). */
+ * cross entropy's log-sum-exp of each row (and its targets).  MS_SAVED_GRAD: its
+ * input's gradient but for the loss's. */
 enum { MS_SAVED_X = 1u, MS_SAVED_W = 2u, MS_SAVED_MEAN = 4u, MS_SAVED_VAR = 8u, MS_SAVED_BITS = 16u,
        MS_SAVED_Y = 32u, MS_SAVED_MASK8 = 64u, MS_SAVED_PROJ = 128u,
-       MS_SAVED_LSE = 256u };
+       MS_SAVED_LSE = 256u, MS_SAVED_GRAD = 512u };
 
 /* Bits of ms_account.kernels: what the record's backward will launch. */
 enum { MS_K_DGRAD = 1u, MS_K_WGRAD = 2u, MS_K_BGRAD = 4u };
@@ -340,30 +341,45 @@ ms_status ms_gated_linear_forward(const ms_tensor *x, const ms_tensor *W, const 
                                   void *proj, uint32_t mask, const ms_tensor *y, ms_record **rec, void *stream);
 
 /*
+ * ms_cross_entropy_kept_bytes -- size of what ms_cross_entropy_forward() leaves in
+ * `kept` for these sizes and mask: a float a row (its log-sum-exp), or the gradient of
+ * x itself (see there): [rows, D] values of 4 bytes for MS_F32, of 3 for MS_BF16
+ * (fp32's leading 24 bits, as ms_gated_projection_bytes()'s).  0 with mask 0 or an
+ * extent that is not positive.
+ */
+uint64_t ms_cross_entropy_kept_bytes(int64_t rows, int64_t D, int64_t V, int32_t dtype, uint32_t mask);
+
+/*
  * ms_cross_entropy_forward -- the loss of a linear head, without its logits.
  *
  * z = x W^T + b;  row i with target t costs log(sum over v of exp(z_iv)) - z_it.
  * The logits of a large vocabulary outweigh every other activation of a model;
  * here they exist a tile at a time, and a record keeps of the softmax one number
  * a row: its log-sum-exp.  Backward takes the logits again, a piece of the
- * vocabulary at a time in transient workspace (at most 512 MiB of them):
+ * vocabulary at a time in transient workspace (about a gigabyte of them):
  *   dz = (exp(z - lse) - [v = t]) g,  dx = dz W,  dW = dz^T x,  db = sum of dz,
  * g the gradient of the row's share of the loss.
+ * With INPUT alone in the mask (a frozen head) and enough rows, features and words
+ * -- where ms_cross_entropy_kept_bytes() says more than a float a row -- the forward
+ * takes dx too, but for g, a chunk of rows at a time in transient workspace of the
+ * same size: two products instead of three.  The record then keeps that gradient and
+ * neither x nor W nor the targets, and backward multiplies it by g.
  * target: M contiguous int64 on the device.  Rows whose target is ignore_index
  * take no part, whatever x holds in them: their loss and their row of dx are 0.
  * Any other target outside [0, V) makes its loss NaN, and the gradients that it
  * reaches.  reduction: MS_REDUCE_MEAN over the rows that count (NaN where none
  * does, and no gradient), MS_REDUCE_SUM (loss[1]) or MS_REDUCE_NONE (loss[M]).
  * x[M, D], W[V, D]: any strides, D, V >= 1; b[V] contiguous or NULL.  loss: fp32,
- * contiguous.  With mask != 0, lse is caller-allocated device memory of M floats,
- * fully overwritten, and borrowed with x, W, b and target (every gradient needs
- * them all); with mask 0 it may be NULL.  dz is rounded to x's dtype before its
+ * contiguous.  With mask != 0, kept is caller-allocated device memory of
+ * ms_cross_entropy_kept_bytes(), 16-byte aligned, fully overwritten, and borrowed (a
+ * log-sum-exp with x, W, b and target, which every gradient then needs); with mask 0
+ * it may be NULL.  dz is rounded to x's dtype before its
  * products, everything else is in fp32.  Backward is ms_layer_backward() with
  * grad_y of the loss's shape, fp32.  ms_layer_forward() rejects MS_CROSS_ENTROPY
  * (MS_E_ARG).
  */
 ms_status ms_cross_entropy_forward(const ms_tensor *x, const ms_tensor *W, const ms_tensor *b, const int64_t *target,
-                                   int64_t ignore_index, int32_t reduction, float *lse, uint32_t mask, const ms_tensor *loss,
+                                   int64_t ignore_index, int32_t reduction, void *kept, uint32_t mask, const ms_tensor *loss,
                                    ms_record **rec, void *stream);
 
 /*

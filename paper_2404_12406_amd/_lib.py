@@ -30,6 +30,7 @@ EXPORTS = (
     "ms_dropout_blocks", "ms_dropout_forward", "ms_layer_backward_noalloc", "ms_noalloc_scratch_bytes",
     "ms_testing_gemm_plan", "ms_testing_float_plan",
     "ms_layer_norm_forward", "ms_gated_linear_forward", "ms_gated_projection_bytes", "ms_cross_entropy_forward",
+    "ms_cross_entropy_kept_bytes",
 )
 MS_PROF_FWD, MS_PROF_DGRAD, MS_PROF_WGRAD, MS_PROF_BN, MS_PROF_ACT, MS_PROF_RED = 1, 2, 4, 8, 16, 32
 
@@ -128,6 +129,8 @@ def configure(lib: ctypes.CDLL) -> ctypes.CDLL:
         lib.ms_cross_entropy_forward.restype = ctypes.c_int
         lib.ms_gated_projection_bytes.argtypes = [ctypes.c_int64, ctypes.c_int64, ctypes.c_int32]
         lib.ms_gated_projection_bytes.restype = ctypes.c_uint64
+        lib.ms_cross_entropy_kept_bytes.argtypes = [ctypes.c_int64, ctypes.c_int64, ctypes.c_int64, ctypes.c_int32, ctypes.c_uint32]
+        lib.ms_cross_entropy_kept_bytes.restype = ctypes.c_uint64
     return lib
 
 

@@ -127,8 +127,10 @@ class LinearCrossEntropy:
     or None, without the logits: loss[1] (reduction "mean" over the rows whose
     target is not ignore_index, or "sum") or loss[M] ("none"), float32.
     target: int64 [M], each a word in [0, V) or ignore_index.  Its record keeps
-    x, the targets and one number a row.  layer_backward takes the gradient of
-    the loss, float32 in its shape."""
+    x, the targets and one number a row; with the INPUT bit alone (a frozen head)
+    and all but small sizes, the gradient of x in their place, which
+    the forward then takes.  layer_backward takes the gradient of the loss, float32
+    in its shape."""
     target: torch.Tensor
     ignore_index: int = -100
     reduction: str = "mean"
@@ -507,16 +509,21 @@ def _block_call(spec, x, W, b, mask, y):
         raise ValueError("target must have one element a row of x")
     _one_gpu(x, t)
     t = t.contiguous()
-    lse = None
+    buf = None
     if mask:
-        lse = kept["lse"] = torch.empty(x.shape[0], dtype=torch.float32, device=x.device)
-        kept["target"] = t
-        if b is not None:
-            kept["b"] = b
+        M = x.shape[0]
+        n = _lib.load().ms_cross_entropy_kept_bytes(M, x.shape[1], W.shape[0], _DT.get(x.dtype, 0), mask)
+        if n > 4 * M:   # the gradient itself: nothing else is needed
+            buf = kept["grad"] = torch.empty(n, dtype=torch.uint8, device=x.device)
+        else:
+            buf = kept["lse"] = torch.empty(M, dtype=torch.float32, device=x.device)
+            kept["target"] = t
+            if b is not None:
+                kept["b"] = b
     if y is None:
         y = torch.empty(x.shape[0] if red == 2 else 1, dtype=torch.float32, device=x.device)
     args = (_packed(x), _packed(W), _packed(b), t.data_ptr() or None, int(spec.ignore_index), red,
-            (lse.data_ptr() or None) if lse is not None else None, mask, _packed(y))
+            (buf.data_ptr() or None) if buf is not None else None, mask, _packed(y))
     return y, "ms_cross_entropy_forward", args, kept, t
 
 

@@ -181,6 +181,17 @@ ms_status xent_backward(ms_record *r, const ms_tensor *gloss, const ms_tensor *g
                         void *stream, bool fixed) {
     const int32_t dt = r->plan.dtype;
     const int64_t M = r->blk.M, D = r->blk.D, V = r->blk.F;
+    if (r->blk.grad) {
+        Stager sg;
+        const size_t ogx = sg.add(gx);
+        Work w;
+        ms_status st = take(&w, sg.bytes, stream, fixed);
+        if (st) return st;
+        int err = ms::launch_xent_scale(dt, M, D, r->blk.grad, static_cast<const float *>(gloss->data), r->blk.reduction,
+                                        kptr(gx, w.base, ogx), stream);
+        if (!err) err = stage_out(gx, w.base, ogx, stream);
+        return err ? hip_fail(err, "backward launch") : MS_OK;
+    }
     Stager sg;
     const size_t ox = sg.add(&r->x), ow = sg.add(&r->W), ogx = gx ? sg.add(gx) : kNoStage, ogw = gw ? sg.add(gw) : kNoStage;
     const HeadPads p = head_pads(dt, D, place(&r->W, ow), r->b.data);
@@ -320,8 +331,15 @@ ms_status ms_gated_linear_forward(const ms_tensor *x, const ms_tensor *W, const 
     return MS_OK;
 }
 
+uint64_t ms_cross_entropy_kept_bytes(int64_t rows, int64_t D, int64_t V, int32_t dtype, uint32_t mask) {
+    if (rows <= 0 || D <= 0 || V <= 0 || !(mask & 7u)) return 0;
+    if (ms::xent_keeps_gradient(dtype, rows, D, V, mask & MS_RG_INPUT, mask & MS_RG_WEIGHT, mask & MS_RG_BIAS))
+        return ms::xent_kept_bytes(dtype, rows, D);
+    return (uint64_t)rows * sizeof(float);
+}
+
 ms_status ms_cross_entropy_forward(const ms_tensor *x, const ms_tensor *W, const ms_tensor *b, const int64_t *target,
-                                   int64_t ignore_index, int32_t reduction, float *lse, uint32_t mask, const ms_tensor *loss,
+                                   int64_t ignore_index, int32_t reduction, void *kept, uint32_t mask, const ms_tensor *loss,
                                    ms_record **rec, void *stream) {
     clear_err();
     if (!rec) return fail(MS_E_NULL, "rec is NULL");
@@ -349,38 +367,48 @@ ms_status ms_cross_entropy_forward(const ms_tensor *x, const ms_tensor *W, const
     const int64_t n = reduction == MS_REDUCE_NONE ? M : 1;
     if (loss->shape[0] != n) return fail(MS_E_SHAPE, "loss must have %lld elements", (long long)n);
     if (!is_contig1(loss)) return fail(MS_E_LAYOUT, "loss must be contiguous");
-    if (mask && M > 0 && !lse) return fail(MS_E_NULL, "lse is NULL but gradients are asked for");
+    if (mask && M > 0 && !kept) return fail(MS_E_NULL, "kept is NULL but gradients are asked for");
+    if (mask && !aligned(kept, 16)) return fail(MS_E_ARG, "kept must be 16-byte aligned");
+    const bool grad = ms::xent_keeps_gradient(x->dtype, M, D, V, mask & MS_RG_INPUT, mask & MS_RG_WEIGHT, mask & MS_RG_BIAS);
+    float *lse = mask && !grad ? static_cast<float *>(kept) : nullptr;
     Stager sg;
     const size_t ox = sg.add(x), ow = sg.add(W);
     const HeadPads p = head_pads(x->dtype, D, place(W, ow), b ? b->data : nullptr);
-    const size_t kb = ms::xent_fwd_workspace(x->dtype, M, D, V, p.w, p.b, reduction);
+    const size_t kb = ms::xent_fwd_workspace(x->dtype, M, D, V, p.w, p.b, reduction, grad);
     Work w;
     if ((st = take(&w, sg.bytes + kb, stream, false))) return st;
     ms_record *r = nullptr;
     if (mask) {
-        r = new_record(MS_CROSS_ENTROPY, x, W, b, loss, mask, MS_SAVED_X | MS_SAVED_W | MS_SAVED_LSE, xent_backward);
+        r = new_record(MS_CROSS_ENTROPY, x, W, b, loss, mask, grad ? (uint32_t)MS_SAVED_GRAD : MS_SAVED_X | MS_SAVED_W | MS_SAVED_LSE,
+                       xent_backward);
         if (!r) return fail(MS_E_NOMEM, "record allocation failed");
         r->blk.M = M;
         r->blk.D = D;
         r->blk.F = V;
         r->blk.reduction = reduction;
-        r->blk.ignore = ignore_index;
-        r->blk.target = target;
-        r->blk.lse = lse;
-        if (b) {
-            r->b.data = b->data;
-            r->acct.referenced_param_bytes += bytes_of(b);
+        if (grad) {
+            r->blk.grad = kept;
+            r->acct.saved_activation_bytes = ms::xent_kept_bytes(x->dtype, M, D);
+            r->acct.transient_workspace_bytes = staging(x, true);
+        } else {
+            r->blk.ignore = ignore_index;
+            r->blk.target = target;
+            r->blk.lse = lse;
+            if (b) {
+                r->b.data = b->data;
+                r->acct.referenced_param_bytes += bytes_of(b);
+            }
+            r->acct.saved_activation_bytes += (uint64_t)M * (sizeof(float) + sizeof(int64_t));
+            const bool dx = mask & MS_RG_INPUT, dw = mask & MS_RG_WEIGHT, db = mask & MS_RG_BIAS;
+            r->acct.transient_workspace_bytes = ms::xent_bwd_workspace(x->dtype, M, D, V, p.w, p.b, dx, dw, db) + staging(x, true) +
+                                                staging(W, true) + staging(x, dx) + staging(W, dw);
         }
-        r->acct.saved_activation_bytes += (uint64_t)M * (sizeof(float) + sizeof(int64_t));
-        const bool dx = mask & MS_RG_INPUT, dw = mask & MS_RG_WEIGHT, db = mask & MS_RG_BIAS;
-        r->acct.transient_workspace_bytes = ms::xent_bwd_workspace(x->dtype, M, D, V, p.w, p.b, dx, dw, db) + staging(x, true) +
-                                            staging(W, true) + staging(x, dx) + staging(W, dw);
     }
     int err = stage_in(x, w.base, ox, stream);
     if (!err) err = stage_in(W, w.base, ow, stream);
     if (!err)
         err = ms::launch_xent_fwd(x->dtype, M, D, V, kptr(x, w.base, ox), kptr(W, w.base, ow), b ? b->data : nullptr, p.w, p.b, target,
-                                  ignore_index, reduction, static_cast<float *>(loss->data), mask ? lse : nullptr,
+                                  ignore_index, reduction, static_cast<float *>(loss->data), lse, grad ? kept : nullptr,
                                   w.base + sg.bytes, stream);
     if (err) {
         delete r;

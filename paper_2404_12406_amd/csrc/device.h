@@ -186,14 +186,20 @@ int launch_linear_bwd(int dtype, int64_t M, int64_t K, int64_t N, const int *cou
 // forward) is what the backward needs.  padw, padb: bf16 weight rows that are no
 // whole 16-byte vectors or not so aligned, a bias not 4-byte aligned (they are
 // copied).  In the backward any of dx, dw, db may be null; gloss is the gradient of
-// the loss, fp32.
-size_t xent_fwd_workspace(int dtype, int64_t M, int64_t D, int64_t V, bool padw, bool padb, int reduction);
+// the loss, fp32.  Where xent_keeps_gradient(), the forward takes `kept` of
+// xent_kept_bytes(), dx but for the loss's gradient (and no lse), and the backward is
+// launch_xent_scale().
+bool xent_keeps_gradient(int dtype, int64_t M, int64_t D, int64_t V, bool dx, bool dw, bool db);
+size_t xent_kept_bytes(int dtype, int64_t M, int64_t D);
+size_t xent_fwd_workspace(int dtype, int64_t M, int64_t D, int64_t V, bool padw, bool padb, int reduction, bool keep);
 int launch_xent_fwd(int dtype, int64_t M, int64_t D, int64_t V, const void *x, const void *w, const void *b, bool padw, bool padb,
-                    const int64_t *target, int64_t ignore, int reduction, float *loss, float *lse, void *ws, void *stream);
+                    const int64_t *target, int64_t ignore, int reduction, float *loss, float *lse, void *kept, void *ws,
+                    void *stream);
 size_t xent_bwd_workspace(int dtype, int64_t M, int64_t D, int64_t V, bool padw, bool padb, bool dx, bool dw, bool db);
 int launch_xent_bwd(int dtype, int64_t M, int64_t D, int64_t V, const void *x, const void *w, const void *b, bool padw, bool padb,
                     const int64_t *target, int64_t ignore, int reduction, const float *gloss, const float *lse, void *dx, void *dw,
                     void *db, void *ws, void *stream);
+int launch_xent_scale(int dtype, int64_t M, int64_t D, const void *kept, const float *gloss, int reduction, void *dx, void *stream);
 
 // Global average pool x[N][L][C] -> y[N][C] and its adjoint.
 int launch_avgpool_fwd(int dtype, const void *x, int N, int L, int C, void *y, void *stream);

@@ -83,6 +83,19 @@ __device__ __forceinline__ floatx2 join_lse(floatx2 a, floatx2 b) {
     return floatx2{m, sa + sb};
 }
 
+// Columns of one statistic and reference of exponentials that are kept.
+constexpr int kProbCols = 64;
+
+// The reference r of the kept exponentials exp(v - r) of values whose largest is
+// top: a multiple of 64 ln 2 that leaves that one between 2^-16 and 2^48.  Parts of
+// a row nearly always agree on it; where they do not, their factor is a power of
+// two, by which the exponentials, rounded to bf16 already, are multiplied without
+// another error.  Far from zero, where such multiples are not exact, top itself.
+__device__ __forceinline__ float prob_ref(float top) {
+    constexpr float kStep = 44.3614195558364998f;
+    return fabsf(top) < 1e6f ? kStep * floorf((top + 11.f) * (1.f / kStep)) : top;
+}
+
 namespace act {
 
 // FAST: on the hardware's exponential and reciprocal (each within some 2 units

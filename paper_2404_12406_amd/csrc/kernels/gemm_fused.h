@@ -8,6 +8,9 @@
 //                 exponentials of each row's part of a column tile, and the
 //                 target's logit; z is not written
 //   kEpiXent      z again, then dz = (exp(z - lse) - [column = target]) scale
+//   kEpiProb      z, then exp(z - r) of the other words than the target, r a
+//                 reference of each row's part of a wave's columns, with those parts'
+//                 sums of exponentials and the target's logit
 //   kEpiAdd       dx += dz W for one piece of the vocabulary, in fp32
 //   kEpiStore     the weight gradient dz^T x over the rows that count, times a factor
 // The main loop is gemm_block_body.inc's.  Everything before the one rounding
@@ -25,7 +28,7 @@
 namespace ms {
 namespace g2 {
 
-enum Epi { kEpiStore = 0, kEpiGate = 1, kEpiGateGrad = 2, kEpiLse = 3, kEpiXent = 4, kEpiAdd = 5 };
+enum Epi { kEpiStore = 0, kEpiGate = 1, kEpiGateGrad = 2, kEpiLse = 3, kEpiXent = 4, kEpiAdd = 5, kEpiProb = 6 };
 
 struct FusedArgs : Args {
     const int *count;      // rows that count (weight gradient: of the reduction), on the device; null: all
@@ -38,8 +41,8 @@ struct FusedArgs : Args {
     // cross entropy; rows are those that count
     const int *target;     // each row's target in the vocabulary
     int v0;                // the piece's first word
-    floatx2 *stat;         // kEpiLse: softmax statistics as join_lse()'s, [column tile][rows]
-    float *tlogit;         // kEpiLse: the target's logit
+    floatx2 *stat;         // kEpiLse, kEpiProb: softmax statistics as join_lse()'s, [column tile][rows], [64 columns][rows]
+    float *tlogit;         // with them: the target's logit
     int64_t stat_ld;
     const float *lse, *scale;   // kEpiXent: of each row
     const float *out_scale;     // kEpiStore: the sums' factor
@@ -129,7 +132,7 @@ __device__ __forceinline__ void put_bytes(uint8_t *stage, const uint32_t (&b)[TG
 // Loaded before the operands' first loads are issued, put into the sums after.
 template <int EPI, class G>
 struct FusedInit {
-    static constexpr bool GATED = EPI == kEpiGate || EPI == kEpiGateGrad, SOFTMAX = EPI == kEpiLse || EPI == kEpiXent;
+    static constexpr bool GATED = EPI == kEpiGate || EPI == kEpiGateGrad, SOFTMAX = EPI == kEpiLse || EPI == kEpiXent || EPI == kEpiProb;
     float b[G::TN][4][4];
 
     __device__ __forceinline__ FusedInit(const FusedArgs &P, int n0, int wn0, int lane) {
@@ -275,7 +278,7 @@ __device__ __forceinline__ void fused_epilogue(const FusedArgs &P, char *smem, f
             }
             stage_order();
         }
-    } else if constexpr (EPI == kEpiLse || EPI == kEpiXent) {
+    } else if constexpr (EPI == kEpiLse || EPI == kEpiXent || EPI == kEpiProb) {
         // the rows' values, every pass's loads in flight at once
         int tgt[TM];
         float lse[EPI == kEpiXent ? TM : 1], scale[EPI == kEpiXent ? TM : 1];
@@ -334,6 +337,50 @@ __device__ __forceinline__ void fused_epilogue(const FusedArgs &P, char *smem, f
 #pragma unroll
                 for (int w = 1; w < WC; ++w) a = join_lse(a, red[w * BM + r]);
                 P.stat[(int64_t)tn * P.stat_ld + m0 + r] = a;
+            }
+        } else if constexpr (EPI == kEpiProb) {
+            static_assert(G::WN == kProbCols, "statistics of 64 columns");
+            constexpr int PITCH = G::EPI_PITCH;
+            const int ncol = min(P.ldc - (n0 + wn0), G::WN);   // the padding columns are zeros
+#pragma unroll
+            for (int i = 0; i < TM; ++i) {
+                __builtin_amdgcn_sched_barrier(0);   // one pass at a time: the sums leave few registers
+                const int mb = m0 + wm0 + 32 * i, m = mb + fr;
+                float top = -INFINITY;
+#pragma unroll
+                for (int j = 0; j < TN; ++j)
+#pragma unroll
+                    for (int v = 0; v < 16; ++v) top = fmaxf(top, acc[i][j][v]);
+                const float r = prob_ref(fmaxf(top, __shfl_xor(top, 32)));
+                const float t0 = r == -INFINITY ? 0.f : r;
+                const int t = m < M ? tgt[i] - (n0 + wn0) : -1;
+                const bool any = __any((unsigned)t < (unsigned)G::WN);
+                float s = 0.f, z = 0.f;
+                bool mine = false;
+#pragma unroll
+                for (int j = 0; j < TN; ++j)
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) {
+                        bf16x4 o;
+#pragma unroll
+                        for (int v = 0; v < 4; ++v) {
+                            float p = exp_below(acc[i][j][4 * q + v], t0);
+                            s += p;
+                            if (any && t == 32 * j + 8 * q + 4 * fh + v) {
+                                z = acc[i][j][4 * q + v];
+                                mine = true;
+                                p = 0.f;
+                            }
+                            o[v] = (bf16)p;
+                        }
+                        *reinterpret_cast<bf16x4 *>(stage + fr * PITCH + 32 * j + 8 * q + 4 * fh) = o;
+                    }
+                s += __shfl_xor(s, 32);
+                if (fh == 0 && m < M) P.stat[(int64_t)((n0 + wn0) / G::WN) * P.stat_ld + m] = floatx2{r, s};
+                if (mine && n0 + wn0 + t < N) P.tlogit[m] = z;
+                stage_order();
+                store_rows<G::WN>(stage, PITCH, P.c + (int64_t)mb * P.ldc + n0 + wn0, P.ldc, M - mb, ncol, lane);
+                stage_order();
             }
         } else {
             constexpr int PITCH = G::EPI_PITCH;

@@ -58,6 +58,29 @@ int xent_grad(int64_t M, int64_t D, int64_t V, const void *x, const void *w, con
     return go_rows<kEpiXent>(p.tile, kProfFwd, a, st);
 }
 
+// Statistics of 64 columns each (rows of xent_prob()'s `stat`).
+int xent_prob_parts(int64_t M, int64_t D, int64_t V) {
+    const Tile &t = kRowTiles[plan(kRowTiles, 2, M, V, D, 1).tile];
+    return (int)((V + t.bn - 1) / t.bn) * (t.bn / kProbCols);
+}
+
+// prob[M][ldz] = exp(z - r) for the words that are not the row's target, zeros there
+// and in columns V .. ldz - 1; r and the sums (the target's among them) go to stat.
+int xent_prob(int64_t M, int64_t D, int64_t V, const void *x, const void *w, const void *bias, const int *count, const int *target,
+              void *stat, int64_t stat_ld, float *tlogit, void *prob, int64_t ldz, hipStream_t st) {
+    const FusedPlan p = plan(kRowTiles, 2, M, V, D, 1);
+    FusedArgs a = rows_args(kRowTiles[p.tile], M, V, D, x, w, V);
+    a.fbias = (const bf16 *)bias;
+    a.count = count;
+    a.target = target;
+    a.stat = (floatx2 *)stat;
+    a.stat_ld = stat_ld;
+    a.tlogit = tlogit;
+    a.c = (bf16 *)prob;
+    a.ldc = (int)ldz;
+    return go_rows<kEpiProb>(p.tile, kProfFwd, a, st);
+}
+
 namespace {
 int dx_tile(int64_t M, int64_t D, int64_t V) { return plan(kGradTiles, 3, M, D, V, (int)std::clamp<int64_t>(V / (4 * BK), 1, 16)).tile; }
 }  // namespace

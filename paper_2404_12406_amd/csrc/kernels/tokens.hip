@@ -241,8 +241,9 @@ __global__ __launch_bounds__(1024) void loss_kernel(const floatx2 *__restrict__ 
             float l = 0.f, c = 0.f;
             if (t != ignore) {
                 const bool word = t >= 0 && t < V;
-                l = !word || a.x == -INFINITY ? NAN : a.x + logf(a.y);
-                c = l - (word ? tlogit[m] : 0.f);
+                const float ls = !word || a.x == -INFINITY ? NAN : logf(a.y);
+                l = a.x + ls;
+                c = (a.x - (word ? tlogit[m] : 0.f)) + ls;   // (the difference first: it is exact where both are large)
             }
             if (lse) lse[m] = l;
             if (reduction == 2) loss[m] = c;

@@ -7,12 +7,20 @@
 //    first (their number stays on the device and bounds every contraction), so
 //    that whatever an ignored row holds, NaN included, reaches no result, and a
 //    prompt costs nothing.
-//  * bf16: the contraction's epilogue (gemm_fused.hip) leaves, per row and column
+//  * bf16: the contraction's epilogue (gemm_xent.hip) leaves, per row and column
 //    tile, the maximum and the sum of exponentials; combine_kernel joins them.
 //    Backward goes over the vocabulary in pieces of at most kPieceBytes of dz:
 //    z again, dz from its epilogue, dx added up in fp32, dW whole.
 //  * fp32: the same steps on the fp32 contraction, z a piece at a time in
 //    workspace and the softmax's passes by the row kernels below.
+//  * dx alone (a frozen head) is taken in the forward, while the exponentials are
+//    at hand, and kept in place of x: two contractions in all instead of three.  It
+//    is dx without the loss's gradient, which backward multiplies it by.  bf16: by
+//    chunks of rows, whose exponentials p = exp(z - r) are written as bf16 beside
+//    their sums, r a reference that adjust_kernel() then makes one of each row:
+//      dx = (1 / sum) p W - (1 - p_t) W_t
+//    with the target's p left out of p W, so that what is left of it at a large
+//    p_t is no difference of rounded numbers.
 // Exponentials are of differences from a maximum or an lse, which no logit of
 // any size overflows; a row's lse is kept in fp32.
 #include <algorithm>
@@ -28,6 +36,9 @@ int xent_lse(int64_t M, int64_t D, int64_t V, const void *x, const void *w, cons
              void *stat, float *tlogit, hipStream_t st);
 int xent_grad(int64_t M, int64_t D, int64_t V, const void *x, const void *w, const void *bias, const int *count, const int *target,
               int v0, const float *lse, const float *scale, void *dz, int64_t ldz, hipStream_t st);
+int xent_prob_parts(int64_t M, int64_t D, int64_t V);
+int xent_prob(int64_t M, int64_t D, int64_t V, const void *x, const void *w, const void *bias, const int *count, const int *target,
+              void *stat, int64_t stat_ld, float *tlogit, void *prob, int64_t ldz, hipStream_t st);
 SplitRule xent_dx_rule(int64_t M, int64_t D, int64_t V);
 int xent_dx(int64_t M, int64_t D, int64_t V, int64_t ldz, int64_t piece, const void *dz, const void *w, const int *count,
             const int *nsplit, float *part, bool add, hipStream_t st);
@@ -101,16 +112,23 @@ __global__ __launch_bounds__(1024) void rows_kernel(const int64_t *__restrict__ 
 // factor of the row's dz, scale[i], and one of all results, scale[M].  Where it is
 // the same for every row (mean, sum) it stays out of dz: that is rounded, and a
 // common factor would give every row's largest entry, near -1 times it, the same
-// rounding error.
+// rounding error.  With nsplit: the splits of dx's contraction for each chunk of
+// `chunk` rows, and (ccount) the chunks' numbers of rows.
 template <typename T>
 __global__ __launch_bounds__(256) void gather_kernel(const T *__restrict__ x, const int *__restrict__ idx,
                                                      const int *__restrict__ count, int64_t M, int D, int ld, bool fill,
                                                      T *__restrict__ xc, const float *__restrict__ lse,
                                                      const float *__restrict__ gloss, int reduction, float *__restrict__ lsec,
-                                                     float *__restrict__ scale, SplitRule rule, int *__restrict__ nsplit) {
+                                                     float *__restrict__ scale, SplitRule rule, int *__restrict__ nsplit,
+                                                     int64_t chunk, int *__restrict__ ccount) {
     constexpr int V = Vec16<T>::N;
     const int n = *count;
-    if (nsplit && blockIdx.x == 0 && threadIdx.x == 64) *nsplit = rule.splits(n);
+    if (nsplit && blockIdx.x == 0)
+        for (int64_t k = (int)threadIdx.x; k * chunk < M; k += 256) {
+            const int rows = (int)min(max(n - k * chunk, (int64_t)0), chunk);
+            nsplit[k] = rule.splits(rows);
+            if (ccount) ccount[k] = rows;
+        }
     // (no row that counts: every result is an empty sum, whatever the factor)
     if (lse && blockIdx.x == 0 && threadIdx.x == 0)
         scale[M] = reduction == 2 || n == 0 ? 1.f : reduction == 1 ? gloss[0] : gloss[0] / (float)n;
@@ -126,37 +144,55 @@ __global__ __launch_bounds__(256) void gather_kernel(const T *__restrict__ x, co
     }
 }
 
-// The loss and lse of every row from `parts` statistics [part][M] of the rows
-// that count (32 rows a block, eight threads each).
-__global__ __launch_bounds__(256) void combine_kernel(const floatx2 *__restrict__ stat, int parts, const float *__restrict__ tlogit,
-                                                      const int *__restrict__ pos, const int *__restrict__ tgt, int64_t M,
-                                                      float *__restrict__ each, float *__restrict__ lse) {
+// What dx needs of a row that counts, by its place: the reference of its
+// exponentials, 1 / their sum, and the coefficient -(1 - p_t) of W_t.
+struct Kept {
+    float *ref, *f, *ct;
+};
+
+// The loss and lse of every row from `parts` statistics [part][ld] of the rows that
+// count, of which this launch has those from place i0 to i0 + ld - 1 (32 rows a
+// block, eight threads each).
+__global__ __launch_bounds__(256) void combine_kernel(const floatx2 *__restrict__ stat, int parts, int64_t ld, int64_t i0,
+                                                      const float *__restrict__ tlogit, const int *__restrict__ pos,
+                                                      const int *__restrict__ tgt, int64_t M, float *__restrict__ each,
+                                                      float *__restrict__ lse, Kept kept) {
     __shared__ floatx2 red[8][32];
     const int row = threadIdx.x & 31, grp = threadIdx.x >> 5;
     const int64_t r = (int64_t)blockIdx.x * 32 + row;
     const int i = r < M ? pos[r] : -1;
+    const bool here = i >= i0 && i < i0 + ld;
     floatx2 a = {-INFINITY, 0.f};
-    if (i >= 0) {
+    if (here) {
+        const floatx2 *s = stat + (i - i0);
         int p = grp;
         for (; p + 24 < parts; p += 32) {
             floatx2 v[4];
 #pragma unroll
-            for (int u = 0; u < 4; ++u) v[u] = stat[(int64_t)(p + 8 * u) * M + i];
+            for (int u = 0; u < 4; ++u) v[u] = s[(int64_t)(p + 8 * u) * ld];
 #pragma unroll
             for (int u = 0; u < 4; ++u) a = join_lse(a, v[u]);
         }
-        for (; p < parts; p += 8) a = join_lse(a, stat[(int64_t)p * M + i]);
+        for (; p < parts; p += 8) a = join_lse(a, s[(int64_t)p * ld]);
     }
     red[grp][row] = a;
     __syncthreads();
-    if (grp != 0 || r >= M) return;
+    if (grp != 0 || r >= M || (i >= 0 && !here)) return;
 #pragma unroll
     for (int q = 1; q < 8; ++q) a = join_lse(a, red[q][row]);
     float l = 0.f, loss = 0.f;
     if (i >= 0) {
         // no word at all, or every one of them minus infinity: no distribution
-        l = tgt[i] < 0 || a.x == -INFINITY ? NAN : a.x + logf(a.y);
-        loss = l - (tgt[i] < 0 ? 0.f : tlogit[i]);
+        const bool none = tgt[i] < 0 || a.x == -INFINITY;
+        const float ls = none ? NAN : logf(a.y);
+        l = a.x + ls;
+        // (the difference first: it is exact where both are large)
+        loss = (a.x - (tgt[i] < 0 ? 0.f : tlogit[i])) + ls;
+        if (kept.ref) {
+            kept.ref[i] = a.x;
+            kept.f[i] = none ? NAN : 1.f / a.y;
+            kept.ct[i] = expm1f(-loss);
+        }
     }
     if (lse) lse[r] = l;
     each[r] = loss;
@@ -175,6 +211,109 @@ __global__ __launch_bounds__(1024) void total_kernel(const float *__restrict__ e
     if (threadIdx.x != 0) return;
     for (int w = 1; w < 16; ++w) s += red[w];
     *out = (float)(mean ? s / (double)*count : s);
+}
+
+// prob[i][64 g ..] *= exp(r - ref[i]) where part g of row i has another reference r.
+__global__ __launch_bounds__(256) void adjust_kernel(bf16 *__restrict__ prob, int64_t ldz, const int *__restrict__ count,
+                                                     const floatx2 *__restrict__ stat, int64_t ld, int parts,
+                                                     const float *__restrict__ ref) {
+    const int i = (int)blockIdx.x * 256 + (int)threadIdx.x;
+    if (i >= *count) return;
+    const float to = ref[i];
+    for (int g = blockIdx.y; g < parts; g += gridDim.y) {
+        const float r = stat[(int64_t)g * ld + i].x;
+        if (r == to || r == -INFINITY) continue;   // (nothing but zeros there)
+        const float f = exp_below(r, to);
+        bf16 *p = prob + i * ldz + g * kProbCols;
+        for (int c = 0; c < kProbCols && g * kProbCols + c < ldz; c += 8) {
+            Vec16<bf16> v = load16(p + c);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v.e[e] = from_f32<bf16>(to_f32(v.e[e]) * f);
+            *reinterpret_cast<u32x4 *>(p + c) = v.u;
+        }
+    }
+}
+
+// The kept gradient of the rows at places i0 .. i0 + chunk - 1, and zeros (by the first
+// chunk's launch) for the rows that do not count: the sum of the partials, with f
+// times it and ct times the target's row of w; over their number where the loss is
+// the mean.  bf16: in 24 bits, a plane [M][D] of the leading 16 and one of the others
+// (rounded once more when backward has multiplied it: 2^-17 does not show).
+template <typename T>
+__global__ __launch_bounds__(256) void keep_kernel(const float *__restrict__ part, const int *__restrict__ nsplit, int64_t stride,
+                                                   const int *__restrict__ pos, int64_t M, int D, int ld, int64_t i0, int64_t chunk,
+                                                   const int *__restrict__ count, bool mean, const float *__restrict__ f,
+                                                   const float *__restrict__ ct, const int *__restrict__ tgt, const T *__restrict__ w,
+                                                   void *__restrict__ kept) {
+    constexpr int V = Vec16<T>::N;
+    const int splits = nsplit ? *nsplit : 1;
+    const float all = mean ? 1.f / (float)*count : 1.f;
+    for (int64_t r = blockIdx.x; r < M; r += gridDim.x) {
+        const int i = pos[r];
+        if (i < 0 ? i0 > 0 : i < i0 || i >= i0 + chunk) continue;
+        const int t = i < 0 || !f ? -1 : tgt[i];
+        for (int c = (int)threadIdx.x * V; c < D; c += 256 * V) {
+            float s[V];
+#pragma unroll
+            for (int e = 0; e < V; ++e) s[e] = 0.f;
+            if (i >= 0) {
+                for (int z = 0; z < splits; ++z) {
+#pragma unroll
+                    for (int h = 0; h < V / 4; ++h) {
+                        const Vec16<float> p = load_vec(part + z * stride + (i - i0) * ld, c + 4 * h, ld);
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) s[4 * h + e] += p.e[e];
+                    }
+                }
+                if (f) {
+                    const Vec16<T> wt = t >= 0 ? load_vec(w + (int64_t)t * ld, c, ld) : zero16<T>();
+#pragma unroll
+                    for (int e = 0; e < V; ++e) s[e] = s[e] * f[i] + ct[i] * to_f32(wt.e[e]);
+                }
+#pragma unroll
+                for (int e = 0; e < V; ++e) s[e] *= all;   // (not for a row that does not count: it may be that none does)
+            }
+            if constexpr (V == 8) {
+                Vec16<bf16> hi;
+                uint8_t *lo = (uint8_t *)kept + 2 * M * D + r * D + c;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const uint32_t u = to_f24(s[e]);
+                    hi.e[e] = __builtin_bit_cast(bf16, (uint16_t)(u >> 8));
+                    if (c + e < D) lo[e] = (uint8_t)u;
+                }
+                store_vec((bf16 *)kept + r * D, c, D, hi);
+            } else {
+                Vec16<float> o;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) o.e[e] = s[e];
+                store_vec((float *)kept + r * D, c, D, o);
+            }
+        }
+    }
+}
+
+// dx = the kept gradient times the loss's.
+template <typename T>
+__global__ __launch_bounds__(256) void scale_kernel(const void *__restrict__ kept, int64_t M, int D, const float *__restrict__ gloss,
+                                                    bool each, T *__restrict__ dx) {
+    constexpr int V = Vec16<T>::N;
+    for (int64_t r = blockIdx.x; r < M; r += gridDim.x) {
+        const float g = gloss[each ? r : 0];
+        for (int c = (int)threadIdx.x * V; c < D; c += 256 * V) {
+            Vec16<T> o = load_vec((const T *)kept + r * D, c, D);
+            const uint8_t *lo = (const uint8_t *)kept + 2 * M * D + r * D + c;
+#pragma unroll
+            for (int e = 0; e < V; ++e) {
+                float v = to_f32(o.e[e]);
+                if constexpr (V == 8)
+                    v = __uint_as_float((uint32_t)__builtin_bit_cast(uint16_t, o.e[e]) << 16 | (c + e < D ? (uint32_t)lo[e] << 8 : 0u));
+                // (a row that does not count stays zero whatever the gradient)
+                o.e[e] = from_f32<T>(v == 0.f ? 0.f : v * g);
+            }
+            store_vec(dx + r * D, c, D, o);
+        }
+    }
 }
 
 // dx[r] = *scale (null: 1) times the sum of the partials of the row's place, or zeros.
@@ -275,20 +414,22 @@ __global__ __launch_bounds__(256) void lse_rows_kernel(const float *__restrict__
 }
 
 // z -> dz in place; the rows that do not count and the columns past V become zeros.
+// The softmax is exp(z - lse), or (inv) inv exp(z - lse), lse then being a reference
+// and inv the sum's inverse.
 __global__ __launch_bounds__(256) void grad_rows_kernel(float *__restrict__ z, int ldz, int V, int v0, int64_t M, const int *__restrict__ count,
                                                         const int *__restrict__ tgt, const float *__restrict__ lse,
-                                                        const float *__restrict__ scale) {
+                                                        const float *__restrict__ inv, const float *__restrict__ scale) {
     const int n = *count;
-    const float factor = scale[M];   // (what a common rounding error of 2^-24 would do does not matter)
+    const float factor = scale ? scale[M] : 1.f;   // (what a common rounding error of 2^-24 would do does not matter)
     for (int64_t i = blockIdx.x; i < M; i += gridDim.x) {
         const bool in = i < n;
-        const float l = in ? lse[i] : 0.f, sc = in ? scale[i] * factor : 0.f;
+        const float l = in ? lse[i] : 0.f, f = in && inv ? inv[i] : 1.f, sc = in ? (scale ? scale[i] : 1.f) * factor : 0.f;
         const int t = in ? tgt[i] - v0 : -1;
         for (int c = (int)threadIdx.x * 4; c < ldz; c += 1024) {
             Vec16<float> v = load_vec(z + i * ldz, c, ldz);
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                const float p = exp_below(v.e[e], l) - (c + e == t ? 1.f : 0.f);
+                const float p = exp_below(v.e[e], l) * f - (c + e == t ? 1.f : 0.f);
                 v.e[e] = in && c + e < V ? p * sc : 0.f;
             }
             store_vec(z + i * ldz, c, ldz, v);
@@ -384,21 +525,45 @@ Rows carve_rows(Carve &c, int dtype, int64_t M, int64_t D, int64_t V, bool padw,
     return r;
 }
 
+// Rows at once where dx is kept: kPieceBytes of exponentials, whole tiles.
+int64_t chunk_rows(int64_t M, int64_t V) { return std::min(M, kPieceBytes / ((V + 7) / 8 * 16) / 256 * 256); }
+
 struct Fwd {
     Rows r;
     void *stat;
     float *tlogit, *each;
     float *z;      // fp32: a piece's logits,
     float *wp, *bp;   // its padded operands
-    void *conv;    // and the contraction's workspace
+    void *conv;    // and the contractions' workspace
+    // where dx is kept
+    Kept kept;
+    int64_t chunk;
+    bf16 *prob;      // bf16: a chunk's exponentials
+    float *part;     // partials of dx
+    SplitRule rule;
+    int *nsplit, *ccount;   // of each chunk
 };
 
-Fwd carve_fwd(Carve &c, int dtype, int64_t M, int64_t D, int64_t V, bool padw, bool padb, bool each) {
+Fwd carve_fwd(Carve &c, int dtype, int64_t M, int64_t D, int64_t V, bool padw, bool padb, bool each, bool keep) {
     Fwd f{};
     f.r = carve_rows(c, dtype, M, D, V, padw, padb);
-    f.stat = c.get<floatx2>((dtype == kBF16 && M ? g2::xent_lse_tiles(M, f.r.D8, V) : 1) * M);
+    f.chunk = keep && dtype == kBF16 ? chunk_rows(M, V) : M;
+    f.stat = c.get<floatx2>((dtype != kBF16 || !M ? 1 : keep ? (V + 255) / 256 * (256 / kProbCols) : g2::xent_lse_tiles(M, f.r.D8, V)) *
+                            f.chunk);
     f.tlogit = c.get<float>(M);
     f.each = each ? c.get<float>(M) : nullptr;
+    if (keep) {
+        f.kept.ref = c.get<float>(M);
+        f.kept.f = c.get<float>(M);
+        f.kept.ct = c.get<float>(M);
+        if (dtype == kBF16) {
+            f.prob = c.get<bf16>(f.chunk * ((V + 7) / 8 * 8));
+            f.rule = g2::xent_dx_rule(f.chunk, f.r.D8, V);
+            f.nsplit = c.get<int>((M + f.chunk - 1) / f.chunk);
+            f.ccount = c.get<int>((M + f.chunk - 1) / f.chunk);
+        }
+        f.part = c.get<float>((dtype == kBF16 ? f.rule.most * f.chunk : M) * f.r.D8);
+    }
     if (dtype != kBF16) {
         const int64_t p = piece(dtype, M, V), last = V - (V - 1) / p * p, most = std::max(f32_words(M, p), f32_words(M, last));
         f.z = c.get<float>(M * most);
@@ -406,6 +571,7 @@ Fwd carve_fwd(Carve &c, int dtype, int64_t M, int64_t D, int64_t V, bool padw, b
         f.bp = M >= kPadRows ? c.get<float>(most) : nullptr;
         size_t ws = 0;
         for (int64_t v : {p, last}) ws = std::max(ws, conv_fwd_workspace(dtype, linear(M, f.r.D8, f32_words(M, v))));
+        if (keep) ws = std::max(ws, linear_bwd_workspace(dtype, M, f.r.D8, f32_words(M, V), true, false, false));
         f.conv = c.raw(ws);
     }
     return f;
@@ -461,14 +627,14 @@ int row_grid(int64_t M) { return (int)std::max<int64_t>(1, std::min<int64_t>(M, 
 // The rows that count and what the contractions read.
 int start(const Rows &r, int dtype, int64_t M, int64_t D, int64_t V, const void *x, const void **w, const void **b,
           const int64_t *target, int64_t ignore, const float *lse, const float *gloss, int reduction, float *lsec, float *scale,
-          const SplitRule &rule, int *nsplit, hipStream_t st) {
+          const SplitRule &rule, int *nsplit, int64_t chunk, int *ccount, hipStream_t st) {
     hipLaunchKernelGGL(rows_kernel, dim3(1), dim3(1024), 0, st, target, ignore, M, V, r.pos, r.idx, r.tgt, r.count);
     if (dtype == kBF16)
         hipLaunchKernelGGL(gather_kernel<bf16>, dim3(row_grid(M)), dim3(256), 0, st, (const bf16 *)x, r.idx, r.count, M, (int)D,
-                           (int)r.D8, false, (bf16 *)r.xc, lse, gloss, reduction, lsec, scale, rule, nsplit);
+                           (int)r.D8, false, (bf16 *)r.xc, lse, gloss, reduction, lsec, scale, rule, nsplit, chunk, ccount);
     else
         hipLaunchKernelGGL(gather_kernel<float>, dim3(row_grid(M)), dim3(256), 0, st, (const float *)x, r.idx, r.count, M, (int)D,
-                           (int)r.D8, true, (float *)r.xc, lse, gloss, reduction, lsec, scale, rule, nsplit);
+                           (int)r.D8, true, (float *)r.xc, lse, gloss, reduction, lsec, scale, rule, nsplit, chunk, ccount);
     int err = (int)hipGetLastError();
     CopyJob j[kCopies];
     int n = 0;
@@ -511,47 +677,106 @@ int logits(const Piece &q, const Rows &r, int64_t M, float *z, void *ws, hipStre
 }  // namespace
 }  // namespace xent
 
-size_t xent_fwd_workspace(int dtype, int64_t M, int64_t D, int64_t V, bool padw, bool padb, int reduction) {
+// Where dx is the only gradient, the forward takes it: from sizes on at which a
+// contraction and two launches less are worth a kept gradient larger than x (fp32: where
+// its logits are one piece).  us of forward and backward, so and with the backward's own
+// contractions, M x 768 x V:
+//                bf16 64 x 5461  512 x 10922  4096 x 5461    fp32 64 x 5461  512 x 10922  4096 x 5461
+//   in the forward         50           68          136               68          213          612
+//   in the backward        59           79          177               88          305          895
+// and 4096 x 4096 x 128000 bf16 7.2 and 10.5 ms.
+bool xent_keeps_gradient(int dtype, int64_t M, int64_t D, int64_t V, bool dx, bool dw, bool db) {
+    if (!dx || dw || db || M <= 16 || (double)M * D * V < double(int64_t(1) << 28)) return false;
+    return dtype == kBF16 ? xent::chunk_rows(M, V) > 0 : xent::piece(dtype, M, V) == V;
+}
+
+size_t xent_kept_bytes(int dtype, int64_t M, int64_t D) { return (size_t)M * D * (dtype == kBF16 ? 3 : 4); }
+
+size_t xent_fwd_workspace(int dtype, int64_t M, int64_t D, int64_t V, bool padw, bool padb, int reduction, bool keep) {
     xent::Carve c{nullptr};
-    xent::carve_fwd(c, dtype, M, D, V, padw, padb, reduction != 2);
+    xent::carve_fwd(c, dtype, M, D, V, padw, padb, reduction != 2, keep);
     return std::max(c.off, tok::xent_workspace());
 }
 
 int launch_xent_fwd(int dtype, int64_t M, int64_t D, int64_t V, const void *x, const void *w, const void *b, bool padw, bool padb,
-                    const int64_t *target, int64_t ignore, int reduction, float *loss, float *lse, void *ws, void *stream) {
+                    const int64_t *target, int64_t ignore, int reduction, float *loss, float *lse, void *kept, void *ws, void *stream) {
     using namespace xent;
     hipStream_t st = (hipStream_t)stream;
-    if (tok::applies(dtype, M, V, D, x, w)) return tok::xent(dtype, M, D, V, x, w, b, target, ignore, reduction, loss, lse, ws, st);
+    if (!kept && tok::applies(dtype, M, V, D, x, w)) return tok::xent(dtype, M, D, V, x, w, b, target, ignore, reduction, loss, lse, ws, st);
     Carve c{static_cast<char *>(ws)};
-    const Fwd f = carve_fwd(c, dtype, M, D, V, padw, padb, reduction != 2);
-    int err = start(f.r, dtype, M, D, V, x, &w, &b, target, ignore, nullptr, nullptr, reduction, nullptr, nullptr, SplitRule{}, nullptr, st);
+    const Fwd f = carve_fwd(c, dtype, M, D, V, padw, padb, reduction != 2, kept != nullptr);
+    const int64_t D8 = f.r.D8;
+    int err = start(f.r, dtype, M, D, V, x, &w, &b, target, ignore, nullptr, nullptr, reduction, nullptr, nullptr, f.rule, f.nsplit, f.chunk,
+                    f.ccount, st);
     if (err) return err;
-    int parts = 1;
+    if (dtype == kBF16 && M > 0 && !g2::rows_ok(M, V, D8, f.r.xc, w)) return (int)hipErrorInvalidValue;
+    float *each = reduction == 2 ? loss : f.each;
+    auto combine = [&](int parts, int64_t ld, int64_t i0) {
+        hipLaunchKernelGGL(combine_kernel, dim3((unsigned)((M + 31) / 32)), dim3(256), 0, st, (const floatx2 *)f.stat, parts, ld, i0, f.tlogit,
+                           f.r.pos, f.r.tgt, M, each, lse, f.kept);
+        return (int)hipGetLastError();
+    };
     if (M == 0) {
+    } else if (kept && dtype == kBF16) {
+        const int64_t ldz = (V + 7) / 8 * 8, R = f.chunk;
+        for (int64_t i0 = 0, k = 0; i0 < M && !err; i0 += R, ++k) {
+            const bf16 *xc = (const bf16 *)f.r.xc + i0 * D8;
+            const int64_t m = std::min(R, M - i0);
+            const int parts = g2::xent_prob_parts(m, D8, V);
+            err = g2::xent_prob(m, D8, V, xc, w, b, f.ccount + k, f.r.tgt + i0, f.stat, R, f.tlogit + i0, f.prob, ldz, st);
+            if (!err) err = combine(parts, R, i0);
+            if (err) break;
+            hipLaunchKernelGGL(adjust_kernel, dim3((unsigned)((R + 255) / 256), (unsigned)std::min(parts, 2048)), dim3(256), 0, st, f.prob, ldz,
+                               f.ccount + k, (const floatx2 *)f.stat, R, parts, f.kept.ref + i0);
+            err = (int)hipGetLastError();
+            if (!err) err = g2::xent_dx(R, D8, V, ldz, V, f.prob, w, f.ccount + k, f.nsplit + k, f.part, false, st);
+            if (err) break;
+            hipLaunchKernelGGL(keep_kernel<bf16>, dim3(row_grid(M)), dim3(256), 0, st, f.part, f.nsplit + k, R * D8, f.r.pos, M, (int)D, (int)D8,
+                               i0, R, f.r.count, reduction == 0, f.kept.f, f.kept.ct, f.r.tgt, (const bf16 *)w, kept);
+            err = (int)hipGetLastError();
+        }
     } else if (dtype == kBF16) {
-        if (!g2::rows_ok(M, V, f.r.D8, f.r.xc, w)) return (int)hipErrorInvalidValue;
-        parts = g2::xent_lse_tiles(M, f.r.D8, V);
-        err = g2::xent_lse(M, f.r.D8, V, f.r.xc, w, b, f.r.count, f.r.tgt, f.stat, f.tlogit, st);
+        err = g2::xent_lse(M, D8, V, f.r.xc, w, b, f.r.count, f.r.tgt, f.stat, f.tlogit, st);
+        if (!err) err = combine(g2::xent_lse_tiles(M, D8, V), M, 0);
     } else {
         const int64_t p = piece(dtype, M, V);
+        Piece q;
         for (int64_t v0 = 0; v0 < V && !err; v0 += p) {
             const int64_t n = std::min(p, V - v0);
-            Piece q;
-            err = take_piece(&q, M, D, f.r.D8, v0, n, w, b, f.wp, f.bp, st);
+            err = take_piece(&q, M, D, D8, v0, n, w, b, f.wp, f.bp, st);
             if (!err) err = logits(q, f.r, M, f.z, f.conv, st);
             if (err) break;
             hipLaunchKernelGGL(lse_rows_kernel, dim3(row_grid(M)), dim3(256), 0, st, f.z, (int)q.np, (int)n, (int)v0, f.r.count, f.r.tgt,
                                v0 == 0, (floatx2 *)f.stat, f.tlogit);
             err = (int)hipGetLastError();
         }
+        if (!err) err = combine(1, M, 0);
+        if (!err && kept) {   // (one piece)
+            hipLaunchKernelGGL(grad_rows_kernel, dim3(row_grid(M)), dim3(256), 0, st, f.z, (int)q.np, (int)V, 0, M, f.r.count, f.r.tgt,
+                               f.kept.ref, f.kept.f, (const float *)nullptr);
+            err = (int)hipGetLastError();
+            if (!err)
+                err = launch_linear_bwd(dtype, M, D8, q.np, f.r.count, f.z, f.r.xc, q.w, f.part, nullptr, nullptr, f.conv, stream);
+            if (err) return err;
+            hipLaunchKernelGGL(keep_kernel<float>, dim3(row_grid(M)), dim3(256), 0, st, f.part, (const int *)nullptr, M * D8, f.r.pos, M,
+                               (int)D, (int)D8, (int64_t)0, M, f.r.count, reduction == 0, (const float *)nullptr, (const float *)nullptr,
+                               f.r.tgt, (const float *)w, kept);
+            err = (int)hipGetLastError();
+        }
     }
     if (err) return err;
-    float *each = reduction == 2 ? loss : f.each;
-    if (M > 0)
-        hipLaunchKernelGGL(combine_kernel, dim3((unsigned)((M + 31) / 32)), dim3(256), 0, st, (const floatx2 *)f.stat, parts, f.tlogit,
-                           f.r.pos, f.r.tgt, M, each, lse);
     if (reduction != 2)
         hipLaunchKernelGGL(total_kernel, dim3(1), dim3(1024), 0, st, each, M, f.r.count, reduction == 0, loss);
+    return (int)hipGetLastError();
+}
+
+int launch_xent_scale(int dtype, int64_t M, int64_t D, const void *kept, const float *gloss, int reduction, void *dx, void *stream) {
+    using namespace xent;
+    hipStream_t st = (hipStream_t)stream;
+    if (dtype == kBF16)
+        hipLaunchKernelGGL(scale_kernel<bf16>, dim3(row_grid(M)), dim3(256), 0, st, kept, M, (int)D, gloss, reduction == 2, (bf16 *)dx);
+    else
+        hipLaunchKernelGGL(scale_kernel<float>, dim3(row_grid(M)), dim3(256), 0, st, kept, M, (int)D, gloss, reduction == 2, (float *)dx);
     return (int)hipGetLastError();
 }
 
@@ -568,7 +793,7 @@ int launch_xent_bwd(int dtype, int64_t M, int64_t D, int64_t V, const void *x, c
     hipStream_t st = (hipStream_t)stream;
     Carve c{static_cast<char *>(ws)};
     const Bwd k = carve_bwd(c, dtype, M, D, V, padw, padb, dx, dw, db);
-    int err = start(k.r, dtype, M, D, V, x, &w, &b, target, ignore, lse, gloss, reduction, k.lse, k.scale, k.rule, k.nsplit, st);
+    int err = start(k.r, dtype, M, D, V, x, &w, &b, target, ignore, lse, gloss, reduction, k.lse, k.scale, k.rule, k.nsplit, M, nullptr, st);
     if (err) return err;
     const int64_t p = piece(dtype, M, V), D8 = k.r.D8;
     if (dtype == kBF16 && M > 0 && !g2::rows_ok(M, V, D8, k.r.xc, w)) return (int)hipErrorInvalidValue;
@@ -598,7 +823,7 @@ int launch_xent_bwd(int dtype, int64_t M, int64_t D, int64_t V, const void *x, c
                 err = logits(q, k.r, M, z, k.work, st);
                 if (err) break;
                 hipLaunchKernelGGL(grad_rows_kernel, dim3(row_grid(M)), dim3(256), 0, st, z, (int)q.np, (int)n, (int)v0, M, k.r.count,
-                                   k.r.tgt, k.lse, k.scale);
+                                   k.r.tgt, k.lse, (const float *)nullptr, k.scale);
                 err = (int)hipGetLastError();
             }
             const bool tw = dw && (q.np != n || D8 != D), tb = db && q.np != n;

@@ -73,11 +73,15 @@ int launch_gated_bwd(int, int64_t M, int64_t, int64_t, int, const void *x, const
     return e;
 }
 
-size_t xent_fwd_workspace(int, int64_t, int64_t, int64_t, bool, bool, int) { return 256; }
+// (the rule's form; its sizes are the library's own business)
+bool xent_keeps_gradient(int, int64_t M, int64_t, int64_t, bool dx, bool dw, bool db) { return dx && !dw && !db && M >= 1000; }
+size_t xent_kept_bytes(int dtype, int64_t M, int64_t D) { return (size_t)M * D * (dtype == kBF16 ? 3 : 4); }
+size_t xent_fwd_workspace(int, int64_t, int64_t, int64_t, bool, bool, int, bool keep) { return keep ? 1024 : 256; }
 
 int launch_xent_fwd(int, int64_t M, int64_t, int64_t, const void *x, const void *w, const void *, bool, bool, const int64_t *target,
-                    int64_t, int, float *loss, float *lse, void *ws, void *) {
-    note(lse ? "xent+lse" : "xent");
+                    int64_t, int, float *loss, float *lse, void *kept, void *ws, void *) {
+    note(kept ? "xent+dx" : lse ? "xent+lse" : "xent");
+    if (kept && lse) return need(false, "xent:both");
     return (M > 0 ? need(x && w && target && loss, "xent:x,w,target,loss") : 0) | need(ws, "xent:ws");
 }
 
@@ -87,6 +91,11 @@ int launch_xent_bwd(int, int64_t M, int64_t, int64_t, const void *x, const void 
                     int64_t, int, const float *gloss, const float *lse, void *dx, void *dw, void *db, void *ws, void *) {
     note(std::string("xent_bwd") + (dx ? "+dx" : "") + (dw ? "+dw" : "") + (db ? "+db" : ""));
     return (M > 0 ? need(x && w && target && gloss && lse, "xent_bwd:x,w,target,gloss,lse") : 0) | need(ws, "xent_bwd:ws");
+}
+
+int launch_xent_scale(int, int64_t, int64_t, const void *kept, const float *gloss, int, void *dx, void *) {
+    note("xent_scale");
+    return need(kept && gloss && dx, "xent_scale:kept,gloss,dx");
 }
 
 }  // namespace ms

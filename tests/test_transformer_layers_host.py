@@ -162,6 +162,38 @@ def test_gated_unit_from_its_input_alone(stub, mask):
     c.free()
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_a_gradient_taken_in_the_forward(stub, dtype):
+    """(The stub keeps it from 1000 rows on.)  The record holds it and nothing else;
+    backward needs no workspace but for a gradient in another layout."""
+    rows, e = 1000, {"f32": 4, "bf16": 3}[dtype]
+    assert stub.ms_cross_entropy_kept_bytes(rows, D, V, DT[dtype], 1) == rows * D * e
+    for mask in (3, 5, 7, 2, 4):
+        assert stub.ms_cross_entropy_kept_bytes(rows, D, V, DT[dtype], mask) == rows * 4
+    assert stub.ms_cross_entropy_kept_bytes(rows - 1, D, V, DT[dtype], 1) == (rows - 1) * 4
+    for args in ((rows, D, V, 0), (0, D, V, 1), (rows, 0, V, 1), (rows, D, -1, 1)):
+        assert stub.ms_cross_entropy_kept_bytes(*args[:3], DT[dtype], args[3]) == 0
+    for strides, copies in ((None, 0), ((1, rows), 1)):
+        c = Call(stub, "xent", dtype, mask=1, x=tensor((rows, D), dtype, strides))
+        before = live(stub)
+        assert c.forward() == 0 and stub.blocks_log() == b"xent+dx;"
+        acct = c.account()
+        assert (acct.borrowed, acct.saved_activation_bytes, acct.referenced_param_bytes) == (512, rows * D * e, 0)
+        assert live(stub) == before + rows * D * e
+        assert (acct.transient_workspace_bytes > 0) == bool(copies)
+        stub.blocks_reset()
+        stub.stub_reset()
+        if not copies:
+            stub.ms_testing_fail_next_workspace(1)   # none is asked for
+        assert c.backward() == 0
+        stub.ms_testing_fail_next_workspace(0)
+        assert stub.blocks_log() == b"xent_scale;" and stub.stub_log() == b"copy4;" * copies
+        assert c.backward() == L.MS_E_CONSUMED
+        c.free()
+        stub.blocks_reset()
+        stub.stub_reset()
+
+
 @pytest.mark.parametrize("rows,f,dtype,want", [(0, 5, 0, 0), (3, 0, 1, 0), (12, 24, 1, 12 * 48 * 3), (7, 17, 0, 7 * 64 * 4),
                                               (2 ** 20, 2 ** 13, 1, 2 ** 34 * 3), (-1, 4, 0, 0)])
 def test_projection_bytes(stub, rows, f, dtype, want):
@@ -198,6 +230,7 @@ REFUSED = [(k, s, o) for k in KINDS for s, o in COMMON if not ("b" in o and o["b
     ("gated", L.MS_E_ARG, dict(proj=FAKE + 8)), ("gated", L.MS_E_LAYOUT, dict(b=tensor((2 * F,), strides=(2,)))),
     ("gated", L.MS_E_UNSUPPORTED, dict(x=tensor((2 ** 26, D)), y=tensor((2 ** 26, F)))),
     ("xent", L.MS_E_NULL, dict(W=None)), ("xent", L.MS_E_NULL, dict(target=None)), ("xent", L.MS_E_NULL, dict(lse=None)),
+    ("xent", L.MS_E_ARG, dict(lse=FAKE + 8)),
     ("xent", L.MS_E_ARG, dict(target=FAKE + 4)), ("xent", L.MS_E_ARG, dict(reduction=3)), ("xent", L.MS_E_ARG, dict(reduction=-1)),
     ("xent", L.MS_E_SHAPE, dict(W=tensor((0, D)))), ("xent", L.MS_E_SHAPE, dict(b=tensor((V + 1,)))),
     ("xent", L.MS_E_DTYPE, dict(y=tensor((1,), "bf16"))), ("xent", L.MS_E_SHAPE, dict(y=tensor((M,), "f32"))),
