@@ -7,7 +7,8 @@
 //   kEpiLse       z = x W^T + b over a vocabulary: the maximum and the sum of
 //                 exponentials of each row's part of a column tile, and the
 //                 target's logit; z is not written
-//   kEpiXent      z again, then dz = (exp(z - lse) - [column = target]) scale
+//   kEpiXent      z again, then dz = (exp(z - lse) - [column = target]) scale, and
+//                 optionally its column sums before it is rounded
 //   kEpiProb      z, then exp(z - r) of the other words than the target, r a
 //                 reference of each row's part of a wave's columns, with those parts'
 //                 sums of exponentials and the target's logit
@@ -402,13 +403,41 @@ __device__ __forceinline__ void fused_epilogue(const FusedArgs &P, char *smem, f
                         for (int v = 0; v < 4; ++v) {
                             float p = exp_below(acc[i][j][4 * q + v], l);
                             if (any && t == 32 * j + 8 * q + 4 * fh + v) p -= 1.f;
-                            o[v] = (bf16)(p * sc);
+                            p = in ? p * sc : 0.f;   // (the other rows hold anything)
+                            o[v] = (bf16)p;
+                            acc[i][j][4 * q + v] = p;
                         }
                         *reinterpret_cast<bf16x4 *>(stage + fr * PITCH + 32 * j + 8 * q + 4 * fh) = o;
                     }
                 stage_order();
                 store_rows<G::WN>(stage, PITCH, P.c + (int64_t)mb * P.ldc + n0 + wn0, P.ldc, M - mb, ncol, lane);
                 stage_order();
+            }
+            if (P.dbpart) {
+                // Column sums of the wave's rows: each of the 32 lanes that share a column's
+                // rows sends half of its columns and keeps the other, five times.
+                float *row = P.dbpart + (int64_t)((m0 + wm0) / G::WM) * N;
+#pragma unroll
+                for (int j = 0; j < TN; ++j) {
+                    float s[16];
+#pragma unroll
+                    for (int v = 0; v < 16; ++v) {
+                        s[v] = acc[0][j][v];
+#pragma unroll
+                        for (int i = 1; i < TM; ++i) s[v] += acc[i][j][v];
+                    }
+#pragma unroll
+                    for (int h = 8; h > 0; h >>= 1)
+#pragma unroll
+                        for (int v = 0; v < h; ++v) {
+                            const bool up = (fr & h) != 0;
+                            const float mine = up ? s[v + h] : s[v], give = up ? s[v] : s[v + h];
+                            s[v] = mine + __shfl_xor(give, h);
+                        }
+                    s[0] += __shfl_xor(s[0], 16);
+                    const int v = fr & 15, n = n0 + wn0 + 32 * j + 8 * (v / 4) + 4 * fh + v % 4;
+                    if (fr < 16 && n < N) row[n] = s[0];
+                }
             }
         }
     } else {

@@ -41,10 +41,19 @@ int xent_lse(int64_t M, int64_t D, int64_t V, const void *x, const void *w, cons
     return go_rows<kEpiLse>(p.tile, kProfFwd, a, st);
 }
 
+// Rows of xent_grad()'s column sums: one for each `rows` rows of dz, of whole tiles
+// of `tile` rows.
+void xent_bias_rows(int64_t M, int64_t D, int64_t V, int *tile, int *rows) {
+    const Tile &t = kRowTiles[plan(kRowTiles, 2, M, V, D, 1).tile];
+    *tile = t.bm;
+    *rows = t.bm / t.wr;
+}
+
 // dz[M][ldz] of the words v0 .. v0 + V - 1, whose rows of W and biases w and
-// bias are; columns V .. ldz - 1 are zeros.
+// bias are; columns V .. ldz - 1 are zeros.  dbpart (null: not wanted): the column
+// sums, rows of V.
 int xent_grad(int64_t M, int64_t D, int64_t V, const void *x, const void *w, const void *bias, const int *count, const int *target,
-              int v0, const float *lse, const float *scale, void *dz, int64_t ldz, hipStream_t st) {
+              int v0, const float *lse, const float *scale, void *dz, int64_t ldz, float *dbpart, hipStream_t st) {
     const FusedPlan p = plan(kRowTiles, 2, M, V, D, 1);
     FusedArgs a = rows_args(kRowTiles[p.tile], M, V, D, x, w, V);
     a.fbias = (const bf16 *)bias;
@@ -53,6 +62,7 @@ int xent_grad(int64_t M, int64_t D, int64_t V, const void *x, const void *w, con
     a.v0 = v0;
     a.lse = lse;
     a.scale = scale;
+    a.dbpart = dbpart;
     a.c = (bf16 *)dz;
     a.ldc = (int)ldz;
     return go_rows<kEpiXent>(p.tile, kProfFwd, a, st);
@@ -127,7 +137,7 @@ int xent_dx(int64_t M, int64_t D, int64_t V, int64_t ldz, int64_t piece, const v
     return go_grad<kEpiAdd, kDgradN>(tile, kProfDgrad, a, st, xent_dx_rule(M, D, piece).most);
 }
 
-// dw[V][Dr] = *scale dz^T x over the rows that count (x has D >= Dr columns), and db.
+// dw[V][Dr] = *scale dz^T x over the rows that count (x has D >= Dr columns).
 int sum_wgrad_partials(const float *part, int splits, int M, int C8, int C, void *out, const float *dbpart, void *db, hipStream_t st);
 
 namespace {
@@ -138,13 +148,13 @@ FusedPlan dw_plan(int64_t M, int64_t D, int64_t Dr, int64_t V) {
 }
 }  // namespace
 
-size_t xent_dw_workspace(int64_t M, int64_t D, int64_t Dr, int64_t V, bool db) {
+size_t xent_dw_workspace(int64_t M, int64_t D, int64_t Dr, int64_t V) {
     const FusedPlan p = dw_plan(M, D, Dr, V);
-    return ((p.splits > 1 ? (size_t)p.splits * V * D : 0) + (db ? (size_t)p.splits * V : 0)) * sizeof(float);
+    return p.splits > 1 ? (size_t)p.splits * V * D * sizeof(float) : 0;
 }
 
 int xent_dw(int64_t M, int64_t D, int64_t Dr, int64_t V, int64_t ldz, const void *dz, const void *x, const int *count,
-            const float *scale, void *dw, void *db, void *ws, hipStream_t st) {
+            const float *scale, void *dw, void *ws, hipStream_t st) {
     const FusedPlan p = dw_plan(M, D, Dr, V);
     const Tile &t = kGradTiles[p.tile];
     FusedArgs a{};
@@ -161,18 +171,15 @@ int xent_dw(int64_t M, int64_t D, int64_t Dr, int64_t V, int64_t ldz, const void
     a.b_bytes = bytes_of(M * D);
     a.count = count;
     a.out_scale = scale;
-    float *f = static_cast<float *>(ws);
     if (p.splits > 1) {
-        a.part = f;
+        a.part = static_cast<float *>(ws);
         a.part_stride = V * D;
-        f += (size_t)p.splits * V * D;
     } else {
         a.c = (bf16 *)dw;
     }
-    a.dbpart = db ? f : nullptr;
     const int err = go_grad<kEpiStore, kWgrad>(p.tile, kProfWgrad, a, st);
-    if (err || (p.splits == 1 && !db)) return err;
-    return sum_wgrad_partials(a.part, p.splits, (int)V, (int)D, (int)Dr, dw, a.dbpart, db, st);
+    if (err || p.splits == 1) return err;
+    return sum_wgrad_partials(a.part, p.splits, (int)V, (int)D, (int)Dr, dw, nullptr, nullptr, st);
 }
 
 }  // namespace g2

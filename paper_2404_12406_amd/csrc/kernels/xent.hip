@@ -35,16 +35,17 @@ int xent_lse_tiles(int64_t M, int64_t D, int64_t V);
 int xent_lse(int64_t M, int64_t D, int64_t V, const void *x, const void *w, const void *bias, const int *count, const int *target,
              void *stat, float *tlogit, hipStream_t st);
 int xent_grad(int64_t M, int64_t D, int64_t V, const void *x, const void *w, const void *bias, const int *count, const int *target,
-              int v0, const float *lse, const float *scale, void *dz, int64_t ldz, hipStream_t st);
+              int v0, const float *lse, const float *scale, void *dz, int64_t ldz, float *dbpart, hipStream_t st);
+void xent_bias_rows(int64_t M, int64_t D, int64_t V, int *tile, int *rows);
 int xent_prob_parts(int64_t M, int64_t D, int64_t V);
 int xent_prob(int64_t M, int64_t D, int64_t V, const void *x, const void *w, const void *bias, const int *count, const int *target,
               void *stat, int64_t stat_ld, float *tlogit, void *prob, int64_t ldz, hipStream_t st);
 SplitRule xent_dx_rule(int64_t M, int64_t D, int64_t V);
 int xent_dx(int64_t M, int64_t D, int64_t V, int64_t ldz, int64_t piece, const void *dz, const void *w, const int *count,
             const int *nsplit, float *part, bool add, hipStream_t st);
-size_t xent_dw_workspace(int64_t M, int64_t D, int64_t Dr, int64_t V, bool db);
+size_t xent_dw_workspace(int64_t M, int64_t D, int64_t Dr, int64_t V);
 int xent_dw(int64_t M, int64_t D, int64_t Dr, int64_t V, int64_t ldz, const void *dz, const void *x, const int *count,
-            const float *scale, void *dw, void *db, void *ws, hipStream_t st);
+            const float *scale, void *dw, void *ws, hipStream_t st);
 }  // namespace g2
 
 namespace tok {
@@ -348,31 +349,24 @@ __global__ __launch_bounds__(256) void finish_kernel(const float *__restrict__ p
     }
 }
 
-// db[v] = *scale times the sum over the rows that count of dz[i][v]: 16 columns of eight a
-// block, 16 threads each (a bias trained without its weight).
-__global__ __launch_bounds__(256) void bias_kernel(const bf16 *__restrict__ dz, int64_t ldz, const int *__restrict__ count, int V,
+// db[v] = *scale times the sum of the contraction's column sums, one row of them for
+// `rows` rows of dz: those of dz before it was rounded.  (A target's entry of dz is
+// near -1 in every row, so a rounded one would be off by much the same in all.)
+__global__ __launch_bounds__(256) void bias_kernel(const float *__restrict__ part, int tile, int rows, const int *__restrict__ count, int V,
                                                    const float *__restrict__ scale, bf16 *__restrict__ db) {
-    __shared__ float red[16][16 * 8 + 4];
-    const int col = threadIdx.x & 15, grp = threadIdx.x >> 4, n = *count;
-    const int c = ((int)blockIdx.x * 16 + col) * 8;
-    float s[8];
+    const int v = (int)blockIdx.x * 256 + (int)threadIdx.x, n = (*count + tile - 1) / tile * (tile / rows);
+    if (v >= V) return;
+    float s = 0.f;
+    int r = 0;
+    for (; r + 4 <= n; r += 4) {
+        float p[4];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) s[e] = 0.f;
-    if (c < V)
-        for (int64_t i = grp; i < n; i += 16) {
-            const Vec16<bf16> v = load16(dz + i * ldz + c);
+        for (int u = 0; u < 4; ++u) p[u] = part[(int64_t)(r + u) * V + v];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) s[e] += to_f32(v.e[e]);
-        }
-#pragma unroll
-    for (int e = 0; e < 8; ++e) red[grp][col * 8 + e] = s[e];
-    __syncthreads();
-    if (threadIdx.x >= 128) return;
-    const int v = (int)blockIdx.x * 128 + (int)threadIdx.x;
-    float t = 0.f;
-#pragma unroll
-    for (int q = 0; q < 16; ++q) t += red[q][threadIdx.x];
-    if (v < V) db[v] = (bf16)(t * *scale);
+        for (int u = 0; u < 4; ++u) s += p[u];
+    }
+    for (; r < n; ++r) s += part[(int64_t)r * V + v];
+    db[v] = (bf16)(s * *scale);
 }
 
 // ------------------------------------------------------------------ fp32 pieces
@@ -583,6 +577,7 @@ struct Bwd {
     void *dz;
     float *part;     // partials of dx (fp32: the sum and a piece's)
     float *wp, *bp, *gwp, *gbp;   // fp32: a piece's padded operands and gradients
+    float *dbpart;                // bf16: column sums of dz
     void *work;      // the contractions' workspace
     SplitRule rule;  // bf16: of the contraction for dx
     int *nsplit;
@@ -605,12 +600,13 @@ Bwd carve_bwd(Carve &c, int dtype, int64_t M, int64_t D, int64_t V, bool padw, b
     size_t ws = 0;
     for (int64_t v : {p, last}) {
         if (dtype == kBF16) {
-            if (dw) ws = std::max(ws, g2::xent_dw_workspace(M, b.r.D8, D, v, db));
+            if (dw) ws = std::max(ws, g2::xent_dw_workspace(M, b.r.D8, D, v));
         } else {
             ws = std::max(ws, conv_fwd_workspace(dtype, linear(M, b.r.D8, f32_words(M, v))));
             ws = std::max(ws, linear_bwd_workspace(dtype, M, b.r.D8, f32_words(M, v), dx, dw, db));
         }
     }
+    if (dtype == kBF16 && db) b.dbpart = c.get<float>((M + 63) / 64 * 4 * most);   // (rows of 64 or more, in whole tiles)
     if (dx) {
         if (dtype == kBF16) {
             b.rule = g2::xent_dx_rule(M, b.r.D8, p);
@@ -804,14 +800,16 @@ int launch_xent_bwd(int dtype, int64_t M, int64_t D, int64_t V, const void *x, c
             const bf16 *wv = (const bf16 *)w + v0 * D8;
             if (M > 0)
                 err = g2::xent_grad(M, D8, n, k.r.xc, wv, b ? (const bf16 *)b + v0 : nullptr, k.r.count, k.r.tgt, (int)v0, k.lse, k.scale,
-                                    k.dz, ldz, st);
+                                    k.dz, ldz, k.dbpart, st);
             if (!err && dx && M > 0) err = g2::xent_dx(M, D8, n, ldz, p, k.dz, wv, k.r.count, k.nsplit, k.part, v0 > 0, st);
             bf16 *dbv = db ? (bf16 *)db + v0 : nullptr;
             if (!err && dw)
-                err = g2::xent_dw(M, D8, D, n, ldz, k.dz, k.r.xc, k.r.count, k.scale + M, (bf16 *)dw + v0 * D, dbv, k.work, st);
-            else if (!err && db) {
-                hipLaunchKernelGGL(bias_kernel, dim3((unsigned)((n + 127) / 128)), dim3(256), 0, st, (const bf16 *)k.dz, ldz, k.r.count,
-                                   (int)n, k.scale + M, dbv);
+                err = g2::xent_dw(M, D8, D, n, ldz, k.dz, k.r.xc, k.r.count, k.scale + M, (bf16 *)dw + v0 * D, k.work, st);
+            if (!err && db) {
+                int tile = 256, rows = 64;
+                if (M > 0) g2::xent_bias_rows(M, D8, n, &tile, &rows);
+                hipLaunchKernelGGL(bias_kernel, dim3((unsigned)((n + 255) / 256)), dim3(256), 0, st, k.dbpart, tile, rows, k.r.count, (int)n,
+                                   k.scale + M, dbv);
                 err = (int)hipGetLastError();
             }
         } else {

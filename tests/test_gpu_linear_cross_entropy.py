@@ -121,6 +121,19 @@ def test_masks(mask, bias, dtype):
     compare(run(*cuda(*t), "sum", mask), t, "sum", mask, dtype)
 
 
+@pytest.mark.parametrize("mask", [4, 7])
+@pytest.mark.parametrize("shape", [(300, 64, 130), (1030, 264, 2050), (2000, 64, 10007)])
+def test_bias_gradient_rounds_once(shape, mask):
+    """bf16: the sums of dz from before its rounding, so no more than the result's own
+    (at most 2^-8 of a value, and fp32's errors), whatever the factor that every row shares."""
+    for factor in (0.7, 1.1):
+        t = inputs(*shape, "bf16", ignored=0.1, reduction="sum", seed=231)[:4] + (torch.tensor([factor]),)
+        got = run(*cuda(*t), "sum", mask)[3]
+        want = ref(*(v.double().numpy() for v in t[:3]), t[3].numpy(), t[4].double().numpy(), "sum")[3]
+        err = np.abs(host(got) - want)
+        assert (err <= 2.0 ** -8 * np.abs(want) + 2e-5 * np.abs(want).max()).all()
+
+
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("reduction", ["mean", "sum", "none"])
 def test_every_row_ignored(reduction, dtype):
