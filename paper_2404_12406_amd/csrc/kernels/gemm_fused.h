@@ -43,7 +43,7 @@ struct FusedArgs : Args {
     const int *target;     // each row's target in the vocabulary
     int v0;                // the piece's first word
     floatx2 *stat;         // kEpiLse, kEpiProb: softmax statistics as join_lse()'s, [column tile][rows], [64 columns][rows]
-    float *tlogit;         // with them: the target's logit
+    float *tlogit;         // with them: the target's logit; kEpiXent: what rounding took from the target's dz
     int64_t stat_ld;
     const float *lse, *scale;   // kEpiXent: of each row
     const float *out_scale;     // kEpiStore: the sums' factor
@@ -394,6 +394,7 @@ __device__ __forceinline__ void fused_epilogue(const FusedArgs &P, char *smem, f
                 const float l = in ? lse[i] : 0.f, sc = in ? scale[i] : 0.f;
                 const int t = in ? tgt[i] - P.v0 - (n0 + wn0) : -1;
                 const bool any = __any((unsigned)t < (unsigned)G::WN);
+                float rest = 0.f;
 #pragma unroll
                 for (int j = 0; j < TN; ++j)
 #pragma unroll
@@ -406,10 +407,13 @@ __device__ __forceinline__ void fused_epilogue(const FusedArgs &P, char *smem, f
                             p = in ? p * sc : 0.f;   // (the other rows hold anything)
                             o[v] = (bf16)p;
                             acc[i][j][4 * q + v] = p;
+                            if (any && t == 32 * j + 8 * q + 4 * fh + v) rest = p - (float)o[v];
                         }
                         *reinterpret_cast<bf16x4 *>(stage + fr * PITCH + 32 * j + 8 * q + 4 * fh) = o;
                     }
                 stage_order();
+                // (of the two lanes of a row the one that has the column: (t / 4) odd in the upper half)
+                if ((unsigned)t < (unsigned)G::WN && ((t >> 2) & 1) == fh) P.tlogit[m] = rest;
                 store_rows<G::WN>(stage, PITCH, P.c + (int64_t)mb * P.ldc + n0 + wn0, P.ldc, M - mb, ncol, lane);
                 stage_order();
             }

@@ -50,10 +50,11 @@ void xent_bias_rows(int64_t M, int64_t D, int64_t V, int *tile, int *rows) {
 }
 
 // dz[M][ldz] of the words v0 .. v0 + V - 1, whose rows of W and biases w and
-// bias are; columns V .. ldz - 1 are zeros.  dbpart (null: not wanted): the column
-// sums, rows of V.
+// bias are; columns V .. ldz - 1 are zeros.  rest: what rounding took from the entry of
+// each row whose target is among them.  dbpart (null: not wanted): the column sums,
+// rows of V.
 int xent_grad(int64_t M, int64_t D, int64_t V, const void *x, const void *w, const void *bias, const int *count, const int *target,
-              int v0, const float *lse, const float *scale, void *dz, int64_t ldz, float *dbpart, hipStream_t st) {
+              int v0, const float *lse, const float *scale, void *dz, int64_t ldz, float *rest, float *dbpart, hipStream_t st) {
     const FusedPlan p = plan(kRowTiles, 2, M, V, D, 1);
     FusedArgs a = rows_args(kRowTiles[p.tile], M, V, D, x, w, V);
     a.fbias = (const bf16 *)bias;
@@ -62,6 +63,7 @@ int xent_grad(int64_t M, int64_t D, int64_t V, const void *x, const void *w, con
     a.v0 = v0;
     a.lse = lse;
     a.scale = scale;
+    a.tlogit = rest;
     a.dbpart = dbpart;
     a.c = (bf16 *)dz;
     a.ldc = (int)ldz;

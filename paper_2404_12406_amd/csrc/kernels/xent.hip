@@ -35,7 +35,7 @@ int xent_lse_tiles(int64_t M, int64_t D, int64_t V);
 int xent_lse(int64_t M, int64_t D, int64_t V, const void *x, const void *w, const void *bias, const int *count, const int *target,
              void *stat, float *tlogit, hipStream_t st);
 int xent_grad(int64_t M, int64_t D, int64_t V, const void *x, const void *w, const void *bias, const int *count, const int *target,
-              int v0, const float *lse, const float *scale, void *dz, int64_t ldz, float *dbpart, hipStream_t st);
+              int v0, const float *lse, const float *scale, void *dz, int64_t ldz, float *rest, float *dbpart, hipStream_t st);
 void xent_bias_rows(int64_t M, int64_t D, int64_t V, int *tile, int *rows);
 int xent_prob_parts(int64_t M, int64_t D, int64_t V);
 int xent_prob(int64_t M, int64_t D, int64_t V, const void *x, const void *w, const void *bias, const int *count, const int *target,
@@ -318,15 +318,18 @@ __global__ __launch_bounds__(256) void scale_kernel(const void *__restrict__ kep
 }
 
 // dx[r] = *scale (null: 1) times the sum of the partials of the row's place, or zeros.
+// With rest: the partials are those of rounded dz, of which a target's entry is most
+// of a row: what rounding took from it, times the target's row of w, is put back.
 template <typename T>
 __global__ __launch_bounds__(256) void finish_kernel(const float *__restrict__ part, const int *__restrict__ nsplit, int64_t stride,
                                                      const int *__restrict__ pos, int64_t M, int D, int ld, const float *__restrict__ scale,
+                                                     const float *__restrict__ rest, const int *__restrict__ tgt, const T *__restrict__ w,
                                                      T *__restrict__ dx) {
     constexpr int V = Vec16<T>::N;
     const float f = scale ? *scale : 1.f;
     const int splits = nsplit ? *nsplit : 1;
     for (int64_t r = blockIdx.x; r < M; r += gridDim.x) {
-        const int i = pos[r];
+        const int i = pos[r], t = rest && i >= 0 ? tgt[i] : -1;
         for (int c = (int)threadIdx.x * V; c < D; c += 256 * V) {
             Vec16<T> o = zero16<T>();
             if (i >= 0) {
@@ -340,6 +343,11 @@ __global__ __launch_bounds__(256) void finish_kernel(const float *__restrict__ p
 #pragma unroll
                         for (int e = 0; e < 4; ++e) s[4 * h + e] += p.e[e];
                     }
+                }
+                if (t >= 0) {
+                    const Vec16<T> wt = load_vec(w + (int64_t)t * ld, c, ld);
+#pragma unroll
+                    for (int e = 0; e < V; ++e) s[e] += rest[i] * to_f32(wt.e[e]);
                 }
 #pragma unroll
                 for (int e = 0; e < V; ++e) o.e[e] = from_f32<T>(s[e] * f);
@@ -573,7 +581,7 @@ Fwd carve_fwd(Carve &c, int dtype, int64_t M, int64_t D, int64_t V, bool padw, b
 
 struct Bwd {
     Rows r;
-    float *lse, *scale;
+    float *lse, *scale, *rest;
     void *dz;
     float *part;     // partials of dx (fp32: the sum and a piece's)
     float *wp, *bp, *gwp, *gbp;   // fp32: a piece's padded operands and gradients
@@ -588,6 +596,7 @@ Bwd carve_bwd(Carve &c, int dtype, int64_t M, int64_t D, int64_t V, bool padw, b
     b.r = carve_rows(c, dtype, M, D, V, padw, padb);
     b.lse = c.get<float>(M);
     b.scale = c.get<float>(M + 1);
+    b.rest = dtype == kBF16 ? c.get<float>(M) : nullptr;
     const int64_t p = piece(dtype, M, V), last = V - (V - 1) / p * p;
     const int64_t most = dtype == kBF16 ? (p + 7) / 8 * 8 : std::max(f32_words(M, p), f32_words(M, last));
     b.dz = c.raw((size_t)M * most * (dtype == kBF16 ? 2 : 4));
@@ -800,7 +809,7 @@ int launch_xent_bwd(int dtype, int64_t M, int64_t D, int64_t V, const void *x, c
             const bf16 *wv = (const bf16 *)w + v0 * D8;
             if (M > 0)
                 err = g2::xent_grad(M, D8, n, k.r.xc, wv, b ? (const bf16 *)b + v0 : nullptr, k.r.count, k.r.tgt, (int)v0, k.lse, k.scale,
-                                    k.dz, ldz, k.dbpart, st);
+                                    k.dz, ldz, k.rest, k.dbpart, st);
             if (!err && dx && M > 0) err = g2::xent_dx(M, D8, n, ldz, p, k.dz, wv, k.r.count, k.nsplit, k.part, v0 > 0, st);
             bf16 *dbv = db ? (bf16 *)db + v0 : nullptr;
             if (!err && dw)
@@ -843,10 +852,10 @@ int launch_xent_bwd(int dtype, int64_t M, int64_t D, int64_t V, const void *x, c
     if (err || !dx || M == 0) return err;
     if (dtype == kBF16)
         hipLaunchKernelGGL(finish_kernel<bf16>, dim3(row_grid(M)), dim3(256), 0, st, k.part, k.nsplit, M * D8, k.r.pos, M, (int)D, (int)D8,
-                           k.scale + M, (bf16 *)dx);
+                           k.scale + M, k.rest, k.r.tgt, (const bf16 *)w, (bf16 *)dx);
     else
         hipLaunchKernelGGL(finish_kernel<float>, dim3(row_grid(M)), dim3(256), 0, st, k.part, (const int *)nullptr, M * D8, k.r.pos, M, (int)D, (int)D8,
-                           (const float *)nullptr, (float *)dx);   // (its dz has the factor)
+                           (const float *)nullptr, (const float *)nullptr, k.r.tgt, (const float *)w, (float *)dx);   // (its dz has the factor)
     return (int)hipGetLastError();
 }
 
