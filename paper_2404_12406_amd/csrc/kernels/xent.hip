@@ -17,7 +17,7 @@
 //    at hand, and kept in place of x: two contractions in all instead of three.  It
 //    is dx without the loss's gradient, which backward multiplies it by.  bf16: by
 //    chunks of rows, whose exponentials p = exp(z - r) are written as bf16 beside
-//    their sums, r a reference that adjust_kernel() then makes one of each row:
+//    their sums, r a reference that combine_kernel() then makes one of each row:
 //      dx = (1 / sum) p W - (1 - p_t) W_t
 //    with the target's p left out of p W, so that what is left of it at a large
 //    p_t is no difference of rounded numbers.
@@ -115,15 +115,46 @@ __global__ __launch_bounds__(1024) void rows_kernel(const int64_t *__restrict__ 
 // common factor would give every row's largest entry, near -1 times it, the same
 // rounding error.  With nsplit: the splits of dx's contraction for each chunk of
 // `chunk` rows, and (ccount) the chunks' numbers of rows.
-template <typename T>
-__global__ __launch_bounds__(256) void gather_kernel(const T *__restrict__ x, const int *__restrict__ idx,
-                                                     const int *__restrict__ count, int64_t M, int D, int ld, bool fill,
+// SCAN: rows_kernel() is part of it: each block counts the rows before its own, for up
+// to kScanRows (one launch less; 16 bits hold a count).
+constexpr int kScanRows = 2048;
+template <typename T, bool SCAN>
+__global__ __launch_bounds__(256) void gather_kernel(const int64_t *__restrict__ target, int64_t ignore, int64_t words, int *__restrict__ pos,
+                                                     int *__restrict__ tgt, const T *__restrict__ x, const int *__restrict__ idx,
+                                                     int *__restrict__ count, int64_t M, int D, int ld, bool fill,
                                                      T *__restrict__ xc, const float *__restrict__ lse,
                                                      const float *__restrict__ gloss, int reduction, float *__restrict__ lsec,
                                                      float *__restrict__ scale, SplitRule rule, int *__restrict__ nsplit,
                                                      int64_t chunk, int *__restrict__ ccount) {
     constexpr int V = Vec16<T>::N;
-    const int n = *count;
+    int n, at = 0;        // the rows that count; SCAN: the place of this block's row
+    bool counts = true;
+    if constexpr (SCAN) {
+        __shared__ int sums[4];
+        const int r = (int)blockIdx.x;
+        int c = 0;   // all of them in the low half, those before r in the high one
+        for (int k = (int)threadIdx.x; k < M; k += 256) c += target[k] != ignore ? (k < r ? 0x10001 : 1) : 0;
+#pragma unroll
+        for (int o = 32; o > 0; o >>= 1) c += __shfl_xor(c, o);
+        if ((threadIdx.x & 63) == 0) sums[threadIdx.x >> 6] = c;
+        __syncthreads();
+        c = sums[0] + sums[1] + sums[2] + sums[3];
+        n = c & 0xffff;
+        at = c >> 16;
+        if (threadIdx.x == 0) {
+            if (r == 0) *count = n;
+            if (r < M) {
+                const int64_t t = target[r];
+                counts = t != ignore;
+                pos[r] = counts ? at : -1;
+                if (counts) tgt[at] = t >= 0 && t < words ? (int)t : -1;
+            }
+        }
+        if (r < M) counts = target[r] != ignore;
+        if (!counts) at = n + r - at;   // the others' places come after
+    } else {
+        n = *count;
+    }
     if (nsplit && blockIdx.x == 0)
         for (int64_t k = (int)threadIdx.x; k * chunk < M; k += 256) {
             const int rows = (int)min(max(n - k * chunk, (int64_t)0), chunk);
@@ -133,9 +164,10 @@ __global__ __launch_bounds__(256) void gather_kernel(const T *__restrict__ x, co
     // (no row that counts: every result is an empty sum, whatever the factor)
     if (lse && blockIdx.x == 0 && threadIdx.x == 0)
         scale[M] = reduction == 2 || n == 0 ? 1.f : reduction == 1 ? gloss[0] : gloss[0] / (float)n;
-    for (int64_t i = blockIdx.x; i < M; i += gridDim.x) {
+    for (int64_t k = blockIdx.x; k < M; k += gridDim.x) {
+        const int64_t i = SCAN ? at : k;
         if (i >= n && !fill) break;
-        const int64_t r = i < n ? idx[i] : 0;
+        const int64_t r = i >= n ? 0 : SCAN ? k : idx[i];
         for (int c = (int)threadIdx.x * V; c < ld; c += 256 * V)
             store_vec(xc + i * ld, c, ld, i < n && c < D ? load_vec(x + r * D, c, D) : zero16<T>());
         if (lse && threadIdx.x == 0) {
@@ -152,104 +184,116 @@ struct Kept {
 };
 
 // The loss and lse of every row from `parts` statistics [part][ld] of the rows that
-// count, of which this launch has those from place i0 to i0 + ld - 1 (32 rows a
-// block, eight threads each).
+// count, of which this launch has those from place i0 to i0 + ld - 1 (8 rows a
+// block, 32 threads each).  With prob (exponentials [ld][ldz] of kProbCols columns a
+// part): the parts of a row with another reference than the row's are brought to it.
 __global__ __launch_bounds__(256) void combine_kernel(const floatx2 *__restrict__ stat, int parts, int64_t ld, int64_t i0,
                                                       const float *__restrict__ tlogit, const int *__restrict__ pos,
                                                       const int *__restrict__ tgt, int64_t M, float *__restrict__ each,
-                                                      float *__restrict__ lse, Kept kept) {
-    __shared__ floatx2 red[8][32];
-    const int row = threadIdx.x & 31, grp = threadIdx.x >> 5;
-    const int64_t r = (int64_t)blockIdx.x * 32 + row;
+                                                      float *__restrict__ lse, Kept kept, bf16 *__restrict__ prob, int64_t ldz) {
+    constexpr int ROWS = 8, GROUPS = 256 / ROWS;
+    __shared__ floatx2 red[GROUPS][ROWS];
+    const int row = threadIdx.x % ROWS, grp = threadIdx.x / ROWS;
+    const int64_t r = (int64_t)blockIdx.x * ROWS + row;
     const int i = r < M ? pos[r] : -1;
     const bool here = i >= i0 && i < i0 + ld;
+    const floatx2 *s = stat + (here ? i - i0 : 0);
     floatx2 a = {-INFINITY, 0.f};
     if (here) {
-        const floatx2 *s = stat + (i - i0);
         int p = grp;
-        for (; p + 24 < parts; p += 32) {
+        for (; p + 3 * GROUPS < parts; p += 4 * GROUPS) {
             floatx2 v[4];
 #pragma unroll
-            for (int u = 0; u < 4; ++u) v[u] = s[(int64_t)(p + 8 * u) * ld];
+            for (int u = 0; u < 4; ++u) v[u] = s[(int64_t)(p + GROUPS * u) * ld];
 #pragma unroll
             for (int u = 0; u < 4; ++u) a = join_lse(a, v[u]);
         }
-        for (; p < parts; p += 8) a = join_lse(a, s[(int64_t)p * ld]);
+        for (; p < parts; p += GROUPS) a = join_lse(a, s[(int64_t)p * ld]);
     }
     red[grp][row] = a;
     __syncthreads();
-    if (grp != 0 || r >= M || (i >= 0 && !here)) return;
-#pragma unroll
-    for (int q = 1; q < 8; ++q) a = join_lse(a, red[q][row]);
-    float l = 0.f, loss = 0.f;
-    if (i >= 0) {
-        // no word at all, or every one of them minus infinity: no distribution
-        const bool none = tgt[i] < 0 || a.x == -INFINITY;
-        const float ls = none ? NAN : logf(a.y);
-        l = a.x + ls;
-        // (the difference first: it is exact where both are large)
-        loss = (a.x - (tgt[i] < 0 ? 0.f : tlogit[i])) + ls;
-        if (kept.ref) {
-            kept.ref[i] = a.x;
-            kept.f[i] = none ? NAN : 1.f / a.y;
-            kept.ct[i] = expm1f(-loss);
+    if (grp == 0) {
+        for (int q = 1; q < GROUPS; ++q) a = join_lse(a, red[q][row]);
+        red[0][row] = a;
+        if (r < M && (i < 0 || here)) {
+            float l = 0.f, loss = 0.f;
+            if (here) {
+                // no word at all, or every one of them minus infinity: no distribution
+                const bool none = tgt[i] < 0 || a.x == -INFINITY;
+                const float ls = none ? NAN : logf(a.y);
+                l = a.x + ls;
+                // (the difference first: it is exact where both are large)
+                loss = (a.x - (tgt[i] < 0 ? 0.f : tlogit[i])) + ls;
+                if (kept.ref) {
+                    kept.ref[i] = a.x;
+                    kept.f[i] = none ? NAN : 1.f / a.y;
+                    kept.ct[i] = expm1f(-loss);
+                }
+            }
+            if (lse) lse[r] = l;
+            each[r] = loss;
         }
     }
-    if (lse) lse[r] = l;
-    each[r] = loss;
+    if (!prob) return;
+    __syncthreads();
+    if (!here) return;
+    const float to = red[0][row].x;
+    for (int p = grp; p < parts; p += GROUPS) {
+        const float from = s[(int64_t)p * ld].x;
+        if (from == to || from == -INFINITY) continue;   // (nothing but zeros there)
+        const float f = exp_below(from, to);
+        bf16 *at = prob + (i - i0) * ldz + (int64_t)p * kProbCols;
+        for (int c = 0; c < kProbCols && (int64_t)p * kProbCols + c < ldz; c += 8) {
+            Vec16<bf16> v = load16(at + c);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v.e[e] = from_f32<bf16>(to_f32(v.e[e]) * f);
+            *reinterpret_cast<u32x4 *>(at + c) = v.u;
+        }
+    }
 }
 
-// *out = the sum of each[0 .. M), over *count where it is to be the mean.
-__global__ __launch_bounds__(1024) void total_kernel(const float *__restrict__ each, int64_t M, const int *__restrict__ count,
-                                                     bool mean, float *__restrict__ out) {
-    __shared__ double red[16];
+// *out = the sum of each[0 .. M), over *count where it is to be the mean: a block of N.
+template <int N>
+__device__ __forceinline__ void total(const float *__restrict__ each, int64_t M, const int *__restrict__ count, bool mean,
+                                      float *__restrict__ out) {
+    __shared__ double red[N / 64];
     double s = 0.0;
-    for (int64_t r = threadIdx.x; r < M; r += 1024) s += (double)each[r];
+    for (int64_t r = threadIdx.x; r < M; r += N) s += (double)each[r];
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) s += __shfl_xor(s, o);
     if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = s;
     __syncthreads();
     if (threadIdx.x != 0) return;
-    for (int w = 1; w < 16; ++w) s += red[w];
+    for (int w = 1; w < N / 64; ++w) s += red[w];
     *out = (float)(mean ? s / (double)*count : s);
 }
 
-// prob[i][64 g ..] *= exp(r - ref[i]) where part g of row i has another reference r.
-__global__ __launch_bounds__(256) void adjust_kernel(bf16 *__restrict__ prob, int64_t ldz, const int *__restrict__ count,
-                                                     const floatx2 *__restrict__ stat, int64_t ld, int parts,
-                                                     const float *__restrict__ ref) {
-    const int i = (int)blockIdx.x * 256 + (int)threadIdx.x;
-    if (i >= *count) return;
-    const float to = ref[i];
-    for (int g = blockIdx.y; g < parts; g += gridDim.y) {
-        const float r = stat[(int64_t)g * ld + i].x;
-        if (r == to || r == -INFINITY) continue;   // (nothing but zeros there)
-        const float f = exp_below(r, to);
-        bf16 *p = prob + i * ldz + g * kProbCols;
-        for (int c = 0; c < kProbCols && g * kProbCols + c < ldz; c += 8) {
-            Vec16<bf16> v = load16(p + c);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) v.e[e] = from_f32<bf16>(to_f32(v.e[e]) * f);
-            *reinterpret_cast<u32x4 *>(p + c) = v.u;
-        }
-    }
+__global__ __launch_bounds__(1024) void total_kernel(const float *__restrict__ each, int64_t M, const int *__restrict__ count,
+                                                     bool mean, float *__restrict__ out) {
+    total<1024>(each, M, count, mean, out);
 }
 
 // The kept gradient of the rows at places i0 .. i0 + chunk - 1, and zeros (by the first
 // chunk's launch) for the rows that do not count: the sum of the partials, with f
 // times it and ct times the target's row of w; over their number where the loss is
 // the mean.  bf16: in 24 bits, a plane [M][D] of the leading 16 and one of the others
-// (rounded once more when backward has multiplied it: 2^-17 does not show).
+// (rounded once more when backward has multiplied it: 2^-17 does not show).  With
+// loss, one more block takes its sum from each row's.
 template <typename T>
 __global__ __launch_bounds__(256) void keep_kernel(const float *__restrict__ part, const int *__restrict__ nsplit, int64_t stride,
                                                    const int *__restrict__ pos, int64_t M, int D, int ld, int64_t i0, int64_t chunk,
                                                    const int *__restrict__ count, bool mean, const float *__restrict__ f,
                                                    const float *__restrict__ ct, const int *__restrict__ tgt, const T *__restrict__ w,
-                                                   void *__restrict__ kept) {
+                                                   void *__restrict__ kept, const float *__restrict__ each, float *__restrict__ loss) {
     constexpr int V = Vec16<T>::N;
+    const int blocks = (int)gridDim.x - (loss ? 1 : 0);
+    if ((int)blockIdx.x == blocks) {
+        total<256>(each, M, count, mean, loss);
+        return;
+    }
     const int splits = nsplit ? *nsplit : 1;
     const float all = mean ? 1.f / (float)*count : 1.f;
-    for (int64_t r = blockIdx.x; r < M; r += gridDim.x) {
+    for (int64_t r = blockIdx.x; r < M; r += blocks) {
         const int i = pos[r];
         if (i < 0 ? i0 > 0 : i < i0 || i >= i0 + chunk) continue;
         const int t = i < 0 || !f ? -1 : tgt[i];
@@ -633,13 +677,14 @@ int row_grid(int64_t M) { return (int)std::max<int64_t>(1, std::min<int64_t>(M, 
 int start(const Rows &r, int dtype, int64_t M, int64_t D, int64_t V, const void *x, const void **w, const void **b,
           const int64_t *target, int64_t ignore, const float *lse, const float *gloss, int reduction, float *lsec, float *scale,
           const SplitRule &rule, int *nsplit, int64_t chunk, int *ccount, hipStream_t st) {
-    hipLaunchKernelGGL(rows_kernel, dim3(1), dim3(1024), 0, st, target, ignore, M, V, r.pos, r.idx, r.tgt, r.count);
-    if (dtype == kBF16)
-        hipLaunchKernelGGL(gather_kernel<bf16>, dim3(row_grid(M)), dim3(256), 0, st, (const bf16 *)x, r.idx, r.count, M, (int)D,
-                           (int)r.D8, false, (bf16 *)r.xc, lse, gloss, reduction, lsec, scale, rule, nsplit, chunk, ccount);
-    else
-        hipLaunchKernelGGL(gather_kernel<float>, dim3(row_grid(M)), dim3(256), 0, st, (const float *)x, r.idx, r.count, M, (int)D,
-                           (int)r.D8, true, (float *)r.xc, lse, gloss, reduction, lsec, scale, rule, nsplit, chunk, ccount);
+    const bool scan = M <= kScanRows;   // (a block a row)
+    if (!scan) hipLaunchKernelGGL(rows_kernel, dim3(1), dim3(1024), 0, st, target, ignore, M, V, r.pos, r.idx, r.tgt, r.count);
+    auto gather = [&](auto kernel, auto *xs, auto *xc, bool fill) {
+        hipLaunchKernelGGL(kernel, dim3(row_grid(M)), dim3(256), 0, st, target, ignore, V, r.pos, r.tgt, xs, r.idx, r.count, M, (int)D, (int)r.D8,
+                           fill, xc, lse, gloss, reduction, lsec, scale, rule, nsplit, chunk, ccount);
+    };
+    if (dtype == kBF16) gather(scan ? gather_kernel<bf16, true> : gather_kernel<bf16, false>, (const bf16 *)x, (bf16 *)r.xc, false);
+    else gather(scan ? gather_kernel<float, true> : gather_kernel<float, false>, (const float *)x, (float *)r.xc, true);
     int err = (int)hipGetLastError();
     CopyJob j[kCopies];
     int n = 0;
@@ -716,9 +761,15 @@ int launch_xent_fwd(int dtype, int64_t M, int64_t D, int64_t V, const void *x, c
     if (err) return err;
     if (dtype == kBF16 && M > 0 && !g2::rows_ok(M, V, D8, f.r.xc, w)) return (int)hipErrorInvalidValue;
     float *each = reduction == 2 ? loss : f.each;
-    auto combine = [&](int parts, int64_t ld, int64_t i0) {
-        hipLaunchKernelGGL(combine_kernel, dim3((unsigned)((M + 31) / 32)), dim3(256), 0, st, (const floatx2 *)f.stat, parts, ld, i0, f.tlogit,
-                           f.r.pos, f.r.tgt, M, each, lse, f.kept);
+    auto combine = [&](int parts, int64_t ld, int64_t i0, bf16 *prob, int64_t ldz) {
+        hipLaunchKernelGGL(combine_kernel, dim3((unsigned)((M + 7) / 8)), dim3(256), 0, st, (const floatx2 *)f.stat, parts, ld, i0, f.tlogit,
+                           f.r.pos, f.r.tgt, M, each, lse, f.kept, prob, ldz);
+        return (int)hipGetLastError();
+    };
+    auto keep = [&](auto kernel, auto *w0, const int *splits, int64_t i0, int64_t R, const float *kf, const float *ct) {
+        float *out = reduction == 2 || i0 + R < M ? nullptr : loss;
+        hipLaunchKernelGGL(kernel, dim3(row_grid(M) + (out ? 1 : 0)), dim3(256), 0, st, f.part, splits, R * D8, f.r.pos, M, (int)D, (int)D8, i0, R,
+                           f.r.count, reduction == 0, kf, ct, f.r.tgt, w0, kept, each, out);
         return (int)hipGetLastError();
     };
     if (M == 0) {
@@ -729,20 +780,13 @@ int launch_xent_fwd(int dtype, int64_t M, int64_t D, int64_t V, const void *x, c
             const int64_t m = std::min(R, M - i0);
             const int parts = g2::xent_prob_parts(m, D8, V);
             err = g2::xent_prob(m, D8, V, xc, w, b, f.ccount + k, f.r.tgt + i0, f.stat, R, f.tlogit + i0, f.prob, ldz, st);
-            if (!err) err = combine(parts, R, i0);
-            if (err) break;
-            hipLaunchKernelGGL(adjust_kernel, dim3((unsigned)((R + 255) / 256), (unsigned)std::min(parts, 2048)), dim3(256), 0, st, f.prob, ldz,
-                               f.ccount + k, (const floatx2 *)f.stat, R, parts, f.kept.ref + i0);
-            err = (int)hipGetLastError();
+            if (!err) err = combine(parts, R, i0, f.prob, ldz);
             if (!err) err = g2::xent_dx(R, D8, V, ldz, V, f.prob, w, f.ccount + k, f.nsplit + k, f.part, false, st);
-            if (err) break;
-            hipLaunchKernelGGL(keep_kernel<bf16>, dim3(row_grid(M)), dim3(256), 0, st, f.part, f.nsplit + k, R * D8, f.r.pos, M, (int)D, (int)D8,
-                               i0, R, f.r.count, reduction == 0, f.kept.f, f.kept.ct, f.r.tgt, (const bf16 *)w, kept);
-            err = (int)hipGetLastError();
+            if (!err) err = keep(keep_kernel<bf16>, (const bf16 *)w, f.nsplit + k, i0, R, f.kept.f, f.kept.ct);
         }
     } else if (dtype == kBF16) {
         err = g2::xent_lse(M, D8, V, f.r.xc, w, b, f.r.count, f.r.tgt, f.stat, f.tlogit, st);
-        if (!err) err = combine(g2::xent_lse_tiles(M, D8, V), M, 0);
+        if (!err) err = combine(g2::xent_lse_tiles(M, D8, V), M, 0, nullptr, 0);
     } else {
         const int64_t p = piece(dtype, M, V);
         Piece q;
@@ -755,22 +799,18 @@ int launch_xent_fwd(int dtype, int64_t M, int64_t D, int64_t V, const void *x, c
                                v0 == 0, (floatx2 *)f.stat, f.tlogit);
             err = (int)hipGetLastError();
         }
-        if (!err) err = combine(1, M, 0);
+        if (!err) err = combine(1, M, 0, nullptr, 0);
         if (!err && kept) {   // (one piece)
             hipLaunchKernelGGL(grad_rows_kernel, dim3(row_grid(M)), dim3(256), 0, st, f.z, (int)q.np, (int)V, 0, M, f.r.count, f.r.tgt,
                                f.kept.ref, f.kept.f, (const float *)nullptr);
             err = (int)hipGetLastError();
             if (!err)
                 err = launch_linear_bwd(dtype, M, D8, q.np, f.r.count, f.z, f.r.xc, q.w, f.part, nullptr, nullptr, f.conv, stream);
-            if (err) return err;
-            hipLaunchKernelGGL(keep_kernel<float>, dim3(row_grid(M)), dim3(256), 0, st, f.part, (const int *)nullptr, M * D8, f.r.pos, M,
-                               (int)D, (int)D8, (int64_t)0, M, f.r.count, reduction == 0, (const float *)nullptr, (const float *)nullptr,
-                               f.r.tgt, (const float *)w, kept);
-            err = (int)hipGetLastError();
+            if (!err) err = keep(keep_kernel<float>, (const float *)w, nullptr, 0, M, nullptr, nullptr);
         }
     }
     if (err) return err;
-    if (reduction != 2)
+    if (reduction != 2 && !kept)
         hipLaunchKernelGGL(total_kernel, dim3(1), dim3(1024), 0, st, each, M, f.r.count, reduction == 0, loss);
     return (int)hipGetLastError();
 }
