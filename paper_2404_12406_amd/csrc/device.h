@@ -35,6 +35,7 @@ struct ConvGeom : ConvDims {
     // the fp32 Linear contractions (1 x 1) take no more than the first *count of the N
     // rows (their results past them are not written), a number on the device; null: all
     const int *count = nullptr;
+    bool fine = false;   // the fp32 Linear input gradient takes small tiles in many blocks
 };
 
 // y = W * x + b (b may be null).  May use conv_fwd_workspace() bytes of

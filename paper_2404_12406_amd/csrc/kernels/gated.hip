@@ -268,7 +268,8 @@ int launch_copy_rows(int dtype, const CopyJob *jobs, int n, void *stream) {
 }
 
 size_t linear_bwd_workspace(int dtype, int64_t M, int64_t K, int64_t N, bool dx, bool dw, bool db) {
-    const ConvGeom g = gated::linear(M, K, N);
+    ConvGeom g = gated::linear(M, K, N);
+    g.fine = true;
     size_t ws = 0;
     if (dx) ws = std::max(ws, conv_dgrad_workspace(dtype, g, db && !dw));
     if (dw) ws = std::max(ws, conv_wgrad_workspace(dtype, g, db));
@@ -280,6 +281,7 @@ int launch_linear_bwd(int dtype, int64_t M, int64_t K, int64_t N, const int *cou
                       void *dx, void *dw, void *db, void *ws, void *stream) {
     ConvGeom g = gated::linear(M, K, N);
     g.count = count;
+    g.fine = true;
     bool done = false;
     int err = 0;
     if (dx) err = launch_conv_dgrad(dtype, g, dy, w, nullptr, dx, ws, stream, dw ? nullptr : db, &done);

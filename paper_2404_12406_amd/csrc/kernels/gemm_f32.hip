@@ -699,7 +699,27 @@ bool geom_ok(const ConvGeom &g) {
 Plan fwd_plan(const ConvGeom &g) {
     return plan(kFwd, (int64_t)g.N * g.P * g.Q, g.K, (int64_t)g.R * g.S * g.C, 1, y_elems(g), kPartialCap);
 }
+// The input gradient of a Linear layer within a larger one (ConvGeom::fine): 64 x 64
+// tiles and some eight blocks a CU.  How many rows count is known on the device only,
+// and small blocks leave the least of a last round idle; with all of them counting they
+// are no slower.  us of a whole fp32 cross entropy's input and bias gradient, forward
+// included, with plan()'s choice and so; a third of the rows ignored:
+//   777 x 544 x 10016    259 -> 228    2000 x 1024 x 20000   1700 -> 1518
+//   300 x 512 x 5024     109 -> 110    4096 x 768 x 8000     1088 -> 1044
+// and none:
+//   777 x 544 x 10016    331 -> 296    2000 x 1024 x 20000   2115 -> 2071
+//   300 x 512 x 5024     112 -> 115    4096 x 768 x 8000     1313 -> 1320
+constexpr int64_t kFineCap = int64_t(32) << 20;
+Plan fine_plan(int64_t M, int64_t N, int64_t K) {
+    const int64_t tiles = std::max<int64_t>(1, (M + 63) / 64 * ((N + 63) / 64));
+    const int64_t most = std::min(K / (6 * BK), kFineCap / std::max<int64_t>(1, 4 * part_stride(M * N)));
+    const int64_t sp = std::clamp<int64_t>(8 * kCUs / tiles, 1, std::max<int64_t>(1, most));
+    Plan p{2, 1, (int)std::max<int64_t>(BK, ((K + sp - 1) / sp + BK - 1) / BK * BK), est_us(kTiles[2], M, N, K, 1, (int)sp)};
+    p.splits = (int)std::max<int64_t>(1, (K + p.k_split - 1) / p.k_split);
+    return p;
+}
 Plan dgrad_plan(const ConvGeom &g) {
+    if (g.fine) return fine_plan(g.N, g.C, g.K);
     const int64_t Hb = (g.H + g.sh - 1) / g.sh, Wb = (g.W + g.sw - 1) / g.sw;
     const int64_t Kb = (int64_t)((g.R + g.sh - 1) / g.sh) * ((g.S + g.sw - 1) / g.sw) * g.K;
     return plan(kDgrad, g.N * Hb * Wb, g.C, Kb, g.sh * g.sw, x_elems(g), kPartialCap);
@@ -819,7 +839,7 @@ int conv_dgrad(const ConvGeom &g, const void *dy, const void *w, const void *bia
     a.K = ((g.R + g.sh - 1) / g.sh) * ((g.S + g.sw - 1) / g.sw) * g.K;
     if (a.M == 0 || a.N == 0) return 0;
     Plan p = dgrad_plan(g);
-    if (few::dgrad_us(g, dy) < p.us) return few::conv_dgrad(g, dy, w, bias, dx, st);
+    if (!g.fine && few::dgrad_us(g, dy) < p.us) return few::conv_dgrad(g, dy, w, bias, dx, st);
     if (p.splits > 1 && (!ws || !al16(ws))) p.splits = 1;
     return run<kDgrad>(p, g.K % 4 == 0 && g.C % 4 == 0 && al16(dy) && al16(w), a, g.sh * g.sw, x_elems(g),
                        (const float *)bias, (float *)dx, ws, st);
