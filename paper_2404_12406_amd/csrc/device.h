@@ -35,6 +35,9 @@ struct ConvGeom : ConvDims {
     // the fp32 Linear contractions (1 x 1) take no more than the first *count of the N
     // rows (their results past them are not written), a number on the device; null: all
     const int *count = nullptr;
+    // the fp32 Linear contractions: W and dW have this many rows, fewer than K (0: K); the
+    // others read as zeros and are not written
+    int wrows = 0;
     bool fine = false;   // the fp32 Linear input gradient takes small tiles in many blocks
 };
 
@@ -176,9 +179,9 @@ size_t gated_bwd_workspace(int dtype, int64_t M, int64_t D, int64_t F, const voi
 int launch_gated_bwd(int dtype, int64_t M, int64_t D, int64_t F, int act, const void *x, const void *w, const void *b, const void *proj,
                      const void *dy, void *dx, void *dw, void *db, void *ws, void *stream);
 // The gradients of a Linear x[M][K] -> [M][N] (any of dx, dw, db may be null); count:
-// as ConvGeom's.
+// as ConvGeom's; wrows: so, or N.
 size_t linear_bwd_workspace(int dtype, int64_t M, int64_t K, int64_t N, bool dx, bool dw, bool db);
-int launch_linear_bwd(int dtype, int64_t M, int64_t K, int64_t N, const int *count, const void *dy, const void *x, const void *w,
+int launch_linear_bwd(int dtype, int64_t M, int64_t K, int64_t N, int64_t wrows, const int *count, const void *dy, const void *x, const void *w,
                       void *dx, void *dw, void *db, void *ws, void *stream);
 
 // Softmax cross entropy of the logits x[M][D] w[V][D]^T + b (b may be null) of the

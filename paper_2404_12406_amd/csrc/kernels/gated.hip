@@ -277,10 +277,11 @@ size_t linear_bwd_workspace(int dtype, int64_t M, int64_t K, int64_t N, bool dx,
     return ws;
 }
 
-int launch_linear_bwd(int dtype, int64_t M, int64_t K, int64_t N, const int *count, const void *dy, const void *x, const void *w,
+int launch_linear_bwd(int dtype, int64_t M, int64_t K, int64_t N, int64_t wrows, const int *count, const void *dy, const void *x, const void *w,
                       void *dx, void *dw, void *db, void *ws, void *stream) {
     ConvGeom g = gated::linear(M, K, N);
     g.count = count;
+    g.wrows = wrows < N ? (int)wrows : 0;
     g.fine = true;
     bool done = false;
     int err = 0;
@@ -378,7 +379,7 @@ int launch_gated_bwd(int dtype, int64_t M, int64_t D, int64_t F, int act, const 
             if (!g2::rows_ok(M, 2 * F, k.p.D, xp, wp)) return (int)hipErrorInvalidValue;
             err = g2::gate_grad(M, k.p.D, F, act, xp, wp, bp, dy, dz, st);
         }
-        return err ? err : launch_linear_bwd(dtype, M, D, 2 * F, nullptr, dz, x, w, dx, dw, db, c + k.work, stream);
+        return err ? err : launch_linear_bwd(dtype, M, D, 2 * F, 2 * F, nullptr, dz, x, w, dx, dw, db, c + k.work, stream);
     }
     const int64_t Dp = k.p.D, Fp = k.p.F;
     if (M && !proj) err = launch_conv_fwd(dtype, gated::linear(M, Dp, 2 * Fp), xp, wp, bp, dz, c + k.work, stream);
@@ -386,7 +387,7 @@ int launch_gated_bwd(int dtype, int64_t M, int64_t D, int64_t F, int act, const 
     const bool tx = dx && Dp != D, tw = dw && k.p.any, tb = db && Fp != F;   // gradients by way of padded ones
     char *gx = c + k.gx, *gw = c + k.gw, *gb = c + k.gb;
     if (!err)
-        err = launch_linear_bwd(dtype, M, Dp, 2 * Fp, nullptr, dz, xp, wp, tx ? gx : dx, tw ? gw : dw, tb ? gb : db, c + k.work, stream);
+        err = launch_linear_bwd(dtype, M, Dp, 2 * Fp, 2 * Fp, nullptr, dz, xp, wp, tx ? gx : dx, tw ? gw : dw, tb ? gb : db, c + k.work, stream);
     CopyJob j[kCopies];
     int n = 0;
     if (tx) j[n++] = {gx, Dp, M, D, dx, M, D};

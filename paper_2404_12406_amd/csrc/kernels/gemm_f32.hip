@@ -789,7 +789,7 @@ int run(const Plan &p, bool vec, Args &a, int z, int64_t out_elems, const float 
     a.c = p.splits > 1 ? static_cast<float *>(ws) : out;
     a.bias = p.splits > 1 ? nullptr : bias;
     a.a_bytes = (uint32_t)(MODE == kFwd ? x_elems(a.g) * 4 : y_elems(a.g) * 4);
-    a.b_bytes = (uint32_t)(MODE == kWgrad ? x_elems(a.g) * 4 : w_elems(a.g) * 4);
+    a.b_bytes = (uint32_t)(MODE == kWgrad ? x_elems(a.g) * 4 : (a.g.wrows ? (int64_t)a.g.wrows * a.g.C : w_elems(a.g)) * 4);
     a.dch = fastdiv(MODE == kDgrad ? a.g.K : a.g.C);
     a.ds = fastdiv(a.g.S);
     a.dpq = fastdiv(a.g.P * a.g.Q);
@@ -850,7 +850,7 @@ int conv_wgrad(const ConvGeom &g, const void *dy, const void *x, void *dw, void 
     if (!geom_ok(g)) return -1;
     Args a{};
     a.a = (const float *)dy; a.b = (const float *)x; a.g = g;
-    a.M = g.K; a.N = g.R * g.S * g.C; a.K = g.N * g.P * g.Q;
+    a.M = g.wrows ? g.wrows : g.K; a.N = g.R * g.S * g.C; a.K = g.N * g.P * g.Q;
     if (a.M == 0 || a.N == 0) return 0;
     const int rows = few_rows(g, cap);
     if (rows && ws && al16(ws)) {
@@ -859,7 +859,7 @@ int conv_wgrad(const ConvGeom &g, const void *dy, const void *x, void *dw, void 
     }
     const Plan p = wgrad_plan(g, (int64_t)cap);
     if (p.splits > 1 && (!ws || !al16(ws))) return (int)hipErrorInvalidValue;
-    return run<kWgrad>(p, g.K % 4 == 0 && g.C % 4 == 0 && al16(dy) && al16(x), a, 1, w_elems(g), nullptr, (float *)dw, ws, st);
+    return run<kWgrad>(p, g.K % 4 == 0 && g.C % 4 == 0 && al16(dy) && al16(x), a, 1, (int64_t)a.M * a.N, nullptr, (float *)dw, ws, st);
 }
 
 // What a pass (0 forward, 1 input gradient, 2 weight gradient) lays out: out =

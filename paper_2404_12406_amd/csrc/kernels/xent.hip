@@ -520,19 +520,25 @@ ConvGeom linear(int64_t M, int64_t K, int64_t N) {
 }
 
 // fp32 contractions take 16-byte loads where widths are multiples of 4 and take
-// twice as long or more where they are not: from kPadRows rows on (fewer are not
-// worth a copy of W) such a piece runs on zero-padded copies of its rows of W and
-// its biases, as wide and as many as these say.
+// twice as long or more where they are not.  So z has as many columns as f32_words()
+// says, of which the contractions know those that are words (ConvGeom::wrows), and
+// from kPadRows rows on (fewer are not worth a copy of W) rows of W of another width
+// run on zero-padded copies as wide as f32_width() says.
+// us, forward alone / with all gradients, with 4-byte loads and on copies:
+//   40 x 511 x 39536    81 / 284 and  93 / 307    70 x 511 x 39536   102 / 381 and 109 / 372
+//   36 x 3485 x 30640  216 / 934 and 303 / 1098   71 x 3485 x 30640  344 / 1488 and 395 / 1473
 constexpr int64_t kPadRows = 96;
 int64_t f32_width(int64_t M, int64_t D) { return M >= kPadRows && D % 4 ? (D + 31) / 32 * 32 : D; }
-int64_t f32_words(int64_t M, int64_t V) { return M >= kPadRows && V % 4 ? (V + 31) / 32 * 32 : V; }
+int64_t f32_words(int64_t M, int64_t D8, int64_t V) {
+    const int64_t n = (V + 31) / 32 * 32;
+    // (past 2^30 elements the contraction is one that does not know them)
+    return V % 4 && std::max({M * D8, n * D8, M * n}) < int64_t(1) << 30 ? n : V;
+}
 
 // A piece's operands as the contractions take them.
 struct Piece {
     int64_t n, np;          // words, and columns of z
     const float *w, *b;
-    float *dw, *db;         // the gradients' places, padded or the caller's
-    bool own;               // padded
 };
 
 // Workspace of a call, carved in order.
@@ -611,13 +617,13 @@ Fwd carve_fwd(Carve &c, int dtype, int64_t M, int64_t D, int64_t V, bool padw, b
         f.part = c.get<float>((dtype == kBF16 ? f.rule.most * f.chunk : M) * f.r.D8);
     }
     if (dtype != kBF16) {
-        const int64_t p = piece(dtype, M, V), last = V - (V - 1) / p * p, most = std::max(f32_words(M, p), f32_words(M, last));
+        const int64_t p = piece(dtype, M, V), last = V - (V - 1) / p * p, most = std::max(f32_words(M, f.r.D8, p), f32_words(M, f.r.D8, last));
         f.z = c.get<float>(M * most);
-        f.wp = M >= kPadRows ? c.get<float>(most * f.r.D8) : nullptr;
-        f.bp = M >= kPadRows ? c.get<float>(most) : nullptr;
+        f.wp = f.r.D8 != D ? c.get<float>(p * f.r.D8) : nullptr;
+        f.bp = c.get<float>(most);
         size_t ws = 0;
-        for (int64_t v : {p, last}) ws = std::max(ws, conv_fwd_workspace(dtype, linear(M, f.r.D8, f32_words(M, v))));
-        if (keep) ws = std::max(ws, linear_bwd_workspace(dtype, M, f.r.D8, f32_words(M, V), true, false, false));
+        for (int64_t v : {p, last}) ws = std::max(ws, conv_fwd_workspace(dtype, linear(M, f.r.D8, f32_words(M, f.r.D8, v))));
+        if (keep) ws = std::max(ws, linear_bwd_workspace(dtype, M, f.r.D8, f32_words(M, f.r.D8, V), true, false, false));
         f.conv = c.raw(ws);
     }
     return f;
@@ -642,12 +648,12 @@ Bwd carve_bwd(Carve &c, int dtype, int64_t M, int64_t D, int64_t V, bool padw, b
     b.scale = c.get<float>(M + 1);
     b.rest = dtype == kBF16 ? c.get<float>(M) : nullptr;
     const int64_t p = piece(dtype, M, V), last = V - (V - 1) / p * p;
-    const int64_t most = dtype == kBF16 ? (p + 7) / 8 * 8 : std::max(f32_words(M, p), f32_words(M, last));
+    const int64_t most = dtype == kBF16 ? (p + 7) / 8 * 8 : std::max(f32_words(M, b.r.D8, p), f32_words(M, b.r.D8, last));
     b.dz = c.raw((size_t)M * most * (dtype == kBF16 ? 2 : 4));
-    if (dtype != kBF16 && M >= kPadRows) {
-        b.wp = c.get<float>(most * b.r.D8);
+    if (dtype != kBF16) {
+        b.wp = b.r.D8 != D ? c.get<float>(p * b.r.D8) : nullptr;
         b.bp = c.get<float>(most);
-        b.gwp = dw ? c.get<float>(most * b.r.D8) : nullptr;
+        b.gwp = dw && b.r.D8 != D ? c.get<float>(p * b.r.D8) : nullptr;
         b.gbp = db ? c.get<float>(most) : nullptr;
     }
     size_t ws = 0;
@@ -655,8 +661,8 @@ Bwd carve_bwd(Carve &c, int dtype, int64_t M, int64_t D, int64_t V, bool padw, b
         if (dtype == kBF16) {
             if (dw) ws = std::max(ws, g2::xent_dw_workspace(M, b.r.D8, D, v));
         } else {
-            ws = std::max(ws, conv_fwd_workspace(dtype, linear(M, b.r.D8, f32_words(M, v))));
-            ws = std::max(ws, linear_bwd_workspace(dtype, M, b.r.D8, f32_words(M, v), dx, dw, db));
+            ws = std::max(ws, conv_fwd_workspace(dtype, linear(M, b.r.D8, f32_words(M, b.r.D8, v))));
+            ws = std::max(ws, linear_bwd_workspace(dtype, M, b.r.D8, f32_words(M, b.r.D8, v), dx, dw, db));
         }
     }
     if (dtype == kBF16 && db) b.dbpart = c.get<float>((M + 63) / 64 * 4 * most);   // (rows of 64 or more, in whole tiles)
@@ -704,23 +710,26 @@ int start(const Rows &r, int dtype, int64_t M, int64_t D, int64_t V, const void 
 int take_piece(Piece *q, int64_t M, int64_t D, int64_t D8, int64_t v0, int64_t n, const void *w, const void *b, float *wp, float *bp,
                hipStream_t st) {
     q->n = n;
-    q->np = f32_words(M, n);
+    q->np = f32_words(M, D8, n);
     q->w = (const float *)w + v0 * D;
     q->b = b ? (const float *)b + v0 : nullptr;
-    q->own = wp && (q->np != n || D8 != D || (reinterpret_cast<uintptr_t>(q->w) & 15u));
-    if (!q->own) return 0;
-    CopyJob j[kCopies] = {{q->w, D, n, D, wp, q->np, D8}};
-    q->w = wp;
-    if (b) {
-        j[1] = {q->b, n, 1, n, bp, 1, q->np};
+    CopyJob j[kCopies];
+    int jobs = 0;
+    if (D8 != D) {
+        j[jobs++] = {q->w, D, n, D, wp, n, D8};
+        q->w = wp;
+    }
+    if (b && q->np != n) {
+        j[jobs++] = {q->b, n, 1, n, bp, 1, q->np};
         q->b = bp;
     }
-    return launch_copy_rows(kF32, j, b ? 2 : 1, st);
+    return launch_copy_rows(kF32, j, jobs, st);
 }
 
 int logits(const Piece &q, const Rows &r, int64_t M, float *z, void *ws, hipStream_t st) {
     ConvGeom g = linear(M, r.D8, q.np);
     g.count = r.count;
+    g.wrows = q.np != q.n ? (int)q.n : 0;
     return launch_conv_fwd(kF32, g, r.xc, q.w, q.b, z, ws, st);
 }
 
@@ -805,7 +814,7 @@ int launch_xent_fwd(int dtype, int64_t M, int64_t D, int64_t V, const void *x, c
                                f.kept.ref, f.kept.f, (const float *)nullptr);
             err = (int)hipGetLastError();
             if (!err)
-                err = launch_linear_bwd(dtype, M, D8, q.np, f.r.count, f.z, f.r.xc, q.w, f.part, nullptr, nullptr, f.conv, stream);
+                err = launch_linear_bwd(dtype, M, D8, q.np, q.n, f.r.count, f.z, f.r.xc, q.w, f.part, nullptr, nullptr, f.conv, stream);
             if (!err) err = keep(keep_kernel<float>, (const float *)w, nullptr, 0, M, nullptr, nullptr);
         }
     }
@@ -873,9 +882,9 @@ int launch_xent_bwd(int dtype, int64_t M, int64_t D, int64_t V, const void *x, c
                                    k.r.tgt, k.lse, (const float *)nullptr, k.scale);
                 err = (int)hipGetLastError();
             }
-            const bool tw = dw && (q.np != n || D8 != D), tb = db && q.np != n;
+            const bool tw = dw && D8 != D, tb = db && q.np != n;
             if (!err)
-                err = launch_linear_bwd(dtype, M, D8, q.np, k.r.count, z, k.r.xc, q.w, dx && M > 0 ? tmp : nullptr, tw ? k.gwp : dwv,
+                err = launch_linear_bwd(dtype, M, D8, q.np, q.n, k.r.count, z, k.r.xc, q.w, dx && M > 0 ? tmp : nullptr, tw ? k.gwp : dwv,
                                         tb ? k.gbp : dbv, k.work, stream);
             CopyJob j[kCopies];
             int jobs = 0;
