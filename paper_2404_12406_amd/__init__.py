@@ -3,7 +3,9 @@ Linear and BatchNorm in evaluation mode whose forward keeps the layer input only
 the weight gradient is requested and whose backward launches only the
 requested gradient work (Sec. 2.2.1 of arXiv 2404.12406), and a ReLU that
 keeps one bit per element instead of its output and a dropout that keeps its
-generator state instead of its mask (Sec. 2.2.2).
+generator state instead of its mask (Sec. 2.2.2).  By the same rule, the layers of a
+transformer around its Linears: layer norm, the gated linear unit, and a linear head with
+its cross entropy.
 
 The compute lives in libmemsave.so (hand-written HIP kernels, C ABI in
 include/memsave.h); this package is its Python binding.  Build the library

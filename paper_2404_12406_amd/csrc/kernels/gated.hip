@@ -2,11 +2,17 @@
 //   dz_g = dy z_u act'(z_g),  dz_u = dy act(z_g),
 // after which the gradients are those of a Linear with the output gradient dz.
 //
-// bf16 runs on the fused contractions of gemm_fused.hip: the forward never
+// bf16 runs on the fused contractions of gemm_gate.hip: the forward never
 // writes z unless it is to be kept, and a backward without it takes z again and
 // leaves dz in one pass.  fp32 runs the Linear contraction and the elementwise
 // kernels below; so does a bf16 backward that kept z.  Those are bound by
 // memory: 16 bytes a thread and access, a row's last vector element by element.
+//
+// Measured, us: 8192 x 768 x 2 x 2048 bf16, trained: forward 78, dz from the kept
+// projections 34 (184 MB, 5.4 TB/s), dx 63 with W's transpose, dW 84 with the sum of
+// its partials.  4096 x 2048 x 2 x 5504, from the input alone: forward 203, dz 214,
+// dx 217 with W's transpose (20) and the partials' sum (14).  1001 x 515 x 2 x 1366
+// fp32, trained: z 36, dx 43, dW 44, everything else 40 of launches of 5.
 #include <algorithm>
 
 #include "block_math.h"

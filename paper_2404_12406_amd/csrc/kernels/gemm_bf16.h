@@ -1,4 +1,4 @@
-// Shared by the bf16 GEMM kernels (gemm_bf16.hip, gemm_fused.hip): arguments,
+// Shared by the bf16 GEMM kernels (gemm_bf16.hip, gemm_fused.h): arguments,
 // LDS layouts, fragment reads, the tile configuration that gemm_block_body.inc
 // is written for, and the host's estimate of a tile's run time.
 #pragma once

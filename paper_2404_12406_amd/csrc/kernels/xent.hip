@@ -23,6 +23,11 @@
 //    p_t is no difference of rounded numbers.
 // Exponentials are of differences from a maximum or an lse, which no logit of
 // any size overflows; a row's lse is kept in fp32.
+//
+// Measured, us.  8192 x 768 x 50000 bf16, a third of the rows ignored, head trained:
+// statistics 443, dz 542, dx 412, dW 433, everything else 80.  4096 x 4096 x 128000,
+// head frozen: exponentials 3645, dx 3428, the rest 120.  777 x 514 x 10007 fp32,
+// trained: z 79 (twice), dx 88, dW 83, the softmax's passes 23, W's padded copies 17.
 #include <algorithm>
 
 #include "block_math.h"
