@@ -52,7 +52,7 @@ typedef float floatx2 __attribute__((ext_vector_type(2)));
 struct SplitRule {
     int bm, ntn, steps, slots, most;   // tile rows, column tiles, steps, blocks at once, splits at most
     float step_us, row_us;             // a step of one round; a row of partials
-    __device__ __forceinline__ int splits(int rows) const {
+    __host__ __device__ __forceinline__ int splits(int rows) const {
         const int tiles = (rows + bm - 1) / bm * ntn;
         int best = 1;
         float us = INFINITY;

@@ -25,6 +25,9 @@ int gate_fwd(int64_t M, int64_t D, int64_t F, int act, const void *x, const void
              hipStream_t st);
 int gate_grad(int64_t M, int64_t D, int64_t F, int act, const void *x, const void *w, const void *bias, const void *dy, void *dz,
               hipStream_t st);
+int place_splits(int64_t M, int64_t D, int64_t K);
+size_t place_dx_workspace(int64_t M, int64_t D, int64_t K);
+int place_dx(int64_t M, int64_t D, int64_t K, const void *dz, const void *w, void *dx, void *ws, hipStream_t st);
 }  // namespace g2
 
 namespace tok {
@@ -332,6 +335,7 @@ namespace {
 // Workspace of a backward: dz, the copies, padded gradients, the contractions'.
 struct Bwd {
     Pads p;
+    bool place;   // dx from W in place
     size_t dz, pad, gx, gw, gb, work, bytes;
 };
 
@@ -348,7 +352,9 @@ Bwd bwd_plan(int dtype, int64_t M, int64_t D, int64_t F, const void *x, const vo
     k.gw = k.gx + (f32 && dx && Dp != D ? al256((size_t)M * Dp * e) : 0);
     k.gb = k.gw + (f32 && dw && k.p.any ? al256((size_t)2 * Fp * Dp * e) : 0);
     k.work = k.gb + (f32 && db && Fp != F ? al256((size_t)2 * Fp * e) : 0);
-    size_t ws = linear_bwd_workspace(dtype, M, Dp, 2 * Fp, dx, dw, db);
+    k.place = !f32 && dx && (reinterpret_cast<uintptr_t>(w) & 15u) == 0 && g2::place_splits(M, D, 2 * F) > 0;
+    size_t ws = linear_bwd_workspace(dtype, M, Dp, 2 * Fp, dx && !k.place, dw, db);
+    if (k.place) ws = std::max(ws, g2::place_dx_workspace(M, D, 2 * F));
     if (f32 && !kept && M) ws = std::max(ws, conv_fwd_workspace(dtype, linear(M, Dp, 2 * Fp)));
     k.bytes = k.work + ws;
     return k;
@@ -385,7 +391,9 @@ int launch_gated_bwd(int dtype, int64_t M, int64_t D, int64_t F, int act, const 
             if (!g2::rows_ok(M, 2 * F, k.p.D, xp, wp)) return (int)hipErrorInvalidValue;
             err = g2::gate_grad(M, k.p.D, F, act, xp, wp, bp, dy, dz, st);
         }
-        return err ? err : launch_linear_bwd(dtype, M, D, 2 * F, 2 * F, nullptr, dz, x, w, dx, dw, db, c + k.work, stream);
+        if (!err && k.place) err = g2::place_dx(M, D, 2 * F, dz, w, dx, c + k.work, st);
+        if (err || (k.place && !dw && !db)) return err;
+        return launch_linear_bwd(dtype, M, D, 2 * F, 2 * F, nullptr, dz, x, w, k.place ? nullptr : dx, dw, db, c + k.work, stream);
     }
     const int64_t Dp = k.p.D, Fp = k.p.F;
     if (M && !proj) err = launch_conv_fwd(dtype, gated::linear(M, Dp, 2 * Fp), xp, wp, bp, dz, c + k.work, stream);

@@ -12,7 +12,8 @@
 //   kEpiProb      z, then exp(z - r) of the other words than the target, r a
 //                 reference of each row's part of a wave's columns, with those parts'
 //                 sums of exponentials and the target's logit
-//   kEpiAdd       dx += dz W for one piece of the vocabulary, in fp32
+//   kEpiAdd       dx += dz W for one piece of the vocabulary, in fp32 (the gated unit's
+//                 dx too, in one piece)
 //   kEpiStore     the weight gradient dz^T x over the rows that count, times a factor
 // The main loop is gemm_block_body.inc's.  Everything before the one rounding
 // of what is stored is in fp32.
@@ -56,7 +57,8 @@ struct FusedArgs : Args {
     const float *lse, *scale;   // kEpiXent: of each row
     const float *out_scale;     // kEpiStore: the sums' factor
     int add;               // kEpiAdd: add to the partials (0: write them)
-    const int *nsplit;     // kEpiAdd: their number, on the device
+    const int *nsplit;     // kEpiAdd: their number, on the device,
+    int fixed_splits;      // or (null) here
 };
 
 // Output column of row `row` of a gated tile's B operand, from the tile's first.

@@ -4,6 +4,8 @@
 namespace ms {
 namespace g2 {
 
+int sum_wgrad_partials(const float *part, int splits, int M, int C8, int C, void *out, const float *dbpart, void *db, hipStream_t st);
+
 namespace {
 // Tiles of the gradients of the cross entropy (an operand along m or n).
 constexpr Tile kGradTiles[] = {
@@ -115,10 +117,9 @@ SplitRule xent_dx_rule(int64_t M, int64_t D, int64_t V) {
     return r;
 }
 
-int xent_dx(int64_t M, int64_t D, int64_t V, int64_t ldz, int64_t piece, const void *dz, const void *w, const int *count,
-            const int *nsplit, float *part, bool add, hipStream_t st) {
-    const int tile = dx_tile(M, D, piece);   // (a last, smaller piece runs as the others)
-    const Tile &t = kGradTiles[tile];
+namespace {
+// part[M][D] (+)= dz[M][ldz] w[V][D], its split arrays one after another
+FusedArgs dx_args(const Tile &t, int64_t M, int64_t D, int64_t V, int64_t ldz, const void *dz, const void *w, float *part) {
     FusedArgs a{};
     a.a = (const bf16 *)dz;
     a.b = (const bf16 *)w;
@@ -131,16 +132,43 @@ int xent_dx(int64_t M, int64_t D, int64_t V, int64_t ldz, int64_t piece, const v
     a.k_split = (int)ldz;
     a.a_bytes = bytes_of(M * ldz);
     a.b_bytes = bytes_of(V * D);
-    a.count = count;
-    a.nsplit = nsplit;
     a.part = part;
     a.part_stride = M * D;
+    return a;
+}
+}  // namespace
+
+int xent_dx(int64_t M, int64_t D, int64_t V, int64_t ldz, int64_t piece, const void *dz, const void *w, const int *count,
+            const int *nsplit, float *part, bool add, hipStream_t st) {
+    const int tile = dx_tile(M, D, piece);   // (a last, smaller piece runs as the others)
+    FusedArgs a = dx_args(kGradTiles[tile], M, D, V, ldz, dz, w, part);
+    a.count = count;
+    a.nsplit = nsplit;
     a.add = add;
     return go_grad<kEpiAdd, kDgradN>(tile, kProfDgrad, a, st, xent_dx_rule(M, D, piece).most);
 }
 
+// A Linear's dx[M][D] = dz[M][K] w[K][D] so, bf16: in how many splits, 0 where it is not
+// to be.  It costs partials of M x D, where the general contraction transposes w, K x D:
+// for K of at least 2 M.  us of a gated unit, forward and input gradient, general / so:
+//   4096 x 2048 x 11008  540 / 513    512 x 2048 x 11008  119 / 104    100 x 4096 x 21888  201 / 107
+//   4096 x 512 x 16384   282 / 268    1024 x 1024 x 2048   50 / 45     300 x 256 x 1024     28 / 26
+// and past that
+//   8192 x 768 x 4096    173 / 188    8192 x 4096 x 2048  336 / 403
+int place_splits(int64_t M, int64_t D, int64_t K) {
+    if (M < 1 || K < 2 * M || D % 8 || K % 8 || !operand_fits(M * K) || !operand_fits(K * D)) return 0;
+    return xent_dx_rule(M, D, K).splits((int)M);
+}
+size_t place_dx_workspace(int64_t M, int64_t D, int64_t K) { return (size_t)place_splits(M, D, K) * M * D * sizeof(float); }
+int place_dx(int64_t M, int64_t D, int64_t K, const void *dz, const void *w, void *dx, void *ws, hipStream_t st) {
+    const int tile = dx_tile(M, D, K), s = place_splits(M, D, K);
+    FusedArgs a = dx_args(kGradTiles[tile], M, D, K, K, dz, w, static_cast<float *>(ws));
+    a.fixed_splits = s;
+    const int err = go_grad<kEpiAdd, kDgradN>(tile, kProfDgrad, a, st, s);
+    return err ? err : sum_wgrad_partials(a.part, s, (int)M, (int)D, (int)D, dx, nullptr, nullptr, st);
+}
+
 // dw[V][Dr] = *scale dz^T x over the rows that count (x has D >= Dr columns).
-int sum_wgrad_partials(const float *part, int splits, int M, int C8, int C, void *out, const float *dbpart, void *db, hipStream_t st);
 
 namespace {
 FusedPlan dw_plan(int64_t M, int64_t D, int64_t Dr, int64_t V) {
