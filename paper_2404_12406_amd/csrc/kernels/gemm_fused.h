@@ -15,6 +15,7 @@
 //   kEpiAdd       dx += dz W for one piece of the vocabulary, in fp32 (the gated unit's
 //                 dx too, in one piece)
 //   kEpiStore     the weight gradient dz^T x over the rows that count, times a factor
+//   kEpiRows      the same into rows of another width, whole vectors or not
 // The main loop is gemm_block_body.inc's.  Everything before the one rounding
 // of what is stored is in fp32.
 //
@@ -38,7 +39,7 @@
 namespace ms {
 namespace g2 {
 
-enum Epi { kEpiStore = 0, kEpiGate = 1, kEpiGateGrad = 2, kEpiLse = 3, kEpiXent = 4, kEpiAdd = 5, kEpiProb = 6 };
+enum Epi { kEpiStore = 0, kEpiGate = 1, kEpiGateGrad = 2, kEpiLse = 3, kEpiXent = 4, kEpiAdd = 5, kEpiProb = 6, kEpiRows = 7 };
 
 struct FusedArgs : Args {
     const int *count;      // rows that count (weight gradient: of the reduction), on the device; null: all
@@ -55,7 +56,7 @@ struct FusedArgs : Args {
     float *tlogit;         // with them: the target's logit; kEpiXent: what rounding took from the target's dz
     int64_t stat_ld;
     const float *lse, *scale;   // kEpiXent: of each row
-    const float *out_scale;     // kEpiStore: the sums' factor
+    const float *out_scale;     // kEpiStore, kEpiRows: the sums' factor
     int add;               // kEpiAdd: add to the partials (0: write them)
     const int *nsplit;     // kEpiAdd: their number, on the device,
     int fixed_splits;      // or (null) here
@@ -453,6 +454,25 @@ __device__ __forceinline__ void fused_epilogue(const FusedArgs &P, char *smem, f
                     if (fr < 16 && n < N) row[n] = s[0];
                 }
             }
+        }
+    } else if constexpr (EPI == kEpiRows) {
+        constexpr int PITCH = G::EPI_PITCH;
+        const int ncol = min(P.ldc - (n0 + wn0), G::WN);
+#pragma unroll
+        for (int i = 0; i < TM; ++i) {
+            const int mb = m0 + wm0 + 32 * i;
+#pragma unroll
+            for (int j = 0; j < TN; ++j)
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    bf16x4 o;
+#pragma unroll
+                    for (int v = 0; v < 4; ++v) o[v] = (bf16)acc[i][j][4 * q + v];
+                    *reinterpret_cast<bf16x4 *>(stage + fr * PITCH + 32 * j + 8 * q + 4 * fh) = o;
+                }
+            stage_order();
+            store_rows<G::WN>(stage, PITCH, P.c + (int64_t)mb * P.ldc + n0 + wn0, P.ldc, M - mb, ncol, lane);
+            stage_order();
         }
     } else {
         static_assert(EPI == kEpiAdd, "epilogue");

@@ -171,21 +171,19 @@ int place_dx(int64_t M, int64_t D, int64_t K, const void *dz, const void *w, voi
 // dw[V][Dr] = *scale dz^T x over the rows that count (x has D >= Dr columns).
 
 namespace {
-FusedPlan dw_plan(int64_t M, int64_t D, int64_t Dr, int64_t V) {
-    FusedPlan p = plan(kGradTiles, 3, V, D, M, (int)std::clamp<int64_t>(M / (4 * BK), 1, 16));
-    if (D != Dr) p.splits = std::max(p.splits, 2);   // the sum of the partials leaves the padding out
-    return p;
+FusedPlan dw_plan(int64_t M, int64_t D, int64_t V) {
+    return plan(kGradTiles, 3, V, D, M, (int)std::clamp<int64_t>(M / (4 * BK), 1, 16));
 }
 }  // namespace
 
-size_t xent_dw_workspace(int64_t M, int64_t D, int64_t Dr, int64_t V) {
-    const FusedPlan p = dw_plan(M, D, Dr, V);
+size_t xent_dw_workspace(int64_t M, int64_t D, int64_t V) {
+    const FusedPlan p = dw_plan(M, D, V);
     return p.splits > 1 ? (size_t)p.splits * V * D * sizeof(float) : 0;
 }
 
 int xent_dw(int64_t M, int64_t D, int64_t Dr, int64_t V, int64_t ldz, const void *dz, const void *x, const int *count,
             const float *scale, void *dw, void *ws, hipStream_t st) {
-    const FusedPlan p = dw_plan(M, D, Dr, V);
+    const FusedPlan p = dw_plan(M, D, V);
     const Tile &t = kGradTiles[p.tile];
     FusedArgs a{};
     a.a = (const bf16 *)dz;
@@ -206,8 +204,11 @@ int xent_dw(int64_t M, int64_t D, int64_t Dr, int64_t V, int64_t ldz, const void
         a.part_stride = V * D;
     } else {
         a.c = (bf16 *)dw;
+        a.ldc = (int)Dr;
     }
-    const int err = go_grad<kEpiStore, kWgrad>(p.tile, kProfWgrad, a, st);
+    // (the sum of the partials leaves the padding out by itself)
+    const int err = p.splits == 1 && D != Dr ? go_grad<kEpiRows, kWgrad>(p.tile, kProfWgrad, a, st)
+                                             : go_grad<kEpiStore, kWgrad>(p.tile, kProfWgrad, a, st);
     if (err || p.splits == 1) return err;
     return sum_wgrad_partials(a.part, p.splits, (int)V, (int)D, (int)Dr, dw, nullptr, nullptr, st);
 }

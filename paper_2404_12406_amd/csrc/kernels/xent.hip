@@ -48,7 +48,7 @@ int xent_prob(int64_t M, int64_t D, int64_t V, const void *x, const void *w, con
 SplitRule xent_dx_rule(int64_t M, int64_t D, int64_t V);
 int xent_dx(int64_t M, int64_t D, int64_t V, int64_t ldz, int64_t piece, const void *dz, const void *w, const int *count,
             const int *nsplit, float *part, bool add, hipStream_t st);
-size_t xent_dw_workspace(int64_t M, int64_t D, int64_t Dr, int64_t V);
+size_t xent_dw_workspace(int64_t M, int64_t D, int64_t V);
 int xent_dw(int64_t M, int64_t D, int64_t Dr, int64_t V, int64_t ldz, const void *dz, const void *x, const int *count,
             const float *scale, void *dw, void *ws, hipStream_t st);
 }  // namespace g2
@@ -664,7 +664,7 @@ Bwd carve_bwd(Carve &c, int dtype, int64_t M, int64_t D, int64_t V, bool padw, b
     size_t ws = 0;
     for (int64_t v : {p, last}) {
         if (dtype == kBF16) {
-            if (dw) ws = std::max(ws, g2::xent_dw_workspace(M, b.r.D8, D, v));
+            if (dw) ws = std::max(ws, g2::xent_dw_workspace(M, b.r.D8, v));
         } else {
             ws = std::max(ws, conv_fwd_workspace(dtype, linear(M, b.r.D8, f32_words(M, b.r.D8, v))));
             ws = std::max(ws, linear_bwd_workspace(dtype, M, b.r.D8, f32_words(M, b.r.D8, v), dx, dw, db));
