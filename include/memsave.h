@@ -373,8 +373,10 @@ uint64_t ms_cross_entropy_kept_bytes(int64_t rows, int64_t D, int64_t V, int32_t
  * contiguous.  With mask != 0, kept is caller-allocated device memory of
  * ms_cross_entropy_kept_bytes(), 16-byte aligned, fully overwritten, and borrowed (a
  * log-sum-exp with x, W, b and target, which every gradient then needs); with mask 0
- * it may be NULL.  dz is rounded to x's dtype before its
- * products, everything else is in fp32.  Backward is ms_layer_backward() with
+ * it may be NULL.  dz is rounded to x's dtype before its products, everything else is
+ * in fp32 (a log-sum-exp too: where every logit of a row is past some 10^6 in size, it
+ * no longer resolves what they differ by, and gradients taken from it suffer; the loss
+ * and a gradient taken in the forward do not).  Backward is ms_layer_backward() with
  * grad_y of the loss's shape, fp32.  ms_layer_forward() rejects MS_CROSS_ENTROPY
  * (MS_E_ARG).
  */

@@ -24,7 +24,7 @@
 // and end, with the softmax's statistics 7.7, with dz of the cross entropy 12.  At k =
 // 768, 12 such steps, that is the difference between 914 (kEpiLse) or 780 TFLOP/s
 // (kEpiXent) and the 1276 that a large product reaches; at k = 4096 kEpiProb has 1178,
-// kEpiGate (k = 2048) 912.  128 x 128 tiles, two a CU, would run one's end under the
+// kEpiGate (k = 2048) 1093.  128 x 128 tiles, two a CU, would run one's end under the
 // other's steps, but their steps are a fifth slower: est_us() has both.
 #pragma once
 
