@@ -121,6 +121,24 @@ def test_masks(mask, bias, dtype):
     compare(run(*cuda(*t), "sum", mask), t, "sum", mask, dtype)
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("shape", [(40, 64, 1025), (300, 96, 513), (300, 515, 130), (70, 515, 2049), (1030, 203, 777)])
+def test_gradients_stay_in_their_rows(shape, dtype):
+    """Words that are no multiple of 4 and widths that are none of 8: W's gradient is
+    written in place, and nothing past it."""
+    M, D, V = shape
+    t = inputs(*shape, dtype, ignored=0.2, seed=241)
+    x, W, b, tgt, gl = cuda(*t)
+    _, rec = ms.layer_forward(ms.LinearCrossEntropy(tgt), x, W, b, 7)
+    outs = [guarded_empty(s, dtype) for s in ((M, D), (V, D), (V,))]
+    ms.layer_backward(rec, gl, *(o[0] for o in outs))
+    torch.cuda.synchronize()
+    refs = ref(*(v.double().numpy() for v in t[:3]), t[3].numpy(), t[4].double().numpy(), "mean")[1:]
+    for o, r, name in zip(outs, refs, ("dx", "dW", "db")):
+        check(name, host(o[0]), r, dtype, BAR[dtype])
+        assert guards_intact(o[1], o[2])
+
+
 @pytest.mark.parametrize("mask", [4, 7])
 @pytest.mark.parametrize("shape", [(300, 64, 130), (1030, 264, 2050), (2000, 64, 10007)])
 def test_bias_gradient_rounds_once(shape, mask):
