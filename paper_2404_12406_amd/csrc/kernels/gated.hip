@@ -317,7 +317,11 @@ int launch_gated_fwd(int dtype, int64_t M, int64_t D, int64_t F, int act, const 
     int err = gated::make_pads(p, dtype, M, D, F, c, &x, &w, &b, stream);
     if (err) return err;
     // (p.F is F wherever the few rows' kernel applies)
-    if (tok::applies(dtype, M, 2 * F, p.D, x, w)) return tok::gate(dtype, M, p.D, F, act, x, w, b, y, proj, st);
+    // (not where fp32 has few outputs for its inputs: the large contraction splits k.  16 x
+    // 4096 x 2 x 256 25 and 33 us from the caches and not, there 16 and 17; 16 x 2048 x 2 x
+    // 1024 15 and 22, there 16 and 19; 16 x 1024 x 2 x 4096 10 and 21, there 18 and 25)
+    const bool split = dtype != kBF16 && D % 4 == 0 && D > 4 * F;
+    if (!split && tok::applies(dtype, M, 2 * F, p.D, x, w)) return tok::gate(dtype, M, p.D, F, act, x, w, b, y, proj, st);
     if (dtype == kBF16) {
         if (!g2::rows_ok(M, 2 * F, p.D, x, w)) return (int)hipErrorInvalidValue;
         return g2::gate_fwd(M, p.D, F, act, x, w, b, y, proj, st);

@@ -12,10 +12,11 @@
 //    their columns of the result are dropped.
 // The gated unit pairs a tile of gate rows with one of up rows, so that a lane has
 // both projections; the softmax keeps running statistics of its words per lane.
-// Measured, us a call, here and with the large contraction: one token, 4096 x 2 x
-// 10944 bf16 39 and 43 (the kernel 33, 5.4 TB/s); four rows, 50000 words of 768, 27
-// and 31 (22 and 4.5).  16 rows are what the matrix instruction takes: one more
-// would read W twice.
+// Measured, us a call, here and with the large contraction, W not in the caches: one
+// token, bf16, 4096 x 2 x 10944 73 and 79 (from the last-level cache 33 and 30), 2048
+// x 2 x 1024 14 and 21, 1024 x 2 x 4096 12 and 15.  16 rows are what the matrix
+// instruction takes: one more would read W twice.  (Which sizes of the cross entropy
+// and of fp32 come here: few_rows() in xent.hip, launch_gated_fwd().)
 #include <algorithm>
 
 #include "block_math.h"

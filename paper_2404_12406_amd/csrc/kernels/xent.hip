@@ -731,6 +731,17 @@ int take_piece(Piece *q, int64_t M, int64_t D, int64_t D8, int64_t v0, int64_t n
     return launch_copy_rows(kF32, j, jobs, st);
 }
 
+// Whether the kernels for few rows take the forward.  bf16: not W of more than 64 MiB,
+// which the large contraction's tiles read faster than its two more launches cost.  us,
+// few rows' / large (W in the last-level cache where it fits, and not):
+//   16 x 2048 x 2000   13 / 31, 19 / 44     4 x 768 x 50000   28 / 26, 47 / 47
+//   16 x 1024 x 10000  15 / 22, 22 / 33    16 x 768 x 50000   32 / 26, 51 / 47
+//                                           1 x 4096 x 100000 221 / 171, 250 / 232
+// fp32: 16 x 768 x 50000 50 / 90, 85 / 112; 16 x 2048 x 2000 19 / 27, 26 / 32.
+bool few_rows(int dtype, int64_t M, int64_t D, int64_t V, const void *x, const void *w) {
+    return (dtype != kBF16 || V * D * 2 <= int64_t(64) << 20) && tok::applies(dtype, M, V, D, x, w);
+}
+
 int logits(const Piece &q, const Rows &r, int64_t M, float *z, void *ws, hipStream_t st) {
     ConvGeom g = linear(M, r.D8, q.np);
     g.count = r.count;
@@ -766,7 +777,7 @@ int launch_xent_fwd(int dtype, int64_t M, int64_t D, int64_t V, const void *x, c
                     const int64_t *target, int64_t ignore, int reduction, float *loss, float *lse, void *kept, void *ws, void *stream) {
     using namespace xent;
     hipStream_t st = (hipStream_t)stream;
-    if (!kept && tok::applies(dtype, M, V, D, x, w)) return tok::xent(dtype, M, D, V, x, w, b, target, ignore, reduction, loss, lse, ws, st);
+    if (!kept && few_rows(dtype, M, D, V, x, w)) return tok::xent(dtype, M, D, V, x, w, b, target, ignore, reduction, loss, lse, ws, st);
     Carve c{static_cast<char *>(ws)};
     const Fwd f = carve_fwd(c, dtype, M, D, V, padw, padb, reduction != 2, kept != nullptr);
     const int64_t D8 = f.r.D8;
