@@ -38,6 +38,13 @@ int32_t ms_testing_gemm_plan(int32_t pass, const int32_t geom[13], int32_t out[1
  * Returns 0, or -1 for operands past 32-bit byte offsets. */
 int32_t ms_testing_float_plan(int32_t pass, const int32_t geom[13], int64_t out[5]);
 
+/* What a gated linear unit's backward of these sizes lays out: out[4] = {bytes of
+ * workspace the runtime asks for, bytes that the launch uses, D and F as its
+ * contractions see them}.  proj: the projections are kept (they never are for no
+ * rows).  aligned: x and W begin on 16 bytes. */
+void ms_testing_gated_plan(int32_t dtype, int64_t rows, int64_t D, int64_t F, int32_t proj, int32_t aligned, uint32_t mask,
+                           int64_t out[4]);
+
 #ifdef __cplusplus
 }
 #endif

@@ -16,6 +16,8 @@
 #include <algorithm>
 
 #include "block_math.h"
+#include "../../../include/memsave.h"
+#include "../../../include/memsave_testing.h"
 
 namespace ms {
 
@@ -364,6 +366,12 @@ Bwd bwd_plan(int dtype, int64_t M, int64_t D, int64_t F, const void *x, const vo
     return k;
 }
 
+// As launch_gated_bwd() lays it out: no rows need no z, as if it were kept.
+Bwd launch_plan(int dtype, int64_t M, int64_t D, int64_t F, const void *x, const void *w, const void *b, const void *proj, bool dx, bool dw,
+                bool db) {
+    return bwd_plan(dtype, M, D, F, x, w, b, proj || M == 0, dx, dw, db);
+}
+
 }  // namespace
 }  // namespace gated
 
@@ -375,7 +383,7 @@ size_t gated_bwd_workspace(int dtype, int64_t M, int64_t D, int64_t F, const voi
 int launch_gated_bwd(int dtype, int64_t M, int64_t D, int64_t F, int act, const void *x, const void *w, const void *b, const void *proj,
                      const void *dy, void *dx, void *dw, void *db, void *ws, void *stream) {
     hipStream_t st = (hipStream_t)stream;
-    const gated::Bwd k = gated::bwd_plan(dtype, M, D, F, x, w, b, proj != nullptr, dx, dw, db);
+    const gated::Bwd k = gated::launch_plan(dtype, M, D, F, x, w, b, proj, dx, dw, db);
     char *c = static_cast<char *>(ws);
     void *dz = c + k.dz;
     const void *xp = x, *wp = w, *bp = b;
@@ -417,3 +425,15 @@ int launch_gated_bwd(int dtype, int64_t M, int64_t D, int64_t F, int act, const 
 }
 
 }  // namespace ms
+
+extern "C" void ms_testing_gated_plan(int32_t dtype, int64_t rows, int64_t D, int64_t F, int32_t proj, int32_t aligned, uint32_t mask,
+                                      int64_t out[4]) {
+    const void *p = aligned ? nullptr : reinterpret_cast<const void *>(uintptr_t(2));   // (nothing is read)
+    const void *z = proj && rows ? out : nullptr;
+    const bool dx = mask & MS_RG_INPUT, dw = mask & MS_RG_WEIGHT, db = mask & MS_RG_BIAS;
+    const ms::gated::Bwd k = ms::gated::launch_plan(dtype, rows, D, F, p, p, nullptr, z, dx, dw, db);
+    out[0] = (int64_t)ms::gated_bwd_workspace(dtype, rows, D, F, p, p, nullptr, proj || !rows, dx, dw, db);
+    out[1] = (int64_t)k.bytes;
+    out[2] = k.p.D;
+    out[3] = k.p.F;
+}
