@@ -45,6 +45,11 @@ int32_t ms_testing_float_plan(int32_t pass, const int32_t geom[13], int64_t out[
 void ms_testing_gated_plan(int32_t dtype, int64_t rows, int64_t D, int64_t F, int32_t proj, int32_t aligned, uint32_t mask,
                            int64_t out[4]);
 
+/* What a cross entropy of these sizes lays out: out[4] = {words of a piece, elements
+ * of the largest piece's dz, columns of the gathered rows, and (fp32) columns of the
+ * last piece's logits}. */
+void ms_testing_cross_entropy_plan(int32_t dtype, int64_t rows, int64_t D, int64_t V, int64_t out[4]);
+
 #ifdef __cplusplus
 }
 #endif

@@ -29,6 +29,7 @@ EXPORTS = (
     "ms_profile_start", "ms_profile_read", "ms_relu_mask_bytes", "ms_relu_forward",
     "ms_dropout_blocks", "ms_dropout_forward", "ms_layer_backward_noalloc", "ms_noalloc_scratch_bytes",
     "ms_testing_gemm_plan", "ms_testing_float_plan", "ms_testing_gated_plan",
+    "ms_testing_cross_entropy_plan",
     "ms_layer_norm_forward", "ms_gated_linear_forward", "ms_gated_projection_bytes", "ms_cross_entropy_forward",
     "ms_cross_entropy_kept_bytes",
 )
@@ -135,6 +136,9 @@ def configure(lib: ctypes.CDLL) -> ctypes.CDLL:
         lib.ms_testing_gated_plan.argtypes = [ctypes.c_int32, ctypes.c_int64, ctypes.c_int64, ctypes.c_int64, ctypes.c_int32,
                                               ctypes.c_int32, ctypes.c_uint32, ctypes.POINTER(ctypes.c_int64)]
         lib.ms_testing_gated_plan.restype = None
+        lib.ms_testing_cross_entropy_plan.argtypes = [ctypes.c_int32, ctypes.c_int64, ctypes.c_int64, ctypes.c_int64,
+                                                      ctypes.POINTER(ctypes.c_int64)]
+        lib.ms_testing_cross_entropy_plan.restype = None
     return lib
 
 

@@ -358,6 +358,7 @@ ms_status ms_cross_entropy_forward(const ms_tensor *x, const ms_tensor *W, const
     // rows padded to whole 16-byte vectors have 32-bit offsets too
     if (capped_product({std::max(M, V), (D + 7) / 8 * 8}) > kMaxElems - 16)
         return fail(MS_E_UNSUPPORTED, "operands have more than 2^31-17 elements");
+    if (M > ms::kMaxHeadRows) return fail(MS_E_UNSUPPORTED, "x has more than 2^27-8 rows");
     if ((st = check_vector(b, "b", V, x->dtype))) return st;
     if (reduction < MS_REDUCE_MEAN || reduction > MS_REDUCE_NONE) return fail(MS_E_ARG, "unknown reduction %d", reduction);
     if (M > 0 && !target) return fail(MS_E_NULL, "target is NULL");

@@ -193,6 +193,7 @@ int launch_linear_bwd(int dtype, int64_t M, int64_t K, int64_t N, int64_t wrows,
 // the loss, fp32.  Where xent_keeps_gradient(), the forward takes `kept` of
 // xent_kept_bytes(), dx but for the loss's gradient (and no lse), and the backward is
 // launch_xent_scale().
+constexpr int64_t kMaxHeadRows = (int64_t(1) << 27) - 8;   // at most so many rows
 bool xent_keeps_gradient(int dtype, int64_t M, int64_t D, int64_t V, bool dx, bool dw, bool db);
 size_t xent_kept_bytes(int dtype, int64_t M, int64_t D);
 size_t xent_fwd_workspace(int dtype, int64_t M, int64_t D, int64_t V, bool padw, bool padb, int reduction, bool keep);

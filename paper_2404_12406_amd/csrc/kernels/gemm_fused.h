@@ -403,7 +403,8 @@ __device__ __forceinline__ void fused_epilogue(const FusedArgs &P, char *smem, f
                 const int mb = m0 + wm0 + 32 * i, m = mb + fr;
                 const bool in = m < M;
                 const float l = in ? lse[i] : 0.f, sc = in ? scale[i] : 0.f;
-                const int t = in ? tgt[i] - P.v0 - (n0 + wn0) : -1;
+                int t = in ? tgt[i] - P.v0 - (n0 + wn0) : -1;
+                if (t >= N - (n0 + wn0)) t = -1;   // (a later piece's: this one may end within a tile)
                 const bool any = __any((unsigned)t < (unsigned)G::WN);
                 float rest = 0.f;
 #pragma unroll

@@ -31,6 +31,8 @@
 #include <algorithm>
 
 #include "block_math.h"
+#include "limits.h"
+#include "../../../include/memsave_testing.h"
 
 namespace ms {
 
@@ -509,10 +511,15 @@ constexpr int64_t kPieceBytes = int64_t(1) << 30;
 
 size_t al256(size_t n) { return (n + 255) / 256 * 256; }
 
+// The contractions' byte offsets have 32 bits: with rows by the million a piece is
+// fewer than the 256 words of a tile, in eights (there are some: kMaxHeadRows).
 int64_t piece(int dtype, int64_t M, int64_t V) {
-    const int64_t bytes = std::max<int64_t>(M, 1) * V * (dtype == kBF16 ? 2 : 4);
+    M = std::max<int64_t>(M, 1);
+    const int64_t bytes = M * V * (dtype == kBF16 ? 2 : 4);
     const int64_t n = (bytes + kPieceBytes - 1) / kPieceBytes;
-    return std::min(V, ((V + n - 1) / n + 255) / 256 * 256);
+    const int64_t p = std::min(V, ((V + n - 1) / n + 255) / 256 * 256);
+    const int64_t most = dtype == kBF16 ? (g2::kOOB / 2 - 8) / M / 8 * 8 : (g2::kOOB - 16) / 4 / M / 8 * 8;
+    return std::min(p, most);
 }
 
 ConvGeom linear(int64_t M, int64_t K, int64_t N) {
@@ -925,3 +932,12 @@ int launch_xent_bwd(int dtype, int64_t M, int64_t D, int64_t V, const void *x, c
 }
 
 }  // namespace ms
+
+extern "C" void ms_testing_cross_entropy_plan(int32_t dtype, int64_t rows, int64_t D, int64_t V, int64_t out[4]) {
+    using namespace ms::xent;
+    const int64_t p = piece(dtype, rows, V), last = V - (V - 1) / p * p;
+    out[0] = p;
+    out[2] = dtype == ms::kBF16 ? (D + 7) / 8 * 8 : f32_width(rows, D);
+    out[3] = f32_words(rows, out[2], last);
+    out[1] = rows * (dtype == ms::kBF16 ? (p + 7) / 8 * 8 : std::max(f32_words(rows, out[2], p), out[3]));
+}

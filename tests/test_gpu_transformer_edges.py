@@ -24,3 +24,37 @@ def test_gated_unit_of_no_rows(dtype, keep):
         torch.cuda.synchronize()
         for view, buf, guard in outs[1:]:
             assert not view.any() and guards_intact(buf, guard)
+
+
+@pytest.mark.parametrize("dtype,rows", [("bf16", 2 ** 23 + 5), ("f32", 2 ** 22 + 3)])
+def test_rows_by_the_million(dtype, rows):
+    """More dz than 32-bit offsets reach in a tile's width of words (bf16: a dense prediction
+    of some classes for every pixel): smaller pieces.  Bars: the gradients' of
+    test_gpu_linear_cross_entropy.py; the fp32 sums of dW have some 1e6 terms a split, whose
+    errors add up as their root, 2^-24 x 1e3 of the root of their squares' sum, which is dW's size."""
+    D, V = 16, 300
+    g = torch.Generator(device="cuda").manual_seed(3)
+    x = torch.randn(rows, D, device="cuda", generator=g).to(TORCH_DT[dtype])
+    W = torch.randn(V, D, device="cuda", generator=g).to(TORCH_DT[dtype])
+    t = torch.randint(0, V, (rows,), device="cuda", generator=g)
+    t[::5] = -100
+    loss, rec = ms.layer_forward(ms.LinearCrossEntropy(t, reduction="sum"), x, W, None, 3)
+    dx, dW, _ = ms.layer_backward(rec, torch.ones(1, device="cuda"))
+    Wd, want, gW, worst, size = W.double(), 0.0, 0.0, 0.0, 0.0
+    for i in range(0, rows, 2 ** 20):
+        xi, ti = x[i:i + 2 ** 20].double(), t[i:i + 2 ** 20]
+        live = ti != -100
+        z = xi @ Wd.t()
+        lse = torch.logsumexp(z, 1)
+        pick = ti.clamp(min=0)[:, None]
+        want += float(((lse - z.gather(1, pick)[:, 0]) * live).sum())
+        z = torch.exp(z - lse[:, None])
+        z.scatter_add_(1, pick, torch.full_like(z[:, :1], -1.0))
+        z *= live[:, None]
+        gx = z @ Wd
+        gW = gW + z.t() @ xi
+        worst, size = max(worst, float((dx[i:i + 2 ** 20].double() - gx).abs().max())), max(size, float(gx.abs().max()))
+    bar = {"bf16": 2.0 ** -7, "f32": 5e-5}[dtype]
+    assert abs(loss.item() - want) <= 2e-5 * abs(want)
+    assert worst <= bar * size
+    assert float((dW.double() - gW).abs().max()) <= (bar + 2.0 ** -14) * float(gW.abs().max())

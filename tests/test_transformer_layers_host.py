@@ -307,3 +307,16 @@ def test_backward_from_the_fixed_scratch(stub, kind):
     assert stub.stub_log() == b"scratch;"
     stub.ms_testing_fail_next_workspace(0)
     c.free()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_cross_entropy_rows_are_bounded(stub, dtype):
+    for rows, status in ((2 ** 27 - 8, 0), (2 ** 27 - 7, L.MS_E_UNSUPPORTED)):
+        c = Call(stub, "xent", dtype, x=tensor((rows, 8), dtype), W=tensor((V, 8), dtype))
+        assert c.forward() == status, stub.ms_last_error()
+        if not status:
+            assert c.backward() == 0
+            c.free()
+        else:
+            assert stub.blocks_log() == b""
+        stub.blocks_reset()

@@ -31,3 +31,27 @@ def test_a_gated_backward_stays_inside_its_workspace(lib, dtype, proj):
                 for mask in range(1, 8):
                     p = gated(lib, dtype, rows, D, F, proj, aligned, mask)
                     assert p["used"] <= p["asked"], (rows, D, F, aligned, mask, p)
+
+
+# The contractions' operands: bytes below 2^32 less the last 16, which stand for "past
+# the end", and less a load (bf16 by the general kernel's 32-bit indexes too).
+MOST = {BF16: 2 ** 31 - 16, F32: 2 ** 30 - 8}
+MOST_ROWS = 2 ** 27 - 8
+
+
+def xent(lib, dtype, rows, D, V):
+    o = (ctypes.c_int64 * 4)()
+    lib.ms_testing_cross_entropy_plan(dtype, rows, D, V, o)
+    return dict(zip(("words", "dz", "columns", "last"), o))
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_a_piece_of_the_logits_has_32_bit_offsets(lib, dtype):
+    for rows in (1, 8192, 2 ** 21, 2 ** 22, 2 ** 23 - 1, 2 ** 23, 10 ** 7, 16800000, 2 ** 25 + 1, 2 ** 26, MOST_ROWS):
+        for V in (1, 7, 129, 150, 255, 256, 1000, 50000, 128001):
+            p = xent(lib, dtype, rows, 8, V)
+            assert 1 <= p["words"] <= V
+            assert p["words"] == V or p["words"] % 8 == 0   # whole vectors of dz; pieces of b begin on 16 bytes
+            assert p["dz"] <= MOST[dtype], (rows, V, p)
+            if rows * V <= 2 ** 28:
+                assert p["words"] == V
