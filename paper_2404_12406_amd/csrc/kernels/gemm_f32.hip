@@ -691,7 +691,7 @@ int64_t x_elems(const ConvGeom &g) { return (int64_t)g.N * g.H * g.W * g.C; }
 int64_t y_elems(const ConvGeom &g) { return (int64_t)g.N * g.P * g.Q * g.K; }
 int64_t w_elems(const ConvGeom &g) { return (int64_t)g.K * g.R * g.S * g.C; }
 // 32-bit byte offsets of 4-byte elements; k and tap indexes below 2^31 / 2^16
-bool fits(int64_t elems) { return elems * 4 <= (int64_t)(kOOB)-16; }
+bool fits(int64_t elems) { return elems <= g2::kMostFloats; }
 bool geom_ok(const ConvGeom &g) {
     return fits(x_elems(g)) && fits(y_elems(g)) && fits(w_elems(g)) && (int64_t)g.R * g.S <= 65535;
 }

@@ -518,7 +518,7 @@ int64_t piece(int dtype, int64_t M, int64_t V) {
     const int64_t bytes = M * V * (dtype == kBF16 ? 2 : 4);
     const int64_t n = (bytes + kPieceBytes - 1) / kPieceBytes;
     const int64_t p = std::min(V, ((V + n - 1) / n + 255) / 256 * 256);
-    const int64_t most = dtype == kBF16 ? (g2::kOOB / 2 - 8) / M / 8 * 8 : (g2::kOOB - 16) / 4 / M / 8 * 8;
+    const int64_t most = dtype == kBF16 ? (g2::kOOB / 2 - 8) / M / 8 * 8 : g2::kMostFloats / M / 8 * 8;
     return std::min(p, most);
 }
 
@@ -543,8 +543,8 @@ constexpr int64_t kPadRows = 96;
 int64_t f32_width(int64_t M, int64_t D) { return M >= kPadRows && D % 4 ? (D + 31) / 32 * 32 : D; }
 int64_t f32_words(int64_t M, int64_t D8, int64_t V) {
     const int64_t n = (V + 31) / 32 * 32;
-    // (past 2^30 elements the contraction is one that does not know them)
-    return V % 4 && std::max({M * D8, n * D8, M * n}) < int64_t(1) << 30 ? n : V;
+    // (larger operands take a contraction that does not know them)
+    return V % 4 && std::max({M * D8, n * D8, M * n}) <= g2::kMostFloats ? n : V;
 }
 
 // A piece's operands as the contractions take them.

@@ -55,3 +55,15 @@ def test_a_piece_of_the_logits_has_32_bit_offsets(lib, dtype):
             assert p["dz"] <= MOST[dtype], (rows, V, p)
             if rows * V <= 2 ** 28:
                 assert p["words"] == V
+
+
+def test_widened_logits_fit_the_contractions_that_know_of_them(lib):
+    """Rows of W past the last word are known to the fp32 contraction alone, not to the
+    general one that takes larger operands (the first: x has 2^30 - 4 elements)."""
+    widened = 0
+    for rows, D, V in ((6242685, 172, 31), (6242600, 172, 31), (33554431, 32, 31), (33554430, 4, 29), (2 ** 20, 900, 1027)):
+        p = xent(lib, F32, rows, D, V)
+        if p["last"] != V - (V - 1) // p["words"] * p["words"]:
+            widened += 1
+            assert max(rows * p["columns"], p["last"] * p["columns"], rows * p["last"]) <= MOST[F32], (rows, D, V, p)
+    assert widened > 1
