@@ -16,6 +16,7 @@
 #include <algorithm>
 
 #include "block_math.h"
+#include "limits.h"
 #include "../../../include/memsave.h"
 #include "../../../include/memsave_testing.h"
 
@@ -219,9 +220,11 @@ Pads pads(int dtype, int64_t M, int64_t D, int64_t F, const void *x, const void 
         p.w = p.D != D || !al(w, 16);
         p.b = b && !al(b, 4);
     } else if (M >= kPadRows) {
-        if (D % 4 || F % 2) {
-            p.D = (D + 31) / 32 * 32;
-            p.F = (F + 15) / 16 * 16;
+        const int64_t Dp = (D + 31) / 32 * 32, Fp = (F + 15) / 16 * 16;
+        // (not past what the contractions take: the narrowest rows grow many times)
+        if ((D % 4 || F % 2) && std::max({M * Dp, M * 2 * Fp, 2 * Fp * Dp}) <= g2::kMostFloats) {
+            p.D = Dp;
+            p.F = Fp;
         }
         p.x = p.D != D || !al(x, 16);
         p.w = p.D != D || p.F != F || !al(w, 16);

@@ -540,7 +540,12 @@ ConvGeom linear(int64_t M, int64_t K, int64_t N) {
 //   40 x 511 x 39536    81 / 284 and  93 / 307    70 x 511 x 39536   102 / 381 and 109 / 372
 //   36 x 3485 x 30640  216 / 934 and 303 / 1098   71 x 3485 x 30640  344 / 1488 and 395 / 1473
 constexpr int64_t kPadRows = 96;
-int64_t f32_width(int64_t M, int64_t D) { return M >= kPadRows && D % 4 ? (D + 31) / 32 * 32 : D; }
+// (not past what the contractions take: with the narrowest rows the copies are many times
+// the tensors, and of more elements than any contraction's indexes reach)
+int64_t f32_width(int64_t M, int64_t D, int64_t V) {
+    const int64_t wide = (D + 31) / 32 * 32;
+    return M >= kPadRows && D % 4 && std::max(M, V) * wide <= g2::kMostFloats ? wide : D;
+}
 int64_t f32_words(int64_t M, int64_t D8, int64_t V) {
     const int64_t n = (V + 31) / 32 * 32;
     // (larger operands take a contraction that does not know them)
@@ -578,7 +583,7 @@ struct Rows {
 
 Rows carve_rows(Carve &c, int dtype, int64_t M, int64_t D, int64_t V, bool padw, bool padb) {
     Rows r{};
-    r.D8 = dtype == kBF16 ? (D + 7) / 8 * 8 : f32_width(M, D);
+    r.D8 = dtype == kBF16 ? (D + 7) / 8 * 8 : f32_width(M, D, V);
     r.pos = c.get<int>(M);
     r.idx = c.get<int>(M);
     r.tgt = c.get<int>(M);
@@ -937,7 +942,7 @@ extern "C" void ms_testing_cross_entropy_plan(int32_t dtype, int64_t rows, int64
     using namespace ms::xent;
     const int64_t p = piece(dtype, rows, V), last = V - (V - 1) / p * p;
     out[0] = p;
-    out[2] = dtype == ms::kBF16 ? (D + 7) / 8 * 8 : f32_width(rows, D);
+    out[2] = dtype == ms::kBF16 ? (D + 7) / 8 * 8 : f32_width(rows, D, V);
     out[3] = f32_words(rows, out[2], last);
     out[1] = rows * (dtype == ms::kBF16 ? (p + 7) / 8 * 8 : std::max(f32_words(rows, out[2], p), out[3]));
 }

@@ -57,6 +57,22 @@ def test_a_piece_of_the_logits_has_32_bit_offsets(lib, dtype):
                 assert p["words"] == V
 
 
+def test_padded_copies_have_32_bit_offsets(lib):
+    """fp32 widths are padded to whole vectors only where the copies, and what is computed
+    from them, stay below the contractions' limit (the general kernel's indexes end at 2^31)."""
+    most = MOST[F32]
+    for rows, D, V in ((2 ** 26, 3, 5), (2 ** 25 + 1, 31, 7), (2 ** 27 - 8, 1, 3), (100, 737, 2880000), (96, 5, 2 ** 27), (777, 514, 10007),
+                       (2 ** 25 - 1, 5, 9)):
+        p = xent(lib, F32, rows, D, V)
+        assert p["columns"] == D or max(rows, p["words"]) * p["columns"] <= most, (rows, D, V, p)
+        assert p["last"] == V - (V - 1) // p["words"] * p["words"] or max(p["last"] * p["columns"], rows * p["last"],
+                                                                       rows * p["columns"]) <= most
+    for rows, D, F in ((2 ** 27, 1, 1), (2 ** 26 + 1, 3, 5), (2 ** 25, 30, 15), (100, 9001, 60001), (1001, 515, 1366), (96, 2 ** 21 + 1, 500)):
+        p = gated(lib, F32, rows, D, F, 0)
+        assert (p["D"], p["F"]) == (D, F) or max(rows * p["D"], rows * 2 * p["F"], 2 * p["F"] * p["D"]) <= most, (rows, D, F, p)
+    assert xent(lib, F32, 777, 514, 10007)["columns"] == 544 and gated(lib, F32, 1001, 515, 1366, 0)["D"] == 544
+
+
 def test_widened_logits_fit_the_contractions_that_know_of_them(lib):
     """Rows of W past the last word are known to the fp32 contraction alone, not to the
     general one that takes larger operands (the first: x has 2^30 - 4 elements)."""
