@@ -331,7 +331,8 @@ uint64_t ms_gated_projection_bytes(int64_t rows, int64_t F, int32_t dtype);
  *    takes z again, a third more matrix work than with z.
  * W is borrowed for bit INPUT or where z is taken again.  With mask 0 nothing is
  * kept and proj must be NULL.  x[M, D], W[2F, D], y[M, F]: any strides (y not
- * overlapping itself), D, F >= 1, M * 2F < 2^31; b[2F] contiguous or NULL.  z is
+ * overlapping itself), D, F >= 1, M * 2F < 2^31 and, in bf16, M and 2F times D rounded up
+ * to 8 at most 2^31 - 17 (MS_E_UNSUPPORTED otherwise); b[2F] contiguous or NULL.  z is
  * in fp32 until it is rounded into proj; y is rounded once, from fp32.  bf16 operands whose
  * D is no multiple of 8 run on zero-padded copies, and every backward on a dz in
  * transient workspace.  Backward is ms_layer_backward().  ms_layer_forward()

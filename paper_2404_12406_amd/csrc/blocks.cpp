@@ -283,6 +283,9 @@ ms_status ms_gated_linear_forward(const ms_tensor *x, const ms_tensor *W, const 
     if (!strides_ok(x) || !strides_ok(W)) return fail(MS_E_LAYOUT, "x and W need non-negative strides");
     if (activation < MS_ACT_SILU || activation > MS_ACT_SIGMOID) return fail(MS_E_ARG, "unknown activation %d", activation);
     if (capped_product({M, 2 * F}) > kMaxElems) return fail(MS_E_UNSUPPORTED, "projections have more than 2^31-1 elements");
+    // rows of bf16 padded to whole 16-byte vectors have 32-bit offsets too
+    if (x->dtype == MS_BF16 && capped_product({std::max(M, 2 * F), (D + 7) / 8 * 8}) > kMaxElems - 16)
+        return fail(MS_E_UNSUPPORTED, "operands have more than 2^31-17 elements");
     if ((st = check_vector(b, "b", 2 * F, x->dtype)) || (st = check_output(y, "y", M, F, x->dtype))) return st;
     if (proj) {
         if (!mask) return fail(MS_E_ARG, "without a mask the projections are not kept: proj must be NULL");

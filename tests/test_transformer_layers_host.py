@@ -320,3 +320,14 @@ def test_cross_entropy_rows_are_bounded(stub, dtype):
         else:
             assert stub.blocks_log() == b""
         stub.blocks_reset()
+
+
+@pytest.mark.parametrize("M_,D_,F_", [(2 ** 28, 1, 1), (2 ** 28 - 1, 7, 3), (4, 3, 2 ** 27), (2 ** 25, 63, 5)])
+def test_bf16_gated_operands_past_32_bit_offsets(stub, M_, D_, F_):
+    """Rows are padded to whole 16-byte vectors: what the contraction cannot take is refused
+    before anything is launched (fp32 runs on rows as they are)."""
+    over = lambda dtype: dict(x=tensor((M_, D_), dtype), W=tensor((2 * F_, D_), dtype), b=None, y=tensor((M_, F_), dtype), mask=0, proj=None)
+    c = Call(stub, "gated", "bf16", **over("bf16"))
+    assert c.forward() == L.MS_E_UNSUPPORTED, stub.ms_last_error()
+    assert stub.blocks_log() == b"" and stub.stub_log() == b""
+    assert Call(stub, "gated", "f32", **over("f32")).forward() == 0
