@@ -371,7 +371,8 @@ uint64_t ms_cross_entropy_kept_bytes(int64_t rows, int64_t D, int64_t V, int32_t
  * reaches.  reduction: MS_REDUCE_MEAN over the rows that count (NaN where none
  * does, and no gradient), MS_REDUCE_SUM (loss[1]) or MS_REDUCE_NONE (loss[M]).
  * x[M, D], W[V, D]: any strides, D, V >= 1, M <= 2^27 - 8 and M and V times D rounded
- * up to 8 at most 2^31 - 17 (MS_E_UNSUPPORTED otherwise); b[V] contiguous or NULL.  loss: fp32,
+ * up to 8 at most 2^31 - 17, in bf16 fewer than 2^24 tiles of 128 x 128 logits
+ * (MS_E_UNSUPPORTED otherwise); b[V] contiguous or NULL.  loss: fp32,
  * contiguous.  With mask != 0, kept is caller-allocated device memory of
  * ms_cross_entropy_kept_bytes(), 16-byte aligned, fully overwritten, and borrowed (a
  * log-sum-exp with x, W, b and target, which every gradient then needs); with mask 0

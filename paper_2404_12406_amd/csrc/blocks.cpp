@@ -362,6 +362,9 @@ ms_status ms_cross_entropy_forward(const ms_tensor *x, const ms_tensor *W, const
     if (capped_product({std::max(M, V), (D + 7) / 8 * 8}) > kMaxElems - 16)
         return fail(MS_E_UNSUPPORTED, "operands have more than 2^31-17 elements");
     if (M > ms::kMaxHeadRows) return fail(MS_E_UNSUPPORTED, "x has more than 2^27-8 rows");
+    // one launch of bf16 tiles of 128 x 128 logits, of 256 threads each: 2^32 - 1 threads
+    if (x->dtype == MS_BF16 && (M + 127) / 128 * ((V + 127) / 128) >= int64_t(1) << 24)
+        return fail(MS_E_UNSUPPORTED, "2^38 or more logits");
     if ((st = check_vector(b, "b", V, x->dtype))) return st;
     if (reduction < MS_REDUCE_MEAN || reduction > MS_REDUCE_NONE) return fail(MS_E_ARG, "unknown reduction %d", reduction);
     if (M > 0 && !target) return fail(MS_E_NULL, "target is NULL");

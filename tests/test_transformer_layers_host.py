@@ -331,3 +331,15 @@ def test_bf16_gated_operands_past_32_bit_offsets(stub, M_, D_, F_):
     assert c.forward() == L.MS_E_UNSUPPORTED, stub.ms_last_error()
     assert stub.blocks_log() == b"" and stub.stub_log() == b""
     assert Call(stub, "gated", "f32", **over("f32")).forward() == 0
+
+
+def test_bf16_logits_of_more_tiles_than_a_launch(stub):
+    """(A launch has 2^32 - 1 threads at most.)"""
+    for rows, words, status in ((2 ** 23, 2 ** 15, L.MS_E_UNSUPPORTED), (2 ** 22, 2 ** 15, 0), (2 ** 27 - 8, 2 ** 11 - 128, 0),
+                                (2 ** 27 - 8, 2 ** 11, L.MS_E_UNSUPPORTED)):
+        c = Call(stub, "xent", "bf16", x=tensor((rows, 8)), W=tensor((words, 8)), b=tensor((words,)), mask=0)
+        assert c.forward() == status, (rows, words, stub.ms_last_error())
+        stub.blocks_reset()
+        c = Call(stub, "xent", "f32", x=tensor((rows, 8), "f32"), W=tensor((words, 8), "f32"), b=tensor((words,), "f32"), mask=0)
+        assert c.forward() == 0
+        stub.blocks_reset()
