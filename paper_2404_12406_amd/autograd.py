@@ -4,7 +4,8 @@ and nn.Modules, and a converter that swaps them into an existing model
 keep from which of its inputs require grad, and whose backward computes only
 the gradients autograd asks for).
 
-Each Function derives its mask from ctx.needs_input_grad, runs the forward
+Each Function derives its mask from ctx.needs_input_grad (without grad mode the
+layer runs outside of it, with no mask), runs the forward
 through the C ABI and keeps the library's record on ctx -- the record holds
 references to exactly the tensors the save rule borrows, so PyTorch's
 allocator retains what the ledger reports and nothing else.  Backward hands
@@ -157,6 +158,21 @@ class _DropoutFn(torch.autograd.Function):
         return gx, None, None
 
 
+# Inside a Function the grad mode is always off and needs_input_grad goes by the tensors
+# alone, so who calls it asks: with the mode off (no_grad, inference_mode) no backward can
+# follow, and the layer is told to keep nothing.
+def _layer(spec, x, W, b):
+    return _LayerFn.apply(spec, x, W, b) if torch.is_grad_enabled() else api.layer_forward(spec, x, W, b)[0]
+
+
+def _relu(x):
+    return _ReLUFn.apply(x) if torch.is_grad_enabled() else api.layer_forward(api.ReLU(), x)[0]
+
+
+def _dropout(x, p, seed):
+    return _DropoutFn.apply(x, p, seed) if torch.is_grad_enabled() else api.layer_forward(api.Dropout(p, seed, 0), x)[0]
+
+
 class MSConv2d(nn.Module):
     """Conv2d (cross-correlation, zero padding, dilation 1, groups 1) with a
     channels-last weight [K, C, R, S] and optional bias [K]."""
@@ -171,7 +187,7 @@ class MSConv2d(nn.Module):
         self.spec = api.Conv2d(stride, padding)
 
     def forward(self, x):
-        return _LayerFn.apply(self.spec, x, self.weight, self.bias)
+        return _layer(self.spec, x, self.weight, self.bias)
 
 
 class MSConvTranspose2d(nn.Module):
@@ -189,7 +205,7 @@ class MSConvTranspose2d(nn.Module):
         self.spec = api.ConvTranspose2d(stride, padding, output_padding)
 
     def forward(self, x):
-        return _LayerFn.apply(self.spec, x, self.weight, self.bias)
+        return _layer(self.spec, x, self.weight, self.bias)
 
 
 class _Conv3dBase(nn.Module):
@@ -201,7 +217,7 @@ class _Conv3dBase(nn.Module):
             self.weight.data = _cl(self.weight.data)
 
     def forward(self, x):
-        return _LayerFn.apply(self.spec, _cl(x), self.weight, self.bias)
+        return _layer(self.spec, _cl(x), self.weight, self.bias)
 
 
 class MSConv3d(_Conv3dBase):
@@ -242,7 +258,7 @@ class _Conv1dBase(nn.Module):
             self.weight.data = _channels_inner(self.weight.data)
 
     def forward(self, x):
-        y = _LayerFn.apply(self.spec, _cl(_channels_inner(x).unsqueeze(2)), self.weight.unsqueeze(2), self.bias)
+        y = _layer(self.spec, _cl(_channels_inner(x).unsqueeze(2)), self.weight.unsqueeze(2), self.bias)
         return y.squeeze(2)
 
 
@@ -275,7 +291,7 @@ class MSLinear(nn.Module):
 
     def forward(self, x):
         lead = x.shape[:-1]
-        y = _LayerFn.apply(self.spec, x.reshape(-1, x.shape[-1]), self.weight, self.bias)
+        y = _layer(self.spec, x.reshape(-1, x.shape[-1]), self.weight, self.bias)
         return y.reshape(*lead, y.shape[-1])
 
 
@@ -293,14 +309,14 @@ class MSBatchNorm2dEval(nn.Module):
 
     def forward(self, x):
         spec = api.BatchNormEval(self.running_mean, self.running_var, self.eps)
-        return _LayerFn.apply(spec, x, self.weight, self.bias)
+        return _layer(spec, x, self.weight, self.bias)
 
 
 class MSReLU(nn.Module):
     """ReLU whose backward keeps one bit per element (Sec. 2.2.2)."""
 
     def forward(self, x):
-        return _ReLUFn.apply(_dense(x))
+        return _relu(_dense(x))
 
 
 class MSDropout(nn.Module):
@@ -324,7 +340,7 @@ class MSDropout(nn.Module):
             return x
         seed = int(torch.randint(0, 2 ** 63 - 1, (), dtype=torch.int64))
         self.last_seed = seed
-        return _DropoutFn.apply(_dense(x), self.p, seed)
+        return _dropout(_dense(x), self.p, seed)
 
 
 class MSLayerNorm(nn.Module):
@@ -338,7 +354,7 @@ class MSLayerNorm(nn.Module):
         self.spec = api.LayerNorm(float(eps))
 
     def forward(self, x):
-        return _LayerFn.apply(self.spec, x.reshape(-1, x.shape[-1]), self.weight, self.bias).reshape(x.shape)
+        return _layer(self.spec, x.reshape(-1, x.shape[-1]), self.weight, self.bias).reshape(x.shape)
 
 
 class MSGatedLinear(nn.Module):
@@ -354,7 +370,7 @@ class MSGatedLinear(nn.Module):
         self.spec = api.GatedLinear(act, keep)
 
     def forward(self, x):
-        y = _LayerFn.apply(self.spec, x.reshape(-1, x.shape[-1]), self.weight, self.bias)
+        y = _layer(self.spec, x.reshape(-1, x.shape[-1]), self.weight, self.bias)
         return y.reshape(*x.shape[:-1], y.shape[-1])
 
 
@@ -372,7 +388,7 @@ class MSLinearCrossEntropy(nn.Module):
 
     def forward(self, x, target):
         spec = api.LinearCrossEntropy(target.reshape(-1), self.ignore_index, self.reduction)
-        loss = _LayerFn.apply(spec, x.reshape(-1, x.shape[-1]), self.weight, self.bias)
+        loss = _layer(spec, x.reshape(-1, x.shape[-1]), self.weight, self.bias)
         return loss.reshape(target.shape if self.reduction == "none" else ())
 
 

@@ -58,3 +58,25 @@ def test_rows_by_the_million(dtype, rows):
     assert abs(loss.item() - want) <= 2e-5 * abs(want)
     assert worst <= bar * size
     assert float((dW.double() - gW).abs().max()) <= (bar + 2.0 ** -14) * float(gW.abs().max())
+
+
+@pytest.mark.parametrize("mode", [torch.no_grad, torch.inference_mode])
+def test_modules_that_train_keep_nothing_where_no_gradient_can_follow(mode):
+    from paper_2404_12406_amd import autograd as msa
+    g = torch.Generator().manual_seed(1)
+    make = lambda *s: torch.randn(*s, generator=g).bfloat16().cuda()
+    x, t = make(600, 64), torch.arange(600, device="cuda") % 50
+    for m, args in ((msa.MSLayerNorm(make(64), make(64)), ()), (msa.MSGatedLinear(make(192, 64), make(192)), ()),
+                    (msa.MSLinearCrossEntropy(make(50, 64), make(50)), (t,))):
+        want = m(x, *args).detach()
+        with mode():
+            h = x + 0
+            m(h, *args)
+            torch.cuda.synchronize()
+            before = torch.cuda.memory_allocated()
+            torch.cuda.reset_peak_memory_stats()
+            ms.ledger_reset()
+            got = m(h, *args)
+            assert torch.cuda.max_memory_allocated() - before <= got.untyped_storage().nbytes() + 512   # the output alone
+            assert ms.ledger_read()[1] == ms.ledger_read()[0] == 0
+        assert torch.equal(got, want)
