@@ -175,7 +175,8 @@ typedef struct ms_record ms_record;
  * the layer output, which stock PyTorch's ReLU keeps; MS_SAVED_MASK8 (policy
  * accounting only): the one-byte-per-element mask stock PyTorch's dropout
  * keeps.  MS_SAVED_PROJ: a gated linear unit's projections.  MS_SAVED_LSE: a
- * cross entropy's log-sum-exp of each row (and its targets).  MS_SAVED_GRAD: its
+ * cross entropy's log-sum-exp of each row's words but the target (and its targets).
+ * MS_SAVED_GRAD: its
  * input's gradient but for the loss's. */
 enum { MS_SAVED_X = 1u, MS_SAVED_W = 2u, MS_SAVED_MEAN = 4u, MS_SAVED_VAR = 8u, MS_SAVED_BITS = 16u,
        MS_SAVED_Y = 32u, MS_SAVED_MASK8 = 64u, MS_SAVED_PROJ = 128u,
@@ -343,7 +344,7 @@ ms_status ms_gated_linear_forward(const ms_tensor *x, const ms_tensor *W, const 
 
 /*
  * ms_cross_entropy_kept_bytes -- size of what ms_cross_entropy_forward() leaves in
- * `kept` for these sizes and mask: a float a row (its log-sum-exp), or the gradient of
+ * `kept` for these sizes and mask: a float a row (see there), or the gradient of
  * x itself (see there): [rows, D] values of 4 bytes for MS_F32, of 3 for MS_BF16
  * (fp32's leading 24 bits, as ms_gated_projection_bytes()'s).  0 with mask 0 or an
  * extent that is not positive.
@@ -356,7 +357,10 @@ uint64_t ms_cross_entropy_kept_bytes(int64_t rows, int64_t D, int64_t V, int32_t
  * z = x W^T + b;  row i with target t costs log(sum over v of exp(z_iv)) - z_it.
  * The logits of a large vocabulary outweigh every other activation of a model;
  * here they exist a tile at a time, and a record keeps of the softmax one number
- * a row: its log-sum-exp.  Backward takes the logits again, a piece of the
+ * a row: l, the log-sum-exp of the words other than its target.  (The loss, log(1 +
+ * exp(l - z_t)), and the target's entry of dz, -g / (1 + exp(z_t - l)), are then
+ * no differences of numbers near each other where the target has nearly all of the
+ * probability.)  Backward takes the logits again, a piece of the
  * vocabulary at a time in transient workspace (about a gigabyte of them):
  *   dz = (exp(z - lse) - [v = t]) g,  dx = dz W,  dW = dz^T x,  db = sum of dz,
  * g the gradient of the row's share of the loss.
@@ -374,12 +378,13 @@ uint64_t ms_cross_entropy_kept_bytes(int64_t rows, int64_t D, int64_t V, int32_t
  * up to 8 at most 2^31 - 17, in bf16 fewer than 2^24 tiles of 128 x 128 logits
  * (MS_E_UNSUPPORTED otherwise); b[V] contiguous or NULL.  loss: fp32,
  * contiguous.  With mask != 0, kept is caller-allocated device memory of
- * ms_cross_entropy_kept_bytes(), 16-byte aligned, fully overwritten, and borrowed (a
- * log-sum-exp with x, W, b and target, which every gradient then needs); with mask 0
+ * ms_cross_entropy_kept_bytes(), 16-byte aligned, fully overwritten, and borrowed (l,
+ * with x, W, b and target, which every gradient then needs); with mask 0
  * it may be NULL.  dz is rounded to x's dtype before its products, everything else is
- * in fp32 (a log-sum-exp too: where every logit of a row is past some 10^6 in size, it
- * no longer resolves what they differ by, and gradients taken from it suffer; the loss
- * and a gradient taken in the forward do not).  Backward is ms_layer_backward() with
+ * in fp32.  So is l: with logits of size Z a gradient taken from it is off by some
+ * 2^-24 Z of itself for that alone (by all of it past some 10^7), as the logits' own
+ * sums have it too; the loss and a gradient taken in the forward have the differences
+ * of the logits themselves.  Backward is ms_layer_backward() with
  * grad_y of the loss's shape, fp32.  ms_layer_forward() rejects MS_CROSS_ENTROPY
  * (MS_E_ARG).
  */

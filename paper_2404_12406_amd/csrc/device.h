@@ -187,7 +187,8 @@ int launch_linear_bwd(int dtype, int64_t M, int64_t K, int64_t N, int64_t wrows,
 // Softmax cross entropy of the logits x[M][D] w[V][D]^T + b (b may be null) of the
 // rows whose target is not `ignore` (a target that is no word gives NaN).
 // reduction: 0 mean, 1 sum (loss[1]), 2 none (loss[M]); lse[M] (may be null in the
-// forward) is what the backward needs.  padw, padb: bf16 weight rows that are no
+// forward), the log-sum-exp of each row's words but the target, is what the backward
+// needs.  padw, padb: bf16 weight rows that are no
 // whole 16-byte vectors or not so aligned, a bias not 4-byte aligned (they are
 // copied).  In the backward any of dx, dw, db may be null; gloss is the gradient of
 // the loss, fp32.  Where xent_keeps_gradient(), the forward takes `kept` of

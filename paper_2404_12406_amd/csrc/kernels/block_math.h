@@ -83,6 +83,29 @@ __device__ __forceinline__ floatx2 join_lse(floatx2 a, floatx2 b) {
     return floatx2{m, sa + sb};
 }
 
+// A row's loss from the statistics a of the words other than its target (as join_lse()'s)
+// and the target's logit z: d, the logarithm of the odds against the target, is a sum of
+// parts with small errors, and neither the loss log(1 + exp(d)) nor what the target's
+// probability lacks of 1, 1 / (1 + exp(-d)), is a difference of numbers near 1: both
+// keep their leading digits however small they are.  NaN where the row has no
+// distribution: no finite logit, an infinite one, or (z NaN) no such word.
+struct RowLoss {
+    float others;   // log of the sum of the other words' exponentials: -inf where there is none
+    float loss;
+    float ct;       // the target's entry of dz: minus what its probability lacks of 1
+};
+__device__ __forceinline__ float target_entry(float d) { return -1.f / (1.f + expf(-d)); }
+__device__ __forceinline__ RowLoss row_loss(floatx2 a, float z) {
+    const float ls = logf(a.y);
+    // (the difference first: it is exact where both are large)
+    const float d = z == INFINITY ? NAN : (a.x - z) + ls;
+    RowLoss r;
+    r.others = d != d ? NAN : a.x + ls;
+    r.loss = fmaxf(d, 0.f) + log1pf(expf(-fabsf(d)));
+    r.ct = target_entry(d);
+    return r;
+}
+
 // Columns of one statistic and reference of exponentials that are kept.
 constexpr int kProbCols = 64;
 

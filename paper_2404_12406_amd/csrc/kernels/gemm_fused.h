@@ -5,10 +5,11 @@
 //   kEpiGateGrad  z again, then the gradient of z for that of y: dz_gate = dy
 //                 z_up act'(z_gate), dz_up = dy act(z_gate)
 //   kEpiLse       z = x W^T + b over a vocabulary: the maximum and the sum of
-//                 exponentials of each row's part of a column tile, and the
-//                 target's logit; z is not written
-//   kEpiXent      z again, then dz = (exp(z - lse) - [column = target]) scale, and
-//                 optionally its column sums before it is rounded
+//                 exponentials of each row's part of a column tile, its target
+//                 left out, and the target's logit; z is not written
+//   kEpiXent      z again, then dz = exp(z - lse) scale, in the target's column its
+//                 own entry times scale, and optionally the column sums of dz before
+//                 it is rounded
 //   kEpiProb      z, then exp(z - r) of the other words than the target, r a
 //                 reference of each row's part of a wave's columns, with those parts'
 //                 sums of exponentials and the target's logit
@@ -56,6 +57,7 @@ struct FusedArgs : Args {
     float *tlogit;         // with them: the target's logit; kEpiXent: what rounding took from the target's dz
     int64_t stat_ld;
     const float *lse, *scale;   // kEpiXent: of each row
+    const float *ct;       // with them: the target's entry of dz but for the scale
     const float *out_scale;     // kEpiStore, kEpiRows: the sums' factor
     int add;               // kEpiAdd: add to the partials (0: write them)
     const int *nsplit;     // kEpiAdd: their number, on the device,
@@ -310,6 +312,23 @@ __device__ __forceinline__ void fused_epilogue(const FusedArgs &P, char *smem, f
             for (int i = 0; i < TM; ++i) {
                 __builtin_amdgcn_sched_barrier(0);   // one pass at a time: the sums leave few registers
                 const int m = m0 + wm0 + 32 * i + fr;
+                const int t = m < M ? tgt[i] - P.v0 - (n0 + wn0) : -1;   // within this wave's columns?
+                if (__any((unsigned)t < (unsigned)G::WN)) {   // the target leaves the sums
+                    float z = 0.f;
+                    bool mine = false;
+#pragma unroll
+                    for (int j = 0; j < TN; ++j)
+#pragma unroll
+                        for (int q = 0; q < 4; ++q)
+#pragma unroll
+                            for (int v = 0; v < 4; ++v)
+                                if (t == 32 * j + 8 * q + 4 * fh + v) {
+                                    z = acc[i][j][4 * q + v];
+                                    acc[i][j][4 * q + v] = -INFINITY;
+                                    mine = true;
+                                }
+                    if (mine && n0 + wn0 + t < N) P.tlogit[m] = z;
+                }
                 float top = -INFINITY;
 #pragma unroll
                 for (int j = 0; j < TN; ++j)
@@ -325,22 +344,6 @@ __device__ __forceinline__ void fused_epilogue(const FusedArgs &P, char *smem, f
                     for (int v = 0; v < 16; ++v) s += exp_below(acc[i][j][v], t0);
                 s += __shfl_xor(s, 32);
                 if (fh == 0) red[(wn0 / G::WN) * BM + wm0 + 32 * i + fr] = floatx2{top, s};
-                const int t = m < M ? tgt[i] - P.v0 - (n0 + wn0) : -1;   // within this wave's columns?
-                if (__any((unsigned)t < (unsigned)G::WN)) {
-                    float z = 0.f;
-                    bool mine = false;
-#pragma unroll
-                    for (int j = 0; j < TN; ++j)
-#pragma unroll
-                        for (int q = 0; q < 4; ++q)
-#pragma unroll
-                            for (int v = 0; v < 4; ++v)
-                                if (t == 32 * j + 8 * q + 4 * fh + v) {
-                                    z = acc[i][j][4 * q + v];
-                                    mine = true;
-                                }
-                    if (mine && n0 + wn0 + t < N) P.tlogit[m] = z;
-                }
             }
             __syncthreads();
             for (int r = wave * 64 + lane; r < BM; r += G::NT) {
@@ -377,12 +380,12 @@ __device__ __forceinline__ void fused_epilogue(const FusedArgs &P, char *smem, f
 #pragma unroll
                         for (int v = 0; v < 4; ++v) {
                             float p = exp_below(acc[i][j][4 * q + v], t0);
-                            s += p;
                             if (any && t == 32 * j + 8 * q + 4 * fh + v) {
                                 z = acc[i][j][4 * q + v];
                                 mine = true;
                                 p = 0.f;
                             }
+                            s += p;
                             o[v] = (bf16)p;
                         }
                         *reinterpret_cast<bf16x4 *>(stage + fr * PITCH + 32 * j + 8 * q + 4 * fh) = o;
@@ -406,6 +409,7 @@ __device__ __forceinline__ void fused_epilogue(const FusedArgs &P, char *smem, f
                 int t = in ? tgt[i] - P.v0 - (n0 + wn0) : -1;
                 if (t >= N - (n0 + wn0)) t = -1;   // (a later piece's: this one may end within a tile)
                 const bool any = __any((unsigned)t < (unsigned)G::WN);
+                const float ct = any && in ? P.ct[m] : 0.f;
                 float rest = 0.f;
 #pragma unroll
                 for (int j = 0; j < TN; ++j)
@@ -415,7 +419,7 @@ __device__ __forceinline__ void fused_epilogue(const FusedArgs &P, char *smem, f
 #pragma unroll
                         for (int v = 0; v < 4; ++v) {
                             float p = exp_below(acc[i][j][4 * q + v], l);
-                            if (any && t == 32 * j + 8 * q + 4 * fh + v) p -= 1.f;
+                            if (any && t == 32 * j + 8 * q + 4 * fh + v) p = ct;
                             p = in ? p * sc : 0.f;   // (the other rows hold anything)
                             o[v] = (bf16)p;
                             acc[i][j][4 * q + v] = p;

@@ -52,11 +52,12 @@ void xent_bias_rows(int64_t M, int64_t D, int64_t V, int *tile, int *rows) {
 }
 
 // dz[M][ldz] of the words v0 .. v0 + V - 1, whose rows of W and biases w and
-// bias are; columns V .. ldz - 1 are zeros.  rest: what rounding took from the entry of
+// bias are; columns V .. ldz - 1 are zeros.  ct: the targets' entries.  rest: what rounding took from the entry of
 // each row whose target is among them.  dbpart (null: not wanted): the column sums,
 // rows of V.
 int xent_grad(int64_t M, int64_t D, int64_t V, const void *x, const void *w, const void *bias, const int *count, const int *target,
-              int v0, const float *lse, const float *scale, void *dz, int64_t ldz, float *rest, float *dbpart, hipStream_t st) {
+              int v0, const float *lse, const float *scale, const float *ct, void *dz, int64_t ldz, float *rest, float *dbpart,
+              hipStream_t st) {
     const FusedPlan p = plan(kRowTiles, 2, M, V, D, 1);
     FusedArgs a = rows_args(kRowTiles[p.tile], M, V, D, x, w, V);
     a.fbias = (const bf16 *)bias;
@@ -65,6 +66,7 @@ int xent_grad(int64_t M, int64_t D, int64_t V, const void *x, const void *w, con
     a.v0 = v0;
     a.lse = lse;
     a.scale = scale;
+    a.ct = ct;
     a.tlogit = rest;
     a.dbpart = dbpart;
     a.c = (bf16 *)dz;
@@ -79,7 +81,7 @@ int xent_prob_parts(int64_t M, int64_t D, int64_t V) {
 }
 
 // prob[M][ldz] = exp(z - r) for the words that are not the row's target, zeros there
-// and in columns V .. ldz - 1; r and the sums (the target's among them) go to stat.
+// and in columns V .. ldz - 1; r and their sums go to stat.
 int xent_prob(int64_t M, int64_t D, int64_t V, const void *x, const void *w, const void *bias, const int *count, const int *target,
               void *stat, int64_t stat_ld, float *tlogit, void *prob, int64_t ldz, hipStream_t st) {
     const FusedPlan p = plan(kRowTiles, 2, M, V, D, 1);

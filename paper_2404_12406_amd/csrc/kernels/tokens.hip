@@ -212,7 +212,10 @@ __global__ __launch_bounds__(KS * 64) void lse_kernel(const Args P) {
                     const bool in = n < P.V;
                     if (P.bias && in) acc[i][v] += to_f32(((const T *)P.bias)[n]);
                     acc[i][v] = in ? acc[i][v] : -INFINITY;
-                    if (in && t == n) P.tlogit[m] = acc[i][v];
+                    if (in && t == n) {   // the target leaves the sums
+                        P.tlogit[m] = acc[i][v];
+                        acc[i][v] = -INFINITY;
+                    }
                     top = fmaxf(top, acc[i][v]);
                 }
             const float t0 = top == -INFINITY ? 0.f : top;
@@ -233,7 +236,7 @@ __global__ __launch_bounds__(KS * 64) void lse_kernel(const Args P) {
 // The rows' losses from the blocks' statistics, a wave a row, and their reduction.
 __global__ __launch_bounds__(1024) void loss_kernel(const floatx2 *__restrict__ stat, int parts, const float *__restrict__ tlogit,
                                                     const int64_t *__restrict__ target, int64_t ignore, int M, int V, int reduction,
-                                                    float *__restrict__ loss, float *__restrict__ lse) {
+                                                    float *__restrict__ loss, float *__restrict__ others) {
     __shared__ float each[kRows];
     const int lane = threadIdx.x & 63, m = threadIdx.x >> 6;
     if (m < M) {
@@ -245,12 +248,11 @@ __global__ __launch_bounds__(1024) void loss_kernel(const floatx2 *__restrict__ 
             const int64_t t = target[m];
             float l = 0.f, c = 0.f;
             if (t != ignore) {
-                const bool word = t >= 0 && t < V;
-                const float ls = !word || a.x == -INFINITY ? NAN : logf(a.y);
-                l = a.x + ls;
-                c = (a.x - (word ? tlogit[m] : 0.f)) + ls;   // (the difference first: it is exact where both are large)
+                const RowLoss q = row_loss(a, t >= 0 && t < V ? tlogit[m] : NAN);
+                l = q.others;
+                c = q.loss;
             }
-            if (lse) lse[m] = l;
+            if (others) others[m] = l;
             if (reduction == 2) loss[m] = c;
             each[m] = c;
         }

@@ -3,6 +3,11 @@
 //   dz = (exp(z - lse) - [v = t]) scale_i,  dx = dz W,  dW = dz^T x,  db = sum of dz,
 // without keeping z.
 //
+//  * A target with nearly all of the probability leaves a loss and a dz that are small
+//    differences of numbers near 1.  So it stays out of the sums: with l the log of the
+//    sum of the others' exponentials, loss = log(1 + exp(l - z_t)) and dz_t = -scale /
+//    (1 + exp(z_t - l)) (row_loss()).  A record keeps l; backward takes z_t of each row
+//    again where it gathers the rows, and has both lse and dz_t from the two.
 //  * Rows whose target is the ignored one take no part: the others are gathered
 //    first (their number stays on the device and bounds every contraction), so
 //    that whatever an ignored row holds, NaN included, reaches no result, and a
@@ -22,13 +27,14 @@
 //    with the target's p left out of p W, so that what is left of it at a large
 //    p_t is no difference of rounded numbers.
 // Exponentials are of differences from a maximum or an lse, which no logit of
-// any size overflows; a row's lse is kept in fp32.
+// any size overflows; what is kept of a row, and its lse, are in fp32.
 //
 // Measured, us.  8192 x 768 x 50000 bf16, a third of the rows ignored, head trained:
 // statistics 443, dz 542, dx 412, dW 433, everything else 80.  4096 x 4096 x 128000,
 // head frozen: exponentials 3645, dx 3428, the rest 120.  777 x 514 x 10007 fp32,
 // trained: z 79 (twice), dx 88, dW 83, the softmax's passes 23, W's padded copies 17.
 #include <algorithm>
+#include <type_traits>
 
 #include "block_math.h"
 #include "limits.h"
@@ -42,7 +48,8 @@ int xent_lse_tiles(int64_t M, int64_t D, int64_t V);
 int xent_lse(int64_t M, int64_t D, int64_t V, const void *x, const void *w, const void *bias, const int *count, const int *target,
              void *stat, float *tlogit, hipStream_t st);
 int xent_grad(int64_t M, int64_t D, int64_t V, const void *x, const void *w, const void *bias, const int *count, const int *target,
-              int v0, const float *lse, const float *scale, void *dz, int64_t ldz, float *rest, float *dbpart, hipStream_t st);
+              int v0, const float *lse, const float *scale, const float *ct, void *dz, int64_t ldz, float *rest, float *dbpart,
+              hipStream_t st);
 void xent_bias_rows(int64_t M, int64_t D, int64_t V, int *tile, int *rows);
 int xent_prob_parts(int64_t M, int64_t D, int64_t V);
 int xent_prob(int64_t M, int64_t D, int64_t V, const void *x, const void *w, const void *bias, const int *count, const int *target,
@@ -59,7 +66,7 @@ namespace tok {
 bool applies(int dtype, int64_t M, int64_t N, int64_t K, const void *x, const void *w);
 size_t xent_workspace();
 int xent(int dtype, int64_t M, int64_t D, int64_t V, const void *x, const void *w, const void *b, const int64_t *target, int64_t ignore,
-         int reduction, float *loss, float *lse, void *ws, hipStream_t st);
+         int reduction, float *loss, float *others, void *ws, hipStream_t st);
 }  // namespace tok
 
 namespace xent {
@@ -116,7 +123,9 @@ __global__ __launch_bounds__(1024) void rows_kernel(const int64_t *__restrict__ 
 }
 
 // xc[i][0 .. ld) = x[idx[i]] and zeros past D, for the rows that count; the others'
-// rows are zeros where `fill`.  With lse: lsec[i], and the loss's gradient as a
+// rows are zeros where `fill`.  With others (the kept log-sums of the words but the
+// targets, w and bias then being theirs): the row's lse[i] and the target's entry of its
+// dz, ct[i], from the target's logit, and the loss's gradient as a
 // factor of the row's dz, scale[i], and one of all results, scale[M].  Where it is
 // the same for every row (mean, sum) it stays out of dz: that is rounded, and a
 // common factor would give every row's largest entry, near -1 times it, the same
@@ -129,11 +138,13 @@ template <typename T, bool SCAN>
 __global__ __launch_bounds__(256) void gather_kernel(const int64_t *__restrict__ target, int64_t ignore, int64_t words, int *__restrict__ pos,
                                                      int *__restrict__ tgt, const T *__restrict__ x, const int *__restrict__ idx,
                                                      int *__restrict__ count, int64_t M, int D, int ld, bool fill,
-                                                     T *__restrict__ xc, const float *__restrict__ lse,
-                                                     const float *__restrict__ gloss, int reduction, float *__restrict__ lsec,
-                                                     float *__restrict__ scale, SplitRule rule, int *__restrict__ nsplit,
-                                                     int64_t chunk, int *__restrict__ ccount) {
+                                                     T *__restrict__ xc, const float *__restrict__ others,
+                                                     const T *__restrict__ w, const T *__restrict__ bias,
+                                                     const float *__restrict__ gloss, int reduction, float *__restrict__ lse,
+                                                     float *__restrict__ ct, float *__restrict__ scale, SplitRule rule,
+                                                     int *__restrict__ nsplit, int64_t chunk, int *__restrict__ ccount) {
     constexpr int V = Vec16<T>::N;
+    __shared__ float red[4];
     int n, at = 0;        // the rows that count; SCAN: the place of this block's row
     bool counts = true;
     if constexpr (SCAN) {
@@ -169,18 +180,42 @@ __global__ __launch_bounds__(256) void gather_kernel(const int64_t *__restrict__
             if (ccount) ccount[k] = rows;
         }
     // (no row that counts: every result is an empty sum, whatever the factor)
-    if (lse && blockIdx.x == 0 && threadIdx.x == 0)
+    if (others && blockIdx.x == 0 && threadIdx.x == 0)
         scale[M] = reduction == 2 || n == 0 ? 1.f : reduction == 1 ? gloss[0] : gloss[0] / (float)n;
     for (int64_t k = blockIdx.x; k < M; k += gridDim.x) {
         const int64_t i = SCAN ? at : k;
         if (i >= n && !fill) break;
         const int64_t r = i >= n ? 0 : SCAN ? k : idx[i];
-        for (int c = (int)threadIdx.x * V; c < ld; c += 256 * V)
-            store_vec(xc + i * ld, c, ld, i < n && c < D ? load_vec(x + r * D, c, D) : zero16<T>());
-        if (lse && threadIdx.x == 0) {
-            lsec[i] = i < n ? lse[r] : 0.f;
+        const int64_t t = others && i < n ? target[r] : -1;
+        const bool word = t >= 0 && t < words;
+        float z = 0.f;   // this thread's part of the target's logit
+        for (int c = (int)threadIdx.x * V; c < ld; c += 256 * V) {
+            const Vec16<T> v = i < n && c < D ? load_vec(x + r * D, c, D) : zero16<T>();
+            store_vec(xc + i * ld, c, ld, v);
+            if (word && c < D) {
+                const Vec16<T> wt = load_vec(w + t * D, c, D);
+#pragma unroll
+                for (int e = 0; e < V; ++e) z += to_f32(v.e[e]) * to_f32(wt.e[e]);
+            }
+        }
+        if (!others) continue;
+#pragma unroll
+        for (int o = 32; o > 0; o >>= 1) z += __shfl_xor(z, o);
+        if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = z;
+        __syncthreads();
+        if (threadIdx.x == 0) {
+            float l = 0.f, c = 0.f;
+            if (i < n) {
+                z = word ? red[0] + red[1] + red[2] + red[3] + (bias ? to_f32(bias[t]) : 0.f) : NAN;
+                const float rest = others[r], d = rest - z;   // (one of them may be minus infinity)
+                l = fmaxf(rest, z) + log1pf(expf(-fabsf(d)));
+                c = target_entry(d);
+            }
+            lse[i] = l;
+            ct[i] = c;
             scale[i] = i >= n ? 0.f : reduction == 2 ? gloss[r] : 1.f;
         }
+        __syncthreads();   // red is read
     }
 }
 
@@ -190,14 +225,14 @@ struct Kept {
     float *ref, *f, *ct;
 };
 
-// The loss and lse of every row from `parts` statistics [part][ld] of the rows that
+// The loss of every row and what is kept of it, others[], from `parts` statistics [part][ld] of the rows that
 // count, of which this launch has those from place i0 to i0 + ld - 1 (8 rows a
 // block, 32 threads each).  With prob (exponentials [ld][ldz] of kProbCols columns a
 // part): the parts of a row with another reference than the row's are brought to it.
 __global__ __launch_bounds__(256) void combine_kernel(const floatx2 *__restrict__ stat, int parts, int64_t ld, int64_t i0,
                                                       const float *__restrict__ tlogit, const int *__restrict__ pos,
                                                       const int *__restrict__ tgt, int64_t M, float *__restrict__ each,
-                                                      float *__restrict__ lse, Kept kept, bf16 *__restrict__ prob, int64_t ldz) {
+                                                      float *__restrict__ others, Kept kept, bf16 *__restrict__ prob, int64_t ldz) {
     constexpr int ROWS = 8, GROUPS = 256 / ROWS;
     __shared__ floatx2 red[GROUPS][ROWS];
     const int row = threadIdx.x % ROWS, grp = threadIdx.x / ROWS;
@@ -225,19 +260,18 @@ __global__ __launch_bounds__(256) void combine_kernel(const floatx2 *__restrict_
         if (r < M && (i < 0 || here)) {
             float l = 0.f, loss = 0.f;
             if (here) {
-                // no word at all, or every one of them minus infinity: no distribution
-                const bool none = tgt[i] < 0 || a.x == -INFINITY;
-                const float ls = none ? NAN : logf(a.y);
-                l = a.x + ls;
-                // (the difference first: it is exact where both are large)
-                loss = (a.x - (tgt[i] < 0 ? 0.f : tlogit[i])) + ls;
-                if (kept.ref) {
-                    kept.ref[i] = a.x;
-                    kept.f[i] = none ? NAN : 1.f / a.y;
-                    kept.ct[i] = expm1f(-loss);
+                const float z = tgt[i] < 0 ? NAN : tlogit[i];
+                const RowLoss q = row_loss(a, z);
+                l = q.others;
+                loss = q.loss;
+                if (kept.ref) {   // (bf16: the exponentials have their reference already)
+                    const floatx2 all = prob ? floatx2{a.x, a.y + exp_below(z, a.x)} : join_lse(a, floatx2{z, 1.f});
+                    kept.ref[i] = all.x;
+                    kept.f[i] = q.loss != q.loss ? NAN : 1.f / all.y;
+                    kept.ct[i] = q.ct;
                 }
             }
-            if (lse) lse[r] = l;
+            if (others) others[r] = l;
             each[r] = loss;
         }
     }
@@ -430,7 +464,7 @@ __global__ __launch_bounds__(256) void bias_kernel(const float *__restrict__ par
 
 // ------------------------------------------------------------------ fp32 pieces
 // A piece's logits z[i][0 .. V) in rows of ldz, words v0 on: joins the row's statistics (those
-// of the first piece start them) and takes the target's logit.  A block a row.
+// of the first piece start them), without its target, whose logit it takes.  A block a row.
 __global__ __launch_bounds__(256) void lse_rows_kernel(const float *__restrict__ z, int ldz, int V, int v0, const int *__restrict__ count,
                                                        const int *__restrict__ tgt, bool first, floatx2 *__restrict__ stat,
                                                        float *__restrict__ tlogit) {
@@ -438,18 +472,19 @@ __global__ __launch_bounds__(256) void lse_rows_kernel(const float *__restrict__
     const int n = *count;
     for (int64_t i = blockIdx.x; i < n; i += gridDim.x) {
         const float *zr = z + i * ldz;
+        const int t = tgt[i] < 0 ? -1 : tgt[i] - v0;
         float top = -INFINITY;
         for (int c = (int)threadIdx.x * 4; c < V; c += 1024) {
             const Vec16<float> v = load_vec(zr, c, V);
 #pragma unroll
-            for (int e = 0; e < 4; ++e) top = c + e < V ? fmaxf(top, v.e[e]) : top;
+            for (int e = 0; e < 4; ++e) top = c + e < V && c + e != t ? fmaxf(top, v.e[e]) : top;
         }
         const float t0 = top == -INFINITY ? 0.f : top;
         float s = 0.f;
         for (int c = (int)threadIdx.x * 4; c < V; c += 1024) {
             const Vec16<float> v = load_vec(zr, c, V);
 #pragma unroll
-            for (int e = 0; e < 4; ++e) s += c + e < V ? exp_below(v.e[e], t0) : 0.f;
+            for (int e = 0; e < 4; ++e) s += c + e < V && c + e != t ? exp_below(v.e[e], t0) : 0.f;
         }
         floatx2 a = {top, s};
 #pragma unroll
@@ -459,8 +494,7 @@ __global__ __launch_bounds__(256) void lse_rows_kernel(const float *__restrict__
         if (threadIdx.x == 0) {
             for (int w = 1; w < 4; ++w) a = join_lse(a, red[w]);
             stat[i] = first ? a : join_lse(stat[i], a);
-            const int t = tgt[i] - v0;
-            if (tgt[i] >= 0 && t >= 0 && t < V) tlogit[i] = zr[t];
+            if (t >= 0 && t < V) tlogit[i] = zr[t];
         }
         __syncthreads();
     }
@@ -468,21 +502,23 @@ __global__ __launch_bounds__(256) void lse_rows_kernel(const float *__restrict__
 
 // z -> dz in place; the rows that do not count and the columns past V become zeros.
 // The softmax is exp(z - lse), or (inv) inv exp(z - lse), lse then being a reference
-// and inv the sum's inverse.
+// and inv the sum's inverse; ct: the target's entry.
 __global__ __launch_bounds__(256) void grad_rows_kernel(float *__restrict__ z, int ldz, int V, int v0, int64_t M, const int *__restrict__ count,
                                                         const int *__restrict__ tgt, const float *__restrict__ lse,
-                                                        const float *__restrict__ inv, const float *__restrict__ scale) {
+                                                        const float *__restrict__ inv, const float *__restrict__ ct,
+                                                        const float *__restrict__ scale) {
     const int n = *count;
     const float factor = scale ? scale[M] : 1.f;   // (what a common rounding error of 2^-24 would do does not matter)
     for (int64_t i = blockIdx.x; i < M; i += gridDim.x) {
         const bool in = i < n;
         const float l = in ? lse[i] : 0.f, f = in && inv ? inv[i] : 1.f, sc = in ? (scale ? scale[i] : 1.f) * factor : 0.f;
         const int t = in ? tgt[i] - v0 : -1;
+        const float pt = in ? ct[i] : 0.f;
         for (int c = (int)threadIdx.x * 4; c < ldz; c += 1024) {
             Vec16<float> v = load_vec(z + i * ldz, c, ldz);
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                const float p = exp_below(v.e[e], l) * f - (c + e == t ? 1.f : 0.f);
+                const float p = c + e == t ? pt : exp_below(v.e[e], l) * f;
                 v.e[e] = in && c + e < V ? p * sc : 0.f;
             }
             store_vec(z + i * ldz, c, ldz, v);
@@ -648,7 +684,7 @@ Fwd carve_fwd(Carve &c, int dtype, int64_t M, int64_t D, int64_t V, bool padw, b
 
 struct Bwd {
     Rows r;
-    float *lse, *scale, *rest;
+    float *lse, *ct, *scale, *rest;
     void *dz;
     float *part;     // partials of dx (fp32: the sum and a piece's)
     float *wp, *bp, *gwp, *gbp;   // fp32: a piece's padded operands and gradients
@@ -662,6 +698,7 @@ Bwd carve_bwd(Carve &c, int dtype, int64_t M, int64_t D, int64_t V, bool padw, b
     Bwd b{};
     b.r = carve_rows(c, dtype, M, D, V, padw, padb);
     b.lse = c.get<float>(M);
+    b.ct = c.get<float>(M);
     b.scale = c.get<float>(M + 1);
     b.rest = dtype == kBF16 ? c.get<float>(M) : nullptr;
     const int64_t p = piece(dtype, M, V), last = V - (V - 1) / p * p;
@@ -698,13 +735,14 @@ int row_grid(int64_t M) { return (int)std::max<int64_t>(1, std::min<int64_t>(M, 
 
 // The rows that count and what the contractions read.
 int start(const Rows &r, int dtype, int64_t M, int64_t D, int64_t V, const void *x, const void **w, const void **b,
-          const int64_t *target, int64_t ignore, const float *lse, const float *gloss, int reduction, float *lsec, float *scale,
+          const int64_t *target, int64_t ignore, const float *others, const float *gloss, int reduction, float *lse, float *ct, float *scale,
           const SplitRule &rule, int *nsplit, int64_t chunk, int *ccount, hipStream_t st) {
     const bool scan = M <= kScanRows;   // (a block a row)
     if (!scan) hipLaunchKernelGGL(rows_kernel, dim3(1), dim3(1024), 0, st, target, ignore, M, V, r.pos, r.idx, r.tgt, r.count);
-    auto gather = [&](auto kernel, auto *xs, auto *xc, bool fill) {
+    auto gather = [&](auto kernel, auto *xs, auto *xc, bool fill) {   // (before w and b move to their copies)
+        using T = std::remove_reference_t<decltype(*xc)>;
         hipLaunchKernelGGL(kernel, dim3(row_grid(M)), dim3(256), 0, st, target, ignore, V, r.pos, r.tgt, xs, r.idx, r.count, M, (int)D, (int)r.D8,
-                           fill, xc, lse, gloss, reduction, lsec, scale, rule, nsplit, chunk, ccount);
+                           fill, xc, others, (const T *)*w, (const T *)*b, gloss, reduction, lse, ct, scale, rule, nsplit, chunk, ccount);
     };
     if (dtype == kBF16) gather(scan ? gather_kernel<bf16, true> : gather_kernel<bf16, false>, (const bf16 *)x, (bf16 *)r.xc, false);
     else gather(scan ? gather_kernel<float, true> : gather_kernel<float, false>, (const float *)x, (float *)r.xc, true);
@@ -793,8 +831,8 @@ int launch_xent_fwd(int dtype, int64_t M, int64_t D, int64_t V, const void *x, c
     Carve c{static_cast<char *>(ws)};
     const Fwd f = carve_fwd(c, dtype, M, D, V, padw, padb, reduction != 2, kept != nullptr);
     const int64_t D8 = f.r.D8;
-    int err = start(f.r, dtype, M, D, V, x, &w, &b, target, ignore, nullptr, nullptr, reduction, nullptr, nullptr, f.rule, f.nsplit, f.chunk,
-                    f.ccount, st);
+    int err = start(f.r, dtype, M, D, V, x, &w, &b, target, ignore, nullptr, nullptr, reduction, nullptr, nullptr, nullptr, f.rule, f.nsplit,
+                    f.chunk, f.ccount, st);
     if (err) return err;
     if (dtype == kBF16 && M > 0 && !g2::rows_ok(M, V, D8, f.r.xc, w)) return (int)hipErrorInvalidValue;
     float *each = reduction == 2 ? loss : f.each;
@@ -839,7 +877,7 @@ int launch_xent_fwd(int dtype, int64_t M, int64_t D, int64_t V, const void *x, c
         if (!err) err = combine(1, M, 0, nullptr, 0);
         if (!err && kept) {   // (one piece)
             hipLaunchKernelGGL(grad_rows_kernel, dim3(row_grid(M)), dim3(256), 0, st, f.z, (int)q.np, (int)V, 0, M, f.r.count, f.r.tgt,
-                               f.kept.ref, f.kept.f, (const float *)nullptr);
+                               f.kept.ref, f.kept.f, f.kept.ct, (const float *)nullptr);
             err = (int)hipGetLastError();
             if (!err)
                 err = launch_linear_bwd(dtype, M, D8, q.np, q.n, f.r.count, f.z, f.r.xc, q.w, f.part, nullptr, nullptr, f.conv, stream);
@@ -875,7 +913,8 @@ int launch_xent_bwd(int dtype, int64_t M, int64_t D, int64_t V, const void *x, c
     hipStream_t st = (hipStream_t)stream;
     Carve c{static_cast<char *>(ws)};
     const Bwd k = carve_bwd(c, dtype, M, D, V, padw, padb, dx, dw, db);
-    int err = start(k.r, dtype, M, D, V, x, &w, &b, target, ignore, lse, gloss, reduction, k.lse, k.scale, k.rule, k.nsplit, M, nullptr, st);
+    int err = start(k.r, dtype, M, D, V, x, &w, &b, target, ignore, lse, gloss, reduction, k.lse, k.ct, k.scale, k.rule, k.nsplit, M, nullptr,
+                    st);
     if (err) return err;
     const int64_t p = piece(dtype, M, V), D8 = k.r.D8;
     if (dtype == kBF16 && M > 0 && !g2::rows_ok(M, V, D8, k.r.xc, w)) return (int)hipErrorInvalidValue;
@@ -886,7 +925,7 @@ int launch_xent_bwd(int dtype, int64_t M, int64_t D, int64_t V, const void *x, c
             const bf16 *wv = (const bf16 *)w + v0 * D8;
             if (M > 0)
                 err = g2::xent_grad(M, D8, n, k.r.xc, wv, b ? (const bf16 *)b + v0 : nullptr, k.r.count, k.r.tgt, (int)v0, k.lse, k.scale,
-                                    k.dz, ldz, k.rest, k.dbpart, st);
+                                    k.ct, k.dz, ldz, k.rest, k.dbpart, st);
             if (!err && dx && M > 0) err = g2::xent_dx(M, D8, n, ldz, p, k.dz, wv, k.r.count, k.nsplit, k.part, v0 > 0, st);
             bf16 *dbv = db ? (bf16 *)db + v0 : nullptr;
             if (!err && dw)
@@ -907,7 +946,7 @@ int launch_xent_bwd(int dtype, int64_t M, int64_t D, int64_t V, const void *x, c
                 err = logits(q, k.r, M, z, k.work, st);
                 if (err) break;
                 hipLaunchKernelGGL(grad_rows_kernel, dim3(row_grid(M)), dim3(256), 0, st, z, (int)q.np, (int)n, (int)v0, M, k.r.count,
-                                   k.r.tgt, k.lse, (const float *)nullptr, k.scale);
+                                   k.r.tgt, k.lse, (const float *)nullptr, k.ct, k.scale);
                 err = (int)hipGetLastError();
             }
             const bool tw = dw && D8 != D, tb = db && q.np != n;

@@ -292,7 +292,7 @@ struct BlockState {
     int64_t ignore = 0;
     const int64_t *target = nullptr;
     void *proj = nullptr;        // gated linear: the kept projections
-    float *lse = nullptr;        // cross entropy: log-sum-exp of each row,
+    float *lse = nullptr;        // cross entropy: log-sum-exp of each row without its target,
     const void *grad = nullptr;  // or the kept gradient
 };
 
