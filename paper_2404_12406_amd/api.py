@@ -346,6 +346,7 @@ class Record:
         self._b_meta = (tuple(b.shape), b.dtype) if b is not None else None
         self.y_shape = y_shape
         self.consumed = False
+        self._stream = _stream(x.device).value   # the forward's
 
     @property
     def saved(self):
@@ -355,6 +356,19 @@ class Record:
         a = MsAccount()
         check(_lib.load().ms_record_account(self._h, ctypes.byref(a)), "ms_record_account")
         return a.as_dict()
+
+    def spent(self, stream: ctypes.c_void_p, device):
+        """A backward that reads what is borrowed has been enqueued on `stream`.  These may
+        be the last references: where that is not the forward's stream, whose allocator
+        would hand the memory out again at once, it is to wait for this one."""
+        if stream.value != self._stream:
+            s = torch.cuda.current_stream(device)
+            for v in self._keep.values():
+                for t in (v if isinstance(v, tuple) else (v,)):
+                    if t is not None:
+                        t.record_stream(s)
+        self.consumed = True
+        self.release_refs()
 
     def release_refs(self):
         self._keep = {}
@@ -536,10 +550,10 @@ def _block_backward(rec, grad_y, grad_x, grad_W, grad_b):
         if m & bit and g is None:   # (the loss of a cross entropy has a dtype of its own)
             g = grad_y.new_empty(meta[0]) if meta[1] == grad_y.dtype else torch.empty(meta[0], dtype=meta[1], device=grad_y.device)
         out.append(g)
-    check(_block_fn("ms_layer_backward")(rec._h, _packed(grad_y), _packed(out[0]), _packed(out[1]), _packed(out[2]),
-                                         _stream(grad_y.device)), "ms_layer_backward")
-    rec.consumed = True
-    rec.release_refs()
+    stream = _stream(grad_y.device)
+    check(_block_fn("ms_layer_backward")(rec._h, _packed(grad_y), _packed(out[0]), _packed(out[1]), _packed(out[2]), stream),
+          "ms_layer_backward")
+    rec.spent(stream, grad_y.device)
     return tuple(out)
 
 
@@ -614,10 +628,10 @@ def layer_backward(rec: Record, grad_y: torch.Tensor, grad_x: Optional[torch.Ten
     if m & MASK_BIAS and grad_b is None:
         grad_b = torch.empty(rec._b_meta[0], dtype=grad_y.dtype, device=grad_y.device)
     gy, gx, gw, gb = tensor_desc(grad_y), tensor_desc(grad_x), tensor_desc(grad_W), tensor_desc(grad_b)
-    st = lib.ms_layer_backward(rec._h, _ptr(gy), _ptr(gx), _ptr(gw), _ptr(gb), _stream(grad_y.device))
+    stream = _stream(grad_y.device)
+    st = lib.ms_layer_backward(rec._h, _ptr(gy), _ptr(gx), _ptr(gw), _ptr(gb), stream)
     check(st, "ms_layer_backward")
-    rec.consumed = True
-    rec.release_refs()
+    rec.spent(stream, grad_y.device)
     return grad_x, grad_W, grad_b
 
 

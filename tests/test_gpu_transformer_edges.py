@@ -80,3 +80,29 @@ def test_modules_that_train_keep_nothing_where_no_gradient_can_follow(mode):
             assert torch.cuda.max_memory_allocated() - before <= got.untyped_storage().nbytes() + 512   # the output alone
             assert ms.ledger_read()[1] == ms.ledger_read()[0] == 0
         assert torch.equal(got, want)
+
+
+def test_backward_on_another_stream_than_the_forward():
+    """The records' buffers are not handed out again before that backward has read them."""
+    g = torch.Generator().manual_seed(5)
+    make = lambda *s: torch.randn(*s, generator=g).bfloat16().cuda()
+    x, dy = make(4096, 256), make(4096, 512)
+    one, t = torch.ones(1, device="cuda"), torch.arange(4096, device="cuda") % 3000
+    for spec, W, gy, mask, kept in ((ms.GatedLinear(), make(1024, 256), dy, 1, "projections"),
+                                    (ms.LinearCrossEntropy(t), make(3000, 256), one, 1, "grad"),
+                                    (ms.LinearCrossEntropy(t), make(3000, 256), one, 2, "lse")):
+        _, rec = ms.layer_forward(spec, x, W, None, mask)
+        want = ms.layer_backward(rec, gy)
+        other, here = torch.cuda.Stream(), torch.cuda.current_stream()
+        torch.cuda.synchronize()
+        with torch.cuda.stream(other):
+            _, rec = ms.layer_forward(spec, x, W, None, mask)
+        n = rec.saved[kept].untyped_storage().nbytes()
+        here.wait_stream(other)
+        torch.cuda._sleep(20_000_000)   # the backward begins well after it is enqueued
+        got = ms.layer_backward(rec, gy)
+        with torch.cuda.stream(other):
+            again = [torch.full((n,), 255, dtype=torch.uint8, device="cuda") for _ in range(4)]
+        torch.cuda.synchronize()
+        assert all(p is q or torch.equal(p, q) for p, q in zip(want, got)), kept
+        del again
