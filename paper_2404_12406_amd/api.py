@@ -323,7 +323,8 @@ class Record:
 
     def __init__(self, handle: ctypes.c_void_p, desc: _LayerDesc, x, W, b, y_shape, y_like, bits=None, extra=None):
         self._h = handle
-        self._desc = desc
+        self._block = isinstance(desc.spec, _BLOCKS)
+        self._desc = None if self._block else desc   # (a cross entropy's holds the targets)
         acct = MsAccount()
         check(_lib.load().ms_record_account(handle, ctypes.byref(acct)), "ms_record_account")
         self.mask = int(acct.mask)
@@ -341,7 +342,6 @@ class Record:
             self._keep.update(extra)
         self._x_meta = (tuple(x.shape), x.dtype, x.device, tuple(x.stride()))
         self._elementwise = isinstance(desc.spec, (ReLU, Dropout))
-        self._block = isinstance(desc.spec, _BLOCKS)
         self._w_meta = (tuple(W.shape), W.dtype) if W is not None else None
         self._b_meta = (tuple(b.shape), b.dtype) if b is not None else None
         self.y_shape = y_shape

@@ -57,3 +57,14 @@ def test_borrowed_memory_outlives_a_backward_on_another_stream(stream, spec):
         for t in (kept["x"], kept["W"], *kept["stats"], kept["projections"]):
             assert t.streams == want
         assert rec.consumed and not rec.saved
+
+
+def test_a_kept_gradient_holds_no_targets(stream):
+    """(8 bytes a row, and what they are a view of.)"""
+    import weakref
+    t = torch.zeros(4, dtype=torch.int64)
+    gone = weakref.ref(t)
+    spec = api.LinearCrossEntropy(t)
+    rec = api.Record(ctypes.c_void_p(1), api._BlockDesc(spec), torch.zeros(4, 8), torch.zeros(6, 8), None, (1,), t, extra={"grad": Tensor()})
+    del t, spec
+    assert gone() is None and "grad" in rec.saved
