@@ -101,8 +101,12 @@ class Dropout:
     offset: int = 0
 
 
+class _Block:
+    """A layer with a C entry point of its own."""
+
+
 @dataclass(frozen=True)
-class LayerNorm:
+class LayerNorm(_Block):
     """y = (x - mean) / sqrt(var + eps) * gamma + beta over the rows of x[M, D];
     W = gamma[D], b = beta[D], either may be None.  Its record keeps x (for
     the gradient of x or gamma) and no statistics: backward takes them again."""
@@ -110,7 +114,7 @@ class LayerNorm:
 
 
 @dataclass(frozen=True)
-class GatedLinear:
+class GatedLinear(_Block):
     """y = act(x Wg^T + bg) * (x Wu^T + bu) for x[M, D], W = [Wg; Wu][2F, D],
     b = [bg; bu][2F] or None; act is "silu", "gelu", "gelu_tanh", "relu" or
     "sigmoid".  Its record keeps, for any gradient, both projections
@@ -122,7 +126,7 @@ class GatedLinear:
 
 
 @dataclass
-class LinearCrossEntropy:
+class LinearCrossEntropy(_Block):
     """Softmax cross entropy of the logits x W^T + b for x[M, D], W[V, D], b[V]
     or None, without the logits: loss[1] (reduction "mean" over the rows whose
     target is not ignore_index, or "sum") or loss[M] ("none"), float32.
@@ -134,9 +138,6 @@ class LinearCrossEntropy:
     target: torch.Tensor
     ignore_index: int = -100
     reduction: str = "mean"
-
-
-_BLOCKS = (LayerNorm, GatedLinear, LinearCrossEntropy)   # layers with a C entry point of their own
 
 
 def _pair(v):
@@ -321,9 +322,10 @@ class Record:
     the tensors it borrows (so the caching allocator sees the same retained
     bytes as the ledger)."""
 
-    def __init__(self, handle: ctypes.c_void_p, desc: _LayerDesc, x, W, b, y_shape, y_like, bits=None, extra=None):
+    def __init__(self, handle: ctypes.c_void_p, desc: _LayerDesc, x, W, b, y_shape, y_like, bits=None, extra=None,
+                 stream: Optional[ctypes.c_void_p] = None):
         self._h = handle
-        self._block = isinstance(desc.spec, _BLOCKS)
+        self._block = type(desc) is _BlockDesc
         self._desc = None if self._block else desc   # (a cross entropy's holds the targets)
         acct = MsAccount()
         check(_lib.load().ms_record_account(handle, ctypes.byref(acct)), "ms_record_account")
@@ -346,7 +348,7 @@ class Record:
         self._b_meta = (tuple(b.shape), b.dtype) if b is not None else None
         self.y_shape = y_shape
         self.consumed = False
-        self._stream = _stream(x.device).value   # the forward's
+        self._stream = (_stream(x.device) if stream is None else stream).value   # the forward's
 
     @property
     def saved(self):
@@ -413,11 +415,11 @@ def relu_mask_buffer(x: torch.Tensor) -> torch.Tensor:
     return torch.empty((x.numel() + 31) // 32, dtype=torch.int32, device=x.device)
 
 
-def _relu_forward(lib, x, y, bits, mask):
+def _relu_forward(lib, x, y, bits, mask, stream=None):
     h = ctypes.c_void_p()
     st = lib.ms_relu_forward(_ptr(tensor_desc(x)), _ptr(tensor_desc(y)),
                              ctypes.c_void_p(bits.data_ptr() if bits is not None and bits.numel() else None),
-                             int(mask), ctypes.byref(h), _stream(x.device))
+                             int(mask), ctypes.byref(h), _stream(x.device) if stream is None else stream)
     check(st, "ms_relu_forward")
     return h
 
@@ -427,10 +429,10 @@ def dropout_blocks(numel: int) -> int:
     return int(_lib.load().ms_dropout_blocks(int(numel)))
 
 
-def _dropout_forward(lib, spec, x, y, mask):
+def _dropout_forward(lib, spec, x, y, mask, stream):
     h = ctypes.c_void_p()
     st = lib.ms_dropout_forward(_ptr(tensor_desc(x)), _ptr(tensor_desc(y)), float(spec.p), int(spec.seed),
-                                int(spec.offset), int(mask), ctypes.byref(h), _stream(x.device))
+                                int(spec.offset), int(mask), ctypes.byref(h), stream)
     check(st, "ms_dropout_forward")
     return h
 
@@ -563,15 +565,16 @@ def layer_forward(spec, x: torch.Tensor, W: Optional[torch.Tensor] = None, b: Op
     record is None when mask == 0 (nothing is saved).  A ReLU with the INPUT
     bit gets a fresh 1-bit mask buffer, owned by its record."""
     lib = _lib.load()
-    if isinstance(spec, _BLOCKS):
+    if isinstance(spec, _Block):
         y, name, args, kept, _alive = _block_call(spec, x, W, b, int(mask), y)
         h = ctypes.c_void_p()
-        status = _block_fn(name)(*args, ctypes.byref(h), _stream(x.device))
+        stream = _stream(x.device)
+        status = _block_fn(name)(*args, ctypes.byref(h), stream)
         if status:
             check(status, name)
         if not h.value:
             return y, None
-        return y, Record(h, _BlockDesc(spec), x, W, b, tuple(y.shape), y, extra=kept)
+        return y, Record(h, _BlockDesc(spec), x, W, b, tuple(y.shape), y, extra=kept, stream=stream)
     if isinstance(spec, ReLU):
         if W is not None or b is not None:
             raise TypeError("ReLU takes no W or b")
@@ -579,20 +582,22 @@ def layer_forward(spec, x: torch.Tensor, W: Optional[torch.Tensor] = None, b: Op
         if y is None:
             y = torch.empty_like(x)   # x's (dense) layout: the mask runs in memory order
         bits = relu_mask_buffer(x) if mask & MASK_INPUT else None
-        h = _relu_forward(lib, x, y, bits, mask)
+        stream = _stream(x.device)
+        h = _relu_forward(lib, x, y, bits, mask, stream)
         if not h.value:
             return y, None
-        return y, Record(h, _layer_desc(spec), x, None, None, tuple(y.shape), y, bits)
+        return y, Record(h, _layer_desc(spec), x, None, None, tuple(y.shape), y, bits, stream=stream)
     if isinstance(spec, Dropout):
         if W is not None or b is not None:
             raise TypeError("dropout takes no W or b")
         _on_gpu(x, y)
         if y is None:
             y = torch.empty_like(x)   # x's (dense) layout: the mask runs in memory order
-        h = _dropout_forward(lib, spec, x, y, mask)
+        stream = _stream(x.device)
+        h = _dropout_forward(lib, spec, x, y, mask, stream)
         if not h.value:
             return y, None
-        return y, Record(h, _LayerDesc(spec), x, None, None, tuple(y.shape), y)
+        return y, Record(h, _LayerDesc(spec), x, None, None, tuple(y.shape), y, stream=stream)
     desc = _layer_desc(spec)
     extra = (spec.running_mean, spec.running_var) if isinstance(spec, BatchNormEval) else ()
     _on_gpu(x, W, b, y, *extra)
@@ -600,12 +605,13 @@ def layer_forward(spec, x: torch.Tensor, W: Optional[torch.Tensor] = None, b: Op
         y = empty_like_layout(output_shape(spec, x, W), x)
     dx, dw, db, dy = tensor_desc(x), tensor_desc(W), tensor_desc(b), tensor_desc(y)
     h = ctypes.c_void_p()
+    stream = _stream(x.device)
     st = lib.ms_layer_forward(ctypes.byref(desc.layer), _ptr(dx), _ptr(dw), _ptr(db), int(mask), _ptr(dy),
-                              ctypes.byref(h), _stream(x.device))
+                              ctypes.byref(h), stream)
     check(st, "ms_layer_forward")
     if not h.value:
         return y, None
-    return y, Record(h, desc, x, W, b, tuple(y.shape), y)
+    return y, Record(h, desc, x, W, b, tuple(y.shape), y, stream=stream)
 
 
 def layer_backward(rec: Record, grad_y: torch.Tensor, grad_x: Optional[torch.Tensor] = None,
@@ -695,7 +701,7 @@ class PreparedLayer:
         _on_gpu(x, W, b, y, grad_y, grad_x, grad_W, grad_b, *extra)
         self.lib = _lib.load()
         self.block = None
-        if isinstance(spec, _BLOCKS):
+        if isinstance(spec, _Block):
             y, *self.block = _block_call(spec, x, W, b, int(mask), y)
         self.desc = _BlockDesc(spec) if self.block else _LayerDesc(spec)
         if y is None:

@@ -48,7 +48,7 @@ def test_borrowed_memory_outlives_a_backward_on_another_stream(stream, spec):
     x, W = torch.zeros(4, 8), torch.zeros(6, 8)
     for back, want in ((11, []), (22, [22])):
         stream(11)
-        block = isinstance(spec, api._BLOCKS)
+        block = not isinstance(spec, (api.Linear, api.ReLU))
         rec = api.Record(ctypes.c_void_p(1), api._BlockDesc(spec) if block else api._LayerDesc(spec), x, W, None, (4, 6), x)
         kept = {"x": Tensor(), "W": Tensor(), "stats": (Tensor(), Tensor()), "projections": Tensor()}
         rec._keep = dict(kept)
