@@ -180,7 +180,7 @@ __global__ __launch_bounds__(256) void gather_kernel(const int64_t *__restrict__
             if (ccount) ccount[k] = rows;
         }
     // (no row that counts: every result is an empty sum, whatever the factor)
-    if (others && blockIdx.x == 0 && threadIdx.x == 0)
+    if (scale && blockIdx.x == 0 && threadIdx.x == 0)   // (nothing is kept of no rows, which still have a factor)
         scale[M] = reduction == 2 || n == 0 ? 1.f : reduction == 1 ? gloss[0] : gloss[0] / (float)n;
     for (int64_t k = blockIdx.x; k < M; k += gridDim.x) {
         const int64_t i = SCAN ? at : k;

@@ -106,3 +106,17 @@ def test_backward_on_another_stream_than_the_forward():
         torch.cuda.synchronize()
         assert all(p is q or torch.equal(p, q) for p, q in zip(want, got)), kept
         del again
+
+
+@pytest.mark.parametrize("reduction", ["mean", "sum", "none"])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_cross_entropy_of_no_rows_whatever_the_workspace_holds(dtype, reduction):
+    """Gradients are zeros: nothing that an earlier call left in the workspace reaches them."""
+    make = lambda *s: torch.randn(*s).to(TORCH_DT[dtype]).cuda()
+    spec = ms.LinearCrossEntropy(torch.empty(0, dtype=torch.int64, device="cuda"), reduction=reduction)
+    for mask in (2, 3, 4, 6, 7):
+        _, rec = ms.layer_forward(ms.GatedLinear(), make(64, 40), make(96, 40), None, 1)
+        ms.layer_backward(rec, make(64, 48) * float("nan"))   # NaN from the workspace's beginning on
+        _, rec = ms.layer_forward(spec, make(0, 40), make(421, 40), make(421), mask)
+        grads = ms.layer_backward(rec, torch.ones(0 if reduction == "none" else 1, device="cuda"))
+        assert not any(g.any() for g in grads if g is not None and g.numel())
