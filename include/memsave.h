@@ -38,7 +38,9 @@
  *  - dtypes: MS_F32 or MS_BF16; all tensors of one call share one dtype (but a
  *    cross entropy's loss, which is MS_F32).
  *    Products are accumulated in fp32 and rounded once to the output dtype
- *    (round to nearest even).
+ *    (round to nearest even).  In bf16 the gradients of MS_GATED_LINEAR and
+ *    MS_CROSS_ENTROPY are products of a dz that is rounded to bf16 itself, and what
+ *    these two keep has 24 bits (see there).
  *  - Every tensor has fewer than 2^31 elements (MS_E_UNSUPPORTED otherwise).
  *  - All work is enqueued on the caller's stream (`stream` is a
  *    hipStream_t; NULL = the null stream); no call synchronises the device
@@ -334,7 +336,8 @@ uint64_t ms_gated_projection_bytes(int64_t rows, int64_t F, int32_t dtype);
  * kept and proj must be NULL.  x[M, D], W[2F, D], y[M, F]: any strides (y not
  * overlapping itself), D, F >= 1, M * 2F < 2^31 and, in bf16, M and 2F times D rounded up
  * to 8 at most 2^31 - 17 (MS_E_UNSUPPORTED otherwise); b[2F] contiguous or NULL.  z is
- * in fp32 until it is rounded into proj; y is rounded once, from fp32.  bf16 operands whose
+ * in fp32 until it is rounded into proj; y is rounded once, from fp32; dz is rounded to x's
+ * dtype, as an operand of dW and dx, and db is summed from that.  bf16 operands whose
  * D is no multiple of 8 run on zero-padded copies, and every backward on a dz in
  * transient workspace.  Backward is ms_layer_backward().  ms_layer_forward()
  * rejects MS_GATED_LINEAR (MS_E_ARG).
@@ -368,7 +371,8 @@ uint64_t ms_cross_entropy_kept_bytes(int64_t rows, int64_t D, int64_t V, int32_t
  * -- where ms_cross_entropy_kept_bytes() says more than a float a row -- the forward
  * takes dx too, but for g, a chunk of rows at a time in transient workspace of the
  * same size: two products instead of three.  The record then keeps that gradient and
- * neither x nor W nor the targets, and backward multiplies it by g.
+ * neither x nor W nor the targets, and backward multiplies it by g.  (That workspace is
+ * the forward's: ms_account.transient_workspace_bytes, the backward's, does not have it.)
  * target: M contiguous int64 on the device.  Rows whose target is ignore_index
  * take no part, whatever x holds in them: their loss and their row of dx are 0.
  * Any other target outside [0, V) makes its loss NaN, and the gradients that it
@@ -380,7 +384,8 @@ uint64_t ms_cross_entropy_kept_bytes(int64_t rows, int64_t D, int64_t V, int32_t
  * contiguous.  With mask != 0, kept is caller-allocated device memory of
  * ms_cross_entropy_kept_bytes(), 16-byte aligned, fully overwritten, and borrowed (l,
  * with x, W, b and target, which every gradient then needs); with mask 0
- * it may be NULL.  dz is rounded to x's dtype before its products, everything else is
+ * it may be NULL.  dz, or the exponentials it is taken from in the forward, are rounded to
+ * x's dtype before their products, a kept gradient in bf16 to 24 bits, everything else is
  * in fp32.  So is l: with logits of size Z a gradient taken from it is off by some
  * 2^-24 Z of itself for that alone (by all of it past some 10^7), as the logits' own
  * sums have it too; the loss and a gradient taken in the forward have the differences

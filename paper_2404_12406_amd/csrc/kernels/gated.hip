@@ -8,15 +8,15 @@
 // kernels below; so does a bf16 backward that kept z.  Those are bound by
 // memory: 16 bytes a thread and access, a row's last vector element by element.
 //
-// Measured, us: 8192 x 768 x 2 x 2048 bf16, trained: forward 78, dz from the kept
-// projections 34 (184 MB, 5.4 TB/s), dx 61 with W's transpose, dW 85 with the sum of
-// its partials.  4096 x 2048 x 2 x 5504, from the input alone: forward 169, dz 183,
-// dx 168 from W in place and 13 for the sum of its two partials.  1001 x 515 x 2 x
-// 1366 fp32, trained: z 35, dx 40, dW 42, everything else some 40 in eight launches.
+// Measured, us: 8192 x 768 x 2 x 2048 bf16, trained: forward 81, dz from the kept
+// projections 33 (184 MB, 5.5 TB/s), dx 60 with W's transpose, dW 84 with the sum of
+// its partials.  4096 x 2048 x 2 x 5504, from the input alone: forward 163, dz 175,
+// dx 158 from W in place and 13 for the sum of its two partials.  1001 x 515 x 2 x
+// 1366 fp32, trained: z 35, dx 40, dW 42, everything else 45 in eight launches.
 #include <algorithm>
 
 #include "block_math.h"
-#include "limits.h"
+#include "limits_f32.h"
 #include "../../../include/memsave.h"
 #include "../../../include/memsave_testing.h"
 

@@ -42,7 +42,7 @@
 
 #include "common.h"
 #include "lds_dma.h"
-#include "limits.h"
+#include "limits_f32.h"
 #include "../device.h"
 
 namespace ms {

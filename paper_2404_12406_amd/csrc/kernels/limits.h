@@ -20,8 +20,5 @@ constexpr bool operand_fits(int64_t elems) {
     return elems >= 0 && elems <= (int64_t)(kOOB / 2) - 8;
 }
 
-// The fp32 contractions' operands and outputs, likewise.
-constexpr int64_t kMostFloats = ((int64_t)kOOB - 16) / 4;
-
 }  // namespace g2
 }  // namespace ms

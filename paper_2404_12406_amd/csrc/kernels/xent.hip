@@ -30,14 +30,15 @@
 // any size overflows; what is kept of a row, and its lse, are in fp32.
 //
 // Measured, us.  8192 x 768 x 50000 bf16, a third of the rows ignored, head trained:
-// statistics 443, dz 542, dx 412, dW 433, everything else 80.  4096 x 4096 x 128000,
-// head frozen: exponentials 3645, dx 3428, the rest 120.  777 x 514 x 10007 fp32,
-// trained: z 79 (twice), dx 88, dW 83, the softmax's passes 23, W's padded copies 17.
+// statistics 414, dz 498, dx 397, dW 414, everything else 84.  4096 x 4096 x 128000,
+// head frozen: exponentials 3632, dx 3313, the rest 120.  777 x 514 x 10007 fp32,
+// trained: z 72 (twice), dx 81 and 7 for the sum of its partials, dW 75, the softmax's
+// passes 23, padded copies 25, eight small launches 42.
 #include <algorithm>
 #include <type_traits>
 
 #include "block_math.h"
-#include "limits.h"
+#include "limits_f32.h"
 #include "../../../include/memsave_testing.h"
 
 namespace ms {
@@ -787,6 +788,7 @@ int take_piece(Piece *q, int64_t M, int64_t D, int64_t D8, int64_t v0, int64_t n
 //   16 x 2048 x 2000   13 / 31, 19 / 44     4 x 768 x 50000   28 / 26, 47 / 47
 //   16 x 1024 x 10000  15 / 22, 22 / 33    16 x 768 x 50000   32 / 26, 51 / 47
 //                                           1 x 4096 x 100000 221 / 171, 250 / 232
+// (Between W of 20 and of 77 MB nothing was measured.)
 // fp32: 16 x 768 x 50000 50 / 90, 85 / 112; 16 x 2048 x 2000 19 / 27, 26 / 32.
 bool few_rows(int dtype, int64_t M, int64_t D, int64_t V, const void *x, const void *w) {
     return (dtype != kBF16 || V * D * 2 <= int64_t(64) << 20) && tok::applies(dtype, M, V, D, x, w);

@@ -43,13 +43,27 @@ def stream(monkeypatch):
     return lambda s: current.__setitem__(0, s)
 
 
+@pytest.fixture
+def record(stream):
+    """api.Record(...) of a handle that no library knows."""
+    made = []
+
+    def make(*args, **kw):
+        made.append(api.Record(ctypes.c_void_p(1), *args, **kw))
+        return made[-1]
+
+    yield make
+    for rec in made:
+        rec._h = None
+
+
 @pytest.mark.parametrize("spec", [api.GatedLinear(), api.Linear(), api.ReLU()], ids=["gated", "linear", "relu"])
-def test_borrowed_memory_outlives_a_backward_on_another_stream(stream, spec):
+def test_borrowed_memory_outlives_a_backward_on_another_stream(stream, record, spec):
     x, W = torch.zeros(4, 8), torch.zeros(6, 8)
     for back, want in ((11, []), (22, [22])):
         stream(11)
         block = not isinstance(spec, (api.Linear, api.ReLU))
-        rec = api.Record(ctypes.c_void_p(1), api._BlockDesc(spec) if block else api._LayerDesc(spec), x, W, None, (4, 6), x)
+        rec = record(api._BlockDesc(spec) if block else api._LayerDesc(spec), x, W, None, (4, 6), x)
         kept = {"x": Tensor(), "W": Tensor(), "stats": (Tensor(), Tensor()), "projections": Tensor()}
         rec._keep = dict(kept)
         stream(back)
@@ -59,12 +73,12 @@ def test_borrowed_memory_outlives_a_backward_on_another_stream(stream, spec):
         assert rec.consumed and not rec.saved
 
 
-def test_a_kept_gradient_holds_no_targets(stream):
+def test_a_kept_gradient_holds_no_targets(record):
     """(8 bytes a row, and what they are a view of.)"""
     import weakref
     t = torch.zeros(4, dtype=torch.int64)
     gone = weakref.ref(t)
     spec = api.LinearCrossEntropy(t)
-    rec = api.Record(ctypes.c_void_p(1), api._BlockDesc(spec), torch.zeros(4, 8), torch.zeros(6, 8), None, (1,), t, extra={"grad": Tensor()})
+    rec = record(api._BlockDesc(spec), torch.zeros(4, 8), torch.zeros(6, 8), None, (1,), t, extra={"grad": Tensor()})
     del t, spec
     assert gone() is None and "grad" in rec.saved
