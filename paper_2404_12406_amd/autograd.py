@@ -93,6 +93,16 @@ def _mask(ctx, ix: int, iw: Optional[int] = None, ib: Optional[int] = None) -> i
     return m
 
 
+def _take(ctx):
+    """The record, for the one backward that consumes it.  (Every Function that autograd
+    calls back has had one: without an input that requires a gradient it does not.)"""
+    rec, ctx.rec = ctx.rec, None
+    if rec is None:
+        raise RuntimeError("backward through a layer a second time: its record was consumed by the first "
+                           "(retain_graph does not keep it); run the forward again")
+    return rec
+
+
 class _LayerFn(torch.autograd.Function):
     """y = layer(x; W, b) through the C ABI; inputs (spec, x, W, b)."""
 
@@ -109,10 +119,7 @@ class _LayerFn(torch.autograd.Function):
 
     @staticmethod
     def backward(ctx, grad_y):
-        rec = ctx.rec
-        ctx.rec = None
-        if rec is None:
-            return None, None, None, None
+        rec = _take(ctx)
         _check_versions(ctx.versions)
         gy = grad_y if grad_y.dim() in (2, 4) else _cl(grad_y.contiguous() if grad_y.dim() < 4 else grad_y)
         gx, gw, gb = api.layer_backward(rec, gy)
@@ -130,10 +137,7 @@ class _ReLUFn(torch.autograd.Function):
 
     @staticmethod
     def backward(ctx, grad_y):
-        rec = ctx.rec
-        ctx.rec = None
-        if rec is None:
-            return None
+        rec = _take(ctx)
         gx, _, _ = api.layer_backward(rec, _as_layout_of(grad_y, ctx.stride))
         rec.free()
         return gx
@@ -149,10 +153,7 @@ class _DropoutFn(torch.autograd.Function):
 
     @staticmethod
     def backward(ctx, grad_y):
-        rec = ctx.rec
-        ctx.rec = None
-        if rec is None:
-            return None, None, None
+        rec = _take(ctx)
         gx, _, _ = api.layer_backward(rec, _as_layout_of(grad_y, ctx.stride))
         rec.free()
         return gx, None, None

@@ -65,3 +65,22 @@ def test_modules_run_in_inference_mode(name, masks):
     with torch.inference_mode():
         y = m(*inputs())
     assert not y.requires_grad and masks == [0]
+
+
+@pytest.mark.parametrize("name", MODULES)
+def test_a_second_backward_is_refused(name, masks, monkeypatch):
+    """The first consumes the record; a graph that is retained has no second gradient to give."""
+    def layer_backward(rec, gy, *buffers):
+        return tuple(torch.zeros_like(t) if t is not None else None for t in rec.grads)
+
+    make, inputs, _ = MODULES[name]
+    m, args = make(), inputs()
+    x = args[0].requires_grad_()
+    monkeypatch.setattr(api, "layer_backward", layer_backward)
+    shapes = (x.reshape(-1, x.shape[-1]) if x.dim() == 2 else x, getattr(m, "weight", None), getattr(m, "bias", None))
+    monkeypatch.setattr(Kept, "grads", shapes, raising=False)
+    loss = m(*args).sum()
+    loss.backward(retain_graph=True)
+    assert x.grad is not None
+    with pytest.raises(RuntimeError, match="second time"):
+        loss.backward()
