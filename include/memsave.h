@@ -34,14 +34,16 @@
  *    kinds) must be channels-last (NDHWC / KTRSC, torch.channels_last_3d);
  *    MS_RELU and MS_DROPOUT take x dense in any order of its dims with y and
  *    the gradients in x's strides; 1-D tensors (biases, BN statistics) are
- *    contiguous.  Anything else returns MS_E_LAYOUT.
+ *    contiguous.  3-D tensors (rows of heads, [T, H, D]) may have any non-negative
+ *    strides; a cache's pages are contiguous.  Anything else returns MS_E_LAYOUT.
  *  - dtypes: MS_F32 or MS_BF16; all tensors of one call share one dtype (but a
  *    cross entropy's loss, which is MS_F32).
  *    Products are accumulated in fp32 and rounded once to the output dtype
  *    (round to nearest even).  In bf16 the gradients of MS_GATED_LINEAR and
  *    MS_CROSS_ENTROPY are products of a dz that is rounded to bf16 itself, and what
  *    these two keep has 24 bits (see there).
- *  - Every tensor has fewer than 2^31 elements (MS_E_UNSUPPORTED otherwise).
+ *  - Every tensor but a cache's pages has fewer than 2^31 elements (MS_E_UNSUPPORTED
+ *    otherwise).
  *  - All work is enqueued on the caller's stream (`stream` is a
  *    hipStream_t; NULL = the null stream); no call synchronises the device
  *    except the first use of a larger transient workspace on a stream.
@@ -89,7 +91,7 @@ typedef enum { MS_F32 = 0, MS_BF16 = 1 } ms_dtype;
 typedef struct {
     void *data;
     int32_t dtype;       /* ms_dtype */
-    int32_t ndim;        /* 1, 2, 4 or 5 */
+    int32_t ndim;        /* 1 to 5 */
     int64_t shape[5];
     int64_t stride[5];   /* in elements */
 } ms_tensor;
@@ -139,9 +141,16 @@ typedef enum {
     MS_GATED_LINEAR = 10, /* y = act(x Wg^T + bg) * (x Wu^T + bu): x[M,D], W = [Wg; Wu][2F,D],
                             b = [bg; bu][2F] or NULL, y[M,F].  Forward through
                             ms_gated_linear_forward() only                                */
-    MS_CROSS_ENTROPY = 11 /* softmax cross entropy of the logits x W^T + b: x[M,D], W[V,D],
+    MS_CROSS_ENTROPY = 11, /* softmax cross entropy of the logits x W^T + b: x[M,D], W[V,D],
                             b[V] or NULL, loss[1] or loss[M] in fp32.  Forward through
                             ms_cross_entropy_forward() only                               */
+    MS_HEAD_NORM_ROTARY = 12, /* root-mean-square norm of each head of x[T,H,D] and its
+                            rotation by the row's position; W = scale of the first q_heads
+                            heads, b = scale of the others, each [D] or NULL.  Forward through
+                            ms_head_norm_rotary_forward() only                            */
+    MS_ATTENTION = 13    /* o = softmax(scale q k^T) v: x = q[Tq,Hq,D], W = k[Tk,Hk,D],
+                            b = v[Tk,Hk,D], y = o[Tq,Hq,D].  Forward through
+                            ms_attention_forward() only                                   */
 } ms_kind;
 
 /* Reductions of MS_CROSS_ENTROPY. */
@@ -179,10 +188,12 @@ typedef struct ms_record ms_record;
  * keeps.  MS_SAVED_PROJ: a gated linear unit's projections.  MS_SAVED_LSE: a
  * cross entropy's log-sum-exp of each row's words but the target (and its targets).
  * MS_SAVED_GRAD: its
- * input's gradient but for the loss's. */
+ * input's gradient but for the loss's.  MS_SAVED_B: the third tensor (an attention's v,
+ * the scale of the keys' heads); an attention's own output is MS_SAVED_Y, its rows'
+ * log-sum-exps MS_SAVED_LSE.  MS_SAVED_INDEX: positions and frequencies, or offsets. */
 enum { MS_SAVED_X = 1u, MS_SAVED_W = 2u, MS_SAVED_MEAN = 4u, MS_SAVED_VAR = 8u, MS_SAVED_BITS = 16u,
        MS_SAVED_Y = 32u, MS_SAVED_MASK8 = 64u, MS_SAVED_PROJ = 128u,
-       MS_SAVED_LSE = 256u, MS_SAVED_GRAD = 512u };
+       MS_SAVED_LSE = 256u, MS_SAVED_GRAD = 512u, MS_SAVED_B = 1024u, MS_SAVED_INDEX = 2048u };
 
 /* Bits of ms_account.kernels: what the record's backward will launch. */
 enum { MS_K_DGRAD = 1u, MS_K_WGRAD = 2u, MS_K_BGRAD = 4u };
@@ -396,6 +407,109 @@ uint64_t ms_cross_entropy_kept_bytes(int64_t rows, int64_t D, int64_t V, int32_t
 ms_status ms_cross_entropy_forward(const ms_tensor *x, const ms_tensor *W, const ms_tensor *b, const int64_t *target,
                                    int64_t ignore_index, int32_t reduction, void *kept, uint32_t mask, const ms_tensor *loss,
                                    ms_record **rec, void *stream);
+
+/*
+ * How heads are normed and turned.  Element pairs of the first rotary_dim elements of a
+ * head, (i, i + rotary_dim / 2) or, interleaved, (2 i, 2 i + 1), turn by the angle
+ * position * inv_freq[i], which is taken in 64 bits from the two as they are.
+ */
+typedef struct {
+    int64_t q_heads;            /* the first heads, with a scale of their own */
+    int32_t rotary_dim;         /* even, 0 (no rotation) to D */
+    int32_t interleaved;
+    int32_t norm;               /* 0: rotation alone, no scales */
+    float eps;                  /* finite, >= 0 */
+    const int32_t *positions;   /* [T] on the device; NULL without rotation */
+    const float *inv_freq;      /* [rotary_dim / 2] on the device */
+} ms_rotary;
+
+/*
+ * ms_head_norm_rotary_forward -- norms of queries and keys for each head and the rotation
+ * by their positions, in one pass:
+ *   r = 1 / sqrt(mean of a head's squares + eps),  z = x r gamma,
+ *   y_i = z_i cos a - z_j sin a,  y_j = z_j cos a + z_i sin a.
+ * The rotation is linear and needs nothing but the positions; the norm is linear in its
+ * scale alone.  With dz the gradient of z (that of y turned back), q = dz gamma:
+ *   dx = r (q - x r^2 mean(q x)),  dgamma = sum over rows and heads of dz x r.
+ * So a record borrows the positions and frequencies, with a norm x, and for INPUT the
+ * scales; no statistics.  Mask bits: INPUT x, WEIGHT gamma_q, BIAS gamma_k.
+ * x, y: [T, H, D], 1 <= D <= 256 (MS_E_UNSUPPORTED otherwise), any strides (y not
+ * overlapping itself); y may be x itself where the record does not borrow it (MS_E_ARG
+ * otherwise).
+ * gamma_q, gamma_k: [D] contiguous or NULL (ones).  Statistics, angles and sums are in 32
+ * bits or more.  Backward is ms_layer_backward().  ms_layer_forward() rejects
+ * MS_HEAD_NORM_ROTARY (MS_E_ARG).
+ */
+ms_status ms_head_norm_rotary_forward(const ms_tensor *x, const ms_tensor *gamma_q, const ms_tensor *gamma_k,
+                                      const ms_rotary *rotary, uint32_t mask, const ms_tensor *y, ms_record **rec,
+                                      void *stream);
+
+/*
+ * ms_attention_kept_bytes -- size of what ms_attention_forward() leaves in `kept`: a float
+ * for each query row and head.  0 with mask 0 or an extent that is not positive.
+ */
+uint64_t ms_attention_kept_bytes(int64_t rows, int64_t heads, uint32_t mask);
+
+/*
+ * ms_attention_forward -- attention over whole prompts: in each sequence and head
+ *   o_i = sum over visible j of P_ij v_j,  P = softmax over j of scale q_i k_j.
+ * Hq / Hk query heads share a head of k and v (Hk divides Hq).  Packed sequences:
+ * q_offsets[sequences + 1], on the device, not falling: sequence b has the rows
+ * q_offsets[b] to q_offsets[b + 1] - 1 of q and o, and those between k_offsets[b] and
+ * k_offsets[b + 1] of k and v (k_offsets NULL: the same).  q_offsets NULL: one sequence, all
+ * rows (sequences is not read).  Rows of no sequence get zeros, in o and in the gradients, as
+ * do rows that see no key.  Offsets outside the rows are taken as their bounds; where they fall,
+ * what the rows concerned hold is undefined.
+ * causal: with m queries and n keys, query i sees the keys to i + n - m, so that the last one
+ * sees all.  What is hidden takes no part, whatever it holds; a row whose visible scores
+ * have NaN or plus infinity among them, or minus infinity alone, is NaN.
+ * Scores and probabilities exist a tile at a time.  The output is linear in v and not in q or
+ * k:  dv = P^T g;  dP = g v^T,  dS = P (dP - sum g o),  dq = scale dS k,  dk = scale dS^T q.
+ * Mask bits: INPUT q, WEIGHT k, BIAS v.  A record borrows q, k and `kept` (a row's log-sum-exp;
+ * caller-allocated device memory of ms_attention_kept_bytes(), fully overwritten) and, for q's or
+ * k's gradient, v and o; the offsets too.  Backward takes P again and computes what its gradients
+ * need: dv alone two products, dq or dk three each, of which the first two are shared by dk and dv.
+ * With mask 0 kept may be NULL.  q, o: [Tq, Hq, D], k, v: [Tk, Hk, D], 1 <= D <= 256
+ * (MS_E_UNSUPPORTED otherwise), any strides (o not overlapping itself); rows that are no whole
+ * aligned 16-byte vectors are staged.  scale: finite, > 0 (MS_E_ARG otherwise).  Sums and statistics are in fp32;
+ * in bf16 P and dS are rounded to bf16 as operands of their products.  Backward is
+ * ms_layer_backward(); ms_layer_forward() rejects MS_ATTENTION (MS_E_ARG).
+ */
+ms_status ms_attention_forward(const ms_tensor *q, const ms_tensor *k, const ms_tensor *v, const int32_t *q_offsets,
+                               const int32_t *k_offsets, int64_t sequences, int32_t causal, float scale, void *kept,
+                               uint32_t mask, const ms_tensor *o, ms_record **rec, void *stream);
+
+/*
+ * ms_cache_append -- keys and values of T tokens into a paged cache, normed and turned on
+ * the way, and the queries beside them, in one pass.
+ * x: [T, q_heads + 2 Hk, D], the heads of queries, keys and values in this order, any strides.
+ * Queries and keys go through ms_head_norm_rotary_forward()'s formulas (gamma_q, gamma_k,
+ * rotary as there; rotary_dim 0 and norm 0: as they are), the queries into q[T, q_heads, D]
+ * (NULL where q_heads is 0); keys and values into k_pages and v_pages [pages, Hk, page, D],
+ * contiguous, of any number of elements (fewer than 2^32 rows): token t at place
+ * positions[t] of sequence rows[t] (t where rows is NULL), which is row p % page of page
+ * tables[sequence][p / page], p the position.  tables: [sequences, width] on the
+ * device.  A token whose position, sequence or page lies outside is not written to the cache
+ * (a negative position marks padding); its query is.  Two tokens of one place: each
+ * 16 bytes of it are one of the two's.  There is no record: the cache is no function of x alone.
+ */
+ms_status ms_cache_append(const ms_tensor *x, const ms_tensor *gamma_q, const ms_tensor *gamma_k, const ms_rotary *rotary,
+                          const ms_tensor *k_pages, const ms_tensor *v_pages, const int32_t *tables, int64_t sequences,
+                          int64_t width, const int32_t *rows, const ms_tensor *q, void *stream);
+
+/*
+ * ms_paged_attention_forward -- attention of one query a sequence over its cache:
+ * o[b] = softmax(scale q[b] k^T) v over the first lengths[b] places of tables[b] (the
+ * query's own among them, if it has been appended).  q, o: [sequences, Hq, D], any strides;
+ * k_pages, v_pages, tables, width as ms_cache_append()'s; Hk divides Hq.  A length of 0 or
+ * less gives zeros; one past width * page, or a used page outside the cache, NaN.  What lies in
+ * the cache past the length takes no part.  A sequence's keys are divided over blocks and their
+ * sums joined in a fixed order, in transient workspace.  Sums and statistics are in fp32; in
+ * bf16 probabilities are rounded to bf16 as an operand.
+ */
+ms_status ms_paged_attention_forward(const ms_tensor *q, const ms_tensor *k_pages, const ms_tensor *v_pages,
+                                     const int32_t *tables, int64_t sequences, int64_t width, const int32_t *lengths,
+                                     float scale, const ms_tensor *o, void *stream);
 
 /*
  * ms_layer_backward -- write exactly the requested gradients for grad_y.

@@ -14,7 +14,7 @@ MS_RG_INPUT, MS_RG_WEIGHT, MS_RG_BIAS = 1, 2, 4
 MS_F32, MS_BF16 = 0, 1
 MS_CONV2D, MS_LINEAR, MS_BN_EVAL, MS_AVGPOOL, MS_RELU, MS_CONV_TRANSPOSE2D, MS_DROPOUT = 0, 1, 2, 3, 4, 5, 6
 MS_CONV3D, MS_CONV_TRANSPOSE3D, MS_LAYER_NORM = 7, 8, 9
-MS_GATED_LINEAR, MS_CROSS_ENTROPY = 10, 11
+MS_GATED_LINEAR, MS_CROSS_ENTROPY, MS_HEAD_NORM_ROTARY, MS_ATTENTION = 10, 11, 12, 13
 MS_ACT = {"silu": 0, "gelu": 1, "gelu_tanh": 2, "relu": 3, "sigmoid": 4}
 MS_REDUCE = {"mean": 0, "sum": 1, "none": 2}
 MS_SAVED_X, MS_SAVED_W, MS_SAVED_MEAN, MS_SAVED_VAR, MS_SAVED_BITS, MS_SAVED_Y, MS_SAVED_MASK8 = 1, 2, 4, 8, 16, 32, 64
@@ -32,6 +32,8 @@ EXPORTS = (
     "ms_testing_cross_entropy_plan",
     "ms_layer_norm_forward", "ms_gated_linear_forward", "ms_gated_projection_bytes", "ms_cross_entropy_forward",
     "ms_cross_entropy_kept_bytes",
+    "ms_head_norm_rotary_forward", "ms_attention_forward", "ms_attention_kept_bytes", "ms_cache_append",
+    "ms_paged_attention_forward",
 )
 MS_PROF_FWD, MS_PROF_DGRAD, MS_PROF_WGRAD, MS_PROF_BN, MS_PROF_ACT, MS_PROF_RED = 1, 2, 4, 8, 16, 32
 
@@ -57,7 +59,14 @@ class MsAccount(ctypes.Structure):
         return {f[0]: int(getattr(self, f[0])) for f in self._fields_ if f[0] != "reserved"}
 
 
+class MsRotary(ctypes.Structure):
+    _fields_ = [("q_heads", ctypes.c_int64), ("rotary_dim", ctypes.c_int32), ("interleaved", ctypes.c_int32),
+                ("norm", ctypes.c_int32), ("eps", ctypes.c_float), ("positions", ctypes.c_void_p),
+                ("inv_freq", ctypes.c_void_p)]
+
+
 _T = ctypes.POINTER(MsTensor)
+_R = ctypes.POINTER(MsRotary)
 _lib = None
 
 
@@ -132,6 +141,18 @@ def configure(lib: ctypes.CDLL) -> ctypes.CDLL:
         lib.ms_gated_projection_bytes.restype = ctypes.c_uint64
         lib.ms_cross_entropy_kept_bytes.argtypes = [ctypes.c_int64, ctypes.c_int64, ctypes.c_int64, ctypes.c_int32, ctypes.c_uint32]
         lib.ms_cross_entropy_kept_bytes.restype = ctypes.c_uint64
+    if hasattr(lib, "ms_attention_forward"):
+        rec, ptr, i64 = ctypes.POINTER(ctypes.c_void_p), ctypes.c_void_p, ctypes.c_int64
+        lib.ms_head_norm_rotary_forward.argtypes = [_T, _T, _T, _R, ctypes.c_uint32, _T, rec, ptr]
+        lib.ms_head_norm_rotary_forward.restype = ctypes.c_int
+        lib.ms_attention_kept_bytes.argtypes = [i64, i64, ctypes.c_uint32]
+        lib.ms_attention_kept_bytes.restype = ctypes.c_uint64
+        lib.ms_attention_forward.argtypes = [_T, _T, _T, ptr, ptr, i64, ctypes.c_int32, ctypes.c_float, ptr, ctypes.c_uint32, _T, rec, ptr]
+        lib.ms_attention_forward.restype = ctypes.c_int
+        lib.ms_cache_append.argtypes = [_T, _T, _T, _R, _T, _T, ptr, i64, i64, ptr, _T, ptr]
+        lib.ms_cache_append.restype = ctypes.c_int
+        lib.ms_paged_attention_forward.argtypes = [_T, _T, _T, ptr, i64, i64, ptr, ctypes.c_float, _T, ptr]
+        lib.ms_paged_attention_forward.restype = ctypes.c_int
     if hasattr(lib, "ms_testing_gated_plan"):
         lib.ms_testing_gated_plan.argtypes = [ctypes.c_int32, ctypes.c_int64, ctypes.c_int64, ctypes.c_int64, ctypes.c_int32,
                                               ctypes.c_int32, ctypes.c_uint32, ctypes.POINTER(ctypes.c_int64)]

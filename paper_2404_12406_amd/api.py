@@ -11,7 +11,8 @@ activations and conv weights and row-major matrices are used in place, any
 other layout (NCHW, slices, transposed views) is staged by the library
 through transient workspace.  5-D tensors must be channels-last-3d, 1-D
 tensors contiguous; ReLU and dropout take any dense layout, with gradients
-in the layout of x.  dtypes float32 or bfloat16.
+in the layout of x.  3-D tensors (rows of heads) may have any strides, a cache's
+pages are contiguous.  dtypes float32 or bfloat16.
 """
 from __future__ import annotations
 
@@ -138,6 +139,76 @@ class LinearCrossEntropy(_Block):
     target: torch.Tensor
     ignore_index: int = -100
     reduction: str = "mean"
+
+
+@dataclass
+class HeadNormRotary(_Block):
+    """Norms of queries and keys for each head, and their rotation by the position, in one
+    pass: each head of x[T, H, D] divided by its root mean square, times W[D] (the first
+    q_heads heads) or b[D] (the others; either may be None: ones); then its first
+    2 len(inv_freq) elements turned in pairs, (i, i + len(inv_freq)) or, interleaved,
+    (2 i, 2 i + 1), by positions[t] * inv_freq[i] (int32 [T]; float32, see
+    rotary_frequencies(); None: no rotation).  norm=False: rotation alone, no W and b.
+    Its record keeps the positions and, with a norm, x; no statistics."""
+    positions: Optional[torch.Tensor] = None
+    inv_freq: Optional[torch.Tensor] = None
+    q_heads: int = 0
+    norm: bool = True
+    eps: float = 1e-6
+    interleaved: bool = False
+
+
+@dataclass
+class Attention(_Block):
+    """o = softmax(scale q k^T) v for x = q[Tq, Hq, D], W = k and b = v[Tk, Hk, D], Hq / Hk
+    query heads to a head of k and v.  offsets: int32 [n + 1], where each of n packed
+    sequences begins in q and where the last one ends, k_offsets the same in k and v (None: as
+    offsets); None: one sequence.  Rows of no sequence are 0.  causal: the last query sees
+    every key, the one before it all but one.  scale: 1 / sqrt(D) where None.
+    The mask's bits ask for the gradients of q, k and v; the record keeps q, k and a number
+    a row and head, and v and o unless v's gradient is the only one."""
+    offsets: Optional[torch.Tensor] = None
+    k_offsets: Optional[torch.Tensor] = None
+    causal: bool = True
+    scale: Optional[float] = None
+
+
+@dataclass
+class CacheAppend(_Block):
+    """Keys and values of x[T, q_heads + 2 Hk, D] into a paged cache k_pages, v_pages
+    [pages, Hk, page, D], queries and keys through HeadNormRotary's formulas on the way (W
+    and b their scales); the output is the queries [T, q_heads, D].  Token t goes to place
+    positions[t] (int32 [T]) of sequence rows[t] (int32 [T], None: t), whose pages
+    tables[sequence] (int32 [sequences, width]) lists.  A token whose place does not exist
+    (a negative position, a page outside the cache) is not written.  No gradients."""
+    k_pages: torch.Tensor
+    v_pages: torch.Tensor
+    tables: torch.Tensor
+    positions: torch.Tensor
+    rows: Optional[torch.Tensor] = None
+    inv_freq: Optional[torch.Tensor] = None
+    q_heads: int = 0
+    norm: bool = True
+    eps: float = 1e-6
+    interleaved: bool = False
+
+
+@dataclass
+class PagedAttention(_Block):
+    """o = softmax(scale q k^T) v for one query a sequence, x = q[n, Hq, D], over the first
+    lengths[b] (int32 [n]) places of the cache that tables[b] lists (see CacheAppend).  A
+    length of 0 gives 0; one past the table, or a page outside the cache, NaN.  No
+    gradients."""
+    k_pages: torch.Tensor
+    v_pages: torch.Tensor
+    tables: torch.Tensor
+    lengths: torch.Tensor
+    scale: Optional[float] = None
+
+
+def rotary_frequencies(dim: int, theta: float = 10000.0, device=None) -> torch.Tensor:
+    """theta ** (-2 i / dim) for i < dim / 2, float32: inv_freq of dim turned elements."""
+    return torch.tensor([theta ** (-2.0 * i / dim) for i in range(dim // 2)], dtype=torch.float32, device=device)
 
 
 def _pair(v):
@@ -298,7 +369,9 @@ def output_shape(spec, x: torch.Tensor, W: Optional[torch.Tensor]):
         return tuple(x.shape)
     if isinstance(spec, AvgPool):
         return (x.shape[0], x.shape[1])
-    if isinstance(spec, (ReLU, Dropout, LayerNorm)):
+    if isinstance(spec, CacheAppend):
+        return (x.shape[0], spec.q_heads, x.shape[2])
+    if isinstance(spec, (ReLU, Dropout, LayerNorm, HeadNormRotary, Attention, PagedAttention)):
         return tuple(x.shape)
     raise TypeError(spec)
 
@@ -452,7 +525,44 @@ def _packed(t: Optional[torch.Tensor]) -> Optional[bytes]:
         return _TENSOR.pack(t.data_ptr(), dt, 2, shape[0], shape[1], 0, 0, 0, stride[0], stride[1], 0, 0, 0)
     if len(shape) == 1:
         return _TENSOR.pack(t.data_ptr(), dt, 1, shape[0], 0, 0, 0, 0, stride[0], 0, 0, 0, 0)
+    if len(shape) == 3:
+        return _TENSOR.pack(t.data_ptr(), dt, 3, *shape, 0, 0, *stride, 0, 0)
+    if len(shape) == 4:
+        return _TENSOR.pack(t.data_ptr(), dt, 4, *shape, 0, *stride, 0)
     return bytes(tensor_desc(t))
+
+
+_ROTARY = struct.Struct("qiiifPP")
+assert _ROTARY.size == ctypes.sizeof(_lib.MsRotary)
+
+
+def _index(name: str, t: Optional[torch.Tensor], like: torch.Tensor, shape=None) -> Optional[int]:
+    """The address of an int32 tensor on like's device, contiguous, of this shape; None
+    where it is None or holds nothing."""
+    if t is None:
+        return None
+    if t.dtype != torch.int32:
+        raise TypeError(f"{name} must be int32, got {t.dtype}")
+    if shape is not None and tuple(t.shape) != shape:
+        raise ValueError(f"{name} must be {list(shape)}; got {list(t.shape)}")
+    if not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous")
+    _one_gpu(like, t)
+    return t.data_ptr() or None
+
+
+def _rotary(spec, x) -> bytes:
+    """The bytes of spec's MsRotary."""
+    f, pos = spec.inv_freq, _index("positions", spec.positions, x, (x.shape[0],))
+    if f is not None:
+        if f.dtype != torch.float32 or f.dim() != 1 or not f.is_contiguous():
+            raise TypeError("inv_freq must be a contiguous vector of float32")
+        if spec.positions is None and f.shape[0]:
+            raise ValueError("inv_freq without positions")
+        _one_gpu(x, f)
+    turned = 2 * f.shape[0] if f is not None else 0
+    return _ROTARY.pack(int(spec.q_heads), turned, 1 if spec.interleaved else 0, 1 if spec.norm else 0, spec.eps, pos or 0,
+                        f.data_ptr() if turned else 0)
 
 
 _block_fns = {}
@@ -466,7 +576,7 @@ def _block_fn(name: str):
         f = lib[name]
         args = []
         for a in getattr(lib, name).argtypes:
-            args.append(ctypes.c_void_p if a in (_lib._T, ctypes.POINTER(ctypes.c_void_p)) else a)
+            args.append(ctypes.c_void_p if a in (_lib._T, _lib._R, ctypes.POINTER(ctypes.c_void_p)) else a)
         f.argtypes, f.restype = args, ctypes.c_int
         _block_fns[name] = f
     return f
@@ -489,6 +599,8 @@ def _block_call(spec, x, W, b, mask, y):
     """The forward call of a block layer: (y, C function's name, its arguments up
     to the record, what the record borrows besides x and W by name, what else has
     to live until the call)."""
+    if isinstance(spec, _HEADS):
+        return _heads_call(spec, x, W, b, mask, y)
     if x.dim() != 2:
         raise ValueError(f"{type(spec).__name__} takes x[M, D]; got {x.dim()} dims")
     _one_gpu(x, W, b, y)
@@ -543,6 +655,84 @@ def _block_call(spec, x, W, b, mask, y):
     return y, "ms_cross_entropy_forward", args, kept, t
 
 
+_HEADS = (HeadNormRotary, Attention, CacheAppend, PagedAttention)
+# Entry points of which nothing can be differentiated: they make no record.
+_NO_RECORD = frozenset(("ms_cache_append", "ms_paged_attention_forward"))
+
+
+def _heads_call(spec, x, W, b, mask, y):
+    """_block_call for the layers whose rows are heads, x[T, H, D]."""
+    if x.dim() != 3:
+        raise ValueError(f"{type(spec).__name__} takes rows of heads, [T, H, D]; got {x.dim()} dims")
+    _one_gpu(x, W, b, y)
+    if isinstance(spec, HeadNormRotary):
+        rot = _rotary(spec, x)
+        if y is None:
+            y = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+        kept = {}
+        if mask:
+            if spec.inv_freq is not None:
+                kept["positions"], kept["inv_freq"] = spec.positions, spec.inv_freq
+            if mask & MASK_INPUT and b is not None:
+                kept["b"] = b
+        return y, "ms_head_norm_rotary_forward", (_packed(x), _packed(W), _packed(b), rot, mask, _packed(y)), kept, None
+    D = x.shape[2]
+    if isinstance(spec, Attention):
+        if W is None or b is None or W.dim() != 3 or b.dim() != 3:
+            raise TypeError("Attention needs W = k and b = v, [Tk, Hk, D]")
+        off, k_off = spec.offsets, spec.k_offsets
+        if off is None and k_off is not None:
+            raise ValueError("k_offsets without offsets")
+        n = 0
+        if off is not None:
+            if off.dim() != 1 or off.shape[0] < 1:
+                raise ValueError("offsets must be [sequences + 1]")
+            n = off.shape[0] - 1
+        if y is None:
+            y = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+        kept, buf = {}, None
+        if mask:
+            buf = kept["lse"] = torch.empty((x.shape[1], x.shape[0]), dtype=torch.float32, device=x.device)
+            if off is not None:
+                kept["offsets"] = (off, k_off)
+            if mask & (MASK_INPUT | MASK_WEIGHT):
+                # (the output without its history, which would hold this record)
+                kept["v"], kept["o"] = b, y.detach()
+        args = (_packed(x), _packed(W), _packed(b), _index("offsets", off, x), _index("k_offsets", k_off, x, (n + 1,)), n,
+                1 if spec.causal else 0, D ** -0.5 if spec.scale is None and D else spec.scale or 0.0,
+                (buf.data_ptr() or None) if buf is not None else None, mask, _packed(y))
+        return y, "ms_attention_forward", args, kept, None
+    if mask:
+        raise ValueError(f"{type(spec).__name__} has no gradients: mask must be 0")
+    kp, vp, tab = spec.k_pages, spec.v_pages, spec.tables
+    _one_gpu(x, kp, vp)
+    if kp.dim() != 4 or vp.dim() != 4:
+        raise ValueError("a cache's pages are [pages, Hk, page, D]")
+    if tab.dim() != 2:
+        raise ValueError("tables must be [sequences, width]")
+    tables = (_index("tables", tab, x), tab.shape[0], tab.shape[1])
+    if isinstance(spec, CacheAppend):
+        if spec.positions is None:
+            raise ValueError("CacheAppend needs positions")
+        rot = _rotary(spec, x)
+        if y is None:
+            y = torch.empty((x.shape[0], spec.q_heads, D), dtype=x.dtype, device=x.device)
+        args = (_packed(x), _packed(W), _packed(b), rot, _packed(kp), _packed(vp), *tables, _index("rows", spec.rows, x, (x.shape[0],)),
+                _packed(y))
+        return y, "ms_cache_append", args, None, None
+    if W is not None or b is not None:
+        raise TypeError("PagedAttention takes no W or b")
+    if y is None:
+        y = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+    args = (_packed(x), _packed(kp), _packed(vp), *tables, _index("lengths", spec.lengths, x, (x.shape[0],)),
+            D ** -0.5 if spec.scale is None and D else spec.scale or 0.0, _packed(y))
+    return y, "ms_paged_attention_forward", args, None, None
+
+
+def _block_run(name, args, handle, stream):
+    return _block_fn(name)(*args, stream) if name in _NO_RECORD else _block_fn(name)(*args, handle, stream)
+
+
 def _block_backward(rec, grad_y, grad_x, grad_W, grad_b):
     """layer_backward for a block layer's record."""
     _one_gpu(grad_y, grad_x, grad_W, grad_b)
@@ -569,7 +759,7 @@ def layer_forward(spec, x: torch.Tensor, W: Optional[torch.Tensor] = None, b: Op
         y, name, args, kept, _alive = _block_call(spec, x, W, b, int(mask), y)
         h = ctypes.c_void_p()
         stream = _stream(x.device)
-        status = _block_fn(name)(*args, ctypes.byref(h), stream)
+        status = _block_run(name, args, ctypes.byref(h), stream)
         if status:
             check(status, name)
         if not h.value:
@@ -728,7 +918,7 @@ class PreparedLayer:
             self._h.value = None
         if self.block:
             name, args = self.block[:2]
-            check(_block_fn(name)(*args, self._hp, self._stream), name)
+            check(_block_run(name, args, self._hp, self._stream), name)
             return
         if self.relu:
             bits = ctypes.c_void_p(self.bits.data_ptr() if self.bits is not None and self.bits.numel() else None)

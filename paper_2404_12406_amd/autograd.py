@@ -35,7 +35,7 @@ from .api import MASK_BIAS, MASK_INPUT, MASK_WEIGHT
 
 __all__ = ["MSConv2d", "MSConvTranspose2d", "MSConv1d", "MSConvTranspose1d", "MSConv3d", "MSConvTranspose3d",
            "MSLinear", "MSBatchNorm2dEval", "MSReLU", "MSDropout", "MSLayerNorm", "MSGatedLinear", "MSLinearCrossEntropy",
-           "convert"]
+           "MSHeadNormRotary", "MSAttention", "convert"]
 
 
 def _cl(t: Optional[torch.Tensor]) -> Optional[torch.Tensor]:
@@ -121,7 +121,7 @@ class _LayerFn(torch.autograd.Function):
     def backward(ctx, grad_y):
         rec = _take(ctx)
         _check_versions(ctx.versions)
-        gy = grad_y if grad_y.dim() in (2, 4) else _cl(grad_y.contiguous() if grad_y.dim() < 4 else grad_y)
+        gy = grad_y if grad_y.dim() in (2, 3, 4) else _cl(grad_y.contiguous() if grad_y.dim() < 4 else grad_y)
         gx, gw, gb = api.layer_backward(rec, gy)
         rec.free()
         return None, gx, gw, gb
@@ -391,6 +391,39 @@ class MSLinearCrossEntropy(nn.Module):
         spec = api.LinearCrossEntropy(target.reshape(-1), self.ignore_index, self.reduction)
         loss = _layer(spec, x.reshape(-1, x.shape[-1]), self.weight, self.bias)
         return loss.reshape(target.shape if self.reduction == "none" else ())
+
+
+class MSHeadNormRotary(nn.Module):
+    """Norms of queries and keys for each head, with the rotation by position in the same
+    pass (see api.HeadNormRotary): forward(x, positions) for x[T, H, D], the first q_heads of
+    its heads scaled by weight_q[D], the others by weight_k[D] (None: ones).  Keeps x and
+    the positions alone; norm=False (no weights) the positions."""
+
+    def __init__(self, weight_q: Optional[torch.Tensor], weight_k: Optional[torch.Tensor], q_heads: int,
+                 inv_freq: Optional[torch.Tensor] = None, eps: float = 1e-6, interleaved: bool = False, norm: bool = True):
+        super().__init__()
+        self.weight_q = weight_q if (weight_q is None or isinstance(weight_q, nn.Parameter)) else nn.Parameter(weight_q)
+        self.weight_k = weight_k if (weight_k is None or isinstance(weight_k, nn.Parameter)) else nn.Parameter(weight_k)
+        self.register_buffer("inv_freq", inv_freq, persistent=False)
+        self.q_heads, self.eps, self.interleaved, self.norm = int(q_heads), float(eps), bool(interleaved), bool(norm)
+
+    def forward(self, x, positions=None):
+        freq = self.inv_freq if positions is not None else None
+        spec = api.HeadNormRotary(positions, freq, self.q_heads, self.norm, self.eps, self.interleaved)
+        return _layer(spec, x, self.weight_q, self.weight_k)
+
+
+class MSAttention(nn.Module):
+    """Attention over whole prompts (see api.Attention): forward(q, k, v, offsets) for
+    q[Tq, Hq, D] and k, v[Tk, Hk, D] of packed sequences.  Each of the three is
+    differentiated where it requires a gradient, and kept where one of these needs it."""
+
+    def __init__(self, causal: bool = True, scale: Optional[float] = None):
+        super().__init__()
+        self.causal, self.scale = bool(causal), scale
+
+    def forward(self, q, k, v, offsets=None, k_offsets=None):
+        return _layer(api.Attention(offsets, k_offsets, self.causal, self.scale), q, k, v)
 
 
 def _convertible_conv(m) -> bool:

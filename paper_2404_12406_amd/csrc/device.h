@@ -207,6 +207,81 @@ int launch_xent_bwd(int dtype, int64_t M, int64_t D, int64_t V, const void *x, c
                     void *db, void *ws, void *stream);
 int launch_xent_scale(int dtype, int64_t M, int64_t D, const void *kept, const float *gloss, int reduction, void *dx, void *stream);
 
+// Head norms with rotation of x[T][Hq + Hk][D] into y (strides of tokens and heads;
+// elements side by side), R elements of each head turned, in pairs (k, k + R/2) or, with `next`,
+// (2k, 2k + 1); norm: 0 rotation alone, else gq, gk [D] (may be null: ones).  Appending:
+// x has Hk heads more, the values; y takes the queries, and keys and values go to
+// pages [pages][Hk][page][D] at the position of each token in sequence rows[t] (t where
+// null) of tables[nseq][width]; a token without a place is not written.
+struct RotaryArgs {
+    const void *x;
+    int64_t xts, xhs;
+    void *y;
+    int64_t yts, yhs;
+    const void *gq, *gk;
+    const int32_t *pos;
+    const float *freq;
+    int64_t T;
+    int Hq, Hk, D, R, next, norm;
+    float eps;
+    void *kp, *vp;
+    const int32_t *tables, *rows;
+    int64_t nseq, pages;
+    int width, page;
+};
+int launch_rotary_fwd(int dtype, const RotaryArgs &a, bool append, void *stream);
+// The gradients for dy (strides dstride): dx (gstride), dgq, dgk, any may be null.  x is
+// read with norm alone; params: of dgq or dgk.
+size_t rotary_bwd_workspace(int dtype, const RotaryArgs &a, bool params);
+int launch_rotary_bwd(int dtype, const RotaryArgs &a, const void *dy, const int64_t dstride[2], void *dx, const int64_t gstride[2],
+                      void *dgq, void *dgk, void *ws, void *stream);
+
+// A tensor [rows][heads][D] as the attention kernels read and write it: elements side by
+// side, both strides, the pointer and D in whole 16-byte vectors.
+struct HeadsView {
+    void *p;
+    int64_t ts, hs;   // elements between rows, heads
+};
+// Attention of Tq query rows over Tk key rows in n sequences (offsets null: one):
+// o = softmax(scale q k^T) v, Hq / Hk query heads to a head of k and v; causal: the last
+// query of a sequence sees all of its keys.  lse[Hq][Tq] (may be null in the forward): the
+// log-sum-exp in base 2 of each row's scaled scores, +infinity where it sees no key.
+struct AttnArgs {
+    HeadsView q, k, v, o, go, dq, dk, dv;
+    int64_t Tq, Tk;
+    int Hq, Hk, D, n;   // D: padded to whole vectors
+    const int32_t *qoff, *koff;
+    int causal;
+    float scale;
+    float *lse, *delta;   // delta[Hq][Tq]: sums of go o
+};
+constexpr int kMaxHeadDim = 256;
+int launch_attention_fwd(int dtype, const AttnArgs &a, void *stream);
+// Gradients whose p is not null; delta is written where q's or k's is among them.
+int launch_attention_bwd(int dtype, const AttnArgs &a, void *stream);
+
+// dst[T][H][Dp] = src's rows, heads and D elements (any strides), zeros past them.
+int launch_pack_heads(int dtype, const void *src, int64_t ts, int64_t hs, int64_t ds, int64_t T, int H, int D, void *dst, int Dp,
+                      void *stream);
+
+// Attention of one query a sequence, q[n][Hq][D], over the first lengths[b] places of the pages
+// [pages][Hk][page][D] that tables[n][width] lists; o[n][Hq][D] (strides of rows and heads;
+// elements side by side).  A length past the table or a page that is none: NaN.
+struct PagedArgs {
+    const void *q;
+    int64_t qts, qhs;
+    void *o;
+    int64_t ots, ohs;
+    const void *kp, *vp;
+    const int32_t *tables, *lengths;
+    int64_t pages;
+    int n, Hq, Hk, D, page, width;
+    float scale;
+};
+int64_t paged_blocks(const PagedArgs &a);   // of the largest launch
+size_t paged_workspace(int dtype, const PagedArgs &a);
+int launch_paged(int dtype, const PagedArgs &a, void *ws, void *stream);
+
 // Global average pool x[N][L][C] -> y[N][C] and its adjoint.
 int launch_avgpool_fwd(int dtype, const void *x, int N, int L, int C, void *y, void *stream);
 int launch_avgpool_bwd(int dtype, const void *dy, int N, int L, int C, void *dx, void *stream);

@@ -1,0 +1,183 @@
+// Attention over whole prompts, forward: for each query row of each packed sequence and head
+//   o = sum over visible keys of exp(c s_j - m) v_j / sum of exp(c s_j - m),  s_j = q k_j
+// with one pass over the keys.  A block takes 128 queries of a head, 32 a wave, and walks
+// the keys BN at a time: S^T = K Q^T, so that a lane holds one query's scores (its maximum
+// and sum are registers of that lane and one exchange with the lane 32 away), and O^T =
+// V^T P^T straight from those registers (attn_tile.h).
+//
+// Bound: matrix cores, 4 D operations a visible pair, and the vector units next to them
+// (an exponential takes four times an addition's time).
+#include <algorithm>
+
+#include "attn_tile.h"
+
+namespace ms {
+namespace att {
+
+constexpr int kRows = 128;   // queries of a block
+
+template <typename T, int DP>
+struct FwdShape {
+    static constexpr int BN = DP * (int)sizeof(T) <= 256 ? 64 : 32;   // keys of a step
+    static constexpr int OCC = DP == 256 ? 1 : 2;                     // blocks a CU
+};
+
+template <typename T, int DP>
+__global__ __launch_bounds__(256, (FwdShape<T, DP>::OCC)) void fwd_kernel(AttnArgs a, int slots) {
+    typedef Mat<T> M;
+    typedef Tile<T, DP> Ti;
+    typedef typename M::Frag Frag;
+    constexpr int BN = FwdShape<T, DP>::BN, NS = BN / 32, NP = 32 / M::KC, BYTES = BN * Ti::RB;
+    __shared__ __align__(16) char lds[4 * BYTES];
+    const int lane = threadIdx.x & 63, w = uniform(threadIdx.x >> 6);
+    const int logical = xcd_remap((int)blockIdx.x, (int)gridDim.x);
+    const int head = logical / slots, hk = head / (a.Hq / a.Hk);
+    // the last tiles of a causal sequence take longest: first
+    const Span s = find_span(a.qoff, a.koff, a.n, (int)a.Tq, (int)a.Tk, slots - 1 - logical % slots, kRows);
+    const int row0 = s.tile * kRows;
+    if (s.tile < 0 || row0 >= s.na) return;
+    const int shift = s.nb - s.na;                 // query i sees keys to i + shift
+    const int end = a.causal ? min(s.nb, min(row0 + kRows, s.na) + shift) : s.nb;
+    const int wrow = row0 + 32 * w, rows = min(32, s.na - wrow);                 // the wave's
+    const int wend = rows <= 0 ? 0 : a.causal ? min(s.nb, wrow + rows + shift) : s.nb;
+    const int wfull = a.causal ? min(s.nb, wrow + 1 + shift) : s.nb;             // keys that all its rows see
+    const int last = a.causal ? min(s.nb - 1, wrow + (lane & 31) + shift) : s.nb - 1;   // the lane's row sees
+
+    const T *qp = static_cast<const T *>(a.q.p) + (int64_t)(s.a0 + wrow) * a.q.ts + head * a.q.hs;
+    const char *kp = reinterpret_cast<const char *>(static_cast<const T *>(a.k.p) + (int64_t)s.b0 * a.k.ts + hk * a.k.hs);
+    const char *vp = reinterpret_cast<const char *>(static_cast<const T *>(a.v.p) + (int64_t)s.b0 * a.v.ts + hk * a.v.hs);
+    Loader<T, DP, BN, 4> lk, lv;
+    lk.init(a.k.ts, a.D, w, lane);
+    lv.init(a.v.ts, a.D, w, lane);
+    auto issue = [&](int k) {
+        char *to = lds + (k / BN & 1) * 2 * BYTES;
+        lk.issue(kp + k * lk.ts, s.nb - k, a.D, to, w);
+        lv.issue(vp + k * lv.ts, s.nb - k, a.D, to + BYTES, w);
+    };
+    if (end > 0) issue(0);
+    Rows<T, DP> q;
+    q.init(qp, a.q.ts, rows, a.D, lane);
+
+    const float c = a.scale * kLog2e;
+    float m = -INFINITY, l = 0.f;
+    floatx16 acc[DP / 32];
+#pragma unroll
+    for (int t = 0; t < DP / 32; ++t) acc[t] = zero16x();
+    for (int k = 0; k < end; k += BN) {
+        tile_sync();
+        if (k + BN < end) issue(k + BN);
+        if (k >= wend) continue;
+        const char *kt = lds + (k / BN & 1) * 2 * BYTES, *vt = kt + BYTES;
+        floatx16 x[NS];
+#pragma unroll
+        for (int n = 0; n < NS; ++n) {
+            x[n] = zero16x();
+#pragma unroll
+            for (int i = 0; i < DP / M::KC; ++i) x[n] = M::mma(Ti::row_frag(kt, 32 * n, i, lane), q.get(i, lane), x[n]);
+        }
+        const bool masked = k + BN > wfull;
+        if (masked) {
+#pragma unroll
+            for (int n = 0; n < NS; ++n)
+#pragma unroll
+                for (int i = 0; i < 16; ++i)
+                    if (k + 32 * n + 8 * (i >> 2) + 4 * (lane >> 5) + (i & 3) > last) x[n][i] = -INFINITY;
+        }
+        float top = x[0][0];
+#pragma unroll
+        for (int n = 0; n < NS; ++n)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) top = fmaxf(top, x[n][i]);
+        top = both_max(top);
+        // The reference follows the maximum only where that is 2^8 above it: what is summed
+        // is then below 2^8 a key, and the sums are seldom multiplied again.
+        if (__any((top - m) * c > 8.f)) {
+            const float to = fmaxf(m, top), f = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((m - to) * c);
+            m = to;
+            l *= f;
+#pragma unroll
+            for (int t = 0; t < DP / 32; ++t)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) acc[t][i] *= f;
+        }
+        const float ref = m == -INFINITY ? 0.f : m;   // (no key yet)
+        Frag p[NS * NP];
+#pragma unroll
+        for (int n = 0; n < NS; ++n) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                x[n][i] = __builtin_amdgcn_exp2f((x[n][i] - ref) * c);
+                l += x[n][i];
+            }
+            // (in bf16 rounded to 8 bits, an operand; the sum has all of them)
+#pragma unroll
+            for (int i = 0; i < NP; ++i) p[n * NP + i] = as_frag<T>(x[n], i);
+        }
+        if (masked && any_wild<T, DP, BN>(vt, 0, lane)) wild_product<T, DP, NS * NP>(acc, vt, 0, p, lane);
+        else add_product<T, DP, NS * NP>(acc, vt, 0, p, lane);
+    }
+    tile_sync();   // no wave reads the tiles any more
+    if (rows <= 0) return;
+    l = both_sum(l);
+    const bool none = last < 0;   // a row that sees no key: zeros
+    if (a.lse && lane < rows)
+        a.lse[(int64_t)head * a.Tq + s.a0 + wrow + lane] = none ? INFINITY : m * c + __builtin_amdgcn_logf(l);
+    store_rows<T, DP>(acc, 1.f / l, none, lds + w * 32 * Ti::RB,
+                      static_cast<T *>(a.o.p) + (int64_t)(s.a0 + wrow) * a.o.ts + head * a.o.hs, a.o.ts, rows, a.D, lane);
+}
+
+// dst[T][H][Dp]: a vector a thread.
+template <typename T>
+__global__ __launch_bounds__(256) void pack_kernel(const T *__restrict__ src, int64_t ts, int64_t hs, int64_t ds, int64_t n, int H, int D,
+                                                   T *__restrict__ dst, int Dp) {
+    constexpr int V = Vec16<T>::N;
+    const int per = Dp / V;
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) {
+        const int64_t row = i / per, t = row / H;
+        const int u = (int)(i - row * per), h = (int)(row - t * H);
+        const T *p = src + t * ts + h * hs;
+        Vec16<T> v;
+#pragma unroll
+        for (int e = 0; e < V; ++e) v.e[e] = u * V + e < D ? p[(u * V + e) * ds] : (T)0.f;
+        store16(dst + i * V, v);
+    }
+}
+
+namespace {
+
+template <typename T, int DP>
+void fwd_run(const AttnArgs &a, hipStream_t st) {
+    const int64_t slots = span_slots(a.qoff != nullptr, a.n, a.Tq, kRows);
+    hipLaunchKernelGGL((fwd_kernel<T, DP>), dim3((unsigned)(slots * a.Hq)), dim3(256), 0, st, a, (int)slots);
+}
+
+template <typename T>
+int fwd_t(const AttnArgs &a, hipStream_t st) {
+    if (a.D <= 64) fwd_run<T, 64>(a, st);
+    else if (a.D <= 128) fwd_run<T, 128>(a, st);
+    else fwd_run<T, 256>(a, st);
+    return (int)hipGetLastError();
+}
+
+}  // namespace
+}  // namespace att
+
+int launch_attention_fwd(int dtype, const AttnArgs &a, void *stream) {
+    if (a.Tq == 0 || a.Hq == 0) return 0;
+    return dtype == kBF16 ? att::fwd_t<bf16>(a, (hipStream_t)stream) : att::fwd_t<float>(a, (hipStream_t)stream);
+}
+
+int launch_pack_heads(int dtype, const void *src, int64_t ts, int64_t hs, int64_t ds, int64_t T, int H, int D, void *dst, int Dp,
+                      void *stream) {
+    const int64_t n = T * H * (Dp / (dtype == kBF16 ? 8 : 4));
+    if (n == 0) return 0;
+    const dim3 grid((unsigned)std::min<int64_t>((n + 255) / 256, 8192));
+    hipStream_t st = (hipStream_t)stream;
+    if (dtype == kBF16)
+        hipLaunchKernelGGL(att::pack_kernel<bf16>, grid, dim3(256), 0, st, (const bf16 *)src, ts, hs, ds, n, H, D, (bf16 *)dst, Dp);
+    else
+        hipLaunchKernelGGL(att::pack_kernel<float>, grid, dim3(256), 0, st, (const float *)src, ts, hs, ds, n, H, D, (float *)dst, Dp);
+    return (int)hipGetLastError();
+}
+
+}  // namespace ms

@@ -1,0 +1,302 @@
+// What the attention kernels share: tiles of rows in LDS, their fragments for the matrix
+// cores, and which rows of which sequence a block works on.
+//
+// A fragment is 16 bytes a lane for both types.  A chunk is what one fragment of each
+// operand contributes to a sum: 16 elements of bf16 (one 32x32x16 instruction), 8 of fp32
+// (four 32x32x2).  Which element is which lane's is the kernels' own choice as long as
+// both operands agree.  The sums of a 32x32 tile lie as column l % 32 in lane l, rows
+// 8 g + 4 (l / 32) + j in element 4 g + j; taken as the other operand of the next
+// product, those elements are the rows 16 c + 4 (l / 32) + {0..3, 8..11} of chunk c in
+// bf16 (8 c + 4 (l / 32) + {0..3} in fp32), so col_frag() reads these rows and no value
+// moves between lanes.
+#pragma once
+
+#include "block_math.h"
+#include "lds_dma.h"
+
+namespace ms {
+namespace att {
+
+template <typename T> struct Mat;
+template <> struct Mat<bf16> {
+    typedef bf16x8 Frag;
+    static constexpr int V = 8, KC = 16;   // elements of a fragment, of a chunk
+    static __device__ __forceinline__ floatx16 mma(Frag a, Frag b, floatx16 c) {
+        return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
+    }
+};
+template <> struct Mat<float> {
+    typedef floatx4 Frag;
+    static constexpr int V = 4, KC = 8;
+    static __device__ __forceinline__ floatx16 mma(Frag a, Frag b, floatx16 c) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) c = __builtin_amdgcn_mfma_f32_32x32x2f32(a[j], b[j], c, 0, 0, 0);
+        return c;
+    }
+};
+
+typedef short v4i16 __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) v4i16 lds_v4i16_t;
+
+// Rows of DP elements in LDS.  The 16-byte units of each eight are swapped by the row, so
+// that eight rows' units of one number lie in different banks (row_frag) and so do the
+// pairs of units of four rows (col_frag).
+template <typename T, int DP>
+struct Tile {
+    typedef typename Mat<T>::Frag Frag;
+    static constexpr int V = Mat<T>::V, U = DP / V, RB = DP * (int)sizeof(T);
+    static __device__ __forceinline__ int swz(int row) { return (row & 3) << 1 | (row >> 2 & 1); }
+    static __device__ __forceinline__ int at(int row, int unit) { return row * RB + ((unit ^ swz(row)) << 4); }
+
+    // Row r0 + l % 32 (r0 a multiple of 8), chunk c of its elements: units 2 c + l / 32.
+    static __device__ __forceinline__ Frag row_frag(const char *base, int r0, int c, int lane) {
+        const int r = lane & 31, low = ((2 * (c & 3) + (lane >> 5)) ^ swz(r)) << 4;
+        return *reinterpret_cast<const Frag *>(base + r * RB + low + r0 * RB + (c >> 2) * 128);
+    }
+    // Column 32 t + l % 32, chunk c of the rows from r0 (a multiple of 8) on.
+    static __device__ __forceinline__ Frag col_frag(const char *base, int r0, int t, int c, int lane) {
+        Frag f;
+        if constexpr (sizeof(T) == 2) {
+            // ds_read_b64_tr_b16: each 16 lanes address four rows of 16 columns, 8 bytes a
+            // lane, and hold a column's four rows afterwards
+            const int r = lane & 15, g = lane >> 4, row = 4 * (g >> 1) + (r >> 2);
+            const int low = ((2 * (g & 1) + ((r & 3) >> 1) + 4 * (t & 1)) ^ swz(row)) << 4;
+            const char *p = base + row * RB + low + ((r & 1) << 3) + (r0 + 16 * c) * RB + (t >> 1) * 128;
+            v4i16 *v = reinterpret_cast<v4i16 *>(&f);
+            v[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4i16_t *)p);
+            v[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4i16_t *)(p + 8 * RB));
+        } else {
+            const int m = lane & 31, hh = lane >> 5;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const int row = 4 * hh + j;
+                f[j] = *reinterpret_cast<const float *>(base + row * RB + (((m >> 2) ^ swz(row)) << 4) + ((m & 3) << 2) +
+                                                        (r0 + 8 * c) * RB + t * 128);
+            }
+        }
+        return f;
+    }
+};
+
+// Loads of ROWS rows into a tile by NW waves, straight into LDS: each wave's lanes fill
+// 1024 bytes in a row.  Rows past the buffer's end and elements past D read as zeros.
+template <typename T, int DP, int ROWS, int NW>
+struct Loader {
+    typedef Tile<T, DP> Ti;
+    static constexpr int PER = ROWS * Ti::U / (64 * NW);
+    static_assert(PER >= 1 && PER * 64 * NW == ROWS * Ti::U, "whole loads");
+    uint32_t off[PER];
+    int64_t ts;   // bytes between rows
+    __device__ __forceinline__ void init(int64_t row_stride, int D, int w, int lane) {
+        ts = row_stride * (int)sizeof(T);
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            const int idx = (i * NW + w) * 64 + lane, row = idx / Ti::U, unit = (idx % Ti::U) ^ Ti::swz(row);
+            off[i] = unit * Ti::V < D ? (uint32_t)(row * (int)ts + unit * 16) : 0x80000000u;
+        }
+    }
+    // base: row 0 of the tile; rows: how many there are from there on
+    __device__ __forceinline__ void issue(const char *base, int rows, int D, char *lds, int w) const {
+        const int n = rows < ROWS ? rows : ROWS;
+        const __amdgpu_buffer_rsrc_t r = g2::rsrc(base, n > 0 ? (uint32_t)((n - 1) * (int)ts + D * (int)sizeof(T)) : 0u);
+#pragma unroll
+        for (int i = 0; i < PER; ++i) g2::dma16<true>(r, lds + (i * NW + w) * 1024, off[i]);
+    }
+};
+
+// All of a wave's own loads have landed and its reads of LDS are done; then the block's.
+__device__ __forceinline__ void tile_sync() {
+    __builtin_amdgcn_s_waitcnt(7 << 4);
+    g2::block_sync<true>();
+}
+
+__device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
+
+// A sequence's rows on the side that blocks divide into tiles, its rows on the other
+// side, and the tile.
+struct Span {
+    int a0, na, b0, nb, tile;
+};
+
+// Tiles of ROWS rows over the sequences aoff[0..n]: sequence i's begin at slot
+// start / ROWS + i, which leaves each as many slots as it can need without a count of
+// tiles having been taken.  Rows before the first and past the last sequence
+// are sequences of their own, without partners.  Offsets are held to [0, Ta].
+__device__ __forceinline__ Span find_span(const int32_t *aoff, const int32_t *boff, int n, int Ta, int Tb, int slot, int rows) {
+    if (!aoff) return Span{0, Ta, 0, Tb, slot};
+    auto edge = [&](int i) {   // of n + 2 sequences
+        return i <= 0 ? 0 : i > n + 1 ? Ta : min(max(aoff[i - 1], 0), Ta);
+    };
+    const int lane = threadIdx.x & 63;
+    int before = 0;
+    for (int i0 = 0; i0 <= n + 1; i0 += 64) {
+        const int i = i0 + lane;
+        before += (int)__popcll(__ballot(i <= n + 1 && edge(i) / rows + i <= slot));
+    }
+    const int i = uniform(before) - 1;
+    const int a0 = uniform(edge(i)), a1 = uniform(max(edge(i + 1), a0));
+    Span s{a0, a1 - a0, 0, 0, slot - (a0 / rows + i)};
+    if (i >= 1 && i <= n) {
+        const int b0 = uniform(min(max(boff[i - 1], 0), Tb));
+        s.b0 = b0;
+        s.nb = uniform(max(min(max(boff[i], 0), Tb), b0)) - b0;
+    }
+    return s;
+}
+
+// Slots of find_span().
+inline int64_t span_slots(bool packed, int n, int64_t Ta, int rows) {
+    return packed ? Ta / rows + n + 2 : (Ta + rows - 1) / rows;
+}
+
+// The sum (maximum) of a lane's value and that of the lane 32 away.
+__device__ __forceinline__ floatx2 halves(float v) {
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return floatx2{__uint_as_float(r[0]), __uint_as_float(r[1])};
+}
+__device__ __forceinline__ float both_sum(float v) {
+    const floatx2 h = halves(v);
+    return h.x + h.y;
+}
+__device__ __forceinline__ float both_max(float v) {
+    const floatx2 h = halves(v);
+    return fmaxf(h.x, h.y);
+}
+
+// A 32x32 tile's sums as fragments: chunk c.
+template <typename T>
+__device__ __forceinline__ typename Mat<T>::Frag as_frag(const floatx16 &s, int c) {
+    typename Mat<T>::Frag f;
+#pragma unroll
+    for (int j = 0; j < Mat<T>::V; ++j) f[j] = from_f32<T>(s[c * Mat<T>::V + j]);
+    return f;
+}
+
+__device__ __forceinline__ floatx16 zero16x() {
+    floatx16 z;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) z[i] = 0.f;
+    return z;
+}
+
+// Whether rows r0.. of a tile hold an infinity or NaN.
+template <typename T, int DP, int ROWS>
+__device__ __forceinline__ bool any_wild(const char *tile, int r0, int lane) {
+    typedef Tile<T, DP> Ti;
+    uint32_t bad = 0;
+#pragma unroll 2
+    for (int i = 0; i < ROWS * Ti::U / 64; ++i) {
+        const u32x4 v = *reinterpret_cast<const u32x4 *>(tile + r0 * Ti::RB + i * 1024 + lane * 16);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            // an exponent of ones carries into the bit above it
+            if constexpr (sizeof(T) == 2) bad |= ((v[j] & 0x7f807f80u) + 0x00800080u) & 0x80008000u;
+            else bad |= ((v[j] & 0x7f800000u) + 0x00800000u) & 0x80000000u;
+        }
+    }
+    return __any(bad != 0);
+}
+
+// acc += columns of `tile` times b (N chunks), a row at a time, where a weight of zero
+// takes no part whatever its row holds: for tiles with masked places where any_wild().
+template <typename T, int DP, int N>
+__device__ __forceinline__ void wild_product(floatx16 (&acc)[DP / 32], const char *tile, int r0, const typename Mat<T>::Frag (&b)[N], int lane) {
+    typedef Mat<T> M;
+    typedef Tile<T, DP> Ti;
+    constexpr int PER = 4 / (int)sizeof(T);   // elements of a word
+    const int n = lane & 31, hh = lane >> 5;
+#pragma unroll
+    for (int t = 0; t < DP / 32; ++t) {
+        __builtin_amdgcn_sched_barrier(0);   // (one tile of columns after the other: together they spill)
+#pragma unroll 1
+        for (int row = 0; row < N * M::KC; ++row) {
+            // whose element is the row's weight: chunk, half of the wave, place in the fragment
+            const int c = row / M::KC, in = row % M::KC, half = in >> 2 & 1, e = (in >> 3 << 2) | (in & 3);
+            uint32_t word = 0;   // (as they are: converted, all weights would be held over the loop)
+#pragma unroll
+            for (int k = 0; k < N; ++k)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) word = k == c && j == e / PER ? __builtin_bit_cast(u32x4, b[k])[j] : word;
+            const float p = __shfl(__uint_as_float(PER == 1 ? word : e & 1 ? word & 0xffff0000u : word << 16), n + 32 * half);
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+                const int d = 32 * t + 8 * g + 4 * hh;
+                const T *v = reinterpret_cast<const T *>(tile + Ti::at(r0 + row, d / M::V)) + d % M::V;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) acc[t][4 * g + j] = p == 0.f ? acc[t][4 * g + j] : acc[t][4 * g + j] + p * to_f32(v[j]);
+            }
+        }
+    }
+    __builtin_amdgcn_sched_barrier(0);
+}
+
+// acc += columns of `tile` times b.
+template <typename T, int DP, int N>
+__device__ __forceinline__ void add_product(floatx16 (&acc)[DP / 32], const char *tile, int r0, const typename Mat<T>::Frag (&b)[N], int lane) {
+#pragma unroll
+    for (int t = 0; t < DP / 32; ++t)
+#pragma unroll
+        for (int i = 0; i < N; ++i) acc[t] = Mat<T>::mma(Tile<T, DP>::col_frag(tile, r0, t, i, lane), b[i], acc[t]);
+}
+
+// A wave's 32 rows of results, which lie as columns of 32x32 tiles (x scale, or zeros), to
+// memory by way of its own part of LDS: whole 16-byte vectors side by side.
+template <typename T, int DP>
+__device__ __forceinline__ void store_rows(const floatx16 (&acc)[DP / 32], float scale, bool zero, char *lds, T *out, int64_t ts, int rows, int D,
+                                           int lane) {
+    typedef Tile<T, DP> Ti;
+    const int n = lane & 31, hh = lane >> 5;
+#pragma unroll
+    for (int t = 0; t < DP / 32; ++t)
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+            T v[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) v[j] = from_f32<T>(zero ? 0.f : acc[t][4 * g + j] * scale);
+            const int d = 32 * t + 8 * g + 4 * hh;
+            char *to = lds + Ti::at(n, d / Ti::V) + (d % Ti::V) * (int)sizeof(T);
+            if constexpr (sizeof(T) == 2) *reinterpret_cast<uint64_t *>(to) = *reinterpret_cast<const uint64_t *>(v);
+            else *reinterpret_cast<u32x4 *>(to) = *reinterpret_cast<const u32x4 *>(v);
+        }
+#pragma unroll
+    for (int i = 0; i < 32 * Ti::U / 64; ++i) {
+        const int idx = i * 64 + lane, row = idx / Ti::U, unit = idx % Ti::U;
+        const u32x4 v = *reinterpret_cast<const u32x4 *>(lds + Ti::at(row, unit));
+        if (row < rows && unit * Ti::V < D) *reinterpret_cast<u32x4 *>(out + row * ts + unit * Ti::V) = v;
+    }
+}
+
+// A wave's 32 rows as the column operand of a product: row l % 32, chunk c; zeros past
+// `rows` and D.
+template <typename T, int DP>
+__device__ __forceinline__ typename Mat<T>::Frag load_row(const T *p, int64_t ts, int rows, int D, int c, int lane) {
+    const int n = lane & 31, d = (2 * c + (lane >> 5)) * Mat<T>::V;
+    typename Mat<T>::Frag v;
+#pragma unroll
+    for (int j = 0; j < Mat<T>::V; ++j) v[j] = (T)0.f;
+    if (n < rows && d < D) v = *reinterpret_cast<const typename Mat<T>::Frag *>(p + n * ts + d);
+    return v;
+}
+
+// All of them, held in registers; or (HOLD false, where they are too many) read where they are used.
+template <typename T, int DP, bool HOLD = true>
+struct Rows {
+    static constexpr int C = DP / Mat<T>::KC;
+    typename Mat<T>::Frag f[HOLD ? C : 1];
+    const T *p;
+    int64_t ts;
+    int rows, D;
+    __device__ __forceinline__ void init(const T *p_, int64_t ts_, int rows_, int D_, int lane) {
+        p = p_, ts = ts_, rows = rows_, D = D_;
+        if constexpr (HOLD)
+#pragma unroll
+            for (int c = 0; c < C; ++c) f[c] = load_row<T, DP>(p, ts, rows, D, c, lane);
+    }
+    __device__ __forceinline__ typename Mat<T>::Frag get(int c, int lane) const {
+        if constexpr (HOLD) return f[c];
+        else return load_row<T, DP>(p, ts, rows, D, c, lane);
+    }
+};
+
+}  // namespace att
+}  // namespace ms

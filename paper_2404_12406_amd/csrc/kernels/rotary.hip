@@ -1,0 +1,366 @@
+// Norms of the heads of x[T][H][D] (a scale for the query heads, one for the key heads)
+// and the rotation of each by its token's position, in one pass; and the same on the way
+// into a paged cache:
+//   r = 1 / sqrt(mean x^2 + eps),  z = x r g
+//   y_i = z_i cos a - z_j sin a,  y_j = z_j cos a + z_i sin a,  a = position freq
+// over the pairs (i, j) of the first R elements: (k, k + R/2) or (2k, 2k + 1).  Backward:
+//   dz = dy turned by -a,  q = dz g,  dx = r (q - x r^2 mean(q x)),  dg = sum of dz x r
+//
+// Bound: memory.  A head lies in the registers of L lanes (a power of two that holds it
+// in 16-byte vectors), so it is read once and the norm is a sum within those lanes.  A
+// group of L lanes takes one token and goes over its heads, so the angles' sines are
+// taken once a token, from position * freq in 64 bits: in 32 an angle of 10^6 would be
+// off by 0.06.
+#include <algorithm>
+
+#include "block_math.h"
+
+namespace ms {
+namespace rot {
+
+// The sum over L lanes (a power of two), in every one of them.
+template <int L>
+__device__ __forceinline__ float group_sum(float v) {
+#define ROT_MOVED(ctrl) __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), ctrl, 0xf, 0xf, false))
+    if constexpr (L > 1) v += ROT_MOVED(0xb1);    // the neighbour
+    if constexpr (L > 2) v += ROT_MOVED(0x4e);    // the other pair of four
+    if constexpr (L > 4) v += ROT_MOVED(0x141);   // mirrored in eight
+    if constexpr (L > 8) v += ROT_MOVED(0x140);   // mirrored in sixteen
+#undef ROT_MOVED
+    if constexpr (L > 16) v += __shfl_xor(v, 16);
+    if constexpr (L > 32) v += __shfl_xor(v, 32);
+    return v;
+}
+
+// How an element finds its partner: within its vector, in another lane's, from memory
+// (halves that are no whole vectors).
+enum Pairing { kNext, kLane, kLoose };
+
+// A lane's part of a token's rotation: cosines and (signed) sines of its elements, and
+// where their partners are.
+template <typename T, int L>
+struct Turn {
+    static constexpr int V = Vec16<T>::N;
+    float cs[V], sn[V];
+    int lane;   // kLane: of the partner
+    __device__ __forceinline__ void take(const RotaryArgs &a, int64_t t, int c, int l, bool back) {
+        const int half = a.R / 2;
+        const double pos = half ? (double)a.pos[t] * 0.15915494309189533577 : 0.0;
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+            const int d = c + e;
+            cs[e] = 1.f;
+            sn[e] = 0.f;
+            if (d < 2 * half) {
+                const bool second = a.next ? d & 1 : d >= half;
+                const double turns = pos * (double)a.freq[a.next ? d >> 1 : second ? d - half : d];
+                float s, k;
+                sincospif(2.f * (float)(turns - rint(turns)), &s, &k);
+                cs[e] = k;
+                sn[e] = second != back ? s : -s;
+            }
+        }
+        const int away = half / V, g = c / V;
+        lane = g < away ? l + away : g < 2 * away ? l - away : l;
+    }
+    // turned z; partner(e) is the partner's value, for kLoose.  (Without a sine nothing
+    // comes from the partner: elements past R stay as they are beside an infinite one.)
+    static __device__ __forceinline__ float sum(float z, float p, float k, float s) { return s == 0.f ? z * k : z * k + p * s; }
+    template <int PAIR, typename F>
+    __device__ __forceinline__ void apply(float (&z)[V], F partner) const {
+        if constexpr (PAIR == kNext) {
+#pragma unroll
+            for (int e = 0; e < V; e += 2) {
+                const float p = z[e], q = z[e + 1];
+                z[e] = sum(p, q, cs[e], sn[e]);
+                z[e + 1] = sum(q, p, cs[e + 1], sn[e + 1]);
+            }
+        } else if constexpr (PAIR == kLane) {
+#pragma unroll
+            for (int e = 0; e < V; ++e) z[e] = sum(z[e], __shfl(z[e], lane), cs[e], sn[e]);
+        } else if constexpr (PAIR == kLoose) {
+#pragma unroll
+            for (int e = 0; e < V; ++e)
+                if (sn[e] != 0.f || cs[e] != 1.f) z[e] = sum(z[e], partner(e), cs[e], sn[e]);
+        }
+    }
+};
+
+template <typename T>
+__device__ __forceinline__ float at(const T *p, int d) { return p ? to_f32(p[d]) : 1.f; }
+
+__device__ __forceinline__ int partner_of(const RotaryArgs &a, int d) {
+    const int half = a.R / 2;
+    return d < half ? d + half : d < 2 * half ? d - half : d;
+}
+
+constexpr int kAhead = 4;   // heads loaded at once
+
+// Forward.  APPEND: heads past the Hq queries go to the cache, the last Hk of them (the
+// values) as they are.
+template <typename T, int L, int PAIR, bool APPEND>
+__global__ __launch_bounds__(256) void fwd_kernel(RotaryArgs a) {
+    constexpr int V = Vec16<T>::N, GROUPS = 256 / L;
+    const int l = threadIdx.x % L, c = l * V;
+    const T *x = static_cast<const T *>(a.x);
+    T *y = static_cast<T *>(a.y);
+    const T *gq = static_cast<const T *>(a.gq), *gk = static_cast<const T *>(a.gk);
+    const int H = a.Hq + (APPEND ? 2 : 1) * a.Hk;
+    float wq[V], wk[V];
+#pragma unroll
+    for (int e = 0; e < V; ++e) {
+        wq[e] = c + e < a.D ? at(gq, c + e) : 0.f;
+        wk[e] = c + e < a.D ? at(gk, c + e) : 0.f;
+    }
+    for (int64_t t = (int64_t)blockIdx.x * GROUPS + threadIdx.x / L; t < a.T; t += (int64_t)gridDim.x * GROUPS) {
+        int64_t place = -1;   // of the token in the cache: page * page size + row in it
+        if constexpr (APPEND) {
+            const int pos = a.pos[t];
+            const int64_t row = a.rows ? (int64_t)a.rows[t] : t;
+            if (pos >= 0 && row >= 0 && row < a.nseq && pos / a.page < a.width) {
+                const int pg = a.tables[row * a.width + pos / a.page];
+                if (pg >= 0 && pg < a.pages) place = (int64_t)pg * a.page + pos % a.page;
+            }
+        }
+        Turn<T, L> turn;
+        turn.take(a, t, c, (int)(threadIdx.x & 63), false);
+        const T *xt = x + t * a.xts;
+        for (int h0 = (int)blockIdx.y * kAhead; h0 < H; h0 += (int)gridDim.y * kAhead) {
+            Vec16<T> in[kAhead];
+#pragma unroll
+            for (int u = 0; u < kAhead; ++u)
+                if (h0 + u < H) in[u] = load_vec<T>(xt + (h0 + u) * a.xhs, c, a.D);
+#pragma unroll
+            for (int u = 0; u < kAhead; ++u) {
+                const int h = h0 + u;
+                if (h >= H) continue;
+                Vec16<T> out = in[u];
+                const bool value = APPEND && h >= a.Hq + a.Hk, query = h < a.Hq;
+                if (!value) {
+                    float z[V], r = 1.f;
+#pragma unroll
+                    for (int e = 0; e < V; ++e) z[e] = to_f32(in[u].e[e]);
+                    if (a.norm) {
+                        float s = 0.f;
+#pragma unroll
+                        for (int e = 0; e < V; ++e) s += z[e] * z[e];
+                        r = 1.f / sqrtf(group_sum<L>(s) / (float)a.D + a.eps);
+#pragma unroll
+                        for (int e = 0; e < V; ++e) z[e] = z[e] * r * (query ? wq[e] : wk[e]);
+                    }
+                    turn.template apply<PAIR>(z, [&](int e) {
+                        const int p = partner_of(a, c + e);
+                        return to_f32(xt[h * a.xhs + p]) * r * (a.norm ? at(query ? gq : gk, p) : 1.f);
+                    });
+#pragma unroll
+                    for (int e = 0; e < V; ++e) out.e[e] = from_f32<T>(z[e]);
+                }
+                if (c >= a.D) continue;
+                if (!APPEND || query) {
+                    store_vec<T>(y + t * a.yts + h * a.yhs, c, a.D, out);
+                } else if (place >= 0) {
+                    const int64_t pg = place / a.page, in_page = place - pg * a.page;
+                    const int hk = h - a.Hq - (value ? a.Hk : 0);
+                    T *to = static_cast<T *>(value ? a.vp : a.kp) + ((pg * a.Hk + hk) * a.page + in_page) * a.D;
+                    store_vec<T>(to, c, a.D, out);
+                }
+            }
+        }
+    }
+}
+
+// dx (may be null) and partial rows of dgq and dgk: part[blocks][2][D] (may be null).
+template <typename T, int L, int PAIR>
+__global__ __launch_bounds__(256) void bwd_kernel(RotaryArgs a, const T *dy, int64_t dts, int64_t dhs, T *dx, int64_t gts,
+                                                  int64_t ghs, float *part) {
+    constexpr int V = Vec16<T>::N, GROUPS = 256 / L;
+    __shared__ float meet[GROUPS][L * V];
+    const int l = threadIdx.x % L, c = l * V;
+    const T *x = static_cast<const T *>(a.x);
+    const T *gq = static_cast<const T *>(a.gq), *gk = static_cast<const T *>(a.gk);
+    const int H = a.Hq + a.Hk;
+    float sq[V], sk[V], wq[V], wk[V];
+#pragma unroll
+    for (int e = 0; e < V; ++e) {
+        sq[e] = sk[e] = 0.f;
+        wq[e] = c + e < a.D ? at(gq, c + e) : 0.f;
+        wk[e] = c + e < a.D ? at(gk, c + e) : 0.f;
+    }
+    for (int64_t t = (int64_t)blockIdx.x * GROUPS + threadIdx.x / L; t < a.T; t += (int64_t)gridDim.x * GROUPS) {
+        Turn<T, L> turn;
+        turn.take(a, t, c, (int)(threadIdx.x & 63), true);
+        const T *xt = x + t * a.xts, *dt = dy + t * dts;
+        for (int h0 = (int)blockIdx.y * kAhead; h0 < H; h0 += (int)gridDim.y * kAhead) {
+            Vec16<T> xi[kAhead], gi[kAhead];
+#pragma unroll
+            for (int u = 0; u < kAhead; ++u) {
+                if (h0 + u >= H) continue;
+                gi[u] = load_vec<T>(dt + (h0 + u) * dhs, c, a.D);
+                xi[u] = a.norm ? load_vec<T>(xt + (h0 + u) * a.xhs, c, a.D) : zero16<T>();
+            }
+#pragma unroll
+            for (int u = 0; u < kAhead; ++u) {
+                const int h = h0 + u;
+                if (h >= H) continue;
+                const bool query = h < a.Hq;
+                float z[V];
+#pragma unroll
+                for (int e = 0; e < V; ++e) z[e] = to_f32(gi[u].e[e]);
+                turn.template apply<PAIR>(z, [&](int e) { return to_f32(dt[h * dhs + partner_of(a, c + e)]); });
+                if (a.norm) {
+                    float s = 0.f, m = 0.f;
+#pragma unroll
+                    for (int e = 0; e < V; ++e) {
+                        const float v = to_f32(xi[u].e[e]);
+                        s += v * v;
+                        m += z[e] * (query ? wq[e] : wk[e]) * v;
+                    }
+                    const float r = 1.f / sqrtf(group_sum<L>(s) / (float)a.D + a.eps);
+                    m = group_sum<L>(m) / (float)a.D * r * r;
+#pragma unroll
+                    for (int e = 0; e < V; ++e) {
+                        const float v = to_f32(xi[u].e[e]), p = z[e] * v * r;
+                        if (query) sq[e] += p;
+                        else sk[e] += p;
+                        z[e] = r * (z[e] * (query ? wq[e] : wk[e]) - v * m);
+                    }
+                }
+                if (dx && c < a.D) {
+                    Vec16<T> out;
+#pragma unroll
+                    for (int e = 0; e < V; ++e) out.e[e] = from_f32<T>(z[e]);
+                    store_vec<T>(dx + t * gts + h * ghs, c, a.D, out);
+                }
+            }
+        }
+    }
+    if (!part) return;
+    float *to = part + ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * 2 * a.D;
+#pragma unroll
+    for (int w = 0; w < 2; ++w) {
+#pragma unroll
+        for (int e = 0; e < V; ++e) meet[threadIdx.x / L][c + e] = w ? sk[e] : sq[e];
+        __syncthreads();
+        for (int d = threadIdx.x; d < a.D; d += 256) {
+            float s = 0.f;
+            for (int g = 0; g < GROUPS; ++g) s += meet[g][d];
+            to[w * a.D + d] = s;
+        }
+        __syncthreads();
+    }
+}
+
+// out[w][d] = the sum of the partial rows, in a fixed order.
+template <typename T>
+__global__ __launch_bounds__(256) void sum_kernel(const float *__restrict__ part, int rows, int D, T *__restrict__ oq, T *__restrict__ ok) {
+    __shared__ float red[16][17];
+    const int col = threadIdx.x & 15, grp = threadIdx.x >> 4, c = (int)blockIdx.x * 16 + col;   // a column of [2 D]
+    float s = 0.f;
+    if (c < 2 * D)
+        for (int r = grp; r < rows; r += 16) s += part[(int64_t)r * 2 * D + c];
+    red[grp][col] = s;
+    __syncthreads();
+    if (grp == 0 && c < 2 * D) {
+#pragma unroll
+        for (int q = 1; q < 16; ++q) s += red[q][col];
+        T *o = c < D ? oq : ok;
+        if (o) o[c < D ? c : c - D] = from_f32<T>(s);
+    }
+}
+
+// ------------------------------------------------------------------ host
+namespace {
+
+constexpr int kMostBlocks = 2048, kMostParts = 512;
+
+int lanes(int dtype, int D) {
+    const int v = dtype == kBF16 ? 8 : 4, n = (D + v - 1) / v;
+    int l = 4;
+    while (l < n) l *= 2;
+    return l;
+}
+
+int pairing(int dtype, const RotaryArgs &a) {
+    if (a.R < 2 || a.next) return kNext;
+    return (a.R / 2) % (dtype == kBF16 ? 8 : 4) == 0 ? kLane : kLoose;
+}
+
+dim3 grid_of(int dtype, const RotaryArgs &a, int heads, int most) {
+    const int groups = 256 / lanes(dtype, a.D);
+    const int64_t bx = std::min<int64_t>((a.T + groups - 1) / groups, most);
+    const int by = (int)std::max<int64_t>(1, std::min<int64_t>((heads + kAhead - 1) / kAhead, most / std::max<int64_t>(bx, 1)));
+    return dim3((unsigned)bx, (unsigned)by);
+}
+
+template <typename T, int L, int PAIR>
+void fwd_run(const RotaryArgs &a, dim3 grid, bool append, hipStream_t st) {
+    if (append) hipLaunchKernelGGL((fwd_kernel<T, L, PAIR, true>), grid, dim3(256), 0, st, a);
+    else hipLaunchKernelGGL((fwd_kernel<T, L, PAIR, false>), grid, dim3(256), 0, st, a);
+}
+
+template <typename T, int L, int PAIR>
+void bwd_run(const RotaryArgs &a, dim3 grid, const void *dy, const int64_t ds[2], void *dx, const int64_t gs[2], float *part,
+             hipStream_t st) {
+    hipLaunchKernelGGL((bwd_kernel<T, L, PAIR>), grid, dim3(256), 0, st, a, (const T *)dy, ds[0], ds[1], (T *)dx, gs[0], gs[1], part);
+}
+
+#define ROT_PAIR(F, L, ...)                                  \
+    switch (pairing(dtype, a)) {                             \
+    case kNext: F<T, L, kNext>(__VA_ARGS__); break;          \
+    case kLane: F<T, L, kLane>(__VA_ARGS__); break;          \
+    default: F<T, L, kLoose>(__VA_ARGS__); break;            \
+    }
+#define ROT_DISPATCH(F, ...)                                 \
+    switch (lanes(dtype, a.D)) {                             \
+    case 4: ROT_PAIR(F, 4, __VA_ARGS__) break;               \
+    case 8: ROT_PAIR(F, 8, __VA_ARGS__) break;               \
+    case 16: ROT_PAIR(F, 16, __VA_ARGS__) break;             \
+    case 32: ROT_PAIR(F, 32, __VA_ARGS__) break;             \
+    default: ROT_PAIR(F, 64, __VA_ARGS__) break;             \
+    }
+
+template <typename T>
+int fwd_t(int dtype, const RotaryArgs &a, bool append, hipStream_t st) {
+    const dim3 grid = grid_of(dtype, a, a.Hq + (append ? 2 : 1) * a.Hk, kMostBlocks);
+    ROT_DISPATCH(fwd_run, a, grid, append, st)
+    return (int)hipGetLastError();
+}
+
+template <typename T>
+int bwd_t(int dtype, const RotaryArgs &a, const void *dy, const int64_t ds[2], void *dx, const int64_t gs[2], void *dgq, void *dgk,
+          void *ws, hipStream_t st) {
+    const bool params = dgq || dgk;
+    float *part = params ? static_cast<float *>(ws) : nullptr;
+    int rows = 0;
+    if (a.T > 0 && a.Hq + a.Hk > 0) {
+        const dim3 grid = grid_of(dtype, a, a.Hq + a.Hk, params ? kMostParts : kMostBlocks);
+        ROT_DISPATCH(bwd_run, a, grid, dy, ds, dx, gs, part, st)
+        rows = (int)(grid.x * grid.y);
+    }
+    if (params)
+        hipLaunchKernelGGL(sum_kernel<T>, dim3((unsigned)((2 * a.D + 15) / 16)), dim3(256), 0, st, part, rows, a.D, (T *)dgq, (T *)dgk);
+    return (int)hipGetLastError();
+}
+
+}  // namespace
+}  // namespace rot
+
+int launch_rotary_fwd(int dtype, const RotaryArgs &a, bool append, void *stream) {
+    if (a.T == 0 || a.Hq + a.Hk == 0) return 0;
+    return dtype == kBF16 ? rot::fwd_t<bf16>(dtype, a, append, (hipStream_t)stream)
+                          : rot::fwd_t<float>(dtype, a, append, (hipStream_t)stream);
+}
+
+size_t rotary_bwd_workspace(int dtype, const RotaryArgs &a, bool params) {
+    if (!params || a.T == 0 || a.Hq + a.Hk == 0) return 0;
+    const dim3 g = rot::grid_of(dtype, a, a.Hq + a.Hk, rot::kMostParts);
+    return ((size_t)g.x * g.y * 2 * a.D * sizeof(float) + 255) / 256 * 256;
+}
+
+int launch_rotary_bwd(int dtype, const RotaryArgs &a, const void *dy, const int64_t dstride[2], void *dx, const int64_t gstride[2],
+                      void *dgq, void *dgk, void *ws, void *stream) {
+    return dtype == kBF16 ? rot::bwd_t<bf16>(dtype, a, dy, dstride, dx, gstride, dgq, dgk, ws, (hipStream_t)stream)
+                          : rot::bwd_t<float>(dtype, a, dy, dstride, dx, gstride, dgq, dgk, ws, (hipStream_t)stream);
+}
+
+}  // namespace ms

@@ -294,6 +294,12 @@ struct BlockState {
     void *proj = nullptr;        // gated linear: the kept projections
     float *lse = nullptr;        // cross entropy: log-sum-exp of each row without its target,
     const void *grad = nullptr;  // or the kept gradient
+    // head norms with rotation; attention (lse as above)
+    const int32_t *positions = nullptr, *qoff = nullptr, *koff = nullptr;
+    const float *freq = nullptr;
+    int64_t heads = 0, n = 0;    // query heads; sequences
+    int32_t turned = 0, next = 0, norm = 0, causal = 0;
+    float scale = 0.f;
 };
 
 }  // namespace rt
@@ -334,6 +340,9 @@ inline void release(ms_record *r) {
         r->blk.target = nullptr;
         r->blk.proj = nullptr;
         r->blk.lse = nullptr;
+        r->y.data = nullptr;
+        r->blk.positions = r->blk.qoff = r->blk.koff = nullptr;
+        r->blk.freq = nullptr;
     }
 }
 
