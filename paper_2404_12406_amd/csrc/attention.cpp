@@ -148,6 +148,21 @@ ms_status rotary_backward(ms_record *r, const ms_tensor *gy, const ms_tensor *gx
 }
 
 // ------------------------------------------------------------------ attention
+ms::AttnArgs attention_args(const ms_tensor *q, const ms_tensor *k, const BlockState &b) {
+    ms::AttnArgs a{};
+    a.Tq = q->shape[0];
+    a.Tk = k->shape[0];
+    a.Hq = (int)q->shape[1];
+    a.Hk = (int)k->shape[1];
+    a.D = (int)padded(q->shape[2], q->dtype);
+    a.n = (int)b.n;
+    a.qoff = b.qoff;
+    a.koff = b.koff;
+    a.causal = b.causal;
+    a.scale = b.scale;
+    return a;
+}
+
 ms_status attention_backward(ms_record *r, const ms_tensor *go, const ms_tensor *gq, const ms_tensor *gk, const ms_tensor *gv, void *stream,
                              bool fixed) {
     const int32_t dt = r->plan.dtype;
@@ -156,15 +171,10 @@ ms_status attention_backward(ms_record *r, const ms_tensor *go, const ms_tensor 
     const Stand q = sg.add(&r->x, true), k = sg.add(&r->W, true), v = sg.add(both ? &r->b : nullptr, true),
                 o = sg.add(both ? &r->y : nullptr, true), g = sg.add(go, true), dq = sg.add(gq, true), dk = sg.add(gk, true),
                 dv = sg.add(gv, true);
-    ms::AttnArgs a{};
-    a.Tq = r->x.shape[0];
-    a.Tk = r->W.shape[0];
-    a.Hq = (int)r->x.shape[1];
-    a.Hk = (int)r->W.shape[1];
-    a.D = (int)padded(r->x.shape[2], dt);
-    const size_t delta = both ? al256((size_t)(a.Tq * a.Hq) * sizeof(float)) : 0;
+    ms::AttnArgs a = attention_args(&r->x, &r->W, r->blk);
+    const size_t kb = ms::attention_bwd_workspace(dt, a, gq, gk, gv);
     Work w;
-    ms_status st = take(&w, sg.bytes + delta, stream, fixed);
+    ms_status st = take(&w, sg.bytes + kb, stream, fixed);
     if (st) return st;
     int err = 0;
     for (const Stand *s : {&q, &k, &v, &o, &g})
@@ -177,14 +187,8 @@ ms_status attention_backward(ms_record *r, const ms_tensor *go, const ms_tensor 
     a.dq = view(dq, w.base);
     a.dk = view(dk, w.base);
     a.dv = view(dv, w.base);
-    a.n = (int)r->blk.n;
-    a.qoff = r->blk.qoff;
-    a.koff = r->blk.koff;
-    a.causal = r->blk.causal;
-    a.scale = r->blk.scale;
     a.lse = r->blk.lse;
-    a.delta = delta ? reinterpret_cast<float *>(w.base + sg.bytes) : nullptr;
-    if (!err) err = ms::launch_attention_bwd(dt, a, stream);
+    if (!err) err = ms::launch_attention_bwd(dt, a, kb ? w.base + sg.bytes : nullptr, stream);
     for (const Stand *s : {&dq, &dk, &dv})
         if (!err) err = put_out(*s, w.base, stream);
     return err ? hip_fail(err, "backward launch") : MS_OK;
@@ -321,10 +325,18 @@ ms_status ms_attention_forward(const ms_tensor *q, const ms_tensor *k, const ms_
         return fail(MS_E_UNSUPPORTED, "2^24 or more blocks of 128 rows");
     if (mask && Tq > 0 && !kept) return fail(MS_E_NULL, "kept is NULL but gradients are asked for");
     if (mask && !aligned(kept, 4)) return fail(MS_E_ARG, "kept must be 4-byte aligned");
+    BlockState blk;
+    blk.qoff = q_offsets;
+    blk.koff = q_offsets && !k_offsets ? q_offsets : k_offsets;
+    blk.n = n;
+    blk.causal = causal != 0;
+    blk.scale = scale;
+    ms::AttnArgs a = attention_args(q, k, blk);
     Stands sg;
     const Stand sq = sg.add(q, true), sk = sg.add(k, true), sv = sg.add(v, true), so = sg.add(o, true);
+    const size_t kb = ms::attention_fwd_workspace(q->dtype, a);
     Work w;
-    if ((st = take(&w, sg.bytes, stream, false))) return st;
+    if ((st = take(&w, sg.bytes + kb, stream, false))) return st;
     ms_record *r = nullptr;
     if (mask) {
         const bool both = mask & (MS_RG_INPUT | MS_RG_WEIGHT);
@@ -341,37 +353,23 @@ ms_status ms_attention_forward(const ms_tensor *q, const ms_tensor *k, const ms_
             r->b.data = v->data;
             r->y.data = o->data;
         }
-        r->blk.qoff = q_offsets;
-        r->blk.koff = q_offsets && !k_offsets ? q_offsets : k_offsets;
-        r->blk.n = n;
-        r->blk.causal = causal != 0;
-        r->blk.scale = scale;
+        r->blk = blk;
         r->blk.lse = static_cast<float *>(kept);
-        r->acct.transient_workspace_bytes = stand_bytes(q, true) + stand_bytes(k, true) + stand_bytes(o, true) +
-                                            (both ? stand_bytes(v, true) + stand_bytes(o, true) + al256((size_t)(Tq * Hq) * sizeof(float)) : 0) +
+        r->acct.transient_workspace_bytes = ms::attention_bwd_workspace(q->dtype, a, mask & MS_RG_INPUT, mask & MS_RG_WEIGHT, mask & MS_RG_BIAS) +
+                                            stand_bytes(q, true) + stand_bytes(k, true) + stand_bytes(o, true) +
+                                            (both ? stand_bytes(v, true) + stand_bytes(o, true) : 0) +
                                             ((mask & MS_RG_INPUT) ? stand_bytes(q, true) : 0) + ((mask & MS_RG_WEIGHT) ? stand_bytes(k, true) : 0) +
                                             ((mask & MS_RG_BIAS) ? stand_bytes(v, true) : 0);
     }
     int err = 0;
     for (const Stand *s : {&sq, &sk, &sv})
         if (!err) err = put_in(*s, w.base, stream);
-    ms::AttnArgs a{};
     a.q = view(sq, w.base);
     a.k = view(sk, w.base);
     a.v = view(sv, w.base);
     a.o = view(so, w.base);
-    a.Tq = Tq;
-    a.Tk = Tk;
-    a.Hq = (int)Hq;
-    a.Hk = (int)Hk;
-    a.D = (int)padded(D, q->dtype);
-    a.n = (int)n;
-    a.qoff = q_offsets;
-    a.koff = q_offsets && !k_offsets ? q_offsets : k_offsets;
-    a.causal = causal != 0;
-    a.scale = scale;
     a.lse = mask ? static_cast<float *>(kept) : nullptr;
-    if (!err) err = ms::launch_attention_fwd(q->dtype, a, stream);
+    if (!err) err = ms::launch_attention_fwd(q->dtype, a, kb ? w.base + sg.bytes : nullptr, stream);
     if (!err) err = put_out(so, w.base, stream);
     if (err) {
         delete r;

@@ -253,12 +253,14 @@ struct AttnArgs {
     const int32_t *qoff, *koff;
     int causal;
     float scale;
-    float *lse, *delta;   // delta[Hq][Tq]: sums of go o
+    float *lse;
 };
 constexpr int kMaxHeadDim = 256;
-int launch_attention_fwd(int dtype, const AttnArgs &a, void *stream);
-// Gradients whose p is not null; delta is written where q's or k's is among them.
-int launch_attention_bwd(int dtype, const AttnArgs &a, void *stream);
+size_t attention_fwd_workspace(int dtype, const AttnArgs &a);
+int launch_attention_fwd(int dtype, const AttnArgs &a, void *ws, void *stream);
+// Gradients whose p is not null; the workspace goes by which are asked for.
+size_t attention_bwd_workspace(int dtype, const AttnArgs &a, bool dq, bool dk, bool dv);
+int launch_attention_bwd(int dtype, const AttnArgs &a, void *ws, void *stream);
 
 // dst[T][H][Dp] = src's rows, heads and D elements (any strides), zeros past them.
 int launch_pack_heads(int dtype, const void *src, int64_t ts, int64_t hs, int64_t ds, int64_t T, int H, int D, void *dst, int Dp,

@@ -16,18 +16,27 @@ namespace att {
 
 constexpr int kRows = 128;   // queries of a block
 
-template <typename T, int DP>
+template <typename T, int DC>
 struct FwdShape {
-    static constexpr int BN = DP * (int)sizeof(T) <= 256 ? 64 : 32;   // keys of a step
-    static constexpr int OCC = DP == 256 ? 1 : 2;                     // blocks a CU
+    static constexpr int BN = kPitch<DC> * (int)sizeof(T) <= 256 ? 64 : 32;   // keys of a step
+    static constexpr int OCC = DC <= 128 ? 2 : 1;   // blocks a CU
 };
 
-template <typename T, int DP>
-__global__ __launch_bounds__(256, (FwdShape<T, DP>::OCC)) void fwd_kernel(AttnArgs a, int slots) {
+// Partial results of a block that takes some of the keys alone: sums[split][Hq][Tq][DC] and
+// floatx2 {reference, sum}[split][Hq][Tq] behind them.
+struct Parts {
+    int splits;
+    float *sums;
+    floatx2 *stat;
+};
+
+template <typename T, int DC>
+__global__ __launch_bounds__(256, (FwdShape<T, DC>::OCC)) void fwd_kernel(AttnArgs a, int slots, Parts part) {
+    constexpr int DP = kPitch<DC>;
     typedef Mat<T> M;
     typedef Tile<T, DP> Ti;
     typedef typename M::Frag Frag;
-    constexpr int BN = FwdShape<T, DP>::BN, NS = BN / 32, NP = 32 / M::KC, BYTES = BN * Ti::RB;
+    constexpr int BN = FwdShape<T, DC>::BN, NS = BN / 32, NP = 32 / M::KC, BYTES = BN * Ti::RB;
     __shared__ __align__(16) char lds[4 * BYTES];
     const int lane = threadIdx.x & 63, w = uniform(threadIdx.x >> 6);
     const int logical = xcd_remap((int)blockIdx.x, (int)gridDim.x);
@@ -37,7 +46,9 @@ __global__ __launch_bounds__(256, (FwdShape<T, DP>::OCC)) void fwd_kernel(AttnAr
     const int row0 = s.tile * kRows;
     if (s.tile < 0 || row0 >= s.na) return;
     const int shift = s.nb - s.na;                 // query i sees keys to i + shift
-    const int end = a.causal ? min(s.nb, min(row0 + kRows, s.na) + shift) : s.nb;
+    const int seen = a.causal ? max(0, min(s.nb, min(row0 + kRows, s.na) + shift)) : s.nb, steps = (seen + BN - 1) / BN;
+    const int begin = (int)((int64_t)steps * blockIdx.y / part.splits) * BN;   // of the block's keys
+    const int end = min(seen, (int)((int64_t)steps * (blockIdx.y + 1) / part.splits) * BN);
     const int wrow = row0 + 32 * w, rows = min(32, s.na - wrow);                 // the wave's
     const int wend = rows <= 0 ? 0 : a.causal ? min(s.nb, wrow + rows + shift) : s.nb;
     const int wfull = a.causal ? min(s.nb, wrow + 1 + shift) : s.nb;             // keys that all its rows see
@@ -54,16 +65,16 @@ __global__ __launch_bounds__(256, (FwdShape<T, DP>::OCC)) void fwd_kernel(AttnAr
         lk.issue(kp + k * lk.ts, s.nb - k, a.D, to, w);
         lv.issue(vp + k * lv.ts, s.nb - k, a.D, to + BYTES, w);
     };
-    if (end > 0) issue(0);
-    Rows<T, DP> q;
+    if (begin < end) issue(begin);
+    Rows<T, DC> q;
     q.init(qp, a.q.ts, rows, a.D, lane);
 
     const float c = a.scale * kLog2e;
     float m = -INFINITY, l = 0.f;
-    floatx16 acc[DP / 32];
+    floatx16 acc[DC / 32];
 #pragma unroll
-    for (int t = 0; t < DP / 32; ++t) acc[t] = zero16x();
-    for (int k = 0; k < end; k += BN) {
+    for (int t = 0; t < DC / 32; ++t) acc[t] = zero16x();
+    for (int k = begin; k < end; k += BN) {
         tile_sync();
         if (k + BN < end) issue(k + BN);
         if (k >= wend) continue;
@@ -73,7 +84,7 @@ __global__ __launch_bounds__(256, (FwdShape<T, DP>::OCC)) void fwd_kernel(AttnAr
         for (int n = 0; n < NS; ++n) {
             x[n] = zero16x();
 #pragma unroll
-            for (int i = 0; i < DP / M::KC; ++i) x[n] = M::mma(Ti::row_frag(kt, 32 * n, i, lane), q.get(i, lane), x[n]);
+            for (int i = 0; i < DC / M::KC; ++i) x[n] = M::mma(Ti::row_frag(kt, 32 * n, i, lane), q.get(i, lane), x[n]);
         }
         const bool masked = k + BN > wfull;
         if (masked) {
@@ -96,7 +107,7 @@ __global__ __launch_bounds__(256, (FwdShape<T, DP>::OCC)) void fwd_kernel(AttnAr
             m = to;
             l *= f;
 #pragma unroll
-            for (int t = 0; t < DP / 32; ++t)
+            for (int t = 0; t < DC / 32; ++t)
 #pragma unroll
                 for (int i = 0; i < 16; ++i) acc[t][i] *= f;
         }
@@ -113,17 +124,55 @@ __global__ __launch_bounds__(256, (FwdShape<T, DP>::OCC)) void fwd_kernel(AttnAr
 #pragma unroll
             for (int i = 0; i < NP; ++i) p[n * NP + i] = as_frag<T>(x[n], i);
         }
-        if (masked && any_wild<T, DP, BN>(vt, 0, lane)) wild_product<T, DP, NS * NP>(acc, vt, 0, p, lane);
-        else add_product<T, DP, NS * NP>(acc, vt, 0, p, lane);
+        if (masked && any_wild<T, DP, BN>(vt, 0, lane)) wild_product<T, DP, DC, NS * NP>(acc, vt, 0, p, lane);
+        else add_product<T, DP, DC, NS * NP>(acc, vt, 0, p, lane);
     }
     tile_sync();   // no wave reads the tiles any more
     if (rows <= 0) return;
     l = both_sum(l);
     const bool none = last < 0;   // a row that sees no key: zeros
+    if (part.splits > 1) {
+        const int64_t at = ((int64_t)blockIdx.y * a.Hq + head) * a.Tq + s.a0 + wrow;
+        store_sums<DC>(acc, part.sums + at * DC, DC, rows, lane);
+        if (lane < rows) part.stat[at + lane] = floatx2{m, none ? -1.f : l};
+        return;
+    }
     if (a.lse && lane < rows)
         a.lse[(int64_t)head * a.Tq + s.a0 + wrow + lane] = none ? INFINITY : m * c + __builtin_amdgcn_logf(l);
-    store_rows<T, DP>(acc, 1.f / l, none, lds + w * 32 * Ti::RB,
+    store_rows<T, DP, DC>(acc, 1.f / l, none, lds + w * 32 * Ti::RB,
                       static_cast<T *>(a.o.p) + (int64_t)(s.a0 + wrow) * a.o.ts + head * a.o.hs, a.o.ts, rows, a.D, lane);
+}
+
+// o and lse from the partial results: a vector a thread.
+template <typename T, int DC>
+__global__ __launch_bounds__(256) void join_kernel(AttnArgs a, Parts part) {
+    constexpr int V = Vec16<T>::N;
+    const int per = a.D / V;
+    const int64_t rows = a.Tq * a.Hq, i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (i >= rows * per) return;
+    const int64_t row = i / per, t = row / a.Hq;
+    const int u = (int)(i - row * per), h = (int)(row - t * a.Hq);
+    const int64_t at = h * a.Tq + t;
+    const float c = a.scale * kLog2e;
+    float top = -INFINITY, sum = 0.f, o[V];
+    bool none = false;
+#pragma unroll
+    for (int e = 0; e < V; ++e) o[e] = 0.f;
+    for (int s = 0; s < part.splits; ++s) top = fmaxf(top, part.stat[s * rows + at].x);
+    for (int s = 0; s < part.splits; ++s) {
+        const floatx2 st = part.stat[s * rows + at];
+        const float f = st.x == top ? 1.f : __builtin_amdgcn_exp2f((st.x - top) * c);
+        none |= st.y < 0.f;
+        sum += f * st.y;
+        const float *p = part.sums + (s * rows + at) * DC + u * V;
+#pragma unroll
+        for (int e = 0; e < V; ++e) o[e] += f * p[e];
+    }
+    Vec16<T> v;
+#pragma unroll
+    for (int e = 0; e < V; ++e) v.e[e] = from_f32<T>(none ? 0.f : o[e] / sum);
+    store16(static_cast<T *>(a.o.p) + t * a.o.ts + h * a.o.hs + u * V, v);
+    if (a.lse && u == 0) a.lse[at] = none ? INFINITY : top * c + __builtin_amdgcn_logf(sum);
 }
 
 // dst[T][H][Dp]: a vector a thread.
@@ -145,26 +194,45 @@ __global__ __launch_bounds__(256) void pack_kernel(const T *__restrict__ src, in
 
 namespace {
 
-template <typename T, int DP>
-void fwd_run(const AttnArgs &a, hipStream_t st) {
-    const int64_t slots = span_slots(a.qoff != nullptr, a.n, a.Tq, kRows);
-    hipLaunchKernelGGL((fwd_kernel<T, DP>), dim3((unsigned)(slots * a.Hq)), dim3(256), 0, st, a, (int)slots);
+int64_t rows_slots(const AttnArgs &a) { return span_slots(a.qoff != nullptr, a.n, a.Tq, kRows); }
+
+template <typename T, int DC>
+int fwd_splits(const AttnArgs &a) {
+    const int64_t keys = a.qoff ? a.Tk / std::max(a.n, 1) : a.Tk;   // of a sequence
+    return span_splits(rows_slots(a) * a.Hq, keys / FwdShape<T, DC>::BN, a.Tq * a.Hq * DC * 4);
 }
 
-template <typename T>
-int fwd_t(const AttnArgs &a, hipStream_t st) {
-    if (a.D <= 64) fwd_run<T, 64>(a, st);
-    else if (a.D <= 128) fwd_run<T, 128>(a, st);
-    else fwd_run<T, 256>(a, st);
+template <typename T, int DC>
+size_t fwd_space(const AttnArgs &a) {
+    const size_t n = fwd_splits<T, DC>(a);
+    return n > 1 ? (n * a.Tq * a.Hq * (DC * sizeof(float) + sizeof(floatx2)) + 255) / 256 * 256 : 0;
+}
+
+template <typename T, int DC>
+int fwd_run(const AttnArgs &a, void *ws, hipStream_t st) {
+    const int64_t slots = rows_slots(a), rows = a.Tq * a.Hq;
+    Parts part{fwd_splits<T, DC>(a), static_cast<float *>(ws), nullptr};
+    part.stat = reinterpret_cast<floatx2 *>(part.sums + part.splits * rows * DC);
+    hipLaunchKernelGGL((fwd_kernel<T, DC>), dim3((unsigned)(slots * a.Hq), (unsigned)part.splits), dim3(256), 0, st, a, (int)slots, part);
+    if (part.splits > 1) {
+        const int64_t n = rows * (a.D / Vec16<T>::N);
+        hipLaunchKernelGGL((join_kernel<T, DC>), dim3((unsigned)((n + 255) / 256)), dim3(256), 0, st, a, part);
+    }
     return (int)hipGetLastError();
 }
 
 }  // namespace
 }  // namespace att
 
-int launch_attention_fwd(int dtype, const AttnArgs &a, void *stream) {
-    if (a.Tq == 0 || a.Hq == 0) return 0;
-    return dtype == kBF16 ? att::fwd_t<bf16>(a, (hipStream_t)stream) : att::fwd_t<float>(a, (hipStream_t)stream);
+size_t attention_fwd_workspace(int dtype, const AttnArgs &a) {
+    if (a.Tq == 0) return 0;
+    return dtype == kBF16 ? ATT_COLUMNS(att::fwd_space, bf16, a) : ATT_COLUMNS(att::fwd_space, float, a);
+}
+
+int launch_attention_fwd(int dtype, const AttnArgs &a, void *ws, void *stream) {
+    if (a.Tq == 0) return 0;
+    hipStream_t st = (hipStream_t)stream;
+    return dtype == kBF16 ? ATT_COLUMNS(att::fwd_run, bf16, a, ws, st) : ATT_COLUMNS(att::fwd_run, float, a, ws, st);
 }
 
 int launch_pack_heads(int dtype, const void *src, int64_t ts, int64_t hs, int64_t ds, int64_t T, int H, int D, void *dst, int Dp,

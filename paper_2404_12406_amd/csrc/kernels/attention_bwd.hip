@@ -20,7 +20,7 @@ namespace att {
 
 // delta[h][t] = sum over d of g o, a row by L lanes.
 template <typename T, int L>
-__global__ __launch_bounds__(256) void delta_kernel(AttnArgs a) {
+__global__ __launch_bounds__(256) void delta_kernel(AttnArgs a, float *__restrict__ delta) {
     constexpr int V = Vec16<T>::N;
     const int l = threadIdx.x % L;
     const int64_t n = a.Tq * a.Hq;
@@ -36,7 +36,7 @@ __global__ __launch_bounds__(256) void delta_kernel(AttnArgs a) {
         }
 #pragma unroll
         for (int d = 1; d < L; d *= 2) s += __shfl_xor(s, d);
-        if (l == 0) a.delta[h * a.Tq + t] = s;
+        if (l == 0) delta[h * a.Tq + t] = s;
     }
 }
 
@@ -44,20 +44,29 @@ __global__ __launch_bounds__(256) void delta_kernel(AttnArgs a) {
 constexpr int kRows = 128;   // queries of a block of dq, keys of a block of dk and dv
 
 // Whether a wave has registers for both operands that it keeps: not for 256 fp32 elements.
-template <typename T, int DP> constexpr bool kHold = DP * sizeof(T) < 1024;
+template <typename T, int DC> constexpr bool kHold = DC * sizeof(T) < 1024;
 
-template <typename T, int DP>
-struct DqShape {
-    static constexpr int BN = DP * (int)sizeof(T) <= 256 ? 64 : 32;
-    static constexpr int OCC = DP * (int)sizeof(T) <= 256 ? 2 : 1;
+// What the kernels take besides: delta, and where they leave sums in fp32 if the other
+// side is divided: [split][rows][heads][DC].
+struct Parts {
+    const float *delta;
+    int splits;
+    float *a, *b;
 };
 
-template <typename T, int DP>
-__global__ __launch_bounds__(256, (DqShape<T, DP>::OCC)) void dq_kernel(AttnArgs a, int slots) {
+template <typename T, int DC>
+struct DqShape {
+    static constexpr int BN = kPitch<DC> * (int)sizeof(T) <= 256 ? 64 : 32;
+    static constexpr int OCC = DC * (int)sizeof(T) <= 256 ? 2 : 1;
+};
+
+template <typename T, int DC>
+__global__ __launch_bounds__(256, (DqShape<T, DC>::OCC)) void dq_kernel(AttnArgs a, int slots, Parts part) {
+    constexpr int DP = kPitch<DC>;
     typedef Mat<T> M;
     typedef Tile<T, DP> Ti;
     typedef typename M::Frag Frag;
-    constexpr int BN = DqShape<T, DP>::BN, NP = 32 / M::KC, BYTES = BN * Ti::RB;
+    constexpr int BN = DqShape<T, DC>::BN, NP = 32 / M::KC, BYTES = BN * Ti::RB;
     __shared__ __align__(16) char lds[4 * BYTES];
     const int lane = threadIdx.x & 63, w = uniform(threadIdx.x >> 6);
     const int logical = xcd_remap((int)blockIdx.x, (int)gridDim.x);
@@ -66,7 +75,9 @@ __global__ __launch_bounds__(256, (DqShape<T, DP>::OCC)) void dq_kernel(AttnArgs
     const int row0 = s.tile * kRows;
     if (s.tile < 0 || row0 >= s.na) return;
     const int shift = s.nb - s.na;
-    const int end = a.causal ? min(s.nb, min(row0 + kRows, s.na) + shift) : s.nb;
+    const int seen = a.causal ? max(0, min(s.nb, min(row0 + kRows, s.na) + shift)) : s.nb, steps = (seen + BN - 1) / BN;
+    const int begin = (int)((int64_t)steps * blockIdx.y / part.splits) * BN;
+    const int end = min(seen, (int)((int64_t)steps * (blockIdx.y + 1) / part.splits) * BN);
     const int wrow = row0 + 32 * w, rows = min(32, s.na - wrow);
     const int wend = rows <= 0 ? 0 : a.causal ? min(s.nb, wrow + rows + shift) : s.nb;
     const int wfull = a.causal ? min(s.nb, wrow + 1 + shift) : s.nb;
@@ -83,21 +94,21 @@ __global__ __launch_bounds__(256, (DqShape<T, DP>::OCC)) void dq_kernel(AttnArgs
         lk.issue(kp + k * lk.ts, s.nb - k, a.D, to, w);
         lv.issue(vp + k * lv.ts, s.nb - k, a.D, to + BYTES, w);
     };
-    if (end > 0) issue(0);
-    Rows<T, DP> q;
-    Rows<T, DP, kHold<T, DP>> g;
+    if (begin < end) issue(begin);
+    Rows<T, DC> q;
+    Rows<T, DC, kHold<T, DC>> g;
     q.init(static_cast<const T *>(a.q.p) + first * a.q.ts + head * a.q.hs, a.q.ts, rows, a.D, lane);
     g.init(static_cast<const T *>(a.go.p) + first * a.go.ts + head * a.go.hs, a.go.ts, rows, a.D, lane);
     float lse = INFINITY, delta = 0.f;
     if ((lane & 31) < rows) {
         lse = a.lse[(int64_t)head * a.Tq + first + (lane & 31)];
-        delta = a.delta[(int64_t)head * a.Tq + first + (lane & 31)];
+        delta = part.delta[(int64_t)head * a.Tq + first + (lane & 31)];
     }
     const float c = a.scale * kLog2e;
-    floatx16 acc[DP / 32];
+    floatx16 acc[DC / 32];
 #pragma unroll
-    for (int t = 0; t < DP / 32; ++t) acc[t] = zero16x();
-    for (int k = 0; k < end; k += BN) {
+    for (int t = 0; t < DC / 32; ++t) acc[t] = zero16x();
+    for (int k = begin; k < end; k += BN) {
         tile_sync();
         if (k + BN < end) issue(k + BN);
         const char *kt = lds + (k / BN & 1) * 2 * BYTES, *vt = kt + BYTES;
@@ -106,7 +117,7 @@ __global__ __launch_bounds__(256, (DqShape<T, DP>::OCC)) void dq_kernel(AttnArgs
             if (k + n >= wend) continue;
             floatx16 x = zero16x(), y = zero16x();
 #pragma unroll
-            for (int i = 0; i < DP / M::KC; ++i) {
+            for (int i = 0; i < DC / M::KC; ++i) {
                 x = M::mma(Ti::row_frag(kt, n, i, lane), q.get(i, lane), x);
                 y = M::mma(Ti::row_frag(vt, n, i, lane), g.get(i, lane), y);
             }
@@ -121,28 +132,36 @@ __global__ __launch_bounds__(256, (DqShape<T, DP>::OCC)) void dq_kernel(AttnArgs
             Frag d[NP];   // (an operand: in bf16 rounded)
 #pragma unroll
             for (int i = 0; i < NP; ++i) d[i] = as_frag<T>(x, i);
-            if (masked && any_wild<T, DP, 32>(kt, n, lane)) wild_product<T, DP, NP>(acc, kt, n, d, lane);
-            else add_product<T, DP, NP>(acc, kt, n, d, lane);
+            if (masked && any_wild<T, DP, 32>(kt, n, lane)) wild_product<T, DP, DC, NP>(acc, kt, n, d, lane);
+            else add_product<T, DP, DC, NP>(acc, kt, n, d, lane);
         }
     }
     tile_sync();
     if (rows <= 0) return;
-    store_rows<T, DP>(acc, a.scale, last < 0, lds + w * 32 * Ti::RB, static_cast<T *>(a.dq.p) + first * a.dq.ts + head * a.dq.hs, a.dq.ts,
+    if (part.splits > 1) {
+        store_sums<DC>(acc, part.a + ((blockIdx.y * a.Tq + first) * a.Hq + head) * DC, (int64_t)a.Hq * DC, rows, lane);
+        return;
+    }
+    store_rows<T, DP, DC>(acc, a.scale, last < 0, lds + w * 32 * Ti::RB, static_cast<T *>(a.dq.p) + first * a.dq.ts + head * a.dq.hs, a.dq.ts,
                       rows, a.D, lane);
 }
 
 // ------------------------------------------------------------------ dk, dv
-template <typename T, int DP>
+template <typename T, int DC, bool DK, bool DV>
 struct DkvShape {
-    static constexpr int BM = DP * (int)sizeof(T) <= 256 ? 64 : 32;   // queries of a step
+    static constexpr int BM = kPitch<DC> * (int)sizeof(T) <= 256 ? 64 : 32;   // queries of a step
+    // two blocks a CU where the sums and operands that a wave keeps leave registers for the rest
+    static constexpr int KEPT = DC / 2 * (DK + DV) + DC / 8 * (int)sizeof(T) * (DK ? 2 : 1);
+    static constexpr int OCC = kPitch<DC> * (int)sizeof(T) <= 256 && KEPT <= (sizeof(T) == 2 ? 128 : 96) ? 2 : 1;
 };
 
-template <typename T, int DP, bool DK, bool DV>
-__global__ __launch_bounds__(256, DP == 64 && sizeof(T) == 2 ? 2 : 1) void dkv_kernel(AttnArgs a, int slots) {
+template <typename T, int DC, bool DK, bool DV>
+__global__ __launch_bounds__(256, (DkvShape<T, DC, DK, DV>::OCC)) void dkv_kernel(AttnArgs a, int slots, Parts part) {
+    constexpr int DP = kPitch<DC>;
     typedef Mat<T> M;
     typedef Tile<T, DP> Ti;
     typedef typename M::Frag Frag;
-    constexpr int BM = DkvShape<T, DP>::BM, NP = 32 / M::KC, BYTES = BM * Ti::RB, C = DP / M::KC;
+    constexpr int BM = DkvShape<T, DC, DK, DV>::BM, NP = 32 / M::KC, BYTES = BM * Ti::RB, C = DC / M::KC;
     constexpr int STAGE = 2 * BYTES + 512;   // q, g, and 64 each of lse and delta
     __shared__ __align__(16) char lds[2 * STAGE];
     const int lane = threadIdx.x & 63, w = uniform(threadIdx.x >> 6);
@@ -170,19 +189,20 @@ __global__ __launch_bounds__(256, DP == 64 && sizeof(T) == 2 ? 2 : 1) void dkv_k
         lq.issue(reinterpret_cast<const char *>(static_cast<const T *>(a.q.p) + row * a.q.ts + head * a.q.hs), s.nb - at, a.D, to, w);
         lg.issue(reinterpret_cast<const char *>(static_cast<const T *>(a.go.p) + row * a.go.ts + head * a.go.hs), s.nb - at, a.D, to + BYTES, w);
         if (w < (DK ? 2 : 1))
-            g2::dma4s(g2::rsrc((w ? a.delta : a.lse) + head * a.Tq + row, (uint32_t)min(BM, s.nb - at) * 4), to + 2 * BYTES + 256 * w, word, 0);
+            g2::dma4s(g2::rsrc((w ? part.delta : a.lse) + head * a.Tq + row, (uint32_t)min(BM, s.nb - at) * 4), to + 2 * BYTES + 256 * w, word, 0);
     };
-    const int total = steps * group;
-    if (total > 0) issue(0);
-    Rows<T, DP> kf;
-    Rows<T, DP, DK && kHold<T, DP>> vf;
+    const int first_step = (int)((int64_t)steps * group * blockIdx.y / part.splits);
+    const int total = (int)((int64_t)steps * group * (blockIdx.y + 1) / part.splits);
+    if (first_step < total) issue(first_step);
+    Rows<T, DC> kf;
+    Rows<T, DC, DK && kHold<T, DC>> vf;
     kf.init(static_cast<const T *>(a.k.p) + first * a.k.ts + hk * a.k.hs, a.k.ts, keys, a.D, lane);
     if constexpr (DK) vf.init(static_cast<const T *>(a.v.p) + first * a.v.ts + hk * a.v.hs, a.v.ts, keys, a.D, lane);
     const float c = a.scale * kLog2e;
-    floatx16 dk[DP / 32], dv[DP / 32];
+    floatx16 dk[DC / 32], dv[DC / 32];
 #pragma unroll
-    for (int t = 0; t < DP / 32; ++t) dk[t] = dv[t] = zero16x();
-    for (int n = 0; n < total; ++n) {
+    for (int t = 0; t < DC / 32; ++t) dk[t] = dv[t] = zero16x();
+    for (int n = first_step; n < total; ++n) {
         tile_sync();
         if (n + 1 < total) issue(n + 1);
         const int at = begin + n % steps * BM;
@@ -218,70 +238,148 @@ __global__ __launch_bounds__(256, DP == 64 && sizeof(T) == 2 ? 2 : 1) void dkv_k
             if constexpr (DV) {
 #pragma unroll
                 for (int i = 0; i < NP; ++i) f[i] = as_frag<T>(x, i);
-                if (masked && any_wild<T, DP, 32>(gt, m, lane)) wild_product<T, DP, NP>(dv, gt, m, f, lane);
-                else add_product<T, DP, NP>(dv, gt, m, f, lane);
+                if (masked && any_wild<T, DP, 32>(gt, m, lane)) wild_product<T, DP, DC, NP>(dv, gt, m, f, lane);
+                else add_product<T, DP, DC, NP>(dv, gt, m, f, lane);
             }
             if constexpr (DK) {
 #pragma unroll
                 for (int i = 0; i < NP; ++i) f[i] = as_frag<T>(y, i);
-                if (masked && any_wild<T, DP, 32>(qt, m, lane)) wild_product<T, DP, NP>(dk, qt, m, f, lane);
-                else add_product<T, DP, NP>(dk, qt, m, f, lane);
+                if (masked && any_wild<T, DP, 32>(qt, m, lane)) wild_product<T, DP, DC, NP>(dk, qt, m, f, lane);
+                else add_product<T, DP, DC, NP>(dk, qt, m, f, lane);
             }
         }
     }
     tile_sync();
     if (keys <= 0) return;
+    if (part.splits > 1) {
+        const int64_t at = ((blockIdx.y * a.Tk + first) * a.Hk + hk) * DC;
+        if constexpr (DK) store_sums<DC>(dk, part.a + at, (int64_t)a.Hk * DC, keys, lane);
+        if constexpr (DV) store_sums<DC>(dv, part.b + at, (int64_t)a.Hk * DC, keys, lane);
+        return;
+    }
     char *mine = lds + w * 32 * Ti::RB;
     if constexpr (DK)
-        store_rows<T, DP>(dk, a.scale, false, mine, static_cast<T *>(a.dk.p) + first * a.dk.ts + hk * a.dk.hs, a.dk.ts, keys, a.D, lane);
+        store_rows<T, DP, DC>(dk, a.scale, false, mine, static_cast<T *>(a.dk.p) + first * a.dk.ts + hk * a.dk.hs, a.dk.ts, keys, a.D, lane);
     if constexpr (DV)
-        store_rows<T, DP>(dv, 1.f, false, mine, static_cast<T *>(a.dv.p) + first * a.dv.ts + hk * a.dv.hs, a.dv.ts, keys, a.D, lane);
+        store_rows<T, DP, DC>(dv, 1.f, false, mine, static_cast<T *>(a.dv.p) + first * a.dv.ts + hk * a.dv.hs, a.dv.ts, keys, a.D, lane);
+}
+
+// A gradient from its partial sums: a vector a thread.
+struct Sum {
+    HeadsView out;
+    const float *part;
+    float scale;
+};
+
+template <typename T>
+__global__ __launch_bounds__(256) void sum_kernel(Sum a, Sum b, int64_t rows, int H, int D, int cols, int splits) {
+    constexpr int V = Vec16<T>::N;
+    const Sum &s = blockIdx.y ? b : a;
+    const int per = D / V;
+    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (i >= rows * H * per) return;
+    const int64_t row = i / per, t = row / H;
+    const int u = (int)(i - row * per), h = (int)(row - t * H);
+    float v[V];
+#pragma unroll
+    for (int e = 0; e < V; ++e) v[e] = 0.f;
+    for (int n = 0; n < splits; ++n) {
+        const float *p = s.part + (n * rows * H + row) * cols + u * V;
+#pragma unroll
+        for (int e = 0; e < V; ++e) v[e] += p[e];
+    }
+    Vec16<T> o;
+#pragma unroll
+    for (int e = 0; e < V; ++e) o.e[e] = from_f32<T>(v[e] * s.scale);
+    store16(static_cast<T *>(s.out.p) + t * s.out.ts + h * s.out.hs + u * V, o);
 }
 
 // ------------------------------------------------------------------ host
 namespace {
 
-template <typename T, int DP>
-void run(const AttnArgs &a, hipStream_t st) {
+size_t al256(size_t n) { return (n + 255) / 256 * 256; }
+
+// What a backward lays out: delta, then partial sums of dq, dk and dv.
+struct Plan {
+    int dq_splits, dkv_splits;
+    size_t dq_at, dk_at, dv_at, bytes;
+};
+
+template <typename T, int DC>
+Plan plan(const AttnArgs &a, bool dq, bool dk, bool dv) {
     const bool packed = a.qoff != nullptr;
-    if ((a.dq.p || a.dk.p) && a.Tq > 0) {
-        constexpr int L = DP / Vec16<T>::N;
-        const int64_t blocks = (a.Tq * a.Hq + 256 / L - 1) / (256 / L);
-        hipLaunchKernelGGL((delta_kernel<T, L>), dim3((unsigned)std::min<int64_t>(blocks, 8192)), dim3(256), 0, st, a);
-    }
-    if (a.dq.p && a.Tq > 0) {
-        const int64_t slots = span_slots(packed, a.n, a.Tq, kRows);
-        hipLaunchKernelGGL((dq_kernel<T, DP>), dim3((unsigned)(slots * a.Hq)), dim3(256), 0, st, a, (int)slots);
-    }
-    if ((a.dk.p || a.dv.p) && a.Tk > 0) {
-        const int64_t slots = span_slots(packed, a.n, a.Tk, kRows);
-        const dim3 grid((unsigned)(slots * a.Hk));
-        // (both sums of 512 bytes a row, and their operands, are more than a wave's registers)
-        constexpr bool both = DP * sizeof(T) < 512;
-        if constexpr (both) {
-            if (a.dk.p && a.dv.p) {
-                hipLaunchKernelGGL((dkv_kernel<T, DP, true, true>), grid, dim3(256), 0, st, a, (int)slots);
-                return;
-            }
-        }
-        if (a.dk.p) hipLaunchKernelGGL((dkv_kernel<T, DP, true, false>), grid, dim3(256), 0, st, a, (int)slots);
-        if (a.dv.p) hipLaunchKernelGGL((dkv_kernel<T, DP, false, true>), grid, dim3(256), 0, st, a, (int)slots);
-    }
+    const int64_t n = packed ? std::max(a.n, 1) : 1, group = a.Hq / a.Hk;
+    Plan p{1, 1, 0, 0, 0, 0};
+    if (dq) p.dq_splits = span_splits(span_slots(packed, a.n, a.Tq, kRows) * a.Hq, a.Tk / n / DqShape<T, DC>::BN, a.Tq * a.Hq * DC * 4);
+    if (dk || dv)
+        p.dkv_splits = span_splits(span_slots(packed, a.n, a.Tk, kRows) * a.Hk, a.Tq / n * group / DkvShape<T, DC, true, true>::BM,
+                                   a.Tk * a.Hk * DC * 8);
+    const size_t keys = p.dkv_splits > 1 ? al256((size_t)p.dkv_splits * a.Tk * a.Hk * DC * sizeof(float)) : 0;
+    p.dq_at = dq || dk ? al256((size_t)a.Tq * a.Hq * sizeof(float)) : 0;
+    p.dk_at = p.dq_at + (p.dq_splits > 1 ? al256((size_t)p.dq_splits * a.Tq * a.Hq * DC * sizeof(float)) : 0);
+    p.dv_at = p.dk_at + (dk ? keys : 0);
+    p.bytes = p.dv_at + (dv ? keys : 0);
+    return p;
 }
 
-template <typename T>
-int bwd_t(const AttnArgs &a, hipStream_t st) {
-    if (a.D <= 64) run<T, 64>(a, st);
-    else if (a.D <= 128) run<T, 128>(a, st);
-    else run<T, 256>(a, st);
+template <typename T, int DC>
+size_t space(const AttnArgs &a, bool dq, bool dk, bool dv) {
+    return plan<T, DC>(a, dq, dk, dv).bytes;
+}
+
+template <typename T, int DC>
+int run(const AttnArgs &a, char *ws, hipStream_t st) {
+    const bool packed = a.qoff != nullptr, dq = a.dq.p, dk = a.dk.p, dv = a.dv.p;
+    const Plan p = plan<T, DC>(a, dq, dk, dv);
+    constexpr int V = Vec16<T>::N;
+    float *delta = reinterpret_cast<float *>(ws);
+    if ((dq || dk) && a.Tq > 0) {
+        constexpr int L = kPitch<DC> / V;
+        const int64_t blocks = (a.Tq * a.Hq + 256 / L - 1) / (256 / L);
+        hipLaunchKernelGGL((delta_kernel<T, L>), dim3((unsigned)std::min<int64_t>(blocks, 8192)), dim3(256), 0, st, a, delta);
+    }
+    if (dq && a.Tq > 0) {
+        const int64_t slots = span_slots(packed, a.n, a.Tq, kRows);
+        const Parts part{delta, p.dq_splits, reinterpret_cast<float *>(ws + p.dq_at), nullptr};
+        hipLaunchKernelGGL((dq_kernel<T, DC>), dim3((unsigned)(slots * a.Hq), (unsigned)part.splits), dim3(256), 0, st, a, (int)slots, part);
+        if (part.splits > 1) {
+            const Sum s{a.dq, part.a, a.scale};
+            hipLaunchKernelGGL(sum_kernel<T>, dim3((unsigned)((a.Tq * a.Hq * (a.D / V) + 255) / 256)), dim3(256), 0, st, s, s, a.Tq, a.Hq,
+                               a.D, DC, part.splits);
+        }
+    }
+    if ((dk || dv) && a.Tk > 0) {
+        const int64_t slots = span_slots(packed, a.n, a.Tk, kRows);
+        const Parts part{delta, p.dkv_splits, reinterpret_cast<float *>(ws + p.dk_at), reinterpret_cast<float *>(ws + p.dv_at)};
+        const dim3 grid((unsigned)(slots * a.Hk), (unsigned)part.splits);
+        // (both sums of 512 bytes a row, and their operands, are more than a wave's registers)
+        constexpr bool both = DC * sizeof(T) < 384;
+        if (both && dk && dv) {
+            if constexpr (both) hipLaunchKernelGGL((dkv_kernel<T, DC, true, true>), grid, dim3(256), 0, st, a, (int)slots, part);
+        } else {
+            if (dk) hipLaunchKernelGGL((dkv_kernel<T, DC, true, false>), grid, dim3(256), 0, st, a, (int)slots, part);
+            if (dv) hipLaunchKernelGGL((dkv_kernel<T, DC, false, true>), grid, dim3(256), 0, st, a, (int)slots, part);
+        }
+        if (part.splits > 1) {
+            const Sum k{a.dk, part.a, a.scale}, v{a.dv, part.b, 1.f};
+            hipLaunchKernelGGL(sum_kernel<T>, dim3((unsigned)((a.Tk * a.Hk * (a.D / V) + 255) / 256), dk && dv ? 2 : 1), dim3(256), 0, st,
+                               dk ? k : v, v, a.Tk, a.Hk, a.D, DC, part.splits);
+        }
+    }
     return (int)hipGetLastError();
 }
 
 }  // namespace
 }  // namespace att
 
-int launch_attention_bwd(int dtype, const AttnArgs &a, void *stream) {
-    return dtype == kBF16 ? att::bwd_t<bf16>(a, (hipStream_t)stream) : att::bwd_t<float>(a, (hipStream_t)stream);
+size_t attention_bwd_workspace(int dtype, const AttnArgs &a, bool dq, bool dk, bool dv) {
+    return dtype == kBF16 ? ATT_COLUMNS(att::space, bf16, a, dq, dk, dv) : ATT_COLUMNS(att::space, float, a, dq, dk, dv);
+}
+
+int launch_attention_bwd(int dtype, const AttnArgs &a, void *ws, void *stream) {
+    char *w = static_cast<char *>(ws);
+    hipStream_t st = (hipStream_t)stream;
+    return dtype == kBF16 ? ATT_COLUMNS(att::run, bf16, a, w, st) : ATT_COLUMNS(att::run, float, a, w, st);
 }
 
 }  // namespace ms

@@ -11,6 +11,8 @@
 // moves between lanes.
 #pragma once
 
+#include <algorithm>
+
 #include "block_math.h"
 #include "lds_dma.h"
 
@@ -37,6 +39,10 @@ template <> struct Mat<float> {
 
 typedef short v4i16 __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) v4i16 lds_v4i16_t;
+
+// How a call of DC padded columns is laid out: rows in LDS have DP of them, a power of two
+// (the swizzle's units are eight at a time).
+template <int DC> constexpr int kPitch = DC <= 64 ? 64 : DC <= 128 ? 128 : 256;
 
 // Rows of DP elements in LDS.  The 16-byte units of each eight are swapped by the row, so
 // that eight rows' units of one number lie in different banks (row_frag) and so do the
@@ -149,6 +155,14 @@ inline int64_t span_slots(bool packed, int n, int64_t Ta, int rows) {
     return packed ? Ta / rows + n + 2 : (Ta + rows - 1) / rows;
 }
 
+// Blocks of few rows' worth of work divide their other side: `splits` of them, of `steps`
+// steps on average, where that leaves each two steps and the partial sums below 24 MiB.
+// attend_ragged's sizes (fp32, 5 sequences, 1777 x 6 heads of 72): see attention_bwd.hip.
+inline int span_splits(int64_t blocks, int64_t steps, int64_t bytes) {
+    const int64_t want = 512 / std::max<int64_t>(blocks, 1), most = (int64_t(24) << 20) / std::max<int64_t>(bytes, 1);
+    return (int)std::max<int64_t>(1, std::min({want, steps / 2, most}));
+}
+
 // The sum (maximum) of a lane's value and that of the lane 32 away.
 __device__ __forceinline__ floatx2 halves(float v) {
     const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
@@ -199,14 +213,14 @@ __device__ __forceinline__ bool any_wild(const char *tile, int r0, int lane) {
 
 // acc += columns of `tile` times b (N chunks), a row at a time, where a weight of zero
 // takes no part whatever its row holds: for tiles with masked places where any_wild().
-template <typename T, int DP, int N>
-__device__ __forceinline__ void wild_product(floatx16 (&acc)[DP / 32], const char *tile, int r0, const typename Mat<T>::Frag (&b)[N], int lane) {
+template <typename T, int DP, int DC, int N>
+__device__ __forceinline__ void wild_product(floatx16 (&acc)[DC / 32], const char *tile, int r0, const typename Mat<T>::Frag (&b)[N], int lane) {
     typedef Mat<T> M;
     typedef Tile<T, DP> Ti;
     constexpr int PER = 4 / (int)sizeof(T);   // elements of a word
     const int n = lane & 31, hh = lane >> 5;
 #pragma unroll
-    for (int t = 0; t < DP / 32; ++t) {
+    for (int t = 0; t < DC / 32; ++t) {
         __builtin_amdgcn_sched_barrier(0);   // (one tile of columns after the other: together they spill)
 #pragma unroll 1
         for (int row = 0; row < N * M::KC; ++row) {
@@ -231,23 +245,23 @@ __device__ __forceinline__ void wild_product(floatx16 (&acc)[DP / 32], const cha
 }
 
 // acc += columns of `tile` times b.
-template <typename T, int DP, int N>
-__device__ __forceinline__ void add_product(floatx16 (&acc)[DP / 32], const char *tile, int r0, const typename Mat<T>::Frag (&b)[N], int lane) {
+template <typename T, int DP, int DC, int N>
+__device__ __forceinline__ void add_product(floatx16 (&acc)[DC / 32], const char *tile, int r0, const typename Mat<T>::Frag (&b)[N], int lane) {
 #pragma unroll
-    for (int t = 0; t < DP / 32; ++t)
+    for (int t = 0; t < DC / 32; ++t)
 #pragma unroll
         for (int i = 0; i < N; ++i) acc[t] = Mat<T>::mma(Tile<T, DP>::col_frag(tile, r0, t, i, lane), b[i], acc[t]);
 }
 
 // A wave's 32 rows of results, which lie as columns of 32x32 tiles (x scale, or zeros), to
 // memory by way of its own part of LDS: whole 16-byte vectors side by side.
-template <typename T, int DP>
-__device__ __forceinline__ void store_rows(const floatx16 (&acc)[DP / 32], float scale, bool zero, char *lds, T *out, int64_t ts, int rows, int D,
+template <typename T, int DP, int DC>
+__device__ __forceinline__ void store_rows(const floatx16 (&acc)[DC / 32], float scale, bool zero, char *lds, T *out, int64_t ts, int rows, int D,
                                            int lane) {
     typedef Tile<T, DP> Ti;
     const int n = lane & 31, hh = lane >> 5;
 #pragma unroll
-    for (int t = 0; t < DP / 32; ++t)
+    for (int t = 0; t < DC / 32; ++t)
 #pragma unroll
         for (int g = 0; g < 4; ++g) {
             T v[4];
@@ -266,9 +280,25 @@ __device__ __forceinline__ void store_rows(const floatx16 (&acc)[DP / 32], float
     }
 }
 
+// The same as sums in fp32, [rows][DC].
+template <int DC>
+__device__ __forceinline__ void store_sums(const floatx16 (&acc)[DC / 32], float *out, int64_t ts, int rows, int lane) {
+    const int n = lane & 31, hh = lane >> 5;
+    if (n >= rows) return;
+#pragma unroll
+    for (int t = 0; t < DC / 32; ++t)
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+            floatx4 v;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) v[j] = acc[t][4 * g + j];
+            *reinterpret_cast<floatx4 *>(out + n * ts + 32 * t + 8 * g + 4 * hh) = v;
+        }
+}
+
 // A wave's 32 rows as the column operand of a product: row l % 32, chunk c; zeros past
 // `rows` and D.
-template <typename T, int DP>
+template <typename T>
 __device__ __forceinline__ typename Mat<T>::Frag load_row(const T *p, int64_t ts, int rows, int D, int c, int lane) {
     const int n = lane & 31, d = (2 * c + (lane >> 5)) * Mat<T>::V;
     typename Mat<T>::Frag v;
@@ -279,9 +309,9 @@ __device__ __forceinline__ typename Mat<T>::Frag load_row(const T *p, int64_t ts
 }
 
 // All of them, held in registers; or (HOLD false, where they are too many) read where they are used.
-template <typename T, int DP, bool HOLD = true>
+template <typename T, int DC, bool HOLD = true>
 struct Rows {
-    static constexpr int C = DP / Mat<T>::KC;
+    static constexpr int C = DC / Mat<T>::KC;
     typename Mat<T>::Frag f[HOLD ? C : 1];
     const T *p;
     int64_t ts;
@@ -290,13 +320,28 @@ struct Rows {
         p = p_, ts = ts_, rows = rows_, D = D_;
         if constexpr (HOLD)
 #pragma unroll
-            for (int c = 0; c < C; ++c) f[c] = load_row<T, DP>(p, ts, rows, D, c, lane);
+            for (int c = 0; c < C; ++c) f[c] = load_row<T>(p, ts, rows, D, c, lane);
+    }
+    // They have arrived.  (Where no later wait for all loads is known to the compiler, it would
+    // put one in front of their first use, in the loop.)
+    __device__ __forceinline__ void settle() {
+        if constexpr (HOLD)
+#pragma unroll
+            for (int c = 0; c < C; ++c) asm volatile("" : "+v"(f[c]));
     }
     __device__ __forceinline__ typename Mat<T>::Frag get(int c, int lane) const {
         if constexpr (HOLD) return f[c];
-        else return load_row<T, DP>(p, ts, rows, D, c, lane);
+        else return load_row<T>(p, ts, rows, D, c, lane);
     }
 };
 
 }  // namespace att
 }  // namespace ms
+
+// F<T, columns>(a, ...) for the columns that heads of a.D elements take.
+#define ATT_COLUMNS(F, T, a, ...)                                    \
+    ((a).D <= 64    ? F<T, 64>(a __VA_OPT__(, ) __VA_ARGS__)         \
+     : (a).D <= 96  ? F<T, 96>(a __VA_OPT__(, ) __VA_ARGS__)         \
+     : (a).D <= 128 ? F<T, 128>(a __VA_OPT__(, ) __VA_ARGS__)        \
+     : (a).D <= 192 ? F<T, 192>(a __VA_OPT__(, ) __VA_ARGS__)        \
+                    : F<T, 256>(a __VA_OPT__(, ) __VA_ARGS__))

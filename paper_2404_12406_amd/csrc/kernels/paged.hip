@@ -4,9 +4,12 @@
 // Bound: memory, one read of the keys and values that are used, however many query heads
 // share them: these are the columns of a 32x32 tile (attn_tile.h), up to 32 at once.
 //  * A block takes `per` keys of one sequence and head of the cache, and each of its waves
-//    32 keys at a time on its own: a wave's loads go straight into its own part of LDS, two
-//    steps of them in flight, and nothing waits for another wave before the end.
-//  * The pages of a step's keys are loaded a step before its keys, into LDS too, so that
+//    32 keys at a time on its own: a wave's loads go straight into its own part of LDS, and
+//    nothing waits for another wave before the end.  The next keys are loaded as soon as
+//    this step's scores are taken, the next values after its sums; eight such waves a CU
+//    keep some 100 KiB in flight.  (Two steps ahead, with half as many waves, was slower:
+//    one wave a SIMD has to wait for each of its own instructions.)
+//  * The pages of a step's keys are loaded a step before these, into LDS too, so that
 //    the loads follow each other in one order and the waits count them.
 //  * A key's row is looked up by itself, so pages may have any size and end anywhere.  Rows
 //    past the length read as zeros, whatever lies there; rows of a page that is none make
@@ -42,20 +45,23 @@ __device__ __forceinline__ void landed() {
 template <typename T, int DP>
 struct PagedShape {
     static constexpr int RB = DP * (int)sizeof(T);
-    static constexpr int NW = RB <= 256 ? 4 : 1024 / RB;       // waves: two steps of 64 rows each in 128 KiB
-    static constexpr int STAGE = 64 * RB, WAVE = 2 * STAGE + 3 * 256;   // + pages of two steps, rows of one
-    static constexpr int LOADS = STAGE / 1024;
+    static constexpr int NW = RB <= 256 ? 4 : 1024 / RB;               // waves of a block
+    static constexpr int HALF = 32 * RB, WAVE = 2 * HALF + 768;        // keys, values, pages of two steps
+    static constexpr int LOADS = HALF / 1024;                          // of a step's keys, of its values
+    static constexpr int PER_SIMD = RB <= 256 ? 2 : 1;                 // waves: two blocks a CU
+    static constexpr int LD = DP + 4;                                  // a row of sums at the end
+    static_assert(32 * LD * 4 <= WAVE, "the sums fit where the keys were");
 };
 
 // FAST: rows of the cache are whole 16-byte vectors, so aligned; else they go through
 // registers, any number of elements side by side.
 template <typename T, int DP, bool FAST>
-__global__ __launch_bounds__((64 * PagedShape<T, DP>::NW), 1) void paged_kernel(PagedArgs a, int splits, int per, float *__restrict__ part) {
+__global__ __launch_bounds__((64 * PagedShape<T, DP>::NW), (PagedShape<T, DP>::PER_SIMD)) void paged_kernel(PagedArgs a, int splits, int per, float *__restrict__ part) {
     typedef Mat<T> M;
     typedef Tile<T, DP> Ti;
     typedef PagedShape<T, DP> Sh;
     typedef typename M::Frag Frag;
-    constexpr int NW = Sh::NW, NP = 32 / M::KC, LD = DP + 4;
+    constexpr int NW = Sh::NW, NP = 32 / M::KC, LD = Sh::LD;
     __shared__ __align__(16) char lds[NW * Sh::WAVE + NW * 256];
     const int lane = threadIdx.x & 63, w = uniform(threadIdx.x >> 6), hh = lane >> 5;
     const int group = a.Hq / a.Hk;
@@ -69,83 +75,104 @@ __global__ __launch_bounds__((64 * PagedShape<T, DP>::NW), 1) void paged_kernel(
     const int begin = (int)min((int64_t)split * per, (int64_t)len), end = (int)min((int64_t)begin + per, (int64_t)len);
     if (split > 0 && begin >= end) return;   // (the join knows how many there are)
 
-    char *mine = lds + w * Sh::WAVE, *pages = mine + 2 * Sh::STAGE, *rows = pages + 512;
+    char *mine = lds + w * Sh::WAVE, *kt = mine, *vt = mine + Sh::HALF, *pages = mine + 2 * Sh::HALF;
     const int32_t *table = a.tables + (int64_t)b * a.width;
-    // the pages of step i's keys
+    const uint32_t magic = a.page > 1 ? (uint32_t)((uint64_t(1) << 32) / (uint32_t)a.page) : ~0u;
+    auto divide = [&](int key, int &in) {   // by the page size
+        int q = (int)__umulhi((uint32_t)key, magic);
+        in = key - q * a.page;
+        if (in >= a.page) {
+            in -= a.page;
+            ++q;
+        }
+        return q;
+    };
+    // Step i: the places of its keys in their pages; their pages are asked for.
     auto look = [&](int i) {
         const int key = min(begin + (i * NW + w) * 32 + (lane & 31), len - 1);
-        far4(table + key / a.page, pages + (i & 1) * 256);
+        int in;
+        far4(table + divide(key, in), pages + (i & 1) * 256);
+        return in;
     };
-    uint32_t bad_of[2] = {0u, 0u};   // keys whose page is none
-    auto issue = [&](int i, uint32_t &bad) {
-        const int key = begin + (i * NW + w) * 32 + (lane & 31);
+    uint32_t at[Sh::LOADS];   // rows of the cache that this lane loads from, ~0 for none
+    bool whole;               // of 32 keys and all of the columns
+    // The rows of step i; which keys have a page that is none.
+    auto find = [&](int i, int in) {
+        const int k = begin + (i * NW + w) * 32;
         const int pg = *reinterpret_cast<const int *>(pages + (i & 1) * 256 + 4 * (lane & 31));
-        const bool used = key < end, none = used && (pg < 0 || pg >= a.pages);
-        bad = (uint32_t)__ballot(none);
-        const uint32_t row = used && !none ? ((uint32_t)pg * (uint32_t)a.Hk + (uint32_t)hk) * (uint32_t)a.page + (uint32_t)(key % a.page) : ~0u;
-        *reinterpret_cast<uint32_t *>(rows + 4 * lane) = row;   // (twice: both halves hold the same keys)
-        __atomic_signal_fence(__ATOMIC_SEQ_CST);
-        char *to = mine + (i & 1) * Sh::STAGE;
+        const bool used = k + (lane & 31) < end, none = used && (uint32_t)pg >= (uint32_t)a.pages;
+        const uint32_t row = used && !none ? ((uint32_t)pg * (uint32_t)a.Hk + (uint32_t)hk) * (uint32_t)a.page + (uint32_t)in : ~0u;
+        const uint32_t bad = (uint32_t)__ballot(none);
+        whole = k + 32 <= end && !bad && a.D == DP;
 #pragma unroll
-        for (int n = 0; n < Sh::LOADS / 2; ++n) {
-            const int idx = n * 64 + lane, r = idx / Ti::U, unit = (idx % Ti::U) ^ Ti::swz(r);
-            const uint32_t at = *reinterpret_cast<const uint32_t *>(rows + 4 * r);
-            const bool there = at != ~0u && unit * M::V < a.D;
-            const T *k = static_cast<const T *>(a.kp) + (int64_t)at * a.D, *v = static_cast<const T *>(a.vp) + (int64_t)at * a.D;
+        for (int n = 0; n < Sh::LOADS; ++n) at[n] = (uint32_t)__shfl((int)row, (n * 64 + lane) / Ti::U);
+        return bad;
+    };
+    auto issue = [&](const void *from, char *to) {
+        const char *base = static_cast<const char *>(from);
+        const uint32_t bytes = (uint32_t)a.D * (uint32_t)sizeof(T);
+        if (FAST && whole) {
+#pragma unroll
+            for (int n = 0; n < Sh::LOADS; ++n) {
+                const int idx = n * 64 + lane, unit = (idx % Ti::U) ^ Ti::swz(idx / Ti::U);
+                far16(base + ((uint64_t)at[n] * bytes + (uint32_t)(unit * 16)), to + n * 1024);
+            }
+            return;
+        }
+#pragma unroll
+        for (int n = 0; n < Sh::LOADS; ++n) {
+            const int idx = n * 64 + lane, unit = (idx % Ti::U) ^ Ti::swz(idx / Ti::U);
+            const bool there = at[n] != ~0u && unit * M::V < a.D;
+            const char *p = base + (uint64_t)at[n] * bytes;
             if constexpr (FAST) {
-                far16(there ? (const void *)(k + unit * M::V) : &kZeros, to + n * 1024);
-                far16(there ? (const void *)(v + unit * M::V) : &kZeros, to + Sh::STAGE / 2 + n * 1024);
+                far16(there ? (const void *)(p + unit * 16) : &kZeros, to + n * 1024);
             } else {
-                Vec16<T> kv = zero16<T>(), vv = zero16<T>();
-                if (there) {
-                    kv = load_vec<T>(k, unit * M::V, a.D);
-                    vv = load_vec<T>(v, unit * M::V, a.D);
-                }
-                store16(reinterpret_cast<T *>(to + n * 1024 + lane * 16), kv);
-                store16(reinterpret_cast<T *>(to + Sh::STAGE / 2 + n * 1024 + lane * 16), vv);
+                Vec16<T> v = zero16<T>();
+                if (there) v = load_vec<T>(reinterpret_cast<const T *>(p), unit * M::V, a.D);
+                store16(reinterpret_cast<T *>(to + n * 1024 + lane * 16), v);
             }
         }
     };
     const int keys = end - begin - w * 32, steps = keys > 0 ? (keys + 32 * NW - 1) / (32 * NW) : 0;   // the wave's
     Rows<T, DP, (DP * sizeof(T) < 1024)> q;   // (256 fp32 elements are too many to hold)
     q.init(static_cast<const T *>(a.q) + b * a.qts + head * a.qhs, a.qhs, heads, a.D, lane);
+    q.settle();
+    uint32_t bad = 0u, bad1 = 0u;   // of this step and the next
+    int in = 0;
     if (steps > 0) {
-        look(0);
+        in = look(0);
         landed<0>();
-        if (steps > 1) look(1);
-        issue(0, bad_of[0]);
+        bad = find(0, in);
+        in = look(1);
+        issue(a.kp, kt);
+        issue(a.vp, vt);
     }
     const float c = a.scale * kLog2e;
     float m = -INFINITY, l = 0.f;
     floatx16 acc[DP / 32];
 #pragma unroll
     for (int t = 0; t < DP / 32; ++t) acc[t] = zero16x();
+    // On their way at the start of a step, in order: the next one's pages, its keys, its values.
     for (int i = 0; i < steps; ++i) {
-        if (i + 1 < steps) {
-            landed<Sh::LOADS>();   // the pages of the next step; this step's keys may be under way
-            g2::wait_lgkm0();      // the stage that is loaded now has been read
-            if (i + 2 < steps) {
-                look(i + 2);
-                issue(i + 1, bad_of[1]);
-                landed<Sh::LOADS + 1>();
-            } else {
-                issue(i + 1, bad_of[1]);
-                landed<Sh::LOADS>();
-            }
-        } else {
-            landed<0>();
-        }
-        const char *kt = mine + (i & 1) * Sh::STAGE, *vt = kt + Sh::STAGE / 2;
+        const bool more = i + 1 < steps;
+        landed<FAST ? Sh::LOADS : 0>();   // all but the values
         floatx16 x = zero16x();
 #pragma unroll
         for (int n = 0; n < DP / M::KC; ++n) x = M::mma(Ti::row_frag(kt, 0, n, lane), q.get(n, lane), x);
+        if (more) {
+            bad1 = find(i + 1, in);
+            in = look(i + 2);
+            __atomic_signal_fence(__ATOMIC_SEQ_CST);
+            g2::wait_lgkm0();   // (the keys have been read)
+            issue(a.kp, kt);
+        }
         const int k = begin + (i * NW + w) * 32;
-        if (k + 32 > end || bad_of[0]) {
+        if (k + 32 > end || bad) {
 #pragma unroll
             for (int n = 0; n < 16; ++n) {
                 const int r = 8 * (n >> 2) + 4 * hh + (n & 3);
-                if (k + r >= end) x[n] = -INFINITY;
-                else if (bad_of[0] >> r & 1) x[n] = NAN;
+                x[n] = bad >> r & 1 ? NAN : x[n];
+                x[n] = k + r >= end ? -INFINITY : x[n];
             }
         }
         float top = x[0];
@@ -170,8 +197,15 @@ __global__ __launch_bounds__((64 * PagedShape<T, DP>::NW), 1) void paged_kernel(
         Frag p[NP];
 #pragma unroll
         for (int n = 0; n < NP; ++n) p[n] = as_frag<T>(x, n);
-        add_product<T, DP, NP>(acc, vt, 0, p, lane);
-        bad_of[0] = bad_of[1];
+        if (more) landed<FAST ? Sh::LOADS + 1 : 0>();   // the values
+        else landed<0>();
+        add_product<T, DP, DP, NP>(acc, vt, 0, p, lane);
+        if (more) {
+            __atomic_signal_fence(__ATOMIC_SEQ_CST);
+            g2::wait_lgkm0();   // (and the values)
+            issue(a.vp, vt);
+        }
+        bad = bad1;
     }
     l = both_sum(l);
     // the waves' sums side by side: [queries][LD] each, and their statistics
@@ -207,39 +241,59 @@ __global__ __launch_bounds__((64 * PagedShape<T, DP>::NW), 1) void paged_kernel(
         if (splits == 1) {
             static_cast<T *>(a.o)[b * a.ots + (head + n) * a.ohs + d] = from_f32<T>(wrong ? NAN : len == 0 ? 0.f : o / sum);
         } else {
-            float *to = part + (((int64_t)b * a.Hq + head + n) * splits + split) * (a.D + 2);
-            to[d] = o;
-            if (d == 0) {
-                to[a.D] = top;
-                to[a.D + 1] = sum;
-            }
+            const int64_t at = ((int64_t)b * a.Hq + head + n) * splits + split;
+            part[2 * (int64_t)a.n * a.Hq * splits + at * a.D + d] = o;
+            if (d == 0) reinterpret_cast<floatx2 *>(part)[at] = floatx2{top, sum};
         }
     }
 }
 
-// o of the splits that a sequence has: a block a query head.
-template <typename T>
+// o of the splits that a sequence has: a block a query head.  Its threads are DL columns
+// and 256 / DL groups, of every so many splits each.
+template <typename T, int DL>
 __global__ __launch_bounds__(256) void join_kernel(PagedArgs a, int splits, int per, const float *__restrict__ part) {
-    const int b = (int)(blockIdx.x / a.Hq), head = (int)(blockIdx.x % a.Hq), d = threadIdx.x;
-    if (d >= a.D) return;
+    constexpr int G = 256 / DL;
+    __shared__ float weight[256], red[8], meet[G][DL + 1];
+    const int b = (int)(blockIdx.x / a.Hq), head = (int)(blockIdx.x % a.Hq), d = threadIdx.x % DL, g = threadIdx.x / DL;
     const int len = a.lengths[b];
-    const int n = (int)(((int64_t)max(len, 0) + per - 1) / per);
-    float out = 0.f;
-    if (len > (int64_t)a.width * a.page) {
-        out = NAN;
-    } else if (n > 0) {
-        const float *p = part + (int64_t)blockIdx.x * splits * (a.D + 2);
-        const float c = a.scale * kLog2e;
-        float top = -INFINITY, sum = 0.f, o = 0.f;
-        for (int s = 0; s < n; ++s) top = fmaxf(top, p[s * (a.D + 2) + a.D]);
-        for (int s = 0; s < n; ++s) {
-            const float m = p[s * (a.D + 2) + a.D], f = m == top ? 1.f : __builtin_amdgcn_exp2f((m - top) * c);
-            sum += f * p[s * (a.D + 2) + a.D + 1];
-            o += f * p[s * (a.D + 2) + d];
+    const bool wrong = len > (int64_t)a.width * a.page;
+    const int n = wrong ? 0 : (int)(((int64_t)max(len, 0) + per - 1) / per);
+    const float c = a.scale * kLog2e;
+    const floatx2 *stat = reinterpret_cast<const floatx2 *>(part) + (int64_t)blockIdx.x * splits;
+    const float *p = part + 2 * (int64_t)a.n * a.Hq * splits + (int64_t)blockIdx.x * splits * a.D;
+    float top = -INFINITY;
+    for (int s = threadIdx.x; s < n; s += 256) top = fmaxf(top, stat[s].x);
+#pragma unroll
+    for (int k = 1; k < 64; k *= 2) top = fmaxf(top, __shfl_xor(top, k));
+    if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = top;
+    __syncthreads();
+    top = fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
+    float o = 0.f, sum = 0.f;
+    for (int s0 = 0; s0 < n; s0 += 256) {
+        const int m = min(256, n - s0);
+        if (threadIdx.x < m) {
+            const floatx2 st = stat[s0 + threadIdx.x];
+            const float f = st.x == top ? 1.f : __builtin_amdgcn_exp2f((st.x - top) * c);
+            weight[threadIdx.x] = f;
+            sum += f * st.y;
         }
-        out = o / sum;
+        __syncthreads();
+        if (d < a.D) {
+#pragma unroll 4
+            for (int s = g; s < m; s += G) o += weight[s] * p[(int64_t)(s0 + s) * a.D + d];
+        }
+        __syncthreads();
     }
-    static_cast<T *>(a.o)[b * a.ots + head * a.ohs + d] = from_f32<T>(out);
+#pragma unroll
+    for (int k = 1; k < 64; k *= 2) sum += __shfl_xor(sum, k);
+    if ((threadIdx.x & 63) == 0) red[4 + (threadIdx.x >> 6)] = sum;
+    meet[g][d] = o;
+    __syncthreads();
+    if (g > 0 || d >= a.D) return;
+    sum = red[4] + red[5] + red[6] + red[7];
+#pragma unroll
+    for (int k = 1; k < G; ++k) o += meet[k][d];
+    static_cast<T *>(a.o)[b * a.ots + head * a.ohs + d] = from_f32<T>(wrong ? NAN : n == 0 ? 0.f : o / sum);
 }
 
 namespace {
@@ -248,11 +302,13 @@ struct PagedPlan {
     int splits, per;   // blocks of a sequence at most, keys of each
 };
 
-// Keys a block: some 4096 blocks if every sequence filled its table, whole steps of a
-// block's waves (128 keys).
+constexpr int kPagedBlocks = 8192;
+
+// Keys a block: some 8192 blocks if every sequence filled its table, whole steps of a
+// block's four waves.
 PagedPlan paged_plan(const PagedArgs &a) {
     const int64_t room = (int64_t)a.width * a.page, work = (int64_t)a.n * a.Hk * ((a.Hq / a.Hk + 31) / 32);
-    const int64_t per = std::max<int64_t>(128, (room * work / 4096 + 127) / 128 * 128);
+    const int64_t per = std::max<int64_t>(128, (room * work / kPagedBlocks + 127) / 128 * 128);
     return {(int)std::max<int64_t>(1, (room + per - 1) / per), (int)std::min<int64_t>(per, INT32_MAX / 2)};
 }
 
@@ -262,7 +318,7 @@ void paged_run(const PagedArgs &a, float *ws, hipStream_t st) {
     const dim3 grid((unsigned)(p.splits * (int64_t)a.n * a.Hk), (unsigned)((a.Hq / a.Hk + 31) / 32));
     hipLaunchKernelGGL((paged_kernel<T, DP, FAST>), grid, dim3(64 * PagedShape<T, DP>::NW), 0, st, a, p.splits, p.per, ws);
     if (p.splits > 1)
-        hipLaunchKernelGGL(join_kernel<T>, dim3((unsigned)((int64_t)a.n * a.Hq)), dim3(256), 0, st, a, p.splits, p.per, ws);
+        hipLaunchKernelGGL((join_kernel<T, DP>), dim3((unsigned)((int64_t)a.n * a.Hq)), dim3(256), 0, st, a, p.splits, p.per, ws);
 }
 
 template <typename T, int DP>

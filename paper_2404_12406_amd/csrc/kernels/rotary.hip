@@ -8,9 +8,9 @@
 //
 // Bound: memory.  A head lies in the registers of L lanes (a power of two that holds it
 // in 16-byte vectors), so it is read once and the norm is a sum within those lanes.  A
-// group of L lanes takes one token and goes over its heads, so the angles' sines are
-// taken once a token, from position * freq in 64 bits: in 32 an angle of 10^6 would be
-// off by 0.06.
+// wave takes one token and goes over its heads, 64 / L side by side, so that its loads
+// are of one piece and the angles' sines are taken once a token, from position * freq in
+// 64 bits: in 32 an angle of 10^6 would be off by 0.06.
 #include <algorithm>
 
 #include "block_math.h"
@@ -100,8 +100,8 @@ constexpr int kAhead = 4;   // heads loaded at once
 // values) as they are.
 template <typename T, int L, int PAIR, bool APPEND>
 __global__ __launch_bounds__(256) void fwd_kernel(RotaryArgs a) {
-    constexpr int V = Vec16<T>::N, GROUPS = 256 / L;
-    const int l = threadIdx.x % L, c = l * V;
+    constexpr int V = Vec16<T>::N, G = 64 / L;
+    const int l = threadIdx.x % L, c = l * V, g = (threadIdx.x & 63) / L, w = threadIdx.x >> 6;
     const T *x = static_cast<const T *>(a.x);
     T *y = static_cast<T *>(a.y);
     const T *gq = static_cast<const T *>(a.gq), *gk = static_cast<const T *>(a.gk);
@@ -112,7 +112,7 @@ __global__ __launch_bounds__(256) void fwd_kernel(RotaryArgs a) {
         wq[e] = c + e < a.D ? at(gq, c + e) : 0.f;
         wk[e] = c + e < a.D ? at(gk, c + e) : 0.f;
     }
-    for (int64_t t = (int64_t)blockIdx.x * GROUPS + threadIdx.x / L; t < a.T; t += (int64_t)gridDim.x * GROUPS) {
+    for (int64_t t = (int64_t)blockIdx.x * 4 + w; t < a.T; t += (int64_t)gridDim.x * 4) {
         int64_t place = -1;   // of the token in the cache: page * page size + row in it
         if constexpr (APPEND) {
             const int pos = a.pos[t];
@@ -125,14 +125,14 @@ __global__ __launch_bounds__(256) void fwd_kernel(RotaryArgs a) {
         Turn<T, L> turn;
         turn.take(a, t, c, (int)(threadIdx.x & 63), false);
         const T *xt = x + t * a.xts;
-        for (int h0 = (int)blockIdx.y * kAhead; h0 < H; h0 += (int)gridDim.y * kAhead) {
+        for (int h0 = (int)blockIdx.y * (kAhead * G) + g; h0 < H; h0 += (int)gridDim.y * (kAhead * G)) {
             Vec16<T> in[kAhead];
 #pragma unroll
             for (int u = 0; u < kAhead; ++u)
-                if (h0 + u < H) in[u] = load_vec<T>(xt + (h0 + u) * a.xhs, c, a.D);
+                if (h0 + u * G < H) in[u] = load_vec<T>(xt + (h0 + u * G) * a.xhs, c, a.D);
 #pragma unroll
             for (int u = 0; u < kAhead; ++u) {
-                const int h = h0 + u;
+                const int h = h0 + u * G;
                 if (h >= H) continue;
                 Vec16<T> out = in[u];
                 const bool value = APPEND && h >= a.Hq + a.Hk, query = h < a.Hq;
@@ -173,9 +173,9 @@ __global__ __launch_bounds__(256) void fwd_kernel(RotaryArgs a) {
 template <typename T, int L, int PAIR>
 __global__ __launch_bounds__(256) void bwd_kernel(RotaryArgs a, const T *dy, int64_t dts, int64_t dhs, T *dx, int64_t gts,
                                                   int64_t ghs, float *part) {
-    constexpr int V = Vec16<T>::N, GROUPS = 256 / L;
+    constexpr int V = Vec16<T>::N, G = 64 / L, GROUPS = 256 / L;
     __shared__ float meet[GROUPS][L * V];
-    const int l = threadIdx.x % L, c = l * V;
+    const int l = threadIdx.x % L, c = l * V, g = (threadIdx.x & 63) / L, w = threadIdx.x >> 6;
     const T *x = static_cast<const T *>(a.x);
     const T *gq = static_cast<const T *>(a.gq), *gk = static_cast<const T *>(a.gk);
     const int H = a.Hq + a.Hk;
@@ -186,21 +186,21 @@ __global__ __launch_bounds__(256) void bwd_kernel(RotaryArgs a, const T *dy, int
         wq[e] = c + e < a.D ? at(gq, c + e) : 0.f;
         wk[e] = c + e < a.D ? at(gk, c + e) : 0.f;
     }
-    for (int64_t t = (int64_t)blockIdx.x * GROUPS + threadIdx.x / L; t < a.T; t += (int64_t)gridDim.x * GROUPS) {
+    for (int64_t t = (int64_t)blockIdx.x * 4 + w; t < a.T; t += (int64_t)gridDim.x * 4) {
         Turn<T, L> turn;
         turn.take(a, t, c, (int)(threadIdx.x & 63), true);
         const T *xt = x + t * a.xts, *dt = dy + t * dts;
-        for (int h0 = (int)blockIdx.y * kAhead; h0 < H; h0 += (int)gridDim.y * kAhead) {
+        for (int h0 = (int)blockIdx.y * (kAhead * G) + g; h0 < H; h0 += (int)gridDim.y * (kAhead * G)) {
             Vec16<T> xi[kAhead], gi[kAhead];
 #pragma unroll
             for (int u = 0; u < kAhead; ++u) {
-                if (h0 + u >= H) continue;
-                gi[u] = load_vec<T>(dt + (h0 + u) * dhs, c, a.D);
-                xi[u] = a.norm ? load_vec<T>(xt + (h0 + u) * a.xhs, c, a.D) : zero16<T>();
+                if (h0 + u * G >= H) continue;
+                gi[u] = load_vec<T>(dt + (h0 + u * G) * dhs, c, a.D);
+                xi[u] = a.norm ? load_vec<T>(xt + (h0 + u * G) * a.xhs, c, a.D) : zero16<T>();
             }
 #pragma unroll
             for (int u = 0; u < kAhead; ++u) {
-                const int h = h0 + u;
+                const int h = h0 + u * G;
                 if (h >= H) continue;
                 const bool query = h < a.Hq;
                 float z[V];
@@ -237,32 +237,35 @@ __global__ __launch_bounds__(256) void bwd_kernel(RotaryArgs a, const T *dy, int
     if (!part) return;
     float *to = part + ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * 2 * a.D;
 #pragma unroll
-    for (int w = 0; w < 2; ++w) {
+    for (int which = 0; which < 2; ++which) {
 #pragma unroll
-        for (int e = 0; e < V; ++e) meet[threadIdx.x / L][c + e] = w ? sk[e] : sq[e];
+        for (int e = 0; e < V; ++e) meet[threadIdx.x / L][c + e] = which ? sk[e] : sq[e];
         __syncthreads();
         for (int d = threadIdx.x; d < a.D; d += 256) {
             float s = 0.f;
-            for (int g = 0; g < GROUPS; ++g) s += meet[g][d];
-            to[w * a.D + d] = s;
+            for (int k = 0; k < GROUPS; ++k) s += meet[k][d];
+            to[which * a.D + d] = s;
         }
         __syncthreads();
     }
 }
 
-// out[w][d] = the sum of the partial rows, in a fixed order.
+// out[which][d] = the sum of the partial rows, in a fixed order: 16 columns a block, 64 groups
+// of every 64th row.
 template <typename T>
-__global__ __launch_bounds__(256) void sum_kernel(const float *__restrict__ part, int rows, int D, T *__restrict__ oq, T *__restrict__ ok) {
-    __shared__ float red[16][17];
+__global__ __launch_bounds__(1024) void sum_kernel(const float *__restrict__ part, int rows, int D, T *__restrict__ oq, T *__restrict__ ok) {
+    __shared__ float red[64][17];
     const int col = threadIdx.x & 15, grp = threadIdx.x >> 4, c = (int)blockIdx.x * 16 + col;   // a column of [2 D]
     float s = 0.f;
-    if (c < 2 * D)
-        for (int r = grp; r < rows; r += 16) s += part[(int64_t)r * 2 * D + c];
+    if (c < 2 * D) {
+#pragma unroll 8
+        for (int r = grp; r < rows; r += 64) s += part[(int64_t)r * 2 * D + c];
+    }
     red[grp][col] = s;
     __syncthreads();
     if (grp == 0 && c < 2 * D) {
 #pragma unroll
-        for (int q = 1; q < 16; ++q) s += red[q][col];
+        for (int q = 1; q < 64; ++q) s += red[q][col];
         T *o = c < D ? oq : ok;
         if (o) o[c < D ? c : c - D] = from_f32<T>(s);
     }
@@ -285,10 +288,11 @@ int pairing(int dtype, const RotaryArgs &a) {
     return (a.R / 2) % (dtype == kBF16 ? 8 : 4) == 0 ? kLane : kLoose;
 }
 
+// A token a wave; where these are few, their heads over several blocks.
 dim3 grid_of(int dtype, const RotaryArgs &a, int heads, int most) {
-    const int groups = 256 / lanes(dtype, a.D);
-    const int64_t bx = std::min<int64_t>((a.T + groups - 1) / groups, most);
-    const int by = (int)std::max<int64_t>(1, std::min<int64_t>((heads + kAhead - 1) / kAhead, most / std::max<int64_t>(bx, 1)));
+    const int at_once = kAhead * 64 / lanes(dtype, a.D);
+    const int64_t bx = std::min<int64_t>((a.T + 3) / 4, most);
+    const int by = (int)std::max<int64_t>(1, std::min<int64_t>((heads + at_once - 1) / at_once, most / std::max<int64_t>(bx, 1)));
     return dim3((unsigned)bx, (unsigned)by);
 }
 
@@ -338,7 +342,7 @@ int bwd_t(int dtype, const RotaryArgs &a, const void *dy, const int64_t ds[2], v
         rows = (int)(grid.x * grid.y);
     }
     if (params)
-        hipLaunchKernelGGL(sum_kernel<T>, dim3((unsigned)((2 * a.D + 15) / 16)), dim3(256), 0, st, part, rows, a.D, (T *)dgq, (T *)dgk);
+        hipLaunchKernelGGL(sum_kernel<T>, dim3((unsigned)((2 * a.D + 15) / 16)), dim3(1024), 0, st, part, rows, a.D, (T *)dgq, (T *)dgk);
     return (int)hipGetLastError();
 }
 
