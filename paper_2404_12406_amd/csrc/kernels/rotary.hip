@@ -36,32 +36,37 @@ __device__ __forceinline__ float group_sum(float v) {
 // (halves that are no whole vectors).
 enum Pairing { kNext, kLane, kLoose };
 
-// A lane's part of a token's rotation: cosines and (signed) sines of its elements, and
-// where their partners are.
+// A lane's part of the rotation: its elements' frequencies (in turns, 64 bits), a token's
+// cosines and (signed) sines, and where the partners are.
 template <typename T, int L>
 struct Turn {
     static constexpr int V = Vec16<T>::N;
+    double freq[V];
     float cs[V], sn[V];
-    int lane;   // kLane: of the partner
-    __device__ __forceinline__ void take(const RotaryArgs &a, int64_t t, int c, int l, bool back) {
+    int lane;        // kLane: of the partner
+    uint32_t flip;   // elements whose sine counts the other way
+    __device__ __forceinline__ void init(const RotaryArgs &a, int c, int l, bool back) {
         const int half = a.R / 2;
-        const double pos = half ? (double)a.pos[t] * 0.15915494309189533577 : 0.0;
+        flip = 0;
 #pragma unroll
         for (int e = 0; e < V; ++e) {
             const int d = c + e;
-            cs[e] = 1.f;
-            sn[e] = 0.f;
-            if (d < 2 * half) {
-                const bool second = a.next ? d & 1 : d >= half;
-                const double turns = pos * (double)a.freq[a.next ? d >> 1 : second ? d - half : d];
-                float s, k;
-                sincospif(2.f * (float)(turns - rint(turns)), &s, &k);
-                cs[e] = k;
-                sn[e] = second != back ? s : -s;
-            }
+            const bool second = a.next ? d & 1 : d >= half;
+            freq[e] = d < 2 * half ? (double)a.freq[a.next ? d >> 1 : second ? d - half : d] * 0.15915494309189533577 : 0.0;
+            flip |= second == back ? 1u << e : 0u;
         }
         const int away = half / V, g = c / V;
         lane = g < away ? l + away : g < 2 * away ? l - away : l;
+    }
+    // (the angle in turns is reduced in 64 bits; what does not turn has frequency 0)
+    __device__ __forceinline__ void take(double pos) {
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+            const double turns = pos * freq[e];
+            float s;
+            sincospif(2.f * (float)(turns - rint(turns)), &s, &cs[e]);
+            sn[e] = flip >> e & 1 ? -s : s;
+        }
     }
     // turned z; partner(e) is the partner's value, for kLoose.  (Without a sine nothing
     // comes from the partner: elements past R stay as they are beside an infinite one.)
@@ -94,144 +99,185 @@ __device__ __forceinline__ int partner_of(const RotaryArgs &a, int d) {
     return d < half ? d + half : d < 2 * half ? d - half : d;
 }
 
-constexpr int kAhead = 4;   // heads loaded at once
+constexpr int kAhead = 4;   // heads of a lane loaded at once, at most
+
+// A wave's way through its tokens and their heads, `ahead` heads of each of its G groups of
+// lanes at a time; the next ones are loaded before these are worked on.
+struct Way {
+    int64_t t;
+    int h;   // the first group's first head
+    __device__ __forceinline__ void next(int ahead_heads, int H) {
+        h += (int)gridDim.y * ahead_heads;
+        if (h >= H) {
+            h = (int)blockIdx.y * ahead_heads;
+            t += (int64_t)gridDim.x * 4;
+        }
+    }
+};
+
+// A scale's elements of this lane; ones without it.
+template <typename T>
+__device__ __forceinline__ void scale_of(const T *p, int c, int D, float (&w)[Vec16<T>::N]) {
+    const Vec16<T> v = p ? load_vec<T>(p, c, D) : zero16<T>();
+#pragma unroll
+    for (int e = 0; e < Vec16<T>::N; ++e) w[e] = p ? to_f32(v.e[e]) : 1.f;
+}
 
 // Forward.  APPEND: heads past the Hq queries go to the cache, the last Hk of them (the
 // values) as they are.
 template <typename T, int L, int PAIR, bool APPEND>
-__global__ __launch_bounds__(256) void fwd_kernel(RotaryArgs a) {
+__global__ __launch_bounds__(256) void fwd_kernel(RotaryArgs a, int ahead) {
     constexpr int V = Vec16<T>::N, G = 64 / L;
-    const int l = threadIdx.x % L, c = l * V, g = (threadIdx.x & 63) / L, w = threadIdx.x >> 6;
+    const int lane = threadIdx.x & 63, c = lane % L * V, g = lane / L;
     const T *x = static_cast<const T *>(a.x);
     T *y = static_cast<T *>(a.y);
     const T *gq = static_cast<const T *>(a.gq), *gk = static_cast<const T *>(a.gk);
     const int H = a.Hq + (APPEND ? 2 : 1) * a.Hk;
+    auto load = [&](const Way &w, Vec16<T> (&v)[kAhead]) {
+        const T *p = x + w.t * a.xts + (w.h + g) * a.xhs;
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u)
+            if (u < ahead && w.h + g + u * G < H) v[u] = load_vec<T>(p + u * G * a.xhs, c, a.D);
+    };
+    Way way{(int64_t)blockIdx.x * 4 + (threadIdx.x >> 6), (int)blockIdx.y * ahead * G};
+    Vec16<T> in[kAhead], after[kAhead];
+    if (way.t < a.T) load(way, in);
     float wq[V], wk[V];
-#pragma unroll
-    for (int e = 0; e < V; ++e) {
-        wq[e] = c + e < a.D ? at(gq, c + e) : 0.f;
-        wk[e] = c + e < a.D ? at(gk, c + e) : 0.f;
-    }
-    for (int64_t t = (int64_t)blockIdx.x * 4 + w; t < a.T; t += (int64_t)gridDim.x * 4) {
-        int64_t place = -1;   // of the token in the cache: page * page size + row in it
-        if constexpr (APPEND) {
-            const int pos = a.pos[t];
-            const int64_t row = a.rows ? (int64_t)a.rows[t] : t;
-            if (pos >= 0 && row >= 0 && row < a.nseq && pos / a.page < a.width) {
-                const int pg = a.tables[row * a.width + pos / a.page];
-                if (pg >= 0 && pg < a.pages) place = (int64_t)pg * a.page + pos % a.page;
-            }
-        }
-        Turn<T, L> turn;
-        turn.take(a, t, c, (int)(threadIdx.x & 63), false);
-        const T *xt = x + t * a.xts;
-        for (int h0 = (int)blockIdx.y * (kAhead * G) + g; h0 < H; h0 += (int)gridDim.y * (kAhead * G)) {
-            Vec16<T> in[kAhead];
-#pragma unroll
-            for (int u = 0; u < kAhead; ++u)
-                if (h0 + u * G < H) in[u] = load_vec<T>(xt + (h0 + u * G) * a.xhs, c, a.D);
-#pragma unroll
-            for (int u = 0; u < kAhead; ++u) {
-                const int h = h0 + u * G;
-                if (h >= H) continue;
-                Vec16<T> out = in[u];
-                const bool value = APPEND && h >= a.Hq + a.Hk, query = h < a.Hq;
-                if (!value) {
-                    float z[V], r = 1.f;
-#pragma unroll
-                    for (int e = 0; e < V; ++e) z[e] = to_f32(in[u].e[e]);
-                    if (a.norm) {
-                        float s = 0.f;
-#pragma unroll
-                        for (int e = 0; e < V; ++e) s += z[e] * z[e];
-                        r = 1.f / sqrtf(group_sum<L>(s) / (float)a.D + a.eps);
-#pragma unroll
-                        for (int e = 0; e < V; ++e) z[e] = z[e] * r * (query ? wq[e] : wk[e]);
+    scale_of<T>(gq, c, a.D, wq);
+    scale_of<T>(gk, c, a.D, wk);
+    Turn<T, L> turn;
+    turn.init(a, c, lane, false);
+    T *kto = nullptr, *vto = nullptr;   // the token's first head in the cache
+    for (int64_t seen = -1; way.t < a.T;) {
+        const Way now = way;
+        way.next(ahead * G, H);
+        if (way.t < a.T) load(way, after);
+        if (now.t != seen) {
+            seen = now.t;
+            const int pos = APPEND || a.R ? a.pos[now.t] : 0;
+            if constexpr (APPEND) {
+                const int64_t row = a.rows ? (int64_t)a.rows[now.t] : now.t;
+                kto = nullptr;
+                if (pos >= 0 && row >= 0 && row < a.nseq && pos / a.page < a.width) {
+                    const int pg = a.tables[row * a.width + pos / a.page];
+                    if (pg >= 0 && pg < a.pages) {
+                        const int64_t to = ((int64_t)pg * a.Hk * a.page + pos % a.page) * a.D;
+                        kto = static_cast<T *>(a.kp) + to;
+                        vto = static_cast<T *>(a.vp) + to;
                     }
-                    turn.template apply<PAIR>(z, [&](int e) {
-                        const int p = partner_of(a, c + e);
-                        return to_f32(xt[h * a.xhs + p]) * r * (a.norm ? at(query ? gq : gk, p) : 1.f);
-                    });
-#pragma unroll
-                    for (int e = 0; e < V; ++e) out.e[e] = from_f32<T>(z[e]);
-                }
-                if (c >= a.D) continue;
-                if (!APPEND || query) {
-                    store_vec<T>(y + t * a.yts + h * a.yhs, c, a.D, out);
-                } else if (place >= 0) {
-                    const int64_t pg = place / a.page, in_page = place - pg * a.page;
-                    const int hk = h - a.Hq - (value ? a.Hk : 0);
-                    T *to = static_cast<T *>(value ? a.vp : a.kp) + ((pg * a.Hk + hk) * a.page + in_page) * a.D;
-                    store_vec<T>(to, c, a.D, out);
                 }
             }
+            turn.take((double)pos);
         }
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) {
+            const int h = now.h + g + u * G;
+            if (u >= ahead || h >= H) continue;
+            Vec16<T> out = in[u];
+            const bool value = APPEND && h >= a.Hq + a.Hk, query = h < a.Hq;
+            if (!value) {
+                float z[V], r = 1.f;
+#pragma unroll
+                for (int e = 0; e < V; ++e) z[e] = to_f32(in[u].e[e]);
+                if (a.norm) {
+                    float s = 0.f;
+#pragma unroll
+                    for (int e = 0; e < V; ++e) s += z[e] * z[e];
+                    r = 1.f / sqrtf(group_sum<L>(s) / (float)a.D + a.eps);
+#pragma unroll
+                    for (int e = 0; e < V; ++e) z[e] = z[e] * r * (query ? wq[e] : wk[e]);
+                }
+                turn.template apply<PAIR>(z, [&](int e) {
+                    const int p = partner_of(a, c + e);
+                    return to_f32(x[now.t * a.xts + h * a.xhs + p]) * r * (a.norm ? at(query ? gq : gk, p) : 1.f);
+                });
+#pragma unroll
+                for (int e = 0; e < V; ++e) out.e[e] = from_f32<T>(z[e]);
+            }
+            if (c >= a.D) continue;
+            if (!APPEND || query) store_vec<T>(y + now.t * a.yts + h * a.yhs, c, a.D, out);
+            else if (kto) store_vec<T>((value ? vto : kto) + (int64_t)(h - a.Hq - (value ? a.Hk : 0)) * a.page * a.D, c, a.D, out);
+        }
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) in[u] = after[u];
     }
 }
 
 // dx (may be null) and partial rows of dgq and dgk: part[blocks][2][D] (may be null).
 template <typename T, int L, int PAIR>
-__global__ __launch_bounds__(256) void bwd_kernel(RotaryArgs a, const T *dy, int64_t dts, int64_t dhs, T *dx, int64_t gts,
+__global__ __launch_bounds__(256) void bwd_kernel(RotaryArgs a, int ahead, const T *dy, int64_t dts, int64_t dhs, T *dx, int64_t gts,
                                                   int64_t ghs, float *part) {
     constexpr int V = Vec16<T>::N, G = 64 / L, GROUPS = 256 / L;
     __shared__ float meet[GROUPS][L * V];
-    const int l = threadIdx.x % L, c = l * V, g = (threadIdx.x & 63) / L, w = threadIdx.x >> 6;
+    const int lane = threadIdx.x & 63, c = lane % L * V, g = lane / L;
     const T *x = static_cast<const T *>(a.x);
     const T *gq = static_cast<const T *>(a.gq), *gk = static_cast<const T *>(a.gk);
     const int H = a.Hq + a.Hk;
+    auto load = [&](const Way &w, Vec16<T> (&v)[kAhead], Vec16<T> (&d)[kAhead]) {
+        const T *p = x + w.t * a.xts + (w.h + g) * a.xhs, *q = dy + w.t * dts + (w.h + g) * dhs;
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) {
+            if (u >= ahead || w.h + g + u * G >= H) continue;
+            d[u] = load_vec<T>(q + u * G * dhs, c, a.D);
+            if (a.norm) v[u] = load_vec<T>(p + u * G * a.xhs, c, a.D);
+        }
+    };
+    Way way{(int64_t)blockIdx.x * 4 + (threadIdx.x >> 6), (int)blockIdx.y * ahead * G};
+    Vec16<T> xi[kAhead], gi[kAhead], xn[kAhead], gn[kAhead];
+    if (way.t < a.T) load(way, xi, gi);
     float sq[V], sk[V], wq[V], wk[V];
 #pragma unroll
-    for (int e = 0; e < V; ++e) {
-        sq[e] = sk[e] = 0.f;
-        wq[e] = c + e < a.D ? at(gq, c + e) : 0.f;
-        wk[e] = c + e < a.D ? at(gk, c + e) : 0.f;
-    }
-    for (int64_t t = (int64_t)blockIdx.x * 4 + w; t < a.T; t += (int64_t)gridDim.x * 4) {
-        Turn<T, L> turn;
-        turn.take(a, t, c, (int)(threadIdx.x & 63), true);
-        const T *xt = x + t * a.xts, *dt = dy + t * dts;
-        for (int h0 = (int)blockIdx.y * (kAhead * G) + g; h0 < H; h0 += (int)gridDim.y * (kAhead * G)) {
-            Vec16<T> xi[kAhead], gi[kAhead];
+    for (int e = 0; e < V; ++e) sq[e] = sk[e] = 0.f;
+    scale_of<T>(gq, c, a.D, wq);
+    scale_of<T>(gk, c, a.D, wk);
+    Turn<T, L> turn;
+    turn.init(a, c, lane, true);
+    for (int64_t seen = -1; way.t < a.T;) {
+        const Way now = way;
+        way.next(ahead * G, H);
+        if (way.t < a.T) load(way, xn, gn);
+        if (now.t != seen) {
+            seen = now.t;
+            turn.take(a.R ? (double)a.pos[now.t] : 0.0);
+        }
 #pragma unroll
-            for (int u = 0; u < kAhead; ++u) {
-                if (h0 + u * G >= H) continue;
-                gi[u] = load_vec<T>(dt + (h0 + u * G) * dhs, c, a.D);
-                xi[u] = a.norm ? load_vec<T>(xt + (h0 + u * G) * a.xhs, c, a.D) : zero16<T>();
-            }
+        for (int u = 0; u < kAhead; ++u) {
+            const int h = now.h + g + u * G;
+            if (u >= ahead || h >= H) continue;
+            const bool query = h < a.Hq;
+            float z[V];
 #pragma unroll
-            for (int u = 0; u < kAhead; ++u) {
-                const int h = h0 + u * G;
-                if (h >= H) continue;
-                const bool query = h < a.Hq;
-                float z[V];
+            for (int e = 0; e < V; ++e) z[e] = to_f32(gi[u].e[e]);
+            turn.template apply<PAIR>(z, [&](int e) { return to_f32(dy[now.t * dts + h * dhs + partner_of(a, c + e)]); });
+            if (a.norm) {
+                float s = 0.f, m = 0.f;
 #pragma unroll
-                for (int e = 0; e < V; ++e) z[e] = to_f32(gi[u].e[e]);
-                turn.template apply<PAIR>(z, [&](int e) { return to_f32(dt[h * dhs + partner_of(a, c + e)]); });
-                if (a.norm) {
-                    float s = 0.f, m = 0.f;
-#pragma unroll
-                    for (int e = 0; e < V; ++e) {
-                        const float v = to_f32(xi[u].e[e]);
-                        s += v * v;
-                        m += z[e] * (query ? wq[e] : wk[e]) * v;
-                    }
-                    const float r = 1.f / sqrtf(group_sum<L>(s) / (float)a.D + a.eps);
-                    m = group_sum<L>(m) / (float)a.D * r * r;
-#pragma unroll
-                    for (int e = 0; e < V; ++e) {
-                        const float v = to_f32(xi[u].e[e]), p = z[e] * v * r;
-                        if (query) sq[e] += p;
-                        else sk[e] += p;
-                        z[e] = r * (z[e] * (query ? wq[e] : wk[e]) - v * m);
-                    }
+                for (int e = 0; e < V; ++e) {
+                    const float v = to_f32(xi[u].e[e]);
+                    s += v * v;
+                    m += z[e] * (query ? wq[e] : wk[e]) * v;
                 }
-                if (dx && c < a.D) {
-                    Vec16<T> out;
+                const float r = 1.f / sqrtf(group_sum<L>(s) / (float)a.D + a.eps);
+                m = group_sum<L>(m) / (float)a.D * r * r;
 #pragma unroll
-                    for (int e = 0; e < V; ++e) out.e[e] = from_f32<T>(z[e]);
-                    store_vec<T>(dx + t * gts + h * ghs, c, a.D, out);
+                for (int e = 0; e < V; ++e) {
+                    const float v = to_f32(xi[u].e[e]), p = z[e] * v * r;
+                    if (query) sq[e] += p;
+                    else sk[e] += p;
+                    z[e] = r * (z[e] * (query ? wq[e] : wk[e]) - v * m);
                 }
             }
+            if (dx && c < a.D) {
+                Vec16<T> out;
+#pragma unroll
+                for (int e = 0; e < V; ++e) out.e[e] = from_f32<T>(z[e]);
+                store_vec<T>(dx + now.t * gts + h * ghs, c, a.D, out);
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) {
+            xi[u] = xn[u];
+            gi[u] = gn[u];
         }
     }
     if (!part) return;
@@ -274,7 +320,7 @@ __global__ __launch_bounds__(1024) void sum_kernel(const float *__restrict__ par
 // ------------------------------------------------------------------ host
 namespace {
 
-constexpr int kMostBlocks = 2048, kMostParts = 512;
+constexpr int kMostBlocks = 1024, kMostParts = 512;
 
 int lanes(int dtype, int D) {
     const int v = dtype == kBF16 ? 8 : 4, n = (D + v - 1) / v;
@@ -288,24 +334,30 @@ int pairing(int dtype, const RotaryArgs &a) {
     return (a.R / 2) % (dtype == kBF16 ? 8 : 4) == 0 ? kLane : kLoose;
 }
 
-// A token a wave; where these are few, their heads over several blocks.
-dim3 grid_of(int dtype, const RotaryArgs &a, int heads, int most) {
-    const int at_once = kAhead * 64 / lanes(dtype, a.D);
+// Blocks of four waves, a token a wave; where these are few, their heads over several
+// blocks.  ahead: a token's heads in equal parts.
+struct Plan {
+    dim3 grid;
+    int ahead;
+};
+
+Plan plan(int dtype, const RotaryArgs &a, int heads, int most) {
+    const int G = 64 / lanes(dtype, a.D), per = (heads + G - 1) / G, parts = (per + kAhead - 1) / kAhead;
     const int64_t bx = std::min<int64_t>((a.T + 3) / 4, most);
-    const int by = (int)std::max<int64_t>(1, std::min<int64_t>((heads + at_once - 1) / at_once, most / std::max<int64_t>(bx, 1)));
-    return dim3((unsigned)bx, (unsigned)by);
+    const int64_t by = std::max<int64_t>(1, std::min<int64_t>(parts, most / std::max<int64_t>(bx, 1)));
+    return {dim3((unsigned)bx, (unsigned)by), std::max(1, (per + parts - 1) / std::max(parts, 1))};
 }
 
 template <typename T, int L, int PAIR>
-void fwd_run(const RotaryArgs &a, dim3 grid, bool append, hipStream_t st) {
-    if (append) hipLaunchKernelGGL((fwd_kernel<T, L, PAIR, true>), grid, dim3(256), 0, st, a);
-    else hipLaunchKernelGGL((fwd_kernel<T, L, PAIR, false>), grid, dim3(256), 0, st, a);
+void fwd_run(const RotaryArgs &a, const Plan &p, bool append, hipStream_t st) {
+    if (append) hipLaunchKernelGGL((fwd_kernel<T, L, PAIR, true>), p.grid, dim3(256), 0, st, a, p.ahead);
+    else hipLaunchKernelGGL((fwd_kernel<T, L, PAIR, false>), p.grid, dim3(256), 0, st, a, p.ahead);
 }
 
 template <typename T, int L, int PAIR>
-void bwd_run(const RotaryArgs &a, dim3 grid, const void *dy, const int64_t ds[2], void *dx, const int64_t gs[2], float *part,
+void bwd_run(const RotaryArgs &a, const Plan &p, const void *dy, const int64_t ds[2], void *dx, const int64_t gs[2], float *part,
              hipStream_t st) {
-    hipLaunchKernelGGL((bwd_kernel<T, L, PAIR>), grid, dim3(256), 0, st, a, (const T *)dy, ds[0], ds[1], (T *)dx, gs[0], gs[1], part);
+    hipLaunchKernelGGL((bwd_kernel<T, L, PAIR>), p.grid, dim3(256), 0, st, a, p.ahead, (const T *)dy, ds[0], ds[1], (T *)dx, gs[0], gs[1], part);
 }
 
 #define ROT_PAIR(F, L, ...)                                  \
@@ -325,8 +377,8 @@ void bwd_run(const RotaryArgs &a, dim3 grid, const void *dy, const int64_t ds[2]
 
 template <typename T>
 int fwd_t(int dtype, const RotaryArgs &a, bool append, hipStream_t st) {
-    const dim3 grid = grid_of(dtype, a, a.Hq + (append ? 2 : 1) * a.Hk, kMostBlocks);
-    ROT_DISPATCH(fwd_run, a, grid, append, st)
+    const Plan p = plan(dtype, a, a.Hq + (append ? 2 : 1) * a.Hk, kMostBlocks);
+    ROT_DISPATCH(fwd_run, a, p, append, st)
     return (int)hipGetLastError();
 }
 
@@ -337,9 +389,9 @@ int bwd_t(int dtype, const RotaryArgs &a, const void *dy, const int64_t ds[2], v
     float *part = params ? static_cast<float *>(ws) : nullptr;
     int rows = 0;
     if (a.T > 0 && a.Hq + a.Hk > 0) {
-        const dim3 grid = grid_of(dtype, a, a.Hq + a.Hk, params ? kMostParts : kMostBlocks);
-        ROT_DISPATCH(bwd_run, a, grid, dy, ds, dx, gs, part, st)
-        rows = (int)(grid.x * grid.y);
+        const Plan p = plan(dtype, a, a.Hq + a.Hk, params ? kMostParts : kMostBlocks);
+        ROT_DISPATCH(bwd_run, a, p, dy, ds, dx, gs, part, st)
+        rows = (int)(p.grid.x * p.grid.y);
     }
     if (params)
         hipLaunchKernelGGL(sum_kernel<T>, dim3((unsigned)((2 * a.D + 15) / 16)), dim3(1024), 0, st, part, rows, a.D, (T *)dgq, (T *)dgk);
@@ -357,7 +409,7 @@ int launch_rotary_fwd(int dtype, const RotaryArgs &a, bool append, void *stream)
 
 size_t rotary_bwd_workspace(int dtype, const RotaryArgs &a, bool params) {
     if (!params || a.T == 0 || a.Hq + a.Hk == 0) return 0;
-    const dim3 g = rot::grid_of(dtype, a, a.Hq + a.Hk, rot::kMostParts);
+    const dim3 g = rot::plan(dtype, a, a.Hq + a.Hk, rot::kMostParts).grid;
     return ((size_t)g.x * g.y * 2 * a.D * sizeof(float) + 255) / 256 * 256;
 }
 
