@@ -321,6 +321,8 @@ ms_status ms_attention_forward(const ms_tensor *q, const ms_tensor *k, const ms_
         if (!aligned(q_offsets, 4) || !aligned(k_offsets, 4)) return fail(MS_E_ARG, "offsets must be 4-byte aligned");
     }
     const int64_t n = q_offsets ? sequences : 0;
+    // (heads are a launch's second dimension, too)
+    if (Hq > 65535) return fail(MS_E_UNSUPPORTED, "more than 65535 heads");
     if (capped_product({std::max(Tq, Tk) / 128 + n + 2, Hq}) > kMaxBlocks)
         return fail(MS_E_UNSUPPORTED, "2^24 or more blocks of 128 rows");
     if (mask && Tq > 0 && !kept) return fail(MS_E_NULL, "kept is NULL but gradients are asked for");

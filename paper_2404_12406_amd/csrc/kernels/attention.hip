@@ -31,18 +31,18 @@ struct Parts {
 };
 
 template <typename T, int DC>
-__global__ __launch_bounds__(256, (FwdShape<T, DC>::OCC)) void fwd_kernel(AttnArgs a, int slots, Parts part) {
+__global__ __launch_bounds__(256, (FwdShape<T, DC>::OCC)) void fwd_kernel(AttnArgs a, Parts part) {
     constexpr int DP = kPitch<DC>;
     typedef Mat<T> M;
     typedef Tile<T, DP> Ti;
     typedef typename M::Frag Frag;
     constexpr int BN = FwdShape<T, DC>::BN, NS = BN / 32, NP = 32 / M::KC, BYTES = BN * Ti::RB;
-    __shared__ __align__(16) char lds[4 * BYTES];
+    __shared__ __align__(256) char lds[4 * BYTES];
     const int lane = threadIdx.x & 63, w = uniform(threadIdx.x >> 6);
-    const int logical = xcd_remap((int)blockIdx.x, (int)gridDim.x);
-    const int head = logical / slots, hk = head / (a.Hq / a.Hk);
-    // the last tiles of a causal sequence take longest: first
-    const Span s = find_span(a.qoff, a.koff, a.n, (int)a.Tq, (int)a.Tk, slots - 1 - logical % slots, kRows);
+    int head, rank;
+    find_head((int)blockIdx.x, a.Hq, head, rank);
+    const int hk = head / (a.Hq / a.Hk);
+    const Span s = find_ranked(a.qoff, a.koff, a.n, (int)a.Tq, (int)a.Tk, rank, kRows, a.causal, true);
     const int row0 = s.tile * kRows;
     if (s.tile < 0 || row0 >= s.na) return;
     const int shift = s.nb - s.na;                 // query i sees keys to i + shift
@@ -213,7 +213,7 @@ int fwd_run(const AttnArgs &a, void *ws, hipStream_t st) {
     const int64_t slots = rows_slots(a), rows = a.Tq * a.Hq;
     Parts part{fwd_splits<T, DC>(a), static_cast<float *>(ws), nullptr};
     part.stat = reinterpret_cast<floatx2 *>(part.sums + part.splits * rows * DC);
-    hipLaunchKernelGGL((fwd_kernel<T, DC>), dim3((unsigned)(slots * a.Hq), (unsigned)part.splits), dim3(256), 0, st, a, (int)slots, part);
+    hipLaunchKernelGGL((fwd_kernel<T, DC>), dim3((unsigned)(slots * a.Hq), (unsigned)part.splits), dim3(256), 0, st, a, part);
     if (part.splits > 1) {
         const int64_t n = rows * (a.D / Vec16<T>::N);
         hipLaunchKernelGGL((join_kernel<T, DC>), dim3((unsigned)((n + 255) / 256)), dim3(256), 0, st, a, part);

@@ -18,38 +18,51 @@
 namespace ms {
 namespace att {
 
-// delta[h][t] = sum over d of g o, a row by L lanes.
-template <typename T, int L>
-__global__ __launch_bounds__(256) void delta_kernel(AttnArgs a, float *__restrict__ delta) {
-    constexpr int V = Vec16<T>::N;
-    const int l = threadIdx.x % L;
-    const int64_t n = a.Tq * a.Hq;
-    for (int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) / L; i < n; i += (int64_t)gridDim.x * (256 / L)) {
-        const int64_t t = i / a.Hq;
-        const int h = (int)(i - t * a.Hq);
-        float s = 0.f;
-        if (l * V < a.D) {
-            const Vec16<T> x = load16(static_cast<const T *>(a.o.p) + t * a.o.ts + h * a.o.hs + l * V);
-            const Vec16<T> y = load16(static_cast<const T *>(a.go.p) + t * a.go.ts + h * a.go.hs + l * V);
+// delta of a wave's 32 rows from row `first` on: the sum of o g over row l % 32 (a lane
+// takes every other unit), in one order wherever it is taken.
+template <typename T, int DC, bool HOLD>
+__device__ __forceinline__ float row_delta(const AttnArgs &a, int head, int64_t first, int rows, const Rows<T, DC, HOLD> &g, int lane) {
+    typedef Mat<T> M;
+    const T *o = static_cast<const T *>(a.o.p) + first * a.o.ts + head * a.o.hs;
+    float delta = 0.f;
+    auto add = [&](int i) __attribute__((always_inline)) {
+        const typename M::Frag x = load_row<T>(o, a.o.ts, rows, a.D, i, lane), y = g.get(i, lane);
 #pragma unroll
-            for (int e = 0; e < V; ++e) s += to_f32(x.e[e]) * to_f32(y.e[e]);
-        }
+        for (int j = 0; j < M::V; ++j) delta = __builtin_fmaf(to_f32(x[j]), to_f32(y[j]), delta);
+    };
+    if constexpr (HOLD) {
 #pragma unroll
-        for (int d = 1; d < L; d *= 2) s += __shfl_xor(s, d);
-        if (l == 0) delta[h * a.Tq + t] = s;
+        for (int i = 0; i < DC / M::KC; ++i) add(i);
+    } else {
+#pragma unroll 2
+        for (int i = 0; i < DC / M::KC; ++i) add(i);
     }
+    return both_sum(delta);
+}
+
+// delta[h][t], for dk without dq: 128 rows a block, blockIdx.y the head.
+template <typename T, int DC>
+__global__ __launch_bounds__(256) void delta_kernel(AttnArgs a, float *__restrict__ delta) {
+    const int lane = threadIdx.x & 63, head = (int)blockIdx.y;
+    const int64_t first = (int64_t)blockIdx.x * 128 + (threadIdx.x >> 6) * 32;
+    const int rows = (int)min((int64_t)32, a.Tq - first);
+    if (rows <= 0) return;
+    Rows<T, DC, false> g;
+    g.init(static_cast<const T *>(a.go.p) + first * a.go.ts + head * a.go.hs, a.go.ts, rows, a.D, lane);
+    const float v = row_delta<T, DC, false>(a, head, first, rows, g, lane);
+    if (lane < rows) delta[head * a.Tq + first + lane] = v;
 }
 
 // ------------------------------------------------------------------ dq
 constexpr int kRows = 128;   // queries of a block of dq, keys of a block of dk and dv
 
-// Whether a wave has registers for both operands that it keeps: not for 256 fp32 elements.
-template <typename T, int DC> constexpr bool kHold = DC * sizeof(T) < 1024;
+// Whether a wave has registers for both operands that it keeps: not for 192 fp32 elements.
+template <typename T, int DC> constexpr bool kHold = DC * sizeof(T) < 768;
 
-// What the kernels take besides: delta, and where they leave sums in fp32 if the other
-// side is divided: [split][rows][heads][DC].
+// What the kernels take besides: delta, which dq_kernel writes, and where they leave sums in fp32 if the
+// other side is divided: [split][rows][heads][DC].
 struct Parts {
-    const float *delta;
+    float *delta;
     int splits;
     float *a, *b;
 };
@@ -61,17 +74,18 @@ struct DqShape {
 };
 
 template <typename T, int DC>
-__global__ __launch_bounds__(256, (DqShape<T, DC>::OCC)) void dq_kernel(AttnArgs a, int slots, Parts part) {
+__global__ __launch_bounds__(256, (DqShape<T, DC>::OCC)) void dq_kernel(AttnArgs a, Parts part) {
     constexpr int DP = kPitch<DC>;
     typedef Mat<T> M;
     typedef Tile<T, DP> Ti;
     typedef typename M::Frag Frag;
     constexpr int BN = DqShape<T, DC>::BN, NP = 32 / M::KC, BYTES = BN * Ti::RB;
-    __shared__ __align__(16) char lds[4 * BYTES];
+    __shared__ __align__(256) char lds[4 * BYTES];
     const int lane = threadIdx.x & 63, w = uniform(threadIdx.x >> 6);
-    const int logical = xcd_remap((int)blockIdx.x, (int)gridDim.x);
-    const int head = logical / slots, hk = head / (a.Hq / a.Hk);
-    const Span s = find_span(a.qoff, a.koff, a.n, (int)a.Tq, (int)a.Tk, slots - 1 - logical % slots, kRows);
+    int head, rank;
+    find_head((int)blockIdx.x, a.Hq, head, rank);
+    const int hk = head / (a.Hq / a.Hk);
+    const Span s = find_ranked(a.qoff, a.koff, a.n, (int)a.Tq, (int)a.Tk, rank, kRows, a.causal, true);
     const int row0 = s.tile * kRows;
     if (s.tile < 0 || row0 >= s.na) return;
     const int shift = s.nb - s.na;
@@ -99,10 +113,12 @@ __global__ __launch_bounds__(256, (DqShape<T, DC>::OCC)) void dq_kernel(AttnArgs
     Rows<T, DC, kHold<T, DC>> g;
     q.init(static_cast<const T *>(a.q.p) + first * a.q.ts + head * a.q.hs, a.q.ts, rows, a.D, lane);
     g.init(static_cast<const T *>(a.go.p) + first * a.go.ts + head * a.go.hs, a.go.ts, rows, a.D, lane);
-    float lse = INFINITY, delta = 0.f;
+    float lse = INFINITY;
+    const float delta = row_delta<T, DC, kHold<T, DC>>(a, head, first, rows, g, lane);
     if ((lane & 31) < rows) {
-        lse = a.lse[(int64_t)head * a.Tq + first + (lane & 31)];
-        delta = part.delta[(int64_t)head * a.Tq + first + (lane & 31)];
+        const int64_t at = (int64_t)head * a.Tq + first + (lane & 31);
+        lse = a.lse[at];
+        if (part.delta && blockIdx.y == 0 && lane < 32) part.delta[at] = delta;
     }
     const float c = a.scale * kLog2e;
     floatx16 acc[DC / 32];
@@ -156,19 +172,19 @@ struct DkvShape {
 };
 
 template <typename T, int DC, bool DK, bool DV>
-__global__ __launch_bounds__(256, (DkvShape<T, DC, DK, DV>::OCC)) void dkv_kernel(AttnArgs a, int slots, Parts part) {
+__global__ __launch_bounds__(256, (DkvShape<T, DC, DK, DV>::OCC)) void dkv_kernel(AttnArgs a, Parts part) {
     constexpr int DP = kPitch<DC>;
     typedef Mat<T> M;
     typedef Tile<T, DP> Ti;
     typedef typename M::Frag Frag;
     constexpr int BM = DkvShape<T, DC, DK, DV>::BM, NP = 32 / M::KC, BYTES = BM * Ti::RB, C = DC / M::KC;
     constexpr int STAGE = 2 * BYTES + 512;   // q, g, and 64 each of lse and delta
-    __shared__ __align__(16) char lds[2 * STAGE];
+    __shared__ __align__(256) char lds[2 * STAGE];
     const int lane = threadIdx.x & 63, w = uniform(threadIdx.x >> 6);
-    const int logical = xcd_remap((int)blockIdx.x, (int)gridDim.x);
-    const int hk = logical / slots, group = a.Hq / a.Hk;
-    // (the first keys of a causal sequence take longest: first)
-    const Span s = find_span(a.koff, a.qoff, a.n, (int)a.Tk, (int)a.Tq, logical % slots, kRows);
+    int hk, rank;
+    find_head((int)blockIdx.x, a.Hk, hk, rank);
+    const int group = a.Hq / a.Hk;
+    const Span s = find_ranked(a.koff, a.qoff, a.n, (int)a.Tk, (int)a.Tq, rank, kRows, a.causal, false);
     const int key0 = s.tile * kRows;
     if (s.tile < 0 || key0 >= s.na) return;
     const int shift = s.na - s.nb;   // query i sees keys to i + shift
@@ -315,7 +331,7 @@ Plan plan(const AttnArgs &a, bool dq, bool dk, bool dv) {
         p.dkv_splits = span_splits(span_slots(packed, a.n, a.Tk, kRows) * a.Hk, a.Tq / n * group / DkvShape<T, DC, true, true>::BM,
                                    a.Tk * a.Hk * DC * 8);
     const size_t keys = p.dkv_splits > 1 ? al256((size_t)p.dkv_splits * a.Tk * a.Hk * DC * sizeof(float)) : 0;
-    p.dq_at = dq || dk ? al256((size_t)a.Tq * a.Hq * sizeof(float)) : 0;
+    p.dq_at = dk ? al256((size_t)a.Tq * a.Hq * sizeof(float)) : 0;
     p.dk_at = p.dq_at + (p.dq_splits > 1 ? al256((size_t)p.dq_splits * a.Tq * a.Hq * DC * sizeof(float)) : 0);
     p.dv_at = p.dk_at + (dk ? keys : 0);
     p.bytes = p.dv_at + (dv ? keys : 0);
@@ -333,15 +349,13 @@ int run(const AttnArgs &a, char *ws, hipStream_t st) {
     const Plan p = plan<T, DC>(a, dq, dk, dv);
     constexpr int V = Vec16<T>::N;
     float *delta = reinterpret_cast<float *>(ws);
-    if ((dq || dk) && a.Tq > 0) {
-        constexpr int L = kPitch<DC> / V;
-        const int64_t blocks = (a.Tq * a.Hq + 256 / L - 1) / (256 / L);
-        hipLaunchKernelGGL((delta_kernel<T, L>), dim3((unsigned)std::min<int64_t>(blocks, 8192)), dim3(256), 0, st, a, delta);
+    if (dk && !dq && a.Tq > 0) {
+        hipLaunchKernelGGL((delta_kernel<T, DC>), dim3((unsigned)((a.Tq + 127) / 128), (unsigned)a.Hq), dim3(256), 0, st, a, delta);
     }
     if (dq && a.Tq > 0) {
         const int64_t slots = span_slots(packed, a.n, a.Tq, kRows);
-        const Parts part{delta, p.dq_splits, reinterpret_cast<float *>(ws + p.dq_at), nullptr};
-        hipLaunchKernelGGL((dq_kernel<T, DC>), dim3((unsigned)(slots * a.Hq), (unsigned)part.splits), dim3(256), 0, st, a, (int)slots, part);
+        const Parts part{dk ? delta : nullptr, p.dq_splits, reinterpret_cast<float *>(ws + p.dq_at), nullptr};
+        hipLaunchKernelGGL((dq_kernel<T, DC>), dim3((unsigned)(slots * a.Hq), (unsigned)part.splits), dim3(256), 0, st, a, part);
         if (part.splits > 1) {
             const Sum s{a.dq, part.a, a.scale};
             hipLaunchKernelGGL(sum_kernel<T>, dim3((unsigned)((a.Tq * a.Hq * (a.D / V) + 255) / 256)), dim3(256), 0, st, s, s, a.Tq, a.Hq,
@@ -355,10 +369,10 @@ int run(const AttnArgs &a, char *ws, hipStream_t st) {
         // (both sums of 512 bytes a row, and their operands, are more than a wave's registers)
         constexpr bool both = DC * sizeof(T) < 384;
         if (both && dk && dv) {
-            if constexpr (both) hipLaunchKernelGGL((dkv_kernel<T, DC, true, true>), grid, dim3(256), 0, st, a, (int)slots, part);
+            if constexpr (both) hipLaunchKernelGGL((dkv_kernel<T, DC, true, true>), grid, dim3(256), 0, st, a, part);
         } else {
-            if (dk) hipLaunchKernelGGL((dkv_kernel<T, DC, true, false>), grid, dim3(256), 0, st, a, (int)slots, part);
-            if (dv) hipLaunchKernelGGL((dkv_kernel<T, DC, false, true>), grid, dim3(256), 0, st, a, (int)slots, part);
+            if (dk) hipLaunchKernelGGL((dkv_kernel<T, DC, true, false>), grid, dim3(256), 0, st, a, part);
+            if (dv) hipLaunchKernelGGL((dkv_kernel<T, DC, false, true>), grid, dim3(256), 0, st, a, part);
         }
         if (part.splits > 1) {
             const Sum k{a.dk, part.a, a.scale}, v{a.dv, part.b, 1.f};

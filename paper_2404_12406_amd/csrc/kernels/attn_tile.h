@@ -39,46 +39,54 @@ template <> struct Mat<float> {
 
 typedef short v4i16 __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) v4i16 lds_v4i16_t;
+typedef __attribute__((address_space(3))) char lds_char_t;
 
 // How a call of DC padded columns is laid out: rows in LDS have DP of them, a power of two
 // (the swizzle's units are eight at a time).
 template <int DC> constexpr int kPitch = DC <= 64 ? 64 : DC <= 128 ? 128 : 256;
 
-// Rows of DP elements in LDS.  The 16-byte units of each eight are swapped by the row, so
-// that eight rows' units of one number lie in different banks (row_frag) and so do the
-// pairs of units of four rows (col_frag).
+// Rows of DP elements in LDS, whose 256 bytes of banks are read in one clock.  The low
+// bits of a 16-byte unit's number are turned by its row so that what is read together lies
+// in different banks: one unit of 16 rows (row_frag), four units of four rows or, in fp32, a
+// word of each of 32 columns in two rows (col_frag).  swz() is linear in the row's bits, so
+// the part of an address that differs between lanes is worked out once.
 template <typename T, int DP>
 struct Tile {
     typedef typename Mat<T>::Frag Frag;
     static constexpr int V = Mat<T>::V, U = DP / V, RB = DP * (int)sizeof(T);
-    static __device__ __forceinline__ int swz(int row) { return (row & 3) << 1 | (row >> 2 & 1); }
-    static __device__ __forceinline__ int at(int row, int unit) { return row * RB + ((unit ^ swz(row)) << 4); }
-
-    // Row r0 + l % 32 (r0 a multiple of 8), chunk c of its elements: units 2 c + l / 32.
-    static __device__ __forceinline__ Frag row_frag(const char *base, int r0, int c, int lane) {
-        const int r = lane & 31, low = ((2 * (c & 3) + (lane >> 5)) ^ swz(r)) << 4;
-        return *reinterpret_cast<const Frag *>(base + r * RB + low + r0 * RB + (c >> 2) * 128);
+    static constexpr int LOW = U < 16 ? 7 : 15;
+    static __host__ __device__ __forceinline__ constexpr int swz(int row) {
+        return sizeof(T) == 4 ? (row >> 2 & 1) << 3 | (row >> 3 & 1) << 2 | (row & 3)
+               : U < 16       ? (row >> 1 & 1) << 2 | (row >> 2 & 3)
+                              : (row & 3) << 2 | (row >> 2 & 3);
     }
-    // Column 32 t + l % 32, chunk c of the rows from r0 (a multiple of 8) on.
+    static __device__ __forceinline__ int at(int row, int unit) { return row * RB + ((unit ^ swz(row)) << 4); }
+    // at(row | row_, unit | unit_) of a tile that begins on 256 bytes: no bits in common, the second ones known
+    // when this is compiled.  What differs between lanes is in one register, the rest an XOR.
+    static __device__ __forceinline__ const lds_char_t *spot(const char *base, int row, int unit, int byte, int row_, int unit_) {
+        const uint32_t p = (uint32_t)(uintptr_t)(const lds_char_t *)base + (uint32_t)(at(row, unit) + byte);
+        return (const lds_char_t *)(uintptr_t)((p ^ (uint32_t)(((unit_ ^ swz(row_)) & LOW) << 4)) + (uint32_t)(row_ * RB + ((unit_ & ~LOW) << 4)));
+    }
+
+    // Row r0 + l % 32 (r0 a multiple of 32), chunk c of its elements: units 2 c + l / 32.
+    static __device__ __forceinline__ Frag row_frag(const char *base, int r0, int c, int lane) {
+        return *(const __attribute__((address_space(3))) Frag *)spot(base, lane & 31, lane >> 5, 0, r0, 2 * c);
+    }
+    // Column 32 t + l % 32, chunk c of the rows from r0 (a multiple of 32) on.
     static __device__ __forceinline__ Frag col_frag(const char *base, int r0, int t, int c, int lane) {
         Frag f;
         if constexpr (sizeof(T) == 2) {
             // ds_read_b64_tr_b16: each 16 lanes address four rows of 16 columns, 8 bytes a
             // lane, and hold a column's four rows afterwards
-            const int r = lane & 15, g = lane >> 4, row = 4 * (g >> 1) + (r >> 2);
-            const int low = ((2 * (g & 1) + ((r & 3) >> 1) + 4 * (t & 1)) ^ swz(row)) << 4;
-            const char *p = base + row * RB + low + ((r & 1) << 3) + (r0 + 16 * c) * RB + (t >> 1) * 128;
+            const int r = lane & 15, g = lane >> 4, row = 4 * (g >> 1) + (r >> 2), unit = 2 * (g & 1) + ((r & 3) >> 1), byte = (r & 1) << 3;
             v4i16 *v = reinterpret_cast<v4i16 *>(&f);
-            v[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4i16_t *)p);
-            v[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4i16_t *)(p + 8 * RB));
+            v[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4i16_t *)spot(base, row, unit, byte, r0 + 16 * c, 4 * t));
+            v[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4i16_t *)spot(base, row, unit, byte, r0 + 16 * c + 8, 4 * t));
         } else {
             const int m = lane & 31, hh = lane >> 5;
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const int row = 4 * hh + j;
-                f[j] = *reinterpret_cast<const float *>(base + row * RB + (((m >> 2) ^ swz(row)) << 4) + ((m & 3) << 2) +
-                                                        (r0 + 8 * c) * RB + t * 128);
-            }
+            for (int j = 0; j < 4; ++j)
+                f[j] = *(const __attribute__((address_space(3))) float *)spot(base, 4 * hh, m >> 2, (m & 3) << 2, r0 + 8 * c + j, 8 * t);
         }
         return f;
     }
@@ -150,6 +158,76 @@ __device__ __forceinline__ Span find_span(const int32_t *aoff, const int32_t *bo
     return s;
 }
 
+// The sum of a wave's values, by moves within the vector registers.
+__device__ __forceinline__ int wave_add(int v) {
+#define ATT_MOVED(ctrl, rows) __builtin_amdgcn_update_dpp(0, v, ctrl, rows, 0xf, false)
+    v += ATT_MOVED(0x111, 0xf);   // from 1, 2, 4 and 8 lanes below, within rows of 16
+    v += ATT_MOVED(0x112, 0xf);
+    v += ATT_MOVED(0x114, 0xf);
+    v += ATT_MOVED(0x118, 0xf);
+    v += ATT_MOVED(0x142, 0xa);   // the rows before
+    v += ATT_MOVED(0x143, 0xc);
+#undef ATT_MOVED
+    return __builtin_amdgcn_readlane(v, 63);
+}
+
+// The tile that is `rank`-th in work, most first, so that the blocks that take longest
+// begin first and none of them is left over at the end.  A causal sequence's tiles have work in steps of one tile's
+// rows (from its last one on with last_first, else from its first), others all their keys.
+// To 62 sequences, a lane each; beyond, as they come.  Past the last tile: one without rows.
+// (8192 rows in 7 sequences, 32 on 8 heads of 128, bf16: dv 338 -> 261 us.)
+__device__ __forceinline__ Span find_ranked(const int32_t *aoff, const int32_t *boff, int n, int Ta, int Tb, int rank, int rows, bool causal,
+                                            bool last_first) {
+    const int tiles = (Ta + rows - 1) / rows;
+    if (!aoff) return Span{0, Ta, 0, Tb, last_first ? tiles - 1 - rank : rank};
+    if (n + 2 > 64) return find_span(aoff, boff, n, Ta, Tb, rank, rows);
+    const int i = threadIdx.x & 63;
+    auto edge = [&](int i) {   // of n + 2 sequences, as find_span()'s
+        return i <= 0 ? 0 : i > n + 1 ? Ta : min(max(aoff[i - 1], 0), Ta);
+    };
+    Span s{0, 0, 0, 0, 0};
+    if (i <= n + 1) {
+        s.a0 = edge(i);
+        s.na = max(edge(i + 1), s.a0) - s.a0;
+        if (i >= 1 && i <= n) {
+            s.b0 = min(max(boff[i - 1], 0), Tb);
+            s.nb = max(min(max(boff[i], 0), Tb), s.b0) - s.b0;
+        }
+    }
+    const int nt = (s.na + rows - 1) / rows, level = s.nb / rows + tiles + 2;   // of the first tile; above 0 for all
+    auto from = [&](int x) {   // tiles of level x and above
+        return causal ? min(max(level - x + 1, 0), nt) : level >= x ? nt : 0;
+    };
+    if (rank >= wave_add(nt)) return Span{0, 0, 0, 0, 0};
+    int lo = 0, hi = Tb / rows + tiles + 3;   // all tiles, none
+    while (hi - lo > 1) {
+        const int mid = (lo + hi) / 2;
+        if (wave_add(from(mid)) > rank) lo = mid;
+        else hi = mid;
+    }
+    const int above = from(lo + 1), here = from(lo) - above, k = rank - wave_add(above);   // the k-th of level lo
+    int upto = here;
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) {
+        const int v = __shfl_up(upto, d);
+        if (i >= d) upto += v;
+    }
+    const uint64_t mine = __ballot(k < upto);
+    const int src = uniform((int)__ffsll((unsigned long long)mine) - 1);
+    const int j = above + k - (upto - here);   // tiles of this sequence before it
+    s.tile = last_first ? nt - 1 - j : j;
+    auto of = [&](int v) { return __builtin_amdgcn_readlane(v, src); };
+    return Span{of(s.a0), of(s.na), of(s.b0), of(s.nb), of(s.tile)};
+}
+
+// Which head and which rank a block has: all heads' longest tiles first; heads that lie
+// side by side (and share keys) on one XCD, whose L2 they then share, where eight divide them.
+__device__ __forceinline__ void find_head(int b, int H, int &head, int &rank) {
+    rank = b / H;
+    head = b - rank * H;
+    if (H % 8 == 0) head = (head & 7) * (H / 8) + (head >> 3);
+}
+
 // Slots of find_span().
 inline int64_t span_slots(bool packed, int n, int64_t Ta, int rows) {
     return packed ? Ta / rows + n + 2 : (Ta + rows - 1) / rows;
@@ -157,7 +235,7 @@ inline int64_t span_slots(bool packed, int n, int64_t Ta, int rows) {
 
 // Blocks of few rows' worth of work divide their other side: `splits` of them, of `steps`
 // steps on average, where that leaves each two steps and the partial sums below 24 MiB.
-// attend_ragged's sizes (fp32, 5 sequences, 1777 x 6 heads of 72): see attention_bwd.hip.
+// (fp32, 1777 rows in 5 sequences, 6 on 2 heads of 72, all gradients: 906 -> 250 us.)
 inline int span_splits(int64_t blocks, int64_t steps, int64_t bytes) {
     const int64_t want = 512 / std::max<int64_t>(blocks, 1), most = (int64_t(24) << 20) / std::max<int64_t>(bytes, 1);
     return (int)std::max<int64_t>(1, std::min({want, steps / 2, most}));

@@ -62,7 +62,7 @@ __global__ __launch_bounds__((64 * PagedShape<T, DP>::NW), (PagedShape<T, DP>::P
     typedef PagedShape<T, DP> Sh;
     typedef typename M::Frag Frag;
     constexpr int NW = Sh::NW, NP = 32 / M::KC, LD = Sh::LD;
-    __shared__ __align__(16) char lds[NW * Sh::WAVE + NW * 256];
+    __shared__ __align__(256) char lds[NW * Sh::WAVE + NW * 256];
     const int lane = threadIdx.x & 63, w = uniform(threadIdx.x >> 6), hh = lane >> 5;
     const int group = a.Hq / a.Hk;
     const int split = (int)(blockIdx.x % splits), hk = (int)(blockIdx.x / splits % a.Hk), b = (int)(blockIdx.x / splits / a.Hk);
@@ -94,18 +94,17 @@ __global__ __launch_bounds__((64 * PagedShape<T, DP>::NW), (PagedShape<T, DP>::P
         far4(table + divide(key, in), pages + (i & 1) * 256);
         return in;
     };
-    uint32_t at[Sh::LOADS];   // rows of the cache that this lane loads from, ~0 for none
+    uint32_t row = ~0u;       // of the cache, of key l % 32; ~0 for none
+    auto at = [&](int n) { return (uint32_t)__shfl((int)row, (n * 64 + lane) / Ti::U); };   // of load n's
     bool whole;               // of 32 keys and all of the columns
     // The rows of step i; which keys have a page that is none.
     auto find = [&](int i, int in) {
         const int k = begin + (i * NW + w) * 32;
         const int pg = *reinterpret_cast<const int *>(pages + (i & 1) * 256 + 4 * (lane & 31));
         const bool used = k + (lane & 31) < end, none = used && (uint32_t)pg >= (uint32_t)a.pages;
-        const uint32_t row = used && !none ? ((uint32_t)pg * (uint32_t)a.Hk + (uint32_t)hk) * (uint32_t)a.page + (uint32_t)in : ~0u;
+        row = used && !none ? ((uint32_t)pg * (uint32_t)a.Hk + (uint32_t)hk) * (uint32_t)a.page + (uint32_t)in : ~0u;
         const uint32_t bad = (uint32_t)__ballot(none);
         whole = k + 32 <= end && !bad && a.D == DP;
-#pragma unroll
-        for (int n = 0; n < Sh::LOADS; ++n) at[n] = (uint32_t)__shfl((int)row, (n * 64 + lane) / Ti::U);
         return bad;
     };
     auto issue = [&](const void *from, char *to) {
@@ -115,15 +114,16 @@ __global__ __launch_bounds__((64 * PagedShape<T, DP>::NW), (PagedShape<T, DP>::P
 #pragma unroll
             for (int n = 0; n < Sh::LOADS; ++n) {
                 const int idx = n * 64 + lane, unit = (idx % Ti::U) ^ Ti::swz(idx / Ti::U);
-                far16(base + ((uint64_t)at[n] * bytes + (uint32_t)(unit * 16)), to + n * 1024);
+                far16(base + ((uint64_t)at(n) * bytes + (uint32_t)(unit * 16)), to + n * 1024);
             }
             return;
         }
 #pragma unroll
         for (int n = 0; n < Sh::LOADS; ++n) {
             const int idx = n * 64 + lane, unit = (idx % Ti::U) ^ Ti::swz(idx / Ti::U);
-            const bool there = at[n] != ~0u && unit * M::V < a.D;
-            const char *p = base + (uint64_t)at[n] * bytes;
+            const uint32_t r = at(n);
+            const bool there = r != ~0u && unit * M::V < a.D;
+            const char *p = base + (uint64_t)r * bytes;
             if constexpr (FAST) {
                 far16(there ? (const void *)(p + unit * 16) : &kZeros, to + n * 1024);
             } else {

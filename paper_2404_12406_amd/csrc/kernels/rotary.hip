@@ -36,13 +36,12 @@ __device__ __forceinline__ float group_sum(float v) {
 // (halves that are no whole vectors).
 enum Pairing { kNext, kLane, kLoose };
 
-// A lane's part of the rotation: its elements' frequencies (in turns, 64 bits), a token's
+// A lane's part of the rotation: its elements' frequencies, a token's
 // cosines and (signed) sines, and where the partners are.
 template <typename T, int L>
 struct Turn {
     static constexpr int V = Vec16<T>::N;
-    double freq[V];
-    float cs[V], sn[V];
+    float freq[V], cs[V], sn[V];
     int lane;        // kLane: of the partner
     uint32_t flip;   // elements whose sine counts the other way
     __device__ __forceinline__ void init(const RotaryArgs &a, int c, int l, bool back) {
@@ -52,7 +51,7 @@ struct Turn {
         for (int e = 0; e < V; ++e) {
             const int d = c + e;
             const bool second = a.next ? d & 1 : d >= half;
-            freq[e] = d < 2 * half ? (double)a.freq[a.next ? d >> 1 : second ? d - half : d] * 0.15915494309189533577 : 0.0;
+            freq[e] = d < 2 * half ? a.freq[a.next ? d >> 1 : second ? d - half : d] : 0.f;
             flip |= second == back ? 1u << e : 0u;
         }
         const int away = half / V, g = c / V;
@@ -62,7 +61,7 @@ struct Turn {
     __device__ __forceinline__ void take(double pos) {
 #pragma unroll
         for (int e = 0; e < V; ++e) {
-            const double turns = pos * freq[e];
+            const double turns = pos * 0.15915494309189533577 * (double)freq[e];
             float s;
             sincospif(2.f * (float)(turns - rint(turns)), &s, &cs[e]);
             sn[e] = flip >> e & 1 ? -s : s;
@@ -99,7 +98,9 @@ __device__ __forceinline__ int partner_of(const RotaryArgs &a, int d) {
     return d < half ? d + half : d < 2 * half ? d - half : d;
 }
 
-constexpr int kAhead = 4;   // heads of a lane loaded at once, at most
+// Heads of a lane loaded at once, at most; backward, which loads two of each, three leave
+// registers for three waves a SIMD.
+constexpr int kAhead = 4, kAheadBwd = 3;
 
 // A wave's way through its tokens and their heads, `ahead` heads of each of its G groups of
 // lanes at a time; the next ones are loaded before these are worked on.
@@ -117,10 +118,13 @@ struct Way {
 
 // A scale's elements of this lane; ones without it.
 template <typename T>
-__device__ __forceinline__ void scale_of(const T *p, int c, int D, float (&w)[Vec16<T>::N]) {
-    const Vec16<T> v = p ? load_vec<T>(p, c, D) : zero16<T>();
+__device__ __forceinline__ Vec16<T> scale_of(const T *p, int c, int D) {
+    Vec16<T> v;
+    if (p) v = load_vec<T>(p, c, D);
+    else
 #pragma unroll
-    for (int e = 0; e < Vec16<T>::N; ++e) w[e] = p ? to_f32(v.e[e]) : 1.f;
+        for (int e = 0; e < Vec16<T>::N; ++e) v.e[e] = (T)1.f;
+    return v;
 }
 
 // Forward.  APPEND: heads past the Hq queries go to the cache, the last Hk of them (the
@@ -142,9 +146,7 @@ __global__ __launch_bounds__(256) void fwd_kernel(RotaryArgs a, int ahead) {
     Way way{(int64_t)blockIdx.x * 4 + (threadIdx.x >> 6), (int)blockIdx.y * ahead * G};
     Vec16<T> in[kAhead], after[kAhead];
     if (way.t < a.T) load(way, in);
-    float wq[V], wk[V];
-    scale_of<T>(gq, c, a.D, wq);
-    scale_of<T>(gk, c, a.D, wk);
+    const Vec16<T> wq = scale_of<T>(gq, c, a.D), wk = scale_of<T>(gk, c, a.D);
     Turn<T, L> turn;
     turn.init(a, c, lane, false);
     T *kto = nullptr, *vto = nullptr;   // the token's first head in the cache
@@ -185,7 +187,7 @@ __global__ __launch_bounds__(256) void fwd_kernel(RotaryArgs a, int ahead) {
                     for (int e = 0; e < V; ++e) s += z[e] * z[e];
                     r = 1.f / sqrtf(group_sum<L>(s) / (float)a.D + a.eps);
 #pragma unroll
-                    for (int e = 0; e < V; ++e) z[e] = z[e] * r * (query ? wq[e] : wk[e]);
+                    for (int e = 0; e < V; ++e) z[e] = z[e] * r * to_f32(query ? wq.e[e] : wk.e[e]);
                 }
                 turn.template apply<PAIR>(z, [&](int e) {
                     const int p = partner_of(a, c + e);
@@ -205,7 +207,7 @@ __global__ __launch_bounds__(256) void fwd_kernel(RotaryArgs a, int ahead) {
 
 // dx (may be null) and partial rows of dgq and dgk: part[blocks][2][D] (may be null).
 template <typename T, int L, int PAIR>
-__global__ __launch_bounds__(256) void bwd_kernel(RotaryArgs a, int ahead, const T *dy, int64_t dts, int64_t dhs, T *dx, int64_t gts,
+__global__ __launch_bounds__(256, PAIR == kLoose || L * Vec16<T>::N == 256 ? 2 : 3) void bwd_kernel(RotaryArgs a, int ahead, const T *dy, int64_t dts, int64_t dhs, T *dx, int64_t gts,
                                                   int64_t ghs, float *part) {
     constexpr int V = Vec16<T>::N, G = 64 / L, GROUPS = 256 / L;
     __shared__ float meet[GROUPS][L * V];
@@ -213,23 +215,22 @@ __global__ __launch_bounds__(256) void bwd_kernel(RotaryArgs a, int ahead, const
     const T *x = static_cast<const T *>(a.x);
     const T *gq = static_cast<const T *>(a.gq), *gk = static_cast<const T *>(a.gk);
     const int H = a.Hq + a.Hk;
-    auto load = [&](const Way &w, Vec16<T> (&v)[kAhead], Vec16<T> (&d)[kAhead]) {
+    auto load = [&](const Way &w, Vec16<T> (&v)[kAheadBwd], Vec16<T> (&d)[kAheadBwd]) {
         const T *p = x + w.t * a.xts + (w.h + g) * a.xhs, *q = dy + w.t * dts + (w.h + g) * dhs;
 #pragma unroll
-        for (int u = 0; u < kAhead; ++u) {
+        for (int u = 0; u < kAheadBwd; ++u) {
             if (u >= ahead || w.h + g + u * G >= H) continue;
             d[u] = load_vec<T>(q + u * G * dhs, c, a.D);
             if (a.norm) v[u] = load_vec<T>(p + u * G * a.xhs, c, a.D);
         }
     };
     Way way{(int64_t)blockIdx.x * 4 + (threadIdx.x >> 6), (int)blockIdx.y * ahead * G};
-    Vec16<T> xi[kAhead], gi[kAhead], xn[kAhead], gn[kAhead];
+    Vec16<T> xi[kAheadBwd], gi[kAheadBwd], xn[kAheadBwd], gn[kAheadBwd];
     if (way.t < a.T) load(way, xi, gi);
-    float sq[V], sk[V], wq[V], wk[V];
+    float sq[V], sk[V];
 #pragma unroll
     for (int e = 0; e < V; ++e) sq[e] = sk[e] = 0.f;
-    scale_of<T>(gq, c, a.D, wq);
-    scale_of<T>(gk, c, a.D, wk);
+    const Vec16<T> wq = scale_of<T>(gq, c, a.D), wk = scale_of<T>(gk, c, a.D);
     Turn<T, L> turn;
     turn.init(a, c, lane, true);
     for (int64_t seen = -1; way.t < a.T;) {
@@ -241,7 +242,7 @@ __global__ __launch_bounds__(256) void bwd_kernel(RotaryArgs a, int ahead, const
             turn.take(a.R ? (double)a.pos[now.t] : 0.0);
         }
 #pragma unroll
-        for (int u = 0; u < kAhead; ++u) {
+        for (int u = 0; u < kAheadBwd; ++u) {
             const int h = now.h + g + u * G;
             if (u >= ahead || h >= H) continue;
             const bool query = h < a.Hq;
@@ -255,7 +256,7 @@ __global__ __launch_bounds__(256) void bwd_kernel(RotaryArgs a, int ahead, const
                 for (int e = 0; e < V; ++e) {
                     const float v = to_f32(xi[u].e[e]);
                     s += v * v;
-                    m += z[e] * (query ? wq[e] : wk[e]) * v;
+                    m += z[e] * to_f32(query ? wq.e[e] : wk.e[e]) * v;
                 }
                 const float r = 1.f / sqrtf(group_sum<L>(s) / (float)a.D + a.eps);
                 m = group_sum<L>(m) / (float)a.D * r * r;
@@ -264,7 +265,7 @@ __global__ __launch_bounds__(256) void bwd_kernel(RotaryArgs a, int ahead, const
                     const float v = to_f32(xi[u].e[e]), p = z[e] * v * r;
                     if (query) sq[e] += p;
                     else sk[e] += p;
-                    z[e] = r * (z[e] * (query ? wq[e] : wk[e]) - v * m);
+                    z[e] = r * (z[e] * to_f32(query ? wq.e[e] : wk.e[e]) - v * m);
                 }
             }
             if (dx && c < a.D) {
@@ -275,7 +276,7 @@ __global__ __launch_bounds__(256) void bwd_kernel(RotaryArgs a, int ahead, const
             }
         }
 #pragma unroll
-        for (int u = 0; u < kAhead; ++u) {
+        for (int u = 0; u < kAheadBwd; ++u) {
             xi[u] = xn[u];
             gi[u] = gn[u];
         }
@@ -320,7 +321,10 @@ __global__ __launch_bounds__(1024) void sum_kernel(const float *__restrict__ par
 // ------------------------------------------------------------------ host
 namespace {
 
-constexpr int kMostBlocks = 1024, kMostParts = 512;
+// Blocks at most: all at once, so that each wave's way is long (a wave begins with loads that depend on
+// each other).  8192 x 40 heads of 128, bf16: forward 512, 1024, 2048 blocks 46, 40, 43 us;
+// backward, whose blocks leave a partial row each, 512, 768, 1024 blocks 64, 59, 71.
+constexpr int kMostBlocks = 1024, kMostParts = 768;
 
 int lanes(int dtype, int D) {
     const int v = dtype == kBF16 ? 8 : 4, n = (D + v - 1) / v;
@@ -341,8 +345,8 @@ struct Plan {
     int ahead;
 };
 
-Plan plan(int dtype, const RotaryArgs &a, int heads, int most) {
-    const int G = 64 / lanes(dtype, a.D), per = (heads + G - 1) / G, parts = (per + kAhead - 1) / kAhead;
+Plan plan(int dtype, const RotaryArgs &a, int heads, int at_once, int most) {
+    const int G = 64 / lanes(dtype, a.D), per = (heads + G - 1) / G, parts = (per + at_once - 1) / at_once;
     const int64_t bx = std::min<int64_t>((a.T + 3) / 4, most);
     const int64_t by = std::max<int64_t>(1, std::min<int64_t>(parts, most / std::max<int64_t>(bx, 1)));
     return {dim3((unsigned)bx, (unsigned)by), std::max(1, (per + parts - 1) / std::max(parts, 1))};
@@ -372,12 +376,15 @@ void bwd_run(const RotaryArgs &a, const Plan &p, const void *dy, const int64_t d
     case 8: ROT_PAIR(F, 8, __VA_ARGS__) break;               \
     case 16: ROT_PAIR(F, 16, __VA_ARGS__) break;             \
     case 32: ROT_PAIR(F, 32, __VA_ARGS__) break;             \
-    default: ROT_PAIR(F, 64, __VA_ARGS__) break;             \
+    default:   /* (256 bf16 elements take 32) */             \
+        if constexpr (sizeof(T) == 4) {                      \
+            ROT_PAIR(F, 64, __VA_ARGS__)                     \
+        }                                                    \
     }
 
 template <typename T>
 int fwd_t(int dtype, const RotaryArgs &a, bool append, hipStream_t st) {
-    const Plan p = plan(dtype, a, a.Hq + (append ? 2 : 1) * a.Hk, kMostBlocks);
+    const Plan p = plan(dtype, a, a.Hq + (append ? 2 : 1) * a.Hk, kAhead, kMostBlocks);
     ROT_DISPATCH(fwd_run, a, p, append, st)
     return (int)hipGetLastError();
 }
@@ -389,7 +396,7 @@ int bwd_t(int dtype, const RotaryArgs &a, const void *dy, const int64_t ds[2], v
     float *part = params ? static_cast<float *>(ws) : nullptr;
     int rows = 0;
     if (a.T > 0 && a.Hq + a.Hk > 0) {
-        const Plan p = plan(dtype, a, a.Hq + a.Hk, params ? kMostParts : kMostBlocks);
+        const Plan p = plan(dtype, a, a.Hq + a.Hk, kAheadBwd, params ? kMostParts : kMostBlocks);
         ROT_DISPATCH(bwd_run, a, p, dy, ds, dx, gs, part, st)
         rows = (int)(p.grid.x * p.grid.y);
     }
@@ -409,7 +416,7 @@ int launch_rotary_fwd(int dtype, const RotaryArgs &a, bool append, void *stream)
 
 size_t rotary_bwd_workspace(int dtype, const RotaryArgs &a, bool params) {
     if (!params || a.T == 0 || a.Hq + a.Hk == 0) return 0;
-    const dim3 g = rot::plan(dtype, a, a.Hq + a.Hk, rot::kMostParts).grid;
+    const dim3 g = rot::plan(dtype, a, a.Hq + a.Hk, rot::kAheadBwd, rot::kMostParts).grid;
     return ((size_t)g.x * g.y * 2 * a.D * sizeof(float) + 255) / 256 * 256;
 }
 
