@@ -51,7 +51,6 @@ __global__ __launch_bounds__(256, (FwdShape<T, DC>::OCC)) void fwd_kernel(AttnAr
     const int end = min(seen, (int)((int64_t)steps * (blockIdx.y + 1) / part.splits) * BN);
     const int wrow = row0 + 32 * w, rows = min(32, s.na - wrow);                 // the wave's
     const int wend = rows <= 0 ? 0 : a.causal ? min(s.nb, wrow + rows + shift) : s.nb;
-    const int wfull = a.causal ? min(s.nb, wrow + 1 + shift) : s.nb;             // keys that all its rows see
     const int last = a.causal ? min(s.nb - 1, wrow + (lane & 31) + shift) : s.nb - 1;   // the lane's row sees
 
     const T *qp = static_cast<const T *>(a.q.p) + (int64_t)(s.a0 + wrow) * a.q.ts + head * a.q.hs;
@@ -70,14 +69,15 @@ __global__ __launch_bounds__(256, (FwdShape<T, DC>::OCC)) void fwd_kernel(AttnAr
     q.init(qp, a.q.ts, rows, a.D, lane);
 
     const float c = a.scale * kLog2e;
-    float m = -INFINITY, l = 0.f;
+    float m = -INFINITY, l[4] = {0.f, 0.f, 0.f, 0.f};
     floatx16 acc[DC / 32];
 #pragma unroll
     for (int t = 0; t < DC / 32; ++t) acc[t] = zero16x();
-    for (int k = begin; k < end; k += BN) {
+    auto step = [&](int k, auto mode) __attribute__((always_inline)) {
+        constexpr bool MASKED = decltype(mode)::value;
         tile_sync();
         if (k + BN < end) issue(k + BN);
-        if (k >= wend) continue;
+        if (MASKED && k >= wend) return;
         const char *kt = lds + (k / BN & 1) * 2 * BYTES, *vt = kt + BYTES;
         floatx16 x[NS];
 #pragma unroll
@@ -86,13 +86,12 @@ __global__ __launch_bounds__(256, (FwdShape<T, DC>::OCC)) void fwd_kernel(AttnAr
 #pragma unroll
             for (int i = 0; i < DC / M::KC; ++i) x[n] = M::mma(Ti::row_frag(kt, 32 * n, i, lane), q.get(i, lane), x[n]);
         }
-        const bool masked = k + BN > wfull;
-        if (masked) {
+        if constexpr (MASKED) {
 #pragma unroll
             for (int n = 0; n < NS; ++n)
 #pragma unroll
                 for (int i = 0; i < 16; ++i)
-                    if (k + 32 * n + 8 * (i >> 2) + 4 * (lane >> 5) + (i & 3) > last) x[n][i] = -INFINITY;
+                    x[n][i] = k + 32 * n + 8 * (i >> 2) + 4 * (lane >> 5) + (i & 3) > last ? -INFINITY : x[n][i];
         }
         float top = x[0][0];
 #pragma unroll
@@ -105,41 +104,46 @@ __global__ __launch_bounds__(256, (FwdShape<T, DC>::OCC)) void fwd_kernel(AttnAr
         if (__any((top - m) * c > 8.f)) {
             const float to = fmaxf(m, top), f = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((m - to) * c);
             m = to;
-            l *= f;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) l[j] *= f;
 #pragma unroll
             for (int t = 0; t < DC / 32; ++t)
 #pragma unroll
                 for (int i = 0; i < 16; ++i) acc[t][i] *= f;
         }
-        const float ref = m == -INFINITY ? 0.f : m;   // (no key yet)
+        const float ref = m == -INFINITY ? 0.f : m, minus = -ref * c;   // (no key yet)
         Frag p[NS * NP];
 #pragma unroll
         for (int n = 0; n < NS; ++n) {
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
-                x[n][i] = __builtin_amdgcn_exp2f((x[n][i] - ref) * c);
-                l += x[n][i];
+                x[n][i] = power<T>(x[n][i], ref, minus, c);
+                l[i & 3] += x[n][i];
             }
             // (in bf16 rounded to 8 bits, an operand; the sum has all of them)
 #pragma unroll
             for (int i = 0; i < NP; ++i) p[n * NP + i] = as_frag<T>(x[n], i);
         }
-        if (masked && any_wild<T, DP, BN>(vt, 0, lane)) wild_product<T, DP, DC, NS * NP>(acc, vt, 0, p, lane);
+        if (MASKED && any_wild<T, DP, BN>(vt, 0, lane)) wild_product<T, DP, DC, NS * NP>(acc, vt, 0, p, lane);
         else add_product<T, DP, DC, NS * NP>(acc, vt, 0, p, lane);
-    }
+    };
+    // Keys that all of the block's rows see, in whole steps; then the others.
+    const int clear = max(begin, min(end, max(0, a.causal ? min(s.nb, row0 + 1 + shift) : s.nb) / BN * BN));
+    for (int k = begin; k < clear; k += BN) step(k, Full{});
+    for (int k = clear; k < end; k += BN) step(k, Masked{});
     tile_sync();   // no wave reads the tiles any more
     if (rows <= 0) return;
-    l = both_sum(l);
+    const float sum = both_sum((l[0] + l[1]) + (l[2] + l[3]));
     const bool none = last < 0;   // a row that sees no key: zeros
     if (part.splits > 1) {
         const int64_t at = ((int64_t)blockIdx.y * a.Hq + head) * a.Tq + s.a0 + wrow;
         store_sums<DC>(acc, part.sums + at * DC, DC, rows, lane);
-        if (lane < rows) part.stat[at + lane] = floatx2{m, none ? -1.f : l};
+        if (lane < rows) part.stat[at + lane] = floatx2{m, none ? -1.f : sum};
         return;
     }
     if (a.lse && lane < rows)
-        a.lse[(int64_t)head * a.Tq + s.a0 + wrow + lane] = none ? INFINITY : m * c + __builtin_amdgcn_logf(l);
-    store_rows<T, DP, DC>(acc, 1.f / l, none, lds + w * 32 * Ti::RB,
+        a.lse[(int64_t)head * a.Tq + s.a0 + wrow + lane] = none ? INFINITY : m * c + __builtin_amdgcn_logf(sum);
+    store_rows<T, DP, DC>(acc, 1.f / sum, none, lds + w * 32 * Ti::RB,
                       static_cast<T *>(a.o.p) + (int64_t)(s.a0 + wrow) * a.o.ts + head * a.o.hs, a.o.ts, rows, a.D, lane);
 }
 

@@ -56,7 +56,9 @@ __global__ __launch_bounds__(256) void delta_kernel(AttnArgs a, float *__restric
 // ------------------------------------------------------------------ dq
 constexpr int kRows = 128;   // queries of a block of dq, keys of a block of dk and dv
 
-// Whether a wave has registers for both operands that it keeps: not for 192 fp32 elements.
+// Whether a wave has registers for the first, and for the second of the two operands that
+// it keeps: not for 256, for 192 fp32 elements.
+template <typename T, int DC> constexpr bool kHold1 = DC * sizeof(T) < 1024;
 template <typename T, int DC> constexpr bool kHold = DC * sizeof(T) < 768;
 
 // What the kernels take besides: delta, which dq_kernel writes, and where they leave sums in fp32 if the
@@ -94,7 +96,6 @@ __global__ __launch_bounds__(256, (DqShape<T, DC>::OCC)) void dq_kernel(AttnArgs
     const int end = min(seen, (int)((int64_t)steps * (blockIdx.y + 1) / part.splits) * BN);
     const int wrow = row0 + 32 * w, rows = min(32, s.na - wrow);
     const int wend = rows <= 0 ? 0 : a.causal ? min(s.nb, wrow + rows + shift) : s.nb;
-    const int wfull = a.causal ? min(s.nb, wrow + 1 + shift) : s.nb;
     const int last = a.causal ? min(s.nb - 1, wrow + (lane & 31) + shift) : s.nb - 1;
 
     const int64_t first = s.a0 + wrow;
@@ -109,7 +110,7 @@ __global__ __launch_bounds__(256, (DqShape<T, DC>::OCC)) void dq_kernel(AttnArgs
         lv.issue(vp + k * lv.ts, s.nb - k, a.D, to + BYTES, w);
     };
     if (begin < end) issue(begin);
-    Rows<T, DC> q;
+    Rows<T, DC, kHold1<T, DC>> q;
     Rows<T, DC, kHold<T, DC>> g;
     q.init(static_cast<const T *>(a.q.p) + first * a.q.ts + head * a.q.hs, a.q.ts, rows, a.D, lane);
     g.init(static_cast<const T *>(a.go.p) + first * a.go.ts + head * a.go.hs, a.go.ts, rows, a.D, lane);
@@ -124,34 +125,36 @@ __global__ __launch_bounds__(256, (DqShape<T, DC>::OCC)) void dq_kernel(AttnArgs
     floatx16 acc[DC / 32];
 #pragma unroll
     for (int t = 0; t < DC / 32; ++t) acc[t] = zero16x();
-    for (int k = begin; k < end; k += BN) {
+    auto step = [&](int k, auto mode) __attribute__((always_inline)) {
+        constexpr bool MASKED = decltype(mode)::value;
         tile_sync();
         if (k + BN < end) issue(k + BN);
         const char *kt = lds + (k / BN & 1) * 2 * BYTES, *vt = kt + BYTES;
 #pragma unroll
         for (int n = 0; n < BN; n += 32) {
-            if (k + n >= wend) continue;
+            if (MASKED && k + n >= wend) continue;
             floatx16 x = zero16x(), y = zero16x();
 #pragma unroll
             for (int i = 0; i < DC / M::KC; ++i) {
                 x = M::mma(Ti::row_frag(kt, n, i, lane), q.get(i, lane), x);
                 y = M::mma(Ti::row_frag(vt, n, i, lane), g.get(i, lane), y);
             }
-            const bool masked = k + n + 32 > wfull;
 #pragma unroll
-            for (int i = 0; i < 16; ++i) x[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[i], c, -lse)) * (y[i] - delta);
-            if (masked) {
-#pragma unroll
-                for (int i = 0; i < 16; ++i)
-                    if (k + n + 8 * (i >> 2) + 4 * (lane >> 5) + (i & 3) > last) x[i] = 0.f;
+            for (int i = 0; i < 16; ++i) {
+                x[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[i], c, -lse)) * (y[i] - delta);
+                if constexpr (MASKED) x[i] = k + n + 8 * (i >> 2) + 4 * (lane >> 5) + (i & 3) > last ? 0.f : x[i];
             }
             Frag d[NP];   // (an operand: in bf16 rounded)
 #pragma unroll
             for (int i = 0; i < NP; ++i) d[i] = as_frag<T>(x, i);
-            if (masked && any_wild<T, DP, 32>(kt, n, lane)) wild_product<T, DP, DC, NP>(acc, kt, n, d, lane);
+            if (MASKED && any_wild<T, DP, 32>(kt, n, lane)) wild_product<T, DP, DC, NP>(acc, kt, n, d, lane);
             else add_product<T, DP, DC, NP>(acc, kt, n, d, lane);
         }
-    }
+    };
+    // Keys that all of the block's rows see, in whole steps; then the others.
+    const int clear = max(begin, min(end, max(0, a.causal ? min(s.nb, row0 + 1 + shift) : s.nb) / BN * BN));
+    for (int k = begin; k < clear; k += BN) step(k, Full{});
+    for (int k = clear; k < end; k += BN) step(k, Masked{});
     tile_sync();
     if (rows <= 0) return;
     if (part.splits > 1) {
@@ -190,6 +193,9 @@ __global__ __launch_bounds__(256, (DkvShape<T, DC, DK, DV>::OCC)) void dkv_kerne
     const int shift = s.na - s.nb;   // query i sees keys to i + shift
     const int begin = a.causal ? max(0, key0 - shift) / BM * BM : 0;
     const int steps = begin < s.nb ? (s.nb - begin + BM - 1) / BM : 0;   // of one head
+    // Of these, the first ones, where some of the block's keys are hidden from some queries, are a loop
+    // of their own before the others; both go through the heads of the group.
+    const int edge = a.causal ? min(steps, (max(0, key0 + kRows - 1 - shift - begin) + BM - 1) / BM) : 0;
     const int wkey = key0 + 32 * w, keys = min(32, s.na - wkey);
     const int key = wkey + (lane & 31);
 
@@ -198,9 +204,29 @@ __global__ __launch_bounds__(256, (DkvShape<T, DC, DK, DV>::OCC)) void dkv_kerne
     lq.init(a.q.ts, a.D, w, lane);
     lg.init(a.go.ts, a.D, w, lane);
     const uint32_t word = lane < BM ? lane * 4 : 0x80000000u;
-    auto issue = [&](int n) {   // step n of group * steps
+    // Step n of group * steps: a head of the group and its first query; the next one's.
+    struct Place {
+        int h, at;
+    };
+    const int split = begin + edge * BM, stop = begin + steps * BM;
+    auto place_of = [&](int n) {
+        const bool first = n < edge * group;
+        const int m = first ? n : n - edge * group, per = first ? edge : steps - edge, h = m / per;
+        return Place{h, (first ? begin : split) + (m - h * per) * BM};
+    };
+    auto after = [&](Place p) {
+        const bool first = p.at < split;
+        p.at += BM;
+        if (p.at >= (first ? split : stop)) {
+            ++p.h;
+            p.at = first && p.h < group ? begin : split;
+            if (p.h == group) p.h = 0;
+        }
+        return p;
+    };
+    auto issue = [&](int n, const Place &p) {
         char *to = lds + (n & 1) * STAGE;
-        const int head = hk * group + n / steps, at = begin + n % steps * BM;
+        const int head = hk * group + p.h, at = p.at;
         const int64_t row = s.b0 + at;
         lq.issue(reinterpret_cast<const char *>(static_cast<const T *>(a.q.p) + row * a.q.ts + head * a.q.hs), s.nb - at, a.D, to, w);
         lg.issue(reinterpret_cast<const char *>(static_cast<const T *>(a.go.p) + row * a.go.ts + head * a.go.hs), s.nb - at, a.D, to + BYTES, w);
@@ -209,8 +235,12 @@ __global__ __launch_bounds__(256, (DkvShape<T, DC, DK, DV>::OCC)) void dkv_kerne
     };
     const int first_step = (int)((int64_t)steps * group * blockIdx.y / part.splits);
     const int total = (int)((int64_t)steps * group * (blockIdx.y + 1) / part.splits);
-    if (first_step < total) issue(first_step);
-    Rows<T, DC> kf;
+    Place now{0, 0}, next{0, 0};
+    if (first_step < total) {
+        next = place_of(first_step);
+        issue(first_step, next);
+    }
+    Rows<T, DC, kHold1<T, DC>> kf;
     Rows<T, DC, DK && kHold<T, DC>> vf;
     kf.init(static_cast<const T *>(a.k.p) + first * a.k.ts + hk * a.k.hs, a.k.ts, keys, a.D, lane);
     if constexpr (DK) vf.init(static_cast<const T *>(a.v.p) + first * a.v.ts + hk * a.v.hs, a.v.ts, keys, a.D, lane);
@@ -218,23 +248,25 @@ __global__ __launch_bounds__(256, (DkvShape<T, DC, DK, DV>::OCC)) void dkv_kerne
     floatx16 dk[DC / 32], dv[DC / 32];
 #pragma unroll
     for (int t = 0; t < DC / 32; ++t) dk[t] = dv[t] = zero16x();
-    for (int n = first_step; n < total; ++n) {
+    auto step = [&](int n, auto mode) __attribute__((always_inline)) {
+        constexpr bool MASKED = decltype(mode)::value;
         tile_sync();
-        if (n + 1 < total) issue(n + 1);
-        const int at = begin + n % steps * BM;
+        now = next;
+        next = after(now);
+        if (n + 1 < total) issue(n + 1, next);
+        const int at = now.at;
         const char *qt = lds + (n & 1) * STAGE, *gt = qt + BYTES;
         const float *lt = reinterpret_cast<const float *>(gt + BYTES), *dt = lt + 64;
 #pragma unroll
         for (int m = 0; m < BM; m += 32) {
-            const int top = min(at + m + 32, s.nb);   // queries below it
-            if (keys <= 0 || at + m >= s.nb || (a.causal && top - 1 + shift < wkey)) continue;
+            // (rows past the last query are zeros; a wave without keys has nothing to do)
+            if (MASKED && (keys <= 0 || min(at + m + 32, s.nb) - 1 + shift < wkey)) continue;
             floatx16 x = zero16x(), y = zero16x();
 #pragma unroll
             for (int i = 0; i < C; ++i) {
                 x = M::mma(Ti::row_frag(qt, m, i, lane), kf.get(i, lane), x);
                 if constexpr (DK) y = M::mma(Ti::row_frag(gt, m, i, lane), vf.get(i, lane), y);
             }
-            const bool masked = a.causal && at + m + shift < wkey + 31;
 #pragma unroll
             for (int g = 0; g < 4; ++g) {
                 const int r = m + 8 * g + 4 * (lane >> 5);
@@ -243,7 +275,7 @@ __global__ __launch_bounds__(256, (DkvShape<T, DC, DK, DV>::OCC)) void dkv_kerne
                 if constexpr (DK) d4 = *reinterpret_cast<const floatx4 *>(dt + r);
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
-                    const bool hidden = masked && key > at + r + j + shift;
+                    const bool hidden = MASKED && key > at + r + j + shift;
                     const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(x[4 * g + j], c, -l4[j]));
                     x[4 * g + j] = hidden ? 0.f : p;
                     if constexpr (DK) y[4 * g + j] = hidden ? 0.f : p * (y[4 * g + j] - d4[j]);
@@ -254,17 +286,20 @@ __global__ __launch_bounds__(256, (DkvShape<T, DC, DK, DV>::OCC)) void dkv_kerne
             if constexpr (DV) {
 #pragma unroll
                 for (int i = 0; i < NP; ++i) f[i] = as_frag<T>(x, i);
-                if (masked && any_wild<T, DP, 32>(gt, m, lane)) wild_product<T, DP, DC, NP>(dv, gt, m, f, lane);
+                if (MASKED && any_wild<T, DP, 32>(gt, m, lane)) wild_product<T, DP, DC, NP>(dv, gt, m, f, lane);
                 else add_product<T, DP, DC, NP>(dv, gt, m, f, lane);
             }
             if constexpr (DK) {
 #pragma unroll
                 for (int i = 0; i < NP; ++i) f[i] = as_frag<T>(y, i);
-                if (masked && any_wild<T, DP, 32>(qt, m, lane)) wild_product<T, DP, DC, NP>(dk, qt, m, f, lane);
+                if (MASKED && any_wild<T, DP, 32>(qt, m, lane)) wild_product<T, DP, DC, NP>(dk, qt, m, f, lane);
                 else add_product<T, DP, DC, NP>(dk, qt, m, f, lane);
             }
         }
-    }
+    };
+    const int hidden_to = max(first_step, min(total, edge * group));
+    for (int n = first_step; n < hidden_to; ++n) step(n, Masked{});
+    for (int n = hidden_to; n < total; ++n) step(n, Full{});
     tile_sync();
     if (keys <= 0) return;
     if (part.splits > 1) {

@@ -255,6 +255,19 @@ __device__ __forceinline__ float both_max(float v) {
     return fmaxf(h.x, h.y);
 }
 
+// Whether a step has places that some of a wave's rows do not see, known when its loop is
+// compiled: the steps without are a loop of their own.  (In one loop the branch around
+// wild_product() made copies of all sums, 64 moves a step.)
+struct Masked { static constexpr bool value = true; };
+struct Full { static constexpr bool value = false; };
+
+// 2^((s - ref) c).  In bf16 in one operation, on -ref c: where that is large its rounding is the same
+// for a whole row and goes out in the quotient.  In fp32 the difference first, which is exact near ref.
+template <typename T>
+__device__ __forceinline__ float power(float s, float ref, float minus, float c) {
+    return __builtin_amdgcn_exp2f(sizeof(T) == 2 ? __builtin_fmaf(s, c, minus) : (s - ref) * c);
+}
+
 // A 32x32 tile's sums as fragments: chunk c.
 template <typename T>
 __device__ __forceinline__ typename Mat<T>::Frag as_frag(const floatx16 &s, int c) {
