@@ -51,6 +51,7 @@ __global__ __launch_bounds__(256, (FwdShape<T, DC>::OCC)) void fwd_kernel(AttnAr
     const int end = min(seen, (int)((int64_t)steps * (blockIdx.y + 1) / part.splits) * BN);
     const int wrow = row0 + 32 * w, rows = min(32, s.na - wrow);                 // the wave's
     const int wend = rows <= 0 ? 0 : a.causal ? min(s.nb, wrow + rows + shift) : s.nb;
+    const int wfull = a.causal ? min(s.nb, wrow + 1 + shift) : s.nb;             // keys that all its rows see
     const int last = a.causal ? min(s.nb - 1, wrow + (lane & 31) + shift) : s.nb - 1;   // the lane's row sees
 
     const T *qp = static_cast<const T *>(a.q.p) + (int64_t)(s.a0 + wrow) * a.q.ts + head * a.q.hs;
@@ -73,29 +74,26 @@ __global__ __launch_bounds__(256, (FwdShape<T, DC>::OCC)) void fwd_kernel(AttnAr
     floatx16 acc[DC / 32];
 #pragma unroll
     for (int t = 0; t < DC / 32; ++t) acc[t] = zero16x();
-    auto step = [&](int k, auto mode) __attribute__((always_inline)) {
-        constexpr bool MASKED = decltype(mode)::value;
-        tile_sync();
-        if (k + BN < end) issue(k + BN);
-        if (MASKED && k >= wend) return;
-        const char *kt = lds + (k / BN & 1) * 2 * BYTES, *vt = kt + BYTES;
-        floatx16 x[NS];
+    // N 32-key tiles from row r0 of the stage on, of which some rows may not see all.
+    auto attend = [&](const char *kt, const char *vt, int k, int r0, bool masked, auto tiles) __attribute__((always_inline)) {
+        constexpr int N = decltype(tiles)::value;
+        floatx16 x[N];
 #pragma unroll
-        for (int n = 0; n < NS; ++n) {
+        for (int n = 0; n < N; ++n) {
             x[n] = zero16x();
 #pragma unroll
-            for (int i = 0; i < DC / M::KC; ++i) x[n] = M::mma(Ti::row_frag(kt, 32 * n, i, lane), q.get(i, lane), x[n]);
+            for (int i = 0; i < DC / M::KC; ++i) x[n] = M::mma(Ti::row_frag(kt, r0 + 32 * n, i, lane), q.get(i, lane), x[n]);
         }
-        if constexpr (MASKED) {
+        if (masked) {
 #pragma unroll
-            for (int n = 0; n < NS; ++n)
+            for (int n = 0; n < N; ++n)
 #pragma unroll
                 for (int i = 0; i < 16; ++i)
-                    x[n][i] = k + 32 * n + 8 * (i >> 2) + 4 * (lane >> 5) + (i & 3) > last ? -INFINITY : x[n][i];
+                    x[n][i] = k + r0 + 32 * n + 8 * (i >> 2) + 4 * (lane >> 5) + (i & 3) > last ? -INFINITY : x[n][i];
         }
         float top = x[0][0];
 #pragma unroll
-        for (int n = 0; n < NS; ++n)
+        for (int n = 0; n < N; ++n)
 #pragma unroll
             for (int i = 0; i < 16; ++i) top = fmaxf(top, x[n][i]);
         top = both_max(top);
@@ -112,9 +110,9 @@ __global__ __launch_bounds__(256, (FwdShape<T, DC>::OCC)) void fwd_kernel(AttnAr
                 for (int i = 0; i < 16; ++i) acc[t][i] *= f;
         }
         const float ref = m == -INFINITY ? 0.f : m, minus = -ref * c;   // (no key yet)
-        Frag p[NS * NP];
+        Frag p[N * NP];
 #pragma unroll
-        for (int n = 0; n < NS; ++n) {
+        for (int n = 0; n < N; ++n) {
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
                 x[n][i] = power<T>(x[n][i], ref, minus, c);
@@ -124,13 +122,28 @@ __global__ __launch_bounds__(256, (FwdShape<T, DC>::OCC)) void fwd_kernel(AttnAr
 #pragma unroll
             for (int i = 0; i < NP; ++i) p[n * NP + i] = as_frag<T>(x[n], i);
         }
-        if (MASKED && any_wild<T, DP, BN>(vt, 0, lane)) wild_product<T, DP, DC, NS * NP>(acc, vt, 0, p, lane);
-        else add_product<T, DP, DC, NS * NP>(acc, vt, 0, p, lane);
+        if (masked && any_wild<T, DP, 32 * N>(vt, r0, lane)) wild_product<T, DP, DC, N * NP>(acc, vt, r0, p, lane);
+        else add_product<T, DP, DC, N * NP>(acc, vt, r0, p, lane);
     };
-    // Keys that all of the block's rows see, in whole steps; then the others.
+    // The keys that all of the block's rows see, in whole steps; then the others, 32 at a time.
+    // (Two loops: around the rare path of masked keys the compiler copies all sums, 64 moves a step.)
     const int clear = max(begin, min(end, max(0, a.causal ? min(s.nb, row0 + 1 + shift) : s.nb) / BN * BN));
-    for (int k = begin; k < clear; k += BN) step(k, Full{});
-    for (int k = clear; k < end; k += BN) step(k, Masked{});
+    int k = begin;
+    auto stage = [&]() __attribute__((always_inline)) {
+        tile_sync();
+        if (k + BN < end) issue(k + BN);
+        return lds + (k / BN & 1) * 2 * BYTES;
+    };
+    for (; k < clear; k += BN) {
+        const char *kt = stage();
+        attend(kt, kt + BYTES, k, 0, false, Number<NS>{});
+    }
+    for (; k < end; k += BN) {
+        const char *kt = stage();
+#pragma unroll
+        for (int r = 0; r < BN; r += 32)
+            if (k + r < wend) attend(kt, kt + BYTES, k, r, k + r + 32 > wfull, Number<1>{});
+    }
     tile_sync();   // no wave reads the tiles any more
     if (rows <= 0) return;
     const float sum = both_sum((l[0] + l[1]) + (l[2] + l[3]));

@@ -96,6 +96,7 @@ __global__ __launch_bounds__(256, (DqShape<T, DC>::OCC)) void dq_kernel(AttnArgs
     const int end = min(seen, (int)((int64_t)steps * (blockIdx.y + 1) / part.splits) * BN);
     const int wrow = row0 + 32 * w, rows = min(32, s.na - wrow);
     const int wend = rows <= 0 ? 0 : a.causal ? min(s.nb, wrow + rows + shift) : s.nb;
+    const int wfull = a.causal ? min(s.nb, wrow + 1 + shift) : s.nb;
     const int last = a.causal ? min(s.nb - 1, wrow + (lane & 31) + shift) : s.nb - 1;
 
     const int64_t first = s.a0 + wrow;
@@ -133,6 +134,7 @@ __global__ __launch_bounds__(256, (DqShape<T, DC>::OCC)) void dq_kernel(AttnArgs
 #pragma unroll
         for (int n = 0; n < BN; n += 32) {
             if (MASKED && k + n >= wend) continue;
+            const bool masked = MASKED && k + n + 32 > wfull;
             floatx16 x = zero16x(), y = zero16x();
 #pragma unroll
             for (int i = 0; i < DC / M::KC; ++i) {
@@ -140,14 +142,15 @@ __global__ __launch_bounds__(256, (DqShape<T, DC>::OCC)) void dq_kernel(AttnArgs
                 y = M::mma(Ti::row_frag(vt, n, i, lane), g.get(i, lane), y);
             }
 #pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                x[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[i], c, -lse)) * (y[i] - delta);
-                if constexpr (MASKED) x[i] = k + n + 8 * (i >> 2) + 4 * (lane >> 5) + (i & 3) > last ? 0.f : x[i];
+            for (int i = 0; i < 16; ++i) x[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[i], c, -lse)) * (y[i] - delta);
+            if (masked) {
+#pragma unroll
+                for (int i = 0; i < 16; ++i) x[i] = k + n + 8 * (i >> 2) + 4 * (lane >> 5) + (i & 3) > last ? 0.f : x[i];
             }
             Frag d[NP];   // (an operand: in bf16 rounded)
 #pragma unroll
             for (int i = 0; i < NP; ++i) d[i] = as_frag<T>(x, i);
-            if (MASKED && any_wild<T, DP, 32>(kt, n, lane)) wild_product<T, DP, DC, NP>(acc, kt, n, d, lane);
+            if (masked && any_wild<T, DP, 32>(kt, n, lane)) wild_product<T, DP, DC, NP>(acc, kt, n, d, lane);
             else add_product<T, DP, DC, NP>(acc, kt, n, d, lane);
         }
     };
@@ -261,6 +264,7 @@ __global__ __launch_bounds__(256, (DkvShape<T, DC, DK, DV>::OCC)) void dkv_kerne
         for (int m = 0; m < BM; m += 32) {
             // (rows past the last query are zeros; a wave without keys has nothing to do)
             if (MASKED && (keys <= 0 || min(at + m + 32, s.nb) - 1 + shift < wkey)) continue;
+            const bool masked = MASKED && at + m + shift < wkey + 31;
             floatx16 x = zero16x(), y = zero16x();
 #pragma unroll
             for (int i = 0; i < C; ++i) {
@@ -275,7 +279,7 @@ __global__ __launch_bounds__(256, (DkvShape<T, DC, DK, DV>::OCC)) void dkv_kerne
                 if constexpr (DK) d4 = *reinterpret_cast<const floatx4 *>(dt + r);
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
-                    const bool hidden = MASKED && key > at + r + j + shift;
+                    const bool hidden = masked && key > at + r + j + shift;
                     const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(x[4 * g + j], c, -l4[j]));
                     x[4 * g + j] = hidden ? 0.f : p;
                     if constexpr (DK) y[4 * g + j] = hidden ? 0.f : p * (y[4 * g + j] - d4[j]);
@@ -286,13 +290,13 @@ __global__ __launch_bounds__(256, (DkvShape<T, DC, DK, DV>::OCC)) void dkv_kerne
             if constexpr (DV) {
 #pragma unroll
                 for (int i = 0; i < NP; ++i) f[i] = as_frag<T>(x, i);
-                if (MASKED && any_wild<T, DP, 32>(gt, m, lane)) wild_product<T, DP, DC, NP>(dv, gt, m, f, lane);
+                if (masked && any_wild<T, DP, 32>(gt, m, lane)) wild_product<T, DP, DC, NP>(dv, gt, m, f, lane);
                 else add_product<T, DP, DC, NP>(dv, gt, m, f, lane);
             }
             if constexpr (DK) {
 #pragma unroll
                 for (int i = 0; i < NP; ++i) f[i] = as_frag<T>(y, i);
-                if (MASKED && any_wild<T, DP, 32>(qt, m, lane)) wild_product<T, DP, DC, NP>(dk, qt, m, f, lane);
+                if (masked && any_wild<T, DP, 32>(qt, m, lane)) wild_product<T, DP, DC, NP>(dk, qt, m, f, lane);
                 else add_product<T, DP, DC, NP>(dk, qt, m, f, lane);
             }
         }

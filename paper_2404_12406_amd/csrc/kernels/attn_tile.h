@@ -38,6 +38,7 @@ template <> struct Mat<float> {
 };
 
 typedef short v4i16 __attribute__((ext_vector_type(4)));
+typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
 typedef __attribute__((address_space(3))) v4i16 lds_v4i16_t;
 typedef __attribute__((address_space(3))) char lds_char_t;
 
@@ -261,6 +262,8 @@ __device__ __forceinline__ float both_max(float v) {
 struct Masked { static constexpr bool value = true; };
 struct Full { static constexpr bool value = false; };
 
+template <int N> struct Number { static constexpr int value = N; };
+
 // 2^((s - ref) c).  In bf16 in one operation, on -ref c: where that is large its rounding is the same
 // for a whole row and goes out in the quotient.  In fp32 the difference first, which is exact near ref.
 template <typename T>
@@ -288,18 +291,20 @@ __device__ __forceinline__ floatx16 zero16x() {
 template <typename T, int DP, int ROWS>
 __device__ __forceinline__ bool any_wild(const char *tile, int r0, int lane) {
     typedef Tile<T, DP> Ti;
-    uint32_t bad = 0;
+    // by the largest magnitude, of halves of words in bf16
+    u16x2 top = {0, 0};
+    uint32_t most = 0;
 #pragma unroll 2
     for (int i = 0; i < ROWS * Ti::U / 64; ++i) {
         const u32x4 v = *reinterpret_cast<const u32x4 *>(tile + r0 * Ti::RB + i * 1024 + lane * 16);
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-            // an exponent of ones carries into the bit above it
-            if constexpr (sizeof(T) == 2) bad |= ((v[j] & 0x7f807f80u) + 0x00800080u) & 0x80008000u;
-            else bad |= ((v[j] & 0x7f800000u) + 0x00800000u) & 0x80000000u;
+            if constexpr (sizeof(T) == 2) top = __builtin_elementwise_max(top, __builtin_bit_cast(u16x2, v[j] & 0x7fff7fffu));
+            else most = max(most, v[j] & 0x7fffffffu);
         }
     }
-    return __any(bad != 0);
+    const bool bad = sizeof(T) == 2 ? top[0] >= 0x7f80u || top[1] >= 0x7f80u : most >= 0x7f800000u;
+    return __any(bad);
 }
 
 // acc += columns of `tile` times b (N chunks), a row at a time, where a weight of zero
