@@ -234,11 +234,12 @@ inline int64_t span_slots(bool packed, int n, int64_t Ta, int rows) {
     return packed ? Ta / rows + n + 2 : (Ta + rows - 1) / rows;
 }
 
-// Blocks of few rows' worth of work divide their other side: `splits` of them, of `steps`
-// steps on average, where that leaves each two steps and the partial sums below 24 MiB.
-// (fp32, 1777 rows in 5 sequences, 6 on 2 heads of 72, all gradients: 906 -> 250 us.)
+// Where there are few blocks they divide their other side: to some 1024 of them, as long as
+// two of the `steps` that they have on average are left to each and the partial sums stay
+// below 24 MiB.
+// (fp32, 1777 rows in 5 sequences, 6 on 2 heads of 72, all gradients: 906 -> 190 us; with 512 blocks 202.)
 inline int span_splits(int64_t blocks, int64_t steps, int64_t bytes) {
-    const int64_t want = 512 / std::max<int64_t>(blocks, 1), most = (int64_t(24) << 20) / std::max<int64_t>(bytes, 1);
+    const int64_t want = 1024 / std::max<int64_t>(blocks, 1), most = (int64_t(24) << 20) / std::max<int64_t>(bytes, 1);
     return (int)std::max<int64_t>(1, std::min({want, steps / 2, most}));
 }
 
