@@ -285,6 +285,15 @@ __global__ __launch_bounds__(256, (DkvShape<T, DC, DK, DV>::OCC)) void dkv_kerne
                     if constexpr (DK) y[4 * g + j] = hidden ? 0.f : p * (y[4 * g + j] - d4[j]);
                 }
             }
+            // Past the last query: zeros, also where a score is none, such as 0 times a key's infinity.
+            if (at + m + 32 > s.nb) {
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    const bool past = at + m + 8 * (i >> 2) + 4 * (lane >> 5) + (i & 3) >= s.nb;
+                    x[i] = past ? 0.f : x[i];
+                    y[i] = past ? 0.f : y[i];
+                }
+            }
             // (both are operands: in bf16 rounded)
             Frag f[NP];
             if constexpr (DV) {

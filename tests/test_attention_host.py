@@ -13,6 +13,7 @@ ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 NATIVE = os.path.join(ROOT, "tests", "native")
 BUILD = os.path.join(NATIVE, "_build")
 FAKE = 0x7f0000000000   # an aligned address that nobody reads
+OUT = FAKE + (1 << 40)  # another, of results
 DT = {"f32": L.MS_F32, "bf16": L.MS_BF16}
 SAVED_X, SAVED_W, SAVED_Y, SAVED_LSE, SAVED_B, SAVED_INDEX = 1, 2, 32, 256, 1024, 2048
 
@@ -85,14 +86,14 @@ class Call:
                           gq=tensor((D,), dtype), gk=tensor((D,), dtype), tables=FAKE, n=TQ, width=WIDTH,
                           kp=tensor((PAGES, HK, PAGE, D), dtype), vp=tensor((PAGES, HK, PAGE, D), dtype))
         if kind == "rotary":
-            a.update(x=tensor((TQ, HQ + HK, D), dtype), y=tensor((TQ, HQ + HK, D), dtype, addr=FAKE + (1 << 30)))
+            a.update(x=tensor((TQ, HQ + HK, D), dtype), y=tensor((TQ, HQ + HK, D), dtype, addr=OUT))
         elif kind == "attention":
-            a.update(x=tensor((TQ, HQ, D), dtype), gq=tensor((TK, HK, D), dtype), gk=tensor((TK, HK, D), dtype), y=tensor((TQ, HQ, D), dtype),
+            a.update(x=tensor((TQ, HQ, D), dtype), gq=tensor((TK, HK, D), dtype), gk=tensor((TK, HK, D), dtype), y=tensor((TQ, HQ, D), dtype, addr=OUT),
                      qoff=FAKE, koff=FAKE, n=3, kept=FAKE)
         elif kind == "append":
-            a.update(x=tensor((TQ, HQ + 2 * HK, D), dtype), y=tensor((TQ, HQ, D), dtype), rows=None, mask=0)
+            a.update(x=tensor((TQ, HQ + 2 * HK, D), dtype), y=tensor((TQ, HQ, D), dtype, addr=OUT), rows=None, mask=0)
         else:
-            a.update(x=tensor((TQ, HQ, D), dtype), y=tensor((TQ, HQ, D), dtype), lengths=FAKE, mask=0)
+            a.update(x=tensor((TQ, HQ, D), dtype), y=tensor((TQ, HQ, D), dtype, addr=OUT), lengths=FAKE, mask=0)
         a.update(over)
         self.h = ctypes.c_void_p()
 
@@ -186,6 +187,10 @@ def heads(T=TQ, H=HQ, D_=D, dtype="bf16", **kw):
     return tensor((T, H, D_), dtype, **kw)
 
 
+def out(*a, **kw):
+    return heads(*a, addr=OUT, **kw)
+
+
 def pages(*shape, dtype="bf16", **kw):
     return tensor(shape or (PAGES, HK, PAGE, D), dtype, **kw)
 
@@ -197,9 +202,9 @@ COMMON = [
     (L.MS_E_SHAPE, dict(x=tensor((TQ, HQ * D)))),
     (L.MS_E_SHAPE, dict(x=heads(T=-1))),
     (L.MS_E_DTYPE, dict(x=tensor((TQ, HQ, D), 9))),
-    (L.MS_E_DTYPE, dict(y=heads(dtype="f32"))),
+    (L.MS_E_DTYPE, dict(y=out(dtype="f32"))),
     (L.MS_E_LAYOUT, dict(x=heads(strides=(-HQ * D, D, 1)))),
-    (L.MS_E_LAYOUT, dict(y=heads(strides=(D, D, 1)))),
+    (L.MS_E_LAYOUT, dict(y=out(strides=(D, D, 1)))),
 ]
 ROTARY = [
     (L.MS_E_NULL, dict(rotary=False)), (L.MS_E_NULL, dict(pos=None)), (L.MS_E_NULL, dict(freq=None)),
@@ -227,10 +232,10 @@ REFUSED = [(k, s, o) for k in KINDS for s, o in COMMON] + [
     (k, L.MS_E_NULL, dict(rec=False)) for k in TRAINED] + [(k, L.MS_E_MASK, dict(mask=8)) for k in TRAINED] + [
     (k, s, o) for k in ("rotary", "append") for s, o in ROTARY] + [(k, s, o) for k in ("append", "paged") for s, o in CACHE] + [
     ("rotary", L.MS_E_MASK, dict(gq=None)), ("rotary", L.MS_E_MASK, dict(gk=None)),
-    ("rotary", L.MS_E_SHAPE, dict(y=heads(H=HQ + HK, T=TQ + 1))),
+    ("rotary", L.MS_E_SHAPE, dict(y=out(H=HQ + HK, T=TQ + 1))),
     ("rotary", L.MS_E_ARG, dict(y=heads(H=HQ + HK))),   # in place, and the backward reads x
-    ("rotary", L.MS_E_UNSUPPORTED, dict(x=heads(H=HQ + HK, D_=257), y=heads(H=HQ + HK, D_=257), gq=None, gk=None, mask=1)),
-    ("rotary", L.MS_E_UNSUPPORTED, dict(x=heads(H=HQ + HK, D_=0), y=heads(H=HQ + HK, D_=0), gq=None, gk=None, mask=1)),
+    ("rotary", L.MS_E_UNSUPPORTED, dict(x=heads(H=HQ + HK, D_=257), y=out(H=HQ + HK, D_=257), gq=None, gk=None, mask=1)),
+    ("rotary", L.MS_E_UNSUPPORTED, dict(x=heads(H=HQ + HK, D_=0), y=out(H=HQ + HK, D_=0), gq=None, gk=None, mask=1)),
     ("rotary", L.MS_E_UNSUPPORTED, dict(x=heads(T=2 ** 24, H=8, D_=16))),
     ("attention", L.MS_E_NULL, dict(gq=None)), ("attention", L.MS_E_NULL, dict(gk=None)), ("attention", L.MS_E_NULL, dict(kept=None)),
     ("attention", L.MS_E_NULL, dict(qoff=None)),   # k_offsets alone
@@ -238,18 +243,22 @@ REFUSED = [(k, s, o) for k in KINDS for s, o in COMMON] + [
     ("attention", L.MS_E_ARG, dict(n=-1)), ("attention", L.MS_E_ARG, dict(scale=0.0)), ("attention", L.MS_E_ARG, dict(scale=-1.0)),
     ("attention", L.MS_E_ARG, dict(scale=float("nan"))), ("attention", L.MS_E_ARG, dict(scale=float("inf"))),
     ("attention", L.MS_E_SHAPE, K(H=4)), ("attention", L.MS_E_SHAPE, K(H=0)), ("attention", L.MS_E_SHAPE, K(D_=D + 8)),
-    ("attention", L.MS_E_SHAPE, dict(gk=heads(T=TK + 1, H=HK))), ("attention", L.MS_E_SHAPE, dict(y=heads(T=TQ + 1))),
+    ("attention", L.MS_E_SHAPE, dict(gk=heads(T=TK + 1, H=HK))), ("attention", L.MS_E_SHAPE, dict(y=out(T=TQ + 1))),
     ("attention", L.MS_E_DTYPE, K(dtype="f32")), ("attention", L.MS_E_LAYOUT, dict(gk=heads(T=TK, H=HK, strides=(HK * D, -D, 1)))),
-    ("attention", L.MS_E_UNSUPPORTED, dict(x=heads(D_=257), y=heads(D_=257), **K(D_=257))),
-    ("attention", L.MS_E_UNSUPPORTED, dict(x=heads(T=1, H=65536, D_=8), y=heads(T=1, H=65536, D_=8), **K(H=1, D_=8))),
-    ("attention", L.MS_E_UNSUPPORTED, dict(x=heads(T=2 ** 28, H=7, D_=1), y=heads(T=2 ** 28, H=7, D_=1), **K(H=1, D_=1))),
+    ("attention", L.MS_E_UNSUPPORTED, dict(x=heads(D_=257), y=out(D_=257), **K(D_=257))),
+    ("attention", L.MS_E_UNSUPPORTED, dict(x=heads(T=1, H=65536, D_=8), y=out(T=1, H=65536, D_=8), **K(H=1, D_=8))),
+    ("attention", L.MS_E_UNSUPPORTED, dict(x=heads(T=2 ** 28, H=7, D_=1), y=out(T=2 ** 28, H=7, D_=1), **K(H=1, D_=1))),
     ("attention", L.MS_E_UNSUPPORTED, dict(n=2 ** 22)),   # blocks of 128 rows
-    ("append", L.MS_E_SHAPE, dict(x=heads(H=HQ + 2 * HK + 1))), ("append", L.MS_E_SHAPE, dict(y=heads(H=HQ + 1))),
+    ("append", L.MS_E_SHAPE, dict(x=heads(H=HQ + 2 * HK + 1))), ("append", L.MS_E_SHAPE, dict(y=out(H=HQ + 1))),
     ("append", L.MS_E_SHAPE, dict(n=TQ - 1)), ("append", L.MS_E_ARG, dict(rows=FAKE + 2)), ("append", L.MS_E_NULL, dict(R=0, pos=None)),
     ("paged", L.MS_E_SHAPE, dict(n=TQ + 1)), ("paged", L.MS_E_NULL, dict(lengths=None)), ("paged", L.MS_E_ARG, dict(lengths=FAKE + 2)),
-    ("paged", L.MS_E_ARG, dict(scale=0.0)), ("paged", L.MS_E_ARG, dict(scale=float("nan"))), ("paged", L.MS_E_SHAPE, dict(y=heads(D_=8))),
-    ("paged", L.MS_E_SHAPE, dict(x=heads(H=5), y=heads(H=5))), ("paged", L.MS_E_SHAPE, dict(x=heads(H=0), y=heads(H=0))),
-    ("paged", L.MS_E_UNSUPPORTED, dict(width=2 ** 28)),
+    ("paged", L.MS_E_ARG, dict(scale=0.0)), ("paged", L.MS_E_ARG, dict(scale=float("nan"))), ("paged", L.MS_E_SHAPE, dict(y=out(D_=8))),
+    ("paged", L.MS_E_SHAPE, dict(x=heads(H=5), y=out(H=5))), ("paged", L.MS_E_SHAPE, dict(x=heads(H=0), y=out(H=0))),
+    ("paged", L.MS_E_UNSUPPORTED, dict(width=2 ** 28)), ("paged", L.MS_E_UNSUPPORTED, dict(width=2 ** 28 - 512)),
+    # results where other blocks, or the backward, read
+    ("attention", L.MS_E_ARG, dict(y=heads())), ("attention", L.MS_E_ARG, dict(y=heads(), x=heads(addr=FAKE + 4096), mask=0)),
+    ("rotary", L.MS_E_ARG, dict(mask=0, y=heads(H=HQ + HK, strides=(D, TQ * D, 1)))), ("append", L.MS_E_ARG, dict(y=heads())),
+    ("paged", L.MS_E_ARG, dict(y=heads(strides=(D, TQ * D, 1)))),
 ]
 
 
@@ -280,8 +289,8 @@ def test_backward_refusals_leave_the_record_usable(stub, kind):
     assert c.backward(dy=None) == L.MS_E_NULL
     assert c.backward(mask=3) == L.MS_E_MASK             # no place for a gradient that was asked for
     H = c.a["y"].shape[1]
-    assert c.backward(dy=heads(T=TQ + 1, H=H)) == L.MS_E_SHAPE
-    assert c.backward(dy=heads(H=H, dtype="f32")) == L.MS_E_DTYPE
+    assert c.backward(dy=out(T=TQ + 1, H=H)) == L.MS_E_SHAPE
+    assert c.backward(dy=out(H=H, dtype="f32")) == L.MS_E_DTYPE
     stub.ms_testing_fail_next_workspace(1)
     assert c.backward() == L.MS_E_NOMEM
     assert stub.attention_log() == b""
@@ -309,7 +318,7 @@ def test_other_layouts_are_staged(stub, kind, dtype):
     c = Call(stub, kind, dtype)
     x, y = shape(c, "x"), shape(c, "y")
     apart = lambda s, addr: tensor(s, dtype, strides=(2 * s[1] * s[2], 2 * s[2], 2), addr=addr)
-    c = Call(stub, kind, dtype, x=apart(x, FAKE), y=apart(y, FAKE + (1 << 30)))
+    c = Call(stub, kind, dtype, x=apart(x, FAKE), y=apart(y, OUT))
     assert c.forward() == 0
     assert stub.attention_log().count(b"pack;") == 1 and stub.stub_log() == b"copy4;"
     if kind in TRAINED:
@@ -346,7 +355,7 @@ def test_unaligned_pointers_are_staged(stub, addr, packs):
 @pytest.mark.parametrize("d", [1, 3, 31, 33, 255])
 def test_odd_head_sizes_are_padded(stub, d):
     for dtype in ("bf16", "f32"):
-        c = Call(stub, "attention", dtype, x=heads(D_=d, dtype=dtype), y=heads(D_=d, dtype=dtype), **K(D_=d, dtype=dtype))
+        c = Call(stub, "attention", dtype, x=heads(D_=d, dtype=dtype), y=out(D_=d, dtype=dtype), **K(D_=d, dtype=dtype))
         assert c.forward() == 0 and stub.attention_log().count(b"pack;") == 3 and stub.stub_log() == b"copy4;"
         reset(stub)
         assert c.backward() == 0 and stub.attention_log().count(b"pack;") == 5 and stub.stub_log() == b"copy4;" * 3
@@ -384,6 +393,10 @@ def test_caches_without_pages_or_heads_of_queries(stub):
     assert Call(stub, "append", rows=FAKE, n=1).forward() == 0          # many tokens of one sequence
 
 
+def test_tables_of_the_most_places(stub):
+    assert Call(stub, "paged", width=2 ** 28 - 513).forward() == 0
+
+
 @pytest.mark.parametrize("kind", TRAINED)
 def test_backward_from_the_fixed_scratch(stub, kind):
     c = Call(stub, kind)
@@ -397,6 +410,9 @@ def test_backward_from_the_fixed_scratch(stub, kind):
 
 
 def test_in_place_without_a_record(stub):
+    H = HQ + 2 * HK
+    assert Call(stub, "append", y=heads(strides=(H * D, D, 1))).forward() == 0   # x's first heads
+    assert Call(stub, "paged", y=heads()).forward() == 0
     for over in (dict(mask=0), dict(mask=1, norm=0, gq=None, gk=None)):   # what the backward reads is not overwritten
         c = Call(stub, "rotary", y=heads(H=HQ + HK), **over)
         assert c.forward() == 0

@@ -262,6 +262,25 @@ def test_hidden_places_hold_anything(bad, D, dtype):
             close("kv"[i - 2], outs[i][at + 1:], refs[i][at + 1:], bars[i][at + 1:])
 
 
+@DTYPES
+@pytest.mark.parametrize("D", [64, 128, 256])
+@pytest.mark.parametrize("n", [1, 40, 64, 150])
+def test_a_key_that_no_query_weighs(n, D, dtype):
+    """Scores of minus infinity with one key, from every query: its gradients are 0, all
+    others as without it (rows past the last query add nothing to it)."""
+    keys, at = 90, 41
+    q, k, v, g = draw((n, 2, D), dtype, 0), draw((keys, 2, D), dtype, 1), draw((keys, 2, D), dtype, 2), draw((n, 2, D), dtype, 3)
+    q[:, :, 0] = 1.0
+    k[:, :, 0] = 0.0
+    rest = torch.arange(keys, device="cuda") != at
+    refs, bars = reference(q, k[rest], v[rest], g, [n], [keys - 1], False, D ** -0.5, dtype)
+    k[at, :, 0] = -math.inf
+    o, _, dk, dv = run(q, k, v, g, 6, ms.Attention(causal=False))
+    assert (dk[at] == 0).all() and (dv[at] == 0).all()
+    for name, got, i in (("o", o, 0), ("k", dk[rest], 2), ("v", dv[rest], 3)):
+        close(name, got, refs[i], bars[i])
+
+
 def test_scores_without_a_distribution():
     """All visible scores minus infinity, or one plus infinity: NaN; a single minus infinity: left out."""
     D = 64
