@@ -30,15 +30,16 @@ struct Parts {
     floatx2 *stat;
 };
 
-template <typename T, int DC>
-__global__ __launch_bounds__(256, (FwdShape<T, DC>::OCC)) void fwd_kernel(AttnArgs a, Parts part) {
+// WG: groups of four waves.  Two take every other step each, from stages of their own, and meet at the end.
+template <typename T, int DC, int WG>
+__global__ __launch_bounds__(256 * WG, (FwdShape<T, DC>::OCC / WG)) void fwd_kernel(AttnArgs a, Parts part) {
     constexpr int DP = kPitch<DC>;
     typedef Mat<T> M;
     typedef Tile<T, DP> Ti;
     typedef typename M::Frag Frag;
     constexpr int BN = FwdShape<T, DC>::BN, NS = BN / 32, NP = 32 / M::KC, BYTES = BN * Ti::RB;
-    __shared__ __align__(256) char lds[4 * BYTES];
-    const int lane = threadIdx.x & 63, w = uniform(threadIdx.x >> 6);
+    __shared__ __align__(256) char lds[4 * BYTES * WG];
+    const int lane = threadIdx.x & 63, w = uniform(threadIdx.x >> 6) & 3, side = WG > 1 ? uniform(threadIdx.x >> 8) : 0;
     int head, rank;
     find_head((int)blockIdx.x, a.Hq, head, rank);
     const int hk = head / (a.Hq / a.Hk);
@@ -60,12 +61,13 @@ __global__ __launch_bounds__(256, (FwdShape<T, DC>::OCC)) void fwd_kernel(AttnAr
     Loader<T, DP, BN, 4> lk, lv;
     lk.init(a.k.ts, a.D, w, lane);
     lv.init(a.v.ts, a.D, w, lane);
+    char *stages = lds + side * 4 * BYTES;
     auto issue = [&](int k) {
-        char *to = lds + (k / BN & 1) * 2 * BYTES;
+        char *to = stages + (k / (BN * WG) & 1) * 2 * BYTES;
         lk.issue(kp + k * lk.ts, s.nb - k, a.D, to, w);
         lv.issue(vp + k * lv.ts, s.nb - k, a.D, to + BYTES, w);
     };
-    if (begin < end) issue(begin);
+    if (begin + side * BN < end) issue(begin + side * BN);
     Rows<T, DC> q;
     q.init(qp, a.q.ts, rows, a.D, lane);
 
@@ -129,24 +131,56 @@ __global__ __launch_bounds__(256, (FwdShape<T, DC>::OCC)) void fwd_kernel(AttnAr
     // (Two loops: around the rare path of masked keys the compiler copies all sums, 64 moves a step.)
     const int clear = max(begin, min(end, max(0, a.causal ? min(s.nb, row0 + 1 + shift) : s.nb) / BN * BN));
     int k = begin;
-    auto stage = [&]() __attribute__((always_inline)) {
+    auto stage = [&](int own) __attribute__((always_inline)) {
         tile_sync();
-        if (k + BN < end) issue(k + BN);
-        return lds + (k / BN & 1) * 2 * BYTES;
+        if (own + BN * WG < end) issue(own + BN * WG);
+        return stages + (own / (BN * WG) & 1) * 2 * BYTES;
     };
-    for (; k < clear; k += BN) {
-        const char *kt = stage();
-        attend(kt, kt + BYTES, k, 0, false, Number<NS>{});
+    for (; k + (WG - 1) * BN < clear; k += BN * WG) {
+        const int own = k + side * BN;
+        const char *kt = stage(own);
+        attend(kt, kt + BYTES, own, 0, false, Number<NS>{});
     }
-    for (; k < end; k += BN) {
-        const char *kt = stage();
+    for (; k < end; k += BN * WG) {
+        const int own = k + side * BN;
+        const char *kt = stage(own);
 #pragma unroll
         for (int r = 0; r < BN; r += 32)
-            if (k + r < wend) attend(kt, kt + BYTES, k, r, k + r + 32 > wfull, Number<1>{});
+            if (own + r < min(wend, end)) attend(kt, kt + BYTES, own, r, own + r + 32 > wfull, Number<1>{});
     }
     tile_sync();   // no wave reads the tiles any more
+    float sum = both_sum((l[0] + l[1]) + (l[2] + l[3]));
+    if constexpr (WG > 1) {   // the second group's sums, maximum and sum of weights to the first
+        char *to = lds + w * (DC * 128 + 512);
+        floatx4 *sums = reinterpret_cast<floatx4 *>(to) + lane;
+        floatx2 *stat = reinterpret_cast<floatx2 *>(to + DC * 128) + lane;
+        if (side) {
+            *stat = floatx2{m, sum};
+#pragma unroll
+            for (int t = 0; t < DC / 32; ++t)
+#pragma unroll
+                for (int g = 0; g < 4; ++g) sums[64 * (4 * t + g)] = floatx4{acc[t][4 * g], acc[t][4 * g + 1], acc[t][4 * g + 2], acc[t][4 * g + 3]};
+        }
+        tile_sync();
+        if (!side) {
+            const floatx2 st = *stat;
+            const float top = fmaxf(m, st.x), f = m == top ? 1.f : __builtin_amdgcn_exp2f((m - top) * c),
+                        h = st.x == top ? 1.f : __builtin_amdgcn_exp2f((st.x - top) * c);
+            m = top;
+            sum = f * sum + h * st.y;
+#pragma unroll
+            for (int t = 0; t < DC / 32; ++t)
+#pragma unroll
+                for (int g = 0; g < 4; ++g) {
+                    const floatx4 v = sums[64 * (4 * t + g)];
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) acc[t][4 * g + j] = f * acc[t][4 * g + j] + h * v[j];
+                }
+        }
+        tile_sync();
+        if (side) return;
+    }
     if (rows <= 0) return;
-    const float sum = both_sum((l[0] + l[1]) + (l[2] + l[3]));
     const bool none = last < 0;   // a row that sees no key: zeros
     if (part.splits > 1) {
         const int64_t at = ((int64_t)blockIdx.y * a.Hq + head) * a.Tq + s.a0 + wrow;
@@ -214,9 +248,13 @@ namespace {
 int64_t rows_slots(const AttnArgs &a) { return span_slots(a.qoff != nullptr, a.n, a.Tq, kRows); }
 
 template <typename T, int DC>
+int64_t fwd_steps(const AttnArgs &a) {   // of a sequence
+    return (a.qoff ? a.Tk / std::max(a.n, 1) : a.Tk) / FwdShape<T, DC>::BN;
+}
+
+template <typename T, int DC>
 int fwd_splits(const AttnArgs &a) {
-    const int64_t keys = a.qoff ? a.Tk / std::max(a.n, 1) : a.Tk;   // of a sequence
-    return span_splits(rows_slots(a) * a.Hq, keys / FwdShape<T, DC>::BN, a.Tq * a.Hq * DC * 4);
+    return span_splits<T>(rows_slots(a) * a.Hq, fwd_steps<T, DC>(a), a.Tq * a.Hq * DC * 4);
 }
 
 template <typename T, int DC>
@@ -230,7 +268,13 @@ int fwd_run(const AttnArgs &a, void *ws, hipStream_t st) {
     const int64_t slots = rows_slots(a), rows = a.Tq * a.Hq;
     Parts part{fwd_splits<T, DC>(a), static_cast<float *>(ws), nullptr};
     part.stat = reinterpret_cast<floatx2 *>(part.sums + part.splits * rows * DC);
-    hipLaunchKernelGGL((fwd_kernel<T, DC>), dim3((unsigned)(slots * a.Hq), (unsigned)part.splits), dim3(256), 0, st, a, part);
+    const dim3 grid((unsigned)(slots * a.Hq), (unsigned)part.splits);
+    constexpr bool pairs = sizeof(T) == 2 && FwdShape<T, DC>::OCC == 2;
+    if (pairs && wide_blocks((int64_t)grid.x * grid.y, fwd_steps<T, DC>(a) / part.splits, 24)) {
+        if constexpr (pairs) hipLaunchKernelGGL((fwd_kernel<T, DC, 2>), grid, dim3(512), 0, st, a, part);
+    } else {
+        hipLaunchKernelGGL((fwd_kernel<T, DC, 1>), grid, dim3(256), 0, st, a, part);
+    }
     if (part.splits > 1) {
         const int64_t n = rows * (a.D / Vec16<T>::N);
         hipLaunchKernelGGL((join_kernel<T, DC>), dim3((unsigned)((n + 255) / 256)), dim3(256), 0, st, a, part);

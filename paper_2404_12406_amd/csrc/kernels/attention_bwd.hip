@@ -53,6 +53,34 @@ __global__ __launch_bounds__(256) void delta_kernel(AttnArgs a, float *__restric
     if (lane < rows) delta[head * a.Tq + first + lane] = v;
 }
 
+// The sums of a block's second group of four waves (side 1) to the wave of the first that has the
+// same rows, through the latter's part of LDS; nobody reads LDS before or after.
+template <int N, typename F>
+__device__ __forceinline__ void add_side(char *lds, int side, int lane, F acc) {
+    floatx4 *sums = reinterpret_cast<floatx4 *>(lds) + lane;
+    if (side) {
+#pragma unroll
+        for (int t = 0; t < N; ++t)
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+                const floatx16 &s = acc(t);
+                sums[64 * (4 * t + g)] = floatx4{s[4 * g], s[4 * g + 1], s[4 * g + 2], s[4 * g + 3]};
+            }
+    }
+    tile_sync();
+    if (!side) {
+#pragma unroll
+        for (int t = 0; t < N; ++t)
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+                const floatx4 v = sums[64 * (4 * t + g)];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) acc(t)[4 * g + j] += v[j];
+            }
+    }
+    tile_sync();
+}
+
 // ------------------------------------------------------------------ dq
 constexpr int kRows = 128;   // queries of a block of dq, keys of a block of dk and dv
 
@@ -75,15 +103,17 @@ struct DqShape {
     static constexpr int OCC = DC * (int)sizeof(T) <= 256 ? 2 : 1;
 };
 
-template <typename T, int DC>
-__global__ __launch_bounds__(256, (DqShape<T, DC>::OCC)) void dq_kernel(AttnArgs a, Parts part) {
+// WG: groups of four waves.  Two take every other step each, from stages of their own, and add
+// their sums at the end: a block that fills a CU alone.
+template <typename T, int DC, int WG>
+__global__ __launch_bounds__(256 * WG, (DqShape<T, DC>::OCC / WG)) void dq_kernel(AttnArgs a, Parts part) {
     constexpr int DP = kPitch<DC>;
     typedef Mat<T> M;
     typedef Tile<T, DP> Ti;
     typedef typename M::Frag Frag;
     constexpr int BN = DqShape<T, DC>::BN, NP = 32 / M::KC, BYTES = BN * Ti::RB;
-    __shared__ __align__(256) char lds[4 * BYTES];
-    const int lane = threadIdx.x & 63, w = uniform(threadIdx.x >> 6);
+    __shared__ __align__(256) char lds[4 * BYTES * WG];
+    const int lane = threadIdx.x & 63, w = uniform(threadIdx.x >> 6) & 3, side = WG > 1 ? uniform(threadIdx.x >> 8) : 0;
     int head, rank;
     find_head((int)blockIdx.x, a.Hq, head, rank);
     const int hk = head / (a.Hq / a.Hk);
@@ -105,12 +135,13 @@ __global__ __launch_bounds__(256, (DqShape<T, DC>::OCC)) void dq_kernel(AttnArgs
     Loader<T, DP, BN, 4> lk, lv;
     lk.init(a.k.ts, a.D, w, lane);
     lv.init(a.v.ts, a.D, w, lane);
+    char *stages = lds + side * 4 * BYTES;
     auto issue = [&](int k) {
-        char *to = lds + (k / BN & 1) * 2 * BYTES;
+        char *to = stages + (k / (BN * WG) & 1) * 2 * BYTES;
         lk.issue(kp + k * lk.ts, s.nb - k, a.D, to, w);
         lv.issue(vp + k * lv.ts, s.nb - k, a.D, to + BYTES, w);
     };
-    if (begin < end) issue(begin);
+    if (begin + side * BN < end) issue(begin + side * BN);
     Rows<T, DC, kHold1<T, DC>> q;
     Rows<T, DC, kHold<T, DC>> g;
     q.init(static_cast<const T *>(a.q.p) + first * a.q.ts + head * a.q.hs, a.q.ts, rows, a.D, lane);
@@ -120,7 +151,7 @@ __global__ __launch_bounds__(256, (DqShape<T, DC>::OCC)) void dq_kernel(AttnArgs
     if ((lane & 31) < rows) {
         const int64_t at = (int64_t)head * a.Tq + first + (lane & 31);
         lse = a.lse[at];
-        if (part.delta && blockIdx.y == 0 && lane < 32) part.delta[at] = delta;
+        if (part.delta && blockIdx.y == 0 && side == 0 && lane < 32) part.delta[at] = delta;
     }
     const float c = a.scale * kLog2e;
     floatx16 acc[DC / 32];
@@ -129,8 +160,9 @@ __global__ __launch_bounds__(256, (DqShape<T, DC>::OCC)) void dq_kernel(AttnArgs
     auto step = [&](int k, auto mode) __attribute__((always_inline)) {
         constexpr bool MASKED = decltype(mode)::value;
         tile_sync();
-        if (k + BN < end) issue(k + BN);
-        const char *kt = lds + (k / BN & 1) * 2 * BYTES, *vt = kt + BYTES;
+        if (k + BN * WG < end) issue(k + BN * WG);
+        if (WG > 1 && k >= end) return;
+        const char *kt = stages + (k / (BN * WG) & 1) * 2 * BYTES, *vt = kt + BYTES;
 #pragma unroll
         for (int n = 0; n < BN; n += 32) {
             if (MASKED && k + n >= wend) continue;
@@ -156,9 +188,14 @@ __global__ __launch_bounds__(256, (DqShape<T, DC>::OCC)) void dq_kernel(AttnArgs
     };
     // Keys that all of the block's rows see, in whole steps; then the others.
     const int clear = max(begin, min(end, max(0, a.causal ? min(s.nb, row0 + 1 + shift) : s.nb) / BN * BN));
-    for (int k = begin; k < clear; k += BN) step(k, Full{});
-    for (int k = clear; k < end; k += BN) step(k, Masked{});
+    int k = begin;
+    for (; k + (WG - 1) * BN < clear; k += BN * WG) step(k + side * BN, Full{});
+    for (; k < end; k += BN * WG) step(k + side * BN, Masked{});
     tile_sync();
+    if constexpr (WG > 1) {   // the second group's sums to the first
+        add_side<DC / 32>(lds + w * DC * 128, side, lane, [&](int t) -> floatx16 & { return acc[t]; });
+        if (side) return;
+    }
     if (rows <= 0) return;
     if (part.splits > 1) {
         store_sums<DC>(acc, part.a + ((blockIdx.y * a.Tq + first) * a.Hq + head) * DC, (int64_t)a.Hq * DC, rows, lane);
@@ -177,16 +214,17 @@ struct DkvShape {
     static constexpr int OCC = kPitch<DC> * (int)sizeof(T) <= 256 && KEPT <= (sizeof(T) == 2 ? 128 : 96) ? 2 : 1;
 };
 
-template <typename T, int DC, bool DK, bool DV>
-__global__ __launch_bounds__(256, (DkvShape<T, DC, DK, DV>::OCC)) void dkv_kernel(AttnArgs a, Parts part) {
+// WG as dq_kernel's.
+template <typename T, int DC, bool DK, bool DV, int WG>
+__global__ __launch_bounds__(256 * WG, (DkvShape<T, DC, DK, DV>::OCC / WG)) void dkv_kernel(AttnArgs a, Parts part) {
     constexpr int DP = kPitch<DC>;
     typedef Mat<T> M;
     typedef Tile<T, DP> Ti;
     typedef typename M::Frag Frag;
     constexpr int BM = DkvShape<T, DC, DK, DV>::BM, NP = 32 / M::KC, BYTES = BM * Ti::RB, C = DC / M::KC;
     constexpr int STAGE = 2 * BYTES + 512;   // q, g, and 64 each of lse and delta
-    __shared__ __align__(256) char lds[2 * STAGE];
-    const int lane = threadIdx.x & 63, w = uniform(threadIdx.x >> 6);
+    __shared__ __align__(256) char lds[2 * STAGE * WG];
+    const int lane = threadIdx.x & 63, w = uniform(threadIdx.x >> 6) & 3, side = WG > 1 ? uniform(threadIdx.x >> 8) : 0;
     int hk, rank;
     find_head((int)blockIdx.x, a.Hk, hk, rank);
     const int group = a.Hq / a.Hk;
@@ -227,8 +265,9 @@ __global__ __launch_bounds__(256, (DkvShape<T, DC, DK, DV>::OCC)) void dkv_kerne
         }
         return p;
     };
-    auto issue = [&](int n, const Place &p) {
-        char *to = lds + (n & 1) * STAGE;
+    char *stages = lds + side * 2 * STAGE;
+    auto issue = [&](int i, const Place &p) {
+        char *to = stages + (i & 1) * STAGE;
         const int head = hk * group + p.h, at = p.at;
         const int64_t row = s.b0 + at;
         lq.issue(reinterpret_cast<const char *>(static_cast<const T *>(a.q.p) + row * a.q.ts + head * a.q.hs), s.nb - at, a.D, to, w);
@@ -239,9 +278,9 @@ __global__ __launch_bounds__(256, (DkvShape<T, DC, DK, DV>::OCC)) void dkv_kerne
     const int first_step = (int)((int64_t)steps * group * blockIdx.y / part.splits);
     const int total = (int)((int64_t)steps * group * (blockIdx.y + 1) / part.splits);
     Place now{0, 0}, next{0, 0};
-    if (first_step < total) {
-        next = place_of(first_step);
-        issue(first_step, next);
+    if (first_step + side < total) {
+        next = place_of(first_step + side);
+        issue(0, next);
     }
     Rows<T, DC, kHold1<T, DC>> kf;
     Rows<T, DC, DK && kHold<T, DC>> vf;
@@ -251,17 +290,21 @@ __global__ __launch_bounds__(256, (DkvShape<T, DC, DK, DV>::OCC)) void dkv_kerne
     floatx16 dk[DC / 32], dv[DC / 32];
 #pragma unroll
     for (int t = 0; t < DC / 32; ++t) dk[t] = dv[t] = zero16x();
-    auto step = [&](int n, auto mode) __attribute__((always_inline)) {
+    // (the i-th of this group of waves, the block's n-th)
+    auto step = [&](int i, int n, auto mode) __attribute__((always_inline)) {
         constexpr bool MASKED = decltype(mode)::value;
         tile_sync();
         now = next;
-        next = after(now);
-        if (n + 1 < total) issue(n + 1, next);
+#pragma unroll
+        for (int k = 0; k < WG; ++k) next = after(next);
+        if (n + WG < total) issue(i + 1, next);
+        if (WG > 1 && n >= total) return;
         const int at = now.at;
-        const char *qt = lds + (n & 1) * STAGE, *gt = qt + BYTES;
+        const char *qt = stages + (i & 1) * STAGE, *gt = qt + BYTES;
         const float *lt = reinterpret_cast<const float *>(gt + BYTES), *dt = lt + 64;
 #pragma unroll
         for (int m = 0; m < BM; m += 32) {
+            if (DK && DV) __builtin_amdgcn_sched_barrier(0);   // (both tiles at once do not fit the registers)
             // (rows past the last query are zeros; a wave without keys has nothing to do)
             if (MASKED && (keys <= 0 || min(at + m + 32, s.nb) - 1 + shift < wkey)) continue;
             const bool masked = MASKED && at + m + shift < wkey + 31;
@@ -311,9 +354,15 @@ __global__ __launch_bounds__(256, (DkvShape<T, DC, DK, DV>::OCC)) void dkv_kerne
         }
     };
     const int hidden_to = max(first_step, min(total, edge * group));
-    for (int n = first_step; n < hidden_to; ++n) step(n, Masked{});
-    for (int n = hidden_to; n < total; ++n) step(n, Full{});
+    int i = 0, n = first_step;
+    for (; n < hidden_to; n += WG, ++i) step(i, n + side, Masked{});
+    for (; n < total; n += WG, ++i) step(i, n + side, Full{});
     tile_sync();
+    if constexpr (WG > 1) {   // the second group's sums to the first
+        if constexpr (DK) add_side<DC / 32>(lds + w * DC * 128, side, lane, [&](int t) -> floatx16 & { return dk[t]; });
+        if constexpr (DV) add_side<DC / 32>(lds + w * DC * 128, side, lane, [&](int t) -> floatx16 & { return dv[t]; });
+        if (side) return;
+    }
     if (keys <= 0) return;
     if (part.splits > 1) {
         const int64_t at = ((blockIdx.y * a.Tk + first) * a.Hk + hk) * DC;
@@ -363,9 +412,10 @@ namespace {
 
 size_t al256(size_t n) { return (n + 255) / 256 * 256; }
 
-// What a backward lays out: delta, then partial sums of dq, dk and dv.
+// What a backward lays out: delta, then partial sums of dq, dk and dv; the steps of their blocks.
 struct Plan {
     int dq_splits, dkv_splits;
+    int64_t dq_steps, dkv_steps;
     size_t dq_at, dk_at, dv_at, bytes;
 };
 
@@ -373,11 +423,11 @@ template <typename T, int DC>
 Plan plan(const AttnArgs &a, bool dq, bool dk, bool dv) {
     const bool packed = a.qoff != nullptr;
     const int64_t n = packed ? std::max(a.n, 1) : 1, group = a.Hq / a.Hk;
-    Plan p{1, 1, 0, 0, 0, 0};
-    if (dq) p.dq_splits = span_splits(span_slots(packed, a.n, a.Tq, kRows) * a.Hq, a.Tk / n / DqShape<T, DC>::BN, a.Tq * a.Hq * DC * 4);
-    if (dk || dv)
-        p.dkv_splits = span_splits(span_slots(packed, a.n, a.Tk, kRows) * a.Hk, a.Tq / n * group / DkvShape<T, DC, true, true>::BM,
-                                   a.Tk * a.Hk * DC * 8);
+    Plan p{1, 1, a.Tk / n / DqShape<T, DC>::BN, a.Tq / n * group / DkvShape<T, DC, true, true>::BM, 0, 0, 0, 0};
+    if (dq) p.dq_splits = span_splits<T>(span_slots(packed, a.n, a.Tq, kRows) * a.Hq, p.dq_steps, a.Tq * a.Hq * DC * 4);
+    if (dk || dv) p.dkv_splits = span_splits<T>(span_slots(packed, a.n, a.Tk, kRows) * a.Hk, p.dkv_steps, a.Tk * a.Hk * DC * 8);
+    p.dq_steps /= p.dq_splits;
+    p.dkv_steps /= p.dkv_splits;
     const size_t keys = p.dkv_splits > 1 ? al256((size_t)p.dkv_splits * a.Tk * a.Hk * DC * sizeof(float)) : 0;
     p.dq_at = dk ? al256((size_t)a.Tq * a.Hq * sizeof(float)) : 0;
     p.dk_at = p.dq_at + (p.dq_splits > 1 ? al256((size_t)p.dq_splits * a.Tq * a.Hq * DC * sizeof(float)) : 0);
@@ -389,6 +439,17 @@ Plan plan(const AttnArgs &a, bool dq, bool dk, bool dv) {
 template <typename T, int DC>
 size_t space(const AttnArgs &a, bool dq, bool dk, bool dv) {
     return plan<T, DC>(a, dq, dk, dv).bytes;
+}
+
+template <typename T, int DC, bool DK, bool DV>
+void dkv_run(dim3 grid, bool few, const AttnArgs &a, const Parts &part, hipStream_t st) {
+    if constexpr (sizeof(T) == 2 && DkvShape<T, DC, DK, DV>::OCC == 2) {
+        if (few) {
+            hipLaunchKernelGGL((dkv_kernel<T, DC, DK, DV, 2>), grid, dim3(512), 0, st, a, part);
+            return;
+        }
+    }
+    hipLaunchKernelGGL((dkv_kernel<T, DC, DK, DV, 1>), grid, dim3(256), 0, st, a, part);
 }
 
 template <typename T, int DC>
@@ -403,7 +464,13 @@ int run(const AttnArgs &a, char *ws, hipStream_t st) {
     if (dq && a.Tq > 0) {
         const int64_t slots = span_slots(packed, a.n, a.Tq, kRows);
         const Parts part{dk ? delta : nullptr, p.dq_splits, reinterpret_cast<float *>(ws + p.dq_at), nullptr};
-        hipLaunchKernelGGL((dq_kernel<T, DC>), dim3((unsigned)(slots * a.Hq), (unsigned)part.splits), dim3(256), 0, st, a, part);
+        const dim3 grid((unsigned)(slots * a.Hq), (unsigned)part.splits);
+        constexpr bool pairs = sizeof(T) == 2 && DqShape<T, DC>::OCC == 2;
+        if (pairs && wide_blocks((int64_t)grid.x * grid.y, p.dq_steps, 24)) {
+            if constexpr (pairs) hipLaunchKernelGGL((dq_kernel<T, DC, 2>), grid, dim3(512), 0, st, a, part);
+        } else {
+            hipLaunchKernelGGL((dq_kernel<T, DC, 1>), grid, dim3(256), 0, st, a, part);
+        }
         if (part.splits > 1) {
             const Sum s{a.dq, part.a, a.scale};
             hipLaunchKernelGGL(sum_kernel<T>, dim3((unsigned)((a.Tq * a.Hq * (a.D / V) + 255) / 256)), dim3(256), 0, st, s, s, a.Tq, a.Hq,
@@ -417,11 +484,17 @@ int run(const AttnArgs &a, char *ws, hipStream_t st) {
         // Both at once up to where both sums and their operands are in a wave's registers: four products
         // instead of five (1777 x 2 heads of 72 in fp32: 74 us against 57 and 49).
         constexpr bool both = DC <= (sizeof(T) == 2 ? 128 : 96);
-        if (both && dk && dv) {
-            if constexpr (both) hipLaunchKernelGGL((dkv_kernel<T, DC, true, true>), grid, dim3(256), 0, st, a, part);
+        // Blocks of two groups (attn_tile.h): dk and dv each for itself where a CU does not hold both sums of eight waves,
+        // the same for all masks, so that a gradient's bits do not depend on which others are asked for.  (7 sequences
+        // of 8192 rows, 32 on 8 heads, bf16: dv alone of 128 columns 206 -> 173 us, dk alone 362 -> 274, both 424 -> 431; of
+        // 64 columns 141 -> 114 and 238 -> 197.  4 x 2048 rows, 8 heads of 128, 32 steps: 57 -> 54, both 117 -> 136.  In fp32 two
+        // kernels instead of one cost more, 8 on 2 heads of 64 483 -> 591.)
+        const bool few = sizeof(T) == 2 && DkvShape<T, DC, true, false>::OCC == 2 && wide_blocks((int64_t)grid.x * grid.y, p.dkv_steps, 40);
+        if (both && dk && dv && !(few && DkvShape<T, DC, true, true>::OCC == 1)) {
+            if constexpr (both) dkv_run<T, DC, true, true>(grid, few, a, part, st);
         } else {
-            if (dk) hipLaunchKernelGGL((dkv_kernel<T, DC, true, false>), grid, dim3(256), 0, st, a, part);
-            if (dv) hipLaunchKernelGGL((dkv_kernel<T, DC, false, true>), grid, dim3(256), 0, st, a, part);
+            if (dk) dkv_run<T, DC, true, false>(grid, few, a, part, st);
+            if (dv) dkv_run<T, DC, false, true>(grid, few, a, part, st);
         }
         if (part.splits > 1) {
             const Sum k{a.dk, part.a, a.scale}, v{a.dv, part.b, 1.f};

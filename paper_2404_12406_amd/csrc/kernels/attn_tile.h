@@ -176,7 +176,6 @@ __device__ __forceinline__ int wave_add(int v) {
 // begin first and none of them is left over at the end.  A causal sequence's tiles have work in steps of one tile's
 // rows (from its last one on with last_first, else from its first), others all their keys.
 // To 62 sequences, a lane each; beyond, as they come.  Past the last tile: one without rows.
-// (8192 rows in 7 sequences, 32 on 8 heads of 128, bf16: dv 338 -> 261 us.)
 __device__ __forceinline__ Span find_ranked(const int32_t *aoff, const int32_t *boff, int n, int Ta, int Tb, int rank, int rows, bool causal,
                                             bool last_first) {
     const int tiles = (Ta + rows - 1) / rows;
@@ -234,14 +233,23 @@ inline int64_t span_slots(bool packed, int n, int64_t Ta, int rows) {
     return packed ? Ta / rows + n + 2 : (Ta + rows - 1) / rows;
 }
 
-// Where there are few blocks they divide their other side: to some 1024 of them, as long as
-// two of the `steps` that they have on average are left to each and the partial sums stay
+// Where there are few blocks they divide their other side: to some 512 of them (1024 in fp32, whose steps take
+// longer), as long as two of the `steps` that they have on average are left to each and the partial sums stay
 // below 24 MiB.
-// (fp32, 1777 rows in 5 sequences, 6 on 2 heads of 72, all gradients: 906 -> 190 us; with 512 blocks 202.)
+// (fp32, 1777 rows in 5 sequences, 6 on 2 heads of 72, all gradients: 906 -> 190 us; with 512 blocks 202.  bf16, 4 x 1024
+// rows, 8 on 2 heads of 64, forward: 30 us with 1024 blocks, 17 with 304.)
+template <typename T>
 inline int span_splits(int64_t blocks, int64_t steps, int64_t bytes) {
-    const int64_t want = 1024 / std::max<int64_t>(blocks, 1), most = (int64_t(24) << 20) / std::max<int64_t>(bytes, 1);
+    const int64_t want = (sizeof(T) == 2 ? 512 : 1024) / std::max<int64_t>(blocks, 1), most = (int64_t(24) << 20) / std::max<int64_t>(bytes, 1);
     return (int)std::max<int64_t>(1, std::min({want, steps / 2, most}));
 }
+
+// Up to 768 blocks, of which a CU holds two, all run at once, and the longest end alone on a CU that they cannot
+// fill.  Where they have `least` steps or more on average, such blocks have eight waves, which take every
+// other step each and meet at the end.  (bf16, 8192 rows of one sequence, 8 heads of 128: forward 178 -> 144 us,
+// dq 251 -> 202, dv 186 -> 148.  With two to 16 steps the longer start costs more: 64 x 128 rows, 4 heads of 64 forward
+// 10 -> 13 us, 8 x 1024 rows 22 -> 24.  With 1152 blocks dv 312 -> 356.)
+inline bool wide_blocks(int64_t blocks, int64_t steps, int64_t least) { return blocks <= 768 && steps >= least; }
 
 // The sum (maximum) of a lane's value and that of the lane 32 away.
 __device__ __forceinline__ floatx2 halves(float v) {

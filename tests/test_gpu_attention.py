@@ -184,6 +184,34 @@ def test_long(D, causal, dtype):
     case([2500, 1100], [2500, 1100], 2, 1, D, dtype, causal, seed=3)
 
 
+@CAUSAL
+@pytest.mark.parametrize("D", [40, 64, 96, 120, 128])
+@pytest.mark.parametrize("q_lens,k_lens", [([2903], [2903]), ([1601], [3333]), ([2903, 1, 0, 1700], [2903, 70, 33, 1600])])
+def test_long_walks_of_few_blocks(q_lens, k_lens, D, causal):
+    """Blocks whose waves take every other step of the other side."""
+    case(q_lens, k_lens, 16, 8, D, "bf16", causal, seed=5)
+
+
+@pytest.mark.parametrize("D", [64, 128])
+def test_long_walks_by_mask(D):
+    q, k, v, g = (draw((2903, h, D), "bf16", i) for i, h in enumerate((16, 8, 8, 16)))
+    first = run(q, k, v, g, 7, ms.Attention())
+    for mask in range(1, 8):
+        for a, b in zip(run(q, k, v, g, mask, ms.Attention()), first):
+            assert a is None or torch.equal(a, b)
+    # keys that are not finite: the rows before them are as without, but for the order of sums in
+    # tiles that hold some (a row of the tile after the other), so as near to the reference
+    at = 1500
+    refs, bars = reference(q, k, v, g, [2903], [2903], True, D ** -0.5, "bf16")
+    for which in range(2):
+        k2, v2 = k.clone(), v.clone()
+        (k2, v2)[which][at:] = math.nan
+        outs = run(q, k2, v2, g, 7, ms.Attention())
+        for i in (0, 1):
+            close("od"[i], outs[i][:at], refs[i][:at], bars[i][:at])
+        assert torch.isnan(outs[0][at:].float()).all()
+
+
 @DTYPES
 def test_large_scores(dtype):
     """Rows near one-hot: the running maximum moves, probabilities underflow."""
