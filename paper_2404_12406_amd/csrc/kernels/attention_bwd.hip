@@ -113,7 +113,7 @@ __global__ __launch_bounds__(256 * WG, (DqShape<T, DC>::OCC / WG)) void dq_kerne
     typedef typename M::Frag Frag;
     constexpr int BN = DqShape<T, DC>::BN, NP = 32 / M::KC, BYTES = BN * Ti::RB;
     __shared__ __align__(256) char lds[4 * BYTES * WG];
-    const int lane = threadIdx.x & 63, w = uniform(threadIdx.x >> 6) & 3, side = WG > 1 ? uniform(threadIdx.x >> 8) : 0;
+    const int lane = threadIdx.x & 63, w = WG > 1 ? uniform(threadIdx.x >> 6) & 3 : uniform(threadIdx.x >> 6), side = WG > 1 ? uniform(threadIdx.x >> 8) : 0;
     int head, rank;
     find_head((int)blockIdx.x, a.Hq, head, rank);
     const int hk = head / (a.Hq / a.Hk);
@@ -157,33 +157,62 @@ __global__ __launch_bounds__(256 * WG, (DqShape<T, DC>::OCC / WG)) void dq_kerne
     floatx16 acc[DC / 32];
 #pragma unroll
     for (int t = 0; t < DC / 32; ++t) acc[t] = zero16x();
-    auto step = [&](int k, auto mode) __attribute__((always_inline)) {
+    // 32 keys, from row n of the stage on.
+    auto tile = [&](const char *kt, const char *vt, int k, int n, auto mode) __attribute__((always_inline)) {
         constexpr bool MASKED = decltype(mode)::value;
+        const bool masked = MASKED && k + n + 32 > wfull;
+        floatx16 x = zero16x(), y = zero16x();
+#pragma unroll
+        for (int i = 0; i < DC / M::KC; ++i) {
+            x = M::mma(Ti::row_frag(kt, n, i, lane), q.get(i, lane), x);
+            y = M::mma(Ti::row_frag(vt, n, i, lane), g.get(i, lane), y);
+        }
+#pragma unroll
+        for (int i = 0; i < 16; ++i) x[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[i], c, -lse)) * (y[i] - delta);
+        if (masked) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) x[i] = k + n + 8 * (i >> 2) + 4 * (lane >> 5) + (i & 3) > last ? 0.f : x[i];
+        }
+        // An operand, in bf16 as the rounded value and what that leaves off: with the first alone dq would have two
+        // roundings next to delta's error, which is o's (7 packed sequences: off by 2.6e-3 in all, with both 1.9e-3; one
+        // rounding alone is 1.7e-3).
+        if (masked && any_wild<T, DP, 32>(kt, n, lane)) {
+            Frag d[NP];
+#pragma unroll
+            for (int i = 0; i < NP; ++i) d[i] = as_frag<T>(x, i);
+            wild_product<T, DP, DC, NP>(acc, kt, n, d, lane);
+            return;
+        }
+#pragma unroll
+        for (int i = 0; i < NP; ++i) {
+            const Frag d = as_frag<T>(x, i);
+            Frag r;
+            if constexpr (sizeof(T) == 2)
+#pragma unroll
+                for (int j = 0; j < M::V; ++j) r[j] = from_f32<T>(x[i * M::V + j] - to_f32(d[j]));
+#pragma unroll
+            for (int t = 0; t < DC / 32; ++t) {
+                const Frag f = Ti::col_frag(kt, n, t, i, lane);
+                acc[t] = M::mma(f, d, acc[t]);
+                if constexpr (sizeof(T) == 2) acc[t] = M::mma(f, r, acc[t]);
+            }
+        }
+    };
+    auto step = [&](int k, auto mode) __attribute__((always_inline)) {
         tile_sync();
         if (k + BN * WG < end) issue(k + BN * WG);
         if (WG > 1 && k >= end) return;
         const char *kt = stages + (k / (BN * WG) & 1) * 2 * BYTES, *vt = kt + BYTES;
-#pragma unroll
-        for (int n = 0; n < BN; n += 32) {
-            if (MASKED && k + n >= wend) continue;
-            const bool masked = MASKED && k + n + 32 > wfull;
-            floatx16 x = zero16x(), y = zero16x();
-#pragma unroll
-            for (int i = 0; i < DC / M::KC; ++i) {
-                x = M::mma(Ti::row_frag(kt, n, i, lane), q.get(i, lane), x);
-                y = M::mma(Ti::row_frag(vt, n, i, lane), g.get(i, lane), y);
+        if constexpr (decltype(mode)::value) {   // (in turn: unrolled, what the rare path holds would not fit the registers)
+#pragma unroll 1
+            for (int n = 0; n < BN && k + n < wend; n += 32) {
+                int row = n;
+                asm volatile("" : "+s"(row));   // (nothing of it is worked out before the loop and held)
+                tile(kt, vt, k, row, mode);
             }
+        } else {
 #pragma unroll
-            for (int i = 0; i < 16; ++i) x[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[i], c, -lse)) * (y[i] - delta);
-            if (masked) {
-#pragma unroll
-                for (int i = 0; i < 16; ++i) x[i] = k + n + 8 * (i >> 2) + 4 * (lane >> 5) + (i & 3) > last ? 0.f : x[i];
-            }
-            Frag d[NP];   // (an operand: in bf16 rounded)
-#pragma unroll
-            for (int i = 0; i < NP; ++i) d[i] = as_frag<T>(x, i);
-            if (masked && any_wild<T, DP, 32>(kt, n, lane)) wild_product<T, DP, DC, NP>(acc, kt, n, d, lane);
-            else add_product<T, DP, DC, NP>(acc, kt, n, d, lane);
+            for (int n = 0; n < BN; n += 32) tile(kt, vt, k, n, mode);
         }
     };
     // Keys that all of the block's rows see, in whole steps; then the others.
@@ -224,7 +253,7 @@ __global__ __launch_bounds__(256 * WG, (DkvShape<T, DC, DK, DV>::OCC / WG)) void
     constexpr int BM = DkvShape<T, DC, DK, DV>::BM, NP = 32 / M::KC, BYTES = BM * Ti::RB, C = DC / M::KC;
     constexpr int STAGE = 2 * BYTES + 512;   // q, g, and 64 each of lse and delta
     __shared__ __align__(256) char lds[2 * STAGE * WG];
-    const int lane = threadIdx.x & 63, w = uniform(threadIdx.x >> 6) & 3, side = WG > 1 ? uniform(threadIdx.x >> 8) : 0;
+    const int lane = threadIdx.x & 63, w = WG > 1 ? uniform(threadIdx.x >> 6) & 3 : uniform(threadIdx.x >> 6), side = WG > 1 ? uniform(threadIdx.x >> 8) : 0;
     int hk, rank;
     find_head((int)blockIdx.x, a.Hk, hk, rank);
     const int group = a.Hq / a.Hk;
@@ -266,8 +295,8 @@ __global__ __launch_bounds__(256 * WG, (DkvShape<T, DC, DK, DV>::OCC / WG)) void
         return p;
     };
     char *stages = lds + side * 2 * STAGE;
-    auto issue = [&](int i, const Place &p) {
-        char *to = stages + (i & 1) * STAGE;
+    auto issue = [&](int n, const Place &p) {
+        char *to = stages + (n / WG & 1) * STAGE;
         const int head = hk * group + p.h, at = p.at;
         const int64_t row = s.b0 + at;
         lq.issue(reinterpret_cast<const char *>(static_cast<const T *>(a.q.p) + row * a.q.ts + head * a.q.hs), s.nb - at, a.D, to, w);
@@ -280,7 +309,7 @@ __global__ __launch_bounds__(256 * WG, (DkvShape<T, DC, DK, DV>::OCC / WG)) void
     Place now{0, 0}, next{0, 0};
     if (first_step + side < total) {
         next = place_of(first_step + side);
-        issue(0, next);
+        issue(first_step + side, next);
     }
     Rows<T, DC, kHold1<T, DC>> kf;
     Rows<T, DC, DK && kHold<T, DC>> vf;
@@ -290,21 +319,20 @@ __global__ __launch_bounds__(256 * WG, (DkvShape<T, DC, DK, DV>::OCC / WG)) void
     floatx16 dk[DC / 32], dv[DC / 32];
 #pragma unroll
     for (int t = 0; t < DC / 32; ++t) dk[t] = dv[t] = zero16x();
-    // (the i-th of this group of waves, the block's n-th)
-    auto step = [&](int i, int n, auto mode) __attribute__((always_inline)) {
+    auto step = [&](int n, auto mode) __attribute__((always_inline)) {
         constexpr bool MASKED = decltype(mode)::value;
         tile_sync();
         now = next;
 #pragma unroll
         for (int k = 0; k < WG; ++k) next = after(next);
-        if (n + WG < total) issue(i + 1, next);
+        if (n + WG < total) issue(n + WG, next);
         if (WG > 1 && n >= total) return;
         const int at = now.at;
-        const char *qt = stages + (i & 1) * STAGE, *gt = qt + BYTES;
+        const char *qt = stages + (n / WG & 1) * STAGE, *gt = qt + BYTES;
         const float *lt = reinterpret_cast<const float *>(gt + BYTES), *dt = lt + 64;
 #pragma unroll
         for (int m = 0; m < BM; m += 32) {
-            if (DK && DV) __builtin_amdgcn_sched_barrier(0);   // (both tiles at once do not fit the registers)
+            if (DK && DV && WG > 1) __builtin_amdgcn_sched_barrier(0);   // (both tiles at once do not fit the registers)
             // (rows past the last query are zeros; a wave without keys has nothing to do)
             if (MASKED && (keys <= 0 || min(at + m + 32, s.nb) - 1 + shift < wkey)) continue;
             const bool masked = MASKED && at + m + shift < wkey + 31;
@@ -354,9 +382,9 @@ __global__ __launch_bounds__(256 * WG, (DkvShape<T, DC, DK, DV>::OCC / WG)) void
         }
     };
     const int hidden_to = max(first_step, min(total, edge * group));
-    int i = 0, n = first_step;
-    for (; n < hidden_to; n += WG, ++i) step(i, n + side, Masked{});
-    for (; n < total; n += WG, ++i) step(i, n + side, Full{});
+    int n = first_step;
+    for (; n < hidden_to; n += WG) step(n + side, Masked{});
+    for (; n < total; n += WG) step(n + side, Full{});
     tile_sync();
     if constexpr (WG > 1) {   // the second group's sums to the first
         if constexpr (DK) add_side<DC / 32>(lds + w * DC * 128, side, lane, [&](int t) -> floatx16 & { return dk[t]; });
