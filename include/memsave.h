@@ -54,7 +54,8 @@
  *  - Calls on different streams that overlap on one device are safe: each
  *    stream gets its own transient workspace.  Calls from several threads on
  *    one stream are too: a call that uses the workspace enqueues all of its
- *    kernels before another takes it.
+ *    kernels before another takes it.  A captured call keeps its stream's workspace:
+ *    graphs captured on one stream are replayed one after the other.
  */
 #ifndef MEMSAVE_H
 #define MEMSAVE_H
@@ -435,7 +436,7 @@ typedef struct {
  * scales; no statistics.  Mask bits: INPUT x, WEIGHT gamma_q, BIAS gamma_k.
  * x, y: [T, H, D], 1 <= D <= 256 (MS_E_UNSUPPORTED otherwise), any strides (y not
  * overlapping itself); y may be x itself where the record does not borrow it (MS_E_ARG
- * otherwise).
+ * otherwise), in the same layout.
  * gamma_q, gamma_k: [D] contiguous or NULL (ones).  Statistics, angles and sums are in 32
  * bits or more.  Backward is ms_layer_backward().  ms_layer_forward() rejects
  * MS_HEAD_NORM_ROTARY (MS_E_ARG).
@@ -470,10 +471,11 @@ uint64_t ms_attention_kept_bytes(int64_t rows, int64_t heads, uint32_t mask);
  * k's gradient, v and o; the offsets too.  Backward takes P again and computes what its gradients
  * need: dv alone two products, dq or dk three each, of which the first two are shared by dk and dv.
  * With mask 0 kept may be NULL.  q, o: [Tq, Hq, D], k, v: [Tk, Hk, D], 1 <= D <= 256
- * (MS_E_UNSUPPORTED otherwise), any strides (o not overlapping itself); rows that are no whole
- * aligned 16-byte vectors are staged.  scale: finite, > 0 (MS_E_ARG otherwise).  Sums and statistics are in fp32;
- * in bf16 P and dS are rounded to bf16 as operands of their products.  Backward is
- * ms_layer_backward(); ms_layer_forward() rejects MS_ATTENTION (MS_E_ARG).
+ * (MS_E_UNSUPPORTED otherwise), any strides (o not overlapping itself, and not q, k or v: MS_E_ARG);
+ * rows that are no whole aligned 16-byte vectors are staged.  scale: finite, > 0 (MS_E_ARG otherwise).
+ * Sums and statistics are in fp32; in bf16 P and dS are rounded to bf16 as operands of their products, but for
+ * dq's, which keeps what the rounding leaves off as a second operand.  A gradient's bits do not depend on which
+ * others are asked for.  Backward is ms_layer_backward(); ms_layer_forward() rejects MS_ATTENTION (MS_E_ARG).
  */
 ms_status ms_attention_forward(const ms_tensor *q, const ms_tensor *k, const ms_tensor *v, const int32_t *q_offsets,
                                const int32_t *k_offsets, int64_t sequences, int32_t causal, float scale, void *kept,
@@ -491,7 +493,7 @@ ms_status ms_attention_forward(const ms_tensor *q, const ms_tensor *k, const ms_
  * tables[sequence][p / page], p the position.  tables: [sequences, width] on the
  * device.  A token whose position, sequence or page lies outside is not written to the cache
  * (a negative position marks padding); its query is.  Two tokens of one place: each
- * 16 bytes of it are one of the two's.  There is no record: the cache is no function of x alone.
+ * element of it is one of the two's.  q may be x's own first heads.  There is no record: the cache is no function of x alone.
  */
 ms_status ms_cache_append(const ms_tensor *x, const ms_tensor *gamma_q, const ms_tensor *gamma_k, const ms_rotary *rotary,
                           const ms_tensor *k_pages, const ms_tensor *v_pages, const int32_t *tables, int64_t sequences,
@@ -505,7 +507,8 @@ ms_status ms_cache_append(const ms_tensor *x, const ms_tensor *gamma_q, const ms
  * less gives zeros; one past width * page, or a used page outside the cache, NaN.  What lies in
  * the cache past the length takes no part.  A sequence's keys are divided over blocks and their
  * sums joined in a fixed order, in transient workspace.  Sums and statistics are in fp32; in
- * bf16 probabilities are rounded to bf16 as an operand.
+ * bf16 probabilities are rounded to bf16 as an operand.  o may be q.  width * page: less than
+ * 2^31 - 2^12 (MS_E_UNSUPPORTED).
  */
 ms_status ms_paged_attention_forward(const ms_tensor *q, const ms_tensor *k_pages, const ms_tensor *v_pages,
                                      const int32_t *tables, int64_t sequences, int64_t width, const int32_t *lengths,

@@ -10,7 +10,10 @@
 // Both at once would take S and dP once instead of twice, five products instead of seven,
 // but one of the sums would then go through memory.  dv alone needs neither v nor o.
 //
-// Bound: matrix cores, 3 products in dq, 2 in dv alone, 3 in dk alone, 4 in both.
+// Bound: matrix cores, 3 products in dq (in bf16 the third twice, see there), 2 in dv alone, 3 in dk alone, 4 in both,
+// and the vector units: 8 operations and an exponential an element of P beside them.  bf16, 8192 rows in 7 sequences,
+// 32 on 8 heads of 128: dq 300 us, 530 TFLOP/s by three products, dv alone 170 to 195, 540 to 620; 16 x 512 rows, 12 heads of
+// 64: dq 39 us, dk and dv 41.  fp32, 1777 rows, 6 on 2 heads of 72: dq 56 us, dk and dv 73, sums of the parts 6 each.
 #include <algorithm>
 
 #include "attn_tile.h"
@@ -176,25 +179,26 @@ __global__ __launch_bounds__(256 * WG, (DqShape<T, DC>::OCC / WG)) void dq_kerne
         // An operand, in bf16 as the rounded value and what that leaves off: with the first alone dq would have two
         // roundings next to delta's error, which is o's (7 packed sequences: off by 2.6e-3 in all, with both 1.9e-3; one
         // rounding alone is 1.7e-3).
-        if (masked && any_wild<T, DP, 32>(kt, n, lane)) {
+        const bool wild = masked && any_wild<T, DP, 32>(kt, n, lane);
+        if (sizeof(T) == 4 || wild) {
             Frag d[NP];
 #pragma unroll
             for (int i = 0; i < NP; ++i) d[i] = as_frag<T>(x, i);
-            wild_product<T, DP, DC, NP>(acc, kt, n, d, lane);
+            if (wild) wild_product<T, DP, DC, NP>(acc, kt, n, d, lane);
+            else add_product<T, DP, DC, NP>(acc, kt, n, d, lane);
             return;
         }
 #pragma unroll
         for (int i = 0; i < NP; ++i) {
             const Frag d = as_frag<T>(x, i);
             Frag r;
-            if constexpr (sizeof(T) == 2)
 #pragma unroll
-                for (int j = 0; j < M::V; ++j) r[j] = from_f32<T>(x[i * M::V + j] - to_f32(d[j]));
+            for (int j = 0; j < M::V; ++j) r[j] = from_f32<T>(x[i * M::V + j] - to_f32(d[j]));
 #pragma unroll
             for (int t = 0; t < DC / 32; ++t) {
                 const Frag f = Ti::col_frag(kt, n, t, i, lane);
                 acc[t] = M::mma(f, d, acc[t]);
-                if constexpr (sizeof(T) == 2) acc[t] = M::mma(f, r, acc[t]);
+                acc[t] = M::mma(f, r, acc[t]);
             }
         }
     };
