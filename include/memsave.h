@@ -473,8 +473,8 @@ uint64_t ms_attention_kept_bytes(int64_t rows, int64_t heads, uint32_t mask);
  * With mask 0 kept may be NULL.  q, o: [Tq, Hq, D], k, v: [Tk, Hk, D], 1 <= D <= 256
  * (MS_E_UNSUPPORTED otherwise), any strides (o not overlapping itself, and not q, k or v: MS_E_ARG);
  * rows that are no whole aligned 16-byte vectors are staged.  scale: finite, > 0 (MS_E_ARG otherwise).
- * Sums and statistics are in fp32; in bf16 P and dS are rounded to bf16 as operands of their products, but for
- * dq's, which keeps what the rounding leaves off as a second operand.  A gradient's bits do not depend on which
+ * Sums and statistics are in fp32; in bf16 P is rounded to bf16 as an operand of its products, dS in two
+ * operands, the rounded value and what that leaves off.  A gradient's bits do not depend on which
  * others are asked for.  Backward is ms_layer_backward(); ms_layer_forward() rejects MS_ATTENTION (MS_E_ARG).
  */
 ms_status ms_attention_forward(const ms_tensor *q, const ms_tensor *k, const ms_tensor *v, const int32_t *q_offsets,

@@ -10,10 +10,10 @@
 // Both at once would take S and dP once instead of twice, five products instead of seven,
 // but one of the sums would then go through memory.  dv alone needs neither v nor o.
 //
-// Bound: matrix cores, 3 products in dq (in bf16 the third twice, see there), 2 in dv alone, 3 in dk alone, 4 in both,
+// Bound: matrix cores, 3 products in dq, 2 in dv alone, 3 in dk alone, 4 in both (in bf16 that with dS twice),
 // and the vector units: 8 operations and an exponential an element of P beside them.  bf16, 8192 rows in 7 sequences,
 // 32 on 8 heads of 128: dq 300 us, 530 TFLOP/s by three products, dv alone 170 to 195, 540 to 620; 16 x 512 rows, 12 heads of
-// 64: dq 39 us, dk and dv 41.  fp32, 1777 rows, 6 on 2 heads of 72: dq 56 us, dk and dv 73, sums of the parts 6 each.
+// 64: dq 39 us, dk and dv 46.  fp32, 1777 rows, 6 on 2 heads of 72: dq 56 us, dk and dv 73, sums of the parts 6 each.
 #include <algorithm>
 
 #include "attn_tile.h"
@@ -54,6 +54,28 @@ __global__ __launch_bounds__(256) void delta_kernel(AttnArgs a, float *__restric
     g.init(static_cast<const T *>(a.go.p) + first * a.go.ts + head * a.go.hs, a.go.ts, rows, a.D, lane);
     const float v = row_delta<T, DC, false>(a, head, first, rows, g, lane);
     if (lane < rows) delta[head * a.Tq + first + lane] = v;
+}
+
+// acc += columns of `tile` times b = dS, in bf16 as the rounded values and what that leaves off: rounded once, dq and
+// dk would have two roundings next to delta's error, which is o's (7 packed sequences: off by 2.6e-3 and 2.5e-3; now 1.9e-3
+// and 2.0e-3, one rounding alone being 1.7e-3).  (7 sequences, 8192 rows, 32 on 8 heads of 128: dq 250 -> 300 us, dk alone 263 ->
+// 310, all gradients 655 -> 702.)
+template <typename T, int DP, int DC>
+__device__ __forceinline__ void add_exactly(floatx16 (&acc)[DC / 32], const char *tile, int r0, const floatx16 &b, int lane) {
+    typedef Mat<T> M;
+#pragma unroll
+    for (int i = 0; i < 32 / M::KC; ++i) {
+        const typename M::Frag d = as_frag<T>(b, i);
+        typename M::Frag r;
+#pragma unroll
+        for (int j = 0; j < M::V; ++j) r[j] = from_f32<T>(b[i * M::V + j] - to_f32(d[j]));
+#pragma unroll
+        for (int t = 0; t < DC / 32; ++t) {
+            const typename M::Frag f = Tile<T, DP>::col_frag(tile, r0, t, i, lane);
+            acc[t] = M::mma(f, d, acc[t]);
+            acc[t] = M::mma(f, r, acc[t]);
+        }
+    }
 }
 
 // The sums of a block's second group of four waves (side 1) to the wave of the first that has the
@@ -176,9 +198,6 @@ __global__ __launch_bounds__(256 * WG, (DqShape<T, DC>::OCC / WG)) void dq_kerne
 #pragma unroll
             for (int i = 0; i < 16; ++i) x[i] = k + n + 8 * (i >> 2) + 4 * (lane >> 5) + (i & 3) > last ? 0.f : x[i];
         }
-        // An operand, in bf16 as the rounded value and what that leaves off: with the first alone dq would have two
-        // roundings next to delta's error, which is o's (7 packed sequences: off by 2.6e-3 in all, with both 1.9e-3; one
-        // rounding alone is 1.7e-3).
         const bool wild = masked && any_wild<T, DP, 32>(kt, n, lane);
         if (sizeof(T) == 4 || wild) {
             Frag d[NP];
@@ -188,19 +207,7 @@ __global__ __launch_bounds__(256 * WG, (DqShape<T, DC>::OCC / WG)) void dq_kerne
             else add_product<T, DP, DC, NP>(acc, kt, n, d, lane);
             return;
         }
-#pragma unroll
-        for (int i = 0; i < NP; ++i) {
-            const Frag d = as_frag<T>(x, i);
-            Frag r;
-#pragma unroll
-            for (int j = 0; j < M::V; ++j) r[j] = from_f32<T>(x[i * M::V + j] - to_f32(d[j]));
-#pragma unroll
-            for (int t = 0; t < DC / 32; ++t) {
-                const Frag f = Ti::col_frag(kt, n, t, i, lane);
-                acc[t] = M::mma(f, d, acc[t]);
-                acc[t] = M::mma(f, r, acc[t]);
-            }
-        }
+        add_exactly<T, DP, DC>(acc, kt, n, x, lane);
     };
     auto step = [&](int k, auto mode) __attribute__((always_inline)) {
         tile_sync();
@@ -323,8 +330,64 @@ __global__ __launch_bounds__(256 * WG, (DkvShape<T, DC, DK, DV>::OCC / WG)) void
     floatx16 dk[DC / 32], dv[DC / 32];
 #pragma unroll
     for (int t = 0; t < DC / 32; ++t) dk[t] = dv[t] = zero16x();
-    auto step = [&](int n, auto mode) __attribute__((always_inline)) {
+    // 32 queries, from row m of the stage on.
+    auto tile = [&](int at, const char *qt, const char *gt, int m, auto mode) __attribute__((always_inline)) {
         constexpr bool MASKED = decltype(mode)::value;
+        const float *lt = reinterpret_cast<const float *>(gt + BYTES), *dt = lt + 64;
+        if (DK && DV && WG > 1) __builtin_amdgcn_sched_barrier(0);   // (both tiles at once do not fit the registers)
+        // (rows past the last query are zeros; a wave without keys has nothing to do)
+        if (MASKED && (keys <= 0 || min(at + m + 32, s.nb) - 1 + shift < wkey)) return;
+        const bool masked = MASKED && at + m + shift < wkey + 31;
+        floatx16 x = zero16x(), y = zero16x();
+#pragma unroll
+        for (int i = 0; i < C; ++i) {
+            x = M::mma(Ti::row_frag(qt, m, i, lane), kf.get(i, lane), x);
+            if constexpr (DK) y = M::mma(Ti::row_frag(gt, m, i, lane), vf.get(i, lane), y);
+        }
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+            const int r = m + 8 * g + 4 * (lane >> 5);
+            const floatx4 l4 = *reinterpret_cast<const floatx4 *>(lt + r);
+            floatx4 d4{};
+            if constexpr (DK) d4 = *reinterpret_cast<const floatx4 *>(dt + r);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const bool hidden = masked && key > at + r + j + shift;
+                const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(x[4 * g + j], c, -l4[j]));
+                x[4 * g + j] = hidden ? 0.f : p;
+                if constexpr (DK) y[4 * g + j] = hidden ? 0.f : p * (y[4 * g + j] - d4[j]);
+            }
+        }
+        // Past the last query: zeros, also where a score is none, such as 0 times a key's infinity.
+        if (at + m + 32 > s.nb) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                const bool past = at + m + 8 * (i >> 2) + 4 * (lane >> 5) + (i & 3) >= s.nb;
+                x[i] = past ? 0.f : x[i];
+                y[i] = past ? 0.f : y[i];
+            }
+        }
+        // (an operand: in bf16 rounded, P to 8 bits)
+        Frag f[NP];
+        if constexpr (DV) {
+#pragma unroll
+            for (int i = 0; i < NP; ++i) f[i] = as_frag<T>(x, i);
+            if (masked && any_wild<T, DP, 32>(gt, m, lane)) wild_product<T, DP, DC, NP>(dv, gt, m, f, lane);
+            else add_product<T, DP, DC, NP>(dv, gt, m, f, lane);
+        }
+        if constexpr (DK) {
+            const bool wild = masked && any_wild<T, DP, 32>(qt, m, lane);
+            if (sizeof(T) == 4 || wild) {
+#pragma unroll
+                for (int i = 0; i < NP; ++i) f[i] = as_frag<T>(y, i);
+                if (wild) wild_product<T, DP, DC, NP>(dk, qt, m, f, lane);
+                else add_product<T, DP, DC, NP>(dk, qt, m, f, lane);
+            } else {
+                add_exactly<T, DP, DC>(dk, qt, m, y, lane);
+            }
+        }
+    };
+    auto step = [&](int n, auto mode) __attribute__((always_inline)) {
         tile_sync();
         now = next;
 #pragma unroll
@@ -333,56 +396,16 @@ __global__ __launch_bounds__(256 * WG, (DkvShape<T, DC, DK, DV>::OCC / WG)) void
         if (WG > 1 && n >= total) return;
         const int at = now.at;
         const char *qt = stages + (n / WG & 1) * STAGE, *gt = qt + BYTES;
-        const float *lt = reinterpret_cast<const float *>(gt + BYTES), *dt = lt + 64;
-#pragma unroll
-        for (int m = 0; m < BM; m += 32) {
-            if (DK && DV && WG > 1) __builtin_amdgcn_sched_barrier(0);   // (both tiles at once do not fit the registers)
-            // (rows past the last query are zeros; a wave without keys has nothing to do)
-            if (MASKED && (keys <= 0 || min(at + m + 32, s.nb) - 1 + shift < wkey)) continue;
-            const bool masked = MASKED && at + m + shift < wkey + 31;
-            floatx16 x = zero16x(), y = zero16x();
-#pragma unroll
-            for (int i = 0; i < C; ++i) {
-                x = M::mma(Ti::row_frag(qt, m, i, lane), kf.get(i, lane), x);
-                if constexpr (DK) y = M::mma(Ti::row_frag(gt, m, i, lane), vf.get(i, lane), y);
+        if constexpr (decltype(mode)::value && DK) {   // (in turn, as dq_kernel's)
+#pragma unroll 1
+            for (int m = 0; m < BM; m += 32) {
+                int row = m;
+                asm volatile("" : "+s"(row));
+                tile(at, qt, gt, row, mode);
             }
+        } else {
 #pragma unroll
-            for (int g = 0; g < 4; ++g) {
-                const int r = m + 8 * g + 4 * (lane >> 5);
-                const floatx4 l4 = *reinterpret_cast<const floatx4 *>(lt + r);
-                floatx4 d4{};
-                if constexpr (DK) d4 = *reinterpret_cast<const floatx4 *>(dt + r);
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const bool hidden = masked && key > at + r + j + shift;
-                    const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(x[4 * g + j], c, -l4[j]));
-                    x[4 * g + j] = hidden ? 0.f : p;
-                    if constexpr (DK) y[4 * g + j] = hidden ? 0.f : p * (y[4 * g + j] - d4[j]);
-                }
-            }
-            // Past the last query: zeros, also where a score is none, such as 0 times a key's infinity.
-            if (at + m + 32 > s.nb) {
-#pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    const bool past = at + m + 8 * (i >> 2) + 4 * (lane >> 5) + (i & 3) >= s.nb;
-                    x[i] = past ? 0.f : x[i];
-                    y[i] = past ? 0.f : y[i];
-                }
-            }
-            // (both are operands: in bf16 rounded)
-            Frag f[NP];
-            if constexpr (DV) {
-#pragma unroll
-                for (int i = 0; i < NP; ++i) f[i] = as_frag<T>(x, i);
-                if (masked && any_wild<T, DP, 32>(gt, m, lane)) wild_product<T, DP, DC, NP>(dv, gt, m, f, lane);
-                else add_product<T, DP, DC, NP>(dv, gt, m, f, lane);
-            }
-            if constexpr (DK) {
-#pragma unroll
-                for (int i = 0; i < NP; ++i) f[i] = as_frag<T>(y, i);
-                if (masked && any_wild<T, DP, 32>(qt, m, lane)) wild_product<T, DP, DC, NP>(dk, qt, m, f, lane);
-                else add_product<T, DP, DC, NP>(dk, qt, m, f, lane);
-            }
+            for (int m = 0; m < BM; m += 32) tile(at, qt, gt, m, mode);
         }
     };
     const int hidden_to = max(first_step, min(total, edge * group));
