@@ -214,7 +214,7 @@ __global__ __launch_bounds__(256 * WG, (DqShape<T, DC>::OCC / WG)) void dq_kerne
         if (k + BN * WG < end) issue(k + BN * WG);
         if (WG > 1 && k >= end) return;
         const char *kt = stages + (k / (BN * WG) & 1) * 2 * BYTES, *vt = kt + BYTES;
-        if constexpr (decltype(mode)::value) {   // (in turn: unrolled, what the rare path holds would not fit the registers)
+        if constexpr (sizeof(T) == 2 && decltype(mode)::value) {   // (in turn: unrolled, what the rare path holds would not fit the registers)
 #pragma unroll 1
             for (int n = 0; n < BN && k + n < wend; n += 32) {
                 int row = n;
@@ -223,7 +223,8 @@ __global__ __launch_bounds__(256 * WG, (DqShape<T, DC>::OCC / WG)) void dq_kerne
             }
         } else {
 #pragma unroll
-            for (int n = 0; n < BN; n += 32) tile(kt, vt, k, n, mode);
+            for (int n = 0; n < BN; n += 32)
+                if (!decltype(mode)::value || k + n < wend) tile(kt, vt, k, n, mode);
         }
     };
     // Keys that all of the block's rows see, in whole steps; then the others.
@@ -396,7 +397,7 @@ __global__ __launch_bounds__(256 * WG, (DkvShape<T, DC, DK, DV>::OCC / WG)) void
         if (WG > 1 && n >= total) return;
         const int at = now.at;
         const char *qt = stages + (n / WG & 1) * STAGE, *gt = qt + BYTES;
-        if constexpr (decltype(mode)::value && DK) {   // (in turn, as dq_kernel's)
+        if constexpr (sizeof(T) == 2 && decltype(mode)::value && DK) {   // (in turn, as dq_kernel's)
 #pragma unroll 1
             for (int m = 0; m < BM; m += 32) {
                 int row = m;

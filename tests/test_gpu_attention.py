@@ -404,6 +404,71 @@ def test_graph_replays(dtype):
         assert all(torch.equal(a, b) for a, b in zip(outs, run(q, k, v, g, 7, spec)))
 
 
+@DTYPES
+def test_graph_replays_of_other_sequences(dtype):
+    """The offsets are read by the kernels: a replay has the sequences that they then name."""
+    T, D = 700, 64
+    q, k, v, g = (draw((T, h, D), dtype, i) for i, h in enumerate((4, 2, 2, 4)))
+    off = starts([100, 300, 300])
+    spec = ms.Attention(off)
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        run(q, k, v, g, 7, spec)
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=s):
+            outs = run(q, k, v, g, 7, spec)
+    torch.cuda.synchronize()
+    for lens in ([700, 0, 0], [1, 698, 1], [200, 33, 7], [0, 0, 0], [100, 300, 300]):
+        off.copy_(starts(lens))
+        for t in outs:
+            t.fill_(7.0)   # (all rows are written, also those of no sequence)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(outs, run(q, k, v, g, 7, spec)))
+        assert (outs[0][sum(lens):] == 0).all() and all(torch.isfinite(t.float()).all() for t in outs)
+
+
+def test_threads():
+    """Calls of several threads, on one stream and on streams of their own."""
+    import threading
+    shapes = [(700, 4, 2, 64), (2903, 16, 8, 128), (90, 2, 1, 100), (1300, 6, 2, 72)]
+    data = [[draw((T, h, D), "bf16" if i % 2 else "f32", 10 * i + j) for j, h in enumerate((Hq, Hk, Hk, Hq))]
+            for i, (T, Hq, Hk, D) in enumerate(shapes)]
+    want = [run(*t, 7, ms.Attention()) for t in data]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.current_stream()] * 2 + [torch.cuda.Stream() for _ in range(2)]
+    bad = []
+
+    def work(i):
+        with torch.cuda.stream(streams[i]):
+            for _ in range(5):
+                got = run(*data[i], 7, ms.Attention())
+                streams[i].synchronize()
+                if not all(torch.equal(a, b) for a, b in zip(got, want[i])):
+                    bad.append(i)
+
+    threads = [threading.Thread(target=work, args=(i,)) for i in range(4)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert not bad
+
+
+@DTYPES
+def test_broadcast_inputs(dtype):
+    """A head of keys and values that all heads share by a stride of 0: its gradient is the sum over them."""
+    T, D = 200, 64
+    q, g = draw((T, 4, D), dtype, 0), draw((T, 4, D), dtype, 3)
+    k1, v1 = draw((T, 1, D), dtype, 1).requires_grad_(), draw((T, 1, D), dtype, 2).requires_grad_()
+    msa.MSAttention()(q, k1.expand(T, 4, D), v1.expand(T, 4, D)).backward(g)
+    refs, bars = reference(q, k1.detach(), v1.detach(), g, [T], [T], True, D ** -0.5, dtype)
+    for name, got, i in (("k", k1.grad, 2), ("v", v1.grad, 3)):
+        # four gradients, each rounded once, and the roundings of their sum
+        close(name, got, refs[i], 4 * bars[i])
+
+
 def test_on_another_stream():
     q, k, v, g = (draw((300, 2, 80), "bf16", i) for i in range(4))
     first = run(q, k, v, g, 7, ms.Attention())
