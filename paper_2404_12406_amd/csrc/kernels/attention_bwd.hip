@@ -541,9 +541,9 @@ int run(const AttnArgs &a, char *ws, hipStream_t st) {
         // instead of five (1777 x 2 heads of 72 in fp32: 74 us against 57 and 49).
         constexpr bool both = DC <= (sizeof(T) == 2 ? 128 : 96);
         // Blocks of two groups (attn_tile.h): dk and dv each for itself where a CU does not hold both sums of eight waves,
-        // the same for all masks, so that a gradient's bits do not depend on which others are asked for.  (7 sequences
-        // of 8192 rows, 32 on 8 heads, bf16: dv alone of 128 columns 206 -> 173 us, dk alone 362 -> 274, both 424 -> 431; of
-        // 64 columns 141 -> 114 and 238 -> 197.  4 x 2048 rows, 8 heads of 128, 32 steps: 57 -> 54, both 117 -> 136.  In fp32 two
+        // the same for all masks, so that a gradient's bits do not depend on which others are asked for.  (7 sequences of
+        // 8192 rows, 32 on 8 heads, bf16: dv alone of 128 columns 208 -> 169 us, dk alone 390 -> 311, both 450 -> 475; of 64
+        // columns 136 -> 110, 243 -> 195, 266 -> 230.  4 x 2048 rows, 8 heads of 128, 32 steps: both 127 -> 151.  In fp32 two
         // kernels instead of one cost more, 8 on 2 heads of 64 483 -> 591.)
         const bool few = sizeof(T) == 2 && DkvShape<T, DC, true, false>::OCC == 2 && wide_blocks((int64_t)grid.x * grid.y, p.dkv_steps, 40);
         if (both && dk && dv && !(few && DkvShape<T, DC, true, true>::OCC == 1)) {

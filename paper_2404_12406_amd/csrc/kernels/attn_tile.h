@@ -247,8 +247,8 @@ inline int span_splits(int64_t blocks, int64_t steps, int64_t bytes) {
 // Up to 768 blocks, of which a CU holds two, all run at once, and the longest end alone on a CU that they cannot
 // fill.  Where they have `least` steps or more on average, such blocks have eight waves, which take every
 // other step each and meet at the end.  (bf16, 8192 rows of one sequence, 8 heads of 128: forward 178 -> 144 us,
-// dq 251 -> 202, dv 186 -> 148.  With two to 16 steps the longer start costs more: 64 x 128 rows, 4 heads of 64 forward
-// 10 -> 13 us, 8 x 1024 rows 22 -> 24.  With 1152 blocks dv 312 -> 356.)
+// dv 186 -> 148.  With two to 16 steps the longer start costs more: 64 x 128 rows, 4 heads of 64 forward
+// 10 -> 13 us, 8 x 1024 rows 22 -> 24.  With 1152 blocks dv 312 -> 356 us.)
 inline bool wide_blocks(int64_t blocks, int64_t steps, int64_t least) { return blocks <= 768 && steps >= least; }
 
 // The sum (maximum) of a lane's value and that of the lane 32 away.
