@@ -192,6 +192,13 @@ def test_long_walks_of_few_blocks(q_lens, k_lens, D, causal):
     case(q_lens, k_lens, 16, 8, D, "bf16", causal, seed=5)
 
 
+@CAUSAL
+@pytest.mark.parametrize("q_lens,k_lens", [([3500], [3500]), ([1800], [5000])])
+def test_long_walks_divided(q_lens, k_lens, causal):
+    """The same where the keys are divided over blocks as well."""
+    case(q_lens, k_lens, 8, 4, 64, "bf16", causal, seed=6)
+
+
 @pytest.mark.parametrize("D", [64, 128])
 def test_long_walks_by_mask(D):
     q, k, v, g = (draw((2903, h, D), "bf16", i) for i, h in enumerate((16, 8, 8, 16)))
