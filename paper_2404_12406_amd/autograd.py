@@ -397,7 +397,8 @@ class MSHeadNormRotary(nn.Module):
     """Norms of queries and keys for each head, with the rotation by position in the same
     pass (see api.HeadNormRotary): forward(x, positions) for x[T, H, D], the first q_heads of
     its heads scaled by weight_q[D], the others by weight_k[D] (None: ones).  Keeps x and
-    the positions alone; norm=False (no weights) the positions."""
+    the positions alone; norm=False (no weights) the positions.  Converting the module
+    (bfloat16(), to(dtype)) converts its weights; inv_freq stays float32."""
 
     def __init__(self, weight_q: Optional[torch.Tensor], weight_k: Optional[torch.Tensor], q_heads: int,
                  inv_freq: Optional[torch.Tensor] = None, eps: float = 1e-6, interleaved: bool = False, norm: bool = True):
@@ -406,6 +407,15 @@ class MSHeadNormRotary(nn.Module):
         self.weight_k = weight_k if (weight_k is None or isinstance(weight_k, nn.Parameter)) else nn.Parameter(weight_k)
         self.register_buffer("inv_freq", inv_freq, persistent=False)
         self.q_heads, self.eps, self.interleaved, self.norm = int(q_heads), float(eps), bool(interleaved), bool(norm)
+
+    def _apply(self, fn, *args, **kwargs):
+        # The frequencies go where the module goes, but keep their type and values: of 8 bits, an
+        # angle of position 5000 is off by radians.
+        freq = self.inv_freq
+        super()._apply(fn, *args, **kwargs)
+        if freq is not None and self.inv_freq.dtype != freq.dtype:
+            self.inv_freq = freq.to(self.inv_freq.device)
+        return self
 
     def forward(self, x, positions=None):
         freq = self.inv_freq if positions is not None else None
