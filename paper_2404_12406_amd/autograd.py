@@ -397,7 +397,8 @@ class MSHeadNormRotary(nn.Module):
     """Norms of queries and keys for each head, with the rotation by position in the same
     pass (see api.HeadNormRotary): forward(x, positions) for x[T, H, D], the first q_heads of
     its heads scaled by weight_q[D], the others by weight_k[D] (None: ones).  Keeps x and
-    the positions alone; norm=False (no weights) the positions.  Converting the module
+    the positions alone; norm=False (no weights) the positions.  With inv_freq a call needs
+    positions (ValueError without).  Converting the module
     (bfloat16(), to(dtype)) converts its weights; inv_freq stays float32."""
 
     def __init__(self, weight_q: Optional[torch.Tensor], weight_k: Optional[torch.Tensor], q_heads: int,
@@ -418,8 +419,7 @@ class MSHeadNormRotary(nn.Module):
         return self
 
     def forward(self, x, positions=None):
-        freq = self.inv_freq if positions is not None else None
-        spec = api.HeadNormRotary(positions, freq, self.q_heads, self.norm, self.eps, self.interleaved)
+        spec = api.HeadNormRotary(positions, self.inv_freq, self.q_heads, self.norm, self.eps, self.interleaved)
         return _layer(spec, x, self.weight_q, self.weight_k)
 
 

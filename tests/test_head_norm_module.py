@@ -52,3 +52,20 @@ def test_frequencies_follow_the_device():
 def test_modules_without_frequencies_convert():
     m = msa.MSHeadNormRotary(torch.rand(8), None, 2).bfloat16()
     assert m.inv_freq is None and m.weight_q.dtype == torch.bfloat16
+
+
+@pytest.mark.parametrize("mode", [torch.no_grad, torch.enable_grad])
+def test_frequencies_without_positions_are_refused(mode, monkeypatch):
+    """As by the layer itself: nothing is computed without the rotation that the module describes."""
+    made = []
+    monkeypatch.setattr(api, "_one_gpu", lambda *a: None)
+    monkeypatch.setattr(api, "_block_run", lambda *a: made.append(a) or 0)
+    monkeypatch.setattr(api, "_stream", lambda d: None)
+    w = torch.rand(64)
+    for m in (msa.MSHeadNormRotary(w, w, 2, FREQ), msa.MSHeadNormRotary(None, None, 2, FREQ, norm=False)):
+        with mode(), pytest.raises(ValueError, match="without positions"):
+            m(torch.randn(3, 4, 64))
+    assert not made
+    with torch.no_grad():   # a module without frequencies needs none
+        assert msa.MSHeadNormRotary(w, w, 2)(torch.randn(3, 4, 64)).shape == (3, 4, 64)
+    assert len(made) == 1
