@@ -20,6 +20,7 @@
 // 4111 keys in pages of 16 some 10 us, two launches.
 #include <algorithm>
 
+#include "../paged_plan.h"
 #include "attn_tile.h"
 
 namespace ms {
@@ -299,21 +300,6 @@ __global__ __launch_bounds__(256) void join_kernel(PagedArgs a, int splits, int 
 }
 
 namespace {
-
-struct PagedPlan {
-    int splits, per;   // blocks of a sequence at most, keys of each
-};
-
-constexpr int kPagedBlocks = 8192;
-
-// Keys a block: some 8192 blocks if every sequence filled its table, whole steps of a
-// block's four waves.  How full the tables are is known on the device alone, so blocks past a sequence's end
-// return at once, and there have to be enough of the others.
-PagedPlan paged_plan(const PagedArgs &a) {
-    const int64_t room = (int64_t)a.width * a.page, work = (int64_t)a.n * a.Hk * ((a.Hq / a.Hk + 31) / 32);
-    const int64_t per = std::max<int64_t>(128, (room * work / kPagedBlocks + 127) / 128 * 128);
-    return {(int)std::max<int64_t>(1, (room + per - 1) / per), (int)std::min<int64_t>(per, INT32_MAX / 2)};
-}
 
 template <typename T, int DP, bool FAST>
 void paged_run(const PagedArgs &a, float *ws, hipStream_t st) {
