@@ -475,7 +475,8 @@ uint64_t ms_attention_kept_bytes(int64_t rows, int64_t heads, uint32_t mask);
  * rows that are no whole aligned 16-byte vectors are staged.  scale: finite, > 0 (MS_E_ARG otherwise).
  * Sums and statistics are in fp32; in bf16 P is rounded to bf16 as an operand of its products, dS in two
  * operands, the rounded value and what that leaves off.  A gradient's bits do not depend on which
- * others are asked for.  Backward is ms_layer_backward(); ms_layer_forward() rejects MS_ATTENTION (MS_E_ARG).
+ * others are asked for, nor on where it lies: gradients may lie on q, k, v, o or grad_y (not on each other).  Where they do,
+ * they are written after the last read, from sums in fp32 in transient workspace.  Backward is ms_layer_backward(); ms_layer_forward() rejects MS_ATTENTION (MS_E_ARG).
  */
 ms_status ms_attention_forward(const ms_tensor *q, const ms_tensor *k, const ms_tensor *v, const int32_t *q_offsets,
                                const int32_t *k_offsets, int64_t sequences, int32_t causal, float scale, void *kept,

@@ -2,6 +2,7 @@
 // over whole prompts, the paged cache and the attention of single tokens over it.
 // Validation, the save rule and the records follow blocks.cpp.
 #include "blocks.h"
+#include "overlap.h"
 
 using namespace ms::rt;
 
@@ -180,6 +181,10 @@ ms_status attention_backward(ms_record *r, const ms_tensor *go, const ms_tensor 
                 o = sg.add(both ? &r->y : nullptr, true), g = sg.add(go, true), dq = sg.add(gq, true), dk = sg.add(gk, true),
                 dv = sg.add(gv, true);
     ms::AttnArgs a = attention_args(&r->x, &r->W, r->blk);
+    // (stand-ins are read, and written, before and after all kernels)
+    for (const Stand *out : {&dq, &dk, &dv})
+        for (const Stand *in : {&q, &k, &v, &o, &g})
+            a.shared |= out->off == kNoStage && in->off == kNoStage && shared(out->t, in->t) != Shared::kNo;
     const size_t kb = ms::attention_bwd_workspace(dt, a, gq, gk, gv);
     Work w;
     ms_status st = take(&w, sg.bytes + kb, stream, fixed);

@@ -254,6 +254,8 @@ struct AttnArgs {
     int causal;
     float scale;
     float *lse;
+    // backward: gradients lie where its kernels read, so all are written after the last of them
+    bool shared;
 };
 constexpr int kMaxHeadDim = 256;
 size_t attention_fwd_workspace(int dtype, const AttnArgs &a);

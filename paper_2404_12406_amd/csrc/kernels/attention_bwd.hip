@@ -115,10 +115,11 @@ template <typename T, int DC> constexpr bool kHold1 = DC * sizeof(T) < 1024;
 template <typename T, int DC> constexpr bool kHold = DC * sizeof(T) < 768;
 
 // What the kernels take besides: delta, which dq_kernel writes, and where they leave sums in fp32 if the
-// other side is divided: [split][rows][heads][DC].
+// other side is divided, or a gradient has to wait until everything is read: [split][rows][heads][DC].
 struct Parts {
     float *delta;
     int splits;
+    bool sums;
     float *a, *b;
 };
 
@@ -238,7 +239,7 @@ __global__ __launch_bounds__(256 * WG, (DqShape<T, DC>::OCC / WG)) void dq_kerne
         if (side) return;
     }
     if (rows <= 0) return;
-    if (part.splits > 1) {
+    if (part.sums) {
         store_sums<DC>(acc, part.a + ((blockIdx.y * a.Tq + first) * a.Hq + head) * DC, (int64_t)a.Hq * DC, rows, lane);
         return;
     }
@@ -420,7 +421,7 @@ __global__ __launch_bounds__(256 * WG, (DkvShape<T, DC, DK, DV>::OCC / WG)) void
         if (side) return;
     }
     if (keys <= 0) return;
-    if (part.splits > 1) {
+    if (part.sums) {
         const int64_t at = ((blockIdx.y * a.Tk + first) * a.Hk + hk) * DC;
         if constexpr (DK) store_sums<DC>(dk, part.a + at, (int64_t)a.Hk * DC, keys, lane);
         if constexpr (DV) store_sums<DC>(dv, part.b + at, (int64_t)a.Hk * DC, keys, lane);
@@ -433,7 +434,7 @@ __global__ __launch_bounds__(256 * WG, (DkvShape<T, DC, DK, DV>::OCC / WG)) void
         store_rows<T, DP, DC>(dv, 1.f, false, mine, static_cast<T *>(a.dv.p) + first * a.dv.ts + hk * a.dv.hs, a.dv.ts, keys, a.D, lane);
 }
 
-// A gradient from its partial sums: a vector a thread.
+// A gradient from its sums: a vector a thread.
 struct Sum {
     HeadsView out;
     const float *part;
@@ -468,9 +469,10 @@ namespace {
 
 size_t al256(size_t n) { return (n + 255) / 256 * 256; }
 
-// What a backward lays out: delta, then partial sums of dq, dk and dv; the steps of their blocks.
+// What a backward lays out: delta, then sums of dq, dk and dv; the steps of their blocks.
 struct Plan {
     int dq_splits, dkv_splits;
+    bool dq_sums, dkv_sums;
     int64_t dq_steps, dkv_steps;
     size_t dq_at, dk_at, dv_at, bytes;
 };
@@ -479,14 +481,16 @@ template <typename T, int DC>
 Plan plan(const AttnArgs &a, bool dq, bool dk, bool dv) {
     const bool packed = a.qoff != nullptr;
     const int64_t n = packed ? std::max(a.n, 1) : 1, group = a.Hq / a.Hk;
-    Plan p{1, 1, a.Tk / n / DqShape<T, DC>::BN, a.Tq / n * group / DkvShape<T, DC, true, true>::BM, 0, 0, 0, 0};
+    Plan p{1, 1, false, false, a.Tk / n / DqShape<T, DC>::BN, a.Tq / n * group / DkvShape<T, DC, true, true>::BM, 0, 0, 0, 0};
     if (dq) p.dq_splits = span_splits<T>(span_slots(packed, a.n, a.Tq, kRows) * a.Hq, p.dq_steps, a.Tq * a.Hq * DC * 4);
     if (dk || dv) p.dkv_splits = span_splits<T>(span_slots(packed, a.n, a.Tk, kRows) * a.Hk, p.dkv_steps, a.Tk * a.Hk * DC * 8);
     p.dq_steps /= p.dq_splits;
     p.dkv_steps /= p.dkv_splits;
-    const size_t keys = p.dkv_splits > 1 ? al256((size_t)p.dkv_splits * a.Tk * a.Hk * DC * sizeof(float)) : 0;
+    p.dq_sums = dq && (p.dq_splits > 1 || a.shared);
+    p.dkv_sums = p.dkv_splits > 1 || a.shared;
+    const size_t keys = p.dkv_sums ? al256((size_t)p.dkv_splits * a.Tk * a.Hk * DC * sizeof(float)) : 0;
     p.dq_at = dk ? al256((size_t)a.Tq * a.Hq * sizeof(float)) : 0;
-    p.dk_at = p.dq_at + (p.dq_splits > 1 ? al256((size_t)p.dq_splits * a.Tq * a.Hq * DC * sizeof(float)) : 0);
+    p.dk_at = p.dq_at + (p.dq_sums ? al256((size_t)p.dq_splits * a.Tq * a.Hq * DC * sizeof(float)) : 0);
     p.dv_at = p.dk_at + (dk ? keys : 0);
     p.bytes = p.dv_at + (dv ? keys : 0);
     return p;
@@ -513,13 +517,14 @@ int run(const AttnArgs &a, char *ws, hipStream_t st) {
     const bool packed = a.qoff != nullptr, dq = a.dq.p, dk = a.dk.p, dv = a.dv.p;
     const Plan p = plan<T, DC>(a, dq, dk, dv);
     constexpr int V = Vec16<T>::N;
-    float *delta = reinterpret_cast<float *>(ws);
+    float *delta = reinterpret_cast<float *>(ws), *dq_sums = reinterpret_cast<float *>(ws + p.dq_at),
+          *dk_sums = reinterpret_cast<float *>(ws + p.dk_at), *dv_sums = reinterpret_cast<float *>(ws + p.dv_at);
     if (dk && !dq && a.Tq > 0) {
         hipLaunchKernelGGL((delta_kernel<T, DC>), dim3((unsigned)((a.Tq + 127) / 128), (unsigned)a.Hq), dim3(256), 0, st, a, delta);
     }
     if (dq && a.Tq > 0) {
         const int64_t slots = span_slots(packed, a.n, a.Tq, kRows);
-        const Parts part{dk ? delta : nullptr, p.dq_splits, reinterpret_cast<float *>(ws + p.dq_at), nullptr};
+        const Parts part{dk ? delta : nullptr, p.dq_splits, p.dq_sums, dq_sums, nullptr};
         const dim3 grid((unsigned)(slots * a.Hq), (unsigned)part.splits);
         constexpr bool pairs = sizeof(T) == 2 && DqShape<T, DC>::OCC == 2;
         if (pairs && wide_blocks((int64_t)grid.x * grid.y, p.dq_steps, 24)) {
@@ -527,15 +532,10 @@ int run(const AttnArgs &a, char *ws, hipStream_t st) {
         } else {
             hipLaunchKernelGGL((dq_kernel<T, DC, 1>), grid, dim3(256), 0, st, a, part);
         }
-        if (part.splits > 1) {
-            const Sum s{a.dq, part.a, a.scale};
-            hipLaunchKernelGGL(sum_kernel<T>, dim3((unsigned)((a.Tq * a.Hq * (a.D / V) + 255) / 256)), dim3(256), 0, st, s, s, a.Tq, a.Hq,
-                               a.D, DC, part.splits);
-        }
     }
     if ((dk || dv) && a.Tk > 0) {
         const int64_t slots = span_slots(packed, a.n, a.Tk, kRows);
-        const Parts part{delta, p.dkv_splits, reinterpret_cast<float *>(ws + p.dk_at), reinterpret_cast<float *>(ws + p.dv_at)};
+        const Parts part{delta, p.dkv_splits, p.dkv_sums, dk_sums, dv_sums};
         const dim3 grid((unsigned)(slots * a.Hk), (unsigned)part.splits);
         // Both at once up to where both sums and their operands are in a wave's registers: four products
         // instead of five (1777 x 2 heads of 72 in fp32: 74 us against 57 and 49).
@@ -552,11 +552,17 @@ int run(const AttnArgs &a, char *ws, hipStream_t st) {
             if (dk) dkv_run<T, DC, true, false>(grid, few, a, part, st);
             if (dv) dkv_run<T, DC, false, true>(grid, few, a, part, st);
         }
-        if (part.splits > 1) {
-            const Sum k{a.dk, part.a, a.scale}, v{a.dv, part.b, 1.f};
-            hipLaunchKernelGGL(sum_kernel<T>, dim3((unsigned)((a.Tk * a.Hk * (a.D / V) + 255) / 256), dk && dv ? 2 : 1), dim3(256), 0, st,
-                               dk ? k : v, v, a.Tk, a.Hk, a.D, DC, part.splits);
-        }
+    }
+    // (gradients may lie where the kernels above read)
+    if (p.dq_sums && a.Tq > 0) {
+        const Sum s{a.dq, dq_sums, a.scale};
+        hipLaunchKernelGGL(sum_kernel<T>, dim3((unsigned)((a.Tq * a.Hq * (a.D / V) + 255) / 256)), dim3(256), 0, st, s, s, a.Tq, a.Hq, a.D, DC,
+                           p.dq_splits);
+    }
+    if ((dk || dv) && p.dkv_sums && a.Tk > 0) {
+        const Sum k{a.dk, dk_sums, a.scale}, v{a.dv, dv_sums, 1.f};
+        hipLaunchKernelGGL(sum_kernel<T>, dim3((unsigned)((a.Tk * a.Hk * (a.D / V) + 255) / 256), dk && dv ? 2 : 1), dim3(256), 0, st,
+                           dk ? k : v, v, a.Tk, a.Hk, a.D, DC, p.dkv_splits);
     }
     return (int)hipGetLastError();
 }
