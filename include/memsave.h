@@ -438,7 +438,8 @@ typedef struct {
  * overlapping itself); y may be x itself where the record does not borrow it (MS_E_ARG
  * otherwise), in the same layout.
  * gamma_q, gamma_k: [D] contiguous or NULL (ones).  Statistics, angles and sums are in 32
- * bits or more.  Backward is ms_layer_backward().  ms_layer_forward() rejects
+ * bits or more.  Backward is ms_layer_backward(); dx may lie on dy or on x, and where it
+ * does in other places than theirs it is staged.  ms_layer_forward() rejects
  * MS_HEAD_NORM_ROTARY (MS_E_ARG).
  */
 ms_status ms_head_norm_rotary_forward(const ms_tensor *x, const ms_tensor *gamma_q, const ms_tensor *gamma_k,

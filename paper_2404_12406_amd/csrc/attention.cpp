@@ -44,9 +44,10 @@ bool in_place(const ms_tensor *t, bool whole) {
 
 struct Stands {
     size_t bytes = 0;
-    Stand add(const ms_tensor *t, bool whole) {
+    // apart: not in its own memory
+    Stand add(const ms_tensor *t, bool whole, bool apart = false) {
         Stand s{t, kNoStage, whole};
-        if (!t || numel(t) == 0 || in_place(t, whole)) return s;
+        if (!t || numel(t) == 0 || (in_place(t, whole) && !apart)) return s;
         s.off = bytes;
         bytes += al256((size_t)(t->shape[0] * t->shape[1] * padded(t->shape[2], t->dtype)) * elt_size(t->dtype));
         return s;
@@ -59,6 +60,11 @@ bool moved(const ms_tensor *x, const ms_tensor *y) {
     for (int i = 0; i < 3; ++i)
         if (y->shape[i] > 1 && x->stride[i] != y->stride[i]) return true;
     return false;
+}
+
+// Whether kernels that write a head where they have read it may not write y where they read x.
+bool crosses(const ms_tensor *x, const ms_tensor *y) {
+    return x && y && !same_places(x, y) && shared(x, y) != Shared::kNo;
 }
 
 // The workspace that a tensor like t takes in a backward, where its gradient is expected
@@ -137,7 +143,9 @@ ms_status rotary_backward(ms_record *r, const ms_tensor *gy, const ms_tensor *gx
     ms::RotaryArgs a = rotary_args(&rot, &r->x, &r->W, &r->b);
     const bool read_x = a.norm && r->x.data;
     Stands sg;
-    const Stand sx = sg.add(read_x ? &r->x : nullptr, false), sy = sg.add(gy, false), so = sg.add(gx, false);
+    const Stand sx = sg.add(read_x ? &r->x : nullptr, false), sy = sg.add(gy, false);
+    const bool apart = (sx.off == kNoStage && crosses(sx.t, gx)) || (sy.off == kNoStage && crosses(gy, gx));
+    const Stand so = sg.add(gx, false, apart);
     const size_t kb = ms::rotary_bwd_workspace(dt, a, gq || gk);
     Work w;
     ms_status st = take(&w, sg.bytes + kb, stream, fixed);

@@ -135,3 +135,28 @@ def test_stand_ins_are_apart(lib):
                                  None) == 0
     assert lib.overlap_noted() == 0
     c.free()
+
+
+# ------------------------------------------------------------------ head norms' backward
+@pytest.mark.parametrize("norm", [1, 0])
+def test_head_norm_gradients_that_cross_what_is_read_are_staged(lib, norm):
+    H, n = HQ + HK, TQ * (HQ + HK) * D * 2
+    over = {} if norm else dict(gq=None, gk=None, mask=1)
+
+    def staged(dx, x=FAKE, dy=OUT, strides=None, **shape):
+        c = Call(lib, "rotary", norm=norm, x=tensor((TQ, H, D), addr=x), y=tensor((TQ, H, D), addr=OUT + (1 << 30)), **over)
+        assert c.forward() == 0
+        lib.stub_reset()
+        to = tensor((TQ, H, D), strides=strides, addr=dx)
+        g = [tensor((D,), addr=OUT + (5 << 30) + (i << 20)) if norm else None for i in range(2)]
+        assert lib.ms_layer_backward(c.h, ref(tensor((TQ, H, D), addr=dy)), ref(to), ref(g[0]), ref(g[1]), None) == 0
+        c.free()
+        return lib.stub_log() == b"copy4;"
+
+    other = (D, TQ * D, 1)
+    assert not staged(OUT + (2 << 30)) and not staged(OUT + (2 << 30), strides=other)
+    assert not staged(OUT) and not staged(FAKE)                        # a head is written where it was read
+    assert staged(OUT, strides=other) and staged(OUT + 2 * D) and staged(OUT + 2 * D * H) and staged(OUT - 2 * D)
+    assert not staged(OUT + n) and not staged(OUT - n)
+    for dx, strides in ((FAKE, other), (FAKE + 2 * D, None)):
+        assert staged(dx, strides=strides) == bool(norm)               # a rotation alone does not read x

@@ -1,5 +1,5 @@
-"""Gradients of attention written where its backward reads: on q, k, v, o or
-the gradient of the output.  Every result has the bits that it has
+"""Gradients of attention and of head norms written where their backward reads: on q, k, v, o or
+the gradient of the output, in the same layout or another.  Every result has the bits that it has
 in memory of its own (each is the same sum, rounded once)."""
 import pytest
 import torch
@@ -117,3 +117,27 @@ def test_a_prepared_call_of_its_own():
         call.backward()
         same([call.y, *grads], [o, *want])
 
+# ------------------------------------------------------------------ head norms
+@DTYPES
+@pytest.mark.parametrize("norm", [True, False])
+@pytest.mark.parametrize("where", ["dy", "dy turned over", "dy a row on", "dy a head on", "x", "x turned over"])
+@pytest.mark.parametrize("D,R", [(64, 64), (90, 36), (33, 30)])
+def test_head_norm_gradients_on_what_is_read(D, R, where, norm, dtype):
+    T, H = 60, 6
+    x, dy = draw((T, H, D), dtype, 0, 1.5), draw((T, H, D), dtype, 1)
+    gq, gk = (1 + draw((D,), dtype, 2 + i, 0.3) if norm else None for i in range(2))
+    pos = torch.arange(T, dtype=torch.int32, device="cuda") * 37
+    spec = ms.HeadNormRotary(pos, ms.rotary_frequencies(R, device="cuda"), 4, norm)
+    mask = 7 if norm else 1
+    want = ms.layer_backward(ms.layer_forward(spec, x, gq, gk, mask)[1], dy)
+    room = torch.zeros((T + 1) * H * D, dtype=x.dtype, device="cuda")
+    room[:T * H * D] = (dy if where[0] == "d" else x).flatten()
+    at = room[:T * H * D].view(T, H, D)
+    if where[0] == "d":
+        dy = at
+    else:
+        x = at
+    to = {"turned over": room[:T * H * D].view(H, T, D).transpose(0, 1), "a row on": room[H * D:].view(T, H, D),
+          "a head on": room[D:][:T * H * D].view(T, H, D)}.get(where.partition(" ")[2], at)
+    _, rec = ms.layer_forward(spec, x, gq, gk, mask)
+    same(ms.layer_backward(rec, dy, to), want)
