@@ -435,8 +435,8 @@ typedef struct {
  * So a record borrows the positions and frequencies, with a norm x, and for INPUT the
  * scales; no statistics.  Mask bits: INPUT x, WEIGHT gamma_q, BIAS gamma_k.
  * x, y: [T, H, D], 1 <= D <= 256 (MS_E_UNSUPPORTED otherwise), any strides (y not
- * overlapping itself); y may be x itself where the record does not borrow it (MS_E_ARG
- * otherwise), in the same layout.
+ * overlapping itself); y may be x itself where the record does not borrow it, in the same
+ * layout (MS_E_ARG otherwise, also where it begins elsewhere in x).
  * gamma_q, gamma_k: [D] contiguous or NULL (ones).  Statistics, angles and sums are in 32
  * bits or more.  Backward is ms_layer_backward(); dx may lie on dy or on x, and where it
  * does in other places than theirs it is staged.  ms_layer_forward() rejects
@@ -495,7 +495,8 @@ ms_status ms_attention_forward(const ms_tensor *q, const ms_tensor *k, const ms_
  * tables[sequence][p / page], p the position.  tables: [sequences, width] on the
  * device.  A token whose position, sequence or page lies outside is not written to the cache
  * (a negative position marks padding); its query is.  Two tokens of one place: each
- * element of it is one of the two's.  q may be x's own first heads.  There is no record: the cache is no function of x alone.
+ * element of it is one of the two's.  q may be x's own first heads, but not
+ * others of x (MS_E_ARG).  There is no record: the cache is no function of x alone.
  */
 ms_status ms_cache_append(const ms_tensor *x, const ms_tensor *gamma_q, const ms_tensor *gamma_k, const ms_rotary *rotary,
                           const ms_tensor *k_pages, const ms_tensor *v_pages, const int32_t *tables, int64_t sequences,
@@ -509,7 +510,7 @@ ms_status ms_cache_append(const ms_tensor *x, const ms_tensor *gamma_q, const ms
  * less gives zeros; one past width * page, or a used page outside the cache, NaN.  What lies in
  * the cache past the length takes no part.  A sequence's keys are divided over blocks and their
  * sums joined in a fixed order, in transient workspace.  Sums and statistics are in fp32; in
- * bf16 probabilities are rounded to bf16 as an operand.  o may be q.  width * page: less than
+ * bf16 probabilities are rounded to bf16 as an operand.  o may be q, but not other heads of it (MS_E_ARG).  width * page: less than
  * 2^31 - 2^12 (MS_E_UNSUPPORTED).
  */
 ms_status ms_paged_attention_forward(const ms_tensor *q, const ms_tensor *k_pages, const ms_tensor *v_pages,

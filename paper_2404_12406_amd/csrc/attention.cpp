@@ -54,17 +54,9 @@ struct Stands {
     }
 };
 
-// Whether y is x's memory in another order: kernels write a head where they have read it.
-bool moved(const ms_tensor *x, const ms_tensor *y) {
-    if (!x->data || x->data != y->data || numel(y) == 0) return false;
-    for (int i = 0; i < 3; ++i)
-        if (y->shape[i] > 1 && x->stride[i] != y->stride[i]) return true;
-    return false;
-}
-
-// Whether kernels that write a head where they have read it may not write y where they read x.
-bool crosses(const ms_tensor *x, const ms_tensor *y) {
-    return x && y && !same_places(x, y) && shared(x, y) != Shared::kNo;
+// Whether y lies where x does, but not its heads where x's are: kernels write a head where they have read it.
+Shared crosses(const ms_tensor *x, const ms_tensor *y) {
+    return !x || !y || same_places(x, y) ? Shared::kNo : shared(x, y);
 }
 
 // The workspace that a tensor like t takes in a backward, where its gradient is expected
@@ -144,7 +136,7 @@ ms_status rotary_backward(ms_record *r, const ms_tensor *gy, const ms_tensor *gx
     const bool read_x = a.norm && r->x.data;
     Stands sg;
     const Stand sx = sg.add(read_x ? &r->x : nullptr, false), sy = sg.add(gy, false);
-    const bool apart = (sx.off == kNoStage && crosses(sx.t, gx)) || (sy.off == kNoStage && crosses(gy, gx));
+    const bool apart = (sx.off == kNoStage && crosses(sx.t, gx) != Shared::kNo) || (sy.off == kNoStage && crosses(gy, gx) != Shared::kNo);
     const Stand so = sg.add(gx, false, apart);
     const size_t kb = ms::rotary_bwd_workspace(dt, a, gq || gk);
     Work w;
@@ -262,8 +254,8 @@ ms_status ms_head_norm_rotary_forward(const ms_tensor *x, const ms_tensor *gamma
     if (!st) st = check_heads(y, "y", x->dtype, true);
     if (st) return st;
     if (!same_shape(x, y)) return fail(MS_E_SHAPE, "y must have the shape of x");
-    if (mask && rotary->norm && x->data && x->data == y->data) return fail(MS_E_ARG, "y must not be x, which the backward reads");
-    if (moved(x, y)) return fail(MS_E_ARG, "y may be x, but not in another layout");
+    if (mask && rotary->norm && shared(x, y) == Shared::kYes) return fail(MS_E_ARG, "y must not be x, which the backward reads");
+    if (crosses(x, y) == Shared::kYes) return fail(MS_E_ARG, "y may be x, but not other heads of x");
     ms::RotaryArgs a = rotary_args(rotary, x, gamma_q, gamma_k);
     Stands sg;
     const Stand sx = sg.add(x, false), sy = sg.add(y, false);
@@ -335,8 +327,8 @@ ms_status ms_attention_forward(const ms_tensor *q, const ms_tensor *k, const ms_
     if (k->shape[2] != D || !same_shape(k, v)) return fail(MS_E_SHAPE, "k and v must be alike, with heads of q's size");
     if (!same_shape(q, o)) return fail(MS_E_SHAPE, "o must have the shape of q");
     // (other blocks read k and v later, and the backward q)
-    if (o->data && Tk > 0 && numel(o) > 0 && (o->data == q->data || o->data == k->data || o->data == v->data))
-        return fail(MS_E_ARG, "o must not be q, k or v");
+    for (const ms_tensor *t : {q, k, v})
+        if (Tk > 0 && shared(t, o) == Shared::kYes) return fail(MS_E_ARG, "o must not be q, k or v");
     // stand-ins of padded rows have 32-bit counts too
     if (capped_product({std::max(Tq * Hq, Tk * Hk), padded(D, q->dtype)}) > kMaxElems) return fail(MS_E_UNSUPPORTED, "2^31 or more padded elements");
     if (!(scale > 0.f) || !std::isfinite(scale)) return fail(MS_E_ARG, "scale must be finite and > 0");
@@ -428,7 +420,7 @@ ms_status ms_cache_append(const ms_tensor *x, const ms_tensor *gamma_q, const ms
         if ((st = check_heads(q, "q", x->dtype, true))) return st;
         if (q->shape[0] != T || q->shape[1] != rotary->q_heads || q->shape[2] != D)
             return fail(MS_E_SHAPE, "q must be [%lld, %lld, %lld]", (long long)T, (long long)rotary->q_heads, (long long)D);
-        if (moved(x, q)) return fail(MS_E_ARG, "q may be x's first heads, but not in another layout");
+        if (crosses(x, q) == Shared::kYes) return fail(MS_E_ARG, "q may be x's first heads, but not others of x");
     }
     ms::RotaryArgs a = rotary_args(rotary, x, gamma_q, gamma_k);
     a.Hk = (int)Hk;
@@ -472,7 +464,7 @@ ms_status ms_paged_attention_forward(const ms_tensor *q, const ms_tensor *k_page
     if (D != k_pages->shape[3]) return fail(MS_E_SHAPE, "q has heads of %lld elements, the cache of %lld", (long long)D, (long long)k_pages->shape[3]);
     if (Hq < 1 || Hq % Hk) return fail(MS_E_SHAPE, "%lld query heads for %lld heads of keys", (long long)Hq, (long long)Hk);
     if (!same_shape(q, o)) return fail(MS_E_SHAPE, "o must have the shape of q");
-    if (moved(q, o)) return fail(MS_E_ARG, "o may be q, but not in another layout");
+    if (crosses(q, o) == Shared::kYes) return fail(MS_E_ARG, "o may be q, but not other heads of q");
     if ((st = check_tables(tables, sequences, width))) return st;
     if (sequences != n) return fail(MS_E_SHAPE, "%lld queries for %lld sequences", (long long)n, (long long)sequences);
     if (n > 0 && !lengths) return fail(MS_E_NULL, "lengths is NULL");

@@ -10,10 +10,9 @@ namespace rt {
 
 enum class Shared { kNo, kYes, kUnknown };
 
-// Of one type, with non-negative strides.  Where the dims that vary in both have the same strides this
-// is exact: an element of each lies at one address if the pointers' difference is a sum of k_i stride_i,
-// -(extents of b) < k_i < (extents of a).  Else it is known only where the ranges that they span do not meet
-// or begin together.
+// Of one type, with non-negative strides.  An element of each lies at one address if the pointers'
+// difference is a sum of i stride over a's dims less one over b's; tried from the largest stride down, which
+// leaves few possibilities where strides nest, as those of slices do (kUnknown where it leaves many).
 inline Shared shared(const ms_tensor *a, const ms_tensor *b) {
     if (!a || !b || !a->data || !b->data || numel(a) == 0 || numel(b) == 0) return Shared::kNo;
     const int64_t e = (int64_t)elt_size(a->dtype);
@@ -25,39 +24,51 @@ inline Shared shared(const ms_tensor *a, const ms_tensor *b) {
     };
     if (pa + bytes(a) <= pb || pb + bytes(b) <= pa) return Shared::kNo;
     if (pa == pb) return Shared::kYes;
-    const int64_t apart = (int64_t)(pb - pa);
-    if (a->dtype != b->dtype || a->ndim != b->ndim || apart % e) return Shared::kUnknown;
+    const int64_t difference = (int64_t)(pb - pa);
+    if (a->dtype != b->dtype || difference % e) return Shared::kUnknown;
     struct Dim {
-        int64_t stride, na, nb;   // steps that a, b can take
-    } d[5];
+        int64_t stride, up, down;   // steps that a, b can take
+    } d[10];
     int n = 0;
-    for (int i = 0; i < a->ndim; ++i) {
-        const int64_t na = a->shape[i] - 1, nb = b->shape[i] - 1;
-        if (na > 0 && nb > 0 && a->stride[i] != b->stride[i]) return Shared::kUnknown;
-        const int64_t s = na > 0 ? a->stride[i] : b->stride[i];
-        if ((na > 0 || nb > 0) && s > 0) d[n++] = Dim{s, na, nb};
+    for (const ms_tensor *t : {a, b}) {
+        Dim own[5];
+        int m = 0;
+        for (int i = 0; i < t->ndim; ++i)
+            if (t->shape[i] > 1 && t->stride[i] > 0) own[m++] = Dim{t->stride[i], t->shape[i] - 1, 0};
+        std::sort(own, own + m, [](const Dim &x, const Dim &y) { return x.stride < y.stride; });
+        int last = -1;   // dims without a gap between them are one
+        for (int i = 0; i < m; ++i) {
+            if (last >= 0 && own[i].stride == own[last].stride * (own[last].up + 1)) own[last].up = (own[last].up + 1) * (own[i].up + 1) - 1;
+            else own[++last] = own[i];
+        }
+        for (int i = 0; i <= last; ++i) d[n++] = t == a ? own[i] : Dim{own[i].stride, 0, own[i].up};
     }
     std::sort(d, d + n, [](const Dim &x, const Dim &y) { return x.stride > y.stride; });
-    int64_t most[6] = {0}, least[6] = {0};   // of the sums over the dims from i on
+    // Of the sums over the dims from i on: the largest, the least, whether all between them are sums.
+    int64_t most[11], least[11];
+    bool every[11];
+    most[n] = least[n] = 0;
+    every[n] = true;
     for (int i = n - 1; i >= 0; --i) {
-        most[i] = most[i + 1] + d[i].na * d[i].stride;
-        least[i] = least[i + 1] - d[i].nb * d[i].stride;
+        most[i] = most[i + 1] + d[i].up * d[i].stride;
+        least[i] = least[i + 1] - d[i].down * d[i].stride;
+        every[i] = every[i + 1] && d[i].stride <= most[i + 1] - least[i + 1] + 1;
     }
-    // The differences that are left after i dims: few where strides nest.
     constexpr int kMany = 64;
-    int64_t left[kMany], next[kMany];
+    int64_t left[kMany], next[kMany];   // what is left of the difference after i dims
     int count = 1;
-    left[0] = apart / e;
+    left[0] = difference / e;
     for (int i = 0; i < n; ++i) {
         int m = 0;
         for (int j = 0; j < count; ++j) {
-            const int64_t s = d[i].stride, v = left[j];
-            // least <= v - k s <= most of the other dims
-            int64_t k = std::max(-d[i].nb, (v - most[i + 1]) / s - 1);
-            for (; k <= d[i].na && v - k * s >= least[i + 1]; ++k) {
-                if (v - k * s > most[i + 1]) continue;
+            if (every[i] && left[j] >= least[i] && left[j] <= most[i]) return Shared::kYes;
+            for (int64_t k = std::max(-d[i].down, (left[j] - most[i + 1]) / d[i].stride - 1); k <= d[i].up; ++k) {
+                const int64_t v = left[j] - k * d[i].stride;
+                if (v < least[i + 1]) break;
+                if (v > most[i + 1]) continue;
+                if (every[i + 1]) return Shared::kYes;
                 if (m == kMany) return Shared::kUnknown;
-                next[m++] = v - k * s;
+                next[m++] = v;
             }
         }
         count = m;
@@ -68,11 +79,11 @@ inline Shared shared(const ms_tensor *a, const ms_tensor *b) {
     return Shared::kNo;
 }
 
-// The same elements in the same places.
-inline bool same_places(const ms_tensor *a, const ms_tensor *b) {
-    if (a->data != b->data || !same_shape(a, b)) return false;
-    for (int i = 0; i < a->ndim; ++i)
-        if (a->shape[i] > 1 && a->stride[i] != b->stride[i]) return false;
+// Whether y's elements lie where x's of the same index do.
+inline bool same_places(const ms_tensor *x, const ms_tensor *y) {
+    if (x->data != y->data) return false;
+    for (int i = 0; i < y->ndim; ++i)
+        if (y->shape[i] > 1 && x->stride[i] != y->stride[i]) return false;
     return true;
 }
 

@@ -80,7 +80,8 @@ def test_slices_of_one_projection(lib, dtype):
     assert lib.overlap_shared(ref(q), ref(part(HEADS, HQ))) == YES     # the next rows' heads
     assert lib.overlap_shared(ref(q), ref(part(HEADS * TQ, HQ))) == NO
     assert lib.overlap_shared(ref(part(HQ, 1)), ref(part(HQ + 1, 1))) == NO
-    assert lib.overlap_shared(ref(q), ref(tensor((TQ, HQ, D), dtype, (D, TQ * D, 1), FAKE + 4))) == UNKNOWN
+    assert lib.overlap_shared(ref(q), ref(tensor((TQ, HQ, D), dtype, (D, TQ * D, 1), FAKE + 4))) == YES
+    assert lib.overlap_shared(ref(k), ref(tensor((1, 1, HQ * D), dtype, addr=FAKE))) == NO
     assert lib.overlap_shared(ref(q), ref(tensor((TQ, HQ, D), dtype, (HEADS * D, D, 1), FAKE + 1))) == UNKNOWN
     big = tensor((2 ** 20, 40, 40), dtype)
     assert lib.overlap_shared(ref(big), ref(tensor((1, 1, 1), dtype, addr=FAKE + (2 ** 20 * 1600 - 1) * SIZE[dtype]))) == YES
@@ -160,3 +161,50 @@ def test_head_norm_gradients_that_cross_what_is_read_are_staged(lib, norm):
     assert not staged(OUT + n) and not staged(OUT - n)
     for dx, strides in ((FAKE, other), (FAKE + 2 * D, None)):
         assert staged(dx, strides=strides) == bool(norm)               # a rotation alone does not read x
+
+
+# ------------------------------------------------------------------ results of the forwards
+def heads(T, H, addr, strides=None):
+    return tensor((T, H, D), strides=strides, addr=addr)
+
+
+ALL = (HEADS * D, D, 1)   # rows of queries, keys and values
+ROW = HEADS * D * 2
+CROSSING = [
+    # an output that begins inside what other blocks read
+    ("attention", dict(y=heads(TQ, HQ, FAKE + D * 2))), ("attention", dict(y=heads(TQ, HQ, FAKE + HQ * D * 2), mask=0)),
+    ("attention", dict(y=heads(TQ, HQ, FAKE - HQ * D * 2))),
+    ("attention", dict(x=heads(TQ, HQ, FAKE + (1 << 30)), y=heads(TQ, HQ, FAKE + D * 2))),   # k and v
+    ("attention", dict(x=heads(TQ, HQ, FAKE, ALL), gq=heads(TQ, HK, FAKE + HQ * D * 2, ALL), gk=heads(TQ, HK, FAKE + (HQ + HK) * D * 2, ALL),
+                       y=heads(TQ, HQ, FAKE + 2 * HK * D * 2, ALL))),
+    ("rotary", dict(y=heads(TQ, HQ + HK, FAKE + D * 2), mask=0)), ("rotary", dict(y=heads(TQ, HQ + HK, FAKE + (HQ + HK) * D * 2))),
+    ("rotary", dict(x=heads(TQ, HQ + HK, FAKE, ALL), y=heads(TQ, HQ + HK, FAKE + D * 2, ALL), mask=0)),
+    ("append", dict(x=heads(TQ, HEADS, FAKE), y=heads(TQ, HQ, FAKE + D * 2, ALL))),
+    ("append", dict(x=heads(TQ, HEADS, FAKE), y=heads(TQ, HQ, FAKE + ROW, ALL))), ("append", dict(y=heads(TQ, HQ, FAKE + 4 * D))),
+    ("paged", dict(y=heads(TQ, HQ, FAKE + D * 2))), ("paged", dict(y=heads(TQ, HQ, FAKE - HQ * D * 2))),
+]
+
+
+@pytest.mark.parametrize("kind,over", CROSSING)
+def test_results_that_cross_what_is_read_are_refused(lib, kind, over):
+    c = Call(lib, kind, **over)
+    assert c.forward() == L.MS_E_ARG, lib.ms_last_error()
+    assert not c.h.value and lib.attention_log() == b"" and lib.stub_log() == b""
+
+
+BESIDE = [
+    # slices of one buffer: the results beside what is read
+    ("attention", dict(x=heads(TQ, HQ, FAKE, (2 * HEADS * D, D, 1)), y=heads(TQ, HQ, FAKE + HEADS * D * 2, (2 * HEADS * D, D, 1)), mask=0,
+                       gq=heads(TK, HK, OUT), gk=heads(TK, HK, OUT))),
+    ("attention", dict(y=heads(TQ, HQ, FAKE + (1 << 20)), mask=0)),
+    ("rotary", dict(x=heads(TQ, HQ + HK, FAKE, ALL), y=heads(TQ, HQ + HK, FAKE, ALL), mask=0)),
+    ("append", dict(x=heads(TQ, HEADS, FAKE), y=heads(TQ, HQ, FAKE, ALL))),
+    ("append", dict(x=heads(TQ, HEADS, FAKE, (2 * HEADS * D, D, 1)), y=heads(TQ, HQ, FAKE + HEADS * D * 2, (2 * HEADS * D, D, 1)))),
+    ("paged", dict(y=heads(TQ, HQ, FAKE))), ("paged", dict(y=heads(TQ, HQ, FAKE + TQ * HQ * D * 2))),
+]
+
+
+@pytest.mark.parametrize("kind,over", BESIDE)
+def test_results_beside_what_is_read_are_written(lib, kind, over):
+    c = Call(lib, kind, **over)
+    assert c.forward() == 0, lib.ms_last_error()
