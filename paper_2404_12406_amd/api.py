@@ -675,7 +675,8 @@ def _heads_call(spec, x, W, b, mask, y):
                 kept["positions"], kept["inv_freq"] = spec.positions, spec.inv_freq
             if mask & MASK_INPUT and b is not None:
                 kept["b"] = b
-        return y, "ms_head_norm_rotary_forward", (_packed(x), _packed(W), _packed(b), rot, mask, _packed(y)), kept, None
+        return y, "ms_head_norm_rotary_forward", (_packed(x), _packed(W), _packed(b), rot, mask, _packed(y)), kept, (
+            spec.positions, spec.inv_freq)
     D = x.shape[2]
     if isinstance(spec, Attention):
         if W is None or b is None or W.dim() != 3 or b.dim() != 3:
@@ -701,7 +702,7 @@ def _heads_call(spec, x, W, b, mask, y):
         args = (_packed(x), _packed(W), _packed(b), _index("offsets", off, x), _index("k_offsets", k_off, x, (n + 1,)), n,
                 1 if spec.causal else 0, D ** -0.5 if spec.scale is None and D else spec.scale or 0.0,
                 (buf.data_ptr() or None) if buf is not None else None, mask, _packed(y))
-        return y, "ms_attention_forward", args, kept, None
+        return y, "ms_attention_forward", args, kept, (off, k_off)
     if mask:
         raise ValueError(f"{type(spec).__name__} has no gradients: mask must be 0")
     kp, vp, tab = spec.k_pages, spec.v_pages, spec.tables
@@ -719,14 +720,14 @@ def _heads_call(spec, x, W, b, mask, y):
             y = torch.empty((x.shape[0], spec.q_heads, D), dtype=x.dtype, device=x.device)
         args = (_packed(x), _packed(W), _packed(b), rot, _packed(kp), _packed(vp), *tables, _index("rows", spec.rows, x, (x.shape[0],)),
                 _packed(y))
-        return y, "ms_cache_append", args, None, None
+        return y, "ms_cache_append", args, None, (kp, vp, tab, spec.positions, spec.rows, spec.inv_freq)
     if W is not None or b is not None:
         raise TypeError("PagedAttention takes no W or b")
     if y is None:
         y = torch.empty(x.shape, dtype=x.dtype, device=x.device)
     args = (_packed(x), _packed(kp), _packed(vp), *tables, _index("lengths", spec.lengths, x, (x.shape[0],)),
             D ** -0.5 if spec.scale is None and D else spec.scale or 0.0, _packed(y))
-    return y, "ms_paged_attention_forward", args, None, None
+    return y, "ms_paged_attention_forward", args, None, (kp, vp, tab, spec.lengths)
 
 
 def _block_run(name, args, handle, stream):
