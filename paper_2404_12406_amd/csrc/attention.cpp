@@ -485,6 +485,8 @@ ms_status ms_paged_attention_forward(const ms_tensor *q, const ms_tensor *k_page
     a.page = (int)k_pages->shape[2];
     a.width = (int)width;
     a.scale = scale;
+    // (blocks of 32 query heads of a group are a launch's second dimension)
+    if (Hq / Hk > 32 * 65535) return fail(MS_E_UNSUPPORTED, "more than 32 x 65535 query heads for a head of the cache");
     if (ms::paged_blocks(a) > kMaxBlocks) return fail(MS_E_UNSUPPORTED, "2^24 or more blocks");
     Stands sg;
     const Stand sq = sg.add(q, true), so = sg.add(o, false);

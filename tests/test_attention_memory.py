@@ -208,3 +208,14 @@ BESIDE = [
 def test_results_beside_what_is_read_are_written(lib, kind, over):
     c = Call(lib, kind, **over)
     assert c.forward() == 0, lib.ms_last_error()
+
+
+# ------------------------------------------------------------------ launches
+@pytest.mark.parametrize("group,status", [(65535 * 32, 0), (65535 * 32 + 1, L.MS_E_UNSUPPORTED), (2 ** 23, L.MS_E_UNSUPPORTED)])
+def test_query_heads_past_a_launchs_second_dimension_are_refused(lib, group, status):
+    """Blocks of 32 query heads to a head of the cache are that dimension, up to 65535."""
+    q, o = (tensor((1, group, 8), addr=a) for a in (FAKE, OUT))
+    pages = tensor((9, 1, 8, 8))
+    c = Call(lib, "paged", x=q, y=o, kp=pages, vp=pages, n=1)
+    assert c.forward() == status
+    assert lib.attention_log() == (b"" if status else b"paged;")
