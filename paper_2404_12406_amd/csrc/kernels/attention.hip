@@ -131,7 +131,7 @@ __global__ __launch_bounds__(256 * WG, (FwdShape<T, DC>::OCC / WG)) void fwd_ker
 #pragma unroll
             for (int i = 0; i < NP; ++i) p[n * NP + i] = as_frag<T>(x[n], i);
         }
-        if (masked && any_wild<T, DP, 32 * N>(vt, r0, lane)) wild_product<T, DP, DC, N * NP>(acc, vt, r0, p, lane);
+        if (masked && any_wild<T, DP, 32 * N>(vt, r0, lane)) wild_product<T, DP, DC, N * NP>(acc, vt, r0, p, 0, last - k - r0, lane);
         else add_product<T, DP, DC, N * NP>(acc, vt, r0, p, lane);
     };
     // The keys that all of the block's rows see, in whole steps; then the others, 32 at a time.

@@ -204,7 +204,7 @@ __global__ __launch_bounds__(256 * WG, (DqShape<T, DC>::OCC / WG)) void dq_kerne
             Frag d[NP];
 #pragma unroll
             for (int i = 0; i < NP; ++i) d[i] = as_frag<T>(x, i);
-            if (wild) wild_product<T, DP, DC, NP>(acc, kt, n, d, lane);
+            if (wild) wild_product<T, DP, DC, NP>(acc, kt, n, d, 0, last - k - n, lane);
             else add_product<T, DP, DC, NP>(acc, kt, n, d, lane);
             return;
         }
@@ -371,10 +371,11 @@ __global__ __launch_bounds__(256 * WG, (DkvShape<T, DC, DK, DV>::OCC / WG)) void
         }
         // (an operand: in bf16 rounded, P to 8 bits)
         Frag f[NP];
+        const int lo = a.causal ? key - shift - at - m : 0, hi = s.nb - 1 - at - m;   // rows that see the lane's key
         if constexpr (DV) {
 #pragma unroll
             for (int i = 0; i < NP; ++i) f[i] = as_frag<T>(x, i);
-            if (masked && any_wild<T, DP, 32>(gt, m, lane)) wild_product<T, DP, DC, NP>(dv, gt, m, f, lane);
+            if (masked && any_wild<T, DP, 32>(gt, m, lane)) wild_product<T, DP, DC, NP>(dv, gt, m, f, lo, hi, lane);
             else add_product<T, DP, DC, NP>(dv, gt, m, f, lane);
         }
         if constexpr (DK) {
@@ -382,7 +383,7 @@ __global__ __launch_bounds__(256 * WG, (DkvShape<T, DC, DK, DV>::OCC / WG)) void
             if (sizeof(T) == 4 || wild) {
 #pragma unroll
                 for (int i = 0; i < NP; ++i) f[i] = as_frag<T>(y, i);
-                if (wild) wild_product<T, DP, DC, NP>(dk, qt, m, f, lane);
+                if (wild) wild_product<T, DP, DC, NP>(dk, qt, m, f, lo, hi, lane);
                 else add_product<T, DP, DC, NP>(dk, qt, m, f, lane);
             } else {
                 add_exactly<T, DP, DC>(dk, qt, m, y, lane);

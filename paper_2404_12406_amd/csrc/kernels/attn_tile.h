@@ -316,10 +316,12 @@ __device__ __forceinline__ bool any_wild(const char *tile, int r0, int lane) {
     return __any(bad);
 }
 
-// acc += columns of `tile` times b (N chunks), a row at a time, where a weight of zero
-// takes no part whatever its row holds: for tiles with masked places where any_wild().
+// acc += columns of `tile` times b (N chunks), a row at a time, where rows outside lo..hi, which the
+// lane's column does not see, take no part whatever they hold: for tiles with masked places where any_wild().
+// (By the rows, not by weights of zero: 0 times an infinity that is seen is NaN, as it is in other tiles.)
 template <typename T, int DP, int DC, int N>
-__device__ __forceinline__ void wild_product(floatx16 (&acc)[DC / 32], const char *tile, int r0, const typename Mat<T>::Frag (&b)[N], int lane) {
+__device__ __forceinline__ void wild_product(floatx16 (&acc)[DC / 32], const char *tile, int r0, const typename Mat<T>::Frag (&b)[N], int lo, int hi,
+                                             int lane) {
     typedef Mat<T> M;
     typedef Tile<T, DP> Ti;
     constexpr int PER = 4 / (int)sizeof(T);   // elements of a word
@@ -337,12 +339,13 @@ __device__ __forceinline__ void wild_product(floatx16 (&acc)[DC / 32], const cha
 #pragma unroll
                 for (int j = 0; j < 4; ++j) word = k == c && j == e / PER ? __builtin_bit_cast(u32x4, b[k])[j] : word;
             const float p = __shfl(__uint_as_float(PER == 1 ? word : e & 1 ? word & 0xffff0000u : word << 16), n + 32 * half);
+            const bool seen = row >= lo && row <= hi;
 #pragma unroll
             for (int g = 0; g < 4; ++g) {
                 const int d = 32 * t + 8 * g + 4 * hh;
                 const T *v = reinterpret_cast<const T *>(tile + Ti::at(r0 + row, d / M::V)) + d % M::V;
 #pragma unroll
-                for (int j = 0; j < 4; ++j) acc[t][4 * g + j] = p == 0.f ? acc[t][4 * g + j] : acc[t][4 * g + j] + p * to_f32(v[j]);
+                for (int j = 0; j < 4; ++j) acc[t][4 * g + j] = seen ? acc[t][4 * g + j] + p * to_f32(v[j]) : acc[t][4 * g + j];
             }
         }
     }
