@@ -474,8 +474,9 @@ uint64_t ms_attention_kept_bytes(int64_t rows, int64_t heads, uint32_t mask);
  * With mask 0 kept may be NULL.  q, o: [Tq, Hq, D], k, v: [Tk, Hk, D], 1 <= D <= 256
  * (MS_E_UNSUPPORTED otherwise), any strides (o not overlapping itself, and not q, k or v: MS_E_ARG);
  * rows that are no whole aligned 16-byte vectors are staged.  scale: finite, > 0 (MS_E_ARG otherwise).
- * Sums and statistics are in fp32; in bf16 P is rounded to bf16 as an operand of its products, dS in two
- * operands, the rounded value and what that leaves off.  A gradient's bits do not depend on which
+ * Sums and statistics are in fp32 (the kept log-sum-exp too, so that in the backward a row's P is off by up to 2^-25 ln 2 times
+ * it); in bf16 P is rounded to bf16 as an operand of its products, dS in two
+ * operands, the rounded value and what that leaves off (in one where hidden places of its 32 rows hold an infinity or NaN).  A gradient's bits do not depend on which
  * others are asked for, nor on where it lies: gradients may lie on q, k, v, o or grad_y (not on each other).  Where they do,
  * they are written after the last read, from sums in fp32 in transient workspace.  Backward is ms_layer_backward(); ms_layer_forward() rejects MS_ATTENTION (MS_E_ARG).
  */

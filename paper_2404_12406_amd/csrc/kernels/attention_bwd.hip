@@ -12,8 +12,12 @@
 //
 // Bound: matrix cores, 3 products in dq, 2 in dv alone, 3 in dk alone, 4 in both (in bf16 that with dS twice),
 // and the vector units: 8 operations and an exponential an element of P beside them.  bf16, 8192 rows in 7 sequences,
-// 32 on 8 heads of 128: dq 300 us, 530 TFLOP/s by three products, dv alone 170 to 195, 540 to 620; 16 x 512 rows, 12 heads of
-// 64: dq 39 us, dk and dv 46.  fp32, 1777 rows, 6 on 2 heads of 72: dq 56 us, dk and dv 73, sums of the parts 6 each.
+// 32 on 8 heads of 128: dq 300 us, 530 TFLOP/s by three products, dv alone 170 to 200, 530 to 620; 16 x 512 rows, 12 heads of
+// 64: dq 38 us, dk and dv 46.  fp32, 1777 rows, 6 on 2 heads of 72: dq 55 us, dk and dv 72, sums of the parts 6 each.
+//
+// P is taken from one float a row, whose rounding moves a row of it by up to 2^-25 ln 2 times the log-sum-exp.  The scores'
+// own rounding in 32 bits is some eight times that: 500 rows of 64 with a score of 700 in common are off by 1.2e-4 here as with
+// softmax taken again, and by 1.6e-5 where every product of q and k is exact.
 #include <algorithm>
 
 #include "attn_tile.h"
@@ -115,7 +119,8 @@ template <typename T, int DC> constexpr bool kHold1 = DC * sizeof(T) < 1024;
 template <typename T, int DC> constexpr bool kHold = DC * sizeof(T) < 768;
 
 // What the kernels take besides: delta, which dq_kernel writes, and where they leave sums in fp32 if the
-// other side is divided, or a gradient has to wait until everything is read: [split][rows][heads][DC].
+// other side is divided, or a gradient has to wait until everything is read: [split][rows][heads][DC].  (8192 rows in 7
+// sequences, 32 on 8 heads of 128, bf16, forward and all gradients: 860 us, 960 with dq where o was.)
 struct Parts {
     float *delta;
     int splits;
@@ -199,6 +204,7 @@ __global__ __launch_bounds__(256 * WG, (DqShape<T, DC>::OCC / WG)) void dq_kerne
 #pragma unroll
             for (int i = 0; i < 16; ++i) x[i] = k + n + 8 * (i >> 2) + 4 * (lane >> 5) + (i & 3) > last ? 0.f : x[i];
         }
+        // (there dS is rounded once: rows that see the infinity or NaN are none, the others have a rounding more)
         const bool wild = masked && any_wild<T, DP, 32>(kt, n, lane);
         if (sizeof(T) == 4 || wild) {
             Frag d[NP];

@@ -244,8 +244,8 @@ inline int span_splits(int64_t blocks, int64_t steps, int64_t bytes) {
     return (int)std::max<int64_t>(1, std::min({want, steps / 2, most}));
 }
 
-// Up to 768 blocks, of which a CU holds two, all run at once, and the longest end alone on a CU that they cannot
-// fill.  Where they have `least` steps or more on average, such blocks have eight waves, which take every
+// Up to 768 blocks are one and a half times what the card's 256 CUs hold at once, two each, and the longest end
+// alone on a CU that they cannot fill.  Where they have `least` steps or more on average, such blocks have eight waves, which take every
 // other step each and meet at the end.  (bf16, 8192 rows of one sequence, 8 heads of 128: forward 178 -> 144 us,
 // dv 186 -> 148.  With two to 16 steps the longer start costs more: 64 x 128 rows, 4 heads of 64 forward
 // 10 -> 13 us, 8 x 1024 rows 22 -> 24.  With 1152 blocks dv 312 -> 356 us.)
@@ -273,8 +273,9 @@ struct Full { static constexpr bool value = false; };
 
 template <int N> struct Number { static constexpr int value = N; };
 
-// 2^((s - ref) c).  In bf16 in one operation, on -ref c: where that is large its rounding is the same
-// for a whole row and goes out in the quotient.  In fp32 the difference first, which is exact near ref.
+// 2^((s - ref) c).  In bf16 in one operation, on -ref c, whose rounding is a factor of all weights that are
+// taken with the same ref; those of another ref, and of other waves or blocks, have another, up to 2^-24 |ref c| ln 2 of
+// themselves apart: less than a weight's own 2^-8 to |ref c| of some 2^16.  In fp32 the difference first, which is exact near ref.
 template <typename T>
 __device__ __forceinline__ float power(float s, float ref, float minus, float c) {
     return __builtin_amdgcn_exp2f(sizeof(T) == 2 ? __builtin_fmaf(s, c, minus) : (s - ref) * c);
