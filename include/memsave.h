@@ -439,7 +439,7 @@ typedef struct {
  * layout (MS_E_ARG otherwise, also where it begins elsewhere in x).
  * gamma_q, gamma_k: [D] contiguous or NULL (ones).  Statistics, angles and sums are in 32
  * bits or more.  Backward is ms_layer_backward(); dx may lie on dy or on x, and where it
- * does in other places than theirs it is staged.  ms_layer_forward() rejects
+ * does in other places than theirs it is staged (beyond what ms_account counts).  ms_layer_forward() rejects
  * MS_HEAD_NORM_ROTARY (MS_E_ARG).
  */
 ms_status ms_head_norm_rotary_forward(const ms_tensor *x, const ms_tensor *gamma_q, const ms_tensor *gamma_k,
@@ -478,7 +478,7 @@ uint64_t ms_attention_kept_bytes(int64_t rows, int64_t heads, uint32_t mask);
  * it); in bf16 P is rounded to bf16 as an operand of its products, dS in two
  * operands, the rounded value and what that leaves off (in one where hidden places of its 32 rows hold an infinity or NaN).  A gradient's bits do not depend on which
  * others are asked for, nor on where it lies: gradients may lie on q, k, v, o or grad_y (not on each other).  Where they do,
- * they are written after the last read, from sums in fp32 in transient workspace.  Backward is ms_layer_backward(); ms_layer_forward() rejects MS_ATTENTION (MS_E_ARG).
+ * they are written after the last read, from sums in fp32 in transient workspace (beyond what ms_account counts).  Backward is ms_layer_backward(); ms_layer_forward() rejects MS_ATTENTION (MS_E_ARG).
  */
 ms_status ms_attention_forward(const ms_tensor *q, const ms_tensor *k, const ms_tensor *v, const int32_t *q_offsets,
                                const int32_t *k_offsets, int64_t sequences, int32_t causal, float scale, void *kept,

@@ -117,6 +117,46 @@ def test_a_prepared_call_of_its_own():
         call.backward()
         same([call.y, *grads], [o, *want])
 
+@DTYPES
+def test_in_place_without_allocation(dtype):
+    import ctypes
+    from paper_2404_12406_amd import _lib
+    q, k, v, g = inputs([300, 40, 90], 4, 2, 64, dtype)
+    spec = ms.Attention(starts([300, 40, 90]))
+    _, want = apart(spec, q, k, v, g, 7)
+    _, rec = ms.layer_forward(spec, q, k, v, 7)
+    assert _lib.load().ms_layer_backward_noalloc(rec._h, *(ctypes.byref(api.tensor_desc(t)) for t in (g, q, k, v)), api._stream(q.device)) == 0
+    same((q, k, v), want)
+
+
+@DTYPES
+def test_graph_replays_in_place(dtype):
+    """dq where o was, dk and dv where k and v are copied to: replays with other inputs, eager calls between."""
+    shape = ([300, 40, 90], 4, 2, 64)
+    q, k, v, g = inputs(*shape, dtype)
+    spec = ms.Attention(starts(shape[0]))
+
+    def step():
+        k2, v2 = k.clone(), v.clone()
+        o, rec = ms.layer_forward(spec, q, k2, v2, 7)
+        return ms.layer_backward(rec, g, o, k2, v2)
+
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        step()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=s):
+            outs = step()
+    torch.cuda.synchronize()
+    for i in range(3):
+        for j, t in enumerate((q, k, v, g)):
+            t.copy_(draw(t.shape, dtype, 20 + 10 * i + j))
+        graph.replay()
+        torch.cuda.synchronize()
+        same(outs, apart(spec, q, k, v, g, 7)[1])
+
+
 # ------------------------------------------------------------------ head norms
 @DTYPES
 @pytest.mark.parametrize("norm", [True, False])
